@@ -314,6 +314,143 @@ int grpo_surrogate_noalloc(const float* new_lp, const float* old_lp, const float
                            const int32_t* G, int32_t P, int32_t N, int32_t max_new, const int32_t* keep,
                            double eps_lo, double eps_hi, int32_t mode, double* out, void* stream);
 
+/* ---- rotary positions and a key/value cache in 8 bits ----
+ * For programs that hold a cache of their own: a serving loop, a scorer, an
+ * engine beside the policy's.  Views.  `x` [rows, heads, head_dim] below is
+ * given by its address and the element strides between rows and between heads
+ * (dims are adjacent), so that q, k and v may be parts of one projection's
+ * output; any alignment and strides work, 16-byte ones run faster.  `dtype` is
+ * that of every view of a call: RG_DTYPE_F32 or RG_DTYPE_BF16.  All entry points
+ * only enqueue work on `stream` and allocate nothing (they can be captured into
+ * HIP graphs); they keep no state, so calls on several streams may overlap
+ * where their outputs do not. */
+
+#define RG_ROPE_HALF        0   /* pairs (x[i], x[i + rot_dim/2])  */
+#define RG_ROPE_INTERLEAVED 1   /* pairs (x[2i], x[2i + 1])        */
+
+/* Scaling of the frequencies w_i = theta^(-2i/rot_dim), i < rot_dim/2, for
+ * contexts beyond the trained length (factor = the context's growth). */
+#define RG_ROPE_PLAIN  0   /* w_i                                                                     */
+#define RG_ROPE_LINEAR 1   /* w_i / factor: positions interpolated                                    */
+#define RG_ROPE_BASE   2   /* theta raised to theta * factor^(rot_dim/(rot_dim - 2)): the slowest pair
+                              is interpolated by the factor, the fastest kept                         */
+#define RG_ROPE_BANDS  3   /* w_i (g + (1 - g)/factor), g = (n_i - slow)/(fast - slow) clipped to
+                              [0, 1], n_i = turns of pair i over `length` positions: fast pairs kept,
+                              slow ones interpolated; cos and sin times 0.1 ln(factor) + 1            */
+
+/* cos and sin of positions 0 .. n_pos-1: DEVICE fp32 [n_pos, rot_dim/2], angles
+ * and functions in 64 bits, rounded once.  factor is used by every scaling but
+ * RG_ROPE_PLAIN; length, slow and fast by RG_ROPE_BANDS alone.  RG_EINVAL for
+ * NULL pointers, n_pos < 1, rot_dim odd or < 2 (RG_ROPE_BASE: < 4), theta <= 0,
+ * factor < 1, length <= 0 or slow >= fast where they are used. */
+int rg_rope_table(float* cos_tab, float* sin_tab, int32_t n_pos, int32_t rot_dim, double theta, int32_t scaling,
+                  double factor, double length, double slow, double fast, void* stream);
+
+/* Rotary positions: y = x with the first rot_dim dims of every head turned,
+ * pair (a, b) at position pos[r] to (a c - b s, b c + a s), c and s from the
+ * tables, computed in fp32; the other dims are copied.  inverse != 0 turns back
+ * (s negated), which is the gradient: the y of that call for x = dL/dy is dL/dx.
+ *   pos        DEVICE int32 [rows]; a row whose position lies outside
+ *              [0, n_pos) gets NaN in its turned dims
+ *   cos_tab, sin_tab   DEVICE fp32 [n_pos, rot_dim/2]
+ * y may be x (same address and strides), not overlap it otherwise.  RG_EINVAL
+ * for NULL pointers, negative sizes, an unknown dtype or layout, an odd head_dim
+ * or rot_dim, or rot_dim outside [2, head_dim]. */
+int rg_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head, void* y, int64_t y_row, int64_t y_head,
+            const int32_t* pos, int32_t rows, int32_t heads, int32_t head_dim, const float* cos_tab,
+            const float* sin_tab, int32_t n_pos, int32_t rot_dim, int32_t layout, int32_t inverse, void* stream);
+
+/* A paged cache of e4m3 codes (4 exponent, 3 mantissa bits, largest value 448).
+ * A block is 16 consecutive tokens of one kv head, with one scale for its keys
+ * and one for its values; a value is its code times its block's scale, a power
+ * of two.  A page holds page_tokens / 16 blocks of every kv head.
+ *   k, v              DEVICE [pages, n_kv, page_tokens/16, 16*head_dim] codes,
+ *                     16-byte aligned.  Inside a block token t, dim d is byte
+ *                     (d/16)*256 + t*16 + d%16 of the keys and
+ *                     (t/4)*4*head_dim + d*4 + t%4 of the values.
+ *   k_scale, v_scale  DEVICE fp32 [pages, n_kv, page_tokens/16]
+ * Supported: head_dim 64 or 128, page_tokens 16, 32, 64, .. 1024,
+ * pages * n_kv * page_tokens/16 < 2^31 (otherwise RG_EUNSUPPORTED). */
+typedef struct rg_kv8_cache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t pages;
+  int32_t n_kv, head_dim, page_tokens;
+} rg_kv8_cache;
+
+/* The rows of a call.  Sequence s holds rows seq_off[s] .. seq_off[s+1]-1, the
+ * last ones of its seq_len[s] tokens: the final row is at position
+ * seq_len[s] - 1.  Rows that would fall before position 0 are padding (a
+ * sequence of length 0 in a padded batch); rows from seq_off[n_seqs] on belong
+ * to nobody and are neither read nor written.  Token j of sequence s lies in page
+ * page_tab[row, j / page_tokens], row = tab_row ? tab_row[s] : s.
+ *   page_tab   DEVICE int32 [tab_rows, tab_stride]; tab_stride * page_tokens <= 2^30
+ *   tab_row    DEVICE int32 [n_seqs] or NULL
+ *   seq_off    DEVICE int32 [n_seqs + 1], ascending from 0, or NULL: one row a
+ *              sequence (rows == n_seqs), as in a decode step
+ *   seq_len    DEVICE int32 [n_seqs], with the call's rows counted
+ * Entries that are out of range never lead to an access outside the buffers
+ * given: see the calls for what such rows get. */
+typedef struct rg_kv8_batch {
+  const int32_t* page_tab;
+  int32_t tab_rows, tab_stride;
+  const int32_t* tab_row;
+  const int32_t* seq_off;
+  const int32_t* seq_len;
+  int32_t n_seqs, rows;
+} rg_kv8_batch;
+
+/* Appends the rows' keys and values, keys turned by their positions first
+ * (rot_dim > 0; 0: as they are), and turns the queries on the way (q != NULL)
+ * into q_out, which may be q.
+ *   k, v     views [rows, n_kv, head_dim];  q, q_out  views [rows, n_q, head_dim]
+ * A block's scale is 2^e, e the least in [-64, 119] with 448 * 2^e >= the
+ * largest finite magnitude among its new rows (of keys after turning), or its
+ * old scale where tokens before the new ones stay in it and that is larger;
+ * tokens that stay are requantized where the scale grows, slots behind the last
+ * new token keep what they hold.  Codes round to nearest even; infinities are
+ * stored as 448 with their sign, NaN as code 255 (NaN).  Each page that receives a row
+ * must be one sequence's alone: where two write to one block its contents are
+ * undefined (shared pages are for reading; copy the last, partly filled page of
+ * a shared prefix before its owners append).  Rows whose page is not in the
+ * table or not in [0, pages) are dropped; a key whose position lies outside
+ * [0, n_pos) becomes NaN; padding rows are skipped, q_out included.  RG_EINVAL
+ * for NULL pointers, bad sizes, n_q not a multiple of n_kv, or rot_dim and layout
+ * as in rg_rope. */
+int rg_kv8_append(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* k, int64_t k_row,
+                  int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const void* q, int64_t q_row,
+                  int64_t q_head, void* q_out, int64_t qo_row, int64_t qo_head, int32_t n_q, const float* cos_tab,
+                  const float* sin_tab, int32_t n_pos, int32_t rot_dim, int32_t layout, void* stream);
+
+/* Bytes of scratch that rg_kv8_attention needs for these sizes (0: none);
+ * has_off: whether seq_off is given.  Negative (RG_E*) for bad sizes. */
+int64_t rg_kv8_attention_scratch(int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rows, int32_t n_seqs,
+                                 int32_t has_off, int32_t max_len);
+
+/* Causal attention of the rows over their sequences' tokens in the cache (the
+ * rows' own included: append first).  Query head h of a row at position p reads
+ * kv head h / (n_q/n_kv):
+ *   out = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale * q.k_j),  j = 0 .. p.
+ *   q        view [rows, n_q, head_dim], turned already
+ *   out      DEVICE [rows, n_q, head_dim] dense, in dtype, 16-byte aligned
+ *   scale    > 0, finite (usually 1/sqrt(head_dim))
+ *   max_len  bound on seq_len[], >= 1: it sizes the launch; longer sequences
+ *            are still computed whole
+ *   scratch  DEVICE, 16-byte aligned, of rg_kv8_attention_scratch() bytes, that
+ *            nothing else uses until the call's kernels have run (NULL when 0)
+ * Scores, softmax and sums are fp32, and so are fp32 queries and their
+ * probabilities; bf16 queries are multiplied as they are, their probabilities as
+ * 17 bits (single rows) or bf16 (runs of four rows a sequence or more).  Padding rows get zeros; a row that needs a page
+ * outside the table or the pool gets NaN.  Tokens past a row's position do not
+ * touch it, whatever their codes.  RG_EINVAL for NULL pointers, bad sizes, n_q
+ * not a multiple of n_kv, or too little scratch; RG_EUNSUPPORTED for more than
+ * 128 query heads per kv head. */
+int rg_kv8_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* q,
+                     int64_t q_row, int64_t q_head, int32_t n_q, void* out, float scale, int32_t max_len,
+                     void* scratch, int64_t scratch_bytes, void* stream);
+
 /* ---- test and measurement hooks ---- */
 
 

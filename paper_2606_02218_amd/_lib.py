@@ -22,7 +22,8 @@ EXPORTS = ["rg_last_error", "rg_policy_create", "rg_policy_destroy", "rg_policy_
            "group_advantage", "rg_philox_blocks", "rg_gumbel_bits", "rg_hbm_probe", "rg_step_history", "rg_kernel_times",
            "sagc_init", "sagc_group_stats", "sagc_step", "sagc_beta_draw", "group_filter",
            "recompute_logprobs", "grpo_surrogate", "rg_decode_attention_chunks", "rg_phase_times",
-           "grpo_surrogate_noalloc", "grpo_surrogate_scratch", "rg_gumbel_noise"]
+           "grpo_surrogate_noalloc", "grpo_surrogate_scratch", "rg_gumbel_noise",
+           "rg_rope_table", "rg_rope", "rg_kv8_append", "rg_kv8_attention_scratch", "rg_kv8_attention"]
 SAGC_MAX_SIZES = 8
 
 

@@ -366,3 +366,78 @@ constexpr int SURROGATE_NOALLOC_MAX_SEQS = 65536;
 // Device address of that array on the current device (looked up with
 // hipGetSymbolAddress on the first call per device, then cached).
 hipError_t surrogate_static_scratch(SurrogateRec** out);
+
+// ---- rotary positions and the 8-bit key/value cache (k_rope.hip, k_kv8.hip)
+// cos and sin of every position and pair, fp32 [n_pos][pairs].
+struct RopeTable {
+  const float* cos; const float* sin;
+  int n_pos, pairs;
+  int layout;   // 0: pairs (i, i + pairs); 1: pairs (2i, 2i + 1)
+};
+// Frequencies of a table; see rg_rope_table in rollout.h.
+struct RopeFreqs {
+  int pairs, mode;
+  double theta, factor, length, slow, fast;
+};
+hipError_t launch_rope_table(float* cos, float* sin, int n_pos, const RopeFreqs& f, hipStream_t st);
+
+// x [rows][heads][hd] with element strides between rows and heads; dtype as elsewhere.
+struct HeadView {
+  const void* p;
+  int64_t row, head;
+};
+struct HeadOut {
+  void* p;
+  int64_t row, head;
+};
+hipError_t launch_rope(int dtype, HeadView x, HeadOut y, const int32_t* pos, int rows, int heads, int hd,
+                       const RopeTable& t, bool inverse, hipStream_t st);
+
+// One layer's 8-bit pool.  A block is 16 consecutive tokens of one kv head with
+// one key and one value scale; page p holds blocks ((p * n_kv + h) << sub_shift)
+// + j.  Byte of token t, dim d in a block of 16 * hd bytes: keys
+// (d / 16) * 256 + t * 16 + d % 16, values (t / 4) * 4 * hd + d * 4 + t % 4.  A
+// wave's 16-byte loads of a block are then linear, and each lane's 16 bytes are
+// MFMA operands after conversion: 16 dims of a token, or 4 tokens of 4 dims.
+struct Kv8Pool {
+  uint8_t* k; uint8_t* v;
+  float* k_scale; float* v_scale;
+  int pages, n_kv, hd, sub_shift;
+};
+// Rows of a ragged batch: sequence s holds rows seq_off[s] .. seq_off[s + 1] - 1
+// (NULL: row s), the last ones of its seq_len[s] + len_add tokens, and reads page
+// table row tab_row[s] (NULL: s) of tab_rows.  d_rows (or NULL) bounds the rows of
+// a batch without offsets on the device.
+struct Kv8Rows {
+  const int32_t* tab; int tab_rows, tab_stride;
+  const int32_t* tab_row; const int32_t* seq_off; const int32_t* seq_len;
+  int len_add, n_seqs, rows;
+  const int* d_rows;
+};
+// Appends the rows' keys (rotated by t; t.pairs == 0: as they are) and values;
+// q (p NULL: none) is rotated to q_out.
+hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, HeadView k, HeadView v, HeadView q,
+                             HeadOut q_out, int n_q, const RopeTable& t, hipStream_t st);
+
+// How an attention over an 8-bit cache is cut: by rows or by tiles of rows that
+// share each staged block, the context into n_split chunks of `chunk` tokens.
+struct Kv8Plan {
+  bool tiles;
+  int n_split, chunk;
+};
+Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_len, int max_split);
+struct Kv8Attn {
+  Kv8Pool c;
+  Kv8Rows b;
+  HeadView q;       // fp32 or bf16 by dtype
+  void* out;        // [rows][n_q][hd] in dtype, or (planes) bf16 hi and lo planes
+  int64_t plane;
+  int n_q;
+  float scale;      // of the scores
+  Kv8Plan plan;
+  float* part;      // n_split > 1: [rows][n_split][n_q][hd] then [rows][n_split][n_q][2]
+};
+inline int64_t kv8_part_floats(int64_t rows, const Kv8Plan& p, int n_q, int hd) {
+  return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
+}
+hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStream_t st);
