@@ -172,6 +172,23 @@ int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits*
                      rg_policy** out);
 void rg_policy_destroy(rg_policy* pol);   /* NULL is a no-op */
 
+/* What a policy's KV pool holds */
+#define RG_KV_MODEL 0   /* keys and values in the config dtype                              */
+#define RG_KV_E4M3  1   /* in 8 bits: e4m3 codes with a power-of-two scale per 16 tokens and
+                           kv head, as rg_kv8_append stores them                            */
+
+/* rg_policy_create with a choice of the KV pool's type (RG_KV_MODEL: the same).
+ * RG_KV_E4M3 is for bf16 models: the pool takes half the bytes and decode
+ * attention reads half; a key or value is then good to 2^-4 of itself in place of
+ * 2^-9, in rollout_group and recompute_logprobs alike, and a token's stored form
+ * may be rounded once more as its block of 16 fills (where a later token raises
+ * the block's scale and pushes it among the subnormal codes).  The two calls
+ * then agree up to that: recompute_logprobs stores a completion's rows at once.
+ * RG_FLAG_GROUP_PREFIX has no effect.  Errors as rg_policy_create;
+ * RG_EUNSUPPORTED for another kv_type or for an fp32 model. */
+int rg_policy_create_kv(const rg_config* cfg, const rg_weights* w, const rg_limits* limits, int32_t kv_type,
+                        rg_policy** out);
+
 /* Bytes of device memory the policy holds (weights + workspace + KV pool). */
 int64_t rg_policy_device_bytes(const rg_policy* pol);
 

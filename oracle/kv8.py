@@ -125,3 +125,55 @@ def attend(q, k, v, pos, scale):
             out[r, h], mass[r, h] = w @ vv, w @ np.abs(vv)
             reach[r, h] = (np.abs(kk) @ np.abs(q[r, h])).max()
     return out, mass, reach
+
+
+class Kv8Model:
+    """The oracle decoder with its keys and values in 8 bits.  ``jitter``: relative noise on keys and values before they
+    are stored, to see what a computation in fewer bits may do to the codes."""
+
+    def __new__(cls, shape, weights, jitter: float = 0.0, seed: int = 0):
+        from .model import OracleModel
+
+        class Model(OracleModel):
+            def new_cache(self):
+                s = self.s
+                return [{"k": Kv8Sequence(s.n_kv_heads, s.head_dim), "v": Kv8Sequence(s.n_kv_heads, s.head_dim)}
+                        for _ in range(s.n_layers)]
+
+            @staticmethod
+            def copy_cache(cache):
+                out = []
+                for c in cache:
+                    d = {}
+                    for n, q in c.items():
+                        d[n] = Kv8Sequence(0, 0)
+                        d[n].codes, d[n].scale = q.codes.copy(), q.scale.copy()
+                    out.append(d)
+                return out
+
+            def noisy(self, a):
+                return a * (1.0 + jitter * rng.standard_normal(a.shape)) if jitter else a
+
+            def forward(self, tokens, positions, cache):
+                s = self.s
+                tokens, positions = np.asarray(tokens, np.int64), np.asarray(positions, np.int64)
+                T = len(tokens)
+                x = np.asarray(self.embed[tokens], np.float64)
+                for lw, c in zip(self.layers, cache):
+                    h = self.rmsnorm(x, lw["attn_norm"])
+                    q = self.rope(self.linear(h, lw["wq"]).reshape(T, s.n_q_heads, s.head_dim), positions)
+                    k = self.rope(self.linear(h, lw["wk"]).reshape(T, s.n_kv_heads, s.head_dim), positions)
+                    v = self.linear(h, lw["wv"]).reshape(T, s.n_kv_heads, s.head_dim)
+                    c["k"].append(self.noisy(k))
+                    c["v"].append(self.noisy(v))
+                    o = self.attention(q, c["k"].values(), c["v"].values(), positions, np.arange(len(c["k"].codes)))
+                    x = x + self.linear(o.reshape(T, s.q_dim), lw["wo"])
+                    h2 = self.rmsnorm(x, lw["ffn_norm"])
+                    x = x + self.linear(self.silu(self.linear(h2, lw["w_gate"])) * self.linear(h2, lw["w_up"]), lw["w_down"])
+                return self.linear(self.rmsnorm(x, self.final_norm), self.lm_head)
+
+            def decode_batch(self, tokens, positions, caches):
+                return np.concatenate([self.forward([t], [p], c) for t, p, c in zip(tokens, positions, caches)])
+
+        rng = np.random.default_rng(seed)
+        return Model(shape, weights)

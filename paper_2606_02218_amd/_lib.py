@@ -18,7 +18,7 @@ RG_FLAG_NO_PREFIX_SHARING, RG_FLAG_PROFILE, RG_FLAG_GROUP_PREFIX, RG_FLAG_NO_ROW
 KERNEL_KINDS = ["embed", "rmsnorm", "gemm_qkv", "qkv_rope", "attn", "attn_merge", "gemm_o", "gemm_gu", "swiglu",
                 "gemm_down", "residual", "gemm_lm", "sample", "compact", "setup", "logprob"]
 
-EXPORTS = ["rg_last_error", "rg_policy_create", "rg_policy_destroy", "rg_policy_device_bytes", "rollout_group",
+EXPORTS = ["rg_last_error", "rg_policy_create", "rg_policy_create_kv", "rg_policy_destroy", "rg_policy_device_bytes", "rollout_group",
            "group_advantage", "rg_philox_blocks", "rg_gumbel_bits", "rg_hbm_probe", "rg_step_history", "rg_kernel_times",
            "sagc_init", "sagc_group_stats", "sagc_step", "sagc_beta_draw", "group_filter",
            "recompute_logprobs", "grpo_surrogate", "rg_decode_attention_chunks", "rg_phase_times",
@@ -110,6 +110,8 @@ def load_library():
     lib.rg_last_error.restype = C.c_char_p
     lib.rg_policy_create.argtypes = [C.POINTER(rg_config), C.POINTER(rg_weights), C.POINTER(rg_limits),
                                      C.POINTER(C.c_void_p)]
+    lib.rg_policy_create_kv.argtypes = [C.POINTER(rg_config), C.POINTER(rg_weights), C.POINTER(rg_limits), C.c_int32,
+                                        C.POINTER(C.c_void_p)]
     lib.rg_policy_destroy.argtypes = [C.c_void_p]
     lib.rg_policy_destroy.restype = None
     lib.rg_policy_device_bytes.argtypes = [C.c_void_p]
@@ -197,13 +199,20 @@ def _gpu(**tensors):
             raise TypeError(f"{name} must be in GPU memory, got device {t.device}")
 
 
+KV_TYPES = {None: 0, "e4m3": 1}
+
+
 class Policy:
-    """A decoder loaded into librollout (the library copies the weights)."""
+    """A decoder loaded into librollout (the library copies the weights).
+    ``kv_dtype="e4m3"`` keeps its keys and values in 8 bits (bf16 models;
+    RG_KV_E4M3 in rollout.h), None in the model's own type."""
 
     def __init__(self, shape, weights, max_seqs: int, max_prompts: int, max_prompt_tokens: int, max_context: int,
-                 kv_pool_pages: int = 0, device: str = "cuda"):
+                 kv_pool_pages: int = 0, device: str = "cuda", kv_dtype: Optional[str] = None):
         import torch
         lib = load_library()
+        if kv_dtype not in KV_TYPES:
+            raise ValueError(f"kv_dtype must be one of {list(KV_TYPES)}")
         self.shape = shape
         self.device = torch.device(device)
         dt = torch.bfloat16 if shape.dtype == "bf16" else torch.float32
@@ -228,7 +237,7 @@ class Policy:
         lim = rg_limits(max_seqs, max_prompts, max_prompt_tokens, max_context, kv_pool_pages)
         h = C.c_void_p()
         torch.cuda.synchronize()
-        _check(lib.rg_policy_create(C.byref(cfg), C.byref(w), C.byref(lim), C.byref(h)))
+        _check(lib.rg_policy_create_kv(C.byref(cfg), C.byref(w), C.byref(lim), KV_TYPES[kv_dtype], C.byref(h)))
         torch.cuda.synchronize()
         del keep
         self._h = h

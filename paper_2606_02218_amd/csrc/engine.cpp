@@ -92,6 +92,11 @@ struct rg_policy {
 
   void* kv_pool = nullptr;
   int64_t pool_pages = 0;
+  bool kv8 = false;            // keys and values in 8 bits: layer l's pool is l * layer_blocks blocks behind kv8_pool
+  Kv8Pool kv8_pool{};
+  int64_t layer_blocks = 0;
+  float* qkv_buf = nullptr;    // kv8: [m_act][qkv_n] products
+  int32_t *run_off = nullptr, *run_len = nullptr;   // kv8: the rows of a recompute chunk by sequence
 
   float* x = nullptr;
   void* abuf = nullptr;   // activation operand (ping)
@@ -291,15 +296,58 @@ struct RowTiles {
   int tiles_ub;         // bound on it, sizes the grid
 };
 
+// The rows of a launch as a batch of the 8-bit cache: single rows (seq_off NULL;
+// their table rows and positions are the policy's row_tab and row_pos) or runs.
+Kv8Rows kv8_steps(const rg_policy* pol, const int* d_rows, int rows_ub) {
+  return Kv8Rows{pol->page_tab, pol->lim.max_seqs + pol->lim.max_prompts, pol->max_pages, pol->row_tab, nullptr,
+                 pol->row_pos, 1, rows_ub, rows_ub, d_rows};
+}
+Kv8Rows kv8_runs(const rg_policy* pol, int tab0, const int32_t* off, const int32_t* len, int n_seqs, int rows) {
+  return Kv8Rows{pol->page_tab + (int64_t)tab0 * pol->max_pages, n_seqs, pol->max_pages, nullptr, off, len, 0, n_seqs,
+                 rows, nullptr};
+}
+
+// RoPE, append and attention of layer l over an 8-bit cache: qkv_buf -> abuf2.
+int kv8_layer(rg_policy* pol, hipStream_t st, int l, const Kv8Rows& batch, int ctx_max, bool tiles) {
+  const int64_t skip = l * pol->layer_blocks;
+  Kv8Attn at{};
+  at.c = pol->kv8_pool;
+  at.c.k += skip * 16 * pol->hd;
+  at.c.v += skip * 16 * pol->hd;
+  at.c.k_scale += skip;
+  at.c.v_scale += skip;
+  at.b = batch;
+  const float* x = pol->qkv_buf;
+  const int64_t ld = pol->qkv_n, hd = pol->hd, qld = pol->q_dim;
+  LAUNCH_TIMED(RG_K_QKV_ROPE,
+               launch_kv8_append(RG_DTYPE_F32, at.c, batch, HeadView{x + pol->q_dim, ld, hd},
+                                 HeadView{x + pol->q_dim + pol->kv_dim, ld, hd}, HeadView{x, ld, hd},
+                                 HeadOut{pol->qbuf, qld, hd}, pol->nq,
+                                 RopeTable{pol->rope_cos, pol->rope_sin, pol->lim.max_context, pol->hd / 2, 0}, st));
+  at.q = HeadView{pol->qbuf, qld, hd};
+  at.out = pol->abuf2;
+  at.plane = pol->a2_plane;
+  at.n_q = pol->nq;
+  at.scale = 1.0f / std::sqrt((float)pol->hd);
+  at.part_o = pol->att_o;
+  at.part_ml = pol->att_ml;
+  at.plan = kv8_plan(batch.rows, batch.n_seqs, tiles, pol->nq, pol->nkv, ctx_max,
+                     (int)std::max<int64_t>(1, std::min<int64_t>(pol->att_rowchunks / batch.rows, INT32_MAX)));
+  LAUNCH_TIMED(RG_K_ATTN, launch_kv8_attention(RG_DTYPE_F32, true, at, st));
+  if (at.plan.n_split > 1) LAUNCH_TIMED(RG_K_ATTN_MERGE, launch_kv8_merge(RG_DTYPE_F32, true, at, st));
+  return RG_OK;
+}
+
 // The decoder blocks over `rows_ub` rows (actual count at *d_rows), whose
 // row_tab / row_pos / row_beg are set and whose first attention norm is in
 // pol->abuf; ctx_max bounds every row's context length.  pre != NULL runs the
 // prefix pass (row_beg then holds each row's prefix length).  On return
 // pol->abuf holds the final norm's operand x * gain of every row, with pol->ssq_n partial sums of squares behind it
 // (final_norm_rows), or x the
-// residual stream after the last block.
+// residual stream after the last block.  An 8-bit cache takes prefill-style rows
+// as `runs` (appended whole; attended to by tiles where `tiles` is given too).
 int run_layers(rg_policy* pol, hipStream_t st, const int* d_rows, int rows_ub, int ctx_max, bool final_norm_rows,
-               const PrefixPass* pre, const RowTiles* tiles = nullptr) {
+               const PrefixPass* pre, const RowTiles* tiles = nullptr, const Kv8Rows* runs = nullptr) {
   if (rows_ub <= 0) return RG_OK;
   const int tab_stride = pol->max_pages;
   const int n_chunks = att_row_chunks(rows_ub, pol->nkv, ctx_max);
@@ -314,12 +362,13 @@ int run_layers(rg_policy* pol, hipStream_t st, const int* d_rows, int rows_ub, i
     plan.pre_slots = (int)ceil_div(pre->max_pref, plan.pre_chunk);
     plan.n_slots = plan.pre_slots + n_chunks;
   }
-  if (!tiles && (int64_t)rows_ub * plan.n_slots > pol->att_rowchunks)
+  if (!tiles && !pol->kv8 && (int64_t)rows_ub * plan.n_slots > pol->att_rowchunks)
     return fail(RG_ENOMEM, "attention workspace too small");
   GemmEpi qkv{};
   qkv.mode = GEMM_EPI_QKV;
   qkv.q_out = pol->qbuf; qkv.kv_pool = pol->kv_pool; qkv.geom = pol->geom;
   qkv.page_tab = pol->page_tab; qkv.tab_stride = tab_stride; qkv.row_tab = pol->row_tab; qkv.row_pos = pol->row_pos;
+  if (pol->kv8) { qkv.mode = GEMM_EPI_STORE; qkv.C = pol->qkv_buf; qkv.ldc = pol->qkv_n; }
   qkv.rope_cos = pol->rope_cos; qkv.rope_sin = pol->rope_sin; qkv.n_q = pol->nq; qkv.n_kv = pol->nkv; qkv.hd = pol->hd;
   GemmEpi resid{};
   resid.mode = GEMM_EPI_RESIDUAL; resid.x = pol->x; resid.ldx = pol->d;
@@ -334,7 +383,9 @@ int run_layers(rg_policy* pol, hipStream_t st, const int* d_rows, int rows_ub, i
     if ((rc = gemm(pol, st, RG_K_GEMM_QKV, pol->abuf, pol->a_plane, pol->d, pol->w_qkv[l], pol->qkv_n, d_rows, rows_ub,
                    qkv, &ssq_n)))
       return rc;
-    if (tiles) {
+    if (pol->kv8) {
+      if ((rc = kv8_layer(pol, st, l, runs ? *runs : kv8_steps(pol, d_rows, rows_ub), ctx_max, runs && tiles))) return rc;
+    } else if (tiles) {
       LAUNCH_TIMED(RG_K_ATTN, launch_attention_tile(pol->qbuf, pol->nq, pol->nkv, pol->hd, pol->kv_pool, pol->geom, l,
                                                     pol->page_tab, tab_stride, pol->row_tab, pol->row_pos,
                                                     pol->tile_r0, pol->tile_nr, tiles->d_tiles, tiles->tiles_ub,
@@ -517,6 +568,7 @@ int stage_groups(rg_policy* pol, hipStream_t st, const GroupRun& gr, const int32
 // the row-tile attention: bf16 models, at most 8 query heads per kv head and
 // contexts within a tile's page list.
 bool att_tiles_apply(const rg_policy* pol, int64_t ctx_max) {
+  if (pol->kv8) return true;   // these tiles keep no page list
   return pol->dtype == RG_DTYPE_BF16 && pol->nq / pol->nkv <= 8 && ctx_max <= 16384;
 }
 
@@ -548,10 +600,12 @@ int prefill_and_fork(rg_policy* pol, hipStream_t st, const GroupRun& gr, const i
   const int tile_rows = att_tile_rows(pol->nq, pol->nkv);
   const bool use_tiles = row_tiles && att_tiles_apply(pol, gr.max_plen);
   RowTiles rt{d_tiles, (int)ceil_div(gr.T_pre, tile_rows) + P};
-  if (use_tiles)
+  if (use_tiles && !pol->kv8)
     LAUNCH(RG_K_SETUP, launch_row_tiles(pol->prompt_off, P, 0, gr.T_pre, tile_rows, d_pre, pol->tile_r0, pol->tile_nr,
                                         d_tiles, st));
-  int rc = run_layers(pol, st, d_pre, gr.T_pre, gr.max_plen, false, nullptr, use_tiles ? &rt : nullptr);
+  const Kv8Rows runs = kv8_runs(pol, N, pol->prompt_off, pol->plen, P, gr.T_pre);
+  int rc = run_layers(pol, st, d_pre, gr.T_pre, gr.max_plen, false, nullptr, use_tiles ? &rt : nullptr,
+                      pol->kv8 ? &runs : nullptr);
   if (rc) return rc;
   if ((rc = run_head(pol, st, pol->state + 6, P, pol->last_rows))) return rc;
 
@@ -568,8 +622,12 @@ int prefill_and_fork(rg_policy* pol, hipStream_t st, const GroupRun& gr, const i
     const int need = share ? (prompt_len[p] % pol->page_tok ? 1 : 0) : n_pref;
     max_pairs += need * G[p];
   }
-  LAUNCH(RG_K_SETUP, launch_page_copy(pol->dtype, pol->kv_pool, pol->geom, pol->copy_pairs, max_pairs,
-                                      pol->state, st));
+  if (pol->kv8)
+    LAUNCH(RG_K_SETUP, launch_kv8_page_copy(pol->kv8_pool, pol->L, pol->layer_blocks, pol->copy_pairs, max_pairs,
+                                            pol->state, st));
+  else
+    LAUNCH(RG_K_SETUP, launch_page_copy(pol->dtype, pol->kv_pool, pol->geom, pol->copy_pairs, max_pairs,
+                                        pol->state, st));
   return RG_OK;
 }
 
@@ -614,6 +672,11 @@ extern "C" {
 const char* rg_last_error(void) { return g_err.c_str(); }
 
 int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits* limits, rg_policy** out) {
+  return rg_policy_create_kv(cfg, w, limits, RG_KV_MODEL, out);
+}
+
+int rg_policy_create_kv(const rg_config* cfg, const rg_weights* w, const rg_limits* limits, int32_t kv_type,
+                        rg_policy** out) {
   if (!cfg || !w || !limits || !out) return fail(RG_EINVAL, "rg_policy_create: NULL argument");
   *out = nullptr;
   const rg_config c = *cfg;
@@ -629,6 +692,9 @@ int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits*
       c.d_model % 64 || (c.n_q_heads * c.head_dim) % 64 || c.ffn_dim % 64 || c.vocab % 16)
     return fail(RG_EUNSUPPORTED, "unsupported shape: need head_dim%8==0, head_dim<=256, n_q/n_kv integer <= 8, "
                                  "d_model, n_q*head_dim, ffn_dim multiples of 64, vocab multiple of 16");
+  if (kv_type != RG_KV_MODEL && kv_type != RG_KV_E4M3) return fail(RG_EUNSUPPORTED, "unsupported kv_type");
+  if (kv_type == RG_KV_E4M3 && c.dtype != RG_DTYPE_BF16)
+    return fail(RG_EUNSUPPORTED, "unsupported kv_type: an 8-bit cache needs a bf16 model");
   const rg_limits lim = *limits;
   if (lim.max_seqs < 1 || lim.max_prompts < 1 || lim.max_prompt_tokens < 1 || lim.max_context < 2 ||
       lim.kv_pool_pages < 0)
@@ -643,6 +709,7 @@ int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits*
   pol->lim = lim;
   pol->dtype = c.dtype;
   pol->eb = c.dtype == RG_DTYPE_BF16 ? 2 : 4;
+  pol->kv8 = kv_type == RG_KV_E4M3;
   pol->d = c.d_model; pol->V = c.vocab; pol->L = c.n_layers; pol->F = c.ffn_dim; pol->hd = c.head_dim;
   pol->nq = c.n_q_heads; pol->nkv = c.n_kv_heads;
   pol->q_dim = c.n_q_heads * c.head_dim;
@@ -671,7 +738,8 @@ int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits*
     float *ga, *gf;
     // [wq; wk; wv] with each head's rows reordered in 16-row tiles as dims
     // (0-15, hd/2..hd/2+15, 16-31, hd/2+16.., ...): a rotated pair (d, d + hd/2)
-    // then sits in two adjacent 16-column tiles of the product
+    // then sits in two adjacent 16-column tiles of the product (as they are for
+    // an 8-bit cache, which turns the stored product)
     if ((rc = pol->alloc(&qkv, (size_t)pol->qkv_n * d * eb))) return bail(rc);
     if (!w->wq[l] || !w->wk[l] || !w->wv[l]) return bail(fail(RG_EINVAL, "weights: NULL wq/wk/wv"));
     {
@@ -682,7 +750,7 @@ int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits*
       size_t base = 0;
       for (int part = 0; part < 3; ++part) {
         for (int t = 0; t < hd / 16; ++t) {   // packed tile t of every head
-          const int d0 = (t & 1) ? half + (t >> 1) * 16 : (t >> 1) * 16;
+          const int d0 = pol->kv8 ? 16 * t : (t & 1) ? half + (t >> 1) * 16 : (t >> 1) * 16;
           HIPTRY(hipMemcpy2D((char*)qkv + (base + (size_t)t * 16) * row, (size_t)hd * row,
                              (const char*)src[part] + (size_t)d0 * row, (size_t)hd * row, 16 * row, heads[part],
                              hipMemcpyDeviceToDevice));
@@ -738,7 +806,19 @@ int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits*
   if (pol->pool_pages > INT32_MAX) return bail(fail(RG_ENOMEM, "KV pool exceeds 2^31 pages"));
   g.page_stride = g.slab_elems;                      // layer-major pool
   g.layer_stride = g.slab_elems * pol->pool_pages;
-  if ((rc = pol->alloc(&pol->kv_pool, (size_t)pol->pool_pages * g.slab_elems * pol->L * eb))) return bail(rc);
+  if (pol->kv8) {
+    pol->layer_blocks = pol->pool_pages * pol->nkv;
+    if (pol->layer_blocks > INT32_MAX) return bail(fail(RG_ENOMEM, "KV pool exceeds 2^31 blocks"));
+    if ((int64_t)pol->max_pages * pol->page_tok > (1 << 30)) return bail(fail(RG_ENOMEM, "max_context exceeds 2^30"));
+    const size_t blocks = (size_t)pol->layer_blocks * pol->L;
+    void *k = nullptr, *v = nullptr, *ks = nullptr, *vs = nullptr;
+    if ((rc = pol->alloc(&k, blocks * 16 * pol->hd)) || (rc = pol->alloc(&v, blocks * 16 * pol->hd)) ||
+        (rc = pol->alloc(&ks, blocks * 4)) || (rc = pol->alloc(&vs, blocks * 4)))
+      return bail(rc);
+    pol->kv8_pool = Kv8Pool{(uint8_t*)k, (uint8_t*)v, (float*)ks, (float*)vs, (int)pol->pool_pages, pol->nkv, pol->hd, 0};
+  } else if ((rc = pol->alloc(&pol->kv_pool, (size_t)pol->pool_pages * g.slab_elems * pol->L * eb))) {
+    return bail(rc);
+  }
 
   // ---- workspace
   const int64_t S = lim.max_seqs, P = lim.max_prompts;
@@ -776,7 +856,7 @@ int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits*
          2 * std::min<int64_t>(M, 2048) + ATT_ITEMS_TARGET});
     pol->a_plane = pol->dtype == RG_DTYPE_BF16 ? M * d + RG_PLANE_PAD : 0;
     pol->a2_plane = pol->dtype == RG_DTYPE_BF16 ? M * kmax + RG_PLANE_PAD : 0;
-    return std::vector<Piece>{
+    std::vector<Piece> ps{
         {(void**)&pol->x, (size_t)(M * d * 4)},
         {&pol->abuf, (size_t)(M * d * 4 + 2 * RG_PLANE_PAD)},   // fp32, or two bf16 planes
         {&pol->abuf2, (size_t)(M * kmax * 4 + 2 * RG_PLANE_PAD)},
@@ -818,6 +898,12 @@ int rg_policy_create(const rg_config* cfg, const rg_weights* w, const rg_limits*
         {(void**)&pol->hist_groups, (size_t)(pol->hist_cap * 4)},
         {(void**)&pol->hist_ctx, (size_t)(pol->hist_cap * 8)},
     };
+    if (pol->kv8) {
+      ps.push_back({(void**)&pol->qkv_buf, (size_t)(M * pol->qkv_n * 4)});
+      ps.push_back({(void**)&pol->run_off, (size_t)((S + 1) * 4)});
+      ps.push_back({(void**)&pol->run_len, (size_t)(S * 4)});
+    }
+    return ps;
   };
   auto bytes_of = [](const std::vector<Piece>& ps) {
     size_t total = 0;
@@ -931,7 +1017,7 @@ int rollout_group(rg_policy* pol, const int32_t* prompts, const int32_t* prompt_
     pp.max_pref = std::max(pp.max_pref, prompt_len[p] / pol->page_tok * pol->page_tok);
   }
   const PrefixPass* pre =
-      pol->dtype == RG_DTYPE_BF16 && (o.flags & RG_FLAG_GROUP_PREFIX) && pp.max_pref > 0 ? &pp : nullptr;
+      pol->dtype == RG_DTYPE_BF16 && !pol->kv8 && (o.flags & RG_FLAG_GROUP_PREFIX) && pp.max_pref > 0 ? &pp : nullptr;
 
   auto snapshot = [&](int t) -> int {
     // the retirement kernel has written the step's state to its ring slot
@@ -1073,9 +1159,16 @@ int recompute_logprobs(rg_policy* pol, const int32_t* prompts, const int32_t* pr
     LAUNCH(RG_K_EMBED, launch_recompute_rows(pol->dtype, pol->w_embed, rr, n, st));
     LAUNCH(RG_K_SETUP, launch_fill_i32(d_chunk, 1, n, st));
     RowTiles rt{d_tiles, (int)ceil_div(n, tile_rows) + std::min(n, N)};
-    if (use_tiles) LAUNCH(RG_K_SETUP, launch_row_tiles(pol->coff, N, (int)r0, n, tile_rows, d_chunk, pol->tile_r0,
-                                                       pol->tile_nr, d_tiles, st));
-    if ((rc = run_layers(pol, st, d_chunk, n, ctx_all, true, nullptr, use_tiles ? &rt : nullptr))) return rc;
+    if (use_tiles && !pol->kv8)
+      LAUNCH(RG_K_SETUP, launch_row_tiles(pol->coff, N, (int)r0, n, tile_rows, d_chunk, pol->tile_r0, pol->tile_nr,
+                                          d_tiles, st));
+    if (pol->kv8)
+      LAUNCH(RG_K_SETUP, launch_kv8_runs(pol->coff, pol->plen, pol->seq_grp, N, (int)r0, n, pol->run_off, pol->run_len,
+                                         st));
+    const Kv8Rows runs = kv8_runs(pol, 0, pol->run_off, pol->run_len, N, n);
+    if ((rc = run_layers(pol, st, d_chunk, n, ctx_all, true, nullptr, use_tiles ? &rt : nullptr,
+                         pol->kv8 ? &runs : nullptr)))
+      return rc;
     // Direct-to-LDS plans take the log-probability in the lm head's epilogue:
     // a row's logits (0.6 MB at 152k tokens) are neither written nor read back,
     // and the rows need no slices (four-layer 1.5B widths, 4096 rows: lm head

@@ -832,6 +832,22 @@ __global__ __launch_bounds__(128) void k_split_epilogue(const int* __restrict__ 
   }
 }
 
+// Sum of split partials + STORE epilogue, four columns a thread (N is a multiple
+// of 16): one wave per (256 columns, row).
+__global__ __launch_bounds__(64) void k_split_store(const int* __restrict__ d_rows, const float* __restrict__ part,
+                                                    int64_t pst, int N, int S, GemmEpi ep) {
+  const int r = blockIdx.y, c = (blockIdx.x * 64 + threadIdx.x) * 4;
+  const int rows_now = *d_rows;
+  const f32x4_t* pr = reinterpret_cast<const f32x4_t*>(part + (int64_t)r * N + min(c, N - 4));
+  const int64_t pst4 = pst / 4;
+  const float inv = wave_row_scale(ep, r, threadIdx.x);
+  f32x4_t a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = 0; s < S; ++s) a += pr[s * pst4];
+  if (r >= rows_now || c >= N) return;
+  *reinterpret_cast<f32x4_t*>(ep.C + (int64_t)r * ep.ldc + c) = a * inv;
+}
+
 // fp32 models: v_mfma_f32_16x16x4_f32 (full fp32 products and sums).  A block
 // owns 16 WMT rows x 32 columns; its four waves split K in turns of 16 and
 // meet in LDS, where the partial sums are added in wave order and the
@@ -1025,6 +1041,10 @@ hipError_t launch_split_epilogue(const int* d_rows, int rows_ub, int N, int S, c
       hipLaunchKernelGGL((k_split_epilogue<GEMM_EPI_SWIGLU>), grid, dim3(64), 0, st, d_rows, ep.part, ep.part_stride,
                          N, S, ep);
       break;
+    case GEMM_EPI_STORE:
+      hipLaunchKernelGGL(k_split_store, dim3((N / 4 + 63) / 64, rows_ub), dim3(64), 0, st, d_rows, ep.part,
+                         ep.part_stride, N, S, ep);
+      break;
     case GEMM_EPI_QKV:
       hipLaunchKernelGGL(k_qkv_epilogue4, dim3((N / 8 + 63) / 64, rows_ub), dim3(64), 0, st, d_rows, ep.part,
                          ep.part_stride, N, S, ep);
@@ -1164,7 +1184,7 @@ hipError_t launch_gemm(int dtype, const GemmPlan& p, const void* A, int lda, int
   if (rows_ub <= 0) return hipSuccess;
   const int S = p.splits, kps = p.k_per_split;
   if (S < 1 || S > GEMM_MAX_SPLITS || (S > 1 && !ep.part)) return hipErrorInvalidValue;
-  if (S > 1 && (ep.mode == GEMM_EPI_STORE || ep.mode == GEMM_EPI_LOGPROB)) return hipErrorInvalidValue;   // lm head: unsplit
+  if (S > 1 && ep.mode == GEMM_EPI_LOGPROB) return hipErrorInvalidValue;
   if ((ep.mode == GEMM_EPI_SWIGLU || ep.mode == GEMM_EPI_QKV) && N % 32) return hipErrorInvalidValue;
   if (ep.mode == GEMM_EPI_QKV && (ep.hd % 32 || 128 % ep.hd)) return hipErrorInvalidValue;
   if (dtype == 1) {

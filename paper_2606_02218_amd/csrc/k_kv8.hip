@@ -20,6 +20,7 @@
 
 #include "kv8_device.h"
 #include "rope_device.h"
+#include <hip/hip_ext.h>
 
 namespace {
 
@@ -221,6 +222,34 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
   }
 }
 
+__global__ __launch_bounds__(256) void k_kv8_runs(const int32_t* __restrict__ coff, const int32_t* __restrict__ plen,
+                                                  const int32_t* __restrict__ seq_grp, int n_seq, int row0, int n,
+                                                  int32_t* __restrict__ off, int32_t* __restrict__ len) {
+  const int s = blockIdx.x * blockDim.x + threadIdx.x;
+  if (s > n_seq) return;
+  const int f = coff[s];
+  off[s] = min(max(f - row0, 0), n);
+  if (s < n_seq) len[s] = plen[seq_grp[s]] + max(min(coff[s + 1], row0 + n) - f, 0);
+}
+
+// Grid (layers, pairs): a workgroup copies one layer of a page.
+__global__ __launch_bounds__(256) void k_kv8_page_copy(Kv8Pool c, int64_t layer_blocks, const int32_t* __restrict__ pairs,
+                                                       const int32_t* __restrict__ state) {
+  const int k = blockIdx.y;
+  if (k >= state[3]) return;
+  const int64_t n = (int64_t)c.n_kv << c.sub_shift, l0 = blockIdx.x * layer_blocks;   // blocks of a page
+  const int64_t src = l0 + pairs[2 * k] * n, dst = l0 + pairs[2 * k + 1] * n;
+  const int64_t pieces = n * c.hd;                  // of 16 bytes
+  for (int64_t i = threadIdx.x; i < pieces; i += blockDim.x) {
+    reinterpret_cast<u32x4_t*>(c.k)[dst * c.hd + i] = reinterpret_cast<const u32x4_t*>(c.k)[src * c.hd + i];
+    reinterpret_cast<u32x4_t*>(c.v)[dst * c.hd + i] = reinterpret_cast<const u32x4_t*>(c.v)[src * c.hd + i];
+  }
+  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) {
+    c.k_scale[dst + i] = c.k_scale[src + i];
+    c.v_scale[dst + i] = c.v_scale[src + i];
+  }
+}
+
 bool views_vector(int dtype, const HeadView& x) {
   const int e = dtype == 1 ? 8 : 4;
   return !x.p || ((uintptr_t)x.p % 16 == 0 && x.row % e == 0 && x.head % e == 0);
@@ -231,6 +260,7 @@ bool views_vector(int dtype, const HeadView& x) {
 hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, HeadView k, HeadView v, HeadView q,
                              HeadOut q_out, int n_q, const RopeTable& t, hipStream_t st) {
   if (b.rows <= 0 || b.n_seqs <= 0) return hipSuccess;
+  if (c.hd != 64 && c.hd != 128) return hipErrorInvalidValue;
   const int64_t items = b.seq_off ? (int64_t)b.rows / 16 + 2 * (int64_t)b.n_seqs : b.n_seqs;
   const AppendArgs a{c, b, k, v, q, q_out, n_q, t, items * c.n_kv * 2};
   const int64_t grid = (a.blocks + (q.p ? b.rows : 0) + 3) / 4;
@@ -239,13 +269,19 @@ hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, Head
   const bool vec = views_vector(dtype, k) && views_vector(dtype, v) && views_vector(dtype, HeadView{q_out.p, q_out.row, q_out.head}) &&
                    views_vector(dtype, q) && (t.layout ? (2 * t.pairs) % 8 == 0 : t.pairs % 8 == 0) &&
                    (uintptr_t)t.cos % 16 == 0 && (uintptr_t)t.sin % 16 == 0;
-#define RG_APP(T, VEC, LAY, HD) \
-  hipLaunchKernelGGL((k_kv8_append<T, VEC, LAY, HD>), dim3((unsigned)grid), dim3(256), 0, st, a)
+  hipEvent_t e0 = nullptr, e1 = nullptr;
+  const bool timed = rg_take_launch_events(&e0, &e1);
+#define RG_APP(T, VEC, LAY, HD)                                                                                        \
+  do {                                                                                                                 \
+    if (timed)                                                                                                         \
+      hipExtLaunchKernelGGL((k_kv8_append<T, VEC, LAY, HD>), dim3((unsigned)grid), dim3(256), 0, st, e0, e1, 0, a);    \
+    else                                                                                                               \
+      hipLaunchKernelGGL((k_kv8_append<T, VEC, LAY, HD>), dim3((unsigned)grid), dim3(256), 0, st, a);                  \
+  } while (0)
 #define RG_APP_HD(T, VEC, LAY) \
-  if (c.hd == 128) RG_APP(T, VEC, LAY, 128); else RG_APP(T, VEC, LAY, 64)
+  if (c.hd == 128) { RG_APP(T, VEC, LAY, 128); } else { RG_APP(T, VEC, LAY, 64); }
 #define RG_APP_L(T, VEC) \
   if (t.layout) { RG_APP_HD(T, VEC, 1); } else { RG_APP_HD(T, VEC, 0); }
-  if (c.hd != 64 && c.hd != 128) return hipErrorInvalidValue;
   if (dtype == 1) {
     if (vec) { RG_APP_L(bf16_t, true); } else { RG_APP_L(bf16_t, false); }
   } else {
@@ -254,5 +290,19 @@ hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, Head
 #undef RG_APP_L
 #undef RG_APP_HD
 #undef RG_APP
+  return hipGetLastError();
+}
+
+hipError_t launch_kv8_runs(const int32_t* coff, const int32_t* plen, const int32_t* seq_grp, int n_seq, int row0, int n,
+                           int32_t* off, int32_t* len, hipStream_t st) {
+  hipLaunchKernelGGL(k_kv8_runs, dim3((n_seq + 256) / 256), dim3(256), 0, st, coff, plen, seq_grp, n_seq, row0, n, off,
+                     len);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv8_page_copy(const Kv8Pool& c, int n_layers, int64_t layer_blocks, const int32_t* copy_pairs,
+                                int max_pairs, const int32_t* state, hipStream_t st) {
+  if (max_pairs <= 0) return hipSuccess;
+  hipLaunchKernelGGL(k_kv8_page_copy, dim3(n_layers, max_pairs), dim3(256), 0, st, c, layer_blocks, copy_pairs, state);
   return hipGetLastError();
 }

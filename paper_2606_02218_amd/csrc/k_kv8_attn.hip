@@ -98,10 +98,10 @@ __device__ __forceinline__ void put(const Kv8Attn& A, int64_t row, int head, int
 
 template <int N>
 __device__ __forceinline__ void put_part(const Kv8Attn& A, int64_t slot, int head, int d, const float (&v)[N]) {
-  st_elems<N, true>(A.part + (slot * A.n_q + head) * A.c.hd + d, v);
+  st_elems<N, true>(A.part_o + (slot * A.n_q + head) * A.c.hd + d, v);
 }
 __device__ __forceinline__ float* part_ml(const Kv8Attn& A, int64_t slot, int head) {
-  return A.part + (int64_t)A.b.rows * A.plan.n_split * A.n_q * A.c.hd + (slot * A.n_q + head) * 2;
+  return A.part_ml + (slot * A.n_q + head) * 2;
 }
 
 // ---------------------------------------------------------------- rows pass
@@ -600,7 +600,7 @@ __global__ __launch_bounds__(256) void k_kv8_merge(Kv8Attn A) {
   for (int c = wave; c < n; c += 4) {
     const int64_t slot = (int64_t)r * A.plan.n_split + c;
     const float* ml = part_ml(A, slot, h);
-    const float* po = A.part + (slot * A.n_q + h) * HD + lane * NV;
+    const float* po = A.part_o + (slot * A.n_q + h) * HD + lane * NV;
     float v[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) v[i] = po[i];
@@ -661,8 +661,12 @@ hipError_t run(const Kv8Attn& a, hipStream_t st) {
     if (8 * per > INT32_MAX) return hipErrorInvalidValue;
     launch(k_kv8_rows<T, HD, OUT>, dim3((unsigned)(8 * per)), dim3(64 * KV8_WAVES), st, a, htiles, (int)per, items);
   }
-  if (a.plan.n_split > 1)
-    hipLaunchKernelGGL((k_kv8_merge<HD, OUT>), dim3(a.b.rows, a.n_q), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+template <int HD, int OUT>
+hipError_t merge(const Kv8Attn& a, hipStream_t st) {
+  launch(k_kv8_merge<HD, OUT>, dim3(a.b.rows, a.n_q), dim3(256), st, a);
   return hipGetLastError();
 }
 
@@ -687,10 +691,19 @@ Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_
 
 hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStream_t st) {
   if (a.b.rows <= 0 || a.b.n_seqs <= 0) return hipSuccess;
-  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.chunk % 64 || (a.plan.n_split > 1 && !a.part))
+  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.chunk % 64 || (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
     return hipErrorInvalidValue;
   const bool w = a.c.hd == 128;
+  if (planes && dtype != 0) return hipErrorInvalidValue;
   if (planes) return w ? run<float, 128, OUT_PLANES>(a, st) : run<float, 64, OUT_PLANES>(a, st);
   if (dtype == 1) return w ? run<bf16_t, 128, OUT_BF16>(a, st) : run<bf16_t, 64, OUT_BF16>(a, st);
   return w ? run<float, 128, OUT_F32>(a, st) : run<float, 64, OUT_F32>(a, st);
+}
+
+hipError_t launch_kv8_merge(int dtype, bool planes, const Kv8Attn& a, hipStream_t st) {
+  if (a.b.rows <= 0 || a.b.n_seqs <= 0 || a.plan.n_split <= 1) return hipSuccess;
+  const bool w = a.c.hd == 128;
+  if (planes) return w ? merge<128, OUT_PLANES>(a, st) : merge<64, OUT_PLANES>(a, st);
+  if (dtype == 1) return w ? merge<128, OUT_BF16>(a, st) : merge<64, OUT_BF16>(a, st);
+  return w ? merge<128, OUT_F32>(a, st) : merge<64, OUT_F32>(a, st);
 }

@@ -144,10 +144,12 @@ int rg_kv8_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32
   a.n_q = n_q;
   a.scale = scale;
   a.plan = kv8_plan(a.b.rows, a.b.n_seqs, a.b.seq_off != nullptr, n_q, a.c.n_kv, max_len, INT32_MAX);
-  a.part = (float*)scratch;
+  a.part_o = (float*)scratch;
+  a.part_ml = a.part_o ? a.part_o + (int64_t)a.b.rows * a.plan.n_split * n_q * a.c.hd : nullptr;
   const int64_t need = 4 * kv8_part_floats(a.b.rows, a.plan, n_q, a.c.hd);
   if (need > 0 && (!scratch || scratch_bytes < need)) return bad(who, "scratch is smaller than rg_kv8_attention_scratch()");
-  return launched(who, launch_kv8_attention(dtype, false, a, (hipStream_t)stream));
+  if ((rc = launched(who, launch_kv8_attention(dtype, false, a, (hipStream_t)stream)))) return rc;
+  return launched(who, launch_kv8_merge(dtype, false, a, (hipStream_t)stream));
 }
 
 }  // extern "C"

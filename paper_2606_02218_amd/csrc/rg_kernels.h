@@ -435,9 +435,21 @@ struct Kv8Attn {
   int n_q;
   float scale;      // of the scores
   Kv8Plan plan;
-  float* part;      // n_split > 1: [rows][n_split][n_q][hd] then [rows][n_split][n_q][2]
+  float* part_o;    // n_split > 1: unnormalised outputs [rows][n_split][n_q][hd]
+  float* part_ml;   // and their (max, sum) [rows][n_split][n_q][2]
 };
 inline int64_t kv8_part_floats(int64_t rows, const Kv8Plan& p, int n_q, int hd) {
   return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
 }
+// The pass over the cache; with n_split > 1 launch_kv8_merge has to follow.
 hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStream_t st);
+hipError_t launch_kv8_merge(int dtype, bool planes, const Kv8Attn& a, hipStream_t st);
+// Rows row0 .. row0 + n - 1 of a teacher-forced forward as a batch of all
+// n_seq sequences (coff as in ReserveArgs): off [n_seq + 1], and the tokens that
+// each has once those rows are appended.
+hipError_t launch_kv8_runs(const int32_t* coff, const int32_t* plen, const int32_t* seq_grp, int n_seq, int row0, int n,
+                           int32_t* off, int32_t* len, hipStream_t st);
+// The blocks and scales of every layer for the fork's page copies; layer l of
+// the pool is layer_blocks * l blocks behind c.
+hipError_t launch_kv8_page_copy(const Kv8Pool& c, int n_layers, int64_t layer_blocks, const int32_t* copy_pairs,
+                                int max_pairs, const int32_t* state, hipStream_t st);
