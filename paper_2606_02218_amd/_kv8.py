@@ -33,17 +33,80 @@ _ARGS = {
                          C.c_int),
 }
 _ready = None
+_torch = _BF16 = _F32 = _E4M3 = _I32 = None
 
 
 def _library():
-    global _ready
+    global _ready, _torch, _BF16, _F32, _E4M3, _I32
     if _ready is None or _ready is not _lib._lib:
         lib = load_library()
         for name, (args, res) in _ARGS.items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, res
+        import torch
+        _torch, _BF16, _F32, _E4M3, _I32 = torch, torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.int32
         _ready = lib
     return _ready
+
+
+# A decode step's calls take a few microseconds on the device, and naming what is
+# wrong with an argument takes longer than that to set up.  So each call first asks
+# whether everything is as it should be, in the fewest questions; only where that
+# fails does it go through the checks that say what and raise, or find nothing
+# wrong (another device, a given stream) and go on.
+def _plain(t, dtype, dev):
+    return isinstance(t, _torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()
+
+
+def _cache_fits(cache, dev):
+    """The struct of a cache whose tensors are all in place, or None."""
+    k, v, ks, vs = cache
+    if not (_plain(k, _E4M3, dev) and _plain(v, _E4M3, dev) and _plain(ks, _F32, dev) and _plain(vs, _F32, dev)):
+        return None
+    shape = k.shape
+    if len(shape) != 4 or v.shape != shape or shape[3] % 16:
+        return None
+    pages, n_kv, parts, n = shape
+    if ks.shape != vs.shape or ks.shape != shape[:3]:
+        return None
+    return rg_kv8_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, n_kv, n // 16, 16 * parts)
+
+
+def _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev):
+    """The struct of a batch whose tensors are all in place, or None."""
+    if not (_plain(page_tab, _I32, dev) and _plain(seq_len, _I32, dev) and page_tab.dim() == 2 and seq_len.dim() == 1):
+        return None
+    n = seq_len.shape[0]
+    tab_rows, stride = page_tab.shape
+    off = row = 0
+    if seq_off is not None:
+        if not (_plain(seq_off, _I32, dev) and seq_off.shape == (n + 1,)):
+            return None
+        off = seq_off.data_ptr()
+    elif n != rows:
+        return None
+    if tab_row is not None:
+        if not (_plain(tab_row, _I32, dev) and tab_row.shape == (n,)):
+            return None
+        row = tab_row.data_ptr()
+    elif tab_rows < n:
+        return None
+    return rg_kv8_batch(page_tab.data_ptr(), tab_rows, stride, row, off, seq_len.data_ptr(), n, rows)
+
+
+def _table_fits(cos, sin, hd, dev):
+    """The turned dims of a rotary table that is in place, or 0."""
+    if not (_plain(cos, _F32, dev) and _plain(sin, _F32, dev)):
+        return 0
+    shape = cos.shape
+    if len(shape) != 2 or sin.shape != shape or shape[0] < 1 or not 2 <= 2 * shape[1] <= hd:
+        return 0
+    return 2 * shape[1]
+
+
+def _here(dev):
+    """Whether launches go to the device's current stream as things stand."""
+    return _torch._C._cuda_getDevice() == dev
 
 
 class _On:
@@ -166,15 +229,30 @@ def rope(x, pos, cos, sin, layout: str = "half", inverse: bool = False, out=None
     a rope_table of at most head_dim dims.  ``inverse=True`` turns back: the
     gradient with respect to x, given the one with respect to the result.
     ``out`` may be x.  See rg_rope in rollout.h."""
-    import torch
     lib = _library()
+    lay = ROPE_LAYOUTS.get(layout)
+    if isinstance(x, _torch.Tensor) and out is None and stream is None and lay is not None:
+        dt, dev = x.dtype, x.get_device()
+        if (dt is _BF16 or dt is _F32) and dev >= 0 and x.dim() == 3:
+            rows, heads, hd = x.shape
+            a, b, one = x.stride()
+            if one == 1 and hd % 2 == 0 and _plain(pos, _I32, dev) and pos.shape == (rows,) and _here(dev):
+                rot = _table_fits(cos, sin, hd, dev)
+                if rot:
+                    y = _torch.empty((rows, heads, hd), dtype=dt, device=x.device)
+                    rc = lib.rg_rope(1 if dt is _BF16 else 0, x.data_ptr(), a, b, y.data_ptr(), heads * hd, hd,
+                                     pos.data_ptr(), rows, heads, hd, cos.data_ptr(), sin.data_ptr(), cos.shape[0], rot,
+                                     lay, 1 if inverse else 0, _torch._C._cuda_getCurrentRawStream(dev))
+                    if rc:
+                        _check(rc)
+                    return y
     dt, code = _float_type("x", x)
     rows, heads, hd = x.shape
     _view("x", x, dt, x.shape)
     if hd < 2 or hd % 2:
         raise ValueError(f"head_dim must be even, got {hd}")
     rot = _tables(cos, sin, hd, layout)
-    _dev("pos", pos, torch.int32, (rows,))
+    _dev("pos", pos, _I32, (rows,))
     if out is not None:
         _written("out", _view("out", out, dt, x.shape))
     _one_device(dict(x=x, pos=pos, cos=cos, sin=sin, out=out))
@@ -253,8 +331,46 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
       seq_off   int32 [sequences + 1]: each sequence's rows, or None for one
                 row a sequence
     See rg_kv8_append in rollout.h for scales, rounding and what padding gets."""
-    import torch
     lib = _library()
+    if isinstance(k, _torch.Tensor) and k.dim() == 3 and q_out is None and stream is None:
+        dt, dev = k.dtype, k.get_device()
+        lay = ROPE_LAYOUTS.get(layout)
+        c = _cache_fits(cache, dev) if (dt is _BF16 or dt is _F32) and dev >= 0 and lay is not None and _here(dev) else None
+        if c is not None:
+            rows, n_kv, hd = shape = k.shape
+            kr, kh, k1 = k.stride()
+            b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
+            ok = (b is not None and n_kv == c.n_kv and hd == c.head_dim and isinstance(v, _torch.Tensor) and
+                  v.dtype is dt and v.get_device() == dev and v.shape == shape)
+            rot = n_pos = cp = sp = 0
+            if ok and cos is not None:
+                rot = _table_fits(cos, sin, hd, dev)
+                ok = rot > 0
+                if ok:
+                    n_pos, cp, sp = cos.shape[0], cos.data_ptr(), sin.data_ptr()
+            elif sin is not None:
+                ok = False
+            if ok:
+                vr, vh, v1 = v.stride()
+                ok = k1 == 1 and v1 == 1
+            y = None
+            n_q = qp = qr = qh = yp = 0
+            if ok and q is not None:
+                ok = isinstance(q, _torch.Tensor) and q.dtype is dt and q.get_device() == dev and q.dim() == 3
+                if ok:
+                    q0, n_q, qd = q.shape
+                    qr, qh, q1 = q.stride()
+                    ok = q0 == rows and qd == hd and q1 == 1 and n_q > 0 and n_q % n_kv == 0
+                if ok:
+                    y = _torch.empty((rows, n_q, hd), dtype=dt, device=q.device)
+                    qp, yp = q.data_ptr(), y.data_ptr()
+            if ok:
+                rc = lib.rg_kv8_append(C.byref(c), C.byref(b), 1 if dt is _BF16 else 0, k.data_ptr(), kr, kh, v.data_ptr(),
+                                       vr, vh, qp, qr, qh, yp, n_q * hd, hd, n_q, cp, sp, n_pos, rot, lay,
+                                       _torch._C._cuda_getCurrentRawStream(dev))
+                if rc:
+                    _check(rc)
+                return y
     dt, code = _float_type("k", k)
     c = _cache_args(cache)
     rows = k.shape[0]
@@ -299,8 +415,30 @@ def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[i
     better launches), ``scale`` defaults to 1/sqrt(head_dim).  Returns
     [rows, n_q, head_dim] in q's dtype, zeros for padding rows; rows past the
     last sequence's are not written.  See rg_kv8_attention in rollout.h."""
-    import torch
     lib = _library()
+    if isinstance(q, _torch.Tensor) and q.dim() == 3 and out is None and stream is None:
+        dt, dev = q.dtype, q.get_device()
+        c = _cache_fits(cache, dev) if (dt is _BF16 or dt is _F32) and dev >= 0 and _here(dev) else None
+        if c is not None:
+            rows, n_q, hd = q.shape
+            qr, qh, q1 = q.stride()
+            n_kv = c.n_kv
+            b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
+            if b is not None and hd == c.head_dim and q1 == 1 and n_q > 0 and n_q % n_kv == 0:
+                bound = max(1, b.tab_stride * c.page_tokens) if max_len is None else int(max_len)
+                if 1 <= bound <= 1 << 30:
+                    y = _torch.empty((rows, n_q, hd), dtype=dt, device=q.device)
+                    need = lib.rg_kv8_attention_scratch(n_q, n_kv, hd, rows, b.n_seqs, 0 if seq_off is None else 1, bound)
+                    scratch, sp = None, 0
+                    if need > 0:
+                        scratch = _torch.empty(need // 4, dtype=_F32, device=q.device)
+                        sp = scratch.data_ptr()
+                    rc = lib.rg_kv8_attention(C.byref(c), C.byref(b), 1 if dt is _BF16 else 0, q.data_ptr(), qr, qh, n_q,
+                                              y.data_ptr(), hd ** -0.5 if scale is None else float(scale), bound, sp, need,
+                                              _torch._C._cuda_getCurrentRawStream(dev))
+                    if rc:
+                        _check(rc)
+                    return y
     dt, code = _float_type("q", q)
     c = _cache_args(cache)
     rows, n_q, hd = q.shape
@@ -308,8 +446,7 @@ def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[i
     if n_q < 1 or n_q % c.n_kv:
         raise ValueError(f"q must have a multiple of {c.n_kv} heads, got {n_q}")
     b = _batch_args(rows, page_tab, seq_len, seq_off, tab_row)
-    if max_len is None:
-        max_len = max(1, b.tab_stride * c.page_tokens)
+    max_len = max(1, b.tab_stride * c.page_tokens) if max_len is None else int(max_len)
     if max_len < 1 or max_len > 1 << 30:
         raise ValueError(f"max_len must be in [1, 2^30], got {max_len}")
     if out is not None:
@@ -322,7 +459,7 @@ def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[i
             out = _empty(q, (rows, n_q, hd), dt, stream)
         need = lib.rg_kv8_attention_scratch(n_q, c.n_kv, hd, rows, b.n_seqs, 0 if seq_off is None else 1, max_len)
         _check(min(need, 0))
-        scratch = _empty(q, (need // 4,), torch.float32, stream) if need else None
+        scratch = _empty(q, (need // 4,), _F32, stream) if need else None
         _check(lib.rg_kv8_attention(C.byref(c), C.byref(b), code, q.data_ptr(), q.stride(0), q.stride(1), n_q,
                                     out.data_ptr(), hd ** -0.5 if scale is None else float(scale), max_len,
                                     0 if scratch is None else scratch.data_ptr(), need, _stream(dev, stream)))
