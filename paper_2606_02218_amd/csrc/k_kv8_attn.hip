@@ -20,11 +20,11 @@
 //   Its four waves take 32-token steps in turn straight from memory, 16 bytes a
 //   lane, and join in LDS.  Bound by the cache's bytes.
 // * Tiles pass (runs of rows): a workgroup per 128 query rows (positions x heads
-//   of a kv head) and chunk.  64-token pieces of codes go through LDS once for the
-//   four waves of 32 query rows.  Bound by the matrix products and, beside them,
-//   the exponentials and conversions of the vector units.
+//   of a kv head) and chunk.  64-token pieces go through LDS once for the four
+//   waves of 32 query rows.
 // * With several chunks a row, a merge joins their partial results in order.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv8_device.h"
 #include <hip/hip_ext.h>
@@ -106,7 +106,7 @@ __device__ __forceinline__ float* part_ml(const Kv8Attn& A, int64_t slot, int he
 
 // ---------------------------------------------------------------- rows pass
 template <typename T, int HD, int OUT>
-__global__ __launch_bounds__(64 * KV8_WAVES) void k_kv8_rows(Kv8Attn A, int htiles, int per_xcd, int64_t items) {
+__global__ __launch_bounds__(64 * KV8_WAVES, sizeof(T) == 2 || HD == 64 ? 4 : 3) void k_kv8_rows(Kv8Attn A, int htiles, int per_xcd, int items) {
   constexpr int QP = q_pieces(OUT), PP = p_pieces(OUT, false);
   constexpr int NJ = HD / 64;       // 16-byte loads of a block per lane
   constexpr int LDO = HD + 4;
@@ -115,13 +115,13 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void k_kv8_rows(Kv8Attn A, int htil
 
   // Blocks are dealt to the 8 XCDs in turn: neighbouring rows, which share
   // pages where they are siblings of a prompt, go to the same one.
-  int64_t item = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (item >= items) return;
-  const int split = (int)(item % A.plan.n_split);
-  item /= A.plan.n_split;
-  const int ht = (int)(item % htiles);
-  item /= htiles;
-  const int kvh = (int)(item % A.c.n_kv), r = (int)(item / A.c.n_kv);
+  unsigned item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if (item >= (unsigned)items) return;
+  const int split = (int)(item % (unsigned)A.plan.n_split);
+  item /= (unsigned)A.plan.n_split;
+  const int ht = (int)(item % (unsigned)htiles);
+  item /= (unsigned)htiles;
+  const int kvh = (int)(item % (unsigned)A.c.n_kv), r = (int)(item / (unsigned)A.c.n_kv);
   const int rep = A.n_q / A.c.n_kv, nh = min(16, rep - ht * 16), head0 = kvh * rep + ht * 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
@@ -171,62 +171,59 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void k_kv8_rows(Kv8Attn A, int htil
     kss = ids < 0 ? 1.f : A.c.k_scale[ids];
     vss = ids < 0 ? 1.f : A.c.v_scale[ids];
   };
-  auto fetch = [&](int i) {
+  auto fetch_k = [&](int i) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int id = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
-      if (id < 0) {                 // a page the pool has not: its tokens are NaN
+      const uint8_t* p = kl + (int64_t)max(__builtin_amdgcn_readlane(ids, 2 * (i & 31) + h), 0) * (16 * HD);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          kr[h][j] = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
-          vr[h][j] = u32x4_t{0, 0, 0, 0};
-        }
-      } else {
-        const int64_t at = (int64_t)id * (16 * HD);
+      for (int j = 0; j < NJ; ++j) kr[h][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + j * 1024));
+    }
+  };
+  auto fetch_v = [&](int i) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) kr[h][j] = *reinterpret_cast<const u32x4_t*>(kl + at + j * 1024);
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* p = vl + (int64_t)max(__builtin_amdgcn_readlane(ids, 2 * (i & 31) + h), 0) * (16 * HD);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) vr[h][j] = *reinterpret_cast<const u32x4_t*>(vl + at + j * 256);
-      }
+      for (int j = 0; j < NJ; ++j) vr[h][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + j * 256));
     }
   };
   if (mine > 0) {
     lists(0);
-    fetch(0);
+    fetch_k(0);
+    fetch_v(0);
   }
   for (int i = 0; i < mine; ++i) {
     const int t0 = c0 + 32 * (wave + KV8_WAVES * i);
     float ks[2], vs[2];
+    int lost = 0;                   // negative: a page the pool has not
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+      const int id = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
+      lost |= id;
       ks[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kss), 2 * (i & 31) + h));
       vs[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vss), 2 * (i & 31) + h));
     }
-    u32x4_t kc[2][NJ], vc[2][NJ];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        kc[h][j] = kr[h][j];
-        vc[h][j] = vr[h][j];
-      }
-    if (i + 1 < mine) {             // the next step's loads run under this step's products
-      if (((i + 1) & 31) == 0) lists(i + 1);
-      fetch(i + 1);
-    }
+    // a lost page's tokens: NaN scores (the codes in the registers are another page's)
+    const float none = lost < 0 ? __uint_as_float(0x7FC00000u) : 0.f;
     f32x4_t st[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      st[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      st[h] = f32x4_t{none, none, none, none};
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const bf16x8_t kf = kv8_bf16x8(kc[h][j][2 * e], kc[h][j][2 * e + 1], ks[h], ks[h]);
+          const bf16x8_t kf = kv8_bf16x8(kr[h][j][2 * e], kr[h][j][2 * e + 1], ks[h], ks[h]);
 #pragma unroll
           for (int n = 0; n < QP; ++n)
             st[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[2 * j + e][n], st[h], 0, 0, 0);
         }
+    }
+    // the next step's keys into the registers just read: they arrive under the
+    // softmax and the values' products, and other waves' work
+    if (i + 1 < mine) {
+      if (((i + 1) & 31) == 0) lists(i + 1);
+      fetch_k(i + 1);
     }
     // lane's tokens: 16 h + 4 grp + e of the step
     const int left = c1 - t0;       // tokens of the step that the chunk has
@@ -240,7 +237,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void k_kv8_rows(Kv8Attn A, int htil
         const int n = min(max(left - 16 * h - 4 * grp, 0), 4);
         const uint32_t keep = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) vc[h][j] &= keep;
+        for (int j = 0; j < NJ; ++j) vr[h][j] &= keep;
       }
     }
     float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])),
@@ -271,10 +268,11 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void k_kv8_rows(Kv8Attn A, int htil
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bf16x8_t vf = kv8_bf16x8(vc[0][j][e], vc[1][j][e], vs[0], vs[1]);
+        const bf16x8_t vf = kv8_bf16x8(vr[0][j][e], vr[1][j][e], vs[0], vs[1]);
 #pragma unroll
         for (int n = 0; n < PP; ++n) o[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], o[j][e], 0, 0, 0);
       }
+    if (i + 1 < mine) fetch_v(i + 1);
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -330,24 +328,36 @@ __device__ __forceinline__ uint32_t clear_nan(uint32_t w) {
   return w & ~(hit * 0xFFu);
 }
 
+// Codes are converted once a workgroup, on their way into LDS: a wave that
+// converted its own operands spent 128 of its 300 vector instructions per 64
+// tokens on it.  What bounds the pass then is shared out evenly between the
+// matrix instructions (32 of 32 cycles per wave and 64 tokens), the vector
+// instructions (exponentials first) and LDS reads (a kilobyte per matrix
+// instruction); two workgroups a CU run beside each other.
+//
+// LDS, in 16-byte pieces.  Keys [dim / 8][token]: a piece is 8 dims of a token.
+// Values [block][half hh][e][m]: a piece is dim DT m + e, tokens 4 hh .. + 3 and
+// 8 + 4 hh .. + 3 of a block, those whose probabilities lane half hh holds.  Lanes
+// read and write neighbouring pieces.
 template <typename T, int HD, int OUT>
 __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int tiles) {
   constexpr int QP = q_pieces(OUT), PP = p_pieces(OUT, true);
   constexpr int NK = HD / 16;       // 32x32x16 steps over the head's dims
   constexpr int DT = HD / 32;       // 32-dim tiles of the output: tile e holds dims DT * row + e
   constexpr int BLK = 16 * HD;      // bytes of a block
-  constexpr int PASSES = 4 * BLK / (256 * 16);   // 16-byte loads per thread and operand
-  __shared__ __attribute__((aligned(16))) uint8_t sK[2][4 * BLK], sV[2][4 * BLK];
-  __shared__ float sS[2][8];        // key, then value scales of the four blocks
+  constexpr int KP = 4 * BLK / (256 * 16);   // key pieces of a thread, 16 codes each
+  constexpr int SUB = QP == 1 ? 2 : 1;       // 32-token products whose scores are held at once
+  __shared__ u32x4_t sK[2][HD / 8][64], sV[2][4][2][DT][32];
+  __shared__ int sNan[2][KV8_WAVES];
 
   // Blocks are dealt to the 8 XCDs in turn, so with the kv heads side by side an
   // XCD keeps to few of them.  Tiles go last first: within a sequence the
   // longest contexts start first.
-  int64_t item = blockIdx.x;
-  const int kvh = (int)(item % A.c.n_kv);
-  item /= A.c.n_kv;
-  const int split = (int)(item % A.plan.n_split);
-  const int k = tiles - 1 - (int)(item / A.plan.n_split);
+  unsigned item = blockIdx.x;
+  const int kvh = (int)(item % (unsigned)A.c.n_kv);
+  item /= (unsigned)A.c.n_kv;
+  const int split = (int)(item % (unsigned)A.plan.n_split);
+  const int k = tiles - 1 - (int)(item / (unsigned)A.plan.n_split);
   const int rep = A.n_q / A.c.n_kv, np = KV8_TILE_Q / rep;
   int key, s, r0, n;
   s = kv8_find(A.b, k, np, 1, key);
@@ -365,6 +375,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
   const int most = kv8_most(A.c, A.b);
   const int limit = valid ? min(pos0 + qi / rep + 1, most) : 0;      // tokens the column sees
   const int wmax = pos0 + min(nr - 1, (wave * 32 + 31) / rep) + 1;   // most of any column of the wave
+  const int wmin = min(pos0 + wave * 32 / rep + 1, most);            // least of them
   const bool active = wave * 32 < nr * rep;
   const int end = min(pos0 + nr, most);   // tokens that the tile's last row sees
   const int64_t c0l = (int64_t)split * A.plan.chunk;
@@ -377,8 +388,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
     const T* qp = (const T*)A.q.p + row * A.q.row + head * A.q.head;
     const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk)
-      query8<T, QP>(qp + 16 * (2 * (kk >> 1) + hh) + 8 * (kk & 1), valid, vec, qf[kk]);
+    for (int kk = 0; kk < NK; ++kk) query8<T, QP>(qp + 16 * kk + 8 * hh, valid, vec, qf[kk]);
   }
   const float sc = A.scale * KV8_LOG2E;
   float m = -INFINITY, l = 0.f;
@@ -388,148 +398,181 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
 
-  // A pass of the workgroup's 16-byte loads covers whole blocks by whole waves:
-  // a wave's block ids and scales are scalars.
+  // A wave's key pieces of one pass lie in one block, and its value pieces too:
+  // block ids and scales are scalars.
   const int last_blk = (max(c1, 1) - 1) >> 4;
-  u32x4_t kr[PASSES], vr[PASSES];
-  float ksr[PASSES], vsr[PASSES];
-  int ids[PASSES];
-  auto piece = [&](int p) { return (p * 256 + wave * 64) * 16 / BLK; };   // block of the wave's piece in pass p
+  u32x4_t kr[KP], vr[2];
+  float ksr[KP], vsr;
+  int ids[KP], vid;
+  auto kpiece = [&](int p) { return (p * 256 + wave * 64) * 16 / BLK; };
+  const int vblk = HD == 128 ? wave : (tid & 127) >> 5;        // values: block, half and m of the thread
+  const int vhh = HD == 128 ? lane >> 5 : (tid >> 4) & 1, vm = HD == 128 ? lane & 31 : tid & 15;
+  const bool vmine = HD == 128 || tid < 128;
   auto list = [&](int t0) {
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p)
+    for (int p = 0; p < KP; ++p)
       ids[p] = __builtin_amdgcn_readfirstlane(
-          kv8_block(A.c, tab, A.b.tab_stride, min((t0 >> 4) + piece(p), last_blk), kvh));
+          kv8_block(A.c, tab, A.b.tab_stride, min((t0 >> 4) + kpiece(p), last_blk), kvh));
+    vid = kv8_block(A.c, tab, A.b.tab_stride, min((t0 >> 4) + vblk, last_blk), kvh);
+    if constexpr (HD == 128) vid = __builtin_amdgcn_readfirstlane(vid);
   };
+  // What is loaded here is first touched by the stash a piece later: a select on
+  // it now would wait for it.
+  int klost[KP], vlost;
   auto fetch = [&]() {
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int off = (p * 256 + tid) * 16 % BLK;
-      if (ids[p] < 0) {             // a page the pool has not: its tokens are NaN
-        kr[p] = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
-        vr[p] = u32x4_t{0, 0, 0, 0};
-        ksr[p] = vsr[p] = 1.f;
-      } else {
-        kr[p] = *reinterpret_cast<const u32x4_t*>(A.c.k + (int64_t)ids[p] * BLK + off);
-        vr[p] = *reinterpret_cast<const u32x4_t*>(A.c.v + (int64_t)ids[p] * BLK + off);
-        ksr[p] = A.c.k_scale[ids[p]];
-        vsr[p] = A.c.v_scale[ids[p]];
-      }
+    for (int p = 0; p < KP; ++p) {
+      kr[p] = *reinterpret_cast<const u32x4_t*>(A.c.k + (int64_t)max(ids[p], 0) * BLK + (p * 256 + tid) * 16 % BLK);
+      ksr[p] = A.c.k_scale[max(ids[p], 0)];
+      klost[p] = ids[p];
+    }
+    const uint8_t* vp = A.c.v + (int64_t)max(vid, 0) * BLK + vhh * (4 * HD) + vm * 16;
+    vr[0] = *reinterpret_cast<const u32x4_t*>(vp);
+    vr[1] = *reinterpret_cast<const u32x4_t*>(vp + 8 * HD);
+    vsr = A.c.v_scale[max(vid, 0)];
+    vlost = vid;
+  };
+  auto stash = [&](int buf, int t0) {
+    // a page the pool has not: its keys are NaN, its values 0
+    if (vlost < 0) vr[0] = vr[1] = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int p = 0; p < KP; ++p) {
+      if (klost[p] < 0) kr[p] = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
+      const int at = (p * 256 + tid) % HD, g = at >> 4, t = kpiece(p) * 16 + (at & 15);   // granule, token
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        sK[buf][2 * g + e][t] =
+            __builtin_bit_cast(u32x4_t, kv8_bf16x8(kr[p][2 * e], kr[p][2 * e + 1], ksr[p], ksr[p]));
+    }
+    if (t0 + 64 > pos0) {           // some rows do not see all of these tokens: 0 * NaN must not reach them
+      bool nan = false;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          nan |= has_nan_code(vr[h][e]);
+          vr[h][e] = clear_nan(vr[h][e]);
+        }
+      const bool any = __any(nan && vmine);
+      if (lane == 0) sNan[buf][wave] = any;
+    }
+    if (vmine) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)   // dim 4 vm + d = DT * (its row) + (its tile)
+        sV[buf][vblk][vhh][d % DT][(4 * vm + d) / DT] =
+            __builtin_bit_cast(u32x4_t, kv8_bf16x8(vr[0][d], vr[1][d], vsr, vsr));
     }
   };
-  auto stash = [&](int buf) {
+  // NaN values among the tokens of a piece: those that a column does see make its
+  // dims NaN.  A product counts them: ones at the NaN codes, ones at the tokens in
+  // sight.
+  auto nan_values = [&](int t0) {
+#pragma unroll 1
+    for (int b = 0; b < 4; ++b) {
+      if (t0 + 16 * b >= c1) break;
+      const int id = kv8_block(A.c, tab, A.b.tab_stride, (t0 >> 4) + b, kvh);
+      if (id < 0) continue;         // its keys made the rows NaN
+      const int left = limit - t0 - 16 * b - 4 * hh;
+      uint32_t seen[4];
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      *reinterpret_cast<u32x4_t*>(&sK[buf][(p * 256 + tid) * 16]) = kr[p];
-      *reinterpret_cast<u32x4_t*>(&sV[buf][(p * 256 + tid) * 16]) = vr[p];
-      if (lane == 0) {
-        sS[buf][piece(p)] = ksr[p];
-        sS[buf][4 + piece(p)] = vsr[p];
+      for (int i = 0; i < 4; ++i) {
+        const int t = i < 2 ? 2 * i : 4 + 2 * i;   // tokens t, t + 1 behind 4 hh
+        seen[i] = (t < left ? 0x3F80u : 0u) | (t + 1 < left ? 0x3F800000u : 0u);
       }
-    }
-  };
-  auto block = [&](int buf, int t0) {
-    f32x16_t st[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) st[u][i] = 0.f;
-      const int b = 2 * u + (c32 >> 4);
-      const float ks = sS[buf][b];
-      const uint8_t* kp = &sK[buf][b * BLK + (c32 & 15) * 16 + hh * 256];
-#pragma unroll
-      for (int j = 0; j < NK / 2; ++j) {
-        const u32x4_t w = *reinterpret_cast<const u32x4_t*>(kp + j * 512);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const bf16x8_t kf = kv8_bf16x8(w[2 * e], w[2 * e + 1], ks, ks);
-#pragma unroll
-          for (int n = 0; n < QP; ++n)
-            st[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[2 * j + e][n], st[u], 0, 0, 0);
-        }
-      }
-    }
-    // lane's tokens: 32 u + 8 (i / 4) + 4 hh + i % 4
-    const bool masked = __any(valid && t0 + 64 > limit);
-    if (masked) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (t0 + 32 * u + 8 * (i / 4) + 4 * hh + i % 4 >= limit) st[u][i] = -INFINITY;
-    }
-    float mx = st[0][0];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[u][i]);
-    mx *= sc;
-    if (__any(mx > m + KV8_SLACK)) {
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float mn = fmaxf(m, mx);
-      const float alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);   // -inf: nothing seen yet
-      l *= alpha;
-#pragma unroll
-      for (int e = 0; e < DT; ++e) o[e] *= alpha;
-      m = mn;
-    }
-    // a column that sees none of the tokens so far keeps m = -inf: its
-    // probabilities are exp2(-inf) = 0
-    const float ms = m == -INFINITY ? 0.f : m;
-    bf16x8_t pf[4][PP];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int a = 0; a < 2; ++a) {
-        float p[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(st[u][8 * a + e], sc, -ms));
-          l += p[e];
-        }
-        operand8<PP>(p, pf[2 * u + a]);
-      }
-    bool nan = false;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {   // 16 tokens: value rows 4 hh .. + 3 and 8 + 4 hh .. + 3
-      const uint8_t* vp = &sV[buf][b * BLK + hh * (4 * HD) + c32 * (4 * DT)];
-      uint32_t lo[DT], hi[DT];
-      if constexpr (DT == 4) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(vp), y = *reinterpret_cast<const u32x4_t*>(vp + 8 * HD);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { lo[e] = x[e]; hi[e] = y[e]; }
-      } else {
-        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(vp), y = *reinterpret_cast<const u32x2_t*>(vp + 8 * HD);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) { lo[e] = x[e]; hi[e] = y[e]; }
-      }
-      if (masked) {                 // 0 * NaN is NaN: masked tokens' NaN codes must not reach the product
-#pragma unroll
-        for (int e = 0; e < DT; ++e) {
-          nan |= has_nan_code(lo[e]) | has_nan_code(hi[e]);
-          lo[e] = clear_nan(lo[e]);
-          hi[e] = clear_nan(hi[e]);
-        }
-      }
-      const float vs = sS[buf][4 + b];
+      const uint32_t* vp = reinterpret_cast<const uint32_t*>(A.c.v + (int64_t)id * BLK + hh * (4 * HD)) + DT * c32;
 #pragma unroll
       for (int e = 0; e < DT; ++e) {
-        const bf16x8_t vf = kv8_bf16x8(lo[e], hi[e], vs, vs);
+        uint32_t one[4];
 #pragma unroll
-        for (int n = 0; n < PP; ++n) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[b][n], o[e], 0, 0, 0);
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t hit = (((vp[e + 2 * HD * h] & KV8_NAN4) + 0x01010101u) & 0x80808080u) >> 7;   // 1 in each such byte
+          one[2 * h] = (hit & 1u) * 0x3F80u | (hit >> 8 & 1u) * 0x3F800000u;
+          one[2 * h + 1] = (hit >> 16 & 1u) * 0x3F80u | (hit >> 24) * 0x3F800000u;
+        }
+        f32x16_t n;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) n[i] = 0.f;
+        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8_t, u32x4_t{one[0], one[1], one[2], one[3]}),
+            __builtin_bit_cast(bf16x8_t, u32x4_t{seen[0], seen[1], seen[2], seen[3]}), n, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if (n[i] > 0.f) o[e][i] = __uint_as_float(0x7FC00000u);
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
-    if (__any(nan)) {               // NaN values: those a column does see make its dims NaN
-      for (int t = 0; t < 64; ++t) {
-        if (t0 + t >= limit) break;
-        const uint8_t* vp = &sV[buf][(t >> 4) * BLK + ((t >> 2) & 3) * (4 * HD) + (t & 3)];
+  };
+  // One piece.  Only those past the wave's first row are masked: a variant of
+  // their own, as selects for all cost a fifth of a step.
+  auto block = [&](auto masked_, int buf, int t0) {
+    constexpr bool masked = decltype(masked_)::value;
+    // lane's tokens: 32 u + 8 (i / 4) + 4 hh + i % 4
 #pragma unroll
-        for (int e = 0; e < DT; ++e)
+    for (int u0 = 0; u0 < 2; u0 += SUB) {
+      f32x16_t st[SUB];
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if ((vp[(DT * (8 * (i / 4) + 4 * hh + i % 4) + e) * 4] & 0x7F) == 0x7F) o[e][i] = __uint_as_float(0x7FC00000u);
+      for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[u][i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, sK[buf][2 * kk + hh][32 * (u0 + u) + c32]);
+#pragma unroll
+          for (int n = 0; n < QP; ++n)
+            st[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk][n], st[u], 0, 0, 0);
+        }
       }
+      if constexpr (masked) {
+        const int left = limit - t0 - 4 * hh;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            if (32 * (u0 + u) + 8 * (i / 4) + i % 4 >= left) st[u][i] = -INFINITY;
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // all compares at once spill scalar registers
+          }
+      }
+      float mx = st[0][0];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[u][i]);
+      mx *= sc;
+      if (__any(mx > m + KV8_SLACK)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mn = fmaxf(m, mx);
+        const float alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);   // -inf: nothing seen yet
+        l *= alpha;
+#pragma unroll
+        for (int e = 0; e < DT; ++e) o[e] *= alpha;
+        m = mn;
+      }
+      // a column that sees none of the tokens so far keeps m = -inf: its
+      // probabilities are exp2(-inf) = 0
+      const float ms = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {   // 16 tokens
+          float p[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(fmaf(st[u][8 * a + e], sc, -ms));
+            l += p[e];
+          }
+          bf16x8_t pf[PP];
+          operand8<PP>(p, pf);
+#pragma unroll
+          for (int e = 0; e < DT; ++e) {
+            const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, sV[buf][2 * (u0 + u) + a][hh][e][c32]);
+#pragma unroll
+            for (int n = 0; n < PP; ++n) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[n], o[e], 0, 0, 0);
+          }
+        }
     }
+    if constexpr (masked)
+      if (sNan[buf][0] | sNan[buf][1] | sNan[buf][2] | sNan[buf][3]) nan_values(t0);
   };
 
   if (c0 < c1) {
@@ -538,13 +581,16 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
     list(c0 + 64);
     int buf = 0;
     for (int t0 = c0; t0 < c1; t0 += 64, buf ^= 1) {
-      stash(buf);
+      stash(buf, t0);
       __syncthreads();              // the piece is in LDS; the other buffer is free
       if (t0 + 64 < c1) {
         fetch();
         list(t0 + 128);
       }
-      if (active && t0 < wmax) block(buf, t0);
+      if (active && t0 < wmax) {
+        if (t0 + 64 <= wmin) block(std::false_type{}, buf, t0);
+        else block(std::true_type{}, buf, t0);
+      }
     }
   }
   if (!active) return;
@@ -583,58 +629,53 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
 }
 
 // ---------------------------------------------------------------- merge
-// One workgroup per (row, head): a wave takes every fourth chunk, a lane HD / 64 dims.
+// One workgroup per (row, head).  The chunks' weights exp2(m_c - M) go to LDS
+// first, so that the outputs' loads do not wait for one another; a thread sums 4
+// dims over every (1024 / HD)-th chunk, and the threads of a dim join in order.
+constexpr int KV8_MAX_SPLIT = 1024;
+
 template <int HD, int OUT>
 __global__ __launch_bounds__(256) void k_kv8_merge(Kv8Attn A) {
-  constexpr int NV = HD / 64;
-  __shared__ float sO[4][HD], sM[4], sL[4];
-  const int r = blockIdx.x, h = blockIdx.y;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int NT = HD / 4, NG = 256 / NT;   // threads of a chunk's output, chunks side by side
+  __shared__ float sw[KV8_MAX_SPLIT], red[16];
+  __shared__ __attribute__((aligned(16))) float sO[NG][HD];
+  const int r = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
   int s, pos;
   if (!kv8_row(A.b, r, s, pos)) return;
   const int ctx = min(pos + 1, kv8_most(A.c, A.b));
   const int n = ctx <= 0 ? 0 : min((ctx - 1) / A.plan.chunk + 1, A.plan.n_split);
-  float m = -INFINITY, l = 0.f, o[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) o[i] = 0.f;
-  for (int c = wave; c < n; c += 4) {
-    const int64_t slot = (int64_t)r * A.plan.n_split + c;
-    const float* ml = part_ml(A, slot, h);
-    const float* po = A.part_o + (slot * A.n_q + h) * HD + lane * NV;
-    float v[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = po[i];
-    const float mc = ml[0], lc = ml[1], mn = fmaxf(m, mc);
-    const float a = c == wave ? 0.f : __builtin_amdgcn_exp2f(m - mn), f = __builtin_amdgcn_exp2f(mc - mn);
-    l = l * a + lc * f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) o[i] = o[i] * a + v[i] * f;
-    m = mn;
+  const int64_t slot0 = (int64_t)r * A.plan.n_split;
+  float m = -INFINITY;
+  for (int c = tid; c < n; c += 256) m = fmaxf(m, part_ml(A, slot0 + c, h)[0]);
+  const float M = block_max(m, red);
+  float l = 0.f;
+  for (int c = tid; c < n; c += 256) {
+    const float* ml = part_ml(A, slot0 + c, h);
+    const float w = __builtin_amdgcn_exp2f(ml[0] - M);   // all -inf: NaN, as the scores were
+    sw[c] = w;
+    l += w * ml[1];
   }
+  const float L = block_sum(l, red);                       // its barriers order sw too
+  const int g = tid / NT, d = tid % NT * 4;
+  const float* po = A.part_o + (slot0 * A.n_q + h) * HD + d;
+  const int64_t step = (int64_t)A.n_q * HD;
+  f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  int c = g;
+  for (; c + 7 * NG < n; c += 8 * NG) {
+    f32x4_t x[8];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) sO[wave][lane * NV + i] = o[i];
-  if (lane == 0) {
-    sM[wave] = m;
-    sL[wave] = l;
+    for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(po + (c + i * NG) * step);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o += sw[c + i * NG] * x[i];
   }
+  for (; c < n; c += NG) o += sw[c] * *reinterpret_cast<const f32x4_t*>(po + c * step);
+  *reinterpret_cast<f32x4_t*>(&sO[g][d]) = o;
   __syncthreads();
-  if (tid >= HD / 4) return;
-  const int d = tid * 4, nw = min(n, 4);
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  if (nw > 0) {
-    float M = sM[0];
-    for (int w = 1; w < nw; ++w) M = fmaxf(M, sM[w]);
-    float L = 0.f;
-    for (int w = 0; w < nw; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sM[w] - M);
-      L += f * sL[w];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] += f * sO[w][d + i];
-    }
-    const float inv = 1.0f / L;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= inv;
-  }
+  if (tid >= NT) return;
+  const float inv = n > 0 ? 1.0f / L : 0.f;
+  f32x4_t acc = *reinterpret_cast<const f32x4_t*>(&sO[0][d]);
+  for (int i = 1; i < NG; ++i) acc += *reinterpret_cast<const f32x4_t*>(&sO[i][d]);
+  const float v[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
   put<OUT>(A, r, h, d, v);
 }
 
@@ -659,7 +700,7 @@ hipError_t run(const Kv8Attn& a, hipStream_t st) {
     const int htiles = (rep + 15) / 16;
     const int64_t items = (int64_t)a.b.rows * a.c.n_kv * htiles * a.plan.n_split, per = (items + 7) / 8;
     if (8 * per > INT32_MAX) return hipErrorInvalidValue;
-    launch(k_kv8_rows<T, HD, OUT>, dim3((unsigned)(8 * per)), dim3(64 * KV8_WAVES), st, a, htiles, (int)per, items);
+    launch(k_kv8_rows<T, HD, OUT>, dim3((unsigned)(8 * per)), dim3(64 * KV8_WAVES), st, a, htiles, (int)per, (int)items);
   }
   return hipGetLastError();
 }
@@ -673,16 +714,22 @@ hipError_t merge(const Kv8Attn& a, hipStream_t st) {
 }  // namespace
 
 // Rows or tiles: a tile's 128 query rows pay from a few rows a sequence on; below,
-// the rows pass keeps the matrix units no busier than the memory.  Chunks: as
-// many as give the chip about four workgroups a CU, of at least 512 tokens.
+// the rows pass keeps the matrix units no busier than the memory.  Chunks cost
+// their partial outputs (8 bytes of fp32 traffic per output, chunk and value) and
+// the merge's launch (4 us), so a context is cut only where there are fewer than
+// 512 workgroups, two a CU, and into no more than that: three rows of 95000 tokens
+// and 4 kv heads take 39 us at 504 workgroups, 41 at 1020, 47 at 1032 (a second
+// round for eight of them).  A chunk has 1024 tokens at least: 8 rows of 12 heads
+// and 600 tokens take 7.1 us whole, 6.1 + 4.2 in two.
 Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_len, int max_split) {
   Kv8Plan p{};
   const int rep = n_q / n_kv;
   p.tiles = has_off && rep <= KV8_TILE_Q && (int64_t)rows >= 4LL * n_seqs;
   const int64_t wgs = p.tiles ? ((int64_t)rows * rep + KV8_TILE_Q - 1) / KV8_TILE_Q * n_kv
                               : (int64_t)rows * n_kv * ((rep + 15) / 16);
-  int64_t n = std::min<int64_t>((1024 + wgs - 1) / wgs, (max_len + 511) / 512);
-  n = std::max<int64_t>(1, std::min<int64_t>(n, max_split));
+  int64_t n = 1;
+  if (wgs < 512) n = std::min<int64_t>(512 / wgs, max_len / 1024);
+  n = std::max<int64_t>(1, std::min<int64_t>({n, max_split, KV8_MAX_SPLIT}));
   p.chunk = (int)std::min<int64_t>((((int64_t)max_len + n - 1) / n + 63) / 64 * 64, 1 << 30);
   p.n_split = (int)((max_len + (int64_t)p.chunk - 1) / p.chunk);
   if (p.n_split < 1) p.n_split = 1;
@@ -691,7 +738,7 @@ Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_
 
 hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStream_t st) {
   if (a.b.rows <= 0 || a.b.n_seqs <= 0) return hipSuccess;
-  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.chunk % 64 || (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
+  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.n_split > KV8_MAX_SPLIT || a.plan.chunk % 64 || (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
     return hipErrorInvalidValue;
   const bool w = a.c.hd == 128;
   if (planes && dtype != 0) return hipErrorInvalidValue;
