@@ -20,7 +20,7 @@
 //   Its four waves take 32-token steps in turn straight from memory, 16 bytes a
 //   lane, and join in LDS.  Bound by the cache's bytes.
 // * Tiles pass (runs of rows): a workgroup per 128 query rows (positions x heads
-//   of a kv head) and chunk.  64-token pieces go through LDS once for the four
+//   of a kv head) and chunk.  32-token pieces go through LDS once for the four
 //   waves of 32 query rows.
 // * With several chunks a row, a merge joins their partial results in order.
 #include <algorithm>
@@ -330,24 +330,22 @@ __device__ __forceinline__ uint32_t clear_nan(uint32_t w) {
 
 // Codes are converted once a workgroup, on their way into LDS: a wave that
 // converted its own operands spent 128 of its 300 vector instructions per 64
-// tokens on it.  What bounds the pass then is shared out evenly between the
-// matrix instructions (32 of 32 cycles per wave and 64 tokens), the vector
-// instructions (exponentials first) and LDS reads (a kilobyte per matrix
-// instruction); two workgroups a CU run beside each other.
+// tokens on it.  A wave's chain through a piece (scores, maximum, exponentials,
+// values) is several times longer than its matrix instructions take, so what
+// counts is how many waves a SIMD has: pieces of 32 tokens and 168 registers leave
+// room for three workgroups a CU.
 //
 // LDS, in 16-byte pieces.  Keys [dim / 8][token]: a piece is 8 dims of a token.
 // Values [block][half hh][e][m]: a piece is dim DT m + e, tokens 4 hh .. + 3 and
 // 8 + 4 hh .. + 3 of a block, those whose probabilities lane half hh holds.  Lanes
-// read and write neighbouring pieces.
+// read neighbouring pieces.
 template <typename T, int HD, int OUT>
-__global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int tiles) {
+__global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8_tiles(Kv8Attn A, int tiles) {
   constexpr int QP = q_pieces(OUT), PP = p_pieces(OUT, true);
   constexpr int NK = HD / 16;       // 32x32x16 steps over the head's dims
   constexpr int DT = HD / 32;       // 32-dim tiles of the output: tile e holds dims DT * row + e
   constexpr int BLK = 16 * HD;      // bytes of a block
-  constexpr int KP = 4 * BLK / (256 * 16);   // key pieces of a thread, 16 codes each
-  constexpr int SUB = QP == 1 ? 2 : 1;       // 32-token products whose scores are held at once
-  __shared__ u32x4_t sK[2][HD / 8][64], sV[2][4][2][DT][32];
+  __shared__ u32x4_t sK[2][HD / 8][32], sV[2][2][2][DT][32];
   __shared__ int sNan[2][KV8_WAVES];
 
   // Blocks are dealt to the 8 XCDs in turn, so with the kv heads side by side an
@@ -375,7 +373,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
   const int most = kv8_most(A.c, A.b);
   const int limit = valid ? min(pos0 + qi / rep + 1, most) : 0;      // tokens the column sees
   const int wmax = pos0 + min(nr - 1, (wave * 32 + 31) / rep) + 1;   // most of any column of the wave
-  const int wmin = min(pos0 + wave * 32 / rep + 1, most);            // least of them
+  const int whole = min(pos0 + 1, most);  // tokens that every row of the tile sees
   const bool active = wave * 32 < nr * rep;
   const int end = min(pos0 + nr, most);   // tokens that the tile's last row sees
   const int64_t c0l = (int64_t)split * A.plan.chunk;
@@ -398,80 +396,71 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
 
-  // A wave's key pieces of one pass lie in one block, and its value pieces too:
-  // block ids and scales are scalars.
+  // Loads of a piece (2 blocks): 16 bytes of keys and 16 of values a thread (head
+  // dim 128), or of one of them (64).  A wave's lie in one block, so its id and
+  // scales are scalars.  What is loaded is first touched by the next stash: a
+  // select on it here would wait for it.
+  constexpr bool BOTH = HD == 128;
+  const bool has_k = BOTH || wave < 2, has_v = BOTH || wave >= 2;
+  const int wblk = BOTH ? wave >> 1 : wave & 1;
+  const int piece = tid & (HD - 1);             // of the block
   const int last_blk = (max(c1, 1) - 1) >> 4;
-  u32x4_t kr[KP], vr[2];
-  float ksr[KP], vsr;
-  int ids[KP], vid;
-  auto kpiece = [&](int p) { return (p * 256 + wave * 64) * 16 / BLK; };
-  const int vblk = HD == 128 ? wave : (tid & 127) >> 5;        // values: block, half and m of the thread
-  const int vhh = HD == 128 ? lane >> 5 : (tid >> 4) & 1, vm = HD == 128 ? lane & 31 : tid & 15;
-  const bool vmine = HD == 128 || tid < 128;
+  u32x4_t kr, vr;
+  float ksr = 1.f, vsr = 1.f;
+  int id, lost;
   auto list = [&](int t0) {
-#pragma unroll
-    for (int p = 0; p < KP; ++p)
-      ids[p] = __builtin_amdgcn_readfirstlane(
-          kv8_block(A.c, tab, A.b.tab_stride, min((t0 >> 4) + kpiece(p), last_blk), kvh));
-    vid = kv8_block(A.c, tab, A.b.tab_stride, min((t0 >> 4) + vblk, last_blk), kvh);
-    if constexpr (HD == 128) vid = __builtin_amdgcn_readfirstlane(vid);
+    id = __builtin_amdgcn_readfirstlane(kv8_block(A.c, tab, A.b.tab_stride, min((t0 >> 4) + wblk, last_blk), kvh));
   };
-  // What is loaded here is first touched by the stash a piece later: a select on
-  // it now would wait for it.
-  int klost[KP], vlost;
   auto fetch = [&]() {
-#pragma unroll
-    for (int p = 0; p < KP; ++p) {
-      kr[p] = *reinterpret_cast<const u32x4_t*>(A.c.k + (int64_t)max(ids[p], 0) * BLK + (p * 256 + tid) * 16 % BLK);
-      ksr[p] = A.c.k_scale[max(ids[p], 0)];
-      klost[p] = ids[p];
+    const int b = max(id, 0);
+    const int64_t at = (int64_t)b * BLK + piece * 16;
+    if (has_k) {
+      kr = *reinterpret_cast<const u32x4_t*>(A.c.k + at);
+      ksr = A.c.k_scale[b];
     }
-    const uint8_t* vp = A.c.v + (int64_t)max(vid, 0) * BLK + vhh * (4 * HD) + vm * 16;
-    vr[0] = *reinterpret_cast<const u32x4_t*>(vp);
-    vr[1] = *reinterpret_cast<const u32x4_t*>(vp + 8 * HD);
-    vsr = A.c.v_scale[max(vid, 0)];
-    vlost = vid;
+    if (has_v) {
+      vr = *reinterpret_cast<const u32x4_t*>(A.c.v + at);
+      vsr = A.c.v_scale[b];
+    }
+    lost = id;
   };
   auto stash = [&](int buf, int t0) {
-    // a page the pool has not: its keys are NaN, its values 0
-    if (vlost < 0) vr[0] = vr[1] = u32x4_t{0, 0, 0, 0};
-#pragma unroll
-    for (int p = 0; p < KP; ++p) {
-      if (klost[p] < 0) kr[p] = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
-      const int at = (p * 256 + tid) % HD, g = at >> 4, t = kpiece(p) * 16 + (at & 15);   // granule, token
+    if (lost < 0) {                 // a page the pool has not: its keys are NaN, its values 0
+      kr = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
+      vr = u32x4_t{0, 0, 0, 0};
+    }
+    if (has_k) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        sK[buf][2 * g + e][t] =
-            __builtin_bit_cast(u32x4_t, kv8_bf16x8(kr[p][2 * e], kr[p][2 * e + 1], ksr[p], ksr[p]));
+        sK[buf][2 * (piece >> 4) + e][16 * wblk + (piece & 15)] =
+            __builtin_bit_cast(u32x4_t, kv8_bf16x8(kr[2 * e], kr[2 * e + 1], ksr, ksr));
     }
-    if (t0 + 64 > pos0) {           // some rows do not see all of these tokens: 0 * NaN must not reach them
-      bool nan = false;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
+    if (has_v) {
+      if (t0 + 32 > whole) {        // some rows do not see all of these tokens: 0 * NaN must not reach them
+        bool nan = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          nan |= has_nan_code(vr[h][e]);
-          vr[h][e] = clear_nan(vr[h][e]);
+          nan |= has_nan_code(vr[e]);
+          vr[e] = clear_nan(vr[e]);
         }
-      const bool any = __any(nan && vmine);
-      if (lane == 0) sNan[buf][wave] = any;
-    }
-    if (vmine) {
+        const bool any = __any(nan);
+        if (lane == 0) sNan[buf][wave] = any;
+      }
+      const int tg = piece / (HD / 4), x = piece % (HD / 4);   // tokens 4 tg .., dims 4 x ..
 #pragma unroll
-      for (int d = 0; d < 4; ++d)   // dim 4 vm + d = DT * (its row) + (its tile)
-        sV[buf][vblk][vhh][d % DT][(4 * vm + d) / DT] =
-            __builtin_bit_cast(u32x4_t, kv8_bf16x8(vr[0][d], vr[1][d], vsr, vsr));
+      for (int d = 0; d < 4; ++d)
+        reinterpret_cast<u32x2_t*>(&sV[buf][wblk][tg & 1][d % DT][(4 * x + d) / DT])[tg >> 1] = kv8_bf16x4(vr[d], vsr);
     }
   };
-  // NaN values among the tokens of a piece: those that a column does see make its
-  // dims NaN.  A product counts them: ones at the NaN codes, ones at the tokens in
-  // sight.
+  // NaN values among the 32 tokens of a piece: those that a column does see make
+  // its dims NaN.  A product counts them: ones at the NaN codes, ones at the tokens
+  // in sight.
   auto nan_values = [&](int t0) {
 #pragma unroll 1
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < 2; ++b) {
       if (t0 + 16 * b >= c1) break;
-      const int id = kv8_block(A.c, tab, A.b.tab_stride, (t0 >> 4) + b, kvh);
-      if (id < 0) continue;         // its keys made the rows NaN
+      const int nid = kv8_block(A.c, tab, A.b.tab_stride, (t0 >> 4) + b, kvh);
+      if (nid < 0) continue;        // its keys made the rows NaN
       const int left = limit - t0 - 16 * b - 4 * hh;
       uint32_t seen[4];
 #pragma unroll
@@ -479,7 +468,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
         const int t = i < 2 ? 2 * i : 4 + 2 * i;   // tokens t, t + 1 behind 4 hh
         seen[i] = (t < left ? 0x3F80u : 0u) | (t + 1 < left ? 0x3F800000u : 0u);
       }
-      const uint32_t* vp = reinterpret_cast<const uint32_t*>(A.c.v + (int64_t)id * BLK + hh * (4 * HD)) + DT * c32;
+      const uint32_t* vp = reinterpret_cast<const uint32_t*>(A.c.v + (int64_t)nid * BLK + hh * (4 * HD)) + DT * c32;
 #pragma unroll
       for (int e = 0; e < DT; ++e) {
         uint32_t one[4];
@@ -503,92 +492,79 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8_tiles(Kv8Attn A, int 
       }
     }
   };
-  // One piece.  Only those past the wave's first row are masked: a variant of
-  // their own, as selects for all cost a fifth of a step.
+  // One piece; lane's tokens are 8 (i / 4) + 4 hh + i % 4.  Only pieces that reach
+  // past the tile's first row are masked (those whose NaN values the stash took
+  // out): a variant of their own, as selects for all cost a fifth of a step.
   auto block = [&](auto masked_, int buf, int t0) {
     constexpr bool masked = decltype(masked_)::value;
-    // lane's tokens: 32 u + 8 (i / 4) + 4 hh + i % 4
+    f32x16_t st;
 #pragma unroll
-    for (int u0 = 0; u0 < 2; u0 += SUB) {
-      f32x16_t st[SUB];
+    for (int i = 0; i < 16; ++i) st[i] = 0.f;
 #pragma unroll
-      for (int u = 0; u < SUB; ++u) {
+    for (int kk = 0; kk < NK; ++kk) {
+      const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, sK[buf][2 * kk + hh][c32]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st[u][i] = 0.f;
+      for (int n = 0; n < QP; ++n) st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk][n], st, 0, 0, 0);
+    }
+    if constexpr (masked) {
+      const int left = limit - t0 - 4 * hh;
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk) {
-          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, sK[buf][2 * kk + hh][32 * (u0 + u) + c32]);
-#pragma unroll
-          for (int n = 0; n < QP; ++n)
-            st[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk][n], st[u], 0, 0, 0);
-        }
+      for (int i = 0; i < 16; ++i) {
+        if (8 * (i / 4) + i % 4 >= left) st[i] = -INFINITY;
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // all compares at once spill scalar registers
       }
-      if constexpr (masked) {
-        const int left = limit - t0 - 4 * hh;
+    }
+    float mx = st[0];
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, st[i]);
+    mx *= sc;
+    if (__any(mx > m + KV8_SLACK)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = fmaxf(m, mx);
+      const float alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);   // -inf: nothing seen yet
+      l *= alpha;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if (32 * (u0 + u) + 8 * (i / 4) + i % 4 >= left) st[u][i] = -INFINITY;
-            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // all compares at once spill scalar registers
-          }
+      for (int e = 0; e < DT; ++e) o[e] *= alpha;
+      m = mn;
+    }
+    // a column that sees none of the tokens so far keeps m = -inf: its
+    // probabilities are exp2(-inf) = 0
+    const float ms = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {   // 16 tokens
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(fmaf(st[8 * a + e], sc, -ms));
+        l += p[e];
       }
-      float mx = st[0][0];
+      bf16x8_t pf[PP];
+      operand8<PP>(p, pf);
 #pragma unroll
-      for (int u = 0; u < SUB; ++u)
+      for (int e = 0; e < DT; ++e) {
+        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, sV[buf][a][hh][e][c32]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[u][i]);
-      mx *= sc;
-      if (__any(mx > m + KV8_SLACK)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float mn = fmaxf(m, mx);
-        const float alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);   // -inf: nothing seen yet
-        l *= alpha;
-#pragma unroll
-        for (int e = 0; e < DT; ++e) o[e] *= alpha;
-        m = mn;
+        for (int n = 0; n < PP; ++n) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[n], o[e], 0, 0, 0);
       }
-      // a column that sees none of the tokens so far keeps m = -inf: its
-      // probabilities are exp2(-inf) = 0
-      const float ms = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int u = 0; u < SUB; ++u)
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {   // 16 tokens
-          float p[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(fmaf(st[u][8 * a + e], sc, -ms));
-            l += p[e];
-          }
-          bf16x8_t pf[PP];
-          operand8<PP>(p, pf);
-#pragma unroll
-          for (int e = 0; e < DT; ++e) {
-            const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, sV[buf][2 * (u0 + u) + a][hh][e][c32]);
-#pragma unroll
-            for (int n = 0; n < PP; ++n) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[n], o[e], 0, 0, 0);
-          }
-        }
     }
     if constexpr (masked)
-      if (sNan[buf][0] | sNan[buf][1] | sNan[buf][2] | sNan[buf][3]) nan_values(t0);
+      if (BOTH ? sNan[buf][0] | sNan[buf][1] | sNan[buf][2] | sNan[buf][3] : sNan[buf][2] | sNan[buf][3]) nan_values(t0);
   };
 
   if (c0 < c1) {
     list(c0);
     fetch();
-    list(c0 + 64);
+    list(c0 + 32);
     int buf = 0;
-    for (int t0 = c0; t0 < c1; t0 += 64, buf ^= 1) {
+    for (int t0 = c0; t0 < c1; t0 += 32, buf ^= 1) {
       stash(buf, t0);
       __syncthreads();              // the piece is in LDS; the other buffer is free
-      if (t0 + 64 < c1) {
+      if (t0 + 32 < c1) {
         fetch();
-        list(t0 + 128);
+        list(t0 + 64);
       }
       if (active && t0 < wmax) {
-        if (t0 + 64 <= wmin) block(std::false_type{}, buf, t0);
+        if (t0 + 32 <= whole) block(std::false_type{}, buf, t0);
         else block(std::true_type{}, buf, t0);
       }
     }

@@ -178,6 +178,25 @@ def test_masked_tokens_do_not_touch_a_row(hd):
                 assert np.all(np.isfinite(out[new[0]:]))
 
 
+@pytest.mark.parametrize("hd,rep", [(64, 1), (64, 3), (128, 7)])
+def test_nan_values_reach_just_the_rows_that_see_them(hd, rep):
+    """One NaN value at a time, at places before, among and behind the rows of tiles: rows in sight get NaN in its dim."""
+    import paper_2606_02218_amd as rg
+    old, new = 30, 150
+    q = None
+    for at in (0, 29, 30, 31, 33, 47, 62, 63, 64, 70, 95, 96, 127, 128, 150, 178, 179):
+        b = Batch([old + new], 1, hd, 16, seed=1)
+        d = (7 * at) % hd
+        b.v[0].codes[at, 0, d] = 0x7F
+        b.write()
+        q = rounded(b.rng.normal(size=(new, rep, hd)), BF16) if q is None else q
+        nan = np.zeros((new, rep, hd), bool)
+        nan[np.arange(old, old + new) >= at, :, d] = True
+        for dtype in (BF16, F32):
+            out = host(rg.kv8_attention(b.cache, dev(q, dtype), dev(b.tab), dev(b.lengths()), offsets([new])))
+            assert np.array_equal(np.isnan(out), nan), (at, dtype)
+
+
 def test_special_queries_stay_in_their_heads():
     import paper_2606_02218_amd as rg
     b = Batch([90, 33], 2, 64, 16, seed=6)
