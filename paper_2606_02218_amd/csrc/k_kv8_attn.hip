@@ -17,8 +17,8 @@
 // between lanes but the maxima and sums.
 //
 // * Rows pass (single tokens): a workgroup per row, kv head and context chunk.
-//   Its four waves take 32-token steps in turn straight from memory, 16 bytes a
-//   lane, and join in LDS.  Bound by the cache's bytes.
+//   Its four or eight waves take 32-token steps in turn straight from memory, 16
+//   bytes a lane, and join in LDS.  Bound by the cache's bytes.
 // * Tiles pass (runs of rows): a workgroup per 128 query rows (positions x heads
 //   of a kv head) and chunk.  32-token pieces go through LDS once for the four
 //   waves of 32 query rows.
@@ -105,13 +105,13 @@ __device__ __forceinline__ float* part_ml(const Kv8Attn& A, int64_t slot, int he
 }
 
 // ---------------------------------------------------------------- rows pass
-template <typename T, int HD, int OUT>
-__global__ __launch_bounds__(64 * KV8_WAVES, sizeof(T) == 2 || HD == 64 ? 4 : 3) void k_kv8_rows(Kv8Attn A, int htiles, int per_xcd, int items) {
+template <typename T, int HD, int OUT, int W>
+__global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / W) void k_kv8_rows(Kv8Attn A, int htiles, int per_xcd, int items) {
   constexpr int QP = q_pieces(OUT), PP = p_pieces(OUT, false);
   constexpr int NJ = HD / 64;       // 16-byte loads of a block per lane
   constexpr int LDO = HD + 4;
-  __shared__ __attribute__((aligned(16))) float sO[KV8_WAVES][16][LDO];
-  __shared__ float sM[KV8_WAVES][16], sL[KV8_WAVES][16];
+  __shared__ __attribute__((aligned(16))) float sO[W][16][LDO];
+  __shared__ float sM[W][16], sL[W][16];
 
   // Blocks are dealt to the 8 XCDs in turn: neighbouring rows, which share
   // pages where they are siblings of a prompt, go to the same one.
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, sizeof(T) == 2 || HD == 64 ? 4 : 3)
   if (!kv8_row(A.b, r, s, pos)) return;
   if (pos < 0) {                    // a padding row sees nothing
     if (A.plan.n_split == 1)
-      for (int i = tid; i < nh * HD / 4; i += 64 * KV8_WAVES) {
+      for (int i = tid; i < nh * HD / 4; i += 64 * W) {
         const float z[4] = {0.f, 0.f, 0.f, 0.f};
         put<OUT>(A, r, head0 + i / (HD / 4), i % (HD / 4) * 4, z);
       }
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, sizeof(T) == 2 || HD == 64 ? 4 : 3)
   if (c0l >= ctx) return;
   const int c0 = (int)c0l, c1 = split == A.plan.n_split - 1 ? ctx : min(ctx, c0 + A.plan.chunk);
   const int steps = (c1 - c0 + 31) / 32, last_blk = (c1 - 1) >> 4;
-  const int mine = (steps - wave + KV8_WAVES - 1) / KV8_WAVES;   // steps wave, wave + 4, ...
+  const int mine = (steps - wave + W - 1) / W;   // steps wave, wave + 4, ...
   const int32_t* tab = kv8_table(A.b, s);
 
   bf16x8_t qf[2 * NJ][QP];
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, sizeof(T) == 2 || HD == 64 ? 4 : 3)
   int ids = 0;                      // lane i: block i & 1 of step i >> 1 of the current 32 steps
   float kss = 1.f, vss = 1.f;
   auto lists = [&](int i0) {
-    const int st = wave + KV8_WAVES * (i0 + (lane >> 1));
+    const int st = wave + W * (i0 + (lane >> 1));
     const int blk = min((c0 >> 4) + 2 * st + (lane & 1), last_blk);
     ids = kv8_block(A.c, tab, A.b.tab_stride, blk, kvh);
     kss = ids < 0 ? 1.f : A.c.k_scale[ids];
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, sizeof(T) == 2 || HD == 64 ? 4 : 3)
     fetch_v(0);
   }
   for (int i = 0; i < mine; ++i) {
-    const int t0 = c0 + 32 * (wave + KV8_WAVES * i);
+    const int t0 = c0 + 32 * (wave + W * i);
     float ks[2], vs[2];
     int lost = 0;                   // negative: a page the pool has not
 #pragma unroll
@@ -291,9 +291,9 @@ __global__ __launch_bounds__(64 * KV8_WAVES, sizeof(T) == 2 || HD == 64 ? 4 : 3)
   }
   __syncthreads();
   const int64_t slot = (int64_t)r * A.plan.n_split + split;
-  for (int i = tid; i < nh * (HD / 4); i += 64 * KV8_WAVES) {
+  for (int i = tid; i < nh * (HD / 4); i += 64 * W) {
     const int h = i / (HD / 4), d = i % (HD / 4) * 4;
-    const int nw = min(steps, KV8_WAVES);        // waves that had a step
+    const int nw = min(steps, W);        // waves that had a step
     float M = sM[0][h];
     for (int w = 1; w < nw; ++w) M = fmaxf(M, sM[w][h]);
     float L = 0.f;
@@ -676,7 +676,9 @@ hipError_t run(const Kv8Attn& a, hipStream_t st) {
     const int htiles = (rep + 15) / 16;
     const int64_t items = (int64_t)a.b.rows * a.c.n_kv * htiles * a.plan.n_split, per = (items + 7) / 8;
     if (8 * per > INT32_MAX) return hipErrorInvalidValue;
-    launch(k_kv8_rows<T, HD, OUT>, dim3((unsigned)(8 * per)), dim3(64 * KV8_WAVES), st, a, htiles, (int)per, (int)items);
+    const dim3 grid((unsigned)(8 * per));
+    if (a.plan.waves == 8) launch(k_kv8_rows<T, HD, OUT, 8>, grid, dim3(512), st, a, htiles, (int)per, (int)items);
+    else launch(k_kv8_rows<T, HD, OUT, 4>, grid, dim3(256), st, a, htiles, (int)per, (int)items);
   }
   return hipGetLastError();
 }
@@ -690,21 +692,27 @@ hipError_t merge(const Kv8Attn& a, hipStream_t st) {
 }  // namespace
 
 // Rows or tiles: a tile's 128 query rows pay from a few rows a sequence on; below,
-// the rows pass keeps the matrix units no busier than the memory.  Chunks cost
-// their partial outputs (8 bytes of fp32 traffic per output, chunk and value) and
-// the merge's launch (4 us), so a context is cut only where there are fewer than
-// 512 workgroups, two a CU, and into no more than that: three rows of 95000 tokens
-// and 4 kv heads take 39 us at 504 workgroups, 41 at 1020, 47 at 1032 (a second
-// round for eight of them).  A chunk has 1024 tokens at least: 8 rows of 12 heads
-// and 600 tokens take 7.1 us whole, 6.1 + 4.2 in two.
+// the rows pass keeps the matrix units no busier than the memory.
+//
+// Waves of a rows workgroup: eight where one round of a workgroup a CU holds them
+// all (a row's chain of steps is then what the launch waits for: 8 rows of 12 heads
+// and 600 tokens 5.5 us, with four waves 6.1), else four (512 rows of 2 kv heads and
+// 1556 tokens 55 us; with eight, in two rounds, 63).
+//
+// Chunks cost their partial outputs and the merge's launch (5 us), so a context is
+// cut only as far as one round goes: three rows of 95000 tokens and 4 kv heads take
+// 37 + 5 us in 21 chunks (252 workgroups), 48 + 5 in 85.  Rows from 2048 tokens on
+// (below, the merge costs what it saves: 600 tokens in two chunks 6.1 + 4.2 us),
+// tiles from 1024, which take some 30 us per 1000 tokens; chunks of 512 at least.
 Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_len, int max_split) {
   Kv8Plan p{};
   const int rep = n_q / n_kv;
   p.tiles = has_off && rep <= KV8_TILE_Q && (int64_t)rows >= 4LL * n_seqs;
   const int64_t wgs = p.tiles ? ((int64_t)rows * rep + KV8_TILE_Q - 1) / KV8_TILE_Q * n_kv
                               : (int64_t)rows * n_kv * ((rep + 15) / 16);
+  p.waves = wgs <= 256 ? 8 : 4;
   int64_t n = 1;
-  if (wgs < 512) n = std::min<int64_t>(512 / wgs, max_len / 1024);
+  if (max_len >= (p.tiles ? 1024 : 2048)) n = std::min<int64_t>((p.tiles ? 512 : 256) / wgs, max_len / 512);
   n = std::max<int64_t>(1, std::min<int64_t>({n, max_split, KV8_MAX_SPLIT}));
   p.chunk = (int)std::min<int64_t>((((int64_t)max_len + n - 1) / n + 63) / 64 * 64, 1 << 30);
   p.n_split = (int)((max_len + (int64_t)p.chunk - 1) / p.chunk);

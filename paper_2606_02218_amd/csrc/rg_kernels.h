@@ -423,6 +423,7 @@ hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, Head
 // share each staged block, the context into n_split chunks of `chunk` tokens.
 struct Kv8Plan {
   bool tiles;
+  int waves;   // of a rows workgroup
   int n_split, chunk;
 };
 Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_len, int max_split);
