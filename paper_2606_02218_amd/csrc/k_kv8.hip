@@ -31,12 +31,27 @@ struct AppendArgs {
   HeadOut q_out;
   int n_q;
   RopeTable t;
-  int64_t blocks;   // block items: bound on the batch's blocks x n_kv x 2
+  unsigned blocks;   // block items: bound on the batch's blocks x n_kv x 2
 };
 
 __device__ __forceinline__ float finite_abs(float x) {
   const float a = fabsf(x);
   return a < INFINITY ? a : 0.f;   // NaN and infinities do not set a scale
+}
+
+// Largest value of the wave's lanes, in every lane: through the vector unit's own
+// lane moves, half the latency of six exchanges through LDS.
+__device__ __forceinline__ float wave_max_dpp(float v) {
+#define RG_DPP_MAX(ctrl) \
+  v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), ctrl, 0xf, 0xf, false)))
+  RG_DPP_MAX(0x111);   // row_shr 1, 2, 4, 8: lane 15 of each row of 16 has its maximum
+  RG_DPP_MAX(0x112);
+  RG_DPP_MAX(0x114);
+  RG_DPP_MAX(0x118);
+  RG_DPP_MAX(0x142);   // row_bcast 15, 31: lane 63 has the wave's
+  RG_DPP_MAX(0x143);
+#undef RG_DPP_MAX
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // Dims d0 .. d0 + 7 of a key, turned.  x: the head; ok: the position is in the table.
@@ -86,11 +101,11 @@ __device__ __forceinline__ void turned8(const T* x, int d0, const RopeTable& t, 
 template <typename T, bool VEC, int LAYOUT, int HD>
 __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
   const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const unsigned item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const Kv8Rows& b = A.b;
   if (item >= A.blocks) {                     // a query row
     const int64_t r = item - A.blocks;
-    if (r >= b.rows || !A.q.p) return;
+    if (r >= b.rows) return;
     int s, pos;
     if (!kv8_row(b, (int)r, s, pos) || pos < 0) return;
     rope_row<T, VEC ? (int)(16 / sizeof(T)) : 1, LAYOUT>((const T*)A.q.p + r * A.q.row, A.q.head,
@@ -99,8 +114,8 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
     return;
   }
   const bool values = item & 1;
-  const int64_t hb = item >> 1;
-  const int kvh = (int)(hb % A.c.n_kv), x = (int)(hb / A.c.n_kv);
+  const unsigned hb = item >> 1;
+  const int x = (int)(hb / (unsigned)A.c.n_kv), kvh = (int)(hb - (unsigned)x * A.c.n_kv);
   // item x of the batch: sequence s, its j-th block.  A sequence of n rows
   // touches at most n / 16 + 2 blocks.
   int s = x, key = x, r0, n;
@@ -113,13 +128,25 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
   if (len <= p0) return;
   const int blk = (p0 >> 4) + (x - key);
   if (blk * 16 >= len) return;
-  const int id = kv8_block(A.c, kv8_table(b, s), b.tab_stride, blk, kvh);
-  if (id < 0) return;                         // no such page: nothing to write to
+  // The chain to the block's address and old scale (table row, page, scale) runs
+  // beside the rows' own loads: its indexes are clipped rather than branched on.
+  const int tr = b.tab_row ? b.tab_row[s] : s, slot = blk >> A.c.sub_shift;
+  const bool on_table = (unsigned)tr < (unsigned)b.tab_rows && slot < b.tab_stride;
+  const int page = b.tab[on_table ? (int64_t)tr * b.tab_stride + slot : 0];
   const int first = max(p0 - blk * 16, 0), last = min(len - blk * 16, 16);   // the block's new tokens
   const int64_t row0 = (int64_t)r0 + (blk * 16 - p0);                        // row of the block's token 0
-  float* sp = (values ? A.c.v_scale : A.c.k_scale) + id;
-  uint8_t* out = (values ? A.c.v : A.c.k) + (int64_t)id * (16 * HD);
-  const float s_old = first > 0 ? *sp : 0.f;
+  int id = -1;
+  float s_old = 0.f;
+  float* sp = nullptr;
+  uint8_t* out = nullptr;
+  auto place = [&]() {                        // false: no such page, nothing to write to
+    if (!on_table || (unsigned)page >= (unsigned)A.c.pages) return false;
+    id = ((page * A.c.n_kv + kvh) << A.c.sub_shift) + (blk & ((1 << A.c.sub_shift) - 1));
+    sp = (values ? A.c.v_scale : A.c.k_scale) + id;
+    out = (values ? A.c.v : A.c.k) + (int64_t)id * (16 * HD);
+    if (first > 0) s_old = *sp;
+    return true;
+  };
   if (!values) {
     constexpr int NG = HD / 64;               // granules of a lane
     const int t = lane >> 2, c = lane & 3;
@@ -136,12 +163,15 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           turned8<T, VEC, LAYOUT>(kp, 16 * (c + 4 * g) + 8 * h, A.t, A.t.cos + to, A.t.sin + to, ok, y[2 * g + h]);
+    }
+    if (!place()) return;
+    if (fresh) {
 #pragma unroll
       for (int g = 0; g < 2 * NG; ++g)
 #pragma unroll
         for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(y[g][i]));
     }
-    const float scale = fmaxf(kv8_scale(wave_max(amax)), s_old), inv = 1.0f / scale;
+    const float scale = fmaxf(kv8_scale(wave_max_dpp(amax)), s_old), inv = 1.0f / scale;
     if (fresh) {
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
@@ -180,11 +210,12 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
         for (int d = 0; d < DV; ++d) y[i][d] = 0.f;
       }
     }
+    if (!place()) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int d = 0; d < DV; ++d) amax = fmaxf(amax, finite_abs(y[i][d]));
-    const float scale = fmaxf(kv8_scale(wave_max(amax)), s_old), inv = 1.0f / scale;
+    const float scale = fmaxf(kv8_scale(wave_max_dpp(amax)), s_old), inv = 1.0f / scale;
     const bool grown = first > 0 && scale > s_old;
     uint32_t fresh = 0, stay = 0;             // byte masks of the lane's tokens
 #pragma unroll
@@ -262,9 +293,9 @@ hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, Head
   if (b.rows <= 0 || b.n_seqs <= 0) return hipSuccess;
   if (c.hd != 64 && c.hd != 128) return hipErrorInvalidValue;
   const int64_t items = b.seq_off ? (int64_t)b.rows / 16 + 2 * (int64_t)b.n_seqs : b.n_seqs;
-  const AppendArgs a{c, b, k, v, q, q_out, n_q, t, items * c.n_kv * 2};
-  const int64_t grid = (a.blocks + (q.p ? b.rows : 0) + 3) / 4;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t blocks = items * c.n_kv * 2, grid = (blocks + (q.p ? b.rows : 0) + 3) / 4;
+  if (grid > (1 << 29)) return hipErrorInvalidValue;   // items are numbered in 32 bits
+  const AppendArgs a{c, b, k, v, q, q_out, n_q, t, (unsigned)blocks};
   // whole 16-byte pieces: keys are turned 8 dims at a time
   const bool vec = views_vector(dtype, k) && views_vector(dtype, v) && views_vector(dtype, HeadView{q_out.p, q_out.row, q_out.head}) &&
                    views_vector(dtype, q) && (t.layout ? (2 * t.pairs) % 8 == 0 : t.pairs % 8 == 0) &&
