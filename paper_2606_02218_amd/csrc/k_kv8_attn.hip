@@ -405,51 +405,54 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   const int wblk = BOTH ? wave >> 1 : wave & 1;
   const int piece = tid & (HD - 1);             // of the block
   const int last_blk = (max(c1, 1) - 1) >> 4;
-  u32x4_t kr, vr;
-  float ksr = 1.f, vsr = 1.f;
-  int id, lost;
+  struct Load { u32x4_t k, v; float ks, vs; int id; };
+  // Pieces in flight: two where two workgroups a CU leave the registers for it (fp32
+  // runs 90 -> 86 us), one where a second set would spill (649 -> 730).
+  constexpr int DEPTH = OUT == OUT_BF16 ? 1 : 2;
+  Load ld[DEPTH];
+  int id;
   auto list = [&](int t0) {
     id = __builtin_amdgcn_readfirstlane(kv8_block(A.c, tab, A.b.tab_stride, min((t0 >> 4) + wblk, last_blk), kvh));
   };
-  auto fetch = [&]() {
+  auto fetch = [&](Load& x) {
     const int b = max(id, 0);
     const int64_t at = (int64_t)b * BLK + piece * 16;
     if (has_k) {
-      kr = *reinterpret_cast<const u32x4_t*>(A.c.k + at);
-      ksr = A.c.k_scale[b];
+      x.k = *reinterpret_cast<const u32x4_t*>(A.c.k + at);
+      x.ks = A.c.k_scale[b];
     }
     if (has_v) {
-      vr = *reinterpret_cast<const u32x4_t*>(A.c.v + at);
-      vsr = A.c.v_scale[b];
+      x.v = *reinterpret_cast<const u32x4_t*>(A.c.v + at);
+      x.vs = A.c.v_scale[b];
     }
-    lost = id;
+    x.id = id;
   };
-  auto stash = [&](int buf, int t0) {
-    if (lost < 0) {                 // a page the pool has not: its keys are NaN, its values 0
-      kr = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
-      vr = u32x4_t{0, 0, 0, 0};
+  auto stash = [&](Load& x, int buf, int t0) {
+    if (x.id < 0) {                 // a page the pool has not: its keys are NaN, its values 0
+      x.k = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
+      x.v = u32x4_t{0, 0, 0, 0};
     }
     if (has_k) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         sK[buf][2 * (piece >> 4) + e][16 * wblk + (piece & 15)] =
-            __builtin_bit_cast(u32x4_t, kv8_bf16x8(kr[2 * e], kr[2 * e + 1], ksr, ksr));
+            __builtin_bit_cast(u32x4_t, kv8_bf16x8(x.k[2 * e], x.k[2 * e + 1], x.ks, x.ks));
     }
     if (has_v) {
       if (t0 + 32 > whole) {        // some rows do not see all of these tokens: 0 * NaN must not reach them
         bool nan = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          nan |= has_nan_code(vr[e]);
-          vr[e] = clear_nan(vr[e]);
+          nan |= has_nan_code(x.v[e]);
+          x.v[e] = clear_nan(x.v[e]);
         }
         const bool any = __any(nan);
         if (lane == 0) sNan[buf][wave] = any;
       }
-      const int tg = piece / (HD / 4), x = piece % (HD / 4);   // tokens 4 tg .., dims 4 x ..
+      const int tg = piece / (HD / 4), x4 = piece % (HD / 4);   // tokens 4 tg .., dims 4 x4 ..
 #pragma unroll
       for (int d = 0; d < 4; ++d)
-        reinterpret_cast<u32x2_t*>(&sV[buf][wblk][tg & 1][d % DT][(4 * x + d) / DT])[tg >> 1] = kv8_bf16x4(vr[d], vsr);
+        reinterpret_cast<u32x2_t*>(&sV[buf][wblk][tg & 1][d % DT][(4 * x4 + d) / DT])[tg >> 1] = kv8_bf16x4(x.v[d], x.vs);
     }
   };
   // NaN values among the 32 tokens of a piece: those that a column does see make
@@ -552,21 +555,27 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   };
 
   if (c0 < c1) {
-    list(c0);
-    fetch();
-    list(c0 + 32);
-    int buf = 0;
-    for (int t0 = c0; t0 < c1; t0 += 32, buf ^= 1) {
-      stash(buf, t0);
+    auto turn = [&](Load& x, int buf, int t0) {
+      stash(x, buf, t0);
       __syncthreads();              // the piece is in LDS; the other buffer is free
-      if (t0 + 32 < c1) {
-        fetch();
-        list(t0 + 64);
+      if (t0 + 32 * DEPTH < c1) {
+        fetch(x);
+        list(t0 + 32 * DEPTH + 32);
       }
       if (active && t0 < wmax) {
         if (t0 + 32 <= whole) block(std::false_type{}, buf, t0);
         else block(std::true_type{}, buf, t0);
       }
+    };
+    list(c0);
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      fetch(ld[i]);
+      list(c0 + 32 * i + 32);
+    }
+    for (int t0 = c0; t0 < c1; t0 += 64) {
+      turn(ld[0], 0, t0);
+      if (t0 + 32 < c1) turn(ld[DEPTH - 1], 1, t0 + 32);
     }
   }
   if (!active) return;
