@@ -127,12 +127,12 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
   if (p0 < 0) { r0 -= p0; p0 = 0; }           // padding rows come first
   if (len <= p0) return;
   const int blk = (p0 >> 4) + (x - key);
-  if (blk * 16 >= len) return;
-  // The chain to the block's address and old scale (table row, page, scale) runs
-  // beside the rows' own loads: its indexes are clipped rather than branched on.
+  if (blk > (len - 1) >> 4) return;
+  // The chain to the block's address and old scale (page, scale) runs beside the
+  // rows' own loads; positions past the table end here.
   const int tr = b.tab_row ? b.tab_row[s] : s, slot = blk >> A.c.sub_shift;
-  const bool on_table = (unsigned)tr < (unsigned)b.tab_rows && slot < b.tab_stride;
-  const int page = b.tab[on_table ? (int64_t)tr * b.tab_stride + slot : 0];
+  if ((unsigned)tr >= (unsigned)b.tab_rows || slot >= b.tab_stride) return;
+  const int page = b.tab[(int64_t)tr * b.tab_stride + slot];
   const int first = max(p0 - blk * 16, 0), last = min(len - blk * 16, 16);   // the block's new tokens
   const int64_t row0 = (int64_t)r0 + (blk * 16 - p0);                        // row of the block's token 0
   int id = -1;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
   float* sp = nullptr;
   uint8_t* out = nullptr;
   auto place = [&]() {                        // false: no such page, nothing to write to
-    if (!on_table || (unsigned)page >= (unsigned)A.c.pages) return false;
+    if ((unsigned)page >= (unsigned)A.c.pages) return false;
     id = ((page * A.c.n_kv + kvh) << A.c.sub_shift) + (blk & ((1 << A.c.sub_shift) - 1));
     sp = (values ? A.c.v_scale : A.c.k_scale) + id;
     out = (values ? A.c.v : A.c.k) + (int64_t)id * (16 * HD);

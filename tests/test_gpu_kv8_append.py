@@ -185,6 +185,12 @@ def test_padding_rows_foreign_rows_and_lost_pages():
         rg.kv8_append(b.cache, one, one, dev(t), dev(np.array(ln, np.int64).astype(np.int32)),
                       tab_row=None if tr is None else dev(np.array(tr, np.int64).astype(np.int32)))
         _same(b.snapshot(), before)
+    # runs that end at the largest length there is: no page holds them
+    rg.kv8_append(b.cache, one, one, dev(np.array([[0, 0]] * 2, np.int32)), dev(np.array([2 ** 31 - 1, 2 ** 31 - 16], np.int32)),
+                  offsets([3, 1]))
+    many = dev(np.repeat(k[:4], 30, 0), BF16)
+    rg.kv8_append(b.cache, many, many, dev(np.array([[0, 0]], np.int32)), dev(np.array([2 ** 31 - 1], np.int32)), offsets([120]))
+    _same(b.snapshot(), before)
     # offsets out of order or out of range reach no row outside the call's
     for off in ([0, 9, 3, 2, 4], [-7, 0, 2, 2, 100], [50, 60, 70, 80, 90]):
         rg.kv8_append(b.cache, one, one, dev(tab), dev(np.array([1, 1, 1, 1], np.int32)), dev(np.array(off, np.int32)),
