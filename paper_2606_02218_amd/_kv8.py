@@ -10,6 +10,7 @@ from ._lib import _check, _dev, _gpu, load_library
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {None: 0, "linear": 1, "base": 2, "bands": 3}
+_MOST = 2 ** 31 - 1     # sizes are int32 in the library; or-ed together, all are at most this or the result is more
 
 
 class rg_kv8_cache(C.Structure):
@@ -78,6 +79,8 @@ def _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev):
         return None
     n = seq_len.shape[0]
     tab_rows, stride = page_tab.shape
+    if rows | n | tab_rows | stride > _MOST:
+        return None
     off = row = 0
     if seq_off is not None:
         if not (_plain(seq_off, _I32, dev) and seq_off.shape == (n + 1,)):
@@ -99,7 +102,7 @@ def _table_fits(cos, sin, hd, dev):
     if not (_plain(cos, _F32, dev) and _plain(sin, _F32, dev)):
         return 0
     shape = cos.shape
-    if len(shape) != 2 or sin.shape != shape or shape[0] < 1 or not 2 <= 2 * shape[1] <= hd:
+    if len(shape) != 2 or sin.shape != shape or shape[0] < 1 or shape[0] > _MOST or not 2 <= 2 * shape[1] <= hd:
         return 0
     return 2 * shape[1]
 
@@ -140,6 +143,12 @@ def _empty(like, shape, dtype, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _sizes(**sizes):
+    for name, n in sizes.items():
+        if n > _MOST:
+            raise ValueError(f"{name} must be below 2^31, got {n}")
 
 
 def _view(name, t, dtype, shape):
@@ -192,6 +201,7 @@ def _tables(cos, sin, head_dim, layout):
     _dev("cos", cos, torch.float32, ndim=2)
     _dev("sin", sin, torch.float32, tuple(cos.shape))
     rot = 2 * int(cos.shape[1])
+    _sizes(positions=cos.shape[0])
     if cos.shape[0] < 1 or not 2 <= rot <= head_dim:
         raise ValueError(f"a table of {tuple(cos.shape)} does not fit head_dim {head_dim}")
     return rot
@@ -209,6 +219,7 @@ def rope_table(n_pos: int, rot_dim: int, theta: float = 1e4, scaling: Optional[s
     n_pos, rot_dim = int(n_pos), int(rot_dim)
     if n_pos < 1 or rot_dim < 2 or rot_dim % 2:
         raise ValueError(f"need n_pos >= 1 and an even rot_dim >= 2, got {n_pos} and {rot_dim}")
+    _sizes(n_pos=n_pos, rot_dim=rot_dim)
     device = torch.device(device)
     if device.type != "cuda":
         raise TypeError(f"tables are made in GPU memory, got device {device}")
@@ -236,7 +247,7 @@ def rope(x, pos, cos, sin, layout: str = "half", inverse: bool = False, out=None
         if (dt is _BF16 or dt is _F32) and dev >= 0 and x.dim() == 3:
             rows, heads, hd = x.shape
             a, b, one = x.stride()
-            if one == 1 and hd % 2 == 0 and _plain(pos, _I32, dev) and pos.shape == (rows,) and _here(dev):
+            if one == 1 and hd % 2 == 0 and rows | heads | hd <= _MOST and _plain(pos, _I32, dev) and pos.shape == (rows,) and _here(dev):
                 rot = _table_fits(cos, sin, hd, dev)
                 if rot:
                     y = _torch.empty((rows, heads, hd), dtype=dt, device=x.device)
@@ -249,6 +260,7 @@ def rope(x, pos, cos, sin, layout: str = "half", inverse: bool = False, out=None
     dt, code = _float_type("x", x)
     rows, heads, hd = x.shape
     _view("x", x, dt, x.shape)
+    _sizes(rows=rows, heads=heads, head_dim=hd)
     if hd < 2 or hd % 2:
         raise ValueError(f"head_dim must be even, got {hd}")
     rot = _tables(cos, sin, hd, layout)
@@ -306,6 +318,7 @@ def _batch_args(rows, page_tab, seq_len, seq_off, tab_row):
     _dev("page_tab", page_tab, torch.int32, ndim=2)
     _dev("seq_len", seq_len, torch.int32, ndim=1)
     n = seq_len.shape[0]
+    _sizes(rows=rows, sequences=n, **{"page_tab's rows": page_tab.shape[0], "page_tab's pages": page_tab.shape[1]})
     if seq_off is not None:
         _dev("seq_off", seq_off, torch.int32, (n + 1,))
     elif n != rows:
@@ -360,7 +373,7 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
                 if ok:
                     q0, n_q, qd = q.shape
                     qr, qh, q1 = q.stride()
-                    ok = q0 == rows and qd == hd and q1 == 1 and n_q > 0 and n_q % n_kv == 0
+                    ok = q0 == rows and qd == hd and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0
                 if ok:
                     y = _torch.empty((rows, n_q, hd), dtype=dt, device=q.device)
                     qp, yp = q.data_ptr(), y.data_ptr()
@@ -385,6 +398,7 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
         if _float_type("q", q)[0] != dt:
             raise TypeError(f"q must have dtype {dt}, got {q.dtype}")
         n_q = q.shape[1]
+        _sizes(heads=n_q)
         _view("q", q, dt, (rows, n_q, c.head_dim))
         if n_q < 1 or n_q % c.n_kv:
             raise ValueError(f"q must have a multiple of {c.n_kv} heads, got {n_q}")
@@ -424,7 +438,7 @@ def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[i
             qr, qh, q1 = q.stride()
             n_kv = c.n_kv
             b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
-            if b is not None and hd == c.head_dim and q1 == 1 and n_q > 0 and n_q % n_kv == 0:
+            if b is not None and hd == c.head_dim and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0:
                 bound = max(1, b.tab_stride * c.page_tokens) if max_len is None else int(max_len)
                 if 1 <= bound <= 1 << 30:
                     y = _torch.empty((rows, n_q, hd), dtype=dt, device=q.device)
@@ -442,6 +456,7 @@ def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[i
     dt, code = _float_type("q", q)
     c = _cache_args(cache)
     rows, n_q, hd = q.shape
+    _sizes(heads=n_q)
     _view("q", q, dt, (rows, n_q, c.head_dim))
     if n_q < 1 or n_q % c.n_kv:
         raise ValueError(f"q must have a multiple of {c.n_kv} heads, got {n_q}")

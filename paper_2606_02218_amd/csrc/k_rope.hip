@@ -19,8 +19,8 @@ template <typename T, int VEC, int LAYOUT>
 __global__ __launch_bounds__(256) void k_rope(const T* x, int64_t x_row, int64_t x_head, T* y, int64_t y_row,
                                               int64_t y_head, const int32_t* __restrict__ pos, int rows, int heads,
                                               int hd, RopeTable t, float sign) {
-  const int r = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-  if (r >= rows) return;
+  const unsigned r = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (r >= (unsigned)rows) return;
   rope_row<T, VEC, LAYOUT>(x + r * x_row, x_head, y + r * y_row, y_head, heads, hd, t, pos[r], sign, threadIdx.x & 63);
 }
 
@@ -56,7 +56,7 @@ hipError_t launch_rope_table(float* co, float* si, int n_pos, const RopeFreqs& f
 hipError_t launch_rope(int dtype, HeadView x, HeadOut y, const int32_t* pos, int rows, int heads, int hd,
                        const RopeTable& t, bool inverse, hipStream_t st) {
   if (rows <= 0 || heads <= 0) return hipSuccess;
-  const dim3 grid((unsigned)((rows + 3) / 4));
+  const dim3 grid(((unsigned)rows + 3) / 4);
   const float sign = inverse ? -1.f : 1.f;
   const bool vec = rope_vectors(dtype, x, hd, t) && rope_vectors(dtype, HeadView{y.p, y.row, y.head}, hd, t);
 #define RG_ROPE(T, VEC, LAY)                                                                                        \

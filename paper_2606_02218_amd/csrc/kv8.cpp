@@ -1,7 +1,7 @@
 // C entry points of the rotary positions and the 8-bit key/value cache
 // (include/rollout.h): argument checks, then the launchers.
 #include <cmath>
-#include <string>
+#include <cstdio>
 
 #include "rollout.h"
 #include "rg_kernels.h"
@@ -11,7 +11,9 @@ int rg_set_error(int code, const char* msg);
 namespace {
 
 int bad(const char* who, const char* what, int code = RG_EINVAL) {
-  return rg_set_error(code, (std::string(who) + ": " + what).c_str());
+  char msg[160];
+  std::snprintf(msg, sizeof msg, "%s: %s", who, what);
+  return rg_set_error(code, msg);
 }
 
 int launched(const char* who, hipError_t e) {

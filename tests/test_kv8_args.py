@@ -60,6 +60,26 @@ def test_rope_refuses():
         rg.rope_table(8, 64, device="cpu")
 
 
+def test_sizes_past_the_librarys_integers():
+    """A size of 2^31 is refused, not wrapped (views without storage: nothing of that size is allocated)."""
+    import paper_2606_02218_amd as rg
+    many, one, cos = 2 ** 31 + 3, torch.zeros(1, dtype=I32), torch.zeros(8, 32)
+    for x in (_zeros(1, 1, 64).expand(many, 1, 64), _zeros(1, 1, 64).expand(1, many, 64)):
+        with pytest.raises(ValueError, match="below 2\\^31"):
+            rg.rope(x, one, cos, cos)
+    with pytest.raises(ValueError, match="below 2\\^31"):
+        rg.rope_table(many, 64)
+    cache = rg.Kv8Cache.empty(4, 2, 64, device="cpu")
+    tab = torch.zeros(1, 1, dtype=I32)
+    kv = _zeros(1, 2, 64).expand(many, 2, 64)
+    with pytest.raises(ValueError, match="below 2\\^31"):
+        rg.kv8_append(cache, kv, kv, tab, one)
+    with pytest.raises(ValueError, match="below 2\\^31"):
+        rg.kv8_attention(cache, kv, tab, one)
+    with pytest.raises(ValueError, match="below 2\\^31"):
+        rg.kv8_attention(cache, _zeros(1, 1, 64).expand(1, 2 * many, 64), tab, one)
+
+
 def test_append_refuses():
     import paper_2606_02218_amd as rg
     c, k = _cache(), _zeros(3, 2, 64)
