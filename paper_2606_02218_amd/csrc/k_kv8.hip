@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
   if (b.seq_off) s = kv8_find(b, x, 16, 2, key);
   kv8_seq_rows(b, s, r0, n);
   if (n <= 0) return;
-  const int len = b.seq_len[s] + b.len_add;
+  const int len = kv8_len(b, s);
   int p0 = len - n;                           // position of row r0
   if (p0 < 0) { r0 -= p0; p0 = 0; }           // padding rows come first
   if (len <= p0) return;

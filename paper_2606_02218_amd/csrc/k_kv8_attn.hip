@@ -106,7 +106,8 @@ __device__ __forceinline__ float* part_ml(const Kv8Attn& A, int64_t slot, int he
 
 // ---------------------------------------------------------------- rows pass
 template <typename T, int HD, int OUT, int W>
-__global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / W) void k_kv8_rows(Kv8Attn A, int htiles, int per_xcd, int items) {
+__global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / W) void k_kv8_rows(
+    Kv8Attn A, int htiles, int per_xcd, int items) {
   constexpr int QP = q_pieces(OUT), PP = p_pieces(OUT, false);
   constexpr int NJ = HD / 64;       // 16-byte loads of a block per lane
   constexpr int LDO = HD + 4;
@@ -242,11 +243,11 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
     }
     float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])),
                      fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3]))) * sc;
-    if (i == 0 || __any(mx > m + KV8_SLACK)) {
+    if (__any(mx > m + KV8_SLACK)) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       const float mn = fmaxf(m, mx);
-      const float alpha = i == 0 ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      const float alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);   // -inf: only scores past fp32's range so far
       l *= alpha;
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
@@ -254,12 +255,13 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
         for (int e = 0; e < 4; ++e) o[j][e] *= alpha;
       m = mn;
     }
+    const float ms = m == -INFINITY ? 0.f : m;   // then every score is -inf and its probability 0
     float p[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        p[4 * h + e] = __builtin_amdgcn_exp2f(fmaf(st[h][e], sc, -m));
+        p[4 * h + e] = __builtin_amdgcn_exp2f(fmaf(st[h][e], sc, -ms));
         l += p[4 * h + e];
       }
     bf16x8_t pf[PP];
@@ -299,7 +301,7 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
     float L = 0.f;
     f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
     for (int w = 0; w < nw; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sM[w][h] - M);
+      const float f = sM[w][h] == M ? 1.f : __builtin_amdgcn_exp2f(sM[w][h] - M);
       L += f * sL[w][h];
       acc += f * *reinterpret_cast<const f32x4_t*>(&sO[w][h][d]);
     }
@@ -363,7 +365,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   const int skip = (k - key) * np;  // rows of the sequence before the tile
   const int nr = min(np, n - skip);
   if (nr <= 0) return;
-  const int pos0 = A.b.seq_len[s] + A.b.len_add - n + skip;   // position of the tile's first row
+  const int pos0 = kv8_len(A.b, s) - n + skip;   // position of the tile's first row
   r0 += skip;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c32 = lane & 31, hh = lane >> 5;
@@ -731,7 +733,8 @@ Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_
 
 hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStream_t st) {
   if (a.b.rows <= 0 || a.b.n_seqs <= 0) return hipSuccess;
-  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.n_split > KV8_MAX_SPLIT || a.plan.chunk % 64 || (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
+  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.n_split > KV8_MAX_SPLIT || a.plan.chunk % 64 ||
+      (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
     return hipErrorInvalidValue;
   const bool w = a.c.hd == 128;
   if (planes && dtype != 0) return hipErrorInvalidValue;

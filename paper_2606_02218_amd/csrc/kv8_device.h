@@ -57,13 +57,16 @@ __device__ __forceinline__ int kv8_find(const Kv8Rows& b, int x, int span, int p
   return lo;
 }
 
+// Tokens of sequence s, this call's rows counted; a length below zero is none.
+__device__ __forceinline__ int kv8_len(const Kv8Rows& b, int s) { return max(b.seq_len[s] + b.len_add, 0); }
+
 // Row r of batch b: its sequence and position there (negative: a padding row).
 // False for rows of no sequence.
 __device__ __forceinline__ bool kv8_row(const Kv8Rows& b, int r, int& s, int& pos) {
   if (!b.seq_off) {
     s = r;
     if (r >= (b.d_rows ? *b.d_rows : b.rows)) return false;
-    pos = b.seq_len[s] + b.len_add - 1;
+    pos = kv8_len(b, s) - 1;
     return true;
   }
   int key;
@@ -71,7 +74,7 @@ __device__ __forceinline__ bool kv8_row(const Kv8Rows& b, int r, int& s, int& po
   int r0, n;
   kv8_seq_rows(b, s, r0, n);
   if (r < r0 || r >= r0 + n) return false;
-  pos = b.seq_len[s] + b.len_add - (r0 + n - r);
+  pos = kv8_len(b, s) - (r0 + n - r);
   return true;
 }
 

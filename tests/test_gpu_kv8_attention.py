@@ -372,3 +372,124 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(o, want[i]) for o in outs[i])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hd,n,dead", [(64, 200, 70), (128, 200, 33), (128, 3000, 2100), (64, 2500, 1), (64, 90, 90)])
+def test_scores_past_the_range(dtype, hd, n, dead):
+    """Scores that overflow to -inf have no weight, whichever steps, waves and chunks they fill; a row with no others
+    is NaN, as a softmax over nothing."""
+    import paper_2606_02218_amd as rg
+    b = Batch([0], 2, hd, 16, capacity=n, seed=40)
+    k = rounded(b.rng.normal(size=(n, 2, hd)), BF16)
+    k[:, :, 0] = np.where(np.arange(n) < dead, 100.0, 0.0)[:, None]
+    b.k[0].append(k)
+    b.v[0].append(rounded(b.rng.normal(size=(n, 2, hd)), BF16))
+    b.write()
+    keys, values = b.k[0].values(), b.v[0].values()
+    assert np.all(keys[:dead, :, 0] > 90) and np.all(keys[dead:, :, 0] == 0)
+    for new in (1, 30):
+        q = rounded(b.rng.normal(size=(new, 6, hd)), dtype)
+        q[:, :, 0] = rounded(np.full((new, 6), -3e37), dtype)         # -3e37 * 90 < -3.4e38
+        out = host(rg.kv8_attention(b.cache, dev(q, dtype), dev(b.tab), dev(b.lengths()), offsets([new]), max_len=n))
+        pos = np.arange(n - new, n) - dead
+        lost = pos < 0
+        assert np.all(np.isnan(out[lost]))
+        if not lost.all():
+            ref, mass, reach = kv8.attend(q[~lost], keys[dead:], values[dead:], pos[~lost], hd ** -0.5)
+            bound = attention_bound(ref, mass, reach, hd, n, hd ** -0.5, dtype, _p_step(dtype, new > 3))
+            assert np.all(np.abs(out[~lost] - ref) <= bound)
+
+
+def test_lengths_below_zero_hold_nothing():
+    """As a length of zero, in single rows and runs, to the smallest integer."""
+    import paper_2606_02218_amd as rg
+    b = Batch([40, 60, 50], 2, 64, 16, seed=41)
+    for dtype in (BF16, F32):
+        for new in ([1, 1, 1], [20, 9, 5]):
+            n = sum(new)
+            off = None if n == 3 else offsets(new)
+            x = dev(rounded(b.rng.normal(size=(n, 4, 64)), dtype), dtype)
+            rows = slice(new[0], new[0] + new[1])
+            want = rg.kv8_attention(b.cache, x, dev(b.tab), dev(b.lengths()), off)
+            want[rows] = 0
+            for low in (0, -1, -7, -2 ** 31 + 3, -2 ** 31):
+                ln = dev(np.array([40, low, 50], np.int32))
+                assert torch.equal(rg.kv8_attention(b.cache, x, dev(b.tab), ln, off), want), low
+                before = b.snapshot()
+                rg.kv8_append(b.cache, x[:, :2], x[:, 2:], dev(b.tab), dev(np.full(3, low, np.int32)), off)
+                assert all(np.array_equal(a, c) for a, c in zip(b.snapshot(), before)), low
+
+
+@pytest.mark.parametrize("page", [256, 1024])
+@pytest.mark.parametrize("new", [1, 50])
+def test_large_pages(page, new):
+    """Pages of many blocks, lengths that end inside one and at its end; sizes given as other integers."""
+    import paper_2606_02218_amd as rg
+    for n in (page - 1, page, page + 1, 2 * page):
+        b = Batch([n, 70], 2, 64, page, capacity=2 * page, seed=42)
+        q = rounded(b.rng.normal(size=(2 * new, 8, 64)), BF16)
+        out = rg.kv8_attention(b.cache, dev(q, BF16), dev(b.tab), dev(b.lengths()), offsets([new, new]),
+                               max_len=np.int64(2 * page))
+        _check(b, q, [new, new], out, BF16, 64 ** -0.5, new > 3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_captured_runs(dtype):
+    """A prompt's piece appended and attended to in a graph, contexts in chunks, replayed with eager work between."""
+    import paper_2606_02218_amd as rg
+    b = Batch([1500, 200], 2, 128, 16, capacity=1700, seed=43)
+    assert rg.load_library().rg_kv8_attention_scratch(8, 2, 128, 60, 2, 1, 1700) > 0
+    x = torch.zeros(60, 12, 128, dtype=dtype, device="cuda")
+    tab, off, ln = dev(b.tab), offsets([40, 20]), dev(b.lengths())
+    cos, sin = rg.rope_table(1700, 128)
+
+    def step():
+        q = rg.kv8_append(b.cache, x[:, 8:10], x[:, 10:], tab, ln, off, q=x[:, :8], cos=cos, sin=sin)
+        return rg.kv8_attention(b.cache, q, tab, ln, off, max_len=1700)
+
+    def put(to):
+        for t, k in zip(b.cache, to):
+            t.view(torch.uint8).copy_(k.view(torch.uint8))
+
+    keep = [t.clone() for t in b.cache]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for i in range(4):
+        put(keep)
+        x.copy_(dev(b.rng.normal(size=(60, 12, 128)).astype(np.float32), dtype))
+        ln.copy_(dev(b.lengths() + 5 * i))
+        want = step().clone()
+        cache = [t.clone() for t in b.cache]
+        torch.cuda.synchronize()
+        put(keep)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.all(out.isfinite())
+        for t, k in zip(b.cache, cache):
+            assert torch.equal(t.view(torch.uint8), k.view(torch.uint8))
+
+
+def test_a_whole_step_on_a_given_stream():
+    """rope_table, append and attention on a stream of the caller's, the results used there."""
+    import paper_2606_02218_amd as rg
+    b = Batch([2500, 30], 2, 64, 16, capacity=2600, seed=44)
+    x = dev(b.rng.normal(size=(2, 12, 64)).astype(np.float32), BF16)
+    ln = dev(b.lengths() + 1)
+    keep = [t.clone() for t in b.cache]
+    tab, got = dev(b.tab), []
+    for stream in (None, torch.cuda.Stream()):
+        for t, k in zip(b.cache, keep):
+            t.view(torch.uint8).copy_(k.view(torch.uint8))
+        torch.cuda.synchronize()
+        cos, sin = rg.rope_table(2600, 64, stream=stream)
+        q = rg.kv8_append(b.cache, x[:, 8:10], x[:, 10:], tab, ln, q=x[:, :8], cos=cos, sin=sin, stream=stream)
+        got.append(rg.kv8_attention(b.cache, q, tab, ln, max_len=2600, stream=stream))
+        torch.cuda.synchronize()
+    assert torch.equal(*got)
