@@ -3,6 +3,7 @@ include/rollout.h.  No computation happens here."""
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import NamedTuple, Optional
 
 from . import _lib
@@ -23,14 +24,18 @@ class rg_kv8_batch(C.Structure):
                 ("seq_off", C.c_void_p), ("seq_len", C.c_void_p), ("n_seqs", C.c_int32), ("rows", C.c_int32)]
 
 
+# The same two as bytes: a call that passes in few questions packs them in a
+# fraction of the time that filling a ctypes structure takes.
+_CACHE, _BATCH = struct.Struct("@4Pq3i4x").pack, struct.Struct("@P2i3P2i").pack
+
 _P, _I, _L, _D = C.c_void_p, C.c_int32, C.c_int64, C.c_double
 _ARGS = {
     "rg_rope_table": ([_P, _P, _I, _I, _D, _I, _D, _D, _D, _D, _P], C.c_int),
     "rg_rope": ([_I, _P, _L, _L, _P, _L, _L, _P, _I, _I, _I, _P, _P, _I, _I, _I, _I, _P], C.c_int),
-    "rg_kv8_append": ([C.POINTER(rg_kv8_cache), C.POINTER(rg_kv8_batch), _I, _P, _L, _L, _P, _L, _L, _P, _L, _L, _P, _L, _L,
+    "rg_kv8_append": ([_P, _P, _I, _P, _L, _L, _P, _L, _L, _P, _L, _L, _P, _L, _L,
                        _I, _P, _P, _I, _I, _I, _P], C.c_int),
     "rg_kv8_attention_scratch": ([_I, _I, _I, _I, _I, _I, _I], C.c_int64),
-    "rg_kv8_attention": ([C.POINTER(rg_kv8_cache), C.POINTER(rg_kv8_batch), _I, _P, _L, _L, _I, _P, C.c_float, _I, _P, _L, _P],
+    "rg_kv8_attention": ([_P, _P, _I, _P, _L, _L, _I, _P, C.c_float, _I, _P, _L, _P],
                          C.c_int),
 }
 _ready = None
@@ -60,7 +65,7 @@ def _plain(t, dtype, dev):
 
 
 def _cache_fits(cache, dev):
-    """The struct of a cache whose tensors are all in place, or None."""
+    """(rg_kv8_cache as bytes, n_kv, head_dim, page_tokens) of a cache whose tensors are all in place, or None."""
     k, v, ks, vs = cache
     if not (_plain(k, _E4M3, dev) and _plain(v, _E4M3, dev) and _plain(ks, _F32, dev) and _plain(vs, _F32, dev)):
         return None
@@ -70,11 +75,12 @@ def _cache_fits(cache, dev):
     pages, n_kv, parts, n = shape
     if ks.shape != vs.shape or ks.shape != shape[:3]:
         return None
-    return rg_kv8_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, n_kv, n // 16, 16 * parts)
+    hd, page = n // 16, 16 * parts
+    return _CACHE(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, n_kv, hd, page), n_kv, hd, page
 
 
 def _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev):
-    """The struct of a batch whose tensors are all in place, or None."""
+    """(rg_kv8_batch as bytes, sequences, pages of a table row) where a batch's tensors are all in place, or None."""
     if not (_plain(page_tab, _I32, dev) and _plain(seq_len, _I32, dev) and page_tab.dim() == 2 and seq_len.dim() == 1):
         return None
     n = seq_len.shape[0]
@@ -94,7 +100,7 @@ def _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev):
         row = tab_row.data_ptr()
     elif tab_rows < n:
         return None
-    return rg_kv8_batch(page_tab.data_ptr(), tab_rows, stride, row, off, seq_len.data_ptr(), n, rows)
+    return _BATCH(page_tab.data_ptr(), tab_rows, stride, row, off, seq_len.data_ptr(), n, rows), n, stride
 
 
 def _table_fits(cos, sin, hd, dev):
@@ -250,7 +256,7 @@ def rope(x, pos, cos, sin, layout: str = "half", inverse: bool = False, out=None
             if one == 1 and hd % 2 == 0 and rows | heads | hd <= _MOST and _plain(pos, _I32, dev) and pos.shape == (rows,) and _here(dev):
                 rot = _table_fits(cos, sin, hd, dev)
                 if rot:
-                    y = _torch.empty((rows, heads, hd), dtype=dt, device=x.device)
+                    y = x.new_empty((rows, heads, hd))
                     rc = lib.rg_rope(1 if dt is _BF16 else 0, x.data_ptr(), a, b, y.data_ptr(), heads * hd, hd,
                                      pos.data_ptr(), rows, heads, hd, cos.data_ptr(), sin.data_ptr(), cos.shape[0], rot,
                                      lay, 1 if inverse else 0, _torch._C._cuda_getCurrentRawStream(dev))
@@ -350,10 +356,12 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
         lay = ROPE_LAYOUTS.get(layout)
         c = _cache_fits(cache, dev) if (dt is _BF16 or dt is _F32) and dev >= 0 and lay is not None and _here(dev) else None
         if c is not None:
-            rows, n_kv, hd = shape = k.shape
+            c, n_kv, hd, _ = c
+            rows = k.shape[0]
+            shape = (rows, n_kv, hd)
             kr, kh, k1 = k.stride()
             b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
-            ok = (b is not None and n_kv == c.n_kv and hd == c.head_dim and isinstance(v, _torch.Tensor) and
+            ok = (b is not None and k.shape == shape and isinstance(v, _torch.Tensor) and
                   v.dtype is dt and v.get_device() == dev and v.shape == shape)
             rot = n_pos = cp = sp = 0
             if ok and cos is not None:
@@ -375,10 +383,10 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
                     qr, qh, q1 = q.stride()
                     ok = q0 == rows and qd == hd and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0
                 if ok:
-                    y = _torch.empty((rows, n_q, hd), dtype=dt, device=q.device)
+                    y = q.new_empty((rows, n_q, hd))
                     qp, yp = q.data_ptr(), y.data_ptr()
             if ok:
-                rc = lib.rg_kv8_append(C.byref(c), C.byref(b), 1 if dt is _BF16 else 0, k.data_ptr(), kr, kh, v.data_ptr(),
+                rc = lib.rg_kv8_append(c, b[0], 1 if dt is _BF16 else 0, k.data_ptr(), kr, kh, v.data_ptr(),
                                        vr, vh, qp, qr, qh, yp, n_q * hd, hd, n_q, cp, sp, n_pos, rot, lay,
                                        _torch._C._cuda_getCurrentRawStream(dev))
                 if rc:
@@ -434,20 +442,21 @@ def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[i
         dt, dev = q.dtype, q.get_device()
         c = _cache_fits(cache, dev) if (dt is _BF16 or dt is _F32) and dev >= 0 and _here(dev) else None
         if c is not None:
+            c, n_kv, head_dim, page = c
             rows, n_q, hd = q.shape
             qr, qh, q1 = q.stride()
-            n_kv = c.n_kv
             b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
-            if b is not None and hd == c.head_dim and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0:
-                bound = max(1, b.tab_stride * c.page_tokens) if max_len is None else int(max_len)
+            if b is not None and hd == head_dim and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0:
+                b, n_seqs, stride = b
+                bound = max(1, stride * page) if max_len is None else int(max_len)
                 if 1 <= bound <= 1 << 30:
-                    y = _torch.empty((rows, n_q, hd), dtype=dt, device=q.device)
-                    need = lib.rg_kv8_attention_scratch(n_q, n_kv, hd, rows, b.n_seqs, 0 if seq_off is None else 1, bound)
+                    y = q.new_empty((rows, n_q, hd))
+                    need = lib.rg_kv8_attention_scratch(n_q, n_kv, hd, rows, n_seqs, 0 if seq_off is None else 1, bound)
                     scratch, sp = None, 0
                     if need > 0:
                         scratch = _torch.empty(need // 4, dtype=_F32, device=q.device)
                         sp = scratch.data_ptr()
-                    rc = lib.rg_kv8_attention(C.byref(c), C.byref(b), 1 if dt is _BF16 else 0, q.data_ptr(), qr, qh, n_q,
+                    rc = lib.rg_kv8_attention(c, b, 1 if dt is _BF16 else 0, q.data_ptr(), qr, qh, n_q,
                                               y.data_ptr(), hd ** -0.5 if scale is None else float(scale), bound, sp, need,
                                               _torch._C._cuda_getCurrentRawStream(dev))
                     if rc:

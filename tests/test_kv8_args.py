@@ -144,6 +144,12 @@ def _abi():
     return m, lib, cache, batch
 
 
+def test_packed_arguments_are_the_structures():
+    import paper_2606_02218_amd._kv8 as m
+    assert m._CACHE(*range(1, 9)) == bytes(m.rg_kv8_cache(*range(1, 9)))
+    assert m._BATCH(*range(1, 9)) == bytes(m.rg_kv8_batch(*range(1, 9)))
+
+
 @pytest.mark.parametrize("change,code,msg", [
     (dict(k=None), -1, "NULL cache"), (dict(v=8200), -1, "aligned"), (dict(pages=0), -1, "pages"),
     (dict(n_kv=0), -1, "n_kv"), (dict(head_dim=96), -4, "head_dim"), (dict(page_tokens=24), -4, "page_tokens"),
