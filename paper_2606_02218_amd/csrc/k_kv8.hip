@@ -14,8 +14,10 @@
 // a block is shared between waves and no order matters.  Keys: four lanes a
 // token, a 16-dim granule each at a time, stored as the 16 bytes the attention
 // loads.  Values: a lane takes 4 tokens of a few dims, whose codes are the
-// stored dwords.  Queries: a wave a row.  Bound by memory for prompts, by the
-// chain position -> page -> scale -> store for single tokens.
+// stored dwords.  Queries: a wave a row.  Bound by memory for prompts (32 of 512
+// tokens, 4 kv and 28 query heads of 128 in bf16, 294 MB: 58 us, 5.1 TB/s), by the
+// chain position -> page -> scale -> store for single tokens (512 rows of 2 kv and
+// 12 query heads 6.5 us, 8 rows 5.2).
 #include <algorithm>
 
 #include "kv8_device.h"

