@@ -39,18 +39,19 @@ _ARGS = {
                          C.c_int),
 }
 _ready = None
-_torch = _BF16 = _F32 = _E4M3 = _I32 = None
+_BF16 = _F32 = _E4M3 = _I32 = _device = _raw_stream = _empty_like = None
 
 
 def _library():
-    global _ready, _torch, _BF16, _F32, _E4M3, _I32
-    if _ready is None or _ready is not _lib._lib:
+    global _ready, _BF16, _F32, _E4M3, _I32, _device, _raw_stream, _empty_like
+    if _ready is None:
         lib = load_library()
         for name, (args, res) in _ARGS.items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, res
         import torch
-        _torch, _BF16, _F32, _E4M3, _I32 = torch, torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.int32
+        _BF16, _F32, _E4M3, _I32 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.int32
+        _device, _raw_stream, _empty_like = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.empty_like
         _ready = lib
     return _ready
 
@@ -59,21 +60,20 @@ def _library():
 # wrong with an argument takes longer than that to set up.  So each call first asks
 # whether everything is as it should be, in the fewest questions; only where that
 # fails does it go through the checks that say what and raise, or find nothing
-# wrong (another device, a given stream) and go on.
-def _plain(t, dtype, dev):
-    return isinstance(t, _torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()
-
-
+# wrong (another device, a given stream) and go on.  What is no tensor answers the
+# questions with an AttributeError, which is a no.
 def _cache_fits(cache, dev):
     """(rg_kv8_cache as bytes, n_kv, head_dim, page_tokens) of a cache whose tensors are all in place, or None."""
     k, v, ks, vs = cache
-    if not (_plain(k, _E4M3, dev) and _plain(v, _E4M3, dev) and _plain(ks, _F32, dev) and _plain(vs, _F32, dev)):
+    if not (k.dtype is v.dtype is _E4M3 and ks.dtype is vs.dtype is _F32 and
+            k.get_device() == v.get_device() == ks.get_device() == vs.get_device() == dev and
+            k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
         return None
-    shape = k.shape
-    if len(shape) != 4 or v.shape != shape or shape[3] % 16:
+    shape, scales = k.shape, ks.shape
+    if len(shape) != 4 or v.shape != shape or vs.shape != scales:
         return None
     pages, n_kv, parts, n = shape
-    if ks.shape != vs.shape or ks.shape != shape[:3]:
+    if n % 16 or scales != (pages, n_kv, parts):
         return None
     hd, page = n // 16, 16 * parts
     return _CACHE(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, n_kv, hd, page), n_kv, hd, page
@@ -81,7 +81,8 @@ def _cache_fits(cache, dev):
 
 def _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev):
     """(rg_kv8_batch as bytes, sequences, pages of a table row) where a batch's tensors are all in place, or None."""
-    if not (_plain(page_tab, _I32, dev) and _plain(seq_len, _I32, dev) and page_tab.dim() == 2 and seq_len.dim() == 1):
+    if not (page_tab.dtype is seq_len.dtype is _I32 and page_tab.get_device() == seq_len.get_device() == dev and
+            page_tab.is_contiguous() and seq_len.is_contiguous() and page_tab.dim() == 2 and seq_len.dim() == 1):
         return None
     n = seq_len.shape[0]
     tab_rows, stride = page_tab.shape
@@ -89,13 +90,14 @@ def _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev):
         return None
     off = row = 0
     if seq_off is not None:
-        if not (_plain(seq_off, _I32, dev) and seq_off.shape == (n + 1,)):
+        if not (seq_off.dtype is _I32 and seq_off.get_device() == dev and seq_off.is_contiguous() and
+                seq_off.shape == (n + 1,)):
             return None
         off = seq_off.data_ptr()
     elif n != rows:
         return None
     if tab_row is not None:
-        if not (_plain(tab_row, _I32, dev) and tab_row.shape == (n,)):
+        if not (tab_row.dtype is _I32 and tab_row.get_device() == dev and tab_row.is_contiguous() and tab_row.shape == (n,)):
             return None
         row = tab_row.data_ptr()
     elif tab_rows < n:
@@ -104,18 +106,20 @@ def _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev):
 
 
 def _table_fits(cos, sin, hd, dev):
-    """The turned dims of a rotary table that is in place, or 0."""
-    if not (_plain(cos, _F32, dev) and _plain(sin, _F32, dev)):
-        return 0
+    """(turned dims, positions) of a rotary table that is in place, or None."""
+    if not (cos.dtype is sin.dtype is _F32 and cos.get_device() == sin.get_device() == dev and cos.is_contiguous() and
+            sin.is_contiguous()):
+        return None
     shape = cos.shape
-    if len(shape) != 2 or sin.shape != shape or shape[0] < 1 or shape[0] > _MOST or not 2 <= 2 * shape[1] <= hd:
-        return 0
-    return 2 * shape[1]
+    if len(shape) != 2 or sin.shape != shape:
+        return None
+    n, pairs = shape
+    return (2 * pairs, n) if 1 <= n <= _MOST and 2 <= 2 * pairs <= hd else None
 
 
-def _here(dev):
-    """Whether launches go to the device's current stream as things stand."""
-    return _torch._C._cuda_getDevice() == dev
+def _dense(like, shape):
+    """A contiguous tensor of like's type and device."""
+    return _empty_like(like) if like.is_contiguous() else like.new_empty(shape)
 
 
 class _On:
@@ -219,7 +223,7 @@ def rope_table(n_pos: int, rot_dim: int, theta: float = 1e4, scaling: Optional[s
     ``scaling``: None, "linear", "base" or "bands" with ``factor`` (and for
     "bands" the trained ``length``); see rg_rope_table in rollout.h."""
     import torch
-    lib = _library()
+    lib = _ready or _library()
     if scaling not in ROPE_SCALINGS:
         raise ValueError(f"scaling must be one of {list(ROPE_SCALINGS)}")
     n_pos, rot_dim = int(n_pos), int(rot_dim)
@@ -240,29 +244,41 @@ def rope_table(n_pos: int, rot_dim: int, theta: float = 1e4, scaling: Optional[s
     return cos, sin
 
 
+def _rope_now(lib, x, pos, cos, sin, layout, inverse):
+    """The call where every argument is in place, else None."""
+    dt, dev = x.dtype, x.get_device()
+    if not ((dt is _BF16 or dt is _F32) and dev >= 0 and _device() == dev and layout in ROPE_LAYOUTS and x.dim() == 3):
+        return None
+    rows, heads, hd = x.shape
+    a, b, one = x.stride()
+    t = _table_fits(cos, sin, hd, dev)
+    if not (t is not None and one == 1 and hd % 2 == 0 and rows | heads | hd <= _MOST and pos.dtype is _I32 and
+            pos.get_device() == dev and pos.is_contiguous() and pos.shape == (rows,)):
+        return None
+    rot, n_pos = t
+    y = _dense(x, (rows, heads, hd))
+    rc = lib.rg_rope(1 if dt is _BF16 else 0, x.data_ptr(), a, b, y.data_ptr(), heads * hd, hd, pos.data_ptr(), rows,
+                     heads, hd, cos.data_ptr(), sin.data_ptr(), n_pos, rot, ROPE_LAYOUTS[layout], 1 if inverse else 0,
+                     _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return y
+
+
 def rope(x, pos, cos, sin, layout: str = "half", inverse: bool = False, out=None, stream=None):
     """Turns the heads of x (bf16 or fp32 [rows, heads, head_dim], rows and heads
     at any strides) by their rows' positions pos (int32 [rows]); cos and sin are
     a rope_table of at most head_dim dims.  ``inverse=True`` turns back: the
     gradient with respect to x, given the one with respect to the result.
     ``out`` may be x.  See rg_rope in rollout.h."""
-    lib = _library()
-    lay = ROPE_LAYOUTS.get(layout)
-    if isinstance(x, _torch.Tensor) and out is None and stream is None and lay is not None:
-        dt, dev = x.dtype, x.get_device()
-        if (dt is _BF16 or dt is _F32) and dev >= 0 and x.dim() == 3:
-            rows, heads, hd = x.shape
-            a, b, one = x.stride()
-            if one == 1 and hd % 2 == 0 and rows | heads | hd <= _MOST and _plain(pos, _I32, dev) and pos.shape == (rows,) and _here(dev):
-                rot = _table_fits(cos, sin, hd, dev)
-                if rot:
-                    y = x.new_empty((rows, heads, hd))
-                    rc = lib.rg_rope(1 if dt is _BF16 else 0, x.data_ptr(), a, b, y.data_ptr(), heads * hd, hd,
-                                     pos.data_ptr(), rows, heads, hd, cos.data_ptr(), sin.data_ptr(), cos.shape[0], rot,
-                                     lay, 1 if inverse else 0, _torch._C._cuda_getCurrentRawStream(dev))
-                    if rc:
-                        _check(rc)
-                    return y
+    lib = _ready or _library()
+    if out is None and stream is None:
+        try:
+            y = _rope_now(lib, x, pos, cos, sin, layout, inverse)
+        except AttributeError:
+            y = None
+        if y is not None:
+            return y
     dt, code = _float_type("x", x)
     rows, heads, hd = x.shape
     _view("x", x, dt, x.shape)
@@ -338,6 +354,51 @@ def _batch_args(rows, page_tab, seq_len, seq_off, tab_row):
                         seq_len.data_ptr(), n, rows)
 
 
+def _append_now(lib, cache, k, v, page_tab, seq_len, seq_off, q, cos, sin, layout, tab_row):
+    """(True, the result) of the call where every argument is in place, else (False, None)."""
+    no = False, None
+    dt, dev = k.dtype, k.get_device()
+    if not ((dt is _BF16 or dt is _F32) and dev >= 0 and _device() == dev and k.dim() == 3 and layout in ROPE_LAYOUTS):
+        return no
+    rows = k.shape[0]
+    c = _cache_fits(cache, dev)
+    b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
+    if c is None or b is None:
+        return no
+    c, n_kv, hd, _ = c
+    shape = rows, n_kv, hd
+    kr, kh, k1 = k.stride()
+    if not (k.shape == shape and v.dtype is dt and v.get_device() == dev and v.shape == shape and k1 == 1):
+        return no
+    vr, vh, v1 = v.stride()
+    if v1 != 1:
+        return no
+    rot = n_pos = cp = sp = 0
+    if cos is not None:
+        t = _table_fits(cos, sin, hd, dev)
+        if t is None:
+            return no
+        rot, n_pos = t
+        cp, sp = cos.data_ptr(), sin.data_ptr()
+    elif sin is not None:
+        return no
+    y, n_q, qp, qr, qh, yp = None, 0, 0, 0, 0, 0
+    if q is not None:
+        if not (q.dtype is dt and q.get_device() == dev and q.dim() == 3):
+            return no
+        q0, n_q, qd = q.shape
+        qr, qh, q1 = q.stride()
+        if not (q0 == rows and qd == hd and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0):
+            return no
+        y = _dense(q, (rows, n_q, hd))
+        qp, yp = q.data_ptr(), y.data_ptr()
+    rc = lib.rg_kv8_append(c, b[0], 1 if dt is _BF16 else 0, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, qp, qr, qh, yp,
+                           n_q * hd, hd, n_q, cp, sp, n_pos, rot, ROPE_LAYOUTS[layout], _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return True, y
+
+
 def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, sin=None, layout: str = "half",
                q_out=None, tab_row=None, stream=None):
     """Appends keys and values (bf16 or fp32 [rows, n_kv, head_dim], rows and
@@ -350,48 +411,14 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
       seq_off   int32 [sequences + 1]: each sequence's rows, or None for one
                 row a sequence
     See rg_kv8_append in rollout.h for scales, rounding and what padding gets."""
-    lib = _library()
-    if isinstance(k, _torch.Tensor) and k.dim() == 3 and q_out is None and stream is None:
-        dt, dev = k.dtype, k.get_device()
-        lay = ROPE_LAYOUTS.get(layout)
-        c = _cache_fits(cache, dev) if (dt is _BF16 or dt is _F32) and dev >= 0 and lay is not None and _here(dev) else None
-        if c is not None:
-            c, n_kv, hd, _ = c
-            rows = k.shape[0]
-            shape = (rows, n_kv, hd)
-            kr, kh, k1 = k.stride()
-            b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
-            ok = (b is not None and k.shape == shape and isinstance(v, _torch.Tensor) and
-                  v.dtype is dt and v.get_device() == dev and v.shape == shape)
-            rot = n_pos = cp = sp = 0
-            if ok and cos is not None:
-                rot = _table_fits(cos, sin, hd, dev)
-                ok = rot > 0
-                if ok:
-                    n_pos, cp, sp = cos.shape[0], cos.data_ptr(), sin.data_ptr()
-            elif sin is not None:
-                ok = False
-            if ok:
-                vr, vh, v1 = v.stride()
-                ok = k1 == 1 and v1 == 1
-            y = None
-            n_q = qp = qr = qh = yp = 0
-            if ok and q is not None:
-                ok = isinstance(q, _torch.Tensor) and q.dtype is dt and q.get_device() == dev and q.dim() == 3
-                if ok:
-                    q0, n_q, qd = q.shape
-                    qr, qh, q1 = q.stride()
-                    ok = q0 == rows and qd == hd and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0
-                if ok:
-                    y = q.new_empty((rows, n_q, hd))
-                    qp, yp = q.data_ptr(), y.data_ptr()
-            if ok:
-                rc = lib.rg_kv8_append(c, b[0], 1 if dt is _BF16 else 0, k.data_ptr(), kr, kh, v.data_ptr(),
-                                       vr, vh, qp, qr, qh, yp, n_q * hd, hd, n_q, cp, sp, n_pos, rot, lay,
-                                       _torch._C._cuda_getCurrentRawStream(dev))
-                if rc:
-                    _check(rc)
-                return y
+    lib = _ready or _library()
+    if q_out is None and stream is None:
+        try:
+            done, y = _append_now(lib, cache, k, v, page_tab, seq_len, seq_off, q, cos, sin, layout, tab_row)
+        except AttributeError:
+            done = False
+        if done:
+            return y
     dt, code = _float_type("k", k)
     c = _cache_args(cache)
     rows = k.shape[0]
@@ -428,6 +455,35 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
     return q_out
 
 
+def _attention_now(lib, cache, q, page_tab, seq_len, seq_off, max_len, scale, tab_row):
+    """The call where every argument is in place, else None."""
+    dt, dev = q.dtype, q.get_device()
+    if not ((dt is _BF16 or dt is _F32) and dev >= 0 and _device() == dev and q.dim() == 3):
+        return None
+    rows, n_q, hd = q.shape
+    qr, qh, q1 = q.stride()
+    c = _cache_fits(cache, dev)
+    b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
+    if c is None or b is None:
+        return None
+    c, n_kv, head_dim, page = c
+    b, n_seqs, stride = b
+    bound = max(1, stride * page) if max_len is None else int(max_len)
+    if not (hd == head_dim and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0 and 1 <= bound <= 1 << 30):
+        return None
+    y = _dense(q, (rows, n_q, hd))
+    need = lib.rg_kv8_attention_scratch(n_q, n_kv, hd, rows, n_seqs, 0 if seq_off is None else 1, bound)
+    scratch, sp = None, 0
+    if need > 0:
+        scratch = q.new_empty(need // 4, dtype=_F32)
+        sp = scratch.data_ptr()
+    rc = lib.rg_kv8_attention(c, b, 1 if dt is _BF16 else 0, q.data_ptr(), qr, qh, n_q, y.data_ptr(),
+                              hd ** -0.5 if scale is None else float(scale), bound, sp, need, _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return y
+
+
 def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[int] = None,
                   scale: Optional[float] = None, out=None, tab_row=None, stream=None):
     """Causal attention of q (bf16 or fp32 [rows, n_q, head_dim], rows and heads
@@ -437,31 +493,14 @@ def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[i
     better launches), ``scale`` defaults to 1/sqrt(head_dim).  Returns
     [rows, n_q, head_dim] in q's dtype, zeros for padding rows; rows past the
     last sequence's are not written.  See rg_kv8_attention in rollout.h."""
-    lib = _library()
-    if isinstance(q, _torch.Tensor) and q.dim() == 3 and out is None and stream is None:
-        dt, dev = q.dtype, q.get_device()
-        c = _cache_fits(cache, dev) if (dt is _BF16 or dt is _F32) and dev >= 0 and _here(dev) else None
-        if c is not None:
-            c, n_kv, head_dim, page = c
-            rows, n_q, hd = q.shape
-            qr, qh, q1 = q.stride()
-            b = _batch_fits(rows, page_tab, seq_len, seq_off, tab_row, dev)
-            if b is not None and hd == head_dim and q1 == 1 and 0 < n_q <= _MOST and n_q % n_kv == 0:
-                b, n_seqs, stride = b
-                bound = max(1, stride * page) if max_len is None else int(max_len)
-                if 1 <= bound <= 1 << 30:
-                    y = q.new_empty((rows, n_q, hd))
-                    need = lib.rg_kv8_attention_scratch(n_q, n_kv, hd, rows, n_seqs, 0 if seq_off is None else 1, bound)
-                    scratch, sp = None, 0
-                    if need > 0:
-                        scratch = _torch.empty(need // 4, dtype=_F32, device=q.device)
-                        sp = scratch.data_ptr()
-                    rc = lib.rg_kv8_attention(c, b, 1 if dt is _BF16 else 0, q.data_ptr(), qr, qh, n_q,
-                                              y.data_ptr(), hd ** -0.5 if scale is None else float(scale), bound, sp, need,
-                                              _torch._C._cuda_getCurrentRawStream(dev))
-                    if rc:
-                        _check(rc)
-                    return y
+    lib = _ready or _library()
+    if out is None and stream is None:
+        try:
+            y = _attention_now(lib, cache, q, page_tab, seq_len, seq_off, max_len, scale, tab_row)
+        except AttributeError:
+            y = None
+        if y is not None:
+            return y
     dt, code = _float_type("q", q)
     c = _cache_args(cache)
     rows, n_q, hd = q.shape
