@@ -22,7 +22,6 @@
 
 #include "kv8_device.h"
 #include "rope_device.h"
-#include <hip/hip_ext.h>
 
 namespace {
 
@@ -302,15 +301,7 @@ hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, Head
   const bool vec = views_vector(dtype, k) && views_vector(dtype, v) && views_vector(dtype, HeadView{q_out.p, q_out.row, q_out.head}) &&
                    views_vector(dtype, q) && (t.layout ? (2 * t.pairs) % 8 == 0 : t.pairs % 8 == 0) &&
                    (uintptr_t)t.cos % 16 == 0 && (uintptr_t)t.sin % 16 == 0;
-  hipEvent_t e0 = nullptr, e1 = nullptr;
-  const bool timed = rg_take_launch_events(&e0, &e1);
-#define RG_APP(T, VEC, LAY, HD)                                                                                        \
-  do {                                                                                                                 \
-    if (timed)                                                                                                         \
-      hipExtLaunchKernelGGL((k_kv8_append<T, VEC, LAY, HD>), dim3((unsigned)grid), dim3(256), 0, st, e0, e1, 0, a);    \
-    else                                                                                                               \
-      hipLaunchKernelGGL((k_kv8_append<T, VEC, LAY, HD>), dim3((unsigned)grid), dim3(256), 0, st, a);                  \
-  } while (0)
+#define RG_APP(T, VEC, LAY, HD) return kv8_launch(k_kv8_append<T, VEC, LAY, HD>, dim3((unsigned)grid), dim3(256), st, a)
 #define RG_APP_HD(T, VEC, LAY) \
   if (c.hd == 128) { RG_APP(T, VEC, LAY, 128); } else { RG_APP(T, VEC, LAY, 64); }
 #define RG_APP_L(T, VEC) \
@@ -323,7 +314,6 @@ hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, Head
 #undef RG_APP_L
 #undef RG_APP_HD
 #undef RG_APP
-  return hipGetLastError();
 }
 
 hipError_t launch_kv8_runs(const int32_t* coff, const int32_t* plen, const int32_t* seq_grp, int n_seq, int row0, int n,

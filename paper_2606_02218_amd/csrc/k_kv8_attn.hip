@@ -31,7 +31,6 @@
 #include <type_traits>
 
 #include "kv8_device.h"
-#include <hip/hip_ext.h>
 
 namespace {
 
@@ -670,15 +669,6 @@ __global__ __launch_bounds__(256) void k_kv8_merge(Kv8Attn A) {
   put<OUT>(A, r, h, d, v);
 }
 
-template <typename F, typename... Args>
-void launch(F kernel, dim3 grid, dim3 block, hipStream_t st, Args... args) {
-  hipEvent_t e0, e1;
-  if (rg_take_launch_events(&e0, &e1))
-    hipExtLaunchKernelGGL(kernel, grid, block, 0, st, e0, e1, 0, args...);
-  else
-    hipLaunchKernelGGL(kernel, grid, block, 0, st, args...);
-}
-
 template <typename T, int HD, int OUT>
 hipError_t run(const Kv8Attn& a, hipStream_t st) {
   const int rep = a.n_q / a.c.n_kv;
@@ -686,22 +676,19 @@ hipError_t run(const Kv8Attn& a, hipStream_t st) {
     const int np = KV8_TILE_Q / rep;
     const int64_t tiles = (int64_t)a.b.rows / np + a.b.n_seqs, grid = tiles * a.c.n_kv * a.plan.n_split;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    launch(k_kv8_tiles<T, HD, OUT>, dim3((unsigned)grid), dim3(64 * KV8_WAVES), st, a, (int)tiles);
-  } else {
-    const int htiles = (rep + 15) / 16;
-    const int64_t items = (int64_t)a.b.rows * a.c.n_kv * htiles * a.plan.n_split, per = (items + 7) / 8;
-    if (8 * per > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(8 * per));
-    if (a.plan.waves == 8) launch(k_kv8_rows<T, HD, OUT, 8>, grid, dim3(512), st, a, htiles, (int)per, (int)items);
-    else launch(k_kv8_rows<T, HD, OUT, 4>, grid, dim3(256), st, a, htiles, (int)per, (int)items);
+    return kv8_launch(k_kv8_tiles<T, HD, OUT>, dim3((unsigned)grid), dim3(64 * KV8_WAVES), st, a, (int)tiles);
   }
-  return hipGetLastError();
+  const int htiles = (rep + 15) / 16;
+  const int64_t items = (int64_t)a.b.rows * a.c.n_kv * htiles * a.plan.n_split, per = (items + 7) / 8;
+  if (8 * per > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)(8 * per));
+  if (a.plan.waves == 8) return kv8_launch(k_kv8_rows<T, HD, OUT, 8>, grid, dim3(512), st, a, htiles, (int)per, (int)items);
+  return kv8_launch(k_kv8_rows<T, HD, OUT, 4>, grid, dim3(256), st, a, htiles, (int)per, (int)items);
 }
 
 template <int HD, int OUT>
 hipError_t merge(const Kv8Attn& a, hipStream_t st) {
-  launch(k_kv8_merge<HD, OUT>, dim3(a.b.rows, a.n_q), dim3(256), st, a);
-  return hipGetLastError();
+  return kv8_launch(k_kv8_merge<HD, OUT>, dim3(a.b.rows, a.n_q), dim3(256), st, a);
 }
 
 }  // namespace

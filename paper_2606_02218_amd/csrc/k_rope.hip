@@ -61,9 +61,9 @@ hipError_t launch_rope(int dtype, HeadView x, HeadOut y, const int32_t* pos, int
   const dim3 grid(((unsigned)rows + 3) / 4);
   const float sign = inverse ? -1.f : 1.f;
   const bool vec = rope_vectors(dtype, x, hd, t) && rope_vectors(dtype, HeadView{y.p, y.row, y.head}, hd, t);
-#define RG_ROPE(T, VEC, LAY)                                                                                        \
-  hipLaunchKernelGGL((k_rope<T, VEC, LAY>), grid, dim3(256), 0, st, (const T*)x.p, x.row, x.head, (T*)y.p, y.row,   \
-                     y.head, pos, rows, heads, hd, t, sign)
+#define RG_ROPE(T, VEC, LAY)                                                                                          \
+  return kv8_launch(k_rope<T, VEC, LAY>, grid, dim3(256), st, (const T*)x.p, x.row, x.head, (T*)y.p, y.row, y.head,   \
+                    pos, rows, heads, hd, t, sign)
 #define RG_ROPE_L(T, VEC) \
   if (t.layout) RG_ROPE(T, VEC, 1); else RG_ROPE(T, VEC, 0)
   if (dtype == 1) {
@@ -75,5 +75,4 @@ hipError_t launch_rope(int dtype, HeadView x, HeadOut y, const int32_t* pos, int
   }
 #undef RG_ROPE_L
 #undef RG_ROPE
-  return hipGetLastError();
 }
