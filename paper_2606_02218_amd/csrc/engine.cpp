@@ -331,7 +331,7 @@ int kv8_layer(rg_policy* pol, hipStream_t st, int l, const Kv8Rows& batch, int c
   at.scale = 1.0f / std::sqrt((float)pol->hd);
   at.part_o = pol->att_o;
   at.part_ml = pol->att_ml;
-  at.plan = kv8_plan(batch.rows, batch.n_seqs, tiles, pol->nq, pol->nkv, ctx_max,
+  at.plan = kv8_plan(batch.rows, batch.n_seqs, batch.seq_off != nullptr, tiles, pol->nq, pol->nkv, ctx_max,
                      (int)std::max<int64_t>(1, std::min<int64_t>(pol->att_rowchunks / batch.rows, INT32_MAX)));
   LAUNCH_TIMED(RG_K_ATTN, launch_kv8_attention(RG_DTYPE_F32, true, at, st));
   if (at.plan.n_split > 1) LAUNCH_TIMED(RG_K_ATTN_MERGE, launch_kv8_merge(RG_DTYPE_F32, true, at, st));

@@ -40,21 +40,6 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a < INFINITY ? a : 0.f;   // NaN and infinities do not set a scale
 }
 
-// Largest value of the wave's lanes, in every lane: through the vector unit's own
-// lane moves, half the latency of six exchanges through LDS.
-__device__ __forceinline__ float wave_max_dpp(float v) {
-#define RG_DPP_MAX(ctrl) \
-  v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), ctrl, 0xf, 0xf, false)))
-  RG_DPP_MAX(0x111);   // row_shr 1, 2, 4, 8: lane 15 of each row of 16 has its maximum
-  RG_DPP_MAX(0x112);
-  RG_DPP_MAX(0x114);
-  RG_DPP_MAX(0x118);
-  RG_DPP_MAX(0x142);   // row_bcast 15, 31: lane 63 has the wave's
-  RG_DPP_MAX(0x143);
-#undef RG_DPP_MAX
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-
 // Dims d0 .. d0 + 7 of a key, turned.  x: the head; ok: the position is in the table.
 template <typename T, bool VEC, int LAYOUT>
 __device__ __forceinline__ void turned8(const T* x, int d0, const RopeTable& t, const float* co, const float* si, bool ok,

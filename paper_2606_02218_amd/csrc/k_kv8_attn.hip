@@ -20,7 +20,7 @@
 //   Its four or eight waves take 32-token steps in turn straight from memory, 16
 //   bytes a lane, and join in LDS.  Bound by the cache's bytes: three rows of 60 to
 //   131 thousand tokens, 4 kv heads (221 MB) 39 us, 5.7 TB/s of the 6.6 that a plain
-//   read reaches; 512 rows of 512 to 2600 tokens, 2 kv heads 67 us.
+//   read reaches; 512 rows of 512 to 2600 tokens, 2 kv heads 60 us.
 // * Tiles pass (runs of rows): a workgroup per 128 query rows (positions x heads
 //   of a kv head) and chunk.  32-token pieces go through LDS once for the four
 //   waves of 32 query rows.  Bound by vector issue beside the matrix instructions:
@@ -108,6 +108,43 @@ __device__ __forceinline__ float* part_ml(const Kv8Attn& A, int64_t slot, int he
 }
 
 // ---------------------------------------------------------------- rows pass
+// Work by length.  An XCD takes an eighth of the rows, in segments of 64, each from
+// its longest row down; every other round of 32 blocks, one for each of its CUs,
+// runs backwards, so that the CUs' sums even out.  512 rows of 512 to 2600 tokens
+// and 2 kv heads: 60 us, 68 as they come (47 where all have the same length); over
+// all XCDs instead of within one 69, since siblings then share no L2.
+//
+// Block `item` of an XCD becomes the item of its row, counted from row0; false
+// where there is none.  The row of a rank is found bit by bit of the lengths in
+// 32-token steps, a row a lane.
+__device__ __forceinline__ bool deal_item(const Kv8Attn& A, int htiles, unsigned& item, int& row0) {
+  const int n = A.b.d_rows ? min(*A.b.d_rows, A.b.rows) : A.b.rows, per = (n + 7) >> 3;
+  const unsigned inner = (unsigned)(A.c.n_kv * htiles), seg = item / (64 * inner);
+  row0 = (int)(blockIdx.x & 7) * per + 64 * (int)seg;
+  const int here = min(64, min(per * (int)((blockIdx.x & 7) + 1), n) - row0);
+  if (here <= 0) return false;
+  const unsigned j = item - seg * (64 * inner), count = (unsigned)here * inner;
+  if (j >= count) return false;
+  const unsigned p = (j & 32) && (j | 31) < count ? (j & ~31u) + 31 - (j & 31) : j;
+  const unsigned rank = p / inner;
+  const int lane = threadIdx.x & 63, bits = A.plan.deal;
+  const int key = lane < here ? min((int)(((unsigned)kv8_len(A.b, row0 + lane) + 31) >> 5), (1 << bits) - 1) : 0;
+  uint64_t left = here == 64 ? ~0ull : (1ull << here) - 1;
+  int k = (int)rank;
+  for (int bit = bits - 1; bit >= 0; --bit) {
+    const uint64_t set = __ballot(key >> bit & 1) & left;
+    const int c = __popcll(set);
+    if (k < c) {
+      left = set;
+    } else {
+      k -= c;
+      left &= ~set;
+    }
+  }
+  item = (unsigned)wave_nth_bit(left, k) * inner + p % inner;
+  return true;
+}
+
 template <typename T, int HD, int OUT, int W>
 __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / W) void k_kv8_rows(
     Kv8Attn A, int htiles, int per_xcd, int items) {
@@ -119,13 +156,19 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
 
   // Blocks are dealt to the 8 XCDs in turn: neighbouring rows, which share
   // pages where they are siblings of a prompt, go to the same one.
-  unsigned item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (item >= (unsigned)items) return;
+  unsigned item = blockIdx.x >> 3;
+  int row0 = 0;
+  if (A.plan.deal) {
+    if (!deal_item(A, htiles, item, row0)) return;
+  } else {
+    item += (blockIdx.x & 7) * per_xcd;
+    if (item >= (unsigned)items) return;
+  }
   const int split = (int)(item % (unsigned)A.plan.n_split);
   item /= (unsigned)A.plan.n_split;
   const int ht = (int)(item % (unsigned)htiles);
   item /= (unsigned)htiles;
-  const int kvh = (int)(item % (unsigned)A.c.n_kv), r = (int)(item / (unsigned)A.c.n_kv);
+  const int kvh = (int)(item % (unsigned)A.c.n_kv), r = row0 + (int)(item / (unsigned)A.c.n_kv);
   const int rep = A.n_q / A.c.n_kv, nh = min(16, rep - ht * 16), head0 = kvh * rep + ht * 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
@@ -333,6 +376,42 @@ __device__ __forceinline__ uint32_t clear_nan(uint32_t w) {
   return w & ~(hit * 0xFFu);
 }
 
+// Tile k of a batch, tiles of np rows: among 64 sequences, a lane each, those with
+// the longest contexts come first, so that none of them starts when the others end:
+// 24 fp32 runs of 37 to 701 rows 78 us, 87 with each sequence's tiles in turn; bf16
+// 40 and 46.
+// A sequence of T tiles behind `old` tokens has them at levels old / np + 1 .. old /
+// np + T; level and place of a rank are found bit by bit.  False past the last tile.
+__device__ __forceinline__ bool tile_of(const Kv8Rows& b, int np, int k, int& s, int& r0, int& n, int& skip) {
+  auto key = [&](int q) { return min(max(b.seq_off[q], 0), b.rows) / np + q; };   // tiles are numbered from here
+  int s0 = 0;
+  for (int hi = (b.n_seqs + 63) >> 6, lo = 0; hi - lo > 1;) {
+    const int mid = (lo + hi) >> 1;
+    if (key(64 * mid) <= k) lo = mid;
+    else hi = mid;
+    s0 = 64 * lo;
+  }
+  const int lane = threadIdx.x & 63, rank = k - key(s0);
+  int f = 0, c = 0, tiles = 0, top = 0;
+  if (s0 + lane < b.n_seqs) {
+    kv8_seq_rows(b, s0 + lane, f, c);
+    tiles = (int)(((unsigned)max(c, 0) + np - 1) / (unsigned)np);
+    top = (int)((unsigned)min(max(kv8_len(b, s0 + lane) - c, 0), 1 << 30) / (unsigned)np) + tiles;
+  }
+  auto from = [&](int level) { return wave_sum_dpp(min(max(top - level + 1, 0), tiles)); };   // tiles at it and above
+  int level = 0;
+  for (int bit = 31 - __clz(wave_max_dpp(top) | 1); bit >= 0; --bit)
+    if (from(level | 1 << bit) > rank) level |= 1 << bit;
+  if (rank < 0 || level == 0) return false;
+  const int down = top - level;
+  const int at = wave_nth_bit(__ballot(down >= 0 && down < tiles), rank - from(level + 1));
+  s = s0 + at;
+  r0 = __builtin_amdgcn_readlane(f, at);
+  n = __builtin_amdgcn_readlane(c, at);
+  skip = __builtin_amdgcn_readlane(tiles - 1 - down, at) * np;
+  return true;
+}
+
 // Codes are converted once a workgroup, on their way into LDS: a wave that
 // converted its own operands spent 128 of its 300 vector instructions per 64
 // tokens on it.  A wave's chain through a piece (scores, maximum, exponentials,
@@ -345,7 +424,7 @@ __device__ __forceinline__ uint32_t clear_nan(uint32_t w) {
 // 8 + 4 hh .. + 3 of a block, those whose probabilities lane half hh holds.  Lanes
 // read neighbouring pieces.
 template <typename T, int HD, int OUT>
-__global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8_tiles(Kv8Attn A, int tiles) {
+__global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8_tiles(Kv8Attn A) {
   constexpr int QP = q_pieces(OUT), PP = p_pieces(OUT, true);
   constexpr int NK = HD / 16;       // 32x32x16 steps over the head's dims
   constexpr int DT = HD / 32;       // 32-dim tiles of the output: tile e holds dims DT * row + e
@@ -354,20 +433,15 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   __shared__ int sNan[2][KV8_WAVES];
 
   // Blocks are dealt to the 8 XCDs in turn, so with the kv heads side by side an
-  // XCD keeps to few of them.  Tiles go last first: within a sequence the
-  // longest contexts start first.
+  // XCD keeps to few of them.
   unsigned item = blockIdx.x;
   const int kvh = (int)(item % (unsigned)A.c.n_kv);
   item /= (unsigned)A.c.n_kv;
   const int split = (int)(item % (unsigned)A.plan.n_split);
-  const int k = tiles - 1 - (int)(item / (unsigned)A.plan.n_split);
   const int rep = A.n_q / A.c.n_kv, np = KV8_TILE_Q / rep;
-  int key, s, r0, n;
-  s = kv8_find(A.b, k, np, 1, key);
-  kv8_seq_rows(A.b, s, r0, n);
-  const int skip = (k - key) * np;  // rows of the sequence before the tile
+  int s, r0, n, skip;               // the tile's sequence, its rows, those before the tile
+  if (!tile_of(A.b, np, (int)(item / (unsigned)A.plan.n_split), s, r0, n, skip)) return;
   const int nr = min(np, n - skip);
-  if (nr <= 0) return;
   const int pos0 = kv8_len(A.b, s) - n + skip;   // position of the tile's first row
   r0 += skip;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -676,10 +750,11 @@ hipError_t run(const Kv8Attn& a, hipStream_t st) {
     const int np = KV8_TILE_Q / rep;
     const int64_t tiles = (int64_t)a.b.rows / np + a.b.n_seqs, grid = tiles * a.c.n_kv * a.plan.n_split;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    return kv8_launch(k_kv8_tiles<T, HD, OUT>, dim3((unsigned)grid), dim3(64 * KV8_WAVES), st, a, (int)tiles);
+    return kv8_launch(k_kv8_tiles<T, HD, OUT>, dim3((unsigned)grid), dim3(64 * KV8_WAVES), st, a);
   }
   const int htiles = (rep + 15) / 16;
-  const int64_t items = (int64_t)a.b.rows * a.c.n_kv * htiles * a.plan.n_split, per = (items + 7) / 8;
+  const int64_t items = (int64_t)a.b.rows * a.c.n_kv * htiles * a.plan.n_split;
+  const int64_t per = a.plan.deal ? ((int64_t)a.b.rows + 7) / 8 * a.c.n_kv * htiles : (items + 7) / 8;
   if (8 * per > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)(8 * per));
   if (a.plan.waves == 8) return kv8_launch(k_kv8_rows<T, HD, OUT, 8>, grid, dim3(512), st, a, htiles, (int)per, (int)items);
@@ -706,10 +781,10 @@ hipError_t merge(const Kv8Attn& a, hipStream_t st) {
 // 37 + 5 us in 21 chunks (252 workgroups), 48 + 5 in 85.  Rows from 2048 tokens on
 // (below, the merge costs what it saves: 600 tokens in two chunks 6.1 + 4.2 us),
 // tiles from 1024, which take some 30 us per 1000 tokens; chunks of 512 at least.
-Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_len, int max_split) {
+Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, bool tiles, int n_q, int n_kv, int max_len, int max_split) {
   Kv8Plan p{};
   const int rep = n_q / n_kv;
-  p.tiles = has_off && rep <= KV8_TILE_Q && (int64_t)rows >= 4LL * n_seqs;
+  p.tiles = has_off && tiles && rep <= KV8_TILE_Q && (int64_t)rows >= 4LL * n_seqs;
   const int64_t wgs = p.tiles ? ((int64_t)rows * rep + KV8_TILE_Q - 1) / KV8_TILE_Q * n_kv
                               : (int64_t)rows * n_kv * ((rep + 15) / 16);
   p.waves = wgs <= 256 ? 8 : 4;
@@ -719,13 +794,17 @@ Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_
   p.chunk = (int)std::min<int64_t>((((int64_t)max_len + n - 1) / n + 63) / 64 * 64, 1 << 30);
   p.n_split = (int)((max_len + (int64_t)p.chunk - 1) / p.chunk);
   if (p.n_split < 1) p.n_split = 1;
+  // By length where there is more than one workgroup a CU to even out, and rows
+  // enough that an eighth of them is the same for every XCD.
+  if (!has_off && p.waves == 4 && p.n_split == 1 && rows >= 64)
+    for (int64_t steps = ((int64_t)max_len + 31) >> 5; steps; steps >>= 1) ++p.deal;
   return p;
 }
 
 hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStream_t st) {
   if (a.b.rows <= 0 || a.b.n_seqs <= 0) return hipSuccess;
   if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.n_split > KV8_MAX_SPLIT || a.plan.chunk % 64 ||
-      (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
+      (a.plan.deal && a.b.seq_off) || (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
     return hipErrorInvalidValue;
   const bool w = a.c.hd == 128;
   if (planes && dtype != 0) return hipErrorInvalidValue;

@@ -123,7 +123,7 @@ int64_t rg_kv8_attention_scratch(int32_t n_q, int32_t n_kv, int32_t head_dim, in
   if (n_q < 1 || n_kv < 1 || n_q % n_kv || head_dim < 1 || rows < 0 || n_seqs < 0 || max_len < 1)
     return bad("rg_kv8_attention_scratch", "bad sizes");
   if (rows == 0 || n_seqs == 0) return 0;
-  const Kv8Plan p = kv8_plan(rows, n_seqs, has_off != 0, n_q, n_kv, max_len, INT32_MAX);
+  const Kv8Plan p = kv8_plan(rows, n_seqs, has_off != 0, true, n_q, n_kv, max_len, INT32_MAX);
   return 4 * kv8_part_floats(rows, p, n_q, head_dim);
 }
 
@@ -145,7 +145,7 @@ int rg_kv8_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32
   a.out = out;
   a.n_q = n_q;
   a.scale = scale;
-  a.plan = kv8_plan(a.b.rows, a.b.n_seqs, a.b.seq_off != nullptr, n_q, a.c.n_kv, max_len, INT32_MAX);
+  a.plan = kv8_plan(a.b.rows, a.b.n_seqs, a.b.seq_off != nullptr, true, n_q, a.c.n_kv, max_len, INT32_MAX);
   a.part_o = (float*)scratch;
   a.part_ml = a.part_o ? a.part_o + (int64_t)a.b.rows * a.plan.n_split * n_q * a.c.hd : nullptr;
   const int64_t need = 4 * kv8_part_floats(a.b.rows, a.plan, n_q, a.c.hd);

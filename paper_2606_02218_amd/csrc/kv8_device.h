@@ -77,6 +77,42 @@ __device__ __forceinline__ int kv8_find(const Kv8Rows& b, int x, int span, int p
 // Tokens of sequence s, this call's rows counted; a length below zero is none.
 __device__ __forceinline__ int kv8_len(const Kv8Rows& b, int s) { return max(b.seq_len[s] + b.len_add, 0); }
 
+// Largest value of the wave's lanes (none below zero), in every lane: through the
+// vector unit's own lane moves, half the latency of six exchanges through LDS.
+template <typename T>
+__device__ __forceinline__ T wave_max_dpp(T x) {
+  static_assert(sizeof(T) == 4, "32 bits a lane");
+  int v = __builtin_bit_cast(int, x);         // the order of floats above zero is that of their bits
+#define RG_DPP_MAX(ctrl) v = max(v, __builtin_amdgcn_update_dpp(v, v, ctrl, 0xf, 0xf, false))
+  RG_DPP_MAX(0x111);   // row_shr 1, 2, 4, 8: lane 15 of each row of 16 has its maximum
+  RG_DPP_MAX(0x112);
+  RG_DPP_MAX(0x114);
+  RG_DPP_MAX(0x118);
+  RG_DPP_MAX(0x142);   // row_bcast 15, 31: lane 63 has the wave's
+  RG_DPP_MAX(0x143);
+#undef RG_DPP_MAX
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(v, 63));
+}
+
+// Sum of the wave's lanes, and the index of the k-th set bit of a wave's mask (one
+// that has more than k), in every lane.
+__device__ __forceinline__ int wave_sum_dpp(int v) {
+#define RG_DPP_ADD(ctrl, rows) v += __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false)
+  RG_DPP_ADD(0x111, 0xf);   // row_shr 1, 2, 4, 8: lane 15 of each row of 16 has its sum
+  RG_DPP_ADD(0x112, 0xf);
+  RG_DPP_ADD(0x114, 0xf);
+  RG_DPP_ADD(0x118, 0xf);
+  RG_DPP_ADD(0x142, 0xa);   // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+  RG_DPP_ADD(0x143, 0xc);
+#undef RG_DPP_ADD
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ int wave_nth_bit(uint64_t mask, int k) {
+  const int lane = threadIdx.x & 63;
+  const int below = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+  return __ffsll((unsigned long long)__ballot((mask >> lane & 1) && below == k)) - 1;
+}
+
 // Row r of batch b: its sequence and position there (negative: a padding row).
 // False for rows of no sequence.
 __device__ __forceinline__ bool kv8_row(const Kv8Rows& b, int r, int& s, int& pos) {

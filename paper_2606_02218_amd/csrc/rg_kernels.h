@@ -424,9 +424,11 @@ hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, Head
 struct Kv8Plan {
   bool tiles;
   int waves;   // of a rows workgroup
+  int deal;    // rows by length, whose 32-token steps have this many bits; 0: as they come
   int n_split, chunk;
 };
-Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, int n_q, int n_kv, int max_len, int max_split);
+// has_off: the batch has offsets; tiles: it may go by tiles then.
+Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, bool tiles, int n_q, int n_kv, int max_len, int max_split);
 struct Kv8Attn {
   Kv8Pool c;
   Kv8Rows b;

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from kv8_helpers import BF16, F32, Batch, attention_bound, dev, host, offsets, rounded
+from kv8_helpers import BF16, F32, UNIT, Batch, attention_bound, dev, host, offsets, rounded
 from oracle import kv8
 
 pytestmark = pytest.mark.gpu
@@ -493,3 +493,56 @@ def test_a_whole_step_on_a_given_stream():
         got.append(rg.kv8_attention(b.cache, q, tab, ln, max_len=2600, stream=stream))
         torch.cuda.synchronize()
     assert torch.equal(*got)
+
+
+@pytest.mark.parametrize("dtype,n_kv,rep,hd", [(BF16, 12, 1, 64), (F32, 5, 2, 64), (BF16, 2, 6, 128), (BF16, 1, 40, 64)])
+@pytest.mark.parametrize("rows", [64, 65, 131, 700])
+def test_many_ragged_rows(dtype, n_kv, rep, hd, rows):
+    """Rows enough to be taken by length: each gets what it gets in a small batch, whatever the lengths (none, equal
+    ones, past the bound given and past the table)."""
+    import paper_2606_02218_amd as rg
+    b = Batch([300, 270], n_kv, hd, 16, capacity=304, seed=50)
+    rng = np.random.default_rng(rows)
+    q = dev(rng.normal(size=(rows, n_kv * rep, hd)).astype(np.float32), dtype)
+    tab = dev(b.tab[rng.integers(0, 2, size=rows)])
+    some = -(-257 // (n_kv * -(-rep // 16)))                      # the fewest rows that take four waves
+    for ln in (rng.integers(1, 271, size=rows), np.full(rows, 77), np.repeat([0, 1, 270], rows)[::3][:rows],
+               np.where(rng.random(rows) < 0.1, rng.choice([2 ** 31 - 1, 400, -3], size=rows), rng.integers(0, 271, size=rows))):
+        ln = dev(ln.astype(np.int32))
+        for bound in (270, 40):
+            out = rg.kv8_attention(b.cache, q, tab, ln, max_len=bound)
+            few = min(some, 63)
+            for a in range(0, rows, few):
+                a = max(min(a, rows - few), 0)
+                part = rg.kv8_attention(b.cache, q[a:a + few], tab[a:a + few], ln[a:a + few], max_len=bound)
+                got = out[a:a + few]
+                if few * n_kv * -(-rep // 16) > 256:
+                    assert torch.equal(got.isnan(), part.isnan()) and torch.equal(got.nan_to_num(7), part.nan_to_num(7))
+                else:                                             # eight waves: other sums
+                    assert torch.allclose(got.float(), part.float(), rtol=2 * UNIT[dtype] + 2 ** -16, atol=2 ** -16, equal_nan=True)
+
+
+@pytest.mark.parametrize("n_kv,rep", [(2, 6), (1, 64)])
+def test_many_sequences_of_runs(n_kv, rep):
+    """More sequences than a wave has lanes, some without rows: each run gets what it gets in a small batch."""
+    import paper_2606_02218_amd as rg
+    b = Batch([300, 270], n_kv, 64, 16, capacity=304, seed=51)
+    rng = np.random.default_rng(3)
+    for seqs in (64, 65, 200):
+        new = rng.choice([0, 3, 17, 40], size=seqs)
+        new[:2] = 0, 60
+        ln = np.maximum(rng.integers(0, 271, size=seqs), new // 2)        # the first rows of some are padding
+        tab = b.tab[rng.integers(0, 2, size=seqs)]
+        off = np.concatenate([[0], np.cumsum(new)])
+        rows = int(off[-1])
+        assert rows >= 4 * seqs
+        q = dev(rng.normal(size=(rows, n_kv * rep, 64)).astype(np.float32), BF16)
+        out = rg.kv8_attention(b.cache, q, dev(tab), dev(ln.astype(np.int32)), dev(off.astype(np.int32)), max_len=270)
+        for a in range(0, seqs, 10):
+            z = min(a + 10, seqs)
+            r = slice(int(off[a]), int(off[z]))
+            if off[z] - off[a] < 4 * (z - a):
+                continue
+            part = rg.kv8_attention(b.cache, q[r], dev(tab[a:z]), dev(ln[a:z].astype(np.int32)),
+                                    dev((off[a:z + 1] - off[a]).astype(np.int32)), max_len=270)
+            assert torch.equal(out[r], part)

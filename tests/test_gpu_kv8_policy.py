@@ -145,6 +145,31 @@ def test_recompute_in_chunks(torch):
             assert np.abs(err).max() <= 4 * top and np.sqrt((err ** 2).mean()) <= 4 * rms
 
 
+def test_many_sequences_that_retire(torch):
+    """Decode steps of rows enough to be taken by length, fewer with every step: sequences against the oracle's alone."""
+    w = make_weights(MHA, 7)
+    prompts, G, max_new = [np.arange(1, 40, dtype=np.int32), np.arange(5, 12, dtype=np.int32)], [50, 45], 40
+    rng = np.random.default_rng(4)
+    t = rng.integers(0, 2047, size=(95, max_new)).astype(np.int32)
+    n = rng.integers(1, max_new + 1, size=95).astype(np.int32)
+    n[[0, 60]], n[[22, 49, 94]] = max_new, (25, 31, 28)
+    t[np.arange(95), n - 1] = 2047                                # the last token of a sequence is the end
+    t[~_valid(n, max_new)] = -1
+    pol = _policy(MHA, w, prompts, G, max_new)
+    dp, force = prompts_to_device(prompts), torch.from_numpy(t).cuda()
+    _, ln, lp = pol.rollout(dp, G, max_new, 1, forced_len=n, force_tokens=force)
+    assert np.array_equal(ln.cpu().numpy(), n)
+    lp, by_rows = lp.cpu().numpy(), pol.recompute_logprobs(dp, G, force, ln, row_tiles=False).cpu().numpy()
+    for s in (0, 22, 49, 60, 94):
+        p = int(s >= 50)
+        ref = dict(tokens=t[s:s + 1], lengths=n[s:s + 1])
+        want, top, rms = _noise(MHA, w, [prompts[p]], [1], ref, max_new)
+        v = _valid(n[s:s + 1], max_new)[0]
+        for got in (lp[s], by_rows[s]):
+            err = (got - want[0])[v]
+            assert np.abs(err).max() <= 4 * top, (s, np.abs(err).max(), top)
+
+
 def test_memory_and_refusals(torch):
     import paper_2606_02218_amd as rg
     w = make_weights(GQA, 4)
