@@ -114,34 +114,45 @@ __device__ __forceinline__ float* part_ml(const Kv8Attn& A, int64_t slot, int he
 // and 2 kv heads: 60 us, 68 as they come (47 where all have the same length); over
 // all XCDs instead of within one 69, since siblings then share no L2.
 //
-// Block `item` of an XCD becomes the item of its row, counted from row0; false
-// where there is none.  The row of a rank is found bit by bit of the lengths in
-// 32-token steps, a row a lane.
-__device__ __forceinline__ bool deal_item(const Kv8Attn& A, int htiles, unsigned& item, int& row0) {
-  const int n = A.b.d_rows ? min(*A.b.d_rows, A.b.rows) : A.b.rows, per = (n + 7) >> 3;
-  const unsigned inner = (unsigned)(A.c.n_kv * htiles), seg = item / (64 * inner);
-  row0 = (int)(blockIdx.x & 7) * per + 64 * (int)seg;
-  const int here = min(64, min(per * (int)((blockIdx.x & 7) + 1), n) - row0);
+// The row of this block of an XCD, its kv head and head tile, tokens and table row;
+// false where there is none.  The row of a rank is found bit by bit of the lengths
+// in 32-token steps, a row a lane.
+__device__ __forceinline__ bool deal_item(const Kv8Attn& A, int htiles, int& r, int& kvh, int& ht, int& tokens, int& tab_row) {
+  const int n = A.b.d_rows ? min(*A.b.d_rows, A.b.rows) : A.b.rows, per = (n + 7) >> 3, xcd = blockIdx.x & 7;
+  const unsigned inner = (unsigned)(A.c.n_kv * htiles), span = 64 * inner;
+  unsigned j = blockIdx.x >> 3;
+  int row0 = xcd * per;
+  if (j >= span) {
+    const unsigned seg = j / span;
+    row0 += 64 * (int)seg;
+    j -= seg * span;
+  }
+  const int here = min(64, min(per * (xcd + 1), n) - row0);
   if (here <= 0) return false;
-  const unsigned j = item - seg * (64 * inner), count = (unsigned)here * inner;
+  const unsigned count = (unsigned)here * inner;
   if (j >= count) return false;
-  const unsigned p = (j & 32) && (j | 31) < count ? (j & ~31u) + 31 - (j & 31) : j;
-  const unsigned rank = p / inner;
   const int lane = threadIdx.x & 63, bits = A.plan.deal;
-  const int key = lane < here ? min((int)(((unsigned)kv8_len(A.b, row0 + lane) + 31) >> 5), (1 << bits) - 1) : 0;
+  int len = 0, tr = row0 + lane;
+  if (lane < here) {
+    len = kv8_len(A.b, row0 + lane);
+    if (A.b.tab_row) tr = A.b.tab_row[row0 + lane];
+  }
+  const unsigned p = (j & 32) && (j | 31) < count ? (j & ~31u) + 31 - (j & 31) : j, rank = p / inner, rest = p - rank * inner;
+  const int key = min((int)(((unsigned)len + 31) >> 5), (1 << bits) - 1);
   uint64_t left = here == 64 ? ~0ull : (1ull << here) - 1;
   int k = (int)rank;
   for (int bit = bits - 1; bit >= 0; --bit) {
     const uint64_t set = __ballot(key >> bit & 1) & left;
     const int c = __popcll(set);
-    if (k < c) {
-      left = set;
-    } else {
-      k -= c;
-      left &= ~set;
-    }
+    left = k < c ? set : left & ~set;
+    k -= k < c ? 0 : c;
   }
-  item = (unsigned)wave_nth_bit(left, k) * inner + p % inner;
+  const int at = wave_nth_bit(left, k);
+  r = row0 + at;
+  ht = htiles == 1 ? 0 : (int)(rest / (unsigned)A.c.n_kv);
+  kvh = (int)rest - ht * A.c.n_kv;
+  tokens = __builtin_amdgcn_readlane(len, at);
+  tab_row = __builtin_amdgcn_readlane(tr, at);
   return true;
 }
 
@@ -156,24 +167,29 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
 
   // Blocks are dealt to the 8 XCDs in turn: neighbouring rows, which share
   // pages where they are siblings of a prompt, go to the same one.
-  unsigned item = blockIdx.x >> 3;
-  int row0 = 0;
+  int r, kvh, ht, split = 0, pos;
+  const int32_t* tab;
   if (A.plan.deal) {
-    if (!deal_item(A, htiles, item, row0)) return;
+    int tokens, tr;
+    if (!deal_item(A, htiles, r, kvh, ht, tokens, tr)) return;
+    pos = tokens - 1;
+    tab = (unsigned)tr < (unsigned)A.b.tab_rows ? A.b.tab + (int64_t)tr * A.b.tab_stride : nullptr;
   } else {
-    item += (blockIdx.x & 7) * per_xcd;
+    unsigned item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if (item >= (unsigned)items) return;
+    split = (int)(item % (unsigned)A.plan.n_split);
+    item /= (unsigned)A.plan.n_split;
+    ht = (int)(item % (unsigned)htiles);
+    item /= (unsigned)htiles;
+    kvh = (int)(item % (unsigned)A.c.n_kv);
+    r = (int)(item / (unsigned)A.c.n_kv);
+    int s;
+    if (!kv8_row(A.b, r, s, pos)) return;
+    tab = kv8_table(A.b, s);
   }
-  const int split = (int)(item % (unsigned)A.plan.n_split);
-  item /= (unsigned)A.plan.n_split;
-  const int ht = (int)(item % (unsigned)htiles);
-  item /= (unsigned)htiles;
-  const int kvh = (int)(item % (unsigned)A.c.n_kv), r = row0 + (int)(item / (unsigned)A.c.n_kv);
   const int rep = A.n_q / A.c.n_kv, nh = min(16, rep - ht * 16), head0 = kvh * rep + ht * 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
-  int s, pos;
-  if (!kv8_row(A.b, r, s, pos)) return;
   if (pos < 0) {                    // a padding row sees nothing
     if (A.plan.n_split == 1)
       for (int i = tid; i < nh * HD / 4; i += 64 * W) {
@@ -187,8 +203,7 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
   if (c0l >= ctx) return;
   const int c0 = (int)c0l, c1 = split == A.plan.n_split - 1 ? ctx : min(ctx, c0 + A.plan.chunk);
   const int steps = (c1 - c0 + 31) / 32, last_blk = (c1 - 1) >> 4;
-  const int mine = (steps - wave + W - 1) / W;   // steps wave, wave + 4, ...
-  const int32_t* tab = kv8_table(A.b, s);
+  const int mine = (steps - wave + W - 1) / W;   // steps wave, wave + W, ...
 
   bf16x8_t qf[2 * NJ][QP];
   {
