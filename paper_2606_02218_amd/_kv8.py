@@ -269,7 +269,8 @@ def rope(x, pos, cos, sin, layout: str = "half", inverse: bool = False, out=None
     """Turns the heads of x (bf16 or fp32 [rows, heads, head_dim], rows and heads
     at any strides) by their rows' positions pos (int32 [rows]); cos and sin are
     a rope_table of at most head_dim dims.  ``inverse=True`` turns back: the
-    gradient with respect to x, given the one with respect to the result.
+    gradient with respect to x, given the one with respect to the result (the
+    call itself is not recorded by autograd).
     ``out`` may be x.  See rg_rope in rollout.h."""
     lib = _ready or _library()
     if out is None and stream is None:
@@ -313,8 +314,10 @@ class Kv8Cache(NamedTuple):
     def empty(cls, pages: int, n_kv: int, head_dim: int, page_tokens: int = 16, device="cuda"):
         """A cache whose pages hold nothing yet (contents undefined)."""
         import torch
-        if page_tokens < 16 or page_tokens % 16:
-            raise ValueError(f"page_tokens must be a multiple of 16, got {page_tokens}")
+        if page_tokens not in (16, 32, 64, 128, 256, 512, 1024):
+            raise ValueError(f"page_tokens must be a multiple of 16 by a power of two, at most 1024, got {page_tokens}")
+        if head_dim not in (64, 128):
+            raise ValueError(f"head_dim must be 64 or 128, got {head_dim}")
         shape = (pages, n_kv, page_tokens // 16)
         k, v = (torch.empty(*shape, 16 * head_dim, dtype=torch.float8_e4m3fn, device=device) for _ in range(2))
         ks, vs = (torch.empty(shape, dtype=torch.float32, device=device) for _ in range(2))

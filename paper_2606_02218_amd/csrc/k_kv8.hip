@@ -283,8 +283,9 @@ hipError_t launch_kv8_append(int dtype, const Kv8Pool& c, const Kv8Rows& b, Head
   if (grid > (1 << 29)) return hipErrorInvalidValue;   // items are numbered in 32 bits
   const AppendArgs a{c, b, k, v, q, q_out, n_q, t, (unsigned)blocks};
   // whole 16-byte pieces: keys are turned 8 dims at a time
-  const bool vec = views_vector(dtype, k) && views_vector(dtype, v) && views_vector(dtype, HeadView{q_out.p, q_out.row, q_out.head}) &&
-                   views_vector(dtype, q) && (t.layout ? (2 * t.pairs) % 8 == 0 : t.pairs % 8 == 0) &&
+  const bool vec = views_vector(dtype, k) && views_vector(dtype, v) && views_vector(dtype, q) &&
+                   views_vector(dtype, HeadView{q_out.p, q_out.row, q_out.head}) &&
+                   (t.layout ? (2 * t.pairs) % 8 == 0 : t.pairs % 8 == 0) &&
                    (uintptr_t)t.cos % 16 == 0 && (uintptr_t)t.sin % 16 == 0;
 #define RG_APP(T, VEC, LAY, HD) return kv8_launch(k_kv8_append<T, VEC, LAY, HD>, dim3((unsigned)grid), dim3(256), st, a)
 #define RG_APP_HD(T, VEC, LAY) \

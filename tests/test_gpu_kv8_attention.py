@@ -546,3 +546,22 @@ def test_many_sequences_of_runs(n_kv, rep):
             part = rg.kv8_attention(b.cache, q[r], dev(tab[a:z]), dev(ln[a:z].astype(np.int32)),
                                     dev((off[a:z + 1] - off[a]).astype(np.int32)), max_len=270)
             assert torch.equal(out[r], part)
+
+
+def test_calls_without_rows():
+    """No rows, with and without sequences, leave nothing to do; sequences without rows do not disturb the others."""
+    import paper_2606_02218_amd as rg
+    b = Batch([40, 60], 2, 64, 16, seed=52)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    for dtype in (BF16, F32):
+        q = torch.zeros(0, 4, 64, dtype=dtype, device="cuda")
+        assert rg.kv8_attention(b.cache, q, dev(b.tab)[:0], none).shape == (0, 4, 64)
+        assert rg.kv8_attention(b.cache, q, dev(b.tab), dev(b.lengths()), offsets([0, 0]), max_len=4000).shape == (0, 4, 64)
+        cos, sin = rg.rope_table(4, 64)
+        assert rg.rope(q, none, cos, sin).shape == (0, 4, 64)
+        assert rg.rope(torch.zeros(3, 0, 64, dtype=dtype, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda"), cos,
+                       sin).shape == (3, 0, 64)
+        x = rounded(b.rng.normal(size=(9, 4, 64)), dtype)
+        out = rg.kv8_attention(b.cache, dev(x, dtype), dev(b.tab), dev(b.lengths()), offsets([0, 9]))
+        _check(b, x, [0, 9], out, dtype, 64 ** -0.5, True)
+    torch.cuda.synchronize()

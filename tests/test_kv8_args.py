@@ -116,6 +116,9 @@ def test_append_refuses():
         rg.kv8_append(c._replace(v=c.v[:3]), k, k, tab, n)
     with pytest.raises(ValueError, match="multiple of 16"):
         rg.Kv8Cache.empty(4, 2, 64, 24, device="cpu")
+    for page, hd, what in ((48, 64, "power of two"), (2048, 64, "at most 1024"), (16, 96, "head_dim")):
+        with pytest.raises(ValueError, match=what):
+            rg.Kv8Cache.empty(4, 2, hd, page, device="cpu")
 
 
 def test_attention_refuses():
