@@ -205,14 +205,6 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
   const int steps = (c1 - c0 + 31) / 32, last_blk = (c1 - 1) >> 4;
   const int mine = (steps - wave + W - 1) / W;   // steps wave, wave + W, ...
 
-  bf16x8_t qf[2 * NJ][QP];
-  {
-    const T* qp = (const T*)A.q.p + r * A.q.row + (head0 + col) * A.q.head;
-    const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
-#pragma unroll
-    for (int kk = 0; kk < 2 * NJ; ++kk)
-      query8<T, QP>(qp + 64 * (kk >> 1) + 16 * grp + 8 * (kk & 1), col < nh, vec, qf[kk]);
-  }
   const float sc = A.scale * KV8_LOG2E;
   float m = -INFINITY, l = 0.f;
   f32x4_t o[NJ][4];
@@ -253,6 +245,14 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
     lists(0);
     fetch_k(0);
     fetch_v(0);
+  }
+  bf16x8_t qf[2 * NJ][QP];
+  {
+    const T* qp = (const T*)A.q.p + r * A.q.row + (head0 + col) * A.q.head;
+    const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
+#pragma unroll
+    for (int kk = 0; kk < 2 * NJ; ++kk)
+      query8<T, QP>(qp + 64 * (kk >> 1) + 16 * grp + 8 * (kk & 1), col < nh, vec, qf[kk]);
   }
   for (int i = 0; i < mine; ++i) {
     const int t0 = c0 + 32 * (wave + W * i);
