@@ -19,8 +19,8 @@
 // * Rows pass (single tokens): a workgroup per row, kv head and context chunk.
 //   Its four or eight waves take 32-token steps in turn straight from memory, 16
 //   bytes a lane, and join in LDS.  Bound by the cache's bytes: three rows of 60 to
-//   131 thousand tokens, 4 kv heads (221 MB) 39 us, 5.7 TB/s of the 6.6 that a plain
-//   read reaches; 512 rows of 512 to 2600 tokens, 2 kv heads 60 us.
+//   131 thousand tokens, 4 kv heads (221 MB) 38 us, 5.9 TB/s of the 6.6 that a plain
+//   read reaches; 512 rows of 512 to 2600 tokens, 2 kv heads 57 us.
 // * Tiles pass (runs of rows): a workgroup per 128 query rows (positions x heads
 //   of a kv head) and chunk.  32-token pieces go through LDS once for the four
 //   waves of 32 query rows.  Bound by vector issue beside the matrix instructions:
@@ -111,7 +111,7 @@ __device__ __forceinline__ float* part_ml(const Kv8Attn& A, int64_t slot, int he
 // Work by length.  An XCD takes an eighth of the rows, in segments of 64, each from
 // its longest row down; every other round of 32 blocks, one for each of its CUs,
 // runs backwards, so that the CUs' sums even out.  512 rows of 512 to 2600 tokens
-// and 2 kv heads: 60 us, 68 as they come (47 where all have the same length); over
+// and 2 kv heads: 60 us in place of 68 (47 where all have the same length); over
 // all XCDs instead of within one 69, since siblings then share no L2.
 //
 // The row of this block of an XCD, its kv head and head tile, tokens and table row;
@@ -241,18 +241,36 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
       for (int j = 0; j < NJ; ++j) vr[h][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + j * 256));
     }
   };
+  // The first step's keys, the queries, the values: all on their way before the
+  // first of them is waited for (queries first, and waited for: 59 us in place of 57).
+  constexpr int NW = sizeof(T) / 2;
+  const T* qp = (const T*)A.q.p + r * A.q.row + (head0 + col) * A.q.head;
+  const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
+  u32x4_t raw[2 * NJ][NW];
   if (mine > 0) {
     lists(0);
     fetch_k(0);
-    fetch_v(0);
   }
-  bf16x8_t qf[2 * NJ][QP];
-  {
-    const T* qp = (const T*)A.q.p + r * A.q.row + (head0 + col) * A.q.head;
-    const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
 #pragma unroll
-    for (int kk = 0; kk < 2 * NJ; ++kk)
-      query8<T, QP>(qp + 64 * (kk >> 1) + 16 * grp + 8 * (kk & 1), col < nh, vec, qf[kk]);
+  for (int kk = 0; kk < 2 * NJ; ++kk)
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+      raw[kk][w] = vec && col < nh ? *reinterpret_cast<const u32x4_t*>(qp + 64 * (kk >> 1) + 16 * grp + 8 * (kk & 1) + w * (16 / sizeof(T)))
+                                   : u32x4_t{0, 0, 0, 0};
+  if (mine > 0) fetch_v(0);
+  bf16x8_t qf[2 * NJ][QP];
+#pragma unroll
+  for (int kk = 0; kk < 2 * NJ; ++kk) {
+    if (!vec) {
+      query8<T, QP>(qp + 64 * (kk >> 1) + 16 * grp + 8 * (kk & 1), col < nh, false, qf[kk]);
+    } else if constexpr (sizeof(T) == 2) {
+      qf[kk][0] = __builtin_bit_cast(bf16x8_t, raw[kk][0]);
+    } else {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(raw[kk][e / 4][e & 3]);
+      operand8<QP>(v, qf[kk]);
+    }
   }
   for (int i = 0; i < mine; ++i) {
     const int t0 = c0 + 32 * (wave + W * i);
