@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void k_kv8_append(AppendArgs A) {
   if (p0 < 0) { r0 -= p0; p0 = 0; }           // padding rows come first
   if (len <= p0) return;
   const int blk = (p0 >> 4) + (x - key);
-  if (blk > (len - 1) >> 4) return;
+  if (x < key || blk > (len - 1) >> 4) return;   // x < key: offsets that do not start at 0
   // The chain to the block's address and old scale (page, scale) runs beside the
   // rows' own loads; positions past the table end here.
   const int tr = b.tab_row ? b.tab_row[s] : s, slot = blk >> A.c.sub_shift;

@@ -1,0 +1,39 @@
+"""Calls of the 8-bit cache at the edges of what its documentation allows: offsets
+that are not what they should be, pages that nobody wrote, the largest values."""
+import numpy as np
+import pytest
+import torch
+
+from kv8_helpers import BF16, Batch, dev, offsets, rounded
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("first", [1, 15, 16, 17, 40, 100])
+@pytest.mark.parametrize("old", [[0, 0, 0], [7, 0, 33]])
+def test_offsets_that_do_not_start_at_zero(first, old):
+    """Rows before the first sequence's belong to nobody, as those behind the last: append stores the sequences' own rows
+    and changes nothing else, the scales of blocks before them among it; attention leaves their outputs alone."""
+    import paper_2606_02218_amd as rg
+    new = [3, 20, 1]
+    b = Batch(old, 2, 64, 16, capacity=64, seed=first)
+    rows = first + sum(new) + 2
+    k, v = (rounded(b.rng.normal(size=(rows, 2, 64)), BF16) for _ in range(2))
+    q = dev(b.rng.normal(size=(rows, 4, 64)).astype(np.float32), BF16)
+    off = first + np.cumsum([0] + new)
+    for s in range(3):
+        b.k[s].append(k[off[s]:off[s + 1]])
+        b.v[s].append(v[off[s]:off[s + 1]])
+    want = b.image()
+    own = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    own[first:-2] = True
+    q_out = torch.full_like(q, 5.0)
+    args = dev(b.tab), dev(b.lengths()), dev(off.astype(np.int32))
+    rg.kv8_append(b.cache, dev(k, BF16), dev(v, BF16), *args, q=q, q_out=q_out)
+    for got, w in zip(b.snapshot(), want):
+        assert np.array_equal(got, w)
+    assert torch.equal(q_out[own], q[own]) and torch.all(q_out[~own] == 5.0)
+    out = torch.full_like(q, 5.0)
+    rg.kv8_attention(b.cache, q, *args, out=out)
+    alone = rg.kv8_attention(b.cache, q[own], args[0], args[1], offsets(new))
+    assert torch.equal(out[own], alone) and torch.all(out[~own] == 5.0)
