@@ -340,7 +340,9 @@ int grpo_surrogate_noalloc(const float* new_lp, const float* old_lp, const float
  * that of every view of a call: RG_DTYPE_F32 or RG_DTYPE_BF16.  All entry points
  * only enqueue work on `stream` and allocate nothing (they can be captured into
  * HIP graphs); they keep no state, so calls on several streams may overlap
- * where their outputs do not. */
+ * where their outputs do not.  RG_EHIP, with nothing enqueued, where a call would
+ * take a launch of 2^32 threads or more: tables of 2^32 entries; appends and
+ * attention of more than some 2^24 rows times kv heads. */
 
 #define RG_ROPE_HALF        0   /* pairs (x[i], x[i + rot_dim/2])  */
 #define RG_ROPE_INTERLEAVED 1   /* pairs (x[2i], x[2i + 1])        */

@@ -58,8 +58,19 @@ hipError_t launch_rope_table(float* co, float* si, int n_pos, const RopeFreqs& f
 hipError_t launch_rope(int dtype, HeadView x, HeadOut y, const int32_t* pos, int rows, int heads, int hd,
                        const RopeTable& t, bool inverse, hipStream_t st) {
   if (rows <= 0 || heads <= 0) return hipSuccess;
-  const dim3 grid(((unsigned)rows + 3) / 4);
   const float sign = inverse ? -1.f : 1.f;
+  constexpr int most = 1 << 25;   // rows of a launch, whose threads have to stay below 2^32
+  if (rows > most) {
+    const int eb = dtype == 1 ? 2 : 4;
+    for (int64_t r = 0; r < rows; r += most) {
+      const hipError_t e = launch_rope(dtype, HeadView{(const char*)x.p + r * x.row * eb, x.row, x.head},
+                                       HeadOut{(char*)y.p + r * y.row * eb, y.row, y.head}, pos + r,
+                                       (int)std::min<int64_t>(most, rows - r), heads, hd, t, inverse, st);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
+  const dim3 grid(((unsigned)rows + 3) / 4);
   const bool vec = rope_vectors(dtype, x, hd, t) && rope_vectors(dtype, HeadView{y.p, y.row, y.head}, hd, t);
 #define RG_ROPE(T, VEC, LAY)                                                                                          \
   return kv8_launch(k_rope<T, VEC, LAY>, grid, dim3(256), st, (const T*)x.p, x.row, x.head, (T*)y.p, y.row, y.head,   \

@@ -8,10 +8,13 @@
 
 // Launches a kernel, timed where the policy's profile asks for it.  Straight
 // through hipLaunchKernel: the chevrons' pushed and popped configuration costs a
-// quarter of a microsecond of the three that a launch takes the host.
+// quarter of a microsecond of the three that a launch takes the host.  Launches of
+// 2^32 threads and more in a dimension, which hipLaunchKernel would wrap without
+// an error, are refused here.
 template <typename T> struct KernelArg { typedef T type; };
 template <typename... Args>
 hipError_t kv8_launch(void (*kernel)(Args...), dim3 grid, dim3 block, hipStream_t st, typename KernelArg<Args>::type... args) {
+  if ((uint64_t)grid.x * block.x >> 32 || (uint64_t)grid.y * block.y >> 32) return hipErrorInvalidConfiguration;
   void* p[] = {(void*)&args...};
   hipEvent_t e0, e1;
   const hipError_t e = rg_take_launch_events(&e0, &e1)

@@ -37,3 +37,15 @@ def test_offsets_that_do_not_start_at_zero(first, old):
     rg.kv8_attention(b.cache, q, *args, out=out)
     alone = rg.kv8_attention(b.cache, q[own], args[0], args[1], offsets(new))
     assert torch.equal(out[own], alone) and torch.all(out[~own] == 5.0)
+
+
+def test_more_rows_than_a_launch_has_threads():
+    """Rotary positions of 2^26 rows and more: each row gets what it gets in a small call."""
+    import paper_2606_02218_amd as rg
+    rows, step = 2 ** 26 + 2 ** 25 + 5, 2 ** 24
+    cos, sin = rg.rope_table(5, 2)
+    x = torch.randn(rows, 1, 2, device="cuda", dtype=BF16)
+    pos = torch.randint(0, 5, (rows,), device="cuda", dtype=torch.int32)
+    y = rg.rope(x, pos, cos, sin)
+    for a in range(0, rows, step):
+        assert torch.equal(y[a:a + step], rg.rope(x[a:a + step], pos[a:a + step], cos, sin))
