@@ -543,6 +543,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
     if (x.id < 0) {                 // a page the pool has not: its keys are NaN, its values 0
       x.k = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
       x.v = u32x4_t{0, 0, 0, 0};
+      x.ks = x.vs = 1.f;            // not those of the block that was read in its place
     }
     if (has_k) {
 #pragma unroll

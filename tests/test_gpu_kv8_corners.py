@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from kv8_helpers import BF16, Batch, dev, offsets, rounded
+from kv8_helpers import BF16, F32, Batch, dev, offsets, rounded
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,32 @@ def test_more_rows_than_a_launch_has_threads():
     y = rg.rope(x, pos, cos, sin)
     for a in range(0, rows, step):
         assert torch.equal(y[a:a + step], rg.rope(x[a:a + step], pos[a:a + step], cos, sin))
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), 1.0])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_lost_pages_leave_the_rows_before_them_alone(hd, scale):
+    """A run whose last pages are none of the pool's, in a cache whose pages of nobody hold any scales: rows before the
+    lost tokens are as ever, the others NaN."""
+    import paper_2606_02218_amd as rg
+    b = Batch([150], 1, hd, 16, capacity=160, seed=hd)
+    nobody = np.setdiff1d(np.arange(b.pages), b.tab)
+    moved = b.tab[0].copy()
+    at0 = np.flatnonzero(moved == 0)
+    if len(at0):                                              # page 0 belongs to nobody too
+        moved[at0[0]], nobody[0] = nobody[0], 0
+        b.tab[0] = moved
+        b.write()
+    for t in (b.cache.k_scale, b.cache.v_scale):
+        t[dev(nobody)] = scale
+    for bad in (-1, b.pages):
+        tab = b.tab.copy()
+        tab[0, 6:] = bad                                      # tokens 96 and up
+        for dtype in (BF16, F32):
+            for new in (150, 60):
+                q = dev(b.rng.normal(size=(new, 3, hd)).astype(np.float32), dtype)
+                out = rg.kv8_attention(b.cache, q, dev(tab), dev(b.lengths()), offsets([new]))
+                fine = rg.kv8_attention(b.cache, q, dev(b.tab), dev(b.lengths()), offsets([new]))
+                lost = torch.arange(150 - new, 150, device="cuda") >= 96
+                assert torch.all(fine.isfinite())
+                assert torch.all(out[lost].isnan()) and torch.equal(out[~lost], fine[~lost]), (bad, dtype, new)
