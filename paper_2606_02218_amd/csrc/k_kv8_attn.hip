@@ -47,16 +47,22 @@ constexpr int q_pieces(int out) { return out == OUT_F32 ? 3 : out == OUT_PLANES 
 constexpr int p_pieces(int out, bool tiles) { return out == OUT_F32 ? 3 : out == OUT_PLANES || !tiles ? 2 : 1; }
 
 // Eight fp32 values as N bf16 operands whose sum they are: rounded, then what
-// rounding left (8, 17 or all 24 bits; each difference is exact in fp32).
-template <int N>
+// rounding left (8, 17 or all 24 bits; each difference is exact in fp32).  LARGE:
+// values that would round past bf16's largest start with that one instead (what is
+// left of infinities and NaN becomes NaN in the third piece).
+template <int N, bool LARGE = false>
 __device__ __forceinline__ void operand8(const float* v, bf16x8_t (&out)[N]) {
+  constexpr float top = 3.38953139e38f;       // 2^128 - 2^120
   uint32_t w[N][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float a = v[2 * i], b = v[2 * i + 1];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      w[n][i] = pack_bf16x2(a, b);
+      if (LARGE && n == 0)
+        w[n][i] = pack_bf16x2(__builtin_amdgcn_fmed3f(a, -top, top), __builtin_amdgcn_fmed3f(b, -top, top));
+      else
+        w[n][i] = pack_bf16x2(a, b);
       if (n + 1 < N) {
         a -= __uint_as_float(w[n][i] << 16);
         b -= __uint_as_float(w[n][i] & 0xFFFF0000u);
@@ -79,7 +85,7 @@ __device__ __forceinline__ void query8(const T* p, bool valid, bool vec, bf16x8_
   } else {
     ld_elems<8, false>(p, v);
   }
-  operand8<N>(v, out);
+  operand8<N, N == 3>(v, out);
 }
 
 // N consecutive outputs of (row, head) from dim d on.
@@ -269,7 +275,7 @@ __global__ __launch_bounds__(64 * W, (sizeof(T) == 2 || HD == 64 ? 4 : 3) * 4 / 
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(raw[kk][e / 4][e & 3]);
-      operand8<QP>(v, qf[kk]);
+      operand8<QP, QP == 3>(v, qf[kk]);
     }
   }
   for (int i = 0; i < mine; ++i) {

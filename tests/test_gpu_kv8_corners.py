@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from kv8_helpers import BF16, F32, Batch, dev, offsets, rounded
+from kv8_helpers import BF16, F32, Batch, attention_bound, dev, host, offsets, rounded
+from oracle import kv8
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +79,38 @@ def test_lost_pages_leave_the_rows_before_them_alone(hd, scale):
                 lost = torch.arange(150 - new, 150, device="cuda") >= 96
                 assert torch.all(fine.isfinite())
                 assert torch.all(out[lost].isnan()) and torch.equal(out[~lost], fine[~lost]), (bad, dtype, new)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_the_largest_fp32_queries(hd):
+    """Queries up to fp32's largest value, which no bf16 is near: beside keys of 0 they do not count, beside small keys
+    their scores are held to what any other's are."""
+    import paper_2606_02218_amd as rg
+    top = float(np.finfo(np.float32).max)
+    b = Batch([0, 0], 2, hd, 16, capacity=80, seed=hd)
+    for s, n in enumerate((70, 33)):
+        k = rounded(b.rng.normal(size=(n, 2, hd)), F32)
+        k[:, :, :4] = 0.0
+        b.k[s].append(k)
+        b.v[s].append(rounded(b.rng.normal(size=(n, 2, hd)), F32))
+    b.write()
+    large = np.array([top, -top, 3.396e38, np.float32(2.0 ** 128 - 2.0 ** 119)])
+    for new in ([1, 1], [40, 9]):
+        q = rounded(b.rng.normal(size=(sum(new), 4, hd)), F32)
+        q[:, :, :4] = large
+        off = None if new == [1, 1] else offsets(new)
+        out = rg.kv8_attention(b.cache, dev(q, F32), dev(b.tab), dev(b.lengths()), off)
+        q[:, :, :4] = 0.0
+        assert torch.equal(out, rg.kv8_attention(b.cache, dev(q, F32), dev(b.tab), dev(b.lengths()), off))
+    # small keys: scores of up to about 8
+    c = Batch([0], 1, hd, 16, capacity=64, seed=hd + 1)
+    c.k[0].append(rounded(c.rng.normal(size=(50, 1, hd)) * 2.0 ** -60, F32))
+    c.v[0].append(rounded(c.rng.normal(size=(50, 1, hd)), F32))
+    c.write()
+    scale = 2.0 ** -66
+    for new in (1, 20):
+        q = rounded(c.rng.uniform(-1, 1, (new, 2, hd)) * top, F32)
+        q[:, :, :3] = top, -top, 3.396e38
+        out = host(rg.kv8_attention(c.cache, dev(q, F32), dev(c.tab), dev(c.lengths()), offsets([new]), scale=scale))
+        ref, mass, reach = kv8.attend(q, c.k[0].values(), c.v[0].values(), np.arange(50 - new, 50), scale)
+        assert np.all(np.abs(out - ref) <= attention_bound(ref, mass, reach, hd, 50, scale, F32, 2.0 ** -24))
