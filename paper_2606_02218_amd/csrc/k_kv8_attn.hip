@@ -549,7 +549,6 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
     if (x.id < 0) {                 // a page the pool has not: its keys are NaN, its values 0
       x.k = u32x4_t{KV8_NAN4, KV8_NAN4, KV8_NAN4, KV8_NAN4};
       x.v = u32x4_t{0, 0, 0, 0};
-      x.ks = x.vs = 1.f;            // not those of the block that was read in its place
     }
     if (has_k) {
 #pragma unroll
@@ -569,9 +568,12 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
         if (lane == 0) sNan[buf][wave] = any;
       }
       const int tg = piece / (HD / 4), x4 = piece % (HD / 4);   // tokens 4 tg .., dims 4 x4 ..
+      // a lost page's zeros do not take the scale of the block that was read in its place; in a scalar register,
+      // as a vector one more costs bf16 rows 12 % (649 -> 730 us)
+      const float vs = x.id < 0 ? 1.f : __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x.vs)));
 #pragma unroll
       for (int d = 0; d < 4; ++d)
-        reinterpret_cast<u32x2_t*>(&sV[buf][wblk][tg & 1][d % DT][(4 * x4 + d) / DT])[tg >> 1] = kv8_bf16x4(x.v[d], x.vs);
+        reinterpret_cast<u32x2_t*>(&sV[buf][wblk][tg & 1][d % DT][(4 * x4 + d) / DT])[tg >> 1] = kv8_bf16x4(x.v[d], vs);
     }
   };
   // NaN values among the 32 tokens of a piece: those that a column does see make
