@@ -463,7 +463,9 @@ int64_t rg_kv8_attention_scratch(int32_t n_q, int32_t n_kv, int32_t head_dim, in
  * probabilities; bf16 queries are multiplied as they are, their probabilities as
  * 17 bits (single rows) or bf16 (batches of four rows a sequence or more, whose
  * rows share what is staged of a sequence: single rows of long contexts belong
- * into a call of their own).  Padding rows get zeros; a row that needs a page
+ * into a call of their own).  Sequences without rows count among n_seqs here: a
+ * few long runs beside many empty ones are faster without those (tab_row picks
+ * the others).  Padding rows get zeros; a row that needs a page
  * outside the table or the pool gets NaN.  Tokens past a row's position do not
  * touch it, whatever their codes.  RG_EINVAL for NULL pointers, bad sizes, n_q
  * not a multiple of n_kv, or too little scratch; RG_EUNSUPPORTED for more than

@@ -126,6 +126,7 @@ struct rg_policy {
 
   int32_t* h_stage = nullptr;  // pinned staging for host inputs
   int32_t* h_ring = nullptr;   // pinned [RG_RING][8] state snapshots
+  int32_t* h_coff = nullptr;   // kv8: pinned [max_seqs + 1] row offsets of a recompute
   hipEvent_t ring_ev[RG_RING]{};
 
   std::vector<void*> allocs;
@@ -163,6 +164,7 @@ struct rg_policy {
     for (void* p : allocs) (void)hipFree(p);
     if (h_stage) (void)hipHostFree(h_stage);
     if (h_ring) (void)hipHostFree(h_ring);
+    if (h_coff) (void)hipHostFree(h_coff);
     for (auto& e : ring_ev) if (e) (void)hipEventDestroy(e);
     for (auto& e : prof_ev) if (e) (void)hipEventDestroy(e);
     for (auto& e : phase_ev) if (e) (void)hipEventDestroy(e);
@@ -302,13 +304,19 @@ Kv8Rows kv8_steps(const rg_policy* pol, const int* d_rows, int rows_ub) {
   return Kv8Rows{pol->page_tab, pol->lim.max_seqs + pol->lim.max_prompts, pol->max_pages, pol->row_tab, nullptr,
                  pol->row_pos, 1, rows_ub, rows_ub, d_rows};
 }
-Kv8Rows kv8_runs(const rg_policy* pol, int tab0, const int32_t* off, const int32_t* len, int n_seqs, int rows) {
-  return Kv8Rows{pol->page_tab + (int64_t)tab0 * pol->max_pages, n_seqs, pol->max_pages, nullptr, off, len, 0, n_seqs,
-                 rows, nullptr};
+struct Kv8Runs {
+  Kv8Rows batch;
+  int filled;   // sequences that have rows
+};
+Kv8Runs kv8_runs(const rg_policy* pol, int tab0, const int32_t* off, const int32_t* len, int n_seqs, int filled, int rows) {
+  return Kv8Runs{Kv8Rows{pol->page_tab + (int64_t)tab0 * pol->max_pages, n_seqs, pol->max_pages, nullptr, off, len, 0,
+                         n_seqs, rows, nullptr},
+                 filled};
 }
 
 // RoPE, append and attention of layer l over an 8-bit cache: qkv_buf -> abuf2.
-int kv8_layer(rg_policy* pol, hipStream_t st, int l, const Kv8Rows& batch, int ctx_max, bool tiles) {
+// filled: the batch's sequences that have rows.
+int kv8_layer(rg_policy* pol, hipStream_t st, int l, const Kv8Rows& batch, int filled, int ctx_max, bool tiles) {
   const int64_t skip = l * pol->layer_blocks;
   Kv8Attn at{};
   at.c = pol->kv8_pool;
@@ -331,7 +339,7 @@ int kv8_layer(rg_policy* pol, hipStream_t st, int l, const Kv8Rows& batch, int c
   at.scale = 1.0f / std::sqrt((float)pol->hd);
   at.part_o = pol->att_o;
   at.part_ml = pol->att_ml;
-  at.plan = kv8_plan(batch.rows, batch.n_seqs, batch.seq_off != nullptr, tiles, pol->nq, pol->nkv, ctx_max,
+  at.plan = kv8_plan(batch.rows, filled, batch.seq_off != nullptr, tiles, pol->nq, pol->nkv, ctx_max,
                      (int)std::max<int64_t>(1, std::min<int64_t>(pol->att_rowchunks / batch.rows, INT32_MAX)));
   LAUNCH_TIMED(RG_K_ATTN, launch_kv8_attention(RG_DTYPE_F32, true, at, st));
   if (at.plan.n_split > 1) LAUNCH_TIMED(RG_K_ATTN_MERGE, launch_kv8_merge(RG_DTYPE_F32, true, at, st));
@@ -347,7 +355,7 @@ int kv8_layer(rg_policy* pol, hipStream_t st, int l, const Kv8Rows& batch, int c
 // residual stream after the last block.  An 8-bit cache takes prefill-style rows
 // as `runs` (appended whole; attended to by tiles where `tiles` is given too).
 int run_layers(rg_policy* pol, hipStream_t st, const int* d_rows, int rows_ub, int ctx_max, bool final_norm_rows,
-               const PrefixPass* pre, const RowTiles* tiles = nullptr, const Kv8Rows* runs = nullptr) {
+               const PrefixPass* pre, const RowTiles* tiles = nullptr, const Kv8Runs* runs = nullptr) {
   if (rows_ub <= 0) return RG_OK;
   const int tab_stride = pol->max_pages;
   const int n_chunks = att_row_chunks(rows_ub, pol->nkv, ctx_max);
@@ -384,7 +392,9 @@ int run_layers(rg_policy* pol, hipStream_t st, const int* d_rows, int rows_ub, i
                    qkv, &ssq_n)))
       return rc;
     if (pol->kv8) {
-      if ((rc = kv8_layer(pol, st, l, runs ? *runs : kv8_steps(pol, d_rows, rows_ub), ctx_max, runs && tiles))) return rc;
+      if ((rc = kv8_layer(pol, st, l, runs ? runs->batch : kv8_steps(pol, d_rows, rows_ub), runs ? runs->filled : rows_ub,
+                          ctx_max, runs && tiles)))
+        return rc;
     } else if (tiles) {
       LAUNCH_TIMED(RG_K_ATTN, launch_attention_tile(pol->qbuf, pol->nq, pol->nkv, pol->hd, pol->kv_pool, pol->geom, l,
                                                     pol->page_tab, tab_stride, pol->row_tab, pol->row_pos,
@@ -603,7 +613,7 @@ int prefill_and_fork(rg_policy* pol, hipStream_t st, const GroupRun& gr, const i
   if (use_tiles && !pol->kv8)
     LAUNCH(RG_K_SETUP, launch_row_tiles(pol->prompt_off, P, 0, gr.T_pre, tile_rows, d_pre, pol->tile_r0, pol->tile_nr,
                                         d_tiles, st));
-  const Kv8Rows runs = kv8_runs(pol, N, pol->prompt_off, pol->plen, P, gr.T_pre);
+  const Kv8Runs runs = kv8_runs(pol, N, pol->prompt_off, pol->plen, P, P, gr.T_pre);
   int rc = run_layers(pol, st, d_pre, gr.T_pre, gr.max_plen, false, nullptr, use_tiles ? &rt : nullptr,
                       pol->kv8 ? &runs : nullptr);
   if (rc) return rc;
@@ -935,6 +945,7 @@ int rg_policy_create_kv(const rg_config* cfg, const rg_weights* w, const rg_limi
     hipError_t e = hipHostMalloc((void**)&pol->h_stage, (size_t)(2 * P + S + 64) * 4, hipHostMallocDefault);
     if (e != hipSuccess) return bail(fail(RG_EHIP, std::string("hipHostMalloc: ") + hipGetErrorString(e)));
     e = hipHostMalloc((void**)&pol->h_ring, (size_t)RG_RING * 8 * 4, hipHostMallocDefault);
+    if (e == hipSuccess && pol->kv8) e = hipHostMalloc((void**)&pol->h_coff, (size_t)(S + 1) * 4, hipHostMallocDefault);
     if (e != hipSuccess) return bail(fail(RG_EHIP, std::string("hipHostMalloc: ") + hipGetErrorString(e)));
     for (auto& ev : pol->ring_ev) {
       e = hipEventCreateWithFlags(&ev, hipEventDisableTiming);
@@ -1126,6 +1137,8 @@ int recompute_logprobs(rg_policy* pol, const int32_t* prompts, const int32_t* pr
   ra.page_tab = pol->page_tab; ra.free_stack = pol->free_stack; ra.coff = pol->coff; ra.state = pol->state;
   LAUNCH(RG_K_SETUP, launch_reserve(ra, st));
   HIPTRY(hipMemcpyAsync(pol->h_ring, pol->state, 16 * sizeof(int32_t), hipMemcpyDeviceToHost, st));
+  const int32_t* coff = pol->h_coff;
+  if (pol->kv8) HIPTRY(hipMemcpyAsync(pol->h_coff, pol->coff, (size_t)(N + 1) * 4, hipMemcpyDeviceToHost, st));
   HIPTRY(hipStreamSynchronize(st));
   if (pol->h_ring[2]) return fail(RG_ENOMEM, "recompute_logprobs: the KV page pool ran out");
   if (pol->h_ring[10]) return fail(RG_EINVAL, "recompute_logprobs: a length is outside [1, max_new]");
@@ -1162,10 +1175,16 @@ int recompute_logprobs(rg_policy* pol, const int32_t* prompts, const int32_t* pr
     if (use_tiles && !pol->kv8)
       LAUNCH(RG_K_SETUP, launch_row_tiles(pol->coff, N, (int)r0, n, tile_rows, d_chunk, pol->tile_r0, pol->tile_nr,
                                           d_tiles, st));
-    if (pol->kv8)
-      LAUNCH(RG_K_SETUP, launch_kv8_runs(pol->coff, pol->plen, pol->seq_grp, N, (int)r0, n, pol->run_off, pol->run_len,
-                                         st));
-    const Kv8Rows runs = kv8_runs(pol, 0, pol->run_off, pol->run_len, N, n);
+    Kv8Runs runs{};
+    if (pol->kv8) {   // sequences s0 .. s1 - 1, from the one that holds the chunk's first row to the one with its last
+      const int s0 = (int)(std::upper_bound(coff, coff + N + 1, (int32_t)r0) - coff) - 1;
+      const int s1 = (int)(std::lower_bound(coff, coff + N + 1, (int32_t)(r0 + n)) - coff);
+      int filled = 0;
+      for (int s = s0; s < s1; ++s) filled += coff[s + 1] > coff[s];
+      LAUNCH(RG_K_SETUP, launch_kv8_runs(pol->coff + s0, pol->plen, pol->seq_grp + s0, s1 - s0, (int)r0, n, pol->run_off,
+                                         pol->run_len, st));
+      runs = kv8_runs(pol, s0, pol->run_off, pol->run_len, s1 - s0, filled, n);
+    }
     if ((rc = run_layers(pol, st, d_chunk, n, ctx_all, true, nullptr, use_tiles ? &rt : nullptr,
                          pol->kv8 ? &runs : nullptr)))
       return rc;

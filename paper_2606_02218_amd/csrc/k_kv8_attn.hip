@@ -810,8 +810,13 @@ hipError_t merge(const Kv8Attn& a, hipStream_t st) {
 
 }  // namespace
 
-// Rows or tiles: a tile's 128 query rows pay from a few rows a sequence on; below,
-// the rows pass keeps the matrix units no busier than the memory.
+// Rows or tiles: a tile's 128 query rows pay from four rows on for each sequence that
+// has rows.  Rows pass / tiles of bf16 runs, 2 kv heads of 6 query heads, us: 256
+// sequences of 600 tokens with 2, 4 and 8 rows each 22/28, 32/29, 54/32; 64 of 10000
+// tokens 71/102, 114/108, 227/118.  Sequences without rows do not count where they are
+// known: a recompute of 2048 sequences of 2 to 600 tokens behind 512, 4096 rows a
+// launch, takes 141/52 (a bf16 pool's 68).  Batches that leave the chip idle either way
+// lose by it: 8 sequences of 600 tokens with 4 to 32 rows each 7/21 to 11/23.
 //
 // Waves of a rows workgroup: eight where one round of a workgroup a CU holds them
 // all (a row's chain of steps is then what the launch waits for: 8 rows of 12 heads

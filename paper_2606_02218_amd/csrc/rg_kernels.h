@@ -427,7 +427,8 @@ struct Kv8Plan {
   int deal;    // rows by length, whose 32-token steps have this many bits; 0: as they come
   int n_split, chunk;
 };
-// has_off: the batch has offsets; tiles: it may go by tiles then.
+// n_seqs: of the sequences, those that have rows where the caller knows; has_off: the
+// batch has offsets; tiles: it may go by tiles then.
 Kv8Plan kv8_plan(int rows, int n_seqs, bool has_off, bool tiles, int n_q, int n_kv, int max_len, int max_split);
 struct Kv8Attn {
   Kv8Pool c;
@@ -447,9 +448,9 @@ inline int64_t kv8_part_floats(int64_t rows, const Kv8Plan& p, int n_q, int hd) 
 // The pass over the cache; with n_split > 1 launch_kv8_merge has to follow.
 hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStream_t st);
 hipError_t launch_kv8_merge(int dtype, bool planes, const Kv8Attn& a, hipStream_t st);
-// Rows row0 .. row0 + n - 1 of a teacher-forced forward as a batch of all
-// n_seq sequences (coff as in ReserveArgs): off [n_seq + 1], and the tokens that
-// each has once those rows are appended.
+// Rows row0 .. row0 + n - 1 of a teacher-forced forward as a batch of n_seq
+// sequences (coff as in ReserveArgs, from the first of them on): off [n_seq + 1],
+// and the tokens that each has once those rows are appended.
 hipError_t launch_kv8_runs(const int32_t* coff, const int32_t* plen, const int32_t* seq_grp, int n_seq, int row0, int n,
                            int32_t* off, int32_t* len, hipStream_t st);
 // The blocks and scales of every layer for the fork's page copies; layer l of
