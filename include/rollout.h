@@ -423,7 +423,8 @@ typedef struct rg_kv8_batch {
 
 /* Appends the rows' keys and values, keys turned by their positions first
  * (rot_dim > 0; 0: as they are), and turns the queries on the way (q != NULL)
- * into q_out, which may be q.
+ * into q_out, which may be q (same address and strides) and otherwise must share
+ * no element with k, v or q: they are read while it is written.
  *   k, v     views [rows, n_kv, head_dim];  q, q_out  views [rows, n_q, head_dim]
  * A block's scale is 2^e, e the least in [-64, 119] with 448 * 2^e >= the
  * largest finite magnitude among its new rows (of keys after turning), or its
@@ -436,8 +437,8 @@ typedef struct rg_kv8_batch {
  * a shared prefix before its owners append).  Rows whose page is not in the
  * table or not in [0, pages) are dropped; a key whose position lies outside
  * [0, n_pos) becomes NaN; padding rows are skipped, q_out included.  RG_EINVAL
- * for NULL pointers, bad sizes, n_q not a multiple of n_kv, or rot_dim and layout
- * as in rg_rope. */
+ * for NULL pointers, bad sizes, n_q not a multiple of n_kv, a q_out that overlaps, or
+ * rot_dim and layout as in rg_rope. */
 int rg_kv8_append(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* k, int64_t k_row,
                   int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const void* q, int64_t q_row,
                   int64_t q_head, void* q_out, int64_t qo_row, int64_t qo_head, int32_t n_q, const float* cos_tab,

@@ -407,7 +407,8 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
     """Appends keys and values (bf16 or fp32 [rows, n_kv, head_dim], rows and
     heads at any strides) to their sequences in ``cache``, keys turned by their
     positions with the rope_table (cos, sin) where one is given, and returns q
-    turned likewise (into ``q_out``, which may be q), or None without q.
+    turned likewise (into ``q_out``, which may be q but must not overlap k, v or q
+    in any other way), or None without q.
       page_tab  int32 [sequences, pages]: each sequence's pages in order
                 (``tab_row`` int32 [sequences] picks rows of a larger table)
       seq_len   int32 [sequences]: tokens of each, the new rows counted

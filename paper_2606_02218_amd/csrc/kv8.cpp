@@ -1,7 +1,9 @@
 // C entry points of the rotary positions and the 8-bit key/value cache
 // (include/rollout.h): argument checks, then the launchers.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <cstdlib>
 
 #include "rollout.h"
 #include "rg_kernels.h"
@@ -21,6 +23,36 @@ int launched(const char* who, hipError_t e) {
 }
 
 bool aligned(const void* p) { return (uintptr_t)p % 16 == 0; }
+
+// Whether two views of `rows` rows, hd elements of eb bytes a head, share an element.
+// Where their ranges meet, as those of parts of one projection's output do, each
+// pair of heads is compared over the rows; rows that do not go in step are taken to
+// meet.  (More pairs of heads than any model has: not looked at.)
+bool overlap(const HeadView& a, int a_heads, const HeadView& b, int b_heads, int rows, int hd, int eb) {
+  auto range = [&](const HeadView& x, int heads, int64_t& lo, int64_t& hi) {
+    const int64_t r = (rows - 1) * x.row, h = (heads - 1) * x.head;
+    lo = (int64_t)x.p + eb * (std::min<int64_t>(r, 0) + std::min<int64_t>(h, 0));
+    hi = (int64_t)x.p + eb * (std::max<int64_t>(r, 0) + std::max<int64_t>(h, 0) + hd);
+  };
+  int64_t al, ah, bl, bh;
+  range(a, a_heads, al, ah);
+  range(b, b_heads, bl, bh);
+  if (ah <= bl || bh <= al) return false;
+  if (rows > 1 && a.row != b.row) return true;
+  if ((int64_t)a_heads * b_heads > 1 << 20) return false;
+  const int64_t wide = (int64_t)hd * eb, step = rows > 1 ? std::abs(a.row) * eb : 0;
+  for (int i = 0; i < a_heads; ++i)
+    for (int j = 0; j < b_heads; ++j) {
+      int64_t d = std::abs((int64_t)b.p + j * b.head * eb - (int64_t)a.p - i * a.head * eb);   // and rows apart: d - n * step
+      if (step) {
+        const int64_t n = std::min<int64_t>(d / step, rows - 1);
+        d -= n * step;
+        if (n + 1 < rows) d = std::min(d, step - d);
+      }
+      if (d < wide) return true;
+    }
+  return false;
+}
 
 // Every host check of a cache and a batch; fills the kernels' forms.
 int cache_args(const char* who, const rg_kv8_cache* c, const rg_kv8_batch* b, int32_t dtype, Kv8Pool* pool,
@@ -113,6 +145,15 @@ int rg_kv8_append(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t 
   if (!k || !v) return bad(who, "NULL k or v");
   if (q && !q_out) return bad(who, "NULL q_out");
   if (q && q == q_out && (q_row != qo_row || q_head != qo_head)) return bad(who, "q_out overlaps q with other strides");
+  if (q) {   // keys, values and queries are taken by different waves, in any order
+    const int eb = dtype == RG_DTYPE_BF16 ? 2 : 4, n = rows.rows;
+    const HeadView o{q_out, qo_row, qo_head};
+    if (overlap(o, n_q, HeadView{k, k_row, k_head}, pool.n_kv, n, pool.hd, eb) ||
+        overlap(o, n_q, HeadView{v, v_row, v_head}, pool.n_kv, n, pool.hd, eb))
+      return bad(who, "q_out overlaps k or v");
+    if (q != q_out && overlap(o, n_q, HeadView{q, q_row, q_head}, n_q, n, pool.hd, eb))
+      return bad(who, "q_out overlaps q without being q");
+  }
   return launched(who, launch_kv8_append(dtype, pool, rows, HeadView{k, k_row, k_head}, HeadView{v, v_row, v_head},
                                          HeadView{q, q_row, q_head}, HeadOut{q_out, qo_row, qo_head}, n_q, t,
                                          (hipStream_t)stream));

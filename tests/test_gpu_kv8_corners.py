@@ -114,3 +114,32 @@ def test_the_largest_fp32_queries(hd):
         out = host(rg.kv8_attention(c.cache, dev(q, F32), dev(c.tab), dev(c.lengths()), offsets([new]), scale=scale))
         ref, mass, reach = kv8.attend(q, c.k[0].values(), c.v[0].values(), np.arange(50 - new, 50), scale)
         assert np.all(np.abs(out - ref) <= attention_bound(ref, mass, reach, hd, 50, scale, F32, 2.0 ** -24))
+
+
+@pytest.mark.parametrize("rows", [1, 3, 70])
+def test_queries_turned_in_place_in_a_fused_projection(rows):
+    """q, k and v are parts of one buffer and the turned queries go where the queries were: the cache and the queries are
+    those of a call on copies; an output that overlaps anything else is refused and writes nothing."""
+    import paper_2606_02218_amd as rg
+    cos, sin = rg.rope_table(100, 64)
+    b = Batch([20], 2, 64, 16, capacity=100, seed=rows)
+    base = dev(b.rng.normal(size=(rows, 10, 64)).astype(np.float32), BF16)
+    heads = base.transpose(0, 1).contiguous().transpose(0, 1)
+    ln = dev(b.lengths() + rows)
+    keep = [t.clone() for t in b.cache]
+    got = []
+    for x in (base, base.clone(), heads):
+        for t, u in zip(b.cache, keep):
+            t.view(torch.uint8).copy_(u.view(torch.uint8))
+        q, k, v = x[:, :6], x[:, 6:8], x[:, 8:]
+        before = x.clone()
+        with pytest.raises(rg.RolloutError, match="overlaps"):
+            rg.kv8_append(b.cache, k, v, dev(b.tab), ln, offsets([rows]), q=q, cos=cos, sin=sin, q_out=x[:, 1:7])
+        assert torch.equal(x, before)
+        if x is base:
+            q, k, v = q.clone(), k.clone(), v.clone()
+        out = rg.kv8_append(b.cache, k, v, dev(b.tab), ln, offsets([rows]), q=q, cos=cos, sin=sin, q_out=q)
+        assert out is q and (x is base or torch.equal(x[:, 6:], before[:, 6:]))
+        got.append([q.clone()] + [t.view(torch.uint8).clone() for t in b.cache])
+    for other in got[1:]:
+        assert all(torch.equal(a, c) for a, c in zip(got[0], other))
