@@ -181,8 +181,9 @@ void rg_policy_destroy(rg_policy* pol);   /* NULL is a no-op */
  * RG_KV_E4M3 is for bf16 models: the pool takes half the bytes and decode
  * attention reads half; a key or value is then good to 2^-4 of itself in place of
  * 2^-9, in rollout_group and recompute_logprobs alike, and a token's stored form
- * may be rounded once more as its block of 16 fills (where a later token raises
- * the block's scale and pushes it among the subnormal codes).  The two calls
+ * is rounded again with every later token that raises the scale of its block of 16
+ * (up to 15 times in a decode; it moves where that pushes it among the subnormal
+ * codes, in all by less than 2^-9 of the last scale, a step of those).  The two calls
  * then agree up to that: recompute_logprobs stores a completion's rows at once.
  * RG_FLAG_GROUP_PREFIX has no effect.  Errors as rg_policy_create;
  * RG_EUNSUPPORTED for another kv_type or for an fp32 model. */
