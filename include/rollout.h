@@ -456,7 +456,8 @@ int64_t rg_kv8_attention_scratch(int32_t n_q, int32_t n_kv, int32_t head_dim, in
  *   out = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale * q.k_j),  j = 0 .. p.
  *   q        view [rows, n_q, head_dim], turned already
  *   out      DEVICE [rows, n_q, head_dim] dense, in dtype, 16-byte aligned
- *   scale    > 0, finite (usually 1/sqrt(head_dim))
+ *   scale    > 0, at most 2.3e38 (usually 1/sqrt(head_dim)); q.k or scale * q.k past
+ *            fp32's range have no weight below it and make their head NaN above
  *   max_len  bound on seq_len[], >= 1: it sizes the launch; longer sequences
  *            are still computed whole
  *   scratch  DEVICE, 16-byte aligned, of rg_kv8_attention_scratch() bytes, that

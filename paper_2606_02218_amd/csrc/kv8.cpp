@@ -177,7 +177,8 @@ int rg_kv8_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32
   if (rc) return rc;
   if (n_q < 1 || n_q % a.c.n_kv) return bad(who, "n_q must be a multiple of n_kv");
   if (n_q / a.c.n_kv > 128) return bad(who, "more than 128 query heads per kv head", RG_EUNSUPPORTED);
-  if (!(scale > 0.f) || !std::isfinite(scale)) return bad(who, "scale must be > 0 and finite");
+  // scores are taken in base 2: 0 times an infinite factor would be NaN
+  if (!(scale > 0.f) || !std::isfinite(scale * 1.44269504f)) return bad(who, "scale must be > 0 and at most 2.3e38");
   if (max_len < 1) return bad(who, "max_len < 1");
   if (a.b.rows == 0) return RG_OK;
   if (!q || !out) return bad(who, "NULL q or out");

@@ -143,3 +143,19 @@ def test_queries_turned_in_place_in_a_fused_projection(rows):
         got.append([q.clone()] + [t.view(torch.uint8).clone() for t in b.cache])
     for other in got[1:]:
         assert all(torch.equal(a, c) for a, c in zip(got[0], other))
+
+
+def test_the_largest_scale():
+    """Scores of 0 times it are 0: the values' mean, to the outputs' rounding and that of n fp32 sums."""
+    import paper_2606_02218_amd as rg
+    b = Batch([50, 20], 2, 64, 16, seed=3)
+    for new in ([1, 1], [20, 5]):
+        q = torch.zeros(sum(new), 4, 64, device="cuda")
+        out = host(rg.kv8_attention(b.cache, q, dev(b.tab), dev(b.lengths()), offsets(new), scale=2.3e38))
+        r = 0
+        for s, n in enumerate((50, 20)):
+            for p in range(n - new[s], n):
+                v = b.v[s].values()[:p + 1]
+                ref = np.repeat(v.mean(0), 2, 0)
+                assert np.all(np.abs(out[r] - ref) <= (p + 4) * 2.0 ** -23 * np.abs(v).mean(0).max())
+                r += 1

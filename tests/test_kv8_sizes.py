@@ -1,5 +1,6 @@
-"""Calls of more work than one launch's 2^32 threads are refused by the library
-before any device work (CPU only; the addresses are stand-ins that nothing reads)."""
+"""Calls of more work than one launch's 2^32 threads, and scales past what fp32
+holds of them, are refused by the library before any device work (CPU only; the
+addresses are stand-ins that nothing reads)."""
 import ctypes as C
 import os
 
@@ -41,3 +42,10 @@ def test_appends_past_a_launch_are_refused(n_kv, rows, seqs, q):
     x = (16, 64, 64, 16, 64, 64) if q else (None, 0, 0, None, 0, 0)
     assert lib.rg_kv8_append(C.byref(c), C.byref(b), 1, 1 << 40, 64, 64, 1 << 41, 64, 64, *x, n_kv, None, None, 0, 0, 0, None) == -3
     assert lib.rg_last_error().decode().split(": ")[1] in REFUSED
+
+
+def test_scales_whose_base_two_form_is_infinite_are_refused():
+    lib, c, b = _call(2, 3, None)
+    for scale in (2.4e38, 3.4e38):
+        assert lib.rg_kv8_attention(C.byref(c), C.byref(b), 1, 16, 128, 64, 4, 32, scale, 64, None, 0, None) == -1
+        assert "scale must be" in lib.rg_last_error().decode()
