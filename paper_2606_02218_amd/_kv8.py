@@ -39,11 +39,11 @@ _ARGS = {
                          C.c_int),
 }
 _ready = None
-_BF16 = _F32 = _E4M3 = _I32 = _device = _raw_stream = _empty_like = None
+_BF16 = _F32 = _E4M3 = _I32 = _device = _raw_stream = _empty_like = _grad_on = _recorded = None
 
 
 def _library():
-    global _ready, _BF16, _F32, _E4M3, _I32, _device, _raw_stream, _empty_like
+    global _ready, _BF16, _F32, _E4M3, _I32, _device, _raw_stream, _empty_like, _grad_on, _recorded
     if _ready is None:
         lib = load_library()
         for name, (args, res) in _ARGS.items():
@@ -52,6 +52,7 @@ def _library():
         import torch
         _BF16, _F32, _E4M3, _I32 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.int32
         _device, _raw_stream, _empty_like = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.empty_like
+        _grad_on, _recorded = torch.is_grad_enabled, _recorded_rope()
         _ready = lib
     return _ready
 
@@ -244,8 +245,30 @@ def rope_table(n_pos: int, rot_dim: int, theta: float = 1e4, scaling: Optional[s
     return cos, sin
 
 
+def _recorded_rope():
+    """rope as a node of an autograd graph: its gradient is the turn the other way."""
+    import torch
+
+    class Rope(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, pos, cos, sin, layout, inverse, stream):
+            ctx.save_for_backward(pos, cos, sin)
+            ctx.turn = layout, inverse
+            return rope(x, pos, cos, sin, layout, inverse, stream=stream)   # grad mode is off here
+
+        @staticmethod
+        def backward(ctx, g):
+            layout, inverse = ctx.turn
+            g = g if g.stride(2) == 1 else g.contiguous()                   # one value expanded, as sum() gives
+            return rope(g, *ctx.saved_tensors, layout, not inverse), None, None, None, None, None, None
+
+    return Rope.apply
+
+
 def _rope_now(lib, x, pos, cos, sin, layout, inverse):
     """The call where every argument is in place, else None."""
+    if (x.requires_grad or cos.requires_grad or sin.requires_grad) and _grad_on():
+        return None
     dt, dev = x.dtype, x.get_device()
     if not ((dt is _BF16 or dt is _F32) and dev >= 0 and _device() == dev and layout in ROPE_LAYOUTS and x.dim() == 3):
         return None
@@ -269,8 +292,9 @@ def rope(x, pos, cos, sin, layout: str = "half", inverse: bool = False, out=None
     """Turns the heads of x (bf16 or fp32 [rows, heads, head_dim], rows and heads
     at any strides) by their rows' positions pos (int32 [rows]); cos and sin are
     a rope_table of at most head_dim dims.  ``inverse=True`` turns back: the
-    gradient with respect to x, given the one with respect to the result (the
-    call itself is not recorded by autograd).
+    gradient with respect to x, given the one with respect to the result.  An x
+    that requires a gradient is recorded so by autograd (without ``out``; the
+    table takes no gradient).
     ``out`` may be x.  See rg_rope in rollout.h."""
     lib = _ready or _library()
     if out is None and stream is None:
@@ -290,6 +314,13 @@ def rope(x, pos, cos, sin, layout: str = "half", inverse: bool = False, out=None
     _dev("pos", pos, _I32, (rows,))
     if out is not None:
         _written("out", _view("out", out, dt, x.shape))
+    if _grad_on():
+        if cos.requires_grad or sin.requires_grad:
+            raise ValueError("cos and sin take no gradient: detach them")
+        if out is not None and (x.requires_grad or out.requires_grad):
+            raise ValueError("with out the call is not recorded and a gradient would be lost: leave it out, or detach x and out")
+        if x.requires_grad:
+            return _recorded(x, pos, cos, sin, layout, inverse, stream)
     _one_device(dict(x=x, pos=pos, cos=cos, sin=sin, out=out))
     dev = x.device
     with _On(dev):
@@ -414,6 +445,7 @@ def kv8_append(cache, k, v, page_tab, seq_len, seq_off=None, q=None, cos=None, s
       seq_len   int32 [sequences]: tokens of each, the new rows counted
       seq_off   int32 [sequences + 1]: each sequence's rows, or None for one
                 row a sequence
+    Not recorded by autograd: the cache and the result carry no gradient.
     See rg_kv8_append in rollout.h for scales, rounding and what padding gets."""
     lib = _ready or _library()
     if q_out is None and stream is None:
@@ -496,7 +528,8 @@ def kv8_attention(cache, q, page_tab, seq_len, seq_off=None, max_len: Optional[i
     bounds seq_len (None: what the page table can hold; a close bound makes
     better launches), ``scale`` defaults to 1/sqrt(head_dim).  Returns
     [rows, n_q, head_dim] in q's dtype, zeros for padding rows; rows past the
-    last sequence's are not written.  See rg_kv8_attention in rollout.h."""
+    last sequence's are not written.  Not recorded by autograd: the result
+    carries no gradient.  See rg_kv8_attention in rollout.h."""
     lib = _ready or _library()
     if out is None and stream is None:
         try:
