@@ -349,7 +349,9 @@ int grpo_surrogate_noalloc(const float* new_lp, const float* old_lp, const float
 #define RG_ROPE_INTERLEAVED 1   /* pairs (x[2i], x[2i + 1])        */
 
 /* Scaling of the frequencies w_i = theta^(-2i/rot_dim), i < rot_dim/2, for
- * contexts beyond the trained length (factor = the context's growth). */
+ * contexts beyond the trained length (factor = the context's growth).  The blend
+ * of RG_ROPE_BANDS goes by a pair's turns, not by its index, and always comes with
+ * its amplitude. */
 #define RG_ROPE_PLAIN  0   /* w_i                                                                     */
 #define RG_ROPE_LINEAR 1   /* w_i / factor: positions interpolated                                    */
 #define RG_ROPE_BASE   2   /* theta raised to theta * factor^(rot_dim/(rot_dim - 2)): the slowest pair
@@ -455,7 +457,8 @@ int64_t rg_kv8_attention_scratch(int32_t n_q, int32_t n_kv, int32_t head_dim, in
  * kv head h / (n_q/n_kv):
  *   out = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale * q.k_j),  j = 0 .. p.
  *   q        view [rows, n_q, head_dim], turned already
- *   out      DEVICE [rows, n_q, head_dim] dense, in dtype, 16-byte aligned
+ *   out      DEVICE [rows, n_q, head_dim] dense, in dtype, 16-byte aligned; may be q
+ *            where that is dense, and must not overlap it otherwise
  *   scale    > 0, at most 2.3e38 (usually 1/sqrt(head_dim)); q.k or scale * q.k past
  *            fp32's range have no weight below it and make their head NaN above
  *   max_len  bound on seq_len[], >= 1: it sizes the launch; longer sequences

@@ -159,3 +159,18 @@ def test_the_largest_scale():
                 ref = np.repeat(v.mean(0), 2, 0)
                 assert np.all(np.abs(out[r] - ref) <= (p + 4) * 2.0 ** -23 * np.abs(v).mean(0).max())
                 r += 1
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [[1, 1], [60, 20]])
+@pytest.mark.parametrize("rep", [3, 40])
+def test_outputs_in_the_place_of_the_queries(dtype, new, rep):
+    """Short and split contexts, single rows and runs, several head tiles."""
+    import paper_2606_02218_amd as rg
+    b = Batch([2600, 90], 2, 64, 16, seed=rep)
+    q = dev(b.rng.normal(size=(sum(new), 2 * rep, 64)).astype(np.float32), dtype)
+    for max_len in (2600, 64):
+        args = dev(b.tab), dev(b.lengths()), offsets(new)
+        want = rg.kv8_attention(b.cache, q, *args, max_len=max_len)
+        x = q.clone()
+        assert rg.kv8_attention(b.cache, x, *args, max_len=max_len, out=x) is x and torch.equal(x, want)
