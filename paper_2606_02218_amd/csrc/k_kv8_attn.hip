@@ -24,8 +24,8 @@
 // * Tiles pass (runs of rows): a workgroup per 128 query rows (positions x heads
 //   of a kv head) and chunk.  32-token pieces go through LDS once for the four
 //   waves of 32 query rows.  Bound by vector issue beside the matrix instructions:
-//   8192 bf16 rows of 28 heads behind 2 to 6 thousand tokens (0.61 Tflop) 624 us,
-//   0.98 of the 1.42 Pflop/s that a large product reaches.
+//   8192 bf16 rows of 28 heads behind 2 to 6 thousand tokens (0.61 Tflop) 630 us,
+//   0.97 of the 1.42 Pflop/s that a large product reaches.
 // * With several chunks a row, a merge joins their partial results in order.
 #include <algorithm>
 #include <type_traits>
@@ -118,7 +118,8 @@ __device__ __forceinline__ float* part_ml(const Kv8Attn& A, int64_t slot, int he
 // its longest row down; every other round of 32 blocks, one for each of its CUs,
 // runs backwards, so that the CUs' sums even out.  512 rows of 512 to 2600 tokens
 // and 2 kv heads: 60 us in place of 68 (47 where all have the same length); over
-// all XCDs instead of within one 69, since siblings then share no L2.
+// all XCDs instead of within one 69, since siblings then share no L2.  Rows that are
+// equal pay for it: 66 us in place of 64.
 //
 // The row of this block of an XCD, its kv head and head tile, tokens and table row;
 // false where there is none.  The row of a rank is found bit by bit of the lengths
@@ -418,7 +419,7 @@ __device__ __forceinline__ uint32_t clear_nan(uint32_t w) {
 // Tile k of a batch, tiles of np rows: among 64 sequences, a lane each, those with
 // the longest contexts come first, so that none of them starts when the others end:
 // 24 fp32 runs of 37 to 701 rows 78 us, 87 with each sequence's tiles in turn; bf16
-// 40 and 46.
+// 40 and 46.  Equal ones pay for it: four of 2048 rows 651 us in place of 643.
 // A sequence of T tiles behind `old` tokens has them at levels old / np + 1 .. old /
 // np + T; level and place of a rank are found bit by bit.  False past the last tile.
 __device__ __forceinline__ bool tile_of(const Kv8Rows& b, int np, int k, int& s, int& r0, int& n, int& skip) {
