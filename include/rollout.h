@@ -51,6 +51,7 @@ extern "C" {
 /* ---- element types ---- */
 #define RG_DTYPE_F32  0
 #define RG_DTYPE_BF16 1
+#define RG_DTYPE_F64  2   /* uniform numbers of rg_sample alone */
 
 /* Decoder shape.  Pre-norm blocks x += Attn(RMSNorm(x)), x += MLP(RMSNorm(x)),
  * final RMSNorm, untied lm_head, no biases.  RMSNorm(x) = x/sqrt(mean(x^2)+eps)*g.
@@ -479,6 +480,121 @@ int64_t rg_kv8_attention_scratch(int32_t n_q, int32_t n_kv, int32_t head_dim, in
 int rg_kv8_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* q,
                      int64_t q_row, int64_t q_head, int32_t n_q, void* out, float scale, int32_t max_len,
                      void* scratch, int64_t scratch_bytes, void* stream);
+
+/* ---- trees of drafted tokens over the 8-bit cache ----
+ * A program that drafts several continuations of a sequence at once checks them in
+ * one forward: a sequence's rows are the nodes of a tree, row i (among the
+ * sequence's own, of n) behind row parent[i] < i, and -1 behind the context, the
+ * tokens held before.  With L = seq_len[s] (the nodes counted), node i lies in slot
+ * L - n + i of the cache, in the order of the rows, and at position L - n + its
+ * depth.  So keys and queries are turned by rg_rope at the positions that
+ * rg_kv8_tree gives, appended without a table by rg_kv8_append, and the nodes
+ * attend by rg_kv8_tree_attention; after the check rg_kv8_accept moves the accepted
+ * path's tokens behind the context.
+ *   A mask is `words` 64-bit words a row, bit i % 64 of word i / 64 for node i of
+ * the row's own sequence; nodes past the last word have no bit.  rg_kv8_tree sets a
+ * node's own bit and its ancestors'; any other mask does as well.
+ *   Where a sequence has more rows than tokens (L < n), the first n - L are padding
+ * and no node's parent; their masks and bits are not looked at.  Rows of nobody
+ * are neither read nor written. */
+#define RG_KV8_TREE_WORDS 64   /* most words of a row's mask */
+
+/* The masks and positions of trees.
+ *   parent    DEVICE int32 [rows]
+ *   seq_off   DEVICE int32 [n_seqs + 1], seq_len DEVICE int32 [n_seqs], as in
+ *             rg_kv8_batch
+ *   mask      DEVICE uint64 [rows, words]
+ *   pos       DEVICE int32 [rows]
+ * Padding rows, rows whose parent is not in [-1, i) and rows behind such a one
+ * get an empty mask and position -1 (rg_rope makes that NaN).  RG_EINVAL for NULL
+ * pointers, negative sizes, words outside [1, 64], n_seqs past 2^24. */
+int rg_kv8_tree(const int32_t* parent, const int32_t* seq_off, const int32_t* seq_len, int32_t n_seqs, int32_t rows,
+                int32_t words, uint64_t* mask, int32_t* pos, void* stream);
+
+/* Bytes of scratch that rg_kv8_tree_attention needs for these sizes (0: none).
+ * Negative (RG_E*) for bad sizes. */
+int64_t rg_kv8_tree_attention_scratch(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rows, int32_t n_seqs,
+                                      int32_t max_len);
+
+/* Attention of the nodes over their sequences' contexts and the nodes that their
+ * masks show them: rg_kv8_attention with j over those tokens, its arguments, limits,
+ * numbers of bits (bf16 queries as they are, their probabilities as bf16; fp32 ones
+ * and theirs with all 24 bits) and errors.  seq_off is required.  A row that sees
+ * nothing, as a padding row, gets zeros; a row that sees a token whose page is not in
+ * the table or the pool gets NaN.  What a row does not see does not touch it, whatever
+ * the codes.
+ *   mask   DEVICE uint64 [rows, words], words in [1, 64] */
+int rg_kv8_tree_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* q, int64_t q_row,
+                          int64_t q_head, int32_t n_q, const uint64_t* mask, int32_t words, void* out, float scale,
+                          int32_t max_len, void* scratch, int64_t scratch_bytes, void* stream);
+
+/* Takes over accepted nodes: of sequence s those that have a bit in the mask of its
+ * node last[s] (rg_kv8_tree's masks: that node and its ancestors) move, in their
+ * order, to the slots behind the context.
+ *   mask      DEVICE uint64 [rows, words]
+ *   last      DEVICE int32 [n_seqs]: the node's number among its sequence's; outside
+ *             [0, n), as -1, none is kept
+ *   new_len   DEVICE int32 [n_seqs]: out, the tokens that are left, context and kept
+ *             nodes.  It must not overlap anything that the call reads.
+ * A block that receives a token takes the largest scale among the tokens that end up
+ * in it.  Their codes are multiplied by old over new scale and rounded to nearest
+ * even: powers of two, so a token keeps its value unless it lands among the subnormal
+ * codes.  NaN stays NaN.  Blocks that receive none, and slots behind new_len, keep
+ * what they hold.  A token whose page is not in the table or the pool arrives as NaN;
+ * one whose new page is not there is dropped.  Each page that receives a token must be
+ * one sequence's alone, as in rg_kv8_append.  The batch's rows say how many nodes each
+ * sequence has; RG_EINVAL as in rg_kv8_append, and for NULL pointers, a missing
+ * seq_off, words outside [1, 64] or an overlapping new_len. */
+int rg_kv8_accept(const rg_kv8_cache* cache, const rg_kv8_batch* batch, const uint64_t* mask, int32_t words,
+                  const int32_t* last, int32_t* new_len, void* stream);
+
+/* ---- sampling from given logits and given random numbers ----
+ * For programs with a decode loop of their own, or nodes of drafted trees to check.
+ * Row by row, of logits z: weights w_i = exp((z_i - max z) / T).  In the order of z,
+ * equal ones by id:
+ *   top_k > 0   keeps the first top_k tokens (0, or vocab and more: all)
+ *   top_p < 1   keeps those before which less than top_p of the weight that top_k
+ *               left lies; the first always
+ *   min_p > 0   keeps those with z_i >= max z + T ln(min_p) (weight min_p or more)
+ * and what all three keep is drawn from: the token is the first, by id, at which the
+ * running sum of the kept weights passes u times their sum.  T = 0 takes the largest
+ * logit, of equal ones the lowest id, whatever the rest. */
+typedef struct rg_sample_options {
+  float temperature;                /* >= 0                                                  */
+  int32_t top_k;                    /* >= 0                                                  */
+  float top_p;                      /* in (0, 1]                                             */
+  float min_p;                      /* in [0, 1]                                             */
+  const float* temperature_rows;    /* DEVICE [rows] or NULL: a row's own in place of the    */
+  const int32_t* top_k_rows;        /* numbers above.  Read by the kernels: top_k < 0 is     */
+  const float* top_p_rows;          /* none, top_p <= 0 keeps the first token, min_p past 1  */
+  const float* min_p_rows;          /* the largest                                           */
+} rg_sample_options;
+
+/* Bytes of scratch that rg_sample needs.  Negative (RG_E*) for bad sizes. */
+int64_t rg_sample_scratch(int32_t rows, int32_t vocab);
+
+/*   logits    DEVICE [rows, vocab] in dtype (fp32 or bf16), rows logits_row elements
+ *             apart; any alignment and stride work, 16-byte ones run faster
+ *   u         DEVICE [rows], fp32 or fp64 (u_dtype), in [0, 1)
+ *   tokens    DEVICE int32 [rows]
+ *   logprobs  DEVICE fp32 [rows]: log-probability of the token under softmax(z / T)
+ *             (T = 0: under softmax(z)), as rollout_group reports it
+ *   kept_logprobs  DEVICE fp32 [rows]: under the distribution that is left to draw
+ *             from (T = 0: 0)
+ *   scratch   DEVICE, 16-byte aligned, of rg_sample_scratch() bytes, that nothing else
+ *             uses until the call's kernels have run
+ * Tokens with logit -inf have weight 0 and are never drawn, nor are those below 2^-43
+ * of the largest weight where something is cut.  A row with a NaN or +inf among its
+ * logits, without any finite one, with u outside [0, 1), or with a temperature below
+ * 0, infinite or NaN, or a NaN top_p or min_p of its own gets token -1 and NaN.  Sums
+ * that decide what is kept and drawn are exact sums of weights in 2^-42 (of a weight
+ * of 1), or fp64 where nothing is cut; weights are fp32.  No atomic changes a result:
+ * the same call gives the same bits.  Enqueues two kernels, keeps no state.
+ * RG_EINVAL for NULL pointers (but the options'), bad sizes, numbers outside the ranges above
+ * or too little scratch; RG_EUNSUPPORTED for vocab past 2^20. */
+int rg_sample(int32_t dtype, const void* logits, int64_t logits_row, int32_t rows, int32_t vocab, int32_t u_dtype, const void* u,
+              const rg_sample_options* options, int32_t* tokens, float* logprobs, float* kept_logprobs, void* scratch,
+              int64_t scratch_bytes, void* stream);
 
 /* ---- test and measurement hooks ---- */
 

@@ -10,3 +10,4 @@ from ._lib import (  # noqa: F401
     KERNEL_KINDS, exported_symbols, Sagc, sagc_beta_draw, group_filter, grpo_surrogate, decode_attention_chunks, hbm_probe,
 )
 from ._kv8 import Kv8Cache, kv8_append, kv8_attention, rope, rope_table  # noqa: F401
+from ._draft import kv8_accept, kv8_tree, kv8_tree_attention, sample  # noqa: F401

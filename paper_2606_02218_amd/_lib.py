@@ -23,7 +23,9 @@ EXPORTS = ["rg_last_error", "rg_policy_create", "rg_policy_create_kv", "rg_polic
            "sagc_init", "sagc_group_stats", "sagc_step", "sagc_beta_draw", "group_filter",
            "recompute_logprobs", "grpo_surrogate", "rg_decode_attention_chunks", "rg_phase_times",
            "grpo_surrogate_noalloc", "grpo_surrogate_scratch", "rg_gumbel_noise",
-           "rg_rope_table", "rg_rope", "rg_kv8_append", "rg_kv8_attention_scratch", "rg_kv8_attention"]
+           "rg_rope_table", "rg_rope", "rg_kv8_append", "rg_kv8_attention_scratch", "rg_kv8_attention",
+           "rg_kv8_tree", "rg_kv8_tree_attention_scratch", "rg_kv8_tree_attention", "rg_kv8_accept", "rg_sample_scratch",
+           "rg_sample"]
 SAGC_MAX_SIZES = 8
 
 

@@ -1,0 +1,658 @@
+// Trees of drafted tokens over the 8-bit key/value cache: what each node sees,
+// attention of the nodes, and the accepted path's move to its place.
+//
+// A sequence's last n tokens are its tree's nodes, each behind its parent; node i
+// lies in slot context + i of the cache, at position context + depth.  Its mask has
+// a bit for itself and every ancestor.
+#include <algorithm>
+#include <type_traits>
+
+#include "kv8_attn_device.h"
+
+namespace {
+
+// ---------------------------------------------------------------- masks
+// A wave a sequence: the parents go to LDS, and each lane walks up from its nodes.
+// Parents come before their children, so a walk meets the bits of a mask from the
+// highest word down and ends after at most n steps.  Latency bound: 8 trees of 5 to
+// 16 nodes and 509 of 17 to 64 take one chain of loads and some depth LDS reads.
+constexpr int TREE_STAGED = 2048;     // parents of a tree that LDS holds
+
+__global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ parent, Kv8Rows b, int words,
+                                                 uint64_t* __restrict__ mask, int32_t* __restrict__ pos) {
+  __shared__ int32_t sp[TREE_STAGED];
+  const int s = blockIdx.x, lane = threadIdx.x;
+  int r0, n;
+  kv8_seq_rows(b, s, r0, n);
+  if (n <= 0) return;
+  const int first = max(n - kv8_len(b, s), 0);          // nodes before it are padding
+  const int ctx = max(kv8_len(b, s) - n, 0);
+  for (int i = lane; i < min(n, TREE_STAGED); i += 64) sp[i] = parent[r0 + i];
+  __syncthreads();
+  for (int i = lane; i < n; i += 64) {
+    uint64_t* out = mask + (int64_t)(r0 + i) * words;
+    int w = words - 1, depth = -1, a = i;
+    uint64_t bits = 0;
+    bool ok = i >= first;
+    while (ok && a >= first) {                          // a walk never goes up in number: it ends
+      if ((a >> 6) < words) {
+        for (; w > (a >> 6); --w) { out[w] = bits; bits = 0; }
+        bits |= 1ull << (a & 63);
+      }
+      ++depth;
+      const int up = a < TREE_STAGED ? sp[a] : parent[r0 + a];
+      ok = up >= -1 && up < a;                          // no parent: neither the node nor what is behind it counts
+      a = up;
+    }
+    if (ok) {
+      for (; w >= 0; --w) { out[w] = bits; bits = 0; }
+    } else {
+      for (w = 0; w < words; ++w) out[w] = 0;
+    }
+    pos[r0 + i] = ok ? (int)min((int64_t)ctx + depth, (int64_t)INT32_MAX) : -1;
+  }
+}
+
+// ---------------------------------------------------------------- attention
+// The tree's queries of one kv head, nodes x heads, are packed as columns, 16 CT of
+// them a workgroup.  Its waves take 32-token steps in turn straight from memory, 16
+// bytes a lane, convert the codes once for all their columns, and join in LDS.
+// Scores are formed transposed, S^T = K Q^T, so that a lane ends up with the
+// probabilities of one column for just those tokens whose V^T operand it loads.
+// Every node sees the context: only steps that reach into the tree are masked.
+enum { TREE_F32 = 0, TREE_BF16 = 1 };
+constexpr int tree_pieces(int size) { return size == 2 ? 1 : 3; }   // bf16 pieces of a query and of a probability
+
+// The sequence whose column groups hold number x: sequence s has its groups of
+// 2^shift columns at (first row * rep >> shift) + s and on.  64 candidates a step.
+__device__ __forceinline__ int find_group(const Kv8Rows& b, int x, int rep, int shift, int& key) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = b.n_seqs, at = 0;
+  auto key_of = [&](int s) { return (int)((int64_t)min(max(b.seq_off[s], 0), b.rows) * rep >> shift) + s; };
+  do {
+    const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
+    int k = INT32_MAX;
+    if (s < hi) k = key_of(s);
+    const uint64_t below = __ballot(s < hi && k <= x) | 1;
+    const int top = 63 - __clzll((long long)below);
+    at = __builtin_amdgcn_readlane(k, top);
+    lo += top * step;
+    hi = min(lo + step, hi);
+  } while (hi - lo > 1);
+  key = at;
+  return lo;
+}
+
+// 32 bits of a node's mask from bit b on; bits before 0, the context's, are set.
+__device__ __forceinline__ uint32_t mask_window(const uint64_t* m, int words, int b) {
+  if (b < 0) return b <= -32 ? ~0u : (uint32_t)(m[0] << -b) | ((1u << -b) - 1u);
+  const int w = b >> 6, o = b & 63;
+  uint64_t x = w < words ? m[w] >> o : 0;
+  if (o > 32 && w + 1 < words) x |= m[w + 1] << (64 - o);
+  return (uint32_t)x;
+}
+
+template <typename T, int HD, int CT, int W>
+__global__ __launch_bounds__(64 * W) void k_kv8_tree_attn(Kv8TreeAttn A, unsigned groups, unsigned items) {
+  constexpr int QP = tree_pieces(sizeof(T)), PP = QP;
+  constexpr int NJ = HD / 64;       // 16-byte loads of a block per lane
+  constexpr int GC = 16 * CT, SHIFT = CT == 4 ? 6 : CT == 2 ? 5 : 4;
+  constexpr int LDO = HD + 4;
+  __shared__ __attribute__((aligned(16))) float sO[W][16][LDO];
+  __shared__ float sM[W][GC], sL[W][GC];
+
+  // Blocks are dealt to the 8 XCDs in turn; runs of eight items, column groups that
+  // read the same tokens, stay on one.
+  unsigned item = (blockIdx.x >> 6) * 64 + (blockIdx.x & 7) * 8 + (blockIdx.x >> 3 & 7);
+  if (item >= items) return;
+  const int x = (int)(item % groups);
+  item /= groups;
+  const int kvh = (int)(item % (unsigned)A.c.n_kv), split = (int)(item / (unsigned)A.c.n_kv);
+  const int rep = A.n_q / A.c.n_kv;
+  int key, r0, n;
+  const int s = find_group(A.b, x, rep, SHIFT, key);
+  kv8_seq_rows(A.b, s, r0, n);
+  const int64_t col0 = (int64_t)(x - key) * GC;
+  if (x < key || col0 >= (int64_t)n * rep) return;
+  const int len = kv8_len(A.b, s), ctx0 = len - n;      // node i is token ctx0 + i
+  const int ctx = max(ctx0, 0);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cl = lane & 15, grp = lane >> 4;
+  // tokens that some node may see; no walk over what the table has not
+  const int total = (int)std::min<int64_t>(std::min<int64_t>(len, std::max<int64_t>(ctx, (int64_t)ctx0 + 64 * A.words)),
+                                           (int64_t)kv8_most(A.c, A.b) + 64 * A.words);
+  const int64_t c0l = (int64_t)split * A.plan.chunk;
+  const int c0 = (int)std::min<int64_t>(c0l, total);
+  const int c1 = split == A.plan.n_split - 1 ? total : (int)std::min<int64_t>(total, c0l + A.plan.chunk);
+  const int steps = (c1 - c0 + 31) / 32, last_blk = (max(c1, 1) - 1) >> 4;
+  const int mine = (steps - wave + W - 1) / W;          // steps wave, wave + W, ...
+  const int whole = min(ctx, c1);                       // tokens that every node sees
+  const int32_t* tab = kv8_table(A.b, s);
+
+  const float sc = A.scale * KV8_LOG2E;
+  float m[CT], l[CT];
+  f32x4_t o[CT][NJ][4];
+  bf16x8_t qf[CT][2 * NJ][QP];
+  const uint64_t* mrow[CT];
+  bool node_ok[CT];
+  const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    m[ct] = -INFINITY;
+    l[ct] = 0.f;
+    const int64_t c = col0 + 16 * ct + cl;
+    const bool valid = c < (int64_t)n * rep;
+    const int node = valid ? (int)((uint64_t)c / (unsigned)rep) : 0, head = kvh * rep + (valid ? (int)(c - (int64_t)node * rep) : 0);
+    node_ok[ct] = valid && ctx0 + node >= 0;            // a padding row sees nothing
+    mrow[ct] = A.mask + (int64_t)(r0 + node) * A.words;
+    const T* qp = (const T*)A.q.p + (r0 + node) * A.q.row + head * A.q.head;
+#pragma unroll
+    for (int kk = 0; kk < 2 * NJ; ++kk) query8<T, QP>(qp + 64 * (kk >> 1) + 16 * grp + 8 * (kk & 1), node_ok[ct], vec, qf[ct][kk]);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[ct][j][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const uint8_t* kl = A.c.k + lane * 16;
+  const uint8_t* vl = A.c.v + grp * (4 * HD) + cl * 16;
+  u32x4_t kr[2][NJ], vr[2][NJ];
+  int ids = 0;                      // lane i: block i & 1 of step i >> 1 of the current 32 steps
+  float kss = 1.f, vss = 1.f;
+  auto lists = [&](int i0) {
+    const int st = wave + W * (i0 + (lane >> 1));
+    const int blk = min((c0 >> 4) + 2 * st + (lane & 1), last_blk);
+    ids = kv8_block(A.c, tab, A.b.tab_stride, blk, kvh);
+    kss = ids < 0 ? 1.f : A.c.k_scale[ids];
+    vss = ids < 0 ? 1.f : A.c.v_scale[ids];
+  };
+  auto fetch_k = [&](int i) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* p = kl + (int64_t)max(__builtin_amdgcn_readlane(ids, 2 * (i & 31) + h), 0) * (16 * HD);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) kr[h][j] = *reinterpret_cast<const u32x4_t*>(p + j * 1024);
+    }
+  };
+  auto fetch_v = [&](int i) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* p = vl + (int64_t)max(__builtin_amdgcn_readlane(ids, 2 * (i & 31) + h), 0) * (16 * HD);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) vr[h][j] = *reinterpret_cast<const u32x4_t*>(p + j * 256);
+    }
+  };
+  if (mine > 0) {
+    lists(0);
+    fetch_k(0);
+    fetch_v(0);
+  }
+  for (int i = 0; i < mine; ++i) {
+    const int t0 = c0 + 32 * (wave + W * i);
+    float ks[2], vs[2];
+    int id[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      id[h] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
+      ks[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kss), 2 * (i & 31) + h));
+      vs[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vss), 2 * (i & 31) + h));
+    }
+    f32x4_t st[CT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // a lost page's tokens: NaN scores (the codes in the registers are another page's)
+      const float none = id[h] < 0 ? __uint_as_float(0x7FC00000u) : 0.f;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) st[ct][h] = f32x4_t{none, none, none, none};
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const bf16x8_t kf = kv8_bf16x8(kr[h][j][2 * e], kr[h][j][2 * e + 1], ks[h], ks[h]);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int n_ = 0; n_ < QP; ++n_)
+              st[ct][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ct][2 * j + e][n_], st[ct][h], 0, 0, 0);
+        }
+    }
+    if (i + 1 < mine) {
+      if (((i + 1) & 31) == 0) lists(i + 1);
+      fetch_k(i + 1);
+    }
+    // lane's tokens: 16 h + 4 grp + e of the step
+    if (t0 + 32 > whole) {
+      uint32_t seen[CT];
+      const uint32_t there = c1 - t0 < 32 ? (1u << (c1 - t0)) - 1u : ~0u;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        seen[ct] = node_ok[ct] ? mask_window(mrow[ct], A.words, t0 - ctx0) & there : 0u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!(seen[ct] >> (16 * h + 4 * grp + e) & 1)) st[ct][h][e] = -INFINITY;
+      }
+      // 0 * NaN is NaN: what some column does not see must hold none.  Stale slots and
+      // lost pages are cleared; NaN codes too, after a product has counted those that a
+      // column does see (ones at the NaN codes, ones at the tokens in sight).
+      bool nan = false;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int left = id[h] < 0 ? 0 : min(max(c1 - t0 - 16 * h - 4 * grp, 0), 4);
+        const uint32_t keep = left == 4 ? ~0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            vr[h][j][e] &= keep;
+            nan |= has_nan_code(vr[h][j][e]);
+          }
+      }
+      if (__any(nan)) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          uint32_t sw[4];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t four = seen[ct] >> (16 * h + 4 * grp);
+            sw[2 * h] = (four & 1u) * 0x3F80u | (four >> 1 & 1u) * 0x3F800000u;
+            sw[2 * h + 1] = (four >> 2 & 1u) * 0x3F80u | (four >> 3 & 1u) * 0x3F800000u;
+          }
+          const bf16x8_t sf = __builtin_bit_cast(bf16x8_t, u32x4_t{sw[0], sw[1], sw[2], sw[3]});
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t one[4];
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t hit = (((vr[h][j][e] & KV8_NAN4) + 0x01010101u) & 0x80808080u) >> 7;
+                one[2 * h] = (hit & 1u) * 0x3F80u | (hit >> 8 & 1u) * 0x3F800000u;
+                one[2 * h + 1] = (hit >> 16 & 1u) * 0x3F80u | (hit >> 24) * 0x3F800000u;
+              }
+              const f32x4_t c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  __builtin_bit_cast(bf16x8_t, u32x4_t{one[0], one[1], one[2], one[3]}), sf, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (c[q] > 0.f) o[ct][j][e][q] = __uint_as_float(0x7FC00000u);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vr[h][j][e] = clear_nan(vr[h][j][e]);
+      }
+    }
+    bf16x8_t pf[CT][PP];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float mx = fmaxf(fmaxf(fmaxf(st[ct][0][0], st[ct][0][1]), fmaxf(st[ct][0][2], st[ct][0][3])),
+                       fmaxf(fmaxf(st[ct][1][0], st[ct][1][1]), fmaxf(st[ct][1][2], st[ct][1][3]))) * sc;
+      if (__any(mx > m[ct] + KV8_SLACK)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mn = fmaxf(m[ct], mx);
+        const float alpha = m[ct] == mn ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);   // -inf: nothing seen yet
+        l[ct] *= alpha;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[ct][j][e] *= alpha;
+        m[ct] = mn;
+      }
+      const float ms = m[ct] == -INFINITY ? 0.f : m[ct];   // nothing seen: every probability is exp2(-inf) = 0
+      float p[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[4 * h + e] = __builtin_amdgcn_exp2f(fmaf(st[ct][h][e], sc, -ms));
+          l[ct] += p[4 * h + e];
+        }
+      operand8<PP>(p, pf[ct]);
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bf16x8_t vf = kv8_bf16x8(vr[0][j][e], vr[1][j][e], vs[0], vs[1]);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int n_ = 0; n_ < PP; ++n_)
+            o[ct][j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[ct][n_], o[ct][j][e], 0, 0, 0);
+      }
+    if (i + 1 < mine) fetch_v(i + 1);
+  }
+
+  // Join the waves, 16 columns at a time: column cl, dims 64 j + 16 grp + 4 i + e of
+  // the lane.  A wave without steps has weight 0.
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    l[ct] += __shfl_xor(l[ct], 16, 64);
+    l[ct] += __shfl_xor(l[ct], 32, 64);
+    if (grp == 0) {
+      sM[wave][16 * ct + cl] = m[ct];
+      sL[wave][16 * ct + cl] = l[ct];
+    }
+  }
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    if (ct) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4_t*>(&sO[wave][cl][64 * j + 16 * grp + 4 * i]) =
+            f32x4_t{o[ct][j][0][i], o[ct][j][1][i], o[ct][j][2][i], o[ct][j][3][i]};
+    __syncthreads();
+    for (int i = tid; i < 16 * (HD / 4); i += 64 * W) {
+      const int h = i / (HD / 4), d = i % (HD / 4) * 4, g = 16 * ct + h;
+      const int64_t c = col0 + g;
+      if (c >= (int64_t)n * rep) break;
+      const int node = (int)((uint64_t)c / (unsigned)rep), head = kvh * rep + (int)(c - (int64_t)node * rep);
+      float M = sM[0][g];
+#pragma unroll
+      for (int w = 1; w < W; ++w) M = fmaxf(M, sM[w][g]);
+      float L = 0.f;
+      f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float f = sM[w][g] == M ? 1.f : __builtin_amdgcn_exp2f(sM[w][g] - M);
+        L += f * sL[w][g];
+        acc += f * *reinterpret_cast<const f32x4_t*>(&sO[w][h][d]);
+      }
+      if (A.plan.n_split == 1) {
+        const float inv = L == 0.f ? 0.f : 1.0f / L;    // 0: the row sees nothing
+        const float v[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+        st_elems<4, true>((T*)A.out + ((int64_t)(r0 + node) * A.n_q + head) * HD + d, v);
+      } else {
+        const int64_t slot = ((int64_t)(r0 + node) * A.plan.n_split + split) * A.n_q + head;
+        const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+        if (steps > 0) st_elems<4, true>(A.part_o + slot * HD + d, v);
+        if (d == 0) {
+          A.part_ml[2 * slot] = M;
+          A.part_ml[2 * slot + 1] = L;
+        }
+      }
+    }
+  }
+}
+
+// A wave per row and head joins the chunks' partial results in order; a chunk that
+// the row sees nothing of has sum 0 and its outputs are not looked at.
+constexpr int TREE_MAX_SPLIT = 64;
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_kv8_tree_merge(Kv8TreeAttn A) {
+  constexpr int ND = HD / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int64_t r = at / A.n_q;
+  const int head = (int)(at - r * A.n_q);
+  if (r >= A.b.rows || r < A.b.seq_off[0] || r >= A.b.seq_off[A.b.n_seqs]) return;
+  const int64_t slot0 = r * A.plan.n_split * A.n_q + head;
+  float m = -INFINITY, l = 0.f;
+  if (lane < A.plan.n_split) {
+    const float* ml = A.part_ml + 2 * (slot0 + (int64_t)lane * A.n_q);
+    m = ml[0];
+    l = ml[1];
+  }
+  const float M = wave_max(m);
+  const float w = l == 0.f ? 0.f : m == M ? 1.f : __builtin_amdgcn_exp2f(m - M);
+  const float L = wave_sum(w * l), inv = L == 0.f ? 0.f : 1.0f / L;
+  float acc[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) acc[i] = 0.f;
+  for (uint64_t some = __ballot(w != 0.f); some; some &= some - 1) {   // NaN weights too
+    const int c = __ffsll((unsigned long long)some) - 1;
+    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), c));
+    const float* o = A.part_o + (slot0 + (int64_t)c * A.n_q) * HD + lane * ND;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) acc[i] += f * o[i];
+  }
+#pragma unroll
+  for (int i = 0; i < ND; ++i) acc[i] *= inv;
+  T* out = (T*)A.out + at * HD + lane * ND;
+  if constexpr (ND == 2 && sizeof(T) == 2) *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0], acc[1]);
+  else st_elems<ND, false>(out, acc);
+}
+
+// ---------------------------------------------------------------- accepted paths
+// The j-th kept node moves to slot ctx + j, which no later kept node comes from: a
+// destination block reads its own slots or ones behind them.  A workgroup per
+// sequence, kv head and keys or values: each wave gathers one block, all of them
+// wait, then store, so that no store passes a load of a round, and later rounds read
+// behind what earlier ones wrote.  A block's scale is the largest of the tokens that
+// end up in it, a power of two, so that a moved code keeps its bits unless it lands
+// among the subnormals.
+constexpr int ACCEPT_WAVES = 4;
+
+struct AcceptArgs {
+  Kv8Pool c;
+  Kv8Rows b;
+  const uint64_t* mask;
+  int words;
+  const int32_t* last;
+  int32_t* new_len;
+};
+
+// Word w of the kept nodes: those that are in the cache and among the n.
+__device__ __forceinline__ uint64_t kept_word(const uint64_t* m, int w, int first, int n) {
+  uint64_t x = m[w];
+  const int lo = first - 64 * w, hi = n - 64 * w;
+  if (lo > 0) x = lo >= 64 ? 0 : x & ~0ull << lo;
+  if (hi < 64) x = hi <= 0 ? 0 : x & ~0ull >> (64 - hi);
+  return x;
+}
+
+// Index of the k-th set bit of x (one that has more than k).
+__device__ __forceinline__ int nth_bit(uint64_t x, int k) {
+  int at = 0;
+#pragma unroll
+  for (int half = 32; half > 0; half >>= 1) {
+    const int c = __popcll(x & ((1ull << half) - 1));
+    if (k >= c) { k -= c; x >>= half; at += half; }
+  }
+  return at;
+}
+
+template <int HD>
+__global__ __launch_bounds__(64 * ACCEPT_WAVES) void k_kv8_accept(AcceptArgs A) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  unsigned item = blockIdx.x;
+  const bool values = item & 1;
+  item >>= 1;
+  const int s = (int)(item / (unsigned)A.c.n_kv), kvh = (int)(item - (unsigned)s * A.c.n_kv);
+  int r0, n;
+  kv8_seq_rows(A.b, s, r0, n);
+  const int len = kv8_len(A.b, s), ctx0 = len - n, ctx = max(ctx0, 0), first = max(-ctx0, 0);
+  const int last = n > 0 ? A.last[s] : -1;
+  const bool some = last >= 0 && last < n;
+  const uint64_t* mask = A.mask + (int64_t)(some ? r0 + last : 0) * A.words;
+  int kept = 0, stay = 0;                                // kept nodes; those before the first gap
+  if (some) {
+    bool gap = false;
+    for (int w = 0; w < A.words; ++w) {
+      const uint64_t x = kept_word(mask, w, first, n);
+      kept += __popcll(x);
+      if (!gap) {
+        const uint64_t y = w == first >> 6 ? x >> (first & 63) : w < first >> 6 ? ~0ull : x;
+        const int run = w < first >> 6 ? 0 : ~y ? __ffsll((unsigned long long)~y) - 1 : 64;
+        stay += run;
+        gap = w >= first >> 6 && run < 64 - (w == first >> 6 ? first & 63 : 0);
+      }
+    }
+  }
+  const int end = ctx + kept;
+  if (kvh == 0 && !values && threadIdx.x == 0) A.new_len[s] = end;
+  if (stay == kept) return;                              // nothing moves
+  const int32_t* tab = kv8_table(A.b, s);
+  uint8_t* codes = values ? A.c.v : A.c.k;
+  float* scales = values ? A.c.v_scale : A.c.k_scale;
+  const int b0 = (ctx + stay) >> 4, b1 = (end - 1) >> 4;
+  for (int base = b0; base <= b1; base += ACCEPT_WAVES) {
+    const int blk = base + wave;
+    const bool on = blk <= b1;
+    // token t of the block: where it is now
+    const int t = lane & 15, p = 16 * blk + t;
+    int src = p;
+    const bool there = on && p < end;
+    if (there && p >= ctx + stay) {
+      int j = p - ctx;
+      for (int w = 0; w < A.words; ++w) {
+        const uint64_t x = kept_word(mask, w, first, n);
+        const int c = __popcll(x);
+        if (j < c) { src = ctx0 + 64 * w + nth_bit(x, j); break; }
+        j -= c;
+      }
+    }
+    int from = -1;
+    float scale = 0.f;
+    if (there) {
+      from = kv8_block(A.c, tab, A.b.tab_stride, src >> 4, kvh);
+      if (from >= 0) scale = scales[from];
+    }
+    const int to = on ? kv8_block(A.c, tab, A.b.tab_stride, blk, kvh) : -1;
+    float top = scale;
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    if (!(top > 0.f)) top = 1.f;                         // pages that are not there: the codes become NaN
+    const float ratio = from < 0 ? __uint_as_float(0x7FC00000u) : scale / top;
+    // what the tokens that end up here hold, as they are
+    u32x4_t kd[HD / 64];
+    uint32_t vd[4][HD / 16];
+    const int kt = lane >> 2, kc = lane & 3;             // keys: four lanes a token
+    const int vq = lane >> 4, vd0 = (lane & 15) * (HD / 16);   // values: four tokens of some dims
+    if (!values) {
+      const int f = max(__shfl(from, kt, 64), 0), ts = __shfl(src, kt, 64) & 15;
+#pragma unroll
+      for (int g = 0; g < HD / 64; ++g)
+        kd[g] = *reinterpret_cast<const u32x4_t*>(codes + (int64_t)f * (16 * HD) + (kc + 4 * g) * 256 + ts * 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int f = max(__shfl(from, 4 * vq + i, 64), 0), ts = __shfl(src, 4 * vq + i, 64) & 15;
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(codes + (int64_t)f * (16 * HD) + (ts >> 2) * (4 * HD)) + vd0;
+#pragma unroll
+        for (int d = 0; d < HD / 16; d += 4) {
+          const u32x4_t z = *reinterpret_cast<const u32x4_t*>(w + d);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vd[i][d + e] = z[e] >> (8 * (ts & 3)) & 0xFFu;
+        }
+      }
+    }
+    __syncthreads();                                     // every load of the round is in registers
+    if (to >= 0) {
+      uint8_t* out = codes + (int64_t)to * (16 * HD);
+      if (!values) {
+        const float f = __shfl(ratio, kt, 64);
+        if (__shfl((int)there, kt, 64)) {
+#pragma unroll
+          for (int g = 0; g < HD / 64; ++g) {
+            u32x4_t z;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = kv8_requant4(kd[g][e], f);
+            *reinterpret_cast<u32x4_t*>(out + (kc + 4 * g) * 256 + kt * 16) = z;
+          }
+        }
+      } else {
+        float f[4];
+        uint32_t fresh = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f[i] = __shfl(ratio, 4 * vq + i, 64);
+          if (__shfl((int)there, 4 * vq + i, 64)) fresh |= 0xFFu << (8 * i);
+        }
+        if (fresh) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(out + vq * (4 * HD)) + vd0;
+#pragma unroll
+          for (int d = 0; d < HD / 16; d += 4) {
+            u32x4_t z = u32x4_t{0, 0, 0, 0};
+            if (fresh != ~0u) z = *reinterpret_cast<const u32x4_t*>(w + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float y[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_cvt_f32_fp8((int)vd[i][d + e], 0) * f[i];
+              z[e] = (kv8_codes4(y[0], y[1], y[2], y[3]) & fresh) | (z[e] & ~fresh);
+            }
+            *reinterpret_cast<u32x4_t*>(w + d) = z;
+          }
+        }
+      }
+      if (lane == 0) scales[to] = top;
+    }
+    __syncthreads();                                     // the next round's loads see none of these slots, but the same scales
+  }
+}
+
+template <typename T, int HD>
+hipError_t run(const Kv8TreeAttn& a, hipStream_t st) {
+  const int rep = a.n_q / a.c.n_kv, gc = 16 * a.plan.ct;
+  const int64_t groups = (int64_t)a.b.rows * rep / gc + a.b.n_seqs, items = groups * a.c.n_kv * a.plan.n_split;
+  if (items > INT32_MAX - 64) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)((items + 63) / 64 * 64));
+#define RG_TREE(CT, W) return kv8_launch(k_kv8_tree_attn<T, HD, CT, W>, grid, dim3(64 * W), st, a, (unsigned)groups, (unsigned)items)
+  if constexpr (sizeof(T) == 2) {
+    if (a.plan.ct == 4) { RG_TREE(4, 4); }
+  }
+  if (a.plan.ct == 2) { RG_TREE(2, 4); }
+  RG_TREE(1, 4);
+#undef RG_TREE
+}
+
+template <typename T, int HD>
+hipError_t merge(const Kv8TreeAttn& a, hipStream_t st) {
+  const int64_t n = ((int64_t)a.b.rows * a.n_q + 3) / 4;
+  if (n > INT32_MAX) return hipErrorInvalidValue;
+  return kv8_launch(k_kv8_tree_merge<T, HD>, dim3((unsigned)n), dim3(256), st, a);
+}
+
+}  // namespace
+
+// Columns of a workgroup by the mean of a sequence; chunks as far as two workgroups a
+// CU go, of 256 tokens at least.
+Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int max_len) {
+  Kv8TreePlan p{};
+  const int64_t rep = n_q / n_kv, cols = ((int64_t)rows * rep + n_seqs - 1) / n_seqs;
+  p.ct = cols <= 16 ? 1 : cols <= 32 || dtype == 0 ? 2 : 4;
+  const int64_t wgs = ((int64_t)rows * rep / (16 * p.ct) + n_seqs) * n_kv;
+  const int64_t n = std::max<int64_t>(1, std::min<int64_t>({512 / wgs, max_len / 256, TREE_MAX_SPLIT}));
+  p.chunk = (int)std::min<int64_t>((((int64_t)max_len + n - 1) / n + 31) / 32 * 32, 1 << 30);
+  p.n_split = (int)((max_len + (int64_t)p.chunk - 1) / p.chunk);
+  return p;
+}
+
+hipError_t launch_kv8_tree(const int32_t* parent, const Kv8Rows& b, int words, uint64_t* mask, int32_t* pos, hipStream_t st) {
+  if (b.rows <= 0 || b.n_seqs <= 0) return hipSuccess;
+  return kv8_launch(k_kv8_tree, dim3(b.n_seqs), dim3(64), st, parent, b, words, mask, pos);
+}
+
+hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& a, hipStream_t st) {
+  if (a.b.rows <= 0 || a.b.n_seqs <= 0) return hipSuccess;
+  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.n_split > TREE_MAX_SPLIT || a.plan.chunk % 32 ||
+      (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
+    return hipErrorInvalidValue;
+  const bool w = a.c.hd == 128;
+  hipError_t e;
+  if (dtype == 1) e = w ? run<bf16_t, 128>(a, st) : run<bf16_t, 64>(a, st);
+  else e = w ? run<float, 128>(a, st) : run<float, 64>(a, st);
+  if (e != hipSuccess || a.plan.n_split == 1) return e;
+  if (dtype == 1) return w ? merge<bf16_t, 128>(a, st) : merge<bf16_t, 64>(a, st);
+  return w ? merge<float, 128>(a, st) : merge<float, 64>(a, st);
+}
+
+hipError_t launch_kv8_accept(const Kv8Pool& c, const Kv8Rows& b, const uint64_t* mask, int words, const int32_t* last,
+                             int32_t* new_len, hipStream_t st) {
+  if (b.n_seqs <= 0) return hipSuccess;
+  if (c.hd != 64 && c.hd != 128) return hipErrorInvalidValue;
+  const int64_t grid = (int64_t)b.n_seqs * c.n_kv * 2;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const AcceptArgs a{c, b, mask, words, last, new_len};
+  const dim3 g((unsigned)grid), t(64 * ACCEPT_WAVES);
+  return c.hd == 128 ? kv8_launch(k_kv8_accept<128>, g, t, st, a) : kv8_launch(k_kv8_accept<64>, g, t, st, a);
+}

@@ -1,5 +1,6 @@
-// C entry points of the rotary positions and the 8-bit key/value cache
-// (include/rollout.h): argument checks, then the launchers.
+// C entry points of the rotary positions, the 8-bit key/value cache, drafted trees
+// over it and sampling from given logits (include/rollout.h): argument checks, then
+// the launchers.
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
@@ -89,6 +90,14 @@ int rope_args(const char* who, const float* co, const float* si, int32_t n_pos, 
   if (!co || !si) return bad(who, "NULL table");
   if (n_pos < 1) return bad(who, "n_pos < 1");
   *t = RopeTable{co, si, n_pos, rot_dim / 2, layout};
+  return RG_OK;
+}
+
+// What the calls on drafted trees ask of their batch beyond cache_args: offsets, and
+// masks where they read them.
+int tree_args(const char* who, const rg_kv8_batch* b, int32_t words) {
+  if (words < 1 || words > RG_KV8_TREE_WORDS) return bad(who, "words must be in [1, 64]");
+  if (b->rows > 0 && !b->seq_off) return bad(who, "NULL seq_off");
   return RG_OK;
 }
 
@@ -194,6 +203,103 @@ int rg_kv8_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32
   if (need > 0 && (!scratch || scratch_bytes < need)) return bad(who, "scratch is smaller than rg_kv8_attention_scratch()");
   if ((rc = launched(who, launch_kv8_attention(dtype, false, a, (hipStream_t)stream)))) return rc;
   return launched(who, launch_kv8_merge(dtype, false, a, (hipStream_t)stream));
+}
+
+int rg_kv8_tree(const int32_t* parent, const int32_t* seq_off, const int32_t* seq_len, int32_t n_seqs, int32_t rows,
+                int32_t words, uint64_t* mask, int32_t* pos, void* stream) {
+  const char* who = "rg_kv8_tree";
+  if (rows < 0 || n_seqs < 0 || n_seqs > (1 << 24)) return bad(who, "rows or n_seqs out of range");
+  if (words < 1 || words > RG_KV8_TREE_WORDS) return bad(who, "words must be in [1, 64]");
+  if (rows == 0 || n_seqs == 0) return RG_OK;
+  if (!parent || !seq_off || !seq_len || !mask || !pos) return bad(who, "NULL argument");
+  const Kv8Rows b{nullptr, 0, 0, nullptr, seq_off, seq_len, 0, n_seqs, rows, nullptr};
+  return launched(who, launch_kv8_tree(parent, b, words, mask, pos, (hipStream_t)stream));
+}
+
+int64_t rg_kv8_tree_attention_scratch(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rows, int32_t n_seqs,
+                                      int32_t max_len) {
+  if ((dtype != RG_DTYPE_F32 && dtype != RG_DTYPE_BF16) || n_q < 1 || n_kv < 1 || n_q % n_kv || head_dim < 1 || rows < 0 ||
+      n_seqs < 0 || max_len < 1)
+    return bad("rg_kv8_tree_attention_scratch", "bad sizes");
+  if (rows == 0 || n_seqs == 0) return 0;
+  return 4 * kv8_tree_part_floats(rows, kv8_tree_plan(dtype, rows, n_seqs, n_q, n_kv, max_len), n_q, head_dim);
+}
+
+int rg_kv8_tree_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* q, int64_t q_row,
+                          int64_t q_head, int32_t n_q, const uint64_t* mask, int32_t words, void* out, float scale,
+                          int32_t max_len, void* scratch, int64_t scratch_bytes, void* stream) {
+  const char* who = "rg_kv8_tree_attention";
+  Kv8TreeAttn a{};
+  int rc = cache_args(who, cache, batch, dtype, &a.c, &a.b);
+  if (rc || (rc = tree_args(who, batch, words))) return rc;
+  if (n_q < 1 || n_q % a.c.n_kv) return bad(who, "n_q must be a multiple of n_kv");
+  if (n_q / a.c.n_kv > 128) return bad(who, "more than 128 query heads per kv head", RG_EUNSUPPORTED);
+  if (!(scale > 0.f) || !std::isfinite(scale * 1.44269504f)) return bad(who, "scale must be > 0 and at most 2.3e38");
+  if (max_len < 1) return bad(who, "max_len < 1");
+  if (a.b.rows == 0) return RG_OK;
+  if (!q || !out || !mask) return bad(who, "NULL q, out or mask");
+  if (!aligned(out) || !aligned(scratch)) return bad(who, "out or scratch is not 16-byte aligned");
+  a.q = HeadView{q, q_row, q_head};
+  a.out = out;
+  a.mask = mask;
+  a.words = words;
+  a.n_q = n_q;
+  a.scale = scale;
+  a.plan = kv8_tree_plan(dtype, a.b.rows, a.b.n_seqs, n_q, a.c.n_kv, max_len);
+  const int64_t need = 4 * kv8_tree_part_floats(a.b.rows, a.plan, n_q, a.c.hd);
+  if (need > 0 && (!scratch || scratch_bytes < need))
+    return bad(who, "scratch is smaller than rg_kv8_tree_attention_scratch()");
+  a.part_o = (float*)scratch;
+  a.part_ml = a.part_o ? a.part_o + (int64_t)a.b.rows * a.plan.n_split * n_q * a.c.hd : nullptr;
+  return launched(who, launch_kv8_tree_attention(dtype, a, (hipStream_t)stream));
+}
+
+int rg_kv8_accept(const rg_kv8_cache* cache, const rg_kv8_batch* batch, const uint64_t* mask, int32_t words,
+                  const int32_t* last, int32_t* new_len, void* stream) {
+  const char* who = "rg_kv8_accept";
+  Kv8Pool pool;
+  Kv8Rows rows;
+  int rc = cache_args(who, cache, batch, RG_DTYPE_BF16, &pool, &rows);
+  if (rc || (rc = tree_args(who, batch, words))) return rc;
+  if (rows.n_seqs == 0) return RG_OK;
+  if (!batch->seq_off || !batch->seq_len || !new_len) return bad(who, "NULL seq_off, seq_len or new_len");
+  if (rows.rows > 0 && (!mask || !last)) return bad(who, "NULL mask or last");
+  // read by workgroups of the sequence that writes it
+  auto meets = [&](const int32_t* p, int64_t n) { return p && p < new_len + rows.n_seqs && new_len < p + n; };
+  if (meets(batch->seq_len, rows.n_seqs) || meets(last, rows.n_seqs) || meets(batch->seq_off, (int64_t)rows.n_seqs + 1) ||
+      meets(batch->tab_row, rows.n_seqs) || meets(batch->page_tab, (int64_t)batch->tab_rows * batch->tab_stride))
+    return bad(who, "new_len overlaps what the call reads");
+  return launched(who, launch_kv8_accept(pool, rows, mask, words, last, new_len, (hipStream_t)stream));
+}
+
+int64_t rg_sample_scratch(int32_t rows, int32_t vocab) {
+  if (rows < 0 || vocab < 1 || vocab > DRAW_MAX_VOCAB) return bad("rg_sample_scratch", "rows < 0, or vocab not in [1, 2^20]");
+  return 4 * draw_scratch_floats(rows, vocab);
+}
+
+int rg_sample(int32_t dtype, const void* logits, int64_t logits_row, int32_t rows, int32_t vocab, int32_t u_dtype, const void* u,
+              const rg_sample_options* options, int32_t* tokens, float* logprobs, float* kept_logprobs, void* scratch,
+              int64_t scratch_bytes, void* stream) {
+  const char* who = "rg_sample";
+  if (!options) return bad(who, "NULL argument");
+  if (dtype != RG_DTYPE_F32 && dtype != RG_DTYPE_BF16) return bad(who, "unknown dtype");
+  if (u_dtype != RG_DTYPE_F32 && u_dtype != RG_DTYPE_F64) return bad(who, "u must be fp32 or fp64");
+  if (rows < 0 || vocab < 1) return bad(who, "rows < 0 or vocab < 1");
+  if (vocab > DRAW_MAX_VOCAB) return bad(who, "vocab exceeds 2^20", RG_EUNSUPPORTED);
+  const rg_sample_options& o = *options;
+  if (!o.temperature_rows && !(o.temperature >= 0.f && std::isfinite(o.temperature))) return bad(who, "temperature must be >= 0");
+  if (!o.top_k_rows && o.top_k < 0) return bad(who, "top_k must be >= 0");
+  if (!o.top_p_rows && !(o.top_p > 0.f && o.top_p <= 1.f)) return bad(who, "top_p must be in (0, 1]");
+  if (!o.min_p_rows && !(o.min_p >= 0.f && o.min_p <= 1.f)) return bad(who, "min_p must be in [0, 1]");
+  if (rows == 0) return RG_OK;
+  if (!logits || !u || !tokens || !logprobs || !kept_logprobs) return bad(who, "NULL argument");
+  const int64_t need = rg_sample_scratch(rows, vocab);
+  if (!scratch || scratch_bytes < need) return bad(who, "scratch is smaller than rg_sample_scratch()");
+  if (!aligned(scratch)) return bad(who, "scratch is not 16-byte aligned");
+  const DrawArgs a{logits, logits_row, dtype, rows, vocab, u, u_dtype == RG_DTYPE_F64, o.temperature, o.top_p, o.min_p, o.top_k,
+                   o.temperature_rows, o.top_k_rows, o.top_p_rows, o.min_p_rows, tokens, logprobs, kept_logprobs,
+                   (float*)scratch};
+  return launched(who, launch_draw(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -448,6 +448,35 @@ inline int64_t kv8_part_floats(int64_t rows, const Kv8Plan& p, int n_q, int hd) 
 // The pass over the cache; with n_split > 1 launch_kv8_merge has to follow.
 hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStream_t st);
 hipError_t launch_kv8_merge(int dtype, bool planes, const Kv8Attn& a, hipStream_t st);
+// Trees of drafted tokens (k_kv8_tree.hip): each row's mask of `words` 64-bit words,
+// a bit for each ancestor and itself, and its position.
+hipError_t launch_kv8_tree(const int32_t* parent, const Kv8Rows& b, int words, uint64_t* mask, int32_t* pos, hipStream_t st);
+// How a tree attention is cut: ct x 16 columns (nodes x heads of a kv head) a
+// workgroup, the context into n_split chunks of `chunk` tokens.
+struct Kv8TreePlan {
+  int ct, n_split, chunk;
+};
+Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int max_len);
+struct Kv8TreeAttn {
+  Kv8Pool c;
+  Kv8Rows b;
+  HeadView q;
+  void* out;
+  const uint64_t* mask;
+  int words;
+  int n_q;
+  float scale;
+  Kv8TreePlan plan;
+  float* part_o;    // n_split > 1: unnormalised outputs [rows][n_split][n_q][hd]
+  float* part_ml;   // and their (max, sum) [rows][n_split][n_q][2]
+};
+inline int64_t kv8_tree_part_floats(int64_t rows, const Kv8TreePlan& p, int n_q, int hd) {
+  return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
+}
+hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& a, hipStream_t st);
+// Moves the nodes of mask row last[s] behind the context; new_len: tokens then.
+hipError_t launch_kv8_accept(const Kv8Pool& c, const Kv8Rows& b, const uint64_t* mask, int words, const int32_t* last,
+                             int32_t* new_len, hipStream_t st);
 // Rows row0 .. row0 + n - 1 of a teacher-forced forward as a batch of n_seq
 // sequences (coff as in ReserveArgs, from the first of them on): off [n_seq + 1],
 // and the tokens that each has once those rows are appended.
@@ -457,3 +486,21 @@ hipError_t launch_kv8_runs(const int32_t* coff, const int32_t* plen, const int32
 // the pool is layer_blocks * l blocks behind c.
 hipError_t launch_kv8_page_copy(const Kv8Pool& c, int n_layers, int64_t layer_blocks, const int32_t* copy_pairs,
                                 int max_pairs, const int32_t* state, hipStream_t st);
+
+// ---- sampling from given logits and uniform numbers (k_draw.hip)
+constexpr int DRAW_MAX_VOCAB = 1 << 20;
+struct DrawArgs {
+  const void* logits;   // fp32 or bf16 by dtype, [rows][vocab], `row` elements apart
+  int64_t row;
+  int dtype, rows, vocab;
+  const void* u;        // [rows] in [0, 1), doubles where u64
+  int u64;
+  float temperature, top_p, min_p;
+  int top_k;
+  const float* temperature_rows; const int32_t* top_k_rows;   // [rows], in the place of the numbers above, or NULL
+  const float* top_p_rows; const float* min_p_rows;
+  int32_t* token; float* logprob; float* kept;                // [rows] each
+  float* seg;           // scratch: maximum and sum of every row's segments
+};
+int64_t draw_scratch_floats(int64_t rows, int vocab);
+hipError_t launch_draw(const DrawArgs& a, hipStream_t st);

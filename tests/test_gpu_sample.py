@@ -1,0 +1,221 @@
+"""Sampling from given logits and uniform numbers against the float64 oracle."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle.draw import Row, weight_slack
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def logits(rng, rows, vocab, kind, dtype):
+    z = rng.normal(0, 2.0, (rows, vocab))
+    if kind == "peaked":                   # as a decoder's: a few far above the rest
+        for r in range(rows):
+            at = rng.integers(0, vocab, min(30, vocab))
+            z[r, at] = rng.uniform(8, 18) - rng.uniform(0, 9, len(at))
+    elif kind == "sharp":
+        z[np.arange(rows), rng.integers(0, vocab, rows)] = 30.0
+    elif kind == "equal":
+        z[:] = 1.25
+    elif kind == "few values":
+        z = rng.integers(-3, 4, (rows, vocab)) * 0.5
+    elif kind == "masked":
+        z[rng.random((rows, vocab)) < 0.9] = -np.inf
+        z[rng.random((rows, vocab)) < 0.2] = -3.3895314e38
+        z[:, vocab // 2] = 1.0
+    elif kind == "ascending":
+        z = np.sort(z, 1)
+    return torch.from_numpy(z).to(dtype).cuda()
+
+
+def check(z, u, got, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """Each row's draw is one that the oracle's sums, moved by no more than the weights' own error, can give."""
+    token, lp, kept = (x.cpu().numpy() for x in got)
+    z, u = z.double().cpu().numpy(), u.double().cpu().numpy()
+    row = lambda x, r: x[r].item() if isinstance(x, torch.Tensor) else x  # noqa: E731
+    wide = 0
+    for r in range(len(z)):
+        t = row(temperature, r)
+        s = weight_slack(z[r], t)
+        o = Row(z[r], t, row(top_k, r), row(top_p, r), row(min_p, r), 2 * s)
+        wide += o.low != o.high
+        fits = []
+        for n in range(o.low, o.high + 1):
+            if token[r] not in o.kept(n):
+                fits.append("not kept")
+                continue
+            a, b = o.span(token[r], n)
+            _, want_lp, want_kept = o.logs(token[r], n)
+            if t == 0:
+                assert token[r] == o.order[0]
+                a, b = 0.0, 1.0
+            ok = a - 4 * s <= u[r] <= b + 4 * s
+            # the sum is off by s, its logarithm so much; the result is rounded once (2^-24)
+            near = all(abs(x - y) <= 2 * s + 2.0 ** -24 * abs(y) * 1.01 + 1e-12 for x, y in ((lp[r], want_lp), (kept[r], want_kept)))
+            fits.append(ok and near or (a, b, u[r], lp[r], want_lp, kept[r], want_kept, s))
+        assert True in fits, (r, token[r], o.low, o.high, fits[:3])
+    return wide
+
+
+KINDS = ["peaked", "flat", "sharp", "equal", "few values", "masked", "ascending"]
+SETTINGS = [dict(), dict(temperature=0.6), dict(top_k=1), dict(top_k=20), dict(top_k=300), dict(top_p=0.9), dict(top_p=0.1),
+            dict(top_p=0.999), dict(min_p=0.05), dict(min_p=1.0), dict(top_k=50, top_p=0.8, temperature=0.7),
+            dict(top_k=40, top_p=0.95, min_p=0.1, temperature=1.3), dict(top_p=0.7, min_p=0.01), dict(top_k=7, min_p=0.3),
+            dict(temperature=0.0), dict(temperature=0.0, top_p=0.5)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab", [1, 7, 512, 1000, 5003])
+def test_small_vocabularies(dtype, kind, vocab):
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(vocab + len(kind))
+    z = logits(rng, 6, vocab, kind, dtype)
+    for i, s in enumerate(SETTINGS):
+        u = torch.from_numpy(rng.random(6)).cuda()
+        if i % 2:
+            u = u.float().clamp(max=1 - 2.0 ** -24)
+        check(z, u, rg.sample(z, u, **s), **s)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", KINDS)
+def test_large_vocabularies(dtype, kind):
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(len(kind))
+    z = logits(rng, 5, 151936, kind, dtype)
+    for s in SETTINGS:
+        u = torch.from_numpy(rng.random(5)).cuda()
+        check(z, u, rg.sample(z, u, **s), **s)
+
+
+def test_largest_vocabulary_and_many_rows():
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(1)
+    z = logits(rng, 2, 1 << 20, "peaked", F32)
+    for s in (dict(), dict(top_p=0.95), dict(top_k=100, top_p=0.9), dict(min_p=1e-6), dict(top_k=1000000)):
+        u = torch.from_numpy(rng.random(2)).cuda()
+        check(z, u, rg.sample(z, u, **s), **s)
+    z = logits(rng, 700, 900, "peaked", BF16)
+    for s in (dict(), dict(top_k=30, top_p=0.9)):
+        u = torch.from_numpy(rng.random(700)).cuda()
+        check(z, u, rg.sample(z, u, **s), **s)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_settings_by_row_strides_and_repeats(dtype):
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(4)
+    rows, vocab = 40, 3001
+    z = logits(rng, rows, vocab, "peaked", dtype)
+    u = torch.from_numpy(rng.random(rows)).float().cuda()
+    s = dict(temperature=torch.from_numpy(np.where(rng.random(rows) < 0.2, 0.0, rng.uniform(0.3, 2, rows))).float().cuda(),
+             top_k=torch.from_numpy(rng.integers(-2, 60, rows)).int().cuda(),
+             top_p=torch.from_numpy(np.where(rng.random(rows) < 0.3, 1.0, rng.uniform(-0.1, 1.2, rows))).float().cuda(),
+             min_p=torch.from_numpy(np.where(rng.random(rows) < 0.5, -1.0, rng.uniform(0, 0.4, rows))).float().cuda())
+    want = rg.sample(z, u, **s)
+    check(z, u, want, **s)
+    for off in (0, 1, 3, 8):               # rows of a wider matrix, at any alignment
+        wide = torch.full((rows, vocab + 13), float("nan"), device="cuda", dtype=dtype)
+        wide[:, off:off + vocab] = z
+        for a, b in zip(rg.sample(wide[:, off:off + vocab], u, **s), want):
+            assert torch.equal(a, b)
+    for _ in range(3):
+        for a, b in zip(rg.sample(z, u, **s), want):
+            assert torch.equal(a, b)
+    # one row for every uniform number: rows that share their memory
+    one = z[:1].expand(rows, vocab)
+    check(one, u, rg.sample(one, u, top_k=20), top_k=20)
+
+
+def test_frequencies():
+    """20000 draws from eight tokens: counts within five deviations, both ways of drawing."""
+    import paper_2606_02218_amd as rg
+    z = torch.tensor([0.0, 1.0, -1.0, 2.0, 0.5, -3.0, 1.5, -0.5], device="cuda")
+    n = 20000
+    u = (torch.arange(n, device="cuda", dtype=torch.float64) + 0.5) / n
+    for s in (dict(), dict(top_k=5), dict(top_p=0.8), dict(min_p=0.1)):
+        token = rg.sample(z.expand(n, 8), u, **s)[0].cpu().numpy()
+        o = Row(z.double().cpu().numpy(), **s)
+        p = np.zeros(8)
+        p[o.kept(o.low)] = o.w[o.kept(o.low)] / o.w[o.kept(o.low)].sum()
+        assert np.all(np.abs(np.bincount(token, minlength=8) - n * p) <= 1.01)
+
+
+@pytest.mark.parametrize("s", [dict(), dict(top_k=5), dict(top_p=0.9), dict(min_p=0.1), dict(temperature=0.0)])
+def test_rows_that_have_no_answer(s):
+    """NaN and infinities, nothing but -inf, u outside [0, 1): token -1 and NaN; the rows beside them as ever."""
+    import paper_2606_02218_amd as rg
+    inf, nan = math.inf, math.nan
+    rng = np.random.default_rng(2)
+    z = logits(rng, 10, 1300, "peaked", F32)
+    z[1, 700] = nan
+    z[2, 1299] = inf
+    z[3] = -inf
+    z[4, 3] = -nan
+    u = torch.tensor([0.5] * 5 + [1.0, -0.1, nan, 0.0, 0.25], device="cuda")
+    token, lp, kept = rg.sample(z, u, **s)
+    for r in range(1, 8):
+        assert token[r] == -1 and lp[r].isnan() and kept[r].isnan(), r
+    good = [0, 8, 9]
+    check(z[good], u[good], [x[good] for x in (token, lp, kept)], **s)
+    t = torch.full((10,), 1.0, device="cuda")
+    t[0], t[8] = -1.0, nan
+    token = rg.sample(z, u, temperature=t, top_k=3)[0]
+    assert token[0] == -1 and token[8] == -1 and token[9] >= 0
+    p = torch.full((10,), 0.5, device="cuda")
+    p[0] = nan
+    assert rg.sample(z, u, top_p=p)[0][0] == -1 and rg.sample(z, u, min_p=p)[0][0] == -1
+
+
+def test_extreme_temperatures_and_logits():
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(3)
+    z = logits(rng, 4, 2000, "flat", F32)
+    u = torch.from_numpy(rng.random(4)).cuda()
+    for t in (1e-38, 1e-30, 1e-5, 1e30):
+        token, lp, kept = rg.sample(z, u, temperature=t)
+        if t < 1e-4:
+            assert torch.equal(token.long(), z.argmax(1)) and bool((lp == 0).all())
+        else:
+            check(z, u, (token, lp, kept), temperature=t)
+        check(z, u, rg.sample(z, u, temperature=t, top_k=3), temperature=t, top_k=3)
+    z = z * 1e37
+    check(z, u, rg.sample(z, u, temperature=1e37, top_p=0.9), temperature=1e37, top_p=0.9)
+    big = torch.full((2, 700), torch.finfo(F32).min, device="cuda")   # the type's lowest value everywhere
+    check(big, u[:2], rg.sample(big, u[:2], top_k=9), top_k=9)
+    check(big, u[:2], rg.sample(big, u[:2]))
+
+
+@pytest.mark.parametrize("s", [dict(), dict(top_k=20, top_p=0.9)])
+def test_graphs_and_streams(s):
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(6)
+    z = logits(rng, 9, 20000, "peaked", BF16)
+    u = torch.from_numpy(rng.random(9)).float().cuda()
+    want = rg.sample(z, u, **s)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = rg.sample(z, u, stream=side, **s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graphs = []
+    for _ in range(2):                     # two graphs, each with scratch of its own
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = rg.sample(z, u, **s)
+        graphs.append((g, out))
+    for i in range(3):
+        u.copy_(torch.from_numpy(rng.random(9)).float())
+        want = rg.sample(z, u, **s)
+        for g, out in graphs:
+            for x in out:
+                x.zero_()
+            g.replay()
+        torch.cuda.synchronize()
+        for _, out in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
