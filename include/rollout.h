@@ -560,18 +560,19 @@ int rg_kv8_accept(const rg_kv8_cache* cache, const rg_kv8_batch* batch, const ui
  * running sum of the kept weights passes u times their sum.  T = 0 takes the largest
  * logit, of equal ones the lowest id, whatever the rest. */
 typedef struct rg_sample_options {
-  float temperature;                /* >= 0                                                  */
-  int32_t top_k;                    /* >= 0                                                  */
-  float top_p;                      /* in (0, 1]                                             */
-  float min_p;                      /* in [0, 1]                                             */
+  double temperature;               /* >= 0                                                  */
+  double top_p;                     /* in (0, 1]                                             */
+  double min_p;                     /* in [0, 1]                                             */
+  int64_t top_k;                    /* >= 0                                                  */
   const float* temperature_rows;    /* DEVICE [rows] or NULL: a row's own in place of the    */
   const int32_t* top_k_rows;        /* numbers above.  Read by the kernels: top_k < 0 is     */
   const float* top_p_rows;          /* none, top_p <= 0 keeps the first token, min_p past 1  */
   const float* min_p_rows;          /* the largest                                           */
 } rg_sample_options;
 
-/* Bytes of scratch that rg_sample needs.  Negative (RG_E*) for bad sizes. */
-int64_t rg_sample_scratch(int32_t rows, int32_t vocab);
+/* Bytes of scratch that rg_sample needs with these options (of its pointers only
+ * whether they are NULL counts).  Negative (RG_E*) for bad sizes. */
+int64_t rg_sample_scratch(int32_t rows, int32_t vocab, const rg_sample_options* options);
 
 /*   logits    DEVICE [rows, vocab] in dtype (fp32 or bf16), rows logits_row elements
  *             apart; any alignment and stride work, 16-byte ones run faster
@@ -586,10 +587,10 @@ int64_t rg_sample_scratch(int32_t rows, int32_t vocab);
  * Tokens with logit -inf have weight 0 and are never drawn, nor are those below 2^-43
  * of the largest weight where something is cut.  A row with a NaN or +inf among its
  * logits, without any finite one, with u outside [0, 1), or with a temperature below
- * 0, infinite or NaN, or a NaN top_p or min_p of its own gets token -1 and NaN.  Sums
- * that decide what is kept and drawn are exact sums of weights in 2^-42 (of a weight
- * of 1), or fp64 where nothing is cut; weights are fp32.  No atomic changes a result:
- * the same call gives the same bits.  Enqueues two kernels, keeps no state.
+ * 0, infinite or NaN, or a NaN top_p or min_p of its own gets token -1 and NaN.
+ * Weights are within 2e-12 of their value, their sums fp64 or, where something is cut,
+ * whole numbers of 2^-42 of the largest weight.  No atomic changes a result: the same
+ * call gives the same bits.  Enqueues two to four kernels, keeps no state.
  * RG_EINVAL for NULL pointers (but the options'), bad sizes, numbers outside the ranges above
  * or too little scratch; RG_EUNSUPPORTED for vocab past 2^20. */
 int rg_sample(int32_t dtype, const void* logits, int64_t logits_row, int32_t rows, int32_t vocab, int32_t u_dtype, const void* u,

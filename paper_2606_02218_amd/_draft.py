@@ -13,19 +13,19 @@ from ._lib import _check, _dev
 
 
 class rg_sample_options(C.Structure):
-    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int64),
                 ("temperature_rows", C.c_void_p), ("top_k_rows", C.c_void_p), ("top_p_rows", C.c_void_p),
                 ("min_p_rows", C.c_void_p)]
 
 
-_OPTIONS = struct.Struct("@fiff4P").pack
+_OPTIONS = struct.Struct("@3dq4P").pack
 _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 _ARGS = {
     "rg_kv8_tree": ([_P, _P, _P, _I, _I, _I, _P, _P, _P], C.c_int),
     "rg_kv8_tree_attention_scratch": ([_I, _I, _I, _I, _I, _I, _I], _L),
     "rg_kv8_tree_attention": ([_P, _P, _I, _P, _L, _L, _I, _P, _I, _P, C.c_float, _I, _P, _L, _P], C.c_int),
     "rg_kv8_accept": ([_P, _P, _P, _I, _P, _P, _P], C.c_int),
-    "rg_sample_scratch": ([_I, _I], _L),
+    "rg_sample_scratch": ([_I, _I, _P], _L),
     "rg_sample": ([_I, _P, _L, _I, _I, _I, _P, _P, _P, _P, _P, _P, _L, _P], C.c_int),
 }
 WORDS = 64              # most words of a row's mask
@@ -268,10 +268,8 @@ def _sample_now(lib, z, u, temperature, top_k, top_p, min_p):
         return None
     t, k, p, m = (_row_option(temperature, _F32, rows, dev), _row_option(top_k, _I32, rows, dev),
                   _row_option(top_p, _F32, rows, dev), _row_option(min_p, _F32, rows, dev))
-    if not k and top_k > _MOST:
-        return None
-    o = _OPTIONS(0.0 if t else temperature, 0 if k else top_k, 0.0 if p else top_p, 0.0 if m else min_p, t, k, p, m)
-    need = lib.rg_sample_scratch(rows, vocab)
+    o = _OPTIONS(0.0 if t else temperature, 0.0 if p else top_p, 0.0 if m else min_p, 0 if k else top_k, t, k, p, m)
+    need = lib.rg_sample_scratch(rows, vocab, o)
     tokens = u.new_empty((rows,), dtype=_I32)
     lp = u.new_empty((2, rows), dtype=_F32)
     scratch = u.new_empty(need // 4, dtype=_F32)
@@ -318,7 +316,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=Non
     _dev("u", u, (_F32, _F64), (rows,))
     tensors = dict(logits=logits, u=u)
     o = rg_sample_options()
-    for name, x, dt, lo, hi in (("temperature", temperature, _F32, 0.0, 3.4e38), ("top_k", top_k, _I32, 0, _MOST),
+    for name, x, dt, lo, hi in (("temperature", temperature, _F32, 0.0, 1.7e308), ("top_k", top_k, _I32, 0, 2 ** 63 - 1),
                                 ("top_p", top_p, _F32, 0.0, 1.0), ("min_p", min_p, _F32, 0.0, 1.0)):
         if isinstance(x, torch.Tensor):
             tensors[name] = _dev(name, x, dt, (rows,))
@@ -330,7 +328,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=Non
         setattr(o, name, x)
     _one_device(tensors)
     with _On(logits.device):
-        need = lib.rg_sample_scratch(rows, vocab)
+        need = lib.rg_sample_scratch(rows, vocab, C.byref(o))
         tokens, lp = _empty(u, (rows,), _I32, stream), _empty(u, (2, rows), _F32, stream)
         scratch = _empty(u, (need // 4,), _F32, stream)
         _check(lib.rg_sample(1 if logits.dtype == _BF16 else 0, logits.data_ptr(), logits.stride(0), rows, vocab,

@@ -7,11 +7,28 @@
 // together keep one: the tokens up to a border (z, id).  The draw is the first token,
 // by id, at which the kept weights' running sum passes u times their sum.
 //
-// Two launches.  The first streams the logits once: maximum and sum of weights of
-// every segment of 512 tokens, the sum in fp32 with respect to that maximum.  The
-// second, a workgroup a row, finds the border and draws.
-// Weights of the kept tokens are whole numbers, w 2^42 to nearest: their sums do not
-// depend on any order, so LDS atomics give the same draw on every run.
+// A vocabulary has as many places where a draw turns on the running sum, so that sums
+// which are 1e-8 off, as those of fp32 weights are, draw another token in one row of a
+// thousand.  Weights are therefore fp64, by a polynomial of their own (exp2_64, 1e-12):
+// 16 instructions a token, which still fit under the bytes of fp32 logits.  Where
+// something is cut the weights are whole numbers, w 2^42 to nearest: their sums do not
+// depend on any order, so atomics give the same draw on every run.
+//
+// Launches:
+// * scan, a wave a segment of 512 tokens: maximum, and sum of weights with respect to
+//   it.  It streams the logits once.
+// * only where top-p or min-p may cut a row without top-k: histogram and collect, some
+//   workgroups a row.  The first adds up weights by bins of z; the second finds the bin
+//   in which the border of top-p lies, sums what is kept above it by segments, and
+//   lists the tokens in it.
+// * pick, a workgroup a row: the border, then the segment, then the token.
+// The last three look only at segments that can hold kept tokens:
+// * weights below 2^-43 of the largest count nothing;
+// * k segments with a maximum of t or more hold k tokens of t or more, so the border of
+//   top-k lies there or above;
+// * what lies below t weighs no more than the segments whose maximum is below t and
+//   512 w(t) of each other, and where that is at most 1 - p of all, the border of
+//   top-p lies at t or above.
 #include <algorithm>
 #include <type_traits>
 
@@ -19,34 +36,105 @@
 
 namespace {
 
+typedef unsigned long long u64;
+
 constexpr int SEG = 512;              // tokens of a segment
 constexpr int MAX_SEGS = 2048;        // of a row: 2^20 tokens
 constexpr int SCAN_WAVES = 4;
-constexpr int PICK = 512;             // threads of a row in the second launch
-constexpr int BINS = 2 * PICK;        // of weights, 16 an octave
-constexpr int LIST = 4096;            // candidates that LDS holds
-constexpr int FEW = 64;               // tokens that a wave puts in order, a lane each
-constexpr float LOG2E = 1.44269504088896341f;
+constexpr int PICK = 512;             // threads of a row's pick
+constexpr int PART = 256;             // threads of a part of a row's histogram
+constexpr int BINS = 2 * PICK;        // of z, 16 an octave of weight
+constexpr int LIST = 4096;            // tokens that a row's list holds
+constexpr int FEW = 128;              // tokens that are put in order by comparing all of them
+constexpr int ID_BITS = 20;
+constexpr double LOG2E = 1.4426950408889634;
+constexpr double FIXED_ONE = 4398046511104.0;   // 2^42
+constexpr float FIXED_OCTAVES = 43.5f;          // weights below 2^-43 are 0 in whole numbers
 
 // Settings of a row.
 struct RowOpts {
-  float temperature, top_p, min_p;
+  double temperature, top_p, min_p;
   int top_k;
+  bool by_k, by_p, by_min;
+  double c;                           // octaves of weight per logit; T = 0 reports at 1
 };
 __device__ __forceinline__ RowOpts row_opts(const DrawArgs& A, int r) {
   RowOpts o;
-  o.temperature = A.temperature_rows ? A.temperature_rows[r] : A.temperature;
+  o.temperature = A.temperature_rows ? (double)A.temperature_rows[r] : A.temperature;
   o.top_k = A.top_k_rows ? A.top_k_rows[r] : A.top_k;
-  o.top_p = A.top_p_rows ? A.top_p_rows[r] : A.top_p;
-  o.min_p = A.min_p_rows ? A.min_p_rows[r] : A.min_p;
+  o.top_p = A.top_p_rows ? (double)A.top_p_rows[r] : A.top_p;
+  o.min_p = A.min_p_rows ? (double)A.min_p_rows[r] : A.min_p;
+  o.by_k = o.top_k > 0 && o.top_k < A.vocab;
+  o.by_p = o.top_p < 1.0;
+  o.by_min = o.min_p > 0.0;
+  o.c = o.temperature == 0.0 ? LOG2E : LOG2E / o.temperature;
   return o;
 }
-// Base-2 exponent of a weight per logit; temperature 0 (the largest logit) reports at 1.
-// Tiny temperatures: a finite factor, as 0 times infinity would be NaN.
-__device__ __forceinline__ float inv_temperature(float t) { return t == 0.f ? LOG2E : fminf(LOG2E / t, 3.0e38f); }
+__device__ __forceinline__ bool usable(const RowOpts& o) {
+  return o.temperature >= 0.0 && o.temperature < (double)INFINITY && o.top_p == o.top_p && o.min_p == o.min_p;
+}
+
+// 2^t for t in [-1000, 1000]: 2^n times a polynomial of degree 8 that interpolates 2^f
+// at the Chebyshev points of [-1/2, 1/2], 1.1e-12 relative.
+__device__ __forceinline__ double exp2_64(double t) {
+  constexpr double shifter = 6755399441055744.0;              // 1.5 * 2^52: the sum's low bits are t to nearest
+  const double s = t + shifter, f = t - (s - shifter);
+  double p = 1.3255224884799127e-06;
+  p = fma(p, f, 1.5310079402383103e-05);
+  p = fma(p, f, 0.00015403455852419016);
+  p = fma(p, f, 0.0013333450568000008);
+  p = fma(p, f, 0.00961812915940262);
+  p = fma(p, f, 0.05550410941205934);
+  p = fma(p, f, 0.2402265069581299);
+  p = fma(p, f, 0.6931471805459335);
+  p = fma(p, f, 1.0);
+  const u64 b = __builtin_bit_cast(u64, p);
+  return __builtin_bit_cast(double, b + ((u64)(uint32_t)__builtin_bit_cast(u64, s) << 52));
+}
+// The weight of z with respect to top (finite, no less): octaves below 1000 count nothing.
+__device__ __forceinline__ double weight_of(float z, float top, double c) {
+  return exp2_64(fmax(((double)z - (double)top) * c, -1000.0));
+}
+// w 2^42 to nearest.
+__device__ __forceinline__ u64 fixed_of(double w) {
+  return __builtin_bit_cast(u64, fma(w, FIXED_ONE, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;   // 2^52 + w 2^42
+}
+
+// NaN where either is.
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v) {            // lanes without a source: 0
+  const u64 b = __builtin_bit_cast(u64, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (u64)hi << 32 | lo);
+}
+// Over the wave's lanes; the result is in lane 63.
+__device__ __forceinline__ double sum_to_63(double v) {
+  v += moved<0x111, 0xf>(v);          // row_shr 1, 2, 4, 8, then row_bcast 15 and 31
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);
+  v += moved<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ float max_nan_wave(float v) {
+#define RG_MAX(ctrl) \
+  v = max_nan(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), ctrl, 0xf, 0xf, false)))
+  RG_MAX(0x111);
+  RG_MAX(0x112);
+  RG_MAX(0x114);
+  RG_MAX(0x118);
+  RG_MAX(0x142);
+  RG_MAX(0x143);
+#undef RG_MAX
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
 
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int64_t i, int64_t n, float (&v)[8]) {
+__device__ __forceinline__ void load8(const T* p, int i, int n, float (&v)[8]) {
   if (VEC && i + 8 <= n) {
     ld_elems<8, true>(p + i, v);
   } else {
@@ -55,36 +143,38 @@ __device__ __forceinline__ void load8(const T* p, int64_t i, int64_t n, float (&
   }
 }
 
-// ---------------------------------------------------------------- segments
+// ---------------------------------------------------------------- scan
 template <typename T, bool VEC>
 __global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int segs, int64_t items) {
   const int lane = threadIdx.x & 63;
   const int64_t item = (int64_t)blockIdx.x * SCAN_WAVES + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (item >= items) return;
   const int r = (int)(item / segs), seg = (int)(item - (int64_t)r * segs);
-  const float c = inv_temperature(A.temperature_rows ? A.temperature_rows[r] : A.temperature);
+  const double temperature = A.temperature_rows ? (double)A.temperature_rows[r] : A.temperature;
+  const double c = temperature == 0.0 ? LOG2E : LOG2E / temperature;
   float v[8];
-  load8<T, VEC>((const T*)A.logits + r * A.row, (int64_t)seg * SEG + 8 * lane, A.vocab, v);
+  load8<T, VEC>((const T*)A.logits + r * A.row, seg * SEG + 8 * lane, A.vocab, v);
   float m = v[0];
 #pragma unroll
-  for (int e = 1; e < 8; ++e) m = fmaxf(m, v[e]);
-  m = wave_max(m);
-  const float ref = m == -INFINITY ? 0.f : m;     // nothing here: weights exp2(-inf) = 0
-  float s = 0.f;
+  for (int e = 1; e < 8; ++e) m = max_nan(m, v[e]);
+  m = max_nan_wave(m);
+  double s = 0.0;
+  if (m > -INFINITY && m < INFINITY) {            // else the sum is not looked at, or nothing
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f((v[e] - ref) * c);
-  s = wave_sum(s);
-  if (lane == 0) {
-    A.seg[2 * item] = m;
-    A.seg[2 * item + 1] = s;
+    for (int e = 0; e < 8; ++e) s += weight_of(v[e], m, c);   // the maximum's is 1 exactly
+    s = sum_to_63(s);
+  }
+  if (lane == 63) {
+    A.seg_m[item] = m;
+    A.seg_s[item] = s;
+  }
+  if (A.bins) {                                   // the histogram begins empty
+    const int per = (BINS + segs - 1) / segs;
+    for (int i = seg * per + lane; i < min(seg * per + per, BINS); i += 64) A.bins[(int64_t)r * BINS + i] = 0;
   }
 }
 
 // ---------------------------------------------------------------- a row
-typedef unsigned long long u64;
-constexpr double FIXED_ONE = 4398046511104.0;   // 2^42
-constexpr int ID_BITS = 20;
-
 // Order of z as whole numbers, and back.
 __device__ __forceinline__ uint32_t key_of(float z) {
   const uint32_t u = __float_as_uint(z == 0.f ? 0.f : z);       // -0 is 0
@@ -98,17 +188,9 @@ __device__ __forceinline__ u64 place_of(float z, int id) {
 __device__ __forceinline__ float z_of(u64 place) { return of_key((uint32_t)(place >> ID_BITS)); }
 __device__ __forceinline__ int id_of(u64 place) { return (1 << ID_BITS) - 1 - (int)(place & ((1 << ID_BITS) - 1)); }
 
-// w 2^42 of a weight in [0, 1], to nearest.
-__device__ __forceinline__ u64 fixed_weight(float w) {
-  const uint32_t u = __float_as_uint(w);
-  const int e = (int)(u >> 23) - 127 + 19;                      // 42 - 23
-  const u64 m = (u & 0x7FFFFFu) | 0x800000u;
-  return e >= 0 ? m << e : e < -24 ? 0 : (m + (1ull << (-e - 1))) >> -e;
-}
-
-// Over the PICK threads of a row; `red` holds a value a wave.
-template <typename V>
-__device__ __forceinline__ V row_prefix(V v, V* red, V* total) {   // inclusive
+// Over a workgroup of N threads; `red` holds a value a wave.
+template <int N, typename V>
+__device__ __forceinline__ V group_prefix(V v, V* red, V* total) {   // inclusive
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -120,25 +202,15 @@ __device__ __forceinline__ V row_prefix(V v, V* red, V* total) {   // inclusive
   __syncthreads();
   V all = 0;
 #pragma unroll
-  for (int i = 0; i < PICK / 64; ++i) {
+  for (int i = 0; i < N / 64; ++i) {
     if (i < w) v += red[i];
     all += red[i];
   }
   *total = all;
   return v;
 }
-__device__ __forceinline__ double row_sum(double v, double* red) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  v = wave_sum_d(v);
-  __syncthreads();
-  if (lane == 0) red[w] = v;
-  __syncthreads();
-  double r = 0.0;
-#pragma unroll
-  for (int i = 0; i < PICK / 64; ++i) r += red[i];
-  return r;
-}
-__device__ __forceinline__ int row_min(int v, int* red) {
+template <int N>
+__device__ __forceinline__ int group_min(int v, int* red) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
@@ -146,84 +218,299 @@ __device__ __forceinline__ int row_min(int v, int* red) {
   if (lane == 0) red[w] = v;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < PICK / 64; ++i) v = min(v, red[i]);
+  for (int i = 0; i < N / 64; ++i) v = min(v, red[i]);
   return v;
 }
 
+// What the threads of a row share.
 struct RowMemory {
-  float m[MAX_SEGS], s[MAX_SEGS];     // of the segments
-  double red[PICK / 64];
-  u64 red64[PICK / 64];
-  float redf[16];
-  int redi[PICK / 64];
-  double start;
+  float m[MAX_SEGS];                  // maxima of the segments
+  float share[MAX_SEGS];              // their sums with respect to the row's maximum
+  uint16_t active[MAX_SEGS];          // segments that can hold kept tokens
+  double redd[8];
+  u64 red[8];
+  float redf[8];
+  int redi[8];
+  int passes[8];
+  int n_active;
 };
+
+template <typename T, bool VEC, int N>
+struct Row {
+  const T* z;
+  int vocab, segs;
+  float zmax;
+  double c, total;
+  RowMemory* S;
+
+  // The row's segments; false where it has no answer.
+  __device__ bool read(const DrawArgs& A, int r, int n_segs, const RowOpts& o) {
+    const int tid = threadIdx.x;
+    z = (const T*)A.logits + r * A.row;
+    vocab = A.vocab;
+    segs = n_segs;
+    c = o.c;
+    float m = -INFINITY;
+    for (int i = tid; i < segs; i += N) {
+      const float x = A.seg_m[(int64_t)r * segs + i];
+      S->m[i] = x;
+      m = max_nan(m, x);
+    }
+    m = max_nan_wave(m);
+    if ((tid & 63) == 0) S->redf[tid >> 6] = m;
+    __syncthreads();
+    m = S->redf[0];
+#pragma unroll
+    for (int i = 1; i < N / 64; ++i) m = max_nan(m, S->redf[i]);
+    zmax = m;
+    if (!(zmax > -INFINITY && zmax < INFINITY) || !usable(o)) return false;   // NaN too
+    double part = 0.0;
+    for (int i = tid; i < segs; i += N) {
+      const double w = share_of(A, r, i);
+      S->share[i] = (float)w;
+      part += w;
+    }
+    part = sum_to_63(part);
+    if ((tid & 63) == 63) S->redd[tid >> 6] = part;
+    __syncthreads();
+    total = 0.0;
+#pragma unroll
+    for (int i = 0; i < N / 64; ++i) total += S->redd[i];
+    return true;
+  }
+  __device__ double share_of(const DrawArgs& A, int r, int i) const {
+    const float m = S->m[i];
+    return m == -INFINITY ? 0.0 : A.seg_s[(int64_t)r * segs + i] * weight_of(m, zmax, c);
+  }
+  __device__ u64 fixed(float x) const { return x == -INFINITY ? 0 : fixed_of(weight_of(x, zmax, c)); }
+  __device__ float octaves(float x) const { return (float)(((double)zmax - (double)x) * c); }
+
+  // The least z that can be kept (see above), of min-p's z where given: thresholds side
+  // by side, a wave each.
+  __device__ float least(bool by_k, int k, bool by_p, double p, float min_z) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int W = N / 64;
+    float lo = 0.f, hi = FIXED_OCTAVES;
+    if (by_k || by_p) {
+      const float spare = (float)((1.0 - fmax(p, 0.0)) * total * (1.0 - 1e-5));
+      for (int round = 0; round < (W == 8 ? 3 : 4); ++round) {
+        const float step = (hi - lo) / (W + 1), y = lo + step * (wave + 1);
+        const float cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
+        float below = 0.f;
+        int n = 0;
+        for (int i = lane; i < segs; i += 64) {
+          const bool above = octaves(S->m[i]) <= y;
+          n += above;
+          below += above ? fminf(S->share[i], cap) : S->share[i];
+        }
+        const bool pass = by_k ? wave_sum_dpp(n) >= k : wave_sum(below) <= spare;
+        __syncthreads();
+        if (lane == 0) S->passes[wave] = pass;
+        __syncthreads();
+        int first = W;
+        for (int i = W - 1; i >= 0; --i)
+          if (S->passes[i]) first = i;
+        hi = first == W ? hi : lo + step * (first + 1);
+        lo = lo + step * first;
+      }
+    }
+    const float t = (float)((double)zmax - ((double)hi + 1e-3) / c);
+    return fmaxf(t <= -3.4e38f ? -INFINITY : of_key(key_of(t) - 2), min_z);   // what was rounded on the way
+  }
+  // Lists the segments that can hold a token of t0 or more.
+  __device__ void activate(float t0) {
+    __syncthreads();
+    if (threadIdx.x == 0) S->n_active = 0;
+    __syncthreads();
+    for (int base = 0; base < segs; base += N) {
+      const int i = base + (int)threadIdx.x;
+      const bool on = i < segs && S->m[i] >= t0;
+      const uint64_t mask = __ballot(on);
+      int at = 0;
+      if ((threadIdx.x & 63) == 0 && mask) at = atomicAdd(&S->n_active, __popcll(mask));
+      at = __builtin_amdgcn_readfirstlane(at);
+      if (on) S->active[at + __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1))] = (uint16_t)i;
+    }
+    __syncthreads();
+  }
+  // f(z, id, whether it is a token of t0 or more) for the tokens of active segments; whole
+  // waves call it.  Four segments are on their way at once.
+  template <typename F>
+  __device__ void from_memory(float t0, F f) const {
+    constexpr int W = N / 64, U = 4;
+    const int lane = threadIdx.x & 63, n = S->n_active;
+    for (int a = (int)threadIdx.x >> 6; a < n; a += W * U) {
+      float v[U][8];
+      int first[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        first[j] = a + j * W < n ? (int)S->active[a + j * W] * SEG + 8 * lane : vocab;
+        load8<T, VEC>(z, first[j], vocab, v[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f(v[j][e], first[j] + e, first[j] + e < vocab && v[j][e] >= t0);
+    }
+  }
+};
+
+// min-p's border: the least fp32 value that is not below max z + T ln(min_p).
+__device__ __forceinline__ float min_p_border(const RowOpts& o, float zmax) {
+  const double lowest = (double)zmax + o.temperature * log(fmin(o.min_p, 1.0));
+  const float t = (float)lowest;
+  return (double)t < lowest ? of_key(key_of(t) + 1) : t;
+}
+
+// Which rows go by histogram: top-k's are few and the pick finds them alone.
+__device__ __forceinline__ bool by_bins(const RowOpts& o) { return o.temperature != 0.0 && !o.by_k && (o.by_p || o.by_min); }
+
+// Bin of z, 16 an octave of weight: falls as z grows.
+__device__ __forceinline__ int bin_of(float z, float zmax, float c) {
+  return (int)fminf(((zmax - z) * c) * 16.f, (float)(BINS - 1));
+}
+__device__ __forceinline__ float bin_factor(double c) { return (float)fmin(c, 3.0e38); }
+__device__ __forceinline__ double mass_limit(const RowOpts& o, double all) { return fmax(o.top_p * all, 0.5); }
+
+// Adds a token to a list where `on`; whole waves call it.
+__device__ __forceinline__ void append(bool on, u64 place, int* count, u64* list) {
+  const uint64_t mask = __ballot(on);
+  if (!mask) return;
+  const int lane = threadIdx.x & 63;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(count, __popcll(mask));
+  at = __builtin_amdgcn_readfirstlane(at) + __popcll(mask & ((1ull << lane) - 1));
+  if (on && at < LIST) list[at] = place;
+}
+
+// ---------------------------------------------------------------- histogram, collect
+template <typename T, bool VEC>
+__global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int parts) {
+  __shared__ RowMemory S;
+  __shared__ u64 mass[BINS];
+  const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
+  const RowOpts o = row_opts(A, r);
+  if (!by_bins(o)) return;
+  Row<T, VEC, PART> row{};
+  row.S = &S;
+  const bool good = row.read(A, r, segs, o);
+  float t0 = 0.f;
+  if (good) t0 = row.least(false, 0, o.by_p, o.top_p, o.by_min ? min_p_border(o, row.zmax) : -INFINITY);
+  if (part == 0 && tid == 0) A.info[r] = DrawRow{row.total, row.zmax, t0, good, 0, BINS, 0};
+  if (!good || !o.by_p) return;
+  for (int i = tid; i < BINS; i += PART) mass[i] = 0;
+  __syncthreads();
+  const float c = bin_factor(o.c);
+  const int lane = tid & 63;
+  for (int s = part + parts * (tid >> 6); s < segs; s += parts * (PART / 64)) {
+    if (S.m[s] < t0) continue;
+    float v[8];
+    load8<T, VEC>(row.z, s * SEG + 8 * lane, A.vocab, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (v[e] >= t0 && v[e] > -INFINITY) atomicAdd(&mass[bin_of(v[e], row.zmax, c)], row.fixed(v[e]));
+  }
+  __syncthreads();
+  for (int i = tid; i < BINS; i += PART)
+    if (mass[i]) atomicAdd(&A.bins[(int64_t)r * BINS + i], mass[i]);
+}
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int parts) {
+  __shared__ u64 red[8];
+  __shared__ int redi[8];
+  const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
+  const RowOpts o = row_opts(A, r);
+  if (!by_bins(o)) return;
+  const DrawRow info = A.info[r];
+  if (!info.good) return;
+  int border = BINS;                  // the bin in which top-p's border lies
+  u64 above = 0;                      // weight of the bins before it
+  if (o.by_p) {
+    const double limit = mass_limit(o, info.total * FIXED_ONE);
+    constexpr int PER = BINS / PART;
+    u64 mine[PER], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      mine[i] = A.bins[(int64_t)r * BINS + tid * PER + i];
+      sum += mine[i];
+    }
+    u64 end = group_prefix<PART>(sum, red, &all);
+    int hit = BINS;
+    u64 before = end;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i) {
+      if (mine[i] && (double)end >= limit) {
+        hit = tid * PER + i;
+        before = end - mine[i];
+      }
+      end -= mine[i];
+    }
+    border = group_min<PART>(hit, redi);
+    if (hit == border && border < BINS) red[0] = before;
+    __syncthreads();
+    above = border < BINS ? red[0] : 0;
+  }
+  if (part == 0 && tid == 0) {
+    A.info[r].bin = border;
+    A.info[r].above = above;
+  }
+  const T* z = (const T*)A.logits + r * A.row;
+  const float c = bin_factor(o.c);
+  const int lane = tid & 63;
+  for (int s = part + parts * (tid >> 6); s < segs; s += parts * (PART / 64)) {
+    u64 kept = 0;
+    if (A.seg_m[(int64_t)r * segs + s] >= info.t0) {
+      float v[8];
+      const int i = s * SEG + 8 * lane;
+      load8<T, VEC>(z, i, A.vocab, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool on = v[e] >= info.t0 && v[e] > -INFINITY;
+        const int b = on ? bin_of(v[e], info.zmax, c) : BINS;
+        if (b < border) kept += fixed_of(weight_of(v[e], info.zmax, o.c));
+        append(b == border && on, place_of(v[e], i + e), &A.info[r].listed, A.list + (int64_t)r * LIST);
+      }
+#pragma unroll
+      for (int x = 32; x > 0; x >>= 1) kept += __shfl_xor(kept, x, 64);
+    }
+    if (lane == 0) A.kept_seg[(int64_t)r * segs + s] = kept;
+  }
+}
+
+// ---------------------------------------------------------------- pick
 struct CutMemory {
   union {
     struct { u64 mass[BINS]; uint32_t count[BINS]; } bin;
     u64 seg[MAX_SEGS];                // kept weight of each segment
   };
   u64 list[LIST];                     // places of the tokens that can be kept
-  u64 few[FEW];
+  u64 few[FEW], weight[FEW];
   u64 found, mass, rank;
   int n_list, n_few;
 };
 
-// What a row's threads know of it.
-template <typename T, bool VEC>
-struct Row {
-  const T* z;
-  int vocab, segs, top;               // top: the first segment that holds the maximum
-  float zmax, c;
-  RowMemory* S;
-
-  __device__ float token(int s) const {   // a thread a token of segment s
-    const int i = s * SEG + (int)threadIdx.x;
-    return i < vocab ? ld_f32<T>(z + i) : -INFINITY;
-  }
-  __device__ float weight(float x) const { return __builtin_amdgcn_exp2f((x - zmax) * c); }
-  __device__ u64 fixed(float x) const { return fixed_weight(weight(x)); }
-  // f(z, id) for every token of at least t0; whole waves call it.
-  template <typename F>
-  __device__ void from_memory(float t0, F f) const {
-    for (int s = (int)threadIdx.x >> 6; s < segs; s += PICK / 64) {
-      if (S->m[s] < t0) continue;
-      float v[8];
-      const int i = s * SEG + 8 * ((int)threadIdx.x & 63);
-      load8<T, VEC>(z, i, vocab, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (i + e < vocab && v[e] >= t0) f(v[e], i + e);
-    }
-  }
-};
-
 // The border of top-k (by rank: fewer than `limit` tokens come before) or top-p (less
-// than `limit` of weight does): the place of the last token that is kept, 0 if all of
-// them are; mass: the weight up to it.  Bins of weight first, then ever finer windows
-// of places, until a wave can put what is left in order.
+// than `limit` of weight does) among the tokens that `each` gives, mass0 of weight in
+// front of them, none outside the places lo .. hi: the place of the last that is kept, 0
+// if all of them are; mass: the weight up to it.  Windows of places, ever finer by 1024,
+// until what is left is few enough to compare with one another.
 template <typename R, typename Each>
-__device__ u64 find_border(const R& row, CutMemory& C, const Each& each, bool by_rank, double limit, u64* mass) {
+__device__ u64 find_border(const R& row, CutMemory& C, const Each& each, bool by_rank, double limit, u64 lo, u64 hi,
+                           u64 mass0, u64* mass) {
   const int tid = threadIdx.x;
-  auto bin_of = [&](float x) { return (int)fminf((row.zmax - x) * row.c * 16.f, (float)(BINS - 1)); };   // falls as x grows
-  u64 rank0 = 0, mass0 = 0;           // before the window
-  u64 lo = 0;
-  int shift = 64, bin = 0;            // the window: places lo .. lo + 2^shift - 1 of the bin
-  for (int level = 0;; ++level) {
+  u64 rank0 = 0;                      // before the window
+  auto reaches = [&](u64 rank, u64 weight) { return by_rank ? (double)rank >= limit : (double)weight >= limit; };
+  for (;;) {
     __syncthreads();
     for (int i = tid; i < BINS; i += PICK) { C.bin.mass[i] = 0; C.bin.count[i] = 0; }
     if (tid == 0) C.n_few = 0;
     __syncthreads();
-    const int next = level == 0 ? 0 : max(shift - 10, 0);
+    const int shift = max(54 - __clzll((long long)(hi - lo | 1)), 0);   // (hi - lo) >> shift is below 1024
     each([&](float x, int id) {
-      int d;
-      if (level == 0) {
-        d = bin_of(x);
-      } else {
-        const u64 p = place_of(x, id);
-        if (bin_of(x) != bin || p < lo || (p - lo) >> shift) return;
-        d = BINS - 1 - (int)((p - lo) >> next);
-      }
+      const u64 p = place_of(x, id);
+      if (p < lo || p > hi) return;
+      const int d = BINS - 1 - (int)((p - lo) >> shift);
       atomicAdd(&C.bin.mass[d], row.fixed(x));
       atomicAdd(&C.bin.count[d], 1u);
     });
@@ -232,13 +519,12 @@ __device__ u64 find_border(const R& row, CutMemory& C, const Each& each, bool by
     const u64 m0 = C.bin.mass[2 * tid], m1 = C.bin.mass[2 * tid + 1];
     const uint32_t n0 = C.bin.count[2 * tid], n1 = C.bin.count[2 * tid + 1];
     u64 all_m, all_n;
-    const u64 m = row_prefix(m0 + m1, row.S->red64, &all_m) + mass0;
-    const u64 n = row_prefix((u64)(n0 + n1), row.S->red64, &all_n) + rank0;
-    auto reaches = [&](u64 rank, u64 weight) { return by_rank ? (double)rank >= limit : (double)weight >= limit; };
+    const u64 m = group_prefix<PICK>(m0 + m1, row.S->red, &all_m) + mass0;
+    const u64 n = group_prefix<PICK>((u64)(n0 + n1), row.S->red, &all_n) + rank0;
     int hit = INT32_MAX;
     if (n1 && reaches(n, m)) hit = 2 * tid + 1;
     if (n0 && reaches(n - n1, m - m1)) hit = 2 * tid;
-    const int d = row_min(hit, row.S->redi);
+    const int d = group_min<PICK>(hit, row.S->redi);
     if (d == INT32_MAX) {             // the limit lies behind the last token
       *mass = mass0 + all_m;
       return 0;
@@ -250,30 +536,31 @@ __device__ u64 find_border(const R& row, CutMemory& C, const Each& each, bool by
     __syncthreads();
     mass0 = C.mass;
     rank0 = C.rank;
-    const uint32_t inside = C.bin.count[d];
-    if (level == 0) {
-      bin = d;
-      lo = 0;
-      shift = 32 + ID_BITS;
-    } else {
-      lo += (u64)(BINS - 1 - d) << next;
-      shift = next;
-    }
-    if (inside > FEW) continue;       // places differ: at the latest a window of 1 has one token
+    const int inside = (int)min(C.bin.count[d], (uint32_t)FEW + 1);
+    lo += (u64)(BINS - 1 - d) << shift;
+    hi = min(hi, lo + ((1ull << shift) - 1));
+    if (inside > FEW) continue;       // places differ: at the latest a window of one has one token
     each([&](float x, int id) {
       const u64 p = place_of(x, id);
-      if (bin_of(x) == bin && p >= lo && !((p - lo) >> shift)) C.few[atomicAdd(&C.n_few, 1)] = p;
+      if (p >= lo && p <= hi) {
+        const int i = atomicAdd(&C.n_few, 1);
+        C.few[i] = p;
+        C.weight[i] = row.fixed(x);
+      }
     });
     __syncthreads();
-    if (tid < 64) {
-      const u64 p = tid < (int)inside ? C.few[tid] : 0;
-      const u64 w = tid < (int)inside ? row.fixed(z_of(p)) : 0;
+    if (tid < inside) {
+      const u64 p = C.few[tid];
       u64 before = mass0, rank = rank0;
-      for (int j = 0; j < (int)inside; ++j) {
-        const u64 q = C.few[j], v = row.fixed(z_of(q));
-        if (q > p) { ++rank; before += v; }
+      for (int j = 0; j < inside; ++j) {
+        const bool in_front = C.few[j] > p;
+        rank += in_front;
+        before += in_front ? C.weight[j] : 0;
       }
-      if (tid < (int)inside && !reaches(rank, before) && reaches(rank + 1, before + w)) { C.found = p; C.mass = before + w; }
+      if (!reaches(rank, before) && reaches(rank + 1, before + C.weight[tid])) {
+        C.found = p;
+        C.mass = before + C.weight[tid];
+      }
     }
     __syncthreads();
     *mass = C.mass;
@@ -285,171 +572,208 @@ template <typename T, bool VEC, bool CUT>
 __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs) {
   __shared__ RowMemory S;
   __shared__ typename std::conditional<CUT, CutMemory, int>::type cut;
+  __shared__ u64 start;
   const int r = blockIdx.x, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
-  const float* seg = A.seg + (int64_t)r * segs * 2;
   const double u = A.u64 ? ((const double*)A.u)[r] : (double)((const float*)A.u)[r];
-  Row<T, VEC> row{(const T*)A.logits + r * A.row, A.vocab, segs, 0, -INFINITY, inv_temperature(o.temperature), &S};
-
-  float zmax = -INFINITY;
-  for (int i = tid; i < segs; i += PICK) {
-    S.m[i] = seg[2 * i];
-    S.s[i] = seg[2 * i + 1];
-    zmax = fmaxf(zmax, S.m[i]);
-  }
-  row.zmax = zmax = block_max(zmax, S.redf);
-  int top = INT32_MAX;
-  for (int i = tid; i < segs; i += PICK)
-    if (S.m[i] == zmax) top = min(top, i);
-  row.top = top = row_min(top, S.redi);
-  // The sum of all weights.  That of the segment which holds the maximum is taken
-  // again in 64 bits: a weight of 1 beside small ones.
-  auto share = [&](int i) { return S.m[i] == -INFINITY ? 0.0 : (double)S.s[i] * (double)row.weight(S.m[i]); };
-  double part = 0.0;
-  for (int i = tid; i < segs; i += PICK)
-    if (i != top) part += share(i);
-  const double others = row_sum(part, S.red);
-  const double largest = row_sum(top < segs && top * SEG + tid < A.vocab ? (double)row.weight(row.token(top)) : 0.0, S.red);
-  const double total = others + largest;
-
-  // NaN logits make the total NaN, as does an infinite maximum
-  const bool good = zmax > -INFINITY && zmax < INFINITY && total < INFINITY && o.temperature >= 0.f &&
-                    o.temperature < INFINITY && u >= 0.0 && u < 1.0 && o.top_p == o.top_p && o.min_p == o.min_p;
-  if (!good) {
+  Row<T, VEC, PICK> row{};
+  row.S = &S;
+  if (!row.read(A, r, segs, o) || !(u >= 0.0 && u < 1.0)) {
     if (tid == 0) {
       A.token[r] = -1;
       A.logprob[r] = A.kept[r] = __uint_as_float(0x7FC00000u);
     }
     return;
   }
-  const double inv_t = o.temperature == 0.f ? 1.0 : 1.0 / (double)o.temperature;
-  auto answer = [&](int id, float zi, double log_kept) {
-    const double lw = ((double)zi - (double)zmax) * inv_t;
+  const double inv_t = o.temperature == 0.0 ? 1.0 : 1.0 / o.temperature;
+  auto answer = [&](int id, float zi, double kept) {
+    const double lw = ((double)zi - (double)row.zmax) * inv_t;
     A.token[r] = id;
-    A.logprob[r] = (float)(lw - log(total));
-    A.kept[r] = (float)(o.temperature == 0.f ? 0.0 : lw - log_kept);
+    A.logprob[r] = (float)(lw - log(row.total));
+    A.kept[r] = (float)(o.temperature == 0.0 ? 0.0 : lw - log(kept));
   };
-  // The token of segment s at which the running sum, `before` in front of it, passes
-  // `want`; w is the weight of the thread's token.
-  auto finish = [&](int s, float zi, auto w, auto before, double want, double log_kept) {
+  static_assert(PICK == SEG, "a thread a token of a segment");
+  auto token = [&](int s) {
+    const int i = s * SEG + tid;
+    return i < A.vocab ? ld_f32<T>(row.z + i) : -INFINITY;
+  };
+  // The token of segment s at which the running sum, `before` in front of the segment,
+  // passes `want`; w is the weight of the thread's token.
+  auto finish = [&](int s, float zi, auto w, auto before, double want, double kept) {
     decltype(w) all;
-    const auto incl = row_prefix(w, reinterpret_cast<decltype(w)*>(S.red64), &all) + before;
-    int hit = row_min(w > 0 && (double)incl > want ? tid : INT32_MAX, S.redi);
-    if (hit == INT32_MAX) hit = -row_min(w > 0 ? -tid : 1, S.redi);   // roundings next to u = 1: the last with a weight
-    if (tid == hit) answer(s * SEG + tid, zi, log_kept);
+    const auto end = group_prefix<PICK>(w, reinterpret_cast<decltype(w)*>(S.red), &all) + before;
+    int hit = group_min<PICK>(w > 0 && (double)end > want ? tid : INT32_MAX, S.redi);
+    if (hit == INT32_MAX) hit = -group_min<PICK>(w > 0 ? -tid : 1, S.redi);   // roundings next to u = 1: the last with a weight
+    if (tid == hit) answer(s * SEG + tid, zi, kept);
   };
   // The first segment at whose end the running sum of f(segment) passes `want`, and the
-  // sum in front of it.
-  auto find_segment = [&](auto f, double want, auto& before) {
+  // sum in front of it.  Where roundings next to u = 1 leave none: the last that has a
+  // weight, and nothing that its tokens could pass.
+  auto find_segment = [&](auto f, double& want, auto& before) {
     using V = typename std::remove_reference<decltype(before)>::type;
     V run = 0;
+    int last = 0;
     for (int base = 0; base < segs; base += PICK) {
       const int i = base + tid;
       const V w = i < segs ? f(i) : 0;
       V all;
-      const V incl = row_prefix(w, reinterpret_cast<V*>(S.red64), &all) + run;
-      const int at = row_min(w > 0 && (double)incl > want ? i : INT32_MAX, S.redi);
+      const V end = group_prefix<PICK>(w, reinterpret_cast<V*>(S.red), &all) + run;
+      const int at = group_min<PICK>(w > 0 && (double)end > want ? i : INT32_MAX, S.redi);
       if (at != INT32_MAX) {
-        if (i == at) *reinterpret_cast<V*>(&S.start) = incl - w;
+        if (i == at) *reinterpret_cast<V*>(&start) = end - w;
         __syncthreads();
-        before = *reinterpret_cast<V*>(&S.start);
+        before = *reinterpret_cast<V*>(&start);
         return at;
       }
+      last = max(last, -group_min<PICK>(w > 0 ? -i : 0, S.redi));
       run += all;
     }
     before = 0;
-    return top;
+    want = INFINITY;
+    return last;
   };
 
-  if (o.temperature == 0.f) {         // the first of the largest
-    const float zi = row.token(top);
-    const int at = row_min(zi == zmax ? tid : INT32_MAX, S.redi);
-    if (tid == at) answer(top * SEG + tid, zi, 0.0);
+  if (o.temperature == 0.0) {         // the first of the largest
+    int top = INT32_MAX;
+    for (int i = tid; i < segs; i += PICK)
+      if (S.m[i] == row.zmax) top = min(top, i);
+    top = group_min<PICK>(top, S.redi);
+    const float zi = token(top);
+    const int at = group_min<PICK>(zi == row.zmax ? tid : INT32_MAX, S.redi);
+    if (tid == at) answer(top * SEG + tid, zi, 1.0);
     return;
   }
-  const bool by_k = o.top_k > 0 && o.top_k < A.vocab, by_p = o.top_p < 1.f, by_min = o.min_p > 0.f;
-  if (!CUT || !(by_k || by_p || by_min)) {   // every token can be drawn
-    double before;
-    const int at = find_segment([&](int i) { return i == top ? largest : share(i); }, u * total, before);
-    const float zi = row.token(at);
-    finish(at, zi, (double)row.weight(zi), before, u * total, log(total));
+  if (!CUT || !(o.by_k || o.by_p || o.by_min)) {   // every token can be drawn
+    double before, want = u * row.total;
+    const int at = find_segment([&](int i) { return row.share_of(A, r, i); }, want, before);
+    const float zi = token(at);
+    finish(at, zi, zi == -INFINITY ? 0.0 : weight_of(zi, row.zmax, row.c), before, want, row.total);
     return;
   }
   if constexpr (CUT) {
     CutMemory* const C = &cut;
-    float t0 = -INFINITY;             // no token below it is kept
-    u64 border = 0;
-    if (by_min) {                     // the least fp32 value that is not below max z + T ln(min_p)
-      const double lowest = (double)zmax + (double)o.temperature * log(fmin((double)o.min_p, 1.0));
-      float t = (float)lowest;
-      if ((double)t < lowest) t = of_key(key_of(t) + 1);
-      border = (u64)key_of(t) << ID_BITS;
-      if (!by_k || !by_p) t0 = t;     // top-p takes its share of all the k
+    u64 border = 0, kept = 0;
+    float t0;                         // no token below it is kept
+    const float min_z = o.by_min ? min_p_border(o, row.zmax) : -INFINITY;
+    if (o.by_min) border = (u64)key_of(min_z) << ID_BITS;
+    DrawRow info{};
+    bool binned = by_bins(o);
+    if (binned) {
+      info = A.info[r];
+      binned = info.listed <= LIST;
+      t0 = info.t0;
+    } else {                          // top-p takes its share of all the k
+      t0 = row.least(o.by_k, o.top_k, false, 1.0, o.by_p ? -INFINITY : min_z);
     }
     if (tid == 0) C->n_list = 0;
+    row.activate(t0);
+    int n_list;
+    if (binned) {
+      n_list = info.listed;
+      for (int i = tid; i < n_list; i += PICK) C->list[i] = A.list[(int64_t)r * LIST + i];
+    } else {
+      row.from_memory(t0, [&](float x, int id, bool on) { append(on && x > -INFINITY, place_of(x, id), &C->n_list, C->list); });
+      __syncthreads();
+      n_list = C->n_list;
+    }
     __syncthreads();
-    row.from_memory(t0, [&](float x, int id) {
-      const int n = atomicAdd(&C->n_list, 1);
-      if (n < LIST) C->list[n] = place_of(x, id);
-    });
-    __syncthreads();
-    const int n_list = C->n_list;
     auto each = [&](auto f) {
       if (n_list <= LIST) {
         for (int i = tid; i < n_list; i += PICK) f(z_of(C->list[i]), id_of(C->list[i]));
       } else {
-        row.from_memory(t0, f);
+        row.from_memory(t0, [&](float x, int id, bool on) {
+          if (on && x > -INFINITY) f(x, id);
+        });
       }
     };
-    double all = total * FIXED_ONE;
-    if (by_k) {
+    const u64 lo = place_of(t0, (1 << ID_BITS) - 1), hi = place_of(row.zmax, 0);
+    if (o.by_k) {
       u64 mass;
-      border = max(border, find_border(row, *C, each, true, (double)o.top_k, &mass));
-      all = (double)mass;
-    }
-    if (by_p) {
+      border = max(border, find_border(row, *C, each, true, (double)o.top_k, lo, hi, 0, &mass));
+      if (o.by_p) border = max(border, find_border(row, *C, each, false, mass_limit(o, (double)mass), lo, hi, 0, &mass));
+    } else if (o.by_p && !(binned && info.bin == BINS)) {
       u64 mass;
-      border = max(border, find_border(row, *C, each, false, fmax((double)o.top_p * all, 0.5), &mass));
+      border = max(border, find_border(row, *C, each, false, mass_limit(o, row.total * FIXED_ONE), lo, hi,
+                                       binned ? info.above : 0, &mass));
     }
     __syncthreads();
-    for (int i = tid; i < MAX_SEGS; i += PICK) C->seg[i] = 0;
+    for (int i = tid; i < segs; i += PICK) C->seg[i] = binned ? A.kept_seg[(int64_t)r * segs + i] : 0;
     __syncthreads();
     each([&](float x, int id) {
       if (place_of(x, id) >= border) atomicAdd(&C->seg[id / SEG], row.fixed(x));
     });
     __syncthreads();
-    u64 mine = 0, kept, before;
+    u64 mine = 0, before;
     for (int i = tid; i < segs; i += PICK) mine += C->seg[i];
-    row_prefix(mine, S.red64, &kept);
-    const int at = find_segment([&](int i) { return C->seg[i]; }, u * (double)kept, before);
-    const float zi = row.token(at);
+    group_prefix<PICK>(mine, S.red, &kept);
+    double want = u * (double)kept;
+    const int at = find_segment([&](int i) { return C->seg[i]; }, want, before);
+    const float zi = token(at);
     const int id = at * SEG + tid;
-    finish(at, zi, id < A.vocab && place_of(zi, id) >= border ? row.fixed(zi) : (u64)0, before, u * (double)kept,
-           log((double)kept / FIXED_ONE));
+    finish(at, zi, id < A.vocab && place_of(zi, id) >= border ? row.fixed(zi) : (u64)0, before, want, (double)kept / FIXED_ONE);
   }
 }
 
 int segments(int vocab) { return (vocab + SEG - 1) / SEG; }
+
+// Whether rows may be cut, and whether some may go by histogram.
+bool may_cut(const DrawArgs& a) { return a.top_k_rows || a.top_p_rows || a.min_p_rows || a.top_k > 0 || a.top_p < 1.0 || a.min_p > 0.0; }
+bool may_bin(const DrawArgs& a) {
+  return (a.top_k_rows || a.top_k == 0 || a.top_k >= a.vocab) && (a.top_p_rows || a.min_p_rows || a.top_p < 1.0 || a.min_p > 0.0);
+}
+
+// Where the parts of the scratch are: a pointer is 0 bytes from its start where there is none.
+struct Scratch {
+  int64_t seg_s, seg_m, kept_seg, bins, list, info, end;
+};
+Scratch scratch_of(const DrawArgs& a) {
+  const int64_t rows = a.rows, n = rows * segments(a.vocab), binned = may_bin(a) ? rows : 0;
+  Scratch s;
+  s.seg_s = 0;
+  s.kept_seg = s.seg_s + 8 * n;
+  s.bins = s.kept_seg + (binned ? 8 * n : 0);
+  s.list = s.bins + 8 * binned * BINS;
+  s.info = s.list + 8 * binned * LIST;
+  s.seg_m = s.info + (int64_t)sizeof(DrawRow) * binned;
+  s.end = (s.seg_m + 4 * n + 15) / 16 * 16;
+  return s;
+}
 
 template <typename T, bool VEC>
 hipError_t run(const DrawArgs& a, hipStream_t st) {
   const int segs = segments(a.vocab);
   const int64_t items = (int64_t)a.rows * segs, grid = (items + SCAN_WAVES - 1) / SCAN_WAVES;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  const hipError_t e = kv8_launch(k_draw_scan<T, VEC>, dim3((unsigned)grid), dim3(64 * SCAN_WAVES), st, a, segs, items);
+  hipError_t e = kv8_launch(k_draw_scan<T, VEC>, dim3((unsigned)grid), dim3(64 * SCAN_WAVES), st, a, segs, items);
   if (e != hipSuccess) return e;
-  const bool cut = a.top_k_rows || a.top_p_rows || a.min_p_rows || a.top_k > 0 || a.top_p < 1.f || a.min_p > 0.f;
-  return cut ? kv8_launch(k_draw_pick<T, VEC, true>, dim3(a.rows), dim3(PICK), st, a, segs)
-             : kv8_launch(k_draw_pick<T, VEC, false>, dim3(a.rows), dim3(PICK), st, a, segs);
+  if (a.bins) {
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / a.rows, (segs + 7) / 8));
+    if ((int64_t)a.rows * parts > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 g((unsigned)(a.rows * parts));
+    if ((e = kv8_launch(k_draw_bins<T, VEC>, g, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
+    if ((e = kv8_launch(k_draw_collect<T, VEC>, g, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
+  }
+  return may_cut(a) ? kv8_launch(k_draw_pick<T, VEC, true>, dim3(a.rows), dim3(PICK), st, a, segs)
+                    : kv8_launch(k_draw_pick<T, VEC, false>, dim3(a.rows), dim3(PICK), st, a, segs);
 }
 
 }  // namespace
 
-int64_t draw_scratch_floats(int64_t rows, int vocab) { return 2 * rows * segments(vocab); }
+int64_t draw_scratch_bytes(const DrawArgs& a) { return scratch_of(a).end; }
 
-hipError_t launch_draw(const DrawArgs& a, hipStream_t st) {
+hipError_t launch_draw(DrawArgs a, void* scratch, hipStream_t st) {
   if (a.rows <= 0) return hipSuccess;
   if (a.vocab < 1 || a.vocab > DRAW_MAX_VOCAB) return hipErrorInvalidValue;
+  const Scratch s = scratch_of(a);
+  char* p = (char*)scratch;
+  a.seg_s = (double*)(p + s.seg_s);
+  a.seg_m = (float*)(p + s.seg_m);
+  if (may_bin(a)) {
+    a.kept_seg = (unsigned long long*)(p + s.kept_seg);
+    a.bins = (unsigned long long*)(p + s.bins);
+    a.list = (unsigned long long*)(p + s.list);
+    a.info = (DrawRow*)(p + s.info);
+  }
   const bool vec = (uintptr_t)a.logits % 16 == 0 && a.row * (a.dtype == 1 ? 2 : 4) % 16 == 0;
   if (a.dtype == 1) return vec ? run<bf16_t, true>(a, st) : run<bf16_t, false>(a, st);
   return vec ? run<float, true>(a, st) : run<float, false>(a, st);

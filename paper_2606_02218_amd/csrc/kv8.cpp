@@ -101,6 +101,22 @@ int tree_args(const char* who, const rg_kv8_batch* b, int32_t words) {
   return RG_OK;
 }
 
+// The sizes and settings of a sampling call.
+DrawArgs draw_args(int32_t rows, int32_t vocab, const rg_sample_options& o) {
+  DrawArgs a{};
+  a.rows = rows;
+  a.vocab = vocab;
+  a.temperature = o.temperature;
+  a.top_k = (int)std::min<int64_t>(o.top_k, INT32_MAX);
+  a.top_p = o.top_p;
+  a.min_p = o.min_p;
+  a.temperature_rows = o.temperature_rows;
+  a.top_k_rows = o.top_k_rows;
+  a.top_p_rows = o.top_p_rows;
+  a.min_p_rows = o.min_p_rows;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -272,9 +288,11 @@ int rg_kv8_accept(const rg_kv8_cache* cache, const rg_kv8_batch* batch, const ui
   return launched(who, launch_kv8_accept(pool, rows, mask, words, last, new_len, (hipStream_t)stream));
 }
 
-int64_t rg_sample_scratch(int32_t rows, int32_t vocab) {
-  if (rows < 0 || vocab < 1 || vocab > DRAW_MAX_VOCAB) return bad("rg_sample_scratch", "rows < 0, or vocab not in [1, 2^20]");
-  return 4 * draw_scratch_floats(rows, vocab);
+int64_t rg_sample_scratch(int32_t rows, int32_t vocab, const rg_sample_options* options) {
+  const char* who = "rg_sample_scratch";
+  if (!options) return bad(who, "NULL argument");
+  if (rows < 0 || vocab < 1 || vocab > DRAW_MAX_VOCAB) return bad(who, "rows < 0, or vocab not in [1, 2^20]");
+  return rows == 0 ? 0 : draw_scratch_bytes(draw_args(rows, vocab, *options));
 }
 
 int rg_sample(int32_t dtype, const void* logits, int64_t logits_row, int32_t rows, int32_t vocab, int32_t u_dtype, const void* u,
@@ -287,19 +305,24 @@ int rg_sample(int32_t dtype, const void* logits, int64_t logits_row, int32_t row
   if (rows < 0 || vocab < 1) return bad(who, "rows < 0 or vocab < 1");
   if (vocab > DRAW_MAX_VOCAB) return bad(who, "vocab exceeds 2^20", RG_EUNSUPPORTED);
   const rg_sample_options& o = *options;
-  if (!o.temperature_rows && !(o.temperature >= 0.f && std::isfinite(o.temperature))) return bad(who, "temperature must be >= 0");
+  if (!o.temperature_rows && !(o.temperature >= 0.0 && std::isfinite(o.temperature))) return bad(who, "temperature must be >= 0");
   if (!o.top_k_rows && o.top_k < 0) return bad(who, "top_k must be >= 0");
-  if (!o.top_p_rows && !(o.top_p > 0.f && o.top_p <= 1.f)) return bad(who, "top_p must be in (0, 1]");
-  if (!o.min_p_rows && !(o.min_p >= 0.f && o.min_p <= 1.f)) return bad(who, "min_p must be in [0, 1]");
+  if (!o.top_p_rows && !(o.top_p > 0.0 && o.top_p <= 1.0)) return bad(who, "top_p must be in (0, 1]");
+  if (!o.min_p_rows && !(o.min_p >= 0.0 && o.min_p <= 1.0)) return bad(who, "min_p must be in [0, 1]");
   if (rows == 0) return RG_OK;
   if (!logits || !u || !tokens || !logprobs || !kept_logprobs) return bad(who, "NULL argument");
-  const int64_t need = rg_sample_scratch(rows, vocab);
-  if (!scratch || scratch_bytes < need) return bad(who, "scratch is smaller than rg_sample_scratch()");
+  DrawArgs a = draw_args(rows, vocab, o);
+  if (!scratch || scratch_bytes < draw_scratch_bytes(a)) return bad(who, "scratch is smaller than rg_sample_scratch()");
   if (!aligned(scratch)) return bad(who, "scratch is not 16-byte aligned");
-  const DrawArgs a{logits, logits_row, dtype, rows, vocab, u, u_dtype == RG_DTYPE_F64, o.temperature, o.top_p, o.min_p, o.top_k,
-                   o.temperature_rows, o.top_k_rows, o.top_p_rows, o.min_p_rows, tokens, logprobs, kept_logprobs,
-                   (float*)scratch};
-  return launched(who, launch_draw(a, (hipStream_t)stream));
+  a.logits = logits;
+  a.row = logits_row;
+  a.dtype = dtype;
+  a.u = u;
+  a.u64 = u_dtype == RG_DTYPE_F64;
+  a.token = tokens;
+  a.logprob = logprobs;
+  a.kept = kept_logprobs;
+  return launched(who, launch_draw(a, scratch, (hipStream_t)stream));
 }
 
 }  // extern "C"

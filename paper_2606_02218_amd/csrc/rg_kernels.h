@@ -489,18 +489,30 @@ hipError_t launch_kv8_page_copy(const Kv8Pool& c, int n_layers, int64_t layer_bl
 
 // ---- sampling from given logits and uniform numbers (k_draw.hip)
 constexpr int DRAW_MAX_VOCAB = 1 << 20;
+// What the histogram finds of a row.
+struct DrawRow {
+  double total;             // sum of its weights
+  float zmax, t0;           // its maximum, and the least z that can be kept
+  int32_t good, listed;     // whether it has an answer; tokens in the bin of the border
+  int32_t bin;              // that bin (the number of bins: none)
+  unsigned long long above; // whole weights of the bins before it
+};
 struct DrawArgs {
   const void* logits;   // fp32 or bf16 by dtype, [rows][vocab], `row` elements apart
   int64_t row;
   int dtype, rows, vocab;
   const void* u;        // [rows] in [0, 1), doubles where u64
   int u64;
-  float temperature, top_p, min_p;
+  double temperature, top_p, min_p;
   int top_k;
   const float* temperature_rows; const int32_t* top_k_rows;   // [rows], in the place of the numbers above, or NULL
   const float* top_p_rows; const float* min_p_rows;
   int32_t* token; float* logprob; float* kept;                // [rows] each
-  float* seg;           // scratch: maximum and sum of every row's segments
+  // of the scratch: maximum and sum of every row's segments and, where rows go by
+  // histogram, what their segments keep, the bins, the lists and what is known of them
+  double* seg_s; float* seg_m;
+  unsigned long long* kept_seg; unsigned long long* bins; unsigned long long* list;
+  DrawRow* info;
 };
-int64_t draw_scratch_floats(int64_t rows, int vocab);
-hipError_t launch_draw(const DrawArgs& a, hipStream_t st);
+int64_t draw_scratch_bytes(const DrawArgs& a);
+hipError_t launch_draw(DrawArgs a, void* scratch, hipStream_t st);

@@ -77,7 +77,7 @@ def test_accept_refuses(change, error, match):
     (dict(u=torch.zeros(3).half()), TypeError, "u must have dtype"), (dict(u=torch.zeros(4)), ValueError, "u must have shape"),
     (dict(u=torch.zeros(6)[::2]), ValueError, "contiguous"), (dict(temperature=-0.1), ValueError, "temperature"),
     (dict(temperature=float("inf")), ValueError, "temperature"), (dict(temperature=float("nan")), ValueError, "temperature"),
-    (dict(top_k=-1), ValueError, "top_k"), (dict(top_k=2 ** 31), ValueError, "top_k"), (dict(top_p=0.0), ValueError, "top_p"),
+    (dict(top_k=-1), ValueError, "top_k"), (dict(top_k=2 ** 63), ValueError, "top_k"), (dict(top_p=0.0), ValueError, "top_p"),
     (dict(top_p=1.1), ValueError, "top_p"), (dict(min_p=-0.1), ValueError, "min_p"), (dict(min_p=1.5), ValueError, "min_p"),
     (dict(min_p=float("nan")), ValueError, "min_p"), (dict(temperature=torch.ones(4)), ValueError, "temperature"),
     (dict(top_k=torch.ones(3)), TypeError, "top_k"), (dict(top_p=torch.ones(3).double()), TypeError, "top_p"),
@@ -182,7 +182,7 @@ def test_library_refuses_samples():
     p = [C.c_void_p(1 << (20 + i)) for i in range(8)]
 
     def call(options=True, t=1.0, k=0, tp=1.0, mp=0.0, **c):
-        o = _draft.rg_sample_options(t, k, tp, mp, None, None, None, None)
+        o = _draft.rg_sample_options(t, tp, mp, k, None, None, None, None)
         f = dict(dtype=1, z=p[0], step=100, rows=3, vocab=100, ut=0, u=p[1], o=C.byref(o) if options else None, tok=p[2], lp=p[3],
                  kp=p[4], scratch=p[5], need=1 << 20, st=None)
         return lib.rg_sample(*{**f, **c}.values())
@@ -196,6 +196,9 @@ def test_library_refuses_samples():
             (dict(need=8), -1, b"scratch"), (dict(scratch=C.c_void_p(1 << 20 | 4)), -1, b"aligned")]:
         _refused(call(**c), code, text)
     assert call(rows=0, z=None) == 0
-    assert lib.rg_sample_scratch(0, 5) == 0 and lib.rg_sample_scratch(4, 1 << 20) > 0
+    plain, cut = _draft.rg_sample_options(1.0, 1.0, 0.0, 0), _draft.rg_sample_options(1.0, 0.9, 0.0, 0)
+    size = lambda rows, vocab, o=plain: lib.rg_sample_scratch(rows, vocab, C.byref(o))  # noqa: E731
+    assert size(0, 5) == 0 and 0 < size(4, 1 << 20) < size(4, 1 << 20, cut)
     for a in [(-1, 5), (1, 0), (1, (1 << 20) + 1)]:
-        assert lib.rg_sample_scratch(*a) == -1
+        assert size(*a) == -1
+    assert lib.rg_sample_scratch(1, 5, None) == -1

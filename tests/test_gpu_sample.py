@@ -146,6 +146,23 @@ def test_frequencies():
         assert np.all(np.abs(np.bincount(token, minlength=8) - n * p) <= 1.01)
 
 
+@pytest.mark.parametrize("s", [dict(), dict(top_k=50), dict(top_p=0.9), dict(top_k=50, top_p=0.9), dict(min_p=0.01)])
+def test_the_ends_of_u(s):
+    """u = 0 and the largest number below 1: the first and the last token that is kept and has a weight."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(9)
+    for vocab in (700, 40000):
+        z = logits(rng, 3, vocab, "masked", F32)
+        z[2] = logits(rng, 1, vocab, "peaked", F32)[0]
+        for u in (torch.zeros(3, device="cuda"), torch.full((3,), 1 - 2.0 ** -53, device="cuda", dtype=torch.float64)):
+            token = rg.sample(z, u, **s)[0].cpu().numpy()
+            for r in range(3):
+                o = Row(z[r].double().cpu().numpy(), **s, slack=1e-6)
+                first = [o.kept(n)[o.w[o.kept(n)] > 2.0 ** -40] for n in (o.low, o.high)]
+                # what weighs less than the sums' steps may or may not be passed
+                assert token[r] <= max(x[0] for x in first) if u[0] == 0 else token[r] >= min(x[-1] for x in first)
+
+
 @pytest.mark.parametrize("s", [dict(), dict(top_k=5), dict(top_p=0.9), dict(min_p=0.1), dict(temperature=0.0)])
 def test_rows_that_have_no_answer(s):
     """NaN and infinities, nothing but -inf, u outside [0, 1): token -1 and NaN; the rows beside them as ever."""
