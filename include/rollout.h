@@ -514,7 +514,7 @@ int rg_kv8_tree(const int32_t* parent, const int32_t* seq_off, const int32_t* se
 /* Bytes of scratch that rg_kv8_tree_attention needs for these sizes (0: none).
  * Negative (RG_E*) for bad sizes. */
 int64_t rg_kv8_tree_attention_scratch(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rows, int32_t n_seqs,
-                                      int32_t max_len);
+                                      int32_t words, int32_t max_len);
 
 /* Attention of the nodes over their sequences' contexts and the nodes that their
  * masks show them: rg_kv8_attention with j over those tokens, its arguments, limits,

@@ -22,7 +22,7 @@ _OPTIONS = struct.Struct("@3dq4P").pack
 _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 _ARGS = {
     "rg_kv8_tree": ([_P, _P, _P, _I, _I, _I, _P, _P, _P], C.c_int),
-    "rg_kv8_tree_attention_scratch": ([_I, _I, _I, _I, _I, _I, _I], _L),
+    "rg_kv8_tree_attention_scratch": ([_I] * 8, _L),
     "rg_kv8_tree_attention": ([_P, _P, _I, _P, _L, _L, _I, _P, _I, _P, C.c_float, _I, _P, _L, _P], C.c_int),
     "rg_kv8_accept": ([_P, _P, _P, _I, _P, _P, _P], C.c_int),
     "rg_sample_scratch": ([_I, _I, _P], _L),
@@ -137,7 +137,7 @@ def _attention_now(lib, cache, q, page_tab, seq_len, seq_off, mask, max_len, sca
         return None
     y = _dense(q, (rows, n_q, hd))
     code = 1 if dt is _BF16 else 0
-    need = lib.rg_kv8_tree_attention_scratch(code, n_q, n_kv, hd, rows, n_seqs, bound)
+    need = lib.rg_kv8_tree_attention_scratch(code, n_q, n_kv, hd, rows, n_seqs, words, bound)
     scratch, sp = None, 0
     if need > 0:
         scratch = q.new_empty(need // 4, dtype=_F32)
@@ -189,7 +189,7 @@ def kv8_tree_attention(cache, q, page_tab, seq_len, seq_off, mask, max_len: Opti
     with _On(dev):
         if out is None:
             out = _empty(q, (rows, n_q, hd), dt, stream)
-        need = lib.rg_kv8_tree_attention_scratch(code, n_q, c.n_kv, hd, rows, b.n_seqs, max_len)
+        need = lib.rg_kv8_tree_attention_scratch(code, n_q, c.n_kv, hd, rows, b.n_seqs, words, max_len)
         _check(min(need, 0))
         scratch = _empty(q, (need // 4,), _F32, stream) if need else None
         _check(lib.rg_kv8_tree_attention(C.byref(c), C.byref(b), code, q.data_ptr(), q.stride(0), q.stride(1), n_q,

@@ -54,14 +54,14 @@ __global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ par
 }
 
 // ---------------------------------------------------------------- attention
-// The tree's queries of one kv head, nodes x heads, are packed as columns, 16 CT of
-// them a workgroup.  Its waves take 32-token steps in turn straight from memory, 16
-// bytes a lane, convert the codes once for all their columns, and join in LDS.
+// The tree's queries of one kv head, nodes x heads, are packed as columns, 16 of them a
+// workgroup.  Its waves take 32-token steps in turn straight from memory, 16 bytes a
+// lane, and join in LDS.
 // Scores are formed transposed, S^T = K Q^T, so that a lane ends up with the
 // probabilities of one column for just those tokens whose V^T operand it loads.
 // Every node sees the context: only steps that reach into the tree are masked.
-enum { TREE_F32 = 0, TREE_BF16 = 1 };
 constexpr int tree_pieces(int size) { return size == 2 ? 1 : 3; }   // bf16 pieces of a query and of a probability
+constexpr int tree_waves(int size, int hd) { return size == 2 || hd == 64 ? 4 : 3; }   // of a SIMD, by the registers
 
 // The sequence whose column groups hold number x: sequence s has its groups of
 // 2^shift columns at (first row * rep >> shift) + s and on.  64 candidates a step.
@@ -83,23 +83,60 @@ __device__ __forceinline__ int find_group(const Kv8Rows& b, int x, int rep, int 
   return lo;
 }
 
-// 32 bits of a node's mask from bit b on; bits before 0, the context's, are set.
-__device__ __forceinline__ uint32_t mask_window(const uint64_t* m, int words, int b) {
-  if (b < 0) return b <= -32 ? ~0u : (uint32_t)(m[0] << -b) | ((1u << -b) - 1u);
-  const int w = b >> 6, o = b & 63;
-  uint64_t x = w < words ? m[w] >> o : 0;
-  if (o > 32 && w + 1 < words) x |= m[w + 1] << (64 - o);
-  return (uint32_t)x;
+// Four dims of column c: the waves' results joined, NaN values of the tokens that its
+// node does see put back (the steps cleared them), and stored, or kept for the join of
+// the chunks.
+template <typename T, int HD, int W>
+__device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W], const float (&sum)[W], const f32x4_t (&acc)[W],
+                                           int64_t c, int d, int rep, int kvh, int r0, int ctx0, int split, int c0, int c1,
+                                           bool fix, const int32_t* tab) {
+  const int node = (int)((uint64_t)c / (unsigned)rep), head = kvh * rep + (int)(c - (int64_t)node * rep);
+  float M = ml[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) M = fmaxf(M, ml[w]);
+  float L = 0.f;
+  f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < W; ++w) {                         // a wave without steps has weight 0
+    const float f = ml[w] == M ? 1.f : __builtin_amdgcn_exp2f(ml[w] - M);
+    L += f * sum[w];
+    o += f * acc[w];
+  }
+  if (fix && ctx0 + node >= 0) {
+    const uint64_t* mask = A.mask + (int64_t)(r0 + node) * A.words;
+    for (int t = max(max(ctx0, 0), c0); t < c1; ++t) {
+      if (!(mask_window(mask, A.words, t - ctx0) & 1)) continue;
+      const int b = kv8_block(A.c, tab, A.b.tab_stride, t >> 4, kvh);
+      if (b < 0) continue;                              // its scores are NaN
+      const uint8_t* v = A.c.v + (int64_t)b * (16 * HD) + (t >> 2 & 3) * (4 * HD) + d * 4 + (t & 3);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if ((v[4 * e] & 0x7F) == 0x7F) o[e] = __uint_as_float(0x7FC00000u);
+    }
+  }
+  if (A.plan.n_split == 1) {
+    const float inv = L == 0.f ? 0.f : 1.0f / L;        // 0: the row sees nothing
+    const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    st_elems<4, true>((T*)A.out + ((int64_t)(r0 + node) * A.n_q + head) * HD + d, v);
+  } else {
+    const int64_t slot = ((int64_t)(r0 + node) * A.plan.n_split + split) * A.n_q + head;
+    const float v[4] = {o[0], o[1], o[2], o[3]};
+    if (c0 < c1) st_elems<4, true>(A.part_o + slot * HD + d, v);
+    if (d == 0) {
+      A.part_ml[2 * slot] = M;
+      A.part_ml[2 * slot + 1] = L;
+    }
+  }
 }
 
-template <typename T, int HD, int CT, int W>
-__global__ __launch_bounds__(64 * W) void k_kv8_tree_attn(Kv8TreeAttn A, unsigned groups, unsigned items) {
+template <typename T, int HD, int W>
+__global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_attn(Kv8Attn A, unsigned groups, unsigned items) {
   constexpr int QP = tree_pieces(sizeof(T)), PP = QP;
   constexpr int NJ = HD / 64;       // 16-byte loads of a block per lane
-  constexpr int GC = 16 * CT, SHIFT = CT == 4 ? 6 : CT == 2 ? 5 : 4;
   constexpr int LDO = HD + 4;
   __shared__ __attribute__((aligned(16))) float sO[W][16][LDO];
-  __shared__ float sM[W][GC], sL[W][GC];
+  __shared__ float sM[W][16], sL[W][16];
+  __shared__ int sNan[W];
 
   // Blocks are dealt to the 8 XCDs in turn; runs of eight items, column groups that
   // read the same tokens, stay on one.
@@ -110,49 +147,21 @@ __global__ __launch_bounds__(64 * W) void k_kv8_tree_attn(Kv8TreeAttn A, unsigne
   const int kvh = (int)(item % (unsigned)A.c.n_kv), split = (int)(item / (unsigned)A.c.n_kv);
   const int rep = A.n_q / A.c.n_kv;
   int key, r0, n;
-  const int s = find_group(A.b, x, rep, SHIFT, key);
+  const int s = find_group(A.b, x, rep, 4, key);
   kv8_seq_rows(A.b, s, r0, n);
-  const int64_t col0 = (int64_t)(x - key) * GC;
+  const int64_t col0 = (int64_t)(x - key) * 16;
   if (x < key || col0 >= (int64_t)n * rep) return;
   const int len = kv8_len(A.b, s), ctx0 = len - n;      // node i is token ctx0 + i
-  const int ctx = max(ctx0, 0);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int cl = lane & 15, grp = lane >> 4;
-  // tokens that some node may see; no walk over what the table has not
-  const int total = (int)std::min<int64_t>(std::min<int64_t>(len, std::max<int64_t>(ctx, (int64_t)ctx0 + 64 * A.words)),
-                                           (int64_t)kv8_most(A.c, A.b) + 64 * A.words);
+  const int total = tree_tokens(A.c, A.b, len, n, A.words);   // those that some node may see
   const int64_t c0l = (int64_t)split * A.plan.chunk;
   const int c0 = (int)std::min<int64_t>(c0l, total);
   const int c1 = split == A.plan.n_split - 1 ? total : (int)std::min<int64_t>(total, c0l + A.plan.chunk);
   const int steps = (c1 - c0 + 31) / 32, last_blk = (max(c1, 1) - 1) >> 4;
   const int mine = (steps - wave + W - 1) / W;          // steps wave, wave + W, ...
-  const int whole = min(ctx, c1);                       // tokens that every node sees
+  const int whole = min(max(ctx0, 0), c1);              // tokens that every node sees
   const int32_t* tab = kv8_table(A.b, s);
-
-  const float sc = A.scale * KV8_LOG2E;
-  float m[CT], l[CT];
-  f32x4_t o[CT][NJ][4];
-  bf16x8_t qf[CT][2 * NJ][QP];
-  const uint64_t* mrow[CT];
-  bool node_ok[CT];
-  const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    m[ct] = -INFINITY;
-    l[ct] = 0.f;
-    const int64_t c = col0 + 16 * ct + cl;
-    const bool valid = c < (int64_t)n * rep;
-    const int node = valid ? (int)((uint64_t)c / (unsigned)rep) : 0, head = kvh * rep + (valid ? (int)(c - (int64_t)node * rep) : 0);
-    node_ok[ct] = valid && ctx0 + node >= 0;            // a padding row sees nothing
-    mrow[ct] = A.mask + (int64_t)(r0 + node) * A.words;
-    const T* qp = (const T*)A.q.p + (r0 + node) * A.q.row + head * A.q.head;
-#pragma unroll
-    for (int kk = 0; kk < 2 * NJ; ++kk) query8<T, QP>(qp + 64 * (kk >> 1) + 16 * grp + 8 * (kk & 1), node_ok[ct], vec, qf[ct][kk]);
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[ct][j][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
 
   const uint8_t* kl = A.c.k + lane * 16;
   const uint8_t* vl = A.c.v + grp * (4 * HD) + cl * 16;
@@ -182,61 +191,72 @@ __global__ __launch_bounds__(64 * W) void k_kv8_tree_attn(Kv8TreeAttn A, unsigne
       for (int j = 0; j < NJ; ++j) vr[h][j] = *reinterpret_cast<const u32x4_t*>(p + j * 256);
     }
   };
-  if (mine > 0) {
+  if (mine > 0) {                   // on their way beside the queries
     lists(0);
     fetch_k(0);
     fetch_v(0);
   }
+
+  const float sc = A.scale * KV8_LOG2E;
+  float m = -INFINITY, l = 0.f;
+  f32x4_t o[NJ][4];
+  bf16x8_t qf[2 * NJ][QP];
+  const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
+  const int64_t c = col0 + cl;
+  const bool valid = c < (int64_t)n * rep;
+  const int node = valid ? (int)((uint64_t)c / (unsigned)rep) : 0, head = kvh * rep + (valid ? (int)(c - (int64_t)node * rep) : 0);
+  const int row = valid && ctx0 + node >= 0 ? r0 + node : -1;   // -1: the column sees nothing, as padding, or is none
+  const T* qp = (const T*)A.q.p + max(row, 0) * A.q.row + head * A.q.head;
+#pragma unroll
+  for (int kk = 0; kk < 2 * NJ; ++kk) query8<T, QP>(qp + 64 * (kk >> 1) + 16 * grp + 8 * (kk & 1), row >= 0, vec, qf[kk]);
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[j][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  bool nan = false;                 // values of the tree's tokens that are NaN
+
   for (int i = 0; i < mine; ++i) {
     const int t0 = c0 + 32 * (wave + W * i);
-    float ks[2], vs[2];
+    float vs[2];
     int id[2];
+    f32x4_t st[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       id[h] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
-      ks[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kss), 2 * (i & 31) + h));
+      const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kss), 2 * (i & 31) + h));
       vs[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vss), 2 * (i & 31) + h));
-    }
-    f32x4_t st[CT][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
       // a lost page's tokens: NaN scores (the codes in the registers are another page's)
       const float none = id[h] < 0 ? __uint_as_float(0x7FC00000u) : 0.f;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) st[ct][h] = f32x4_t{none, none, none, none};
+      st[h] = f32x4_t{none, none, none, none};
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const bf16x8_t kf = kv8_bf16x8(kr[h][j][2 * e], kr[h][j][2 * e + 1], ks[h], ks[h]);
+          const bf16x8_t kf = kv8_bf16x8(kr[h][j][2 * e], kr[h][j][2 * e + 1], ks, ks);
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int n_ = 0; n_ < QP; ++n_)
-              st[ct][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ct][2 * j + e][n_], st[ct][h], 0, 0, 0);
+          for (int n_ = 0; n_ < QP; ++n_)
+            st[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[2 * j + e][n_], st[h], 0, 0, 0);
         }
     }
+    // the next step's keys into the registers just read: they arrive under the softmax
+    // and the values' products, and other waves' work
     if (i + 1 < mine) {
       if (((i + 1) & 31) == 0) lists(i + 1);
       fetch_k(i + 1);
     }
     // lane's tokens: 16 h + 4 grp + e of the step
     if (t0 + 32 > whole) {
-      uint32_t seen[CT];
       const uint32_t there = c1 - t0 < 32 ? (1u << (c1 - t0)) - 1u : ~0u;
+      uint32_t seen = 0;
+      if (row >= 0) seen = mask_window(A.mask + (int64_t)row * A.words, A.words, t0 - ctx0) & there;
+      seen >>= 4 * grp;
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        seen[ct] = node_ok[ct] ? mask_window(mrow[ct], A.words, t0 - ctx0) & there : 0u;
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!(seen[ct] >> (16 * h + 4 * grp + e) & 1)) st[ct][h][e] = -INFINITY;
-      }
-      // 0 * NaN is NaN: what some column does not see must hold none.  Stale slots and
-      // lost pages are cleared; NaN codes too, after a product has counted those that a
-      // column does see (ones at the NaN codes, ones at the tokens in sight).
-      bool nan = false;
+        for (int e = 0; e < 4; ++e)
+          if (!(seen >> (16 * h + e) & 1)) st[h][e] = -INFINITY;
+      // 0 * NaN is NaN: what some column does not see must hold none.  Stale slots and lost
+      // pages are cleared, and NaN codes, which the end looks after.
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int left = id[h] < 0 ? 0 : min(max(c1 - t0 - 16 * h - 4 * grp, 0), 4);
@@ -245,140 +265,81 @@ __global__ __launch_bounds__(64 * W) void k_kv8_tree_attn(Kv8TreeAttn A, unsigne
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            vr[h][j][e] &= keep;
-            nan |= has_nan_code(vr[h][j][e]);
+            const uint32_t w = vr[h][j][e] & keep;
+            nan |= has_nan_code(w);
+            vr[h][j][e] = clear_nan(w);
           }
       }
-      if (__any(nan)) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          uint32_t sw[4];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t four = seen[ct] >> (16 * h + 4 * grp);
-            sw[2 * h] = (four & 1u) * 0x3F80u | (four >> 1 & 1u) * 0x3F800000u;
-            sw[2 * h + 1] = (four >> 2 & 1u) * 0x3F80u | (four >> 3 & 1u) * 0x3F800000u;
-          }
-          const bf16x8_t sf = __builtin_bit_cast(bf16x8_t, u32x4_t{sw[0], sw[1], sw[2], sw[3]});
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t one[4];
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const uint32_t hit = (((vr[h][j][e] & KV8_NAN4) + 0x01010101u) & 0x80808080u) >> 7;
-                one[2 * h] = (hit & 1u) * 0x3F80u | (hit >> 8 & 1u) * 0x3F800000u;
-                one[2 * h + 1] = (hit >> 16 & 1u) * 0x3F80u | (hit >> 24) * 0x3F800000u;
-              }
-              const f32x4_t c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  __builtin_bit_cast(bf16x8_t, u32x4_t{one[0], one[1], one[2], one[3]}), sf, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                if (c[q] > 0.f) o[ct][j][e][q] = __uint_as_float(0x7FC00000u);
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vr[h][j][e] = clear_nan(vr[h][j][e]);
-      }
     }
-    bf16x8_t pf[CT][PP];
+    bf16x8_t pf[PP];
+    float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])),
+                     fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3]))) * sc;
+    if (__any(mx > m + KV8_SLACK)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = fmaxf(m, mx);
+      const float alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);   // -inf: nothing seen yet
+      l *= alpha;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      float mx = fmaxf(fmaxf(fmaxf(st[ct][0][0], st[ct][0][1]), fmaxf(st[ct][0][2], st[ct][0][3])),
-                       fmaxf(fmaxf(st[ct][1][0], st[ct][1][1]), fmaxf(st[ct][1][2], st[ct][1][3]))) * sc;
-      if (__any(mx > m[ct] + KV8_SLACK)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float mn = fmaxf(m[ct], mx);
-        const float alpha = m[ct] == mn ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);   // -inf: nothing seen yet
-        l[ct] *= alpha;
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[ct][j][e] *= alpha;
-        m[ct] = mn;
-      }
-      const float ms = m[ct] == -INFINITY ? 0.f : m[ct];   // nothing seen: every probability is exp2(-inf) = 0
-      float p[8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[4 * h + e] = __builtin_amdgcn_exp2f(fmaf(st[ct][h][e], sc, -ms));
-          l[ct] += p[4 * h + e];
-        }
-      operand8<PP>(p, pf[ct]);
+        for (int e = 0; e < 4; ++e) o[j][e] *= alpha;
+      m = mn;
     }
+    const float ms = m == -INFINITY ? 0.f : m;   // nothing seen: every probability is exp2(-inf) = 0
+    float p[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[4 * h + e] = __builtin_amdgcn_exp2f(fmaf(st[h][e], sc, -ms));
+        l += p[4 * h + e];
+      }
+    operand8<PP>(p, pf);
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bf16x8_t vf = kv8_bf16x8(vr[0][j][e], vr[1][j][e], vs[0], vs[1]);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int n_ = 0; n_ < PP; ++n_)
-            o[ct][j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[ct][n_], o[ct][j][e], 0, 0, 0);
+        for (int n_ = 0; n_ < PP; ++n_)
+          o[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n_], o[j][e], 0, 0, 0);
       }
     if (i + 1 < mine) fetch_v(i + 1);
   }
 
-  // Join the waves, 16 columns at a time: column cl, dims 64 j + 16 grp + 4 i + e of
+  // Join the waves: column cl, dims 64 j + 16 grp + 4 i + e of
   // the lane.  A wave without steps has weight 0.
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    l[ct] += __shfl_xor(l[ct], 16, 64);
-    l[ct] += __shfl_xor(l[ct], 32, 64);
-    if (grp == 0) {
-      sM[wave][16 * ct + cl] = m[ct];
-      sL[wave][16 * ct + cl] = l[ct];
-    }
+  const bool any_nan = __any(nan);
+  if (lane == 0) sNan[wave] = any_nan;
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (grp == 0) {
+    sM[wave][cl] = m;
+    sL[wave][cl] = l;
   }
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    if (ct) __syncthreads();
+  for (int j = 0; j < NJ; ++j)
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4_t*>(&sO[wave][cl][64 * j + 16 * grp + 4 * i]) =
+          f32x4_t{o[j][0][i], o[j][1][i], o[j][2][i], o[j][3][i]};
+  __syncthreads();
+  bool fix = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4_t*>(&sO[wave][cl][64 * j + 16 * grp + 4 * i]) =
-            f32x4_t{o[ct][j][0][i], o[ct][j][1][i], o[ct][j][2][i], o[ct][j][3][i]};
-    __syncthreads();
-    for (int i = tid; i < 16 * (HD / 4); i += 64 * W) {
-      const int h = i / (HD / 4), d = i % (HD / 4) * 4, g = 16 * ct + h;
-      const int64_t c = col0 + g;
-      if (c >= (int64_t)n * rep) break;
-      const int node = (int)((uint64_t)c / (unsigned)rep), head = kvh * rep + (int)(c - (int64_t)node * rep);
-      float M = sM[0][g];
+  for (int w = 0; w < W; ++w) fix |= sNan[w] != 0;
+  for (int i = tid; i < 16 * (HD / 4); i += 64 * W) {
+    const int h = i / (HD / 4), d = i % (HD / 4) * 4;
+    if (col0 + h >= (int64_t)n * rep) break;
+    float ml[W], sum[W];
+    f32x4_t acc[W];
 #pragma unroll
-      for (int w = 1; w < W; ++w) M = fmaxf(M, sM[w][g]);
-      float L = 0.f;
-      f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const float f = sM[w][g] == M ? 1.f : __builtin_amdgcn_exp2f(sM[w][g] - M);
-        L += f * sL[w][g];
-        acc += f * *reinterpret_cast<const f32x4_t*>(&sO[w][h][d]);
-      }
-      if (A.plan.n_split == 1) {
-        const float inv = L == 0.f ? 0.f : 1.0f / L;    // 0: the row sees nothing
-        const float v[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
-        st_elems<4, true>((T*)A.out + ((int64_t)(r0 + node) * A.n_q + head) * HD + d, v);
-      } else {
-        const int64_t slot = ((int64_t)(r0 + node) * A.plan.n_split + split) * A.n_q + head;
-        const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-        if (steps > 0) st_elems<4, true>(A.part_o + slot * HD + d, v);
-        if (d == 0) {
-          A.part_ml[2 * slot] = M;
-          A.part_ml[2 * slot + 1] = L;
-        }
-      }
+    for (int w = 0; w < W; ++w) {
+      ml[w] = sM[w][h];
+      sum[w] = sL[w][h];
+      acc[w] = *reinterpret_cast<const f32x4_t*>(&sO[w][h][d]);
     }
+    tree_store<T, HD, W>(A, ml, sum, acc, col0 + h, d, rep, kvh, r0, ctx0, split, c0, c1, fix, tab);
   }
 }
 
@@ -387,7 +348,7 @@ __global__ __launch_bounds__(64 * W) void k_kv8_tree_attn(Kv8TreeAttn A, unsigne
 constexpr int TREE_MAX_SPLIT = 64;
 
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_kv8_tree_merge(Kv8TreeAttn A) {
+__global__ __launch_bounds__(256) void k_kv8_tree_merge(Kv8Attn A) {
   constexpr int ND = HD / 64;
   const int lane = threadIdx.x & 63;
   const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -407,7 +368,7 @@ __global__ __launch_bounds__(256) void k_kv8_tree_merge(Kv8TreeAttn A) {
   float acc[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i) acc[i] = 0.f;
-  for (uint64_t some = __ballot(w != 0.f); some; some &= some - 1) {   // NaN weights too
+  for (uint64_t some = __ballot(l != 0.f); some; some &= some - 1) {   // NaN sums too
     const int c = __ffsll((unsigned long long)some) - 1;
     const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), c));
     const float* o = A.part_o + (slot0 + (int64_t)c * A.n_q) * HD + lane * ND;
@@ -591,22 +552,17 @@ __global__ __launch_bounds__(64 * ACCEPT_WAVES) void k_kv8_accept(AcceptArgs A) 
 }
 
 template <typename T, int HD>
-hipError_t run(const Kv8TreeAttn& a, hipStream_t st) {
-  const int rep = a.n_q / a.c.n_kv, gc = 16 * a.plan.ct;
-  const int64_t groups = (int64_t)a.b.rows * rep / gc + a.b.n_seqs, items = groups * a.c.n_kv * a.plan.n_split;
+hipError_t run(const Kv8Attn& a, hipStream_t st) {
+  const int rep = a.n_q / a.c.n_kv;
+  const int64_t groups = (int64_t)a.b.rows * rep / 16 + a.b.n_seqs, items = groups * a.c.n_kv * a.plan.n_split;
   if (items > INT32_MAX - 64) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((items + 63) / 64 * 64));
-#define RG_TREE(CT, W) return kv8_launch(k_kv8_tree_attn<T, HD, CT, W>, grid, dim3(64 * W), st, a, (unsigned)groups, (unsigned)items)
-  if constexpr (sizeof(T) == 2) {
-    if (a.plan.ct == 4) { RG_TREE(4, 4); }
-  }
-  if (a.plan.ct == 2) { RG_TREE(2, 4); }
-  RG_TREE(1, 4);
-#undef RG_TREE
+  if (a.plan.waves == 8) return kv8_launch(k_kv8_tree_attn<T, HD, 8>, grid, dim3(512), st, a, (unsigned)groups, (unsigned)items);
+  return kv8_launch(k_kv8_tree_attn<T, HD, 4>, grid, dim3(256), st, a, (unsigned)groups, (unsigned)items);
 }
 
 template <typename T, int HD>
-hipError_t merge(const Kv8TreeAttn& a, hipStream_t st) {
+hipError_t merge(const Kv8Attn& a, hipStream_t st) {
   const int64_t n = ((int64_t)a.b.rows * a.n_q + 3) / 4;
   if (n > INT32_MAX) return hipErrorInvalidValue;
   return kv8_launch(k_kv8_tree_merge<T, HD>, dim3((unsigned)n), dim3(256), st, a);
@@ -614,15 +570,25 @@ hipError_t merge(const Kv8TreeAttn& a, hipStream_t st) {
 
 }  // namespace
 
-// Columns of a workgroup by the mean of a sequence; chunks as far as two workgroups a
-// CU go, of 256 tokens at least.
-Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int max_len) {
+// Tiles where trees are wide and contexts long: 2 trees of 64 nodes, 28 heads, at 60 to
+// 131 thousand tokens 202 us, by 16 columns 246; 64 of 64 nodes, 12 heads, at 4000 tokens
+// 200 and 185.  Elsewhere 16 columns a workgroup: half the trees of 4 to 63 nodes at 512
+// to 4500 tokens 84 us, by tiles 103.  A context is cut only where that fills the chip,
+// since the chunks' partial results and the join's launch cost more than they even out
+// (84 us in one piece, 92 in two, 101 in four), and 8 waves share a workgroup's tokens
+// where one round holds them.
+Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int words, int max_len) {
   Kv8TreePlan p{};
   const int64_t rep = n_q / n_kv, cols = ((int64_t)rows * rep + n_seqs - 1) / n_seqs;
-  p.ct = cols <= 16 ? 1 : cols <= 32 || dtype == 0 ? 2 : 4;
-  const int64_t wgs = ((int64_t)rows * rep / (16 * p.ct) + n_seqs) * n_kv;
-  const int64_t n = std::max<int64_t>(1, std::min<int64_t>({512 / wgs, max_len / 256, TREE_MAX_SPLIT}));
-  p.chunk = (int)std::min<int64_t>((((int64_t)max_len + n - 1) / n + 31) / 32 * 32, 1 << 30);
+  p.tiles = dtype == 1 && cols >= 256 && max_len >= 8192 && words <= KV8_TREE_TILE_WORDS;
+  const int64_t wgs = p.tiles ? std::max<int64_t>((int64_t)rows / (128 / rep) + n_seqs / 2, 1) * n_kv
+                              : ((int64_t)rows * rep / 16 + n_seqs / 2 + 1) * n_kv;
+  p.waves = wgs <= 256 ? 8 : 4;
+  int64_t n = 1;
+  if (p.tiles) n = std::min<int64_t>(768 / wgs, max_len / 512);
+  else if (max_len >= 2048) n = std::min<int64_t>(256 / wgs, max_len / 640);
+  n = std::max<int64_t>(1, std::min<int64_t>(n, TREE_MAX_SPLIT));
+  p.chunk = (int)std::min<int64_t>((((int64_t)max_len + n - 1) / n + 63) / 64 * 64, 1 << 30);
   p.n_split = (int)((max_len + (int64_t)p.chunk - 1) / p.chunk);
   return p;
 }
@@ -632,14 +598,16 @@ hipError_t launch_kv8_tree(const int32_t* parent, const Kv8Rows& b, int words, u
   return kv8_launch(k_kv8_tree, dim3(b.n_seqs), dim3(64), st, parent, b, words, mask, pos);
 }
 
-hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& a, hipStream_t st) {
+hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& t, hipStream_t st) {
+  const Kv8Attn& a = t.a;
   if (a.b.rows <= 0 || a.b.n_seqs <= 0) return hipSuccess;
-  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.n_split > TREE_MAX_SPLIT || a.plan.chunk % 32 ||
+  if ((a.c.hd != 64 && a.c.hd != 128) || a.plan.n_split < 1 || a.plan.n_split > TREE_MAX_SPLIT || a.plan.chunk % 64 ||
       (a.plan.n_split > 1 && (!a.part_o || !a.part_ml)))
     return hipErrorInvalidValue;
   const bool w = a.c.hd == 128;
   hipError_t e;
-  if (dtype == 1) e = w ? run<bf16_t, 128>(a, st) : run<bf16_t, 64>(a, st);
+  if (t.plan.tiles) e = launch_kv8_tree_tiles(dtype, a, st);
+  else if (dtype == 1) e = w ? run<bf16_t, 128>(a, st) : run<bf16_t, 64>(a, st);
   else e = w ? run<float, 128>(a, st) : run<float, 64>(a, st);
   if (e != hipSuccess || a.plan.n_split == 1) return e;
   if (dtype == 1) return w ? merge<bf16_t, 128>(a, st) : merge<bf16_t, 64>(a, st);

@@ -233,19 +233,20 @@ int rg_kv8_tree(const int32_t* parent, const int32_t* seq_off, const int32_t* se
 }
 
 int64_t rg_kv8_tree_attention_scratch(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rows, int32_t n_seqs,
-                                      int32_t max_len) {
-  if ((dtype != RG_DTYPE_F32 && dtype != RG_DTYPE_BF16) || n_q < 1 || n_kv < 1 || n_q % n_kv || head_dim < 1 || rows < 0 ||
-      n_seqs < 0 || max_len < 1)
+                                      int32_t words, int32_t max_len) {
+  if ((dtype != RG_DTYPE_F32 && dtype != RG_DTYPE_BF16) || n_q < 1 || n_kv < 1 || n_q % n_kv || n_q / n_kv > 128 || head_dim < 1 || rows < 0 ||
+      n_seqs < 0 || max_len < 1 || words < 1 || words > RG_KV8_TREE_WORDS)
     return bad("rg_kv8_tree_attention_scratch", "bad sizes");
   if (rows == 0 || n_seqs == 0) return 0;
-  return 4 * kv8_tree_part_floats(rows, kv8_tree_plan(dtype, rows, n_seqs, n_q, n_kv, max_len), n_q, head_dim);
+  return 4 * kv8_tree_part_floats(rows, kv8_tree_plan(dtype, rows, n_seqs, n_q, n_kv, words, max_len), n_q, head_dim);
 }
 
 int rg_kv8_tree_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* q, int64_t q_row,
                           int64_t q_head, int32_t n_q, const uint64_t* mask, int32_t words, void* out, float scale,
                           int32_t max_len, void* scratch, int64_t scratch_bytes, void* stream) {
   const char* who = "rg_kv8_tree_attention";
-  Kv8TreeAttn a{};
+  Kv8TreeAttn t{};
+  Kv8Attn& a = t.a;
   int rc = cache_args(who, cache, batch, dtype, &a.c, &a.b);
   if (rc || (rc = tree_args(who, batch, words))) return rc;
   if (n_q < 1 || n_q % a.c.n_kv) return bad(who, "n_q must be a multiple of n_kv");
@@ -261,13 +262,16 @@ int rg_kv8_tree_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, 
   a.words = words;
   a.n_q = n_q;
   a.scale = scale;
-  a.plan = kv8_tree_plan(dtype, a.b.rows, a.b.n_seqs, n_q, a.c.n_kv, max_len);
-  const int64_t need = 4 * kv8_tree_part_floats(a.b.rows, a.plan, n_q, a.c.hd);
+  t.plan = kv8_tree_plan(dtype, a.b.rows, a.b.n_seqs, n_q, a.c.n_kv, words, max_len);
+  a.plan.waves = t.plan.waves;
+  a.plan.n_split = t.plan.n_split;
+  a.plan.chunk = t.plan.chunk;
+  const int64_t need = 4 * kv8_tree_part_floats(a.b.rows, t.plan, n_q, a.c.hd);
   if (need > 0 && (!scratch || scratch_bytes < need))
     return bad(who, "scratch is smaller than rg_kv8_tree_attention_scratch()");
   a.part_o = (float*)scratch;
   a.part_ml = a.part_o ? a.part_o + (int64_t)a.b.rows * a.plan.n_split * n_q * a.c.hd : nullptr;
-  return launched(who, launch_kv8_tree_attention(dtype, a, (hipStream_t)stream));
+  return launched(who, launch_kv8_tree_attention(dtype, t, (hipStream_t)stream));
 }
 
 int rg_kv8_accept(const rg_kv8_cache* cache, const rg_kv8_batch* batch, const uint64_t* mask, int32_t words,

@@ -441,6 +441,8 @@ struct Kv8Attn {
   Kv8Plan plan;
   float* part_o;    // n_split > 1: unnormalised outputs [rows][n_split][n_q][hd]
   float* part_ml;   // and their (max, sum) [rows][n_split][n_q][2]
+  const uint64_t* mask;   // launch_kv8_tree_tiles: what each row sees of its tree
+  int words;
 };
 inline int64_t kv8_part_floats(int64_t rows, const Kv8Plan& p, int n_q, int hd) {
   return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
@@ -451,28 +453,24 @@ hipError_t launch_kv8_merge(int dtype, bool planes, const Kv8Attn& a, hipStream_
 // Trees of drafted tokens (k_kv8_tree.hip): each row's mask of `words` 64-bit words,
 // a bit for each ancestor and itself, and its position.
 hipError_t launch_kv8_tree(const int32_t* parent, const Kv8Rows& b, int words, uint64_t* mask, int32_t* pos, hipStream_t st);
-// How a tree attention is cut: ct x 16 columns (nodes x heads of a kv head) a
-// workgroup, the context into n_split chunks of `chunk` tokens.
+// How a tree attention is cut: tiles (of 128 query rows, launch_kv8_tree_tiles), or 16
+// columns (nodes x heads of a kv head) a workgroup of 4 or 8 waves; the context into
+// n_split chunks of `chunk` tokens.
 struct Kv8TreePlan {
-  int ct, n_split, chunk;
+  bool tiles;
+  int waves, n_split, chunk;
 };
-Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int max_len);
+constexpr int KV8_TREE_TILE_WORDS = 8;   // most mask words of a tile, which keeps them in LDS
+Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int words, int max_len);
 struct Kv8TreeAttn {
-  Kv8Pool c;
-  Kv8Rows b;
-  HeadView q;
-  void* out;
-  const uint64_t* mask;
-  int words;
-  int n_q;
-  float scale;
+  Kv8Attn a;        // its plan's chunks as the tree's
   Kv8TreePlan plan;
-  float* part_o;    // n_split > 1: unnormalised outputs [rows][n_split][n_q][hd]
-  float* part_ml;   // and their (max, sum) [rows][n_split][n_q][2]
 };
 inline int64_t kv8_tree_part_floats(int64_t rows, const Kv8TreePlan& p, int n_q, int hd) {
   return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
 }
+// The tiles' pass over the cache; the tree's join has to follow where n_split > 1.
+hipError_t launch_kv8_tree_tiles(int dtype, const Kv8Attn& a, hipStream_t st);
 hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& a, hipStream_t st);
 // Moves the nodes of mask row last[s] behind the context; new_len: tokens then.
 hipError_t launch_kv8_accept(const Kv8Pool& c, const Kv8Rows& b, const uint64_t* mask, int words, const int32_t* last,

@@ -155,8 +155,9 @@ def test_library_refuses_attention():
         _refused(call(**c), code, text)
     assert call(batch=dict(rows=0)) == 0
     s = lib.rg_kv8_tree_attention_scratch
-    assert s(1, 12, 2, 128, 0, 0, 100) == 0 and s(1, 12, 2, 128, 30, 1, 100000) > 0
-    for a in [(3, 12, 2, 128, 4, 1, 9), (1, 12, 5, 128, 4, 1, 9), (1, 12, 2, 128, -1, 1, 9), (1, 12, 2, 128, 4, 1, 0), (1, 0, 1, 64, 1, 1, 1)]:
+    assert s(1, 12, 2, 128, 0, 0, 1, 100) == 0 and s(1, 12, 2, 128, 30, 1, 1, 100000) > 0
+    for a in [(3, 12, 2, 128, 4, 1, 1, 9), (1, 12, 5, 128, 4, 1, 1, 9), (1, 12, 2, 128, -1, 1, 1, 9), (1, 12, 2, 128, 4, 1, 1, 0),
+              (1, 0, 1, 64, 1, 1, 1, 1), (1, 12, 2, 128, 4, 1, 0, 9), (1, 12, 2, 128, 4, 1, 65, 9), (1, 129, 1, 64, 1, 1, 1, 9)]:
         assert s(*a) == -1
 
 
