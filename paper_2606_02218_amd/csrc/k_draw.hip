@@ -15,17 +15,17 @@
 // depend on any order, so atomics give the same draw on every run.
 //
 // Launches:
-// * scan, a wave a segment of 512 tokens: maximum, and sum of weights with respect to
-//   it.  It streams the logits once.
+// * scan, a wave four segments of 512 tokens: maximum, and sum of weights with respect to
+//   it; maxima of strips of 64.  It streams the logits once.
 // * only where top-p or min-p may cut a row without top-k: histogram and collect, some
-//   workgroups a row.  The first adds up weights by bins of z; the second finds the bin
-//   in which the border of top-p lies, sums what is kept above it by segments, and
-//   lists the tokens in it.
-// * pick, a workgroup a row: the border, then the segment, then the token.
+//   workgroups a row, each a part of it.  The first adds up weights by bins of z; the
+//   second finds the bin in which the border of top-p lies, sums what each part keeps
+//   above it, and lists the tokens in it.
+// * pick, a workgroup a row: the border, then where the running sum passes.
 // The last three look only at segments that can hold kept tokens:
 // * weights below 2^-43 of the largest count nothing;
-// * k segments with a maximum of t or more hold k tokens of t or more, so the border of
-//   top-k lies there or above;
+// * k segments, or strips, with a maximum of t or more hold k tokens of t or more, so the
+//   border of top-k lies there or above;
 // * what lies below t weighs no more than the segments whose maximum is below t and
 //   512 w(t) of each other, and where that is at most 1 - p of all, the border of
 //   top-p lies at t or above.
@@ -51,12 +51,19 @@ constexpr double LOG2E = 1.4426950408889634;
 constexpr double FIXED_ONE = 4398046511104.0;   // 2^42
 constexpr float FIXED_OCTAVES = 43.5f;          // weights below 2^-43 are 0 in whole numbers
 
+// Octaves of weight per logit; temperature 0 reports at 1.
+__device__ __forceinline__ double octaves_per_logit(const DrawArgs& A, int r) {
+  if (!A.temperature_rows) return A.c;
+  const float t = A.temperature_rows[r];
+  return t == 0.f ? LOG2E : LOG2E / (double)t;
+}
+
 // Settings of a row.
 struct RowOpts {
   double temperature, top_p, min_p;
   int top_k;
   bool by_k, by_p, by_min;
-  double c;                           // octaves of weight per logit; T = 0 reports at 1
+  double c;
 };
 __device__ __forceinline__ RowOpts row_opts(const DrawArgs& A, int r) {
   RowOpts o;
@@ -67,7 +74,7 @@ __device__ __forceinline__ RowOpts row_opts(const DrawArgs& A, int r) {
   o.by_k = o.top_k > 0 && o.top_k < A.vocab;
   o.by_p = o.top_p < 1.0;
   o.by_min = o.min_p > 0.0;
-  o.c = o.temperature == 0.0 ? LOG2E : LOG2E / o.temperature;
+  o.c = octaves_per_logit(A, r);
   return o;
 }
 __device__ __forceinline__ bool usable(const RowOpts& o) {
@@ -88,8 +95,9 @@ __device__ __forceinline__ double exp2_64(double t) {
   p = fma(p, f, 0.2402265069581299);
   p = fma(p, f, 0.6931471805459335);
   p = fma(p, f, 1.0);
-  const u64 b = __builtin_bit_cast(u64, p);
-  return __builtin_bit_cast(double, b + ((u64)(uint32_t)__builtin_bit_cast(u64, s) << 52));
+  const u64 b = __builtin_bit_cast(u64, p);                   // n into the exponent: of the high word alone
+  const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)__builtin_bit_cast(u64, s) << 20);
+  return __builtin_bit_cast(double, (u64)hi << 32 | (uint32_t)b);
 }
 // The weight of z with respect to top (finite, no less): octaves below 1000 count nothing.
 __device__ __forceinline__ double weight_of(float z, float top, double c) {
@@ -120,17 +128,22 @@ __device__ __forceinline__ double sum_to_63(double v) {
   v += moved<0x143, 0xc>(v);
   return v;
 }
+template <int CTRL>
+__device__ __forceinline__ float max_moved(float v) {
+  return max_nan(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, 0xf, 0xf, false)));
+}
 __device__ __forceinline__ float max_nan_wave(float v) {
-#define RG_MAX(ctrl) \
-  v = max_nan(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), ctrl, 0xf, 0xf, false)))
-  RG_MAX(0x111);
-  RG_MAX(0x112);
-  RG_MAX(0x114);
-  RG_MAX(0x118);
-  RG_MAX(0x142);
-  RG_MAX(0x143);
-#undef RG_MAX
+  v = max_moved<0x111>(v);
+  v = max_moved<0x112>(v);
+  v = max_moved<0x114>(v);
+  v = max_moved<0x118>(v);
+  v = max_moved<0x142>(v);
+  v = max_moved<0x143>(v);
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ float sum_wave(float v) {
+  double d = sum_to_63((double)v);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int((float)d), 63));
 }
 
 template <typename T, bool VEC>
@@ -144,33 +157,68 @@ __device__ __forceinline__ void load8(const T* p, int i, int n, float (&v)[8]) {
 }
 
 // ---------------------------------------------------------------- scan
-template <typename T, bool VEC>
-__global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int segs, int64_t items) {
+// Four segments a wave: their loads are on their way together, and the lane moves of one
+// fill the waits of another.
+template <typename T, bool VEC, bool CUT>
+__global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int segs, unsigned per_row, unsigned items) {
+  constexpr int U = 4;
   const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * SCAN_WAVES + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const unsigned item = blockIdx.x * SCAN_WAVES + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (item >= items) return;
-  const int r = (int)(item / segs), seg = (int)(item - (int64_t)r * segs);
-  const double temperature = A.temperature_rows ? (double)A.temperature_rows[r] : A.temperature;
-  const double c = temperature == 0.0 ? LOG2E : LOG2E / temperature;
-  float v[8];
-  load8<T, VEC>((const T*)A.logits + r * A.row, seg * SEG + 8 * lane, A.vocab, v);
-  float m = v[0];
+  const unsigned r = item / per_row;
+  const int s0 = (int)(item - r * per_row) * U;
+  const T* z = (const T*)A.logits + r * A.row;
+  float v[U][8], m[U];
 #pragma unroll
-  for (int e = 1; e < 8; ++e) m = max_nan(m, v[e]);
-  m = max_nan_wave(m);
-  double s = 0.0;
-  if (m > -INFINITY && m < INFINITY) {            // else the sum is not looked at, or nothing
+  for (int j = 0; j < U; ++j) load8<T, VEC>(z, (s0 + j) * SEG + 8 * lane, A.vocab, v[j]);
+  const double c = octaves_per_logit(A, r);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += weight_of(v[e], m, c);   // the maximum's is 1 exactly
-    s = sum_to_63(s);
+  for (int j = 0; j < U; ++j) {
+    m[j] = v[j][0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) m[j] = max_nan(m[j], v[j][e]);
   }
-  if (lane == 63) {
-    A.seg_m[item] = m;
-    A.seg_s[item] = s;
+  auto steps = [&](auto ctrl) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) m[j] = max_moved<decltype(ctrl)::value>(m[j]);
+  };
+  steps(std::integral_constant<int, 0x111>{});
+  steps(std::integral_constant<int, 0x112>{});
+  steps(std::integral_constant<int, 0x114>{});
+  if constexpr (CUT) {                            // lanes 7, 15, ..: of eight lanes
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if ((lane & 7) == 7 && s0 + j < segs) A.strip_m[((int64_t)r * segs + s0 + j) * 8 + (lane >> 3)] = m[j];
   }
-  if (A.bins) {                                   // the histogram begins empty
-    const int per = (BINS + segs - 1) / segs;
-    for (int i = seg * per + lane; i < min(seg * per + per, BINS); i += 64) A.bins[(int64_t)r * BINS + i] = 0;
+  steps(std::integral_constant<int, 0x118>{});
+  steps(std::integral_constant<int, 0x142>{});
+  steps(std::integral_constant<int, 0x143>{});
+  double s[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    m[j] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m[j]), 63));
+    s[j] = 0.0;
+    if (!(m[j] > -INFINITY && m[j] < INFINITY)) continue;   // the sum is not looked at, or nothing
+    const double mc = (double)m[j] * c;
+    if (fabs(mc) < 1024.0) {                      // z c - m c to 2^-44
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[j] += exp2_64(fmax(fma((double)v[j][e], c, -mc), -1000.0));
+    } else {
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) s[j] += weight_of(v[j][e], m[j], c);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) s[j] = sum_to_63(s[j]);
+#pragma unroll
+  for (int j = 0; j < U; ++j)
+    if (lane == 63 && s0 + j < segs) {
+      A.seg_m[(int64_t)r * segs + s0 + j] = m[j];
+      A.seg_s[(int64_t)r * segs + s0 + j] = s[j];
+    }
+  if (CUT && A.bins) {                            // the histogram begins empty
+    const int per = (BINS + (int)per_row - 1) / (int)per_row, b0 = s0 / U * per;
+    for (int i = b0 + lane; i < min(b0 + per, BINS); i += 64) A.bins[(int64_t)r * BINS + i] = 0;
   }
 }
 
@@ -222,17 +270,20 @@ __device__ __forceinline__ int group_min(int v, int* red) {
   return v;
 }
 
+// Bin of z, 16 an octave of weight: falls as z grows.
+__device__ __forceinline__ int bin_of(float z, float zmax, float c) {
+  return (int)fminf(((zmax - z) * c) * 16.f, (float)(BINS - 1));
+}
+__device__ __forceinline__ float bin_factor(double c) { return (float)fmin(c, 3.0e38); }
+
 // What the threads of a row share.
 struct RowMemory {
   float m[MAX_SEGS];                  // maxima of the segments
   float share[MAX_SEGS];              // their sums with respect to the row's maximum
-  uint16_t active[MAX_SEGS];          // segments that can hold kept tokens
   double redd[8];
   u64 red[8];
   float redf[8];
   int redi[8];
-  int passes[8];
-  int n_active;
 };
 
 template <typename T, bool VEC, int N>
@@ -244,15 +295,18 @@ struct Row {
   RowMemory* S;
 
   // The row's segments; false where it has no answer.
-  __device__ bool read(const DrawArgs& A, int r, int n_segs, const RowOpts& o) {
+  __device__ __forceinline__ bool read(const DrawArgs& A, int r, int n_segs, const RowOpts& o) {
     const int tid = threadIdx.x;
     z = (const T*)A.logits + r * A.row;
     vocab = A.vocab;
     segs = n_segs;
     c = o.c;
+    double s0 = 0.0;                  // the first round's sums come beside its maxima
     float m = -INFINITY;
+#pragma unroll 1
     for (int i = tid; i < segs; i += N) {
       const float x = A.seg_m[(int64_t)r * segs + i];
+      if (i == tid) s0 = A.seg_s[(int64_t)r * segs + i];
       S->m[i] = x;
       m = max_nan(m, x);
     }
@@ -265,8 +319,9 @@ struct Row {
     zmax = m;
     if (!(zmax > -INFINITY && zmax < INFINITY) || !usable(o)) return false;   // NaN too
     double part = 0.0;
+#pragma unroll 1
     for (int i = tid; i < segs; i += N) {
-      const double w = share_of(A, r, i);
+      const double w = share_of(i, i == tid ? s0 : A.seg_s[(int64_t)r * segs + i]);
       S->share[i] = (float)w;
       part += w;
     }
@@ -278,79 +333,71 @@ struct Row {
     for (int i = 0; i < N / 64; ++i) total += S->redd[i];
     return true;
   }
-  __device__ double share_of(const DrawArgs& A, int r, int i) const {
+  __device__ __forceinline__ double share_of(int i, double s) const {
     const float m = S->m[i];
-    return m == -INFINITY ? 0.0 : A.seg_s[(int64_t)r * segs + i] * weight_of(m, zmax, c);
+    return m == -INFINITY ? 0.0 : s * weight_of(m, zmax, c);
   }
-  __device__ u64 fixed(float x) const { return x == -INFINITY ? 0 : fixed_of(weight_of(x, zmax, c)); }
-  __device__ float octaves(float x) const { return (float)(((double)zmax - (double)x) * c); }
+  __device__ __forceinline__ u64 fixed(float x) const { return x == -INFINITY ? 0 : fixed_of(weight_of(x, zmax, c)); }
 
-  // The least z that can be kept (see above), of min-p's z where given: thresholds side
-  // by side, a wave each.
-  __device__ float least(bool by_k, int k, bool by_p, double p, float min_z) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr int W = N / 64;
+  // The least z that can be kept (see above).  Every wave halves the octaves that are left
+  // by itself, with what the lanes have of the segments, or of the strips where given.
+  __device__ __forceinline__ float least(const float* strips, int k, bool by_p, double p) const {
+    const int lane = threadIdx.x & 63;
     float lo = 0.f, hi = FIXED_OCTAVES;
-    if (by_k || by_p) {
-      const float spare = (float)((1.0 - fmax(p, 0.0)) * total * (1.0 - 1e-5));
-      for (int round = 0; round < (W == 8 ? 3 : 4); ++round) {
-        const float step = (hi - lo) / (W + 1), y = lo + step * (wave + 1);
-        const float cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
-        float below = 0.f;
-        int n = 0;
-        for (int i = lane; i < segs; i += 64) {
-          const bool above = octaves(S->m[i]) <= y;
-          n += above;
-          below += above ? fminf(S->share[i], cap) : S->share[i];
+    if (k > 0 || by_p) {
+      const float* const top = strips ? strips : S->m;
+      const int n = strips ? 8 * segs : segs;
+      const float spare = (float)((1.0 - fmax(p, 0.0)) * total * (1.0 - 1e-5)), cf = bin_factor(c);
+      if (by_p || k <= n) {
+#pragma unroll 1
+        for (int round = 0; round < 8; ++round) {
+          const float y = 0.5f * (lo + hi), cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
+          float below = 0.f;
+          int count = 0;
+#pragma unroll 4
+          for (int i = lane; i < n; i += 64) {
+            const bool above = (zmax - top[i]) * cf <= y;
+            count += above;
+            if (by_p) below += above ? fminf(S->share[i], cap) : S->share[i];
+          }
+          const bool pass = by_p ? sum_wave(below) <= spare : wave_sum_dpp(count) >= k;
+          if (pass) hi = y;
+          else lo = y;
         }
-        const bool pass = by_k ? wave_sum_dpp(n) >= k : wave_sum(below) <= spare;
-        __syncthreads();
-        if (lane == 0) S->passes[wave] = pass;
-        __syncthreads();
-        int first = W;
-        for (int i = W - 1; i >= 0; --i)
-          if (S->passes[i]) first = i;
-        hi = first == W ? hi : lo + step * (first + 1);
-        lo = lo + step * first;
       }
     }
-    const float t = (float)((double)zmax - ((double)hi + 1e-3) / c);
-    return fmaxf(t <= -3.4e38f ? -INFINITY : of_key(key_of(t) - 2), min_z);   // what was rounded on the way
+    const float t = (float)((double)zmax - ((double)hi + 2e-3) / c);
+    return t <= -3.4e38f ? -INFINITY : of_key(key_of(t) - 2);   // 2e-3 and two steps: what was rounded on the way
   }
-  // Lists the segments that can hold a token of t0 or more.
-  __device__ void activate(float t0) {
-    __syncthreads();
-    if (threadIdx.x == 0) S->n_active = 0;
-    __syncthreads();
-    for (int base = 0; base < segs; base += N) {
-      const int i = base + (int)threadIdx.x;
-      const bool on = i < segs && S->m[i] >= t0;
-      const uint64_t mask = __ballot(on);
-      int at = 0;
-      if ((threadIdx.x & 63) == 0 && mask) at = atomicAdd(&S->n_active, __popcll(mask));
-      at = __builtin_amdgcn_readfirstlane(at);
-      if (on) S->active[at + __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1))] = (uint16_t)i;
-    }
-    __syncthreads();
-  }
-  // f(z, id, whether it is a token of t0 or more) for the tokens of active segments; whole
-  // waves call it.  Four segments are on their way at once.
+  // f(z, id) for every token of t0 or more, of segments s0 .. s1 - 1; whole waves call it.
+  // The next segment is on its way while one is looked at.
   template <typename F>
-  __device__ void from_memory(float t0, F f) const {
-    constexpr int W = N / 64, U = 4;
-    const int lane = threadIdx.x & 63, n = S->n_active;
-    for (int a = (int)threadIdx.x >> 6; a < n; a += W * U) {
-      float v[U][8];
-      int first[U];
+  __device__ __forceinline__ void tokens(float t0, int s0, int s1, F f) const {
+    const int lane = threadIdx.x & 63;
+    auto next = [&](int s) {
+      while (s < s1 && S->m[s] < t0) s += N / 64;
+      return __builtin_amdgcn_readfirstlane(s);
+    };
+    int s = next(s0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
+    float v[8];
+    if (s < s1) load8<T, VEC>(z, s * SEG + 8 * lane, vocab, v);
+#pragma unroll 1
+    while (s < s1) {
+      const int after = next(s + N / 64);
+      float w[8];
+      if (after < s1) load8<T, VEC>(z, after * SEG + 8 * lane, vocab, w);
+      float m = v[0];
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        first[j] = a + j * W < n ? (int)S->active[a + j * W] * SEG + 8 * lane : vocab;
-        load8<T, VEC>(z, first[j], vocab, v[j]);
+      for (int e = 1; e < 8; ++e) m = fmaxf(m, v[e]);
+      if (m >= t0 && m > -INFINITY) {
+        const int i = s * SEG + 8 * lane;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (v[e] >= t0 && v[e] > -INFINITY) f(v[e], i + e);   // tokens past the vocabulary are -inf
       }
+      s = after;
 #pragma unroll
-      for (int j = 0; j < U; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f(v[j][e], first[j] + e, first[j] + e < vocab && v[j][e] >= t0);
+      for (int e = 0; e < 8; ++e) v[e] = w[e];
     }
   }
 };
@@ -365,25 +412,12 @@ __device__ __forceinline__ float min_p_border(const RowOpts& o, float zmax) {
 // Which rows go by histogram: top-k's are few and the pick finds them alone.
 __device__ __forceinline__ bool by_bins(const RowOpts& o) { return o.temperature != 0.0 && !o.by_k && (o.by_p || o.by_min); }
 
-// Bin of z, 16 an octave of weight: falls as z grows.
-__device__ __forceinline__ int bin_of(float z, float zmax, float c) {
-  return (int)fminf(((zmax - z) * c) * 16.f, (float)(BINS - 1));
-}
-__device__ __forceinline__ float bin_factor(double c) { return (float)fmin(c, 3.0e38); }
 __device__ __forceinline__ double mass_limit(const RowOpts& o, double all) { return fmax(o.top_p * all, 0.5); }
 
-// Adds a token to a list where `on`; whole waves call it.
-__device__ __forceinline__ void append(bool on, u64 place, int* count, u64* list) {
-  const uint64_t mask = __ballot(on);
-  if (!mask) return;
-  const int lane = threadIdx.x & 63;
-  int at = 0;
-  if (lane == 0) at = atomicAdd(count, __popcll(mask));
-  at = __builtin_amdgcn_readfirstlane(at) + __popcll(mask & ((1ull << lane) - 1));
-  if (on && at < LIST) list[at] = place;
-}
-
 // ---------------------------------------------------------------- histogram, collect
+// Part p of a row's segments: a run of them.
+__device__ __forceinline__ int part_start(int p, int segs, int parts) { return (int)((int64_t)p * segs / parts); }
+
 template <typename T, bool VEC>
 __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int parts) {
   __shared__ RowMemory S;
@@ -391,45 +425,45 @@ __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int pa
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
   if (!by_bins(o)) return;
+  for (int i = tid; i < BINS; i += PART) mass[i] = 0;
   Row<T, VEC, PART> row{};
   row.S = &S;
   const bool good = row.read(A, r, segs, o);
   float t0 = 0.f;
-  if (good) t0 = row.least(false, 0, o.by_p, o.top_p, o.by_min ? min_p_border(o, row.zmax) : -INFINITY);
-  if (part == 0 && tid == 0) A.info[r] = DrawRow{row.total, row.zmax, t0, good, 0, BINS, 0};
-  if (!good || !o.by_p) return;
-  for (int i = tid; i < BINS; i += PART) mass[i] = 0;
-  __syncthreads();
-  const float c = bin_factor(o.c);
-  const int lane = tid & 63;
-  for (int s = part + parts * (tid >> 6); s < segs; s += parts * (PART / 64)) {
-    if (S.m[s] < t0) continue;
-    float v[8];
-    load8<T, VEC>(row.z, s * SEG + 8 * lane, A.vocab, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (v[e] >= t0 && v[e] > -INFINITY) atomicAdd(&mass[bin_of(v[e], row.zmax, c)], row.fixed(v[e]));
+  if (good) {
+    t0 = row.least(nullptr, 0, o.by_p, o.top_p);
+    if (o.by_min) t0 = fmaxf(t0, min_p_border(o, row.zmax));
   }
+  if (part == 0 && tid == 0) A.info[r] = DrawRow{row.total, row.zmax, t0, good, 0, BINS, 0};
+  if (!good) return;
+  const float c = bin_factor(o.c);
+  row.tokens(t0, part_start(part, segs, parts), part_start(part + 1, segs, parts),
+             [&](float x, int) { atomicAdd(&mass[bin_of(x, row.zmax, c)], row.fixed(x)); });
   __syncthreads();
-  for (int i = tid; i < BINS; i += PART)
-    if (mass[i]) atomicAdd(&A.bins[(int64_t)r * BINS + i], mass[i]);
+  u64* bins = A.part_bins + (int64_t)blockIdx.x * BINS;
+  for (int i = tid; i < BINS; i += PART) {
+    const u64 m = mass[i];
+    bins[i] = m;
+    if (m) atomicAdd(&A.bins[(int64_t)r * BINS + i], m);
+  }
 }
 
 template <typename T, bool VEC>
 __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int parts) {
-  __shared__ u64 red[8];
-  __shared__ int redi[8];
+  __shared__ u64 red[8], list[LIST];
+  __shared__ int redi[8], n_list, at;
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
   if (!by_bins(o)) return;
   const DrawRow info = A.info[r];
   if (!info.good) return;
+  if (tid == 0) n_list = 0;
+  constexpr int PER = BINS / PART;
+  u64 mine[PER], all;
   int border = BINS;                  // the bin in which top-p's border lies
-  u64 above = 0;                      // weight of the bins before it
   if (o.by_p) {
     const double limit = mass_limit(o, info.total * FIXED_ONE);
-    constexpr int PER = BINS / PART;
-    u64 mine[PER], sum = 0, all;
+    u64 sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       mine[i] = A.bins[(int64_t)r * BINS + tid * PER + i];
@@ -447,35 +481,44 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
       end -= mine[i];
     }
     border = group_min<PART>(hit, redi);
-    if (hit == border && border < BINS) red[0] = before;
-    __syncthreads();
-    above = border < BINS ? red[0] : 0;
+    if (part == 0 && hit == border && border < BINS) {
+      A.info[r].bin = border;
+      A.info[r].above = before;
+    }
   }
-  if (part == 0 && tid == 0) {
-    A.info[r].bin = border;
-    A.info[r].above = above;
+  // what the part keeps above it
+  u64 kept = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = tid * PER + i;
+    if (b < border) kept += A.part_bins[(int64_t)blockIdx.x * BINS + b];
   }
+  group_prefix<PART>(kept, red, &all);
+  if (tid == 0) A.part_kept[blockIdx.x] = all;
+  if (border == BINS) return;
+  // the tokens in it
   const T* z = (const T*)A.logits + r * A.row;
   const float c = bin_factor(o.c);
-  const int lane = tid & 63;
-  for (int s = part + parts * (tid >> 6); s < segs; s += parts * (PART / 64)) {
-    u64 kept = 0;
-    if (A.seg_m[(int64_t)r * segs + s] >= info.t0) {
-      float v[8];
-      const int i = s * SEG + 8 * lane;
-      load8<T, VEC>(z, i, A.vocab, v);
+  const int lane = tid & 63, s1 = part_start(part + 1, segs, parts);
+#pragma unroll 2
+  for (int s = part_start(part, segs, parts) + (tid >> 6); s < s1; s += PART / 64) {
+    if (A.seg_m[(int64_t)r * segs + s] < info.t0) continue;
+    float v[8];
+    const int i = s * SEG + 8 * lane;
+    load8<T, VEC>(z, i, A.vocab, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool on = v[e] >= info.t0 && v[e] > -INFINITY;
-        const int b = on ? bin_of(v[e], info.zmax, c) : BINS;
-        if (b < border) kept += fixed_of(weight_of(v[e], info.zmax, o.c));
-        append(b == border && on, place_of(v[e], i + e), &A.info[r].listed, A.list + (int64_t)r * LIST);
+    for (int e = 0; e < 8; ++e)
+      if (v[e] >= info.t0 && v[e] > -INFINITY && bin_of(v[e], info.zmax, c) == border) {
+        const int k = atomicAdd(&n_list, 1);
+        if (k < LIST) list[k] = place_of(v[e], i + e);
       }
-#pragma unroll
-      for (int x = 32; x > 0; x >>= 1) kept += __shfl_xor(kept, x, 64);
-    }
-    if (lane == 0) A.kept_seg[(int64_t)r * segs + s] = kept;
   }
+  __syncthreads();
+  const int n = n_list;
+  if (tid == 0) at = atomicAdd(&A.info[r].listed, n);
+  __syncthreads();
+  for (int i = tid; i < min(n, LIST); i += PART)
+    if (at + i < LIST) A.list[(int64_t)r * LIST + at + i] = list[i];
 }
 
 // ---------------------------------------------------------------- pick
@@ -490,21 +533,32 @@ struct CutMemory {
   int n_list, n_few;
 };
 
+// Of n tokens in C.few, a thread each: how many come before one in the order, and what they weigh.
+__device__ __forceinline__ void compare_few(const CutMemory& C, int n, u64 p, u64& rank, u64& before) {
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) {
+    const bool in_front = C.few[j] > p;
+    rank += in_front;
+    before += in_front ? C.weight[j] : 0;
+  }
+}
+
 // The border of top-k (by rank: fewer than `limit` tokens come before) or top-p (less
-// than `limit` of weight does) among the tokens that `each` gives, mass0 of weight in
-// front of them, none outside the places lo .. hi: the place of the last that is kept, 0
-// if all of them are; mass: the weight up to it.  Windows of places, ever finer by 1024,
-// until what is left is few enough to compare with one another.
+// than `limit` of weight does) among the tokens that `each` gives, n of them, mass0 of
+// weight in front of them, none outside the places lo .. hi: the place of the last that is
+// kept, 0 if all of them are; mass: the weight up to it.  Windows of places, ever finer by
+// 1024, until what is left is few enough to compare with one another.
 template <typename R, typename Each>
-__device__ u64 find_border(const R& row, CutMemory& C, const Each& each, bool by_rank, double limit, u64 lo, u64 hi,
-                           u64 mass0, u64* mass) {
+__device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Each& each, int n, bool by_rank, double limit, u64 lo,
+                                           u64 hi, u64 mass0, u64* mass) {
   const int tid = threadIdx.x;
   u64 rank0 = 0;                      // before the window
+  int inside = n;
   auto reaches = [&](u64 rank, u64 weight) { return by_rank ? (double)rank >= limit : (double)weight >= limit; };
-  for (;;) {
+#pragma unroll 1
+  while (inside > FEW) {              // places differ: at the latest a window of one has one token
     __syncthreads();
     for (int i = tid; i < BINS; i += PICK) { C.bin.mass[i] = 0; C.bin.count[i] = 0; }
-    if (tid == 0) C.n_few = 0;
     __syncthreads();
     const int shift = max(54 - __clzll((long long)(hi - lo | 1)), 0);   // (hi - lo) >> shift is below 1024
     each([&](float x, int id) {
@@ -520,10 +574,10 @@ __device__ u64 find_border(const R& row, CutMemory& C, const Each& each, bool by
     const uint32_t n0 = C.bin.count[2 * tid], n1 = C.bin.count[2 * tid + 1];
     u64 all_m, all_n;
     const u64 m = group_prefix<PICK>(m0 + m1, row.S->red, &all_m) + mass0;
-    const u64 n = group_prefix<PICK>((u64)(n0 + n1), row.S->red, &all_n) + rank0;
+    const u64 rank = group_prefix<PICK>((u64)(n0 + n1), row.S->red, &all_n) + rank0;
     int hit = INT32_MAX;
-    if (n1 && reaches(n, m)) hit = 2 * tid + 1;
-    if (n0 && reaches(n - n1, m - m1)) hit = 2 * tid;
+    if (n1 && reaches(rank, m)) hit = 2 * tid + 1;
+    if (n0 && reaches(rank - n1, m - m1)) hit = 2 * tid;
     const int d = group_min<PICK>(hit, row.S->redi);
     if (d == INT32_MAX) {             // the limit lies behind the last token
       *mass = mass0 + all_m;
@@ -531,45 +585,46 @@ __device__ u64 find_border(const R& row, CutMemory& C, const Each& each, bool by
     }
     if (hit == d) {
       C.mass = hit & 1 ? m - m1 : m - m1 - m0;
-      C.rank = hit & 1 ? n - n1 : n - n1 - n0;
+      C.rank = hit & 1 ? rank - n1 : rank - n1 - n0;
     }
     __syncthreads();
     mass0 = C.mass;
     rank0 = C.rank;
-    const int inside = (int)min(C.bin.count[d], (uint32_t)FEW + 1);
+    inside = (int)min(C.bin.count[d], (uint32_t)FEW + 1);
     lo += (u64)(BINS - 1 - d) << shift;
     hi = min(hi, lo + ((1ull << shift) - 1));
-    if (inside > FEW) continue;       // places differ: at the latest a window of one has one token
-    each([&](float x, int id) {
-      const u64 p = place_of(x, id);
-      if (p >= lo && p <= hi) {
-        const int i = atomicAdd(&C.n_few, 1);
-        C.few[i] = p;
-        C.weight[i] = row.fixed(x);
-      }
-    });
-    __syncthreads();
-    if (tid < inside) {
-      const u64 p = C.few[tid];
-      u64 before = mass0, rank = rank0;
-      for (int j = 0; j < inside; ++j) {
-        const bool in_front = C.few[j] > p;
-        rank += in_front;
-        before += in_front ? C.weight[j] : 0;
-      }
-      if (!reaches(rank, before) && reaches(rank + 1, before + C.weight[tid])) {
-        C.found = p;
-        C.mass = before + C.weight[tid];
-      }
-    }
-    __syncthreads();
-    *mass = C.mass;
-    return C.found;
   }
+  __syncthreads();
+  if (tid == 0) { C.n_few = 0; C.found = 0; C.mass = mass0; }
+  __syncthreads();
+  each([&](float x, int id) {
+    const u64 p = place_of(x, id);
+    if (p >= lo && p <= hi) {
+      const int i = atomicAdd(&C.n_few, 1);
+      C.few[i] = p;
+      C.weight[i] = row.fixed(x);
+    }
+  });
+  __syncthreads();
+  inside = C.n_few;
+  if (tid < inside) {
+    u64 before = mass0, rank = rank0;
+    compare_few(C, inside, C.few[tid], rank, before);
+    const u64 end = before + C.weight[tid];
+    if (!reaches(rank, before) && reaches(rank + 1, end)) {
+      C.found = C.few[tid];
+      C.mass = end;
+    } else if (rank + 1 == rank0 + inside && !reaches(rank + 1, end)) {
+      C.mass = end;                   // the limit lies behind the last token
+    }
+  }
+  __syncthreads();
+  *mass = C.mass;
+  return C.found;
 }
 
 template <typename T, bool VEC, bool CUT>
-__global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs) {
+__global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int parts) {
   __shared__ RowMemory S;
   __shared__ typename std::conditional<CUT, CutMemory, int>::type cut;
   __shared__ u64 start;
@@ -585,9 +640,8 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs) {
     }
     return;
   }
-  const double inv_t = o.temperature == 0.0 ? 1.0 : 1.0 / o.temperature;
   auto answer = [&](int id, float zi, double kept) {
-    const double lw = ((double)zi - (double)row.zmax) * inv_t;
+    const double lw = ((double)zi - (double)row.zmax) * row.c * 0.6931471805599453;
     A.token[r] = id;
     A.logprob[r] = (float)(lw - log(row.total));
     A.kept[r] = (float)(o.temperature == 0.0 ? 0.0 : lw - log(kept));
@@ -606,16 +660,17 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs) {
     if (hit == INT32_MAX) hit = -group_min<PICK>(w > 0 ? -tid : 1, S.redi);   // roundings next to u = 1: the last with a weight
     if (tid == hit) answer(s * SEG + tid, zi, kept);
   };
-  // The first segment at whose end the running sum of f(segment) passes `want`, and the
+  // The first of n entries at whose end the running sum of f(entry) passes `want`, and the
   // sum in front of it.  Where roundings next to u = 1 leave none: the last that has a
   // weight, and nothing that its tokens could pass.
-  auto find_segment = [&](auto f, double& want, auto& before) {
+  auto find_entry = [&](int n, auto f, double& want, auto& before) {
     using V = typename std::remove_reference<decltype(before)>::type;
-    V run = 0;
+    V run = before;
     int last = 0;
-    for (int base = 0; base < segs; base += PICK) {
+#pragma unroll 1
+    for (int base = 0; base < n; base += PICK) {
       const int i = base + tid;
-      const V w = i < segs ? f(i) : 0;
+      const V w = i < n ? f(i) : 0;
       V all;
       const V end = group_prefix<PICK>(w, reinterpret_cast<V*>(S.red), &all) + run;
       const int at = group_min<PICK>(w > 0 && (double)end > want ? i : INT32_MAX, S.redi);
@@ -628,7 +683,6 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs) {
       last = max(last, -group_min<PICK>(w > 0 ? -i : 0, S.redi));
       run += all;
     }
-    before = 0;
     want = INFINITY;
     return last;
   };
@@ -644,18 +698,17 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs) {
     return;
   }
   if (!CUT || !(o.by_k || o.by_p || o.by_min)) {   // every token can be drawn
-    double before, want = u * row.total;
-    const int at = find_segment([&](int i) { return row.share_of(A, r, i); }, want, before);
+    double before = 0.0, want = u * row.total;
+    const int at = find_entry(segs, [&](int i) { return row.share_of(i, A.seg_s[(int64_t)r * segs + i]); }, want, before);
     const float zi = token(at);
     finish(at, zi, zi == -INFINITY ? 0.0 : weight_of(zi, row.zmax, row.c), before, want, row.total);
     return;
   }
   if constexpr (CUT) {
-    CutMemory* const C = &cut;
-    u64 border = 0, kept = 0;
-    float t0;                         // no token below it is kept
+    CutMemory& C = *&cut;
     const float min_z = o.by_min ? min_p_border(o, row.zmax) : -INFINITY;
-    if (o.by_min) border = (u64)key_of(min_z) << ID_BITS;
+    u64 border = o.by_min ? (u64)key_of(min_z) << ID_BITS : 0;
+    float t0;                         // no token below it is kept
     DrawRow info{};
     bool binned = by_bins(o);
     if (binned) {
@@ -663,51 +716,114 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs) {
       binned = info.listed <= LIST;
       t0 = info.t0;
     } else {                          // top-p takes its share of all the k
-      t0 = row.least(o.by_k, o.top_k, false, 1.0, o.by_p ? -INFINITY : min_z);
+      float* strips = nullptr;        // where k is too many for the segments
+      if (o.by_k && 2 * o.top_k > segs && 4 * segs <= LIST) {
+        strips = reinterpret_cast<float*>(C.list);
+        for (int i = tid; i < 8 * segs; i += PICK) strips[i] = A.strip_m[(int64_t)r * segs * 8 + i];
+        __syncthreads();
+      }
+      t0 = row.least(strips, o.by_k ? o.top_k : 0, false, 1.0);
+      if (!o.by_p) t0 = fmaxf(t0, min_z);
     }
-    if (tid == 0) C->n_list = 0;
-    row.activate(t0);
-    int n_list;
+    if (tid == 0) C.n_list = 0;
+    __syncthreads();
     if (binned) {
-      n_list = info.listed;
-      for (int i = tid; i < n_list; i += PICK) C->list[i] = A.list[(int64_t)r * LIST + i];
+      if (tid == 0) C.n_list = info.listed;
+      for (int i = tid; i < info.listed; i += PICK) C.list[i] = A.list[(int64_t)r * LIST + i];
     } else {
-      row.from_memory(t0, [&](float x, int id, bool on) { append(on && x > -INFINITY, place_of(x, id), &C->n_list, C->list); });
-      __syncthreads();
-      n_list = C->n_list;
+      row.tokens(t0, 0, segs, [&](float x, int id) {
+        const int i = atomicAdd(&C.n_list, 1);
+        if (i < LIST) C.list[i] = place_of(x, id);
+      });
     }
     __syncthreads();
+    const int n_list = C.n_list;
+    if (!binned && n_list <= FEW) {   // few: compared with one another, drawn from by comparing ids
+      u64 p = 0, w = 0, rank = 0, before = 0, all;
+      if (tid < n_list) {
+        p = C.few[tid] = C.list[tid];
+        w = C.weight[tid] = row.fixed(z_of(p));
+      }
+      __syncthreads();
+      if (tid < n_list) compare_few(C, n_list, p, rank, before);
+      bool in = tid < n_list && (!o.by_k || rank < (u64)o.top_k);
+      group_prefix<PICK>(in ? w : 0, S.red, &all);
+      if (o.by_p) in = in && (double)before < mass_limit(o, o.by_k ? (double)all : row.total * FIXED_ONE);
+      in = in && p >= border;
+      __syncthreads();
+      if (tid < FEW) C.weight[tid] = in ? w : 0;
+      group_prefix<PICK>(in ? w : 0, S.red, &all);
+      const double want = u * (double)all;
+      const int id = id_of(p);
+      u64 end = 0;
+      if (in)
+#pragma unroll 4
+        for (int j = 0; j < n_list; ++j) end += id_of(C.few[j]) <= id ? C.weight[j] : 0;
+      int hit = group_min<PICK>(in && w > 0 && (double)end > want ? id : INT32_MAX, S.redi);
+      if (hit == INT32_MAX) hit = -group_min<PICK>(in && w > 0 ? -id : 1, S.redi);
+      if (in && id == hit) answer(id, z_of(p), (double)all / FIXED_ONE);
+      return;
+    }
     auto each = [&](auto f) {
       if (n_list <= LIST) {
-        for (int i = tid; i < n_list; i += PICK) f(z_of(C->list[i]), id_of(C->list[i]));
+        for (int i = tid; i < n_list; i += PICK) f(z_of(C.list[i]), id_of(C.list[i]));
       } else {
-        row.from_memory(t0, [&](float x, int id, bool on) {
-          if (on && x > -INFINITY) f(x, id);
-        });
+        row.tokens(t0, 0, segs, f);
       }
     };
     const u64 lo = place_of(t0, (1 << ID_BITS) - 1), hi = place_of(row.zmax, 0);
-    if (o.by_k) {
+    double share = row.total * FIXED_ONE;
+#pragma unroll 1
+    for (int rule = 0; rule < 2; ++rule) {
+      if (rule == 0 ? !o.by_k : !o.by_p || (binned && info.bin == BINS)) continue;
       u64 mass;
-      border = max(border, find_border(row, *C, each, true, (double)o.top_k, lo, hi, 0, &mass));
-      if (o.by_p) border = max(border, find_border(row, *C, each, false, mass_limit(o, (double)mass), lo, hi, 0, &mass));
-    } else if (o.by_p && !(binned && info.bin == BINS)) {
-      u64 mass;
-      border = max(border, find_border(row, *C, each, false, mass_limit(o, row.total * FIXED_ONE), lo, hi,
+      border = max(border, find_border(row, C, each, n_list, rule == 0, rule == 0 ? (double)o.top_k : mass_limit(o, share), lo, hi,
                                        binned ? info.above : 0, &mass));
+      share = (double)mass;
+    }
+    // What is kept of each segment or, where the histogram knows the parts', of each part
+    // and then of that part's segments.
+    __syncthreads();
+    int s0 = 0, s1 = segs;
+    u64 before = 0, mine = 0, kept;
+    double want = 0.0;
+    if (binned) {
+      for (int i = tid; i < parts; i += PICK) C.seg[i] = A.part_kept[(int64_t)r * parts + i];
+      __syncthreads();
+      for (int i = tid; i < n_list; i += PICK)
+        if (C.list[i] >= border) {
+          const int s = id_of(C.list[i]) / SEG;
+          int p = (int)((int64_t)s * parts / segs);
+          while (part_start(p + 1, segs, parts) <= s) ++p;
+          atomicAdd(&C.seg[p], row.fixed(z_of(C.list[i])));
+        }
+      __syncthreads();
+      for (int i = tid; i < parts; i += PICK) mine += C.seg[i];
+      group_prefix<PICK>(mine, S.red, &kept);
+      want = u * (double)kept;
+      const int p = find_entry(parts, [&](int i) { return C.seg[i]; }, want, before);
+      s0 = part_start(p, segs, parts);
+      s1 = part_start(p + 1, segs, parts);
+      __syncthreads();
+    }
+    for (int i = tid; i < segs; i += PICK) C.seg[i] = 0;
+    __syncthreads();
+    if (!binned && n_list <= LIST) {
+      each([&](float x, int id) {
+        if (place_of(x, id) >= border) atomicAdd(&C.seg[id / SEG], row.fixed(x));
+      });
+    } else {
+      row.tokens(t0, s0, s1, [&](float x, int id) {
+        if (place_of(x, id) >= border) atomicAdd(&C.seg[id / SEG], row.fixed(x));
+      });
     }
     __syncthreads();
-    for (int i = tid; i < segs; i += PICK) C->seg[i] = binned ? A.kept_seg[(int64_t)r * segs + i] : 0;
-    __syncthreads();
-    each([&](float x, int id) {
-      if (place_of(x, id) >= border) atomicAdd(&C->seg[id / SEG], row.fixed(x));
-    });
-    __syncthreads();
-    u64 mine = 0, before;
-    for (int i = tid; i < segs; i += PICK) mine += C->seg[i];
-    group_prefix<PICK>(mine, S.red, &kept);
-    double want = u * (double)kept;
-    const int at = find_segment([&](int i) { return C->seg[i]; }, want, before);
+    if (!binned) {
+      for (int i = tid; i < segs; i += PICK) mine += C.seg[i];
+      group_prefix<PICK>(mine, S.red, &kept);
+      want = u * (double)kept;
+    }
+    const int at = s0 + find_entry(s1 - s0, [&](int i) { return C.seg[s0 + i]; }, want, before);
     const float zi = token(at);
     const int id = at * SEG + tid;
     finish(at, zi, id < A.vocab && place_of(zi, id) >= border ? row.fixed(zi) : (u64)0, before, want, (double)kept / FIXED_ONE);
@@ -722,39 +838,52 @@ bool may_bin(const DrawArgs& a) {
   return (a.top_k_rows || a.top_k == 0 || a.top_k >= a.vocab) && (a.top_p_rows || a.min_p_rows || a.top_p < 1.0 || a.min_p > 0.0);
 }
 
-// Where the parts of the scratch are: a pointer is 0 bytes from its start where there is none.
+// Parts of a row in the histogram: enough to fill the chip, of eight segments at least,
+// and few enough to go through one again in the pick.
+int parts_of(const DrawArgs& a) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(1024 / a.rows, 4), (segments(a.vocab) + 7) / 8));
+}
+
+// Where the parts of the scratch are.
 struct Scratch {
-  int64_t seg_s, seg_m, kept_seg, bins, list, info, end;
+  int64_t seg_s, part_bins, part_kept, bins, list, info, seg_m, strip_m, end;
 };
 Scratch scratch_of(const DrawArgs& a) {
-  const int64_t rows = a.rows, n = rows * segments(a.vocab), binned = may_bin(a) ? rows : 0;
+  const int64_t rows = a.rows, n = rows * segments(a.vocab), binned = may_bin(a) ? rows : 0, parts = binned * parts_of(a);
   Scratch s;
   s.seg_s = 0;
-  s.kept_seg = s.seg_s + 8 * n;
-  s.bins = s.kept_seg + (binned ? 8 * n : 0);
+  s.part_bins = s.seg_s + 8 * n;
+  s.part_kept = s.part_bins + 8 * parts * BINS;
+  s.bins = s.part_kept + 8 * parts;
   s.list = s.bins + 8 * binned * BINS;
   s.info = s.list + 8 * binned * LIST;
   s.seg_m = s.info + (int64_t)sizeof(DrawRow) * binned;
-  s.end = (s.seg_m + 4 * n + 15) / 16 * 16;
+  s.strip_m = s.seg_m + 4 * n;
+  s.end = (s.strip_m + (may_cut(a) ? 32 * n : 0) + 15) / 16 * 16;
   return s;
 }
 
 template <typename T, bool VEC>
 hipError_t run(const DrawArgs& a, hipStream_t st) {
   const int segs = segments(a.vocab);
-  const int64_t items = (int64_t)a.rows * segs, grid = (items + SCAN_WAVES - 1) / SCAN_WAVES;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  hipError_t e = kv8_launch(k_draw_scan<T, VEC>, dim3((unsigned)grid), dim3(64 * SCAN_WAVES), st, a, segs, items);
-  if (e != hipSuccess) return e;
+  const unsigned per_row = (unsigned)(segs + 3) / 4;
+  const int64_t items = (int64_t)a.rows * per_row;
+  if (items > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)((items + SCAN_WAVES - 1) / SCAN_WAVES)), scan(64 * SCAN_WAVES), row(PICK);
+  hipError_t e;
+  if (!may_cut(a)) {
+    if ((e = kv8_launch(k_draw_scan<T, VEC, false>, grid, scan, st, a, segs, per_row, (unsigned)items)) != hipSuccess) return e;
+    return kv8_launch(k_draw_pick<T, VEC, false>, dim3(a.rows), row, st, a, segs, 0);
+  }
+  if ((e = kv8_launch(k_draw_scan<T, VEC, true>, grid, scan, st, a, segs, per_row, (unsigned)items)) != hipSuccess) return e;
+  const int parts = parts_of(a);
   if (a.bins) {
-    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / a.rows, (segs + 7) / 8));
     if ((int64_t)a.rows * parts > INT32_MAX) return hipErrorInvalidValue;
     const dim3 g((unsigned)(a.rows * parts));
     if ((e = kv8_launch(k_draw_bins<T, VEC>, g, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
     if ((e = kv8_launch(k_draw_collect<T, VEC>, g, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
   }
-  return may_cut(a) ? kv8_launch(k_draw_pick<T, VEC, true>, dim3(a.rows), dim3(PICK), st, a, segs)
-                    : kv8_launch(k_draw_pick<T, VEC, false>, dim3(a.rows), dim3(PICK), st, a, segs);
+  return kv8_launch(k_draw_pick<T, VEC, true>, dim3(a.rows), row, st, a, segs, parts);
 }
 
 }  // namespace
@@ -766,10 +895,13 @@ hipError_t launch_draw(DrawArgs a, void* scratch, hipStream_t st) {
   if (a.vocab < 1 || a.vocab > DRAW_MAX_VOCAB) return hipErrorInvalidValue;
   const Scratch s = scratch_of(a);
   char* p = (char*)scratch;
+  a.c = a.temperature == 0.0 ? LOG2E : LOG2E / a.temperature;
   a.seg_s = (double*)(p + s.seg_s);
   a.seg_m = (float*)(p + s.seg_m);
+  a.strip_m = (float*)(p + s.strip_m);
   if (may_bin(a)) {
-    a.kept_seg = (unsigned long long*)(p + s.kept_seg);
+    a.part_bins = (unsigned long long*)(p + s.part_bins);
+    a.part_kept = (unsigned long long*)(p + s.part_kept);
     a.bins = (unsigned long long*)(p + s.bins);
     a.list = (unsigned long long*)(p + s.list);
     a.info = (DrawRow*)(p + s.info);

@@ -506,10 +506,12 @@ struct DrawArgs {
   const float* temperature_rows; const int32_t* top_k_rows;   // [rows], in the place of the numbers above, or NULL
   const float* top_p_rows; const float* min_p_rows;
   int32_t* token; float* logprob; float* kept;                // [rows] each
-  // of the scratch: maximum and sum of every row's segments and, where rows go by
-  // histogram, what their segments keep, the bins, the lists and what is known of them
-  double* seg_s; float* seg_m;
-  unsigned long long* kept_seg; unsigned long long* bins; unsigned long long* list;
+  double c;             // octaves of weight per logit at that temperature
+  // of the scratch: maximum and sum of every row's segments, maxima of their strips and,
+  // where rows go by histogram, the bins of each part and of all, what each part keeps,
+  // the lists and what is known of a row
+  double* seg_s; float* seg_m; float* strip_m;
+  unsigned long long* part_bins; unsigned long long* part_kept; unsigned long long* bins; unsigned long long* list;
   DrawRow* info;
 };
 int64_t draw_scratch_bytes(const DrawArgs& a);
