@@ -82,23 +82,34 @@ __device__ __forceinline__ bool usable(const RowOpts& o) {
 }
 
 // 2^t for t in [-1000, 1000]: 2^n times a polynomial of degree 8 that interpolates 2^f
-// at the Chebyshev points of [-1/2, 1/2], 1.1e-12 relative.
-__device__ __forceinline__ double exp2_64(double t) {
-  constexpr double shifter = 6755399441055744.0;              // 1.5 * 2^52: the sum's low bits are t to nearest
-  const double s = t + shifter, f = t - (s - shifter);
-  double p = 1.3255224884799127e-06;
-  p = fma(p, f, 1.5310079402383103e-05);
-  p = fma(p, f, 0.00015403455852419016);
-  p = fma(p, f, 0.0013333450568000008);
-  p = fma(p, f, 0.00961812915940262);
-  p = fma(p, f, 0.05550410941205934);
-  p = fma(p, f, 0.2402265069581299);
-  p = fma(p, f, 0.6931471805459335);
-  p = fma(p, f, 1.0);
-  const u64 b = __builtin_bit_cast(u64, p);                   // n into the exponent: of the high word alone
-  const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)__builtin_bit_cast(u64, s) << 20);
-  return __builtin_bit_cast(double, (u64)hi << 32 | (uint32_t)b);
-}
+// at the Chebyshev points of [-1/2, 1/2], 1.1e-12 relative.  Its coefficients are held in
+// scalar registers: as literals they were moved into vector ones again for every segment.
+struct Exp2 {
+  static constexpr int N = 8;
+  u64 a[N];
+  __device__ __forceinline__ Exp2() {
+    constexpr double coefficients[N] = {1.3255224884799127e-06, 1.5310079402383103e-05, 0.00015403455852419016,
+                                        0.0013333450568000008,  0.00961812915940262,    0.05550410941205934,
+                                        0.2402265069581299,     0.6931471805459335};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      a[i] = __builtin_bit_cast(u64, coefficients[i]);
+      asm("" : "+s"(a[i]));
+    }
+  }
+  __device__ __forceinline__ double operator()(double t) const {
+    constexpr double shifter = 6755399441055744.0;            // 1.5 * 2^52: the sum's low bits are t to nearest
+    const double s = t + shifter, f = t - (s - shifter);
+    double p = __builtin_bit_cast(double, a[0]);
+#pragma unroll
+    for (int i = 1; i < N; ++i) p = fma(p, f, __builtin_bit_cast(double, a[i]));
+    p = fma(p, f, 1.0);
+    u32x2_t w = __builtin_bit_cast(u32x2_t, p);               // n into the exponent: of the high word alone
+    w[1] += __builtin_bit_cast(u32x2_t, s)[0] << 20;
+    return __builtin_bit_cast(double, w);
+  }
+};
+__device__ __forceinline__ double exp2_64(double t) { return Exp2()(t); }
 // The weight of z with respect to top (finite, no less): octaves below 1000 count nothing.
 __device__ __forceinline__ double weight_of(float z, float top, double c) {
   return exp2_64(fmax(((double)z - (double)top) * c, -1000.0));
@@ -111,40 +122,52 @@ __device__ __forceinline__ u64 fixed_of(double w) {
 // NaN where either is.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double moved(double v) {            // lanes without a source: 0
-  const u64 b = __builtin_bit_cast(u64, v);
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xf, false);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xf, false);
-  return __builtin_bit_cast(double, (u64)hi << 32 | lo);
+// The wave's sum, in lane 63 alone: lanes past a row's end, and rows without a source, add
+// 0; what the middle rows take in twice never gets there.
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+  const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+  return __builtin_bit_cast(double, u32x2_t{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, 0xf, 0xf, true),
+                                            (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, 0xf, 0xf, true)});
 }
-// Over the wave's lanes; the result is in lane 63.
 __device__ __forceinline__ double sum_to_63(double v) {
-  v += moved<0x111, 0xf>(v);          // row_shr 1, 2, 4, 8, then row_bcast 15 and 31
-  v += moved<0x112, 0xf>(v);
-  v += moved<0x114, 0xf>(v);
-  v += moved<0x118, 0xf>(v);
-  v += moved<0x142, 0xa>(v);
-  v += moved<0x143, 0xc>(v);
+  v += moved<0x111>(v);               // row_shr 1, 2, 4, 8, then row_bcast 15 and 31
+  v += moved<0x112>(v);
+  v += moved<0x114>(v);
+  v += moved<0x118>(v);
+  v += moved<0x142>(v);
+  v += moved<0x143>(v);
   return v;
 }
-template <int CTRL>
-__device__ __forceinline__ float max_moved(float v) {
-  return max_nan(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, 0xf, 0xf, false)));
+__device__ __forceinline__ double from_63(double v) {
+  const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+  return __builtin_bit_cast(double, u32x2_t{(uint32_t)__builtin_amdgcn_readlane((int)w[0], 63),
+                                            (uint32_t)__builtin_amdgcn_readlane((int)w[1], 63)});
 }
-__device__ __forceinline__ float max_nan_wave(float v) {
+// Maxima over lanes go by whole numbers in the order of z, NaN above all: one lane move
+// and comparison a step.
+__device__ __forceinline__ int rank_of(float z) {
+  const int u = __float_as_int(z);
+  return z == z ? u ^ (u >> 31 & 0x7FFFFFFF) : INT32_MAX;
+}
+__device__ __forceinline__ float of_rank(int k) {
+  return k == INT32_MAX ? __uint_as_float(0x7FC00000u) : __int_as_float(k ^ (k >> 31 & 0x7FFFFFFF));
+}
+template <int CTRL>
+__device__ __forceinline__ int max_moved(int v) {
+  return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float max_nan_wave(float z) {
+  int v = rank_of(z);
   v = max_moved<0x111>(v);
   v = max_moved<0x112>(v);
   v = max_moved<0x114>(v);
   v = max_moved<0x118>(v);
   v = max_moved<0x142>(v);
   v = max_moved<0x143>(v);
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+  return of_rank(__builtin_amdgcn_readlane(v, 63));
 }
-__device__ __forceinline__ float sum_wave(float v) {
-  double d = sum_to_63((double)v);
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int((float)d), 63));
-}
+__device__ __forceinline__ float sum_wave(float v) { return (float)from_63(sum_to_63((double)v)); }
 
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const T* p, int i, int n, float (&v)[8]) {
@@ -172,41 +195,50 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int s
 #pragma unroll
   for (int j = 0; j < U; ++j) load8<T, VEC>(z, (s0 + j) * SEG + 8 * lane, A.vocab, v[j]);
   const double c = octaves_per_logit(A, r);
+  int rank[U];
 #pragma unroll
   for (int j = 0; j < U; ++j) {
-    m[j] = v[j][0];
+    float top = v[j][0];
 #pragma unroll
-    for (int e = 1; e < 8; ++e) m[j] = max_nan(m[j], v[j][e]);
+    for (int e = 1; e < 8; ++e) top = max_nan(top, v[j][e]);
+    rank[j] = rank_of(top);
   }
-  auto steps = [&](auto ctrl) {
+  auto step = [&](auto ctrl) {
 #pragma unroll
-    for (int j = 0; j < U; ++j) m[j] = max_moved<decltype(ctrl)::value>(m[j]);
+    for (int j = 0; j < U; ++j) rank[j] = max_moved<decltype(ctrl)::value>(rank[j]);
   };
-  steps(std::integral_constant<int, 0x111>{});
-  steps(std::integral_constant<int, 0x112>{});
-  steps(std::integral_constant<int, 0x114>{});
+  step(std::integral_constant<int, 0x111>{});
+  step(std::integral_constant<int, 0x112>{});
+  step(std::integral_constant<int, 0x114>{});
   if constexpr (CUT) {                            // lanes 7, 15, ..: of eight lanes
 #pragma unroll
     for (int j = 0; j < U; ++j)
-      if ((lane & 7) == 7 && s0 + j < segs) A.strip_m[((int64_t)r * segs + s0 + j) * 8 + (lane >> 3)] = m[j];
+      if ((lane & 7) == 7 && s0 + j < segs) A.strip_m[((int64_t)r * segs + s0 + j) * 8 + (lane >> 3)] = of_rank(rank[j]);
   }
-  steps(std::integral_constant<int, 0x118>{});
-  steps(std::integral_constant<int, 0x142>{});
-  steps(std::integral_constant<int, 0x143>{});
-  double s[U];
+  step(std::integral_constant<int, 0x118>{});
+  step(std::integral_constant<int, 0x142>{});
+  step(std::integral_constant<int, 0x143>{});
+  bool plain = true;                              // finite maxima, z c - m c good to 2^-44
+  double mc[U], s[U];
 #pragma unroll
   for (int j = 0; j < U; ++j) {
-    m[j] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m[j]), 63));
+    m[j] = of_rank(__builtin_amdgcn_readlane(rank[j], 63));
+    mc[j] = (double)m[j] * c;
+    plain = plain && fabs(mc[j]) < 1024.0;
     s[j] = 0.0;
-    if (!(m[j] > -INFINITY && m[j] < INFINITY)) continue;   // the sum is not looked at, or nothing
-    const double mc = (double)m[j] * c;
-    if (fabs(mc) < 1024.0) {                      // z c - m c to 2^-44
+  }
+  const Exp2 exp2;
+  if (plain) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[j] += exp2_64(fmax(fma((double)v[j][e], c, -mc), -1000.0));
-    } else {
-#pragma unroll 1
-      for (int e = 0; e < 8; ++e) s[j] += weight_of(v[j][e], m[j], c);
-    }
+    for (int j = 0; j < U; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[j] += exp2(fmax(fma((double)v[j][e], c, -mc[j]), -1000.0));
+  } else {
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (m[j] > -INFINITY && m[j] < INFINITY)    // else the sum is not looked at, or nothing
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[j] += weight_of(v[j][e], m[j], c);
   }
 #pragma unroll
   for (int j = 0; j < U; ++j) s[j] = sum_to_63(s[j]);
@@ -280,124 +312,155 @@ __device__ __forceinline__ float bin_factor(double c) { return (float)fmin(c, 3.
 struct RowMemory {
   float m[MAX_SEGS];                  // maxima of the segments
   float share[MAX_SEGS];              // their sums with respect to the row's maximum
-  double redd[8];
   u64 red[8];
-  float redf[8];
   int redi[8];
 };
+template <int N>
+struct ActiveMemory {                 // each wave's segments that can hold kept tokens
+  uint16_t seg[N / 64][MAX_SEGS * 64 / N + 1];
+};
 
+// A row as every wave sees it: each reads all of the segments, so that nothing waits for
+// another wave.  Lane l has those numbered l + 64 j, the first REGS in registers.
 template <typename T, bool VEC, int N>
 struct Row {
+  static constexpr int REGS = 5;      // segments of a lane: 163840 tokens
   const T* z;
   int vocab, segs;
   float zmax;
   double c, total;
   RowMemory* S;
+  float m[REGS], share[REGS];
+
+  // f(index, maximum, share) for every segment of the lane
+  template <typename F>
+  __device__ __forceinline__ void each_segment(F f) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < REGS; ++j)
+      if (64 * j < segs) f(lane + 64 * j, m[j], share[j]);   // past the last: -inf and 0
+#pragma unroll 1
+    for (int i = lane + 64 * REGS; i - lane < segs; i += 64) f(i, i < segs ? S->m[i] : -INFINITY, i < segs ? S->share[i] : 0.f);
+  }
 
   // The row's segments; false where it has no answer.
   __device__ __forceinline__ bool read(const DrawArgs& A, int r, int n_segs, const RowOpts& o) {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const float* seg_m = A.seg_m + (int64_t)r * n_segs;
+    const double* seg_s = A.seg_s + (int64_t)r * n_segs;
     z = (const T*)A.logits + r * A.row;
     vocab = A.vocab;
     segs = n_segs;
     c = o.c;
-    double s0 = 0.0;                  // the first round's sums come beside its maxima
-    float m = -INFINITY;
-#pragma unroll 1
-    for (int i = tid; i < segs; i += N) {
-      const float x = A.seg_m[(int64_t)r * segs + i];
-      if (i == tid) s0 = A.seg_s[(int64_t)r * segs + i];
-      S->m[i] = x;
-      m = max_nan(m, x);
-    }
-    m = max_nan_wave(m);
-    if ((tid & 63) == 0) S->redf[tid >> 6] = m;
-    __syncthreads();
-    m = S->redf[0];
+    double s[REGS];
+    float top = -INFINITY;
 #pragma unroll
-    for (int i = 1; i < N / 64; ++i) m = max_nan(m, S->redf[i]);
-    zmax = m;
+    for (int j = 0; j < REGS; ++j) {
+      const int i = lane + 64 * j;
+      m[j] = i < segs ? seg_m[i] : -INFINITY;
+      s[j] = i < segs ? seg_s[i] : 0.0;
+    }
+#pragma unroll
+    for (int j = 0; j < REGS; ++j) top = max_nan(top, m[j]);
+#pragma unroll 1
+    for (int i = lane + 64 * REGS; i < segs; i += 64) top = max_nan(top, seg_m[i]);
+    zmax = max_nan_wave(top);
     if (!(zmax > -INFINITY && zmax < INFINITY) || !usable(o)) return false;   // NaN too
     double part = 0.0;
+#pragma unroll
+    for (int j = 0; j < REGS; ++j) {
+      const double w = share_of(m[j], s[j]);
+      share[j] = (float)w;
+      part += w;
+      const int i = lane + 64 * j;
+      if (i < segs) {                 // every wave writes the same
+        S->m[i] = m[j];
+        S->share[i] = share[j];
+      }
+    }
 #pragma unroll 1
-    for (int i = tid; i < segs; i += N) {
-      const double w = share_of(i, i == tid ? s0 : A.seg_s[(int64_t)r * segs + i]);
+    for (int i = lane + 64 * REGS; i < segs; i += 64) {
+      const double w = share_of(seg_m[i], seg_s[i]);
+      S->m[i] = seg_m[i];
       S->share[i] = (float)w;
       part += w;
     }
-    part = sum_to_63(part);
-    if ((tid & 63) == 63) S->redd[tid >> 6] = part;
-    __syncthreads();
-    total = 0.0;
-#pragma unroll
-    for (int i = 0; i < N / 64; ++i) total += S->redd[i];
+    total = from_63(sum_to_63(part));
     return true;
   }
-  __device__ __forceinline__ double share_of(int i, double s) const {
-    const float m = S->m[i];
-    return m == -INFINITY ? 0.0 : s * weight_of(m, zmax, c);
+  __device__ __forceinline__ double share_of(float top, double s) const {
+    return top == -INFINITY ? 0.0 : s * weight_of(top, zmax, c);
   }
   __device__ __forceinline__ u64 fixed(float x) const { return x == -INFINITY ? 0 : fixed_of(weight_of(x, zmax, c)); }
 
-  // The least z that can be kept (see above).  Every wave halves the octaves that are left
-  // by itself, with what the lanes have of the segments, or of the strips where given.
-  __device__ __forceinline__ float least(const float* strips, int k, bool by_p, double p) const {
+  // The least z that can be kept (see above), the octaves that are left halved again and
+  // again.  strips (n_strips of them, or none): taken in the place of the segments.
+  __device__ __forceinline__ float least(const float* strips, int n_strips, int k, bool by_p, double p) const {
     const int lane = threadIdx.x & 63;
     float lo = 0.f, hi = FIXED_OCTAVES;
-    if (k > 0 || by_p) {
-      const float* const top = strips ? strips : S->m;
-      const int n = strips ? 8 * segs : segs;
+    if (by_p || (k > 0 && k <= max(n_strips, segs))) {
       const float spare = (float)((1.0 - fmax(p, 0.0)) * total * (1.0 - 1e-5)), cf = bin_factor(c);
-      if (by_p || k <= n) {
 #pragma unroll 1
-        for (int round = 0; round < 8; ++round) {
-          const float y = 0.5f * (lo + hi), cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
+      for (int round = 0; round < 8; ++round) {
+        const float y = 0.5f * (lo + hi);
+        bool pass;
+        if (by_p) {
+          const float cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
           float below = 0.f;
+          each_segment([&](int, float top, float part) { below += (zmax - top) * cf <= y ? fminf(part, cap) : part; });
+          pass = sum_wave(below) <= spare;
+        } else {
           int count = 0;
+          if (n_strips) {
 #pragma unroll 4
-          for (int i = lane; i < n; i += 64) {
-            const bool above = (zmax - top[i]) * cf <= y;
-            count += above;
-            if (by_p) below += above ? fminf(S->share[i], cap) : S->share[i];
+            for (int i = lane; i < n_strips; i += 64) count += (zmax - strips[i]) * cf <= y;
+            count = wave_sum_dpp(count);
+          } else {
+            each_segment([&](int, float top, float) { count += __popcll(__ballot((zmax - top) * cf <= y)); });
           }
-          const bool pass = by_p ? sum_wave(below) <= spare : wave_sum_dpp(count) >= k;
-          if (pass) hi = y;
-          else lo = y;
+          pass = count >= k;
         }
+        if (pass) hi = y;
+        else lo = y;
       }
     }
     const float t = (float)((double)zmax - ((double)hi + 2e-3) / c);
     return t <= -3.4e38f ? -INFINITY : of_key(key_of(t) - 2);   // 2e-3 and two steps: what was rounded on the way
   }
   // f(z, id) for every token of t0 or more, of segments s0 .. s1 - 1; whole waves call it.
-  // The next segment is on its way while one is looked at.
+  // The waves take the segments that have one in turn, four on their way at once.
   template <typename F>
-  __device__ __forceinline__ void tokens(float t0, int s0, int s1, F f) const {
-    const int lane = threadIdx.x & 63;
-    auto next = [&](int s) {
-      while (s < s1 && S->m[s] < t0) s += N / 64;
-      return __builtin_amdgcn_readfirstlane(s);
-    };
-    int s = next(s0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
-    float v[8];
-    if (s < s1) load8<T, VEC>(z, s * SEG + 8 * lane, vocab, v);
+  __device__ __forceinline__ void tokens(ActiveMemory<N>& M, float t0, int s0, int s1, F f) const {
+    constexpr int W = N / 64, U = 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    int found = 0;
+    each_segment([&](int i, float top, float) {
+      const bool on = i >= s0 && i < s1 && top >= t0 && top > -INFINITY;
+      const uint64_t mask = __ballot(on);
+      const int at = found + __popcll(mask & ((1ull << lane) - 1));
+      if (on && at % W == wave) M.seg[wave][at / W] = (uint16_t)i;
+      found += __popcll(mask);
+    });
+    const int n = (found - wave + W - 1) / W;
 #pragma unroll 1
-    while (s < s1) {
-      const int after = next(s + N / 64);
-      float w[8];
-      if (after < s1) load8<T, VEC>(z, after * SEG + 8 * lane, vocab, w);
-      float m = v[0];
+    for (int a = 0; a < n; a += U) {
+      float v[U][8];
+      int first[U];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) m = fmaxf(m, v[e]);
-      if (m >= t0 && m > -INFINITY) {
-        const int i = s * SEG + 8 * lane;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (v[e] >= t0 && v[e] > -INFINITY) f(v[e], i + e);   // tokens past the vocabulary are -inf
+      for (int j = 0; j < U; ++j) {
+        first[j] = a + j < n ? (int)M.seg[wave][a + j] * SEG + 8 * lane : vocab;
+        load8<T, VEC>(z, first[j], vocab, v[j]);
       }
-      s = after;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = w[e];
+      for (int j = 0; j < U; ++j) {
+        float top = v[j][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, v[j][e]);
+        if (top >= t0 && top > -INFINITY)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (v[j][e] >= t0 && v[j][e] > -INFINITY) f(v[j][e], first[j] + e);   // tokens past the vocabulary are -inf
+      }
     }
   }
 };
@@ -421,6 +484,7 @@ __device__ __forceinline__ int part_start(int p, int segs, int parts) { return (
 template <typename T, bool VEC>
 __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int parts) {
   __shared__ RowMemory S;
+  __shared__ ActiveMemory<PART> active;
   __shared__ u64 mass[BINS];
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
@@ -431,13 +495,14 @@ __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int pa
   const bool good = row.read(A, r, segs, o);
   float t0 = 0.f;
   if (good) {
-    t0 = row.least(nullptr, 0, o.by_p, o.top_p);
+    t0 = row.least(nullptr, 0, 0, o.by_p, o.top_p);
     if (o.by_min) t0 = fmaxf(t0, min_p_border(o, row.zmax));
   }
   if (part == 0 && tid == 0) A.info[r] = DrawRow{row.total, row.zmax, t0, good, 0, BINS, 0};
   if (!good) return;
+  __syncthreads();
   const float c = bin_factor(o.c);
-  row.tokens(t0, part_start(part, segs, parts), part_start(part + 1, segs, parts),
+  row.tokens(active, t0, part_start(part, segs, parts), part_start(part + 1, segs, parts),
              [&](float x, int) { atomicAdd(&mass[bin_of(x, row.zmax, c)], row.fixed(x)); });
   __syncthreads();
   u64* bins = A.part_bins + (int64_t)blockIdx.x * BINS;
@@ -623,9 +688,15 @@ __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Eac
   return C.found;
 }
 
+__device__ __forceinline__ u64 lane_of(u64 v, int lane) {
+  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+
 template <typename T, bool VEC, bool CUT>
-__global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int parts) {
+__global__ __launch_bounds__(PICK, 4) void k_draw_pick(DrawArgs A, int segs, int parts) {
   __shared__ RowMemory S;
+  __shared__ ActiveMemory<PICK> active;
   __shared__ typename std::conditional<CUT, CutMemory, int>::type cut;
   __shared__ u64 start;
   const int r = blockIdx.x, tid = threadIdx.x;
@@ -687,6 +758,7 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
     return last;
   };
 
+  __syncthreads();                    // S.m is there
   if (o.temperature == 0.0) {         // the first of the largest
     int top = INT32_MAX;
     for (int i = tid; i < segs; i += PICK)
@@ -699,7 +771,7 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
   }
   if (!CUT || !(o.by_k || o.by_p || o.by_min)) {   // every token can be drawn
     double before = 0.0, want = u * row.total;
-    const int at = find_entry(segs, [&](int i) { return row.share_of(i, A.seg_s[(int64_t)r * segs + i]); }, want, before);
+    const int at = find_entry(segs, [&](int i) { return row.share_of(S.m[i], A.seg_s[(int64_t)r * segs + i]); }, want, before);
     const float zi = token(at);
     finish(at, zi, zi == -INFINITY ? 0.0 : weight_of(zi, row.zmax, row.c), before, want, row.total);
     return;
@@ -716,13 +788,14 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
       binned = info.listed <= LIST;
       t0 = info.t0;
     } else {                          // top-p takes its share of all the k
-      float* strips = nullptr;        // where k is too many for the segments
+      float* const strips = reinterpret_cast<float*>(C.list);   // where k is too many for the segments
+      int n_strips = 0;
       if (o.by_k && 2 * o.top_k > segs && 4 * segs <= LIST) {
-        strips = reinterpret_cast<float*>(C.list);
-        for (int i = tid; i < 8 * segs; i += PICK) strips[i] = A.strip_m[(int64_t)r * segs * 8 + i];
+        n_strips = 8 * segs;
+        for (int i = tid; i < n_strips; i += PICK) strips[i] = A.strip_m[(int64_t)r * n_strips + i];
         __syncthreads();
       }
-      t0 = row.least(strips, o.by_k ? o.top_k : 0, false, 1.0);
+      t0 = row.least(strips, n_strips, o.by_k ? o.top_k : 0, false, 1.0);
       if (!o.by_p) t0 = fmaxf(t0, min_z);
     }
     if (tid == 0) C.n_list = 0;
@@ -731,36 +804,52 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
       if (tid == 0) C.n_list = info.listed;
       for (int i = tid; i < info.listed; i += PICK) C.list[i] = A.list[(int64_t)r * LIST + i];
     } else {
-      row.tokens(t0, 0, segs, [&](float x, int id) {
+      row.tokens(active, t0, 0, segs, [&](float x, int id) {
         const int i = atomicAdd(&C.n_list, 1);
         if (i < LIST) C.list[i] = place_of(x, id);
       });
     }
     __syncthreads();
     const int n_list = C.n_list;
-    if (!binned && n_list <= FEW) {   // few: compared with one another, drawn from by comparing ids
-      u64 p = 0, w = 0, rank = 0, before = 0, all;
-      if (tid < n_list) {
-        p = C.few[tid] = C.list[tid];
-        w = C.weight[tid] = row.fixed(z_of(p));
+    // Few: a lane each of one wave, compared with one another and drawn from by their ids.
+    if (!binned && n_list <= 64) {
+      if (tid >= 64) return;
+      const bool is = tid < n_list;
+      const u64 p = is ? C.list[tid] : 0, w = is ? row.fixed(z_of(p)) : 0;
+      const int id = is ? id_of(p) : INT32_MAX;
+      u64 before = 0, all = 0;
+      int rank = 0;
+      for (int j = 0; j < n_list; ++j) {
+        const bool in_front = lane_of(p, j) > p;
+        rank += in_front;
+        before += in_front ? lane_of(w, j) : 0;
       }
-      __syncthreads();
-      if (tid < n_list) compare_few(C, n_list, p, rank, before);
-      bool in = tid < n_list && (!o.by_k || rank < (u64)o.top_k);
-      group_prefix<PICK>(in ? w : 0, S.red, &all);
-      if (o.by_p) in = in && (double)before < mass_limit(o, o.by_k ? (double)all : row.total * FIXED_ONE);
+      bool in = is && (!o.by_k || rank < o.top_k);
+      if (o.by_p) {
+        double share = row.total * FIXED_ONE;
+        if (o.by_k) {
+          for (uint64_t left = __ballot(in); left; left &= left - 1) all += lane_of(w, __ffsll((unsigned long long)left) - 1);
+          share = (double)all;
+        }
+        in = in && (double)before < mass_limit(o, share);
+      }
       in = in && p >= border;
-      __syncthreads();
-      if (tid < FEW) C.weight[tid] = in ? w : 0;
-      group_prefix<PICK>(in ? w : 0, S.red, &all);
-      const double want = u * (double)all;
-      const int id = id_of(p);
       u64 end = 0;
-      if (in)
-#pragma unroll 4
-        for (int j = 0; j < n_list; ++j) end += id_of(C.few[j]) <= id ? C.weight[j] : 0;
-      int hit = group_min<PICK>(in && w > 0 && (double)end > want ? id : INT32_MAX, S.redi);
-      if (hit == INT32_MAX) hit = -group_min<PICK>(in && w > 0 ? -id : 1, S.redi);
+      all = 0;
+      for (uint64_t left = __ballot(in); left; left &= left - 1) {
+        const int j = __ffsll((unsigned long long)left) - 1;
+        const u64 x = lane_of(w, j);
+        all += x;
+        end += __builtin_amdgcn_readlane(id, j) <= id ? x : 0;
+      }
+      const double want = u * (double)all;
+      const uint64_t past = __ballot(in && w > 0 && (double)end > want), some = __ballot(in && w > 0);
+      // the lowest id of those past it; roundings next to u = 1: the highest with a weight
+      int hit = past ? INT32_MAX : -1;
+      for (uint64_t left = past ? past : some; left; left &= left - 1) {
+        const int x = __builtin_amdgcn_readlane(id, __ffsll((unsigned long long)left) - 1);
+        hit = past ? min(hit, x) : max(hit, x);
+      }
       if (in && id == hit) answer(id, z_of(p), (double)all / FIXED_ONE);
       return;
     }
@@ -768,7 +857,7 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
       if (n_list <= LIST) {
         for (int i = tid; i < n_list; i += PICK) f(z_of(C.list[i]), id_of(C.list[i]));
       } else {
-        row.tokens(t0, 0, segs, f);
+        row.tokens(active, t0, 0, segs, f);
       }
     };
     const u64 lo = place_of(t0, (1 << ID_BITS) - 1), hi = place_of(row.zmax, 0);
@@ -813,7 +902,7 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
         if (place_of(x, id) >= border) atomicAdd(&C.seg[id / SEG], row.fixed(x));
       });
     } else {
-      row.tokens(t0, s0, s1, [&](float x, int id) {
+      row.tokens(active, t0, s0, s1, [&](float x, int id) {
         if (place_of(x, id) >= border) atomicAdd(&C.seg[id / SEG], row.fixed(x));
       });
     }
