@@ -17,12 +17,14 @@
 // Launches:
 // * scan, a wave four segments of 512 tokens: maximum, and sum of weights with respect to
 //   it; maxima of strips of 64.  It streams the logits once.
-// * only where top-p or min-p may cut a row without top-k: histogram and collect, some
-//   workgroups a row, each a part of it.  The first adds up weights by bins of z; the
-//   second finds the bin in which the border of top-p lies, sums what each part keeps
-//   above it, and lists the tokens in it.
+// * where nothing can be cut: plain, a wave a row.  The segment at which the running sum
+//   passes, then the token.
+// * only where top-p or min-p may cut a row without top-k: rows (a wave a row: its sum, and
+//   the least z that can be kept), bins and collect (some workgroups a row, each a part of
+//   it).  The bins add up weights by z; collect finds the bin in which the border of top-p
+//   lies, sums what each part keeps above it, and lists the tokens in it.
 // * pick, a workgroup a row: the border, then where the running sum passes.
-// The last three look only at segments that can hold kept tokens:
+// All after the scan look only at segments that can hold kept tokens:
 // * weights below 2^-43 of the largest count nothing;
 // * k segments, or strips, with a maximum of t or more hold k tokens of t or more, so the
 //   border of top-k lies there or above;
@@ -41,11 +43,11 @@ typedef unsigned long long u64;
 constexpr int SEG = 512;              // tokens of a segment
 constexpr int MAX_SEGS = 2048;        // of a row: 2^20 tokens
 constexpr int SCAN_WAVES = 4;
-constexpr int PICK = 512;             // threads of a row's pick
+constexpr int PICK = 256;             // threads of a row's pick
 constexpr int PART = 256;             // threads of a part of a row's histogram
-constexpr int BINS = 2 * PICK;        // of z, 16 an octave of weight
+constexpr int BINS = 1024;            // of z, 16 an octave of weight
 constexpr int LIST = 4096;            // tokens that a row's list holds
-constexpr int FEW = 128;              // tokens that are put in order by comparing all of them
+constexpr int FEW = 64;               // tokens that a wave compares with one another
 constexpr int ID_BITS = 20;
 constexpr double LOG2E = 1.4426950408889634;
 constexpr double FIXED_ONE = 4398046511104.0;   // 2^42
@@ -301,98 +303,101 @@ __device__ __forceinline__ int group_min(int v, int* red) {
   for (int i = 0; i < N / 64; ++i) v = min(v, red[i]);
   return v;
 }
+template <typename V>
+__device__ __forceinline__ V wave_prefix(V v) {                      // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const V y = __shfl_up(v, o, 64);
+    if (lane >= o) v += y;
+  }
+  return v;
+}
+template <typename V>
+__device__ __forceinline__ V lane_of(V v, int lane) {
+  const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+  return __builtin_bit_cast(V, u32x2_t{(uint32_t)__builtin_amdgcn_readlane((int)w[0], lane),
+                                       (uint32_t)__builtin_amdgcn_readlane((int)w[1], lane)});
+}
+__device__ __forceinline__ int first_lane(uint64_t mask) { return __ffsll((unsigned long long)mask) - 1; }
+__device__ __forceinline__ int last_lane(uint64_t mask) { return 63 - __clzll((long long)mask); }
 
 // Bin of z, 16 an octave of weight: falls as z grows.
 __device__ __forceinline__ int bin_of(float z, float zmax, float c) {
   return (int)fminf(((zmax - z) * c) * 16.f, (float)(BINS - 1));
 }
 __device__ __forceinline__ float bin_factor(double c) { return (float)fmin(c, 3.0e38); }
+// Weight, or u of it, at which top-p ends: the first token is always kept.
+__device__ __forceinline__ double mass_limit(const RowOpts& o, double all) { return fmax((double)o.top_p * all, 0.5); }
+// Which rows go by histogram: top-k's are few and the pick finds them alone.
+__device__ __forceinline__ bool by_bins(const RowOpts& o) { return o.temperature != 0.0 && !o.by_k && (o.by_p || o.by_min); }
+// min-p's border: the least fp32 value that is not below max z + T ln(min_p).
+__device__ __forceinline__ float min_p_border(const RowOpts& o, float zmax) {
+  const double lowest = (double)zmax + o.temperature * log(fmin(o.min_p, 1.0));
+  const float t = (float)lowest;
+  return (double)t < lowest ? of_key(key_of(t) + 1) : t;
+}
+// Part p of a row's segments: a run of them.
+__device__ __forceinline__ int part_start(int p, int segs, int parts) { return (int)((int64_t)p * segs / parts); }
 
-// What the threads of a row share.
-struct RowMemory {
-  float m[MAX_SEGS];                  // maxima of the segments
-  float share[MAX_SEGS];              // their sums with respect to the row's maximum
-  u64 red[8];
-  int redi[8];
-};
-template <int N>
-struct ActiveMemory {                 // each wave's segments that can hold kept tokens
-  uint16_t seg[N / 64][MAX_SEGS * 64 / N + 1];
-};
-
-// A row as every wave sees it: each reads all of the segments, so that nothing waits for
-// another wave.  Lane l has those numbered l + 64 j, the first REGS in registers.
-template <typename T, bool VEC, int N>
-struct Row {
-  static constexpr int REGS = 5;      // segments of a lane: 163840 tokens
-  const T* z;
-  int vocab, segs;
+// The segments of a row, for one wave: lane l has those numbered l + 64 j, the first REGS
+// in registers, others from memory again and again.
+struct Segments {
+  static constexpr int REGS = 8;      // 262144 tokens
+  const float* top_of;
+  const double* sum_of;
+  int segs;
   float zmax;
   double c, total;
-  RowMemory* S;
-  float m[REGS], share[REGS];
+  float top[REGS];
+  double share[REGS];
 
-  // f(index, maximum, share) for every segment of the lane
+  __device__ __forceinline__ double share_of(float m, double s) const { return m == -INFINITY ? 0.0 : s * weight_of(m, zmax, c); }
+  // f(index, maximum, share) for every segment of the lane, in order; past the last -inf and 0
   template <typename F>
-  __device__ __forceinline__ void each_segment(F f) const {
+  __device__ __forceinline__ void each(F f) const {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int j = 0; j < REGS; ++j)
-      if (64 * j < segs) f(lane + 64 * j, m[j], share[j]);   // past the last: -inf and 0
+      if (64 * j < segs) f(lane + 64 * j, top[j], share[j]);
 #pragma unroll 1
-    for (int i = lane + 64 * REGS; i - lane < segs; i += 64) f(i, i < segs ? S->m[i] : -INFINITY, i < segs ? S->share[i] : 0.f);
+    for (int i = lane + 64 * REGS; i - lane < segs; i += 64) {
+      const float m = i < segs ? top_of[i] : -INFINITY;
+      f(i, m, i < segs ? share_of(m, sum_of[i]) : 0.0);
+    }
   }
-
-  // The row's segments; false where it has no answer.
-  __device__ __forceinline__ bool read(const DrawArgs& A, int r, int n_segs, const RowOpts& o) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    const float* seg_m = A.seg_m + (int64_t)r * n_segs;
-    const double* seg_s = A.seg_s + (int64_t)r * n_segs;
-    z = (const T*)A.logits + r * A.row;
-    vocab = A.vocab;
-    segs = n_segs;
+  // False where the row has no answer.
+  __device__ __forceinline__ bool read(const DrawArgs& A, int r, int n, const RowOpts& o) {
+    const int lane = threadIdx.x & 63;
+    top_of = A.seg_m + (int64_t)r * n;
+    sum_of = A.seg_s + (int64_t)r * n;
+    segs = n;
     c = o.c;
-    double s[REGS];
-    float top = -INFINITY;
+    float m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < REGS; ++j) {
       const int i = lane + 64 * j;
-      m[j] = i < segs ? seg_m[i] : -INFINITY;
-      s[j] = i < segs ? seg_s[i] : 0.0;
+      top[j] = i < segs ? top_of[i] : -INFINITY;
+      share[j] = i < segs ? sum_of[i] : 0.0;
     }
 #pragma unroll
-    for (int j = 0; j < REGS; ++j) top = max_nan(top, m[j]);
+    for (int j = 0; j < REGS; ++j) m = max_nan(m, top[j]);
 #pragma unroll 1
-    for (int i = lane + 64 * REGS; i < segs; i += 64) top = max_nan(top, seg_m[i]);
-    zmax = max_nan_wave(top);
+    for (int i = lane + 64 * REGS; i < segs; i += 64) m = max_nan(m, top_of[i]);
+    zmax = max_nan_wave(m);
     if (!(zmax > -INFINITY && zmax < INFINITY) || !usable(o)) return false;   // NaN too
     double part = 0.0;
 #pragma unroll
-    for (int j = 0; j < REGS; ++j) {
-      const double w = share_of(m[j], s[j]);
-      share[j] = (float)w;
-      part += w;
-      const int i = lane + 64 * j;
-      if (i < segs) {                 // every wave writes the same
-        S->m[i] = m[j];
-        S->share[i] = share[j];
+    for (int j = 0; j < REGS; ++j)
+      if (64 * j < segs) {
+        share[j] = share_of(top[j], share[j]);
+        part += share[j];
       }
-    }
 #pragma unroll 1
-    for (int i = lane + 64 * REGS; i < segs; i += 64) {
-      const double w = share_of(seg_m[i], seg_s[i]);
-      S->m[i] = seg_m[i];
-      S->share[i] = (float)w;
-      part += w;
-    }
+    for (int i = lane + 64 * REGS; i < segs; i += 64) part += share_of(top_of[i], sum_of[i]);
     total = from_63(sum_to_63(part));
     return true;
   }
-  __device__ __forceinline__ double share_of(float top, double s) const {
-    return top == -INFINITY ? 0.0 : s * weight_of(top, zmax, c);
-  }
-  __device__ __forceinline__ u64 fixed(float x) const { return x == -INFINITY ? 0 : fixed_of(weight_of(x, zmax, c)); }
-
   // The least z that can be kept (see above), the octaves that are left halved again and
   // again.  strips (n_strips of them, or none): taken in the place of the segments.
   __device__ __forceinline__ float least(const float* strips, int n_strips, int k, bool by_p, double p) const {
@@ -407,7 +412,7 @@ struct Row {
         if (by_p) {
           const float cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
           float below = 0.f;
-          each_segment([&](int, float top, float part) { below += (zmax - top) * cf <= y ? fminf(part, cap) : part; });
+          each([&](int, float m, double part) { below += (zmax - m) * cf <= y ? fminf((float)part, cap) : (float)part; });
           pass = sum_wave(below) <= spare;
         } else {
           int count = 0;
@@ -416,7 +421,7 @@ struct Row {
             for (int i = lane; i < n_strips; i += 64) count += (zmax - strips[i]) * cf <= y;
             count = wave_sum_dpp(count);
           } else {
-            each_segment([&](int, float top, float) { count += __popcll(__ballot((zmax - top) * cf <= y)); });
+            each([&](int, float m, double) { count += __popcll(__ballot((zmax - m) * cf <= y)); });
           }
           pass = count >= k;
         }
@@ -427,83 +432,224 @@ struct Row {
     const float t = (float)((double)zmax - ((double)hi + 2e-3) / c);
     return t <= -3.4e38f ? -INFINITY : of_key(key_of(t) - 2);   // 2e-3 and two steps: what was rounded on the way
   }
-  // f(z, id) for every token of t0 or more, of segments s0 .. s1 - 1; whole waves call it.
-  // The waves take the segments that have one in turn, four on their way at once.
-  template <typename F>
-  __device__ __forceinline__ void tokens(ActiveMemory<N>& M, float t0, int s0, int s1, F f) const {
+};
+
+// Where f of a row's tokens can be had from: its logits.
+template <typename T, bool VEC>
+struct Logits {
+  const T* z;
+  int vocab;
+  float zmax;
+  double c;
+
+  __device__ __forceinline__ u64 fixed(float x) const { return x == -INFINITY ? 0 : fixed_of(weight_of(x, zmax, c)); }
+  // f(segment, its tokens' z, 8 a lane, the first's id) for the segments s0 .. s1 - 1 that
+  // have a token of t0 or more, by their maxima top_of; called by N threads, whose waves
+  // take them in turn, four on their way at once.
+  template <int N, typename F>
+  __device__ __forceinline__ void segments(uint16_t (&seg)[N / 64][MAX_SEGS * 64 / N + 1], const float* top_of, float t0, int s0,
+                                           int s1, F f) const {
     constexpr int W = N / 64, U = 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     int found = 0;
-    each_segment([&](int i, float top, float) {
-      const bool on = i >= s0 && i < s1 && top >= t0 && top > -INFINITY;
+#pragma unroll 2
+    for (int base = s0; base < s1; base += 64) {
+      const float top = base + lane < s1 ? top_of[base + lane] : -INFINITY;
+      const bool on = top >= t0 && top > -INFINITY;
       const uint64_t mask = __ballot(on);
       const int at = found + __popcll(mask & ((1ull << lane) - 1));
-      if (on && at % W == wave) M.seg[wave][at / W] = (uint16_t)i;
+      if (on && at % W == wave) seg[wave][at / W] = (uint16_t)(base + lane);
       found += __popcll(mask);
-    });
+    }
     const int n = (found - wave + W - 1) / W;
 #pragma unroll 1
     for (int a = 0; a < n; a += U) {
       float v[U][8];
-      int first[U];
+      int s[U];
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        first[j] = a + j < n ? (int)M.seg[wave][a + j] * SEG + 8 * lane : vocab;
-        load8<T, VEC>(z, first[j], vocab, v[j]);
+        s[j] = a + j < n ? __builtin_amdgcn_readfirstlane((int)seg[wave][a + j]) : -1;
+        load8<T, VEC>(z, s[j] < 0 ? vocab : s[j] * SEG + 8 * lane, vocab, v[j]);
       }
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        float top = v[j][0];
+      for (int j = 0; j < U; ++j)
+        if (s[j] >= 0) f(s[j], v[j], s[j] * SEG + 8 * lane);
+    }
+  }
+  // f(z, id) for their tokens of t0 or more.
+  template <int N, typename F>
+  __device__ __forceinline__ void tokens(uint16_t (&seg)[N / 64][MAX_SEGS * 64 / N + 1], const float* top_of, float t0, int s0,
+                                         int s1, F f) const {
+    segments<N>(seg, top_of, t0, s0, s1, [&](int, const float (&v)[8], int first) {
+      float top = v[0];
 #pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, v[j][e]);
-        if (top >= t0 && top > -INFINITY)
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, v[e]);
+      if (top >= t0 && top > -INFINITY)
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (v[j][e] >= t0 && v[j][e] > -INFINITY) f(v[j][e], first[j] + e);   // tokens past the vocabulary are -inf
+        for (int e = 0; e < 8; ++e)
+          if (v[e] >= t0 && v[e] > -INFINITY) f(v[e], first + e);   // tokens past the vocabulary are -inf
+    });
+  }
+  // By one wave: the token of segment s at which the running sum of weigh(z, id), `before` in
+  // front of the segment, passes `want`; the last with a weight where none does.
+  template <typename V, typename W>
+  __device__ __forceinline__ int token_at(int s, V before, double want, W weigh, float& at) const {
+    const int first = s * SEG + 8 * ((int)threadIdx.x & 63);
+    float v[8];
+    load8<T, VEC>(z, first, vocab, v);
+    V w[8], sum = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = first + e < vocab ? weigh(v[e], first + e) : 0;
+      sum += w[e];
+    }
+    V run = wave_prefix(sum) + before - sum;
+    int hit = INT32_MAX, last = -1;
+    float z_hit = 0.f, z_last = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      run += w[e];
+      if (w[e] > 0) {
+        last = first + e;
+        z_last = v[e];
+        if (hit == INT32_MAX && (double)run > want) {
+          hit = first + e;
+          z_hit = v[e];
+        }
       }
     }
+    const uint64_t hits = __ballot(hit != INT32_MAX), lasts = __ballot(last >= 0);
+    const int from = hits ? first_lane(hits) : last_lane(lasts | 1);
+    at = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(hits ? z_hit : z_last), from));
+    return __builtin_amdgcn_readlane(hits ? hit : last, from);
   }
 };
 
-// min-p's border: the least fp32 value that is not below max z + T ln(min_p).
-__device__ __forceinline__ float min_p_border(const RowOpts& o, float zmax) {
-  const double lowest = (double)zmax + o.temperature * log(fmin(o.min_p, 1.0));
-  const float t = (float)lowest;
-  return (double)t < lowest ? of_key(key_of(t) + 1) : t;
+// By one wave: the first of n entries, a lane each in turn, at whose end the running sum of
+// f(entry), `before` in front of them, passes `want`, and the sum in front of it.  Where
+// roundings next to u = 1 leave none: the last that has a weight, and nothing that its
+// tokens could pass.
+template <typename V, typename F>
+__device__ __forceinline__ int entry_at(int n, F f, double& want, V& before) {
+  const int lane = threadIdx.x & 63;
+  int last = 0;
+#pragma unroll 1
+  for (int base = 0; base < n; base += 64) {
+    const V w = base + lane < n ? f(base + lane) : 0;
+    const V end = wave_prefix(w) + before;
+    const uint64_t past = __ballot(w > 0 && (double)end > want), some = __ballot(w > 0);
+    if (past) {
+      const int at = first_lane(past);
+      before = lane_of(end - w, at);
+      return base + at;
+    }
+    if (some) last = base + last_lane(some);
+    before = lane_of(end, 63);
+  }
+  want = INFINITY;
+  return last;
 }
 
-// Which rows go by histogram: top-k's are few and the pick finds them alone.
-__device__ __forceinline__ bool by_bins(const RowOpts& o) { return o.temperature != 0.0 && !o.by_k && (o.by_p || o.by_min); }
+__device__ __forceinline__ double given_u(const DrawArgs& A, int r) {
+  return A.u64 ? ((const double*)A.u)[r] : (double)((const float*)A.u)[r];
+}
+__device__ __forceinline__ void no_answer(const DrawArgs& A, int r) {
+  A.token[r] = -1;
+  A.logprob[r] = A.kept[r] = __uint_as_float(0x7FC00000u);
+}
+__device__ __forceinline__ void answer(const DrawArgs& A, int r, int id, float z, float zmax, double c, double total, double kept) {
+  const double lw = ((double)z - (double)zmax) * c * 0.6931471805599453;
+  A.token[r] = id;
+  A.logprob[r] = (float)(lw - log(total));
+  A.kept[r] = (float)(lw - log(kept));
+}
 
-__device__ __forceinline__ double mass_limit(const RowOpts& o, double all) { return fmax(o.top_p * all, 0.5); }
+// By one wave: a row of which nothing is cut, or all but the first of the largest (T = 0).
+template <typename T, bool VEC>
+__device__ __forceinline__ void draw_plain(const DrawArgs& A, int r, const Segments& S, const Logits<T, VEC>& z, const RowOpts& o,
+                                           double u) {
+  double want = u * S.total, before = 0.0;
+  float at_z;
+  int at = -1, id;
+  if (o.temperature == 0.0) {
+    S.each([&](int i, float m, double) {
+      const uint64_t mask = __ballot(m == S.zmax);
+      if (at < 0 && mask) at = __builtin_amdgcn_readfirstlane(i) + first_lane(mask);
+    });
+    id = z.token_at(at, 0.0, 0.0, [&](float x, int) { return x == S.zmax ? 1.0 : 0.0; }, at_z);
+  } else {
+    int last = 0;
+    S.each([&](int i, float, double w) {
+      if (at >= 0) return;
+      const double end = wave_prefix(w) + before;
+      const uint64_t past = __ballot(w > 0.0 && end > want), some = __ballot(w > 0.0);
+      const int base = __builtin_amdgcn_readfirstlane(i);
+      if (past) {
+        at = base + first_lane(past);
+        before = lane_of(end - w, first_lane(past));
+      } else {
+        if (some) last = base + last_lane(some);
+        before = lane_of(end, 63);
+      }
+    });
+    if (at < 0) {                     // roundings next to u = 1
+      at = last;
+      want = INFINITY;
+    }
+    id = z.token_at(at, before, want, [&](float x, int) { return x == -INFINITY ? 0.0 : weight_of(x, S.zmax, S.c); }, at_z);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    answer(A, r, id, at_z, S.zmax, S.c, S.total, S.total);
+    if (o.temperature == 0.0) A.kept[r] = 0.f;
+  }
+}
 
-// ---------------------------------------------------------------- histogram, collect
-// Part p of a row's segments: a run of them.
-__device__ __forceinline__ int part_start(int p, int segs, int parts) { return (int)((int64_t)p * segs / parts); }
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_draw_plain(DrawArgs A, int segs) {
+  const int r = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
+  if (r >= A.rows) return;
+  const RowOpts o = row_opts(A, r);
+  const double u = given_u(A, r);
+  Segments S;
+  if (!S.read(A, r, segs, o) || !(u >= 0.0 && u < 1.0)) {
+    if ((threadIdx.x & 63) == 0) no_answer(A, r);
+    return;
+  }
+  draw_plain<T, VEC>(A, r, S, Logits<T, VEC>{(const T*)A.logits + r * A.row, A.vocab, S.zmax, S.c}, o, u);
+}
+
+// ---------------------------------------------------------------- rows, bins, collect
+__global__ __launch_bounds__(256) void k_draw_rows(DrawArgs A, int segs) {
+  const int r = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
+  if (r >= A.rows) return;
+  const RowOpts o = row_opts(A, r);
+  if (!by_bins(o)) return;
+  Segments S;
+  const bool good = S.read(A, r, segs, o);
+  float t0 = 0.f;
+  if (good) {
+    t0 = S.least(nullptr, 0, 0, o.by_p, o.top_p);
+    if (o.by_min) t0 = fmaxf(t0, min_p_border(o, S.zmax));
+  }
+  if ((threadIdx.x & 63) == 0) A.info[r] = DrawRow{S.total, S.zmax, t0, good, 0, BINS, 0};
+}
 
 template <typename T, bool VEC>
 __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int parts) {
-  __shared__ RowMemory S;
-  __shared__ ActiveMemory<PART> active;
+  __shared__ uint16_t active[PART / 64][MAX_SEGS * 64 / PART + 1];
   __shared__ u64 mass[BINS];
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
   if (!by_bins(o)) return;
+  const DrawRow info = A.info[r];
+  if (!info.good) return;
   for (int i = tid; i < BINS; i += PART) mass[i] = 0;
-  Row<T, VEC, PART> row{};
-  row.S = &S;
-  const bool good = row.read(A, r, segs, o);
-  float t0 = 0.f;
-  if (good) {
-    t0 = row.least(nullptr, 0, 0, o.by_p, o.top_p);
-    if (o.by_min) t0 = fmaxf(t0, min_p_border(o, row.zmax));
-  }
-  if (part == 0 && tid == 0) A.info[r] = DrawRow{row.total, row.zmax, t0, good, 0, BINS, 0};
-  if (!good) return;
   __syncthreads();
   const float c = bin_factor(o.c);
-  row.tokens(active, t0, part_start(part, segs, parts), part_start(part + 1, segs, parts),
-             [&](float x, int) { atomicAdd(&mass[bin_of(x, row.zmax, c)], row.fixed(x)); });
+  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, info.zmax, o.c};
+  z.template tokens<PART>(active, A.seg_m + (int64_t)r * segs, info.t0, part_start(part, segs, parts),
+                          part_start(part + 1, segs, parts),
+                          [&](float x, int) { atomicAdd(&mass[bin_of(x, info.zmax, c)], z.fixed(x)); });
   __syncthreads();
   u64* bins = A.part_bins + (int64_t)blockIdx.x * BINS;
   for (int i = tid; i < BINS; i += PART) {
@@ -515,6 +661,7 @@ __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int pa
 
 template <typename T, bool VEC>
 __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int parts) {
+  __shared__ uint16_t active[PART / 64][MAX_SEGS * 64 / PART + 1];
   __shared__ u64 red[8], list[LIST];
   __shared__ int redi[8], n_list, at;
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
@@ -524,16 +671,18 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
   if (!info.good) return;
   if (tid == 0) n_list = 0;
   constexpr int PER = BINS / PART;
-  u64 mine[PER], all;
+  u64 mine[PER], own[PER], all, kept = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    mine[i] = A.bins[(int64_t)r * BINS + tid * PER + i];
+    own[i] = A.part_bins[(int64_t)blockIdx.x * BINS + tid * PER + i];
+  }
   int border = BINS;                  // the bin in which top-p's border lies
   if (o.by_p) {
     const double limit = mass_limit(o, info.total * FIXED_ONE);
     u64 sum = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      mine[i] = A.bins[(int64_t)r * BINS + tid * PER + i];
-      sum += mine[i];
-    }
+    for (int i = 0; i < PER; ++i) sum += mine[i];
     u64 end = group_prefix<PART>(sum, red, &all);
     int hit = BINS;
     u64 before = end;
@@ -551,35 +700,23 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
       A.info[r].above = before;
     }
   }
-  // what the part keeps above it
-  u64 kept = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int b = tid * PER + i;
-    if (b < border) kept += A.part_bins[(int64_t)blockIdx.x * BINS + b];
-  }
+  for (int i = 0; i < PER; ++i)
+    if (tid * PER + i < border) kept += own[i];       // what the part keeps above it
   group_prefix<PART>(kept, red, &all);
   if (tid == 0) A.part_kept[blockIdx.x] = all;
   if (border == BINS) return;
-  // the tokens in it
-  const T* z = (const T*)A.logits + r * A.row;
   const float c = bin_factor(o.c);
-  const int lane = tid & 63, s1 = part_start(part + 1, segs, parts);
-#pragma unroll 2
-  for (int s = part_start(part, segs, parts) + (tid >> 6); s < s1; s += PART / 64) {
-    if (A.seg_m[(int64_t)r * segs + s] < info.t0) continue;
-    float v[8];
-    const int i = s * SEG + 8 * lane;
-    load8<T, VEC>(z, i, A.vocab, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (v[e] >= info.t0 && v[e] > -INFINITY && bin_of(v[e], info.zmax, c) == border) {
-        const int k = atomicAdd(&n_list, 1);
-        if (k < LIST) list[k] = place_of(v[e], i + e);
-      }
-  }
+  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, info.zmax, o.c};
+  z.template tokens<PART>(active, A.seg_m + (int64_t)r * segs, info.t0, part_start(part, segs, parts),
+                          part_start(part + 1, segs, parts), [&](float x, int id) {
+                            if (bin_of(x, info.zmax, c) != border) return;
+                            const int k = atomicAdd(&n_list, 1);
+                            if (k < LIST) list[k] = place_of(x, id);
+                          });
   __syncthreads();
   const int n = n_list;
+  if (n == 0) return;
   if (tid == 0) at = atomicAdd(&A.info[r].listed, n);
   __syncthreads();
   for (int i = tid; i < min(n, LIST); i += PART)
@@ -593,18 +730,20 @@ struct CutMemory {
     u64 seg[MAX_SEGS];                // kept weight of each segment
   };
   u64 list[LIST];                     // places of the tokens that can be kept
+  uint16_t active[PICK / 64][MAX_SEGS * 64 / PICK + 1];
   u64 few[FEW], weight[FEW];
-  u64 found, mass, rank;
-  int n_list, n_few;
+  u64 red[8], found, mass, rank, lo, hi;
+  int redi[8], n_list, n_few;
 };
 
-// Of n tokens in C.few, a thread each: how many come before one in the order, and what they weigh.
-__device__ __forceinline__ void compare_few(const CutMemory& C, int n, u64 p, u64& rank, u64& before) {
-#pragma unroll 4
+// By one wave, a token (place p, weight w) in each of the first n lanes: how many of them
+// come before the lane's, and what those weigh.
+__device__ __forceinline__ void compare(int n, u64 p, u64 w, int& rank, u64& before) {
+#pragma unroll 1
   for (int j = 0; j < n; ++j) {
-    const bool in_front = C.few[j] > p;
+    const bool in_front = lane_of(p, j) > p;
     rank += in_front;
-    before += in_front ? C.weight[j] : 0;
+    before += in_front ? lane_of(w, j) : 0;
   }
 }
 
@@ -612,11 +751,12 @@ __device__ __forceinline__ void compare_few(const CutMemory& C, int n, u64 p, u6
 // than `limit` of weight does) among the tokens that `each` gives, n of them, mass0 of
 // weight in front of them, none outside the places lo .. hi: the place of the last that is
 // kept, 0 if all of them are; mass: the weight up to it.  Windows of places, ever finer by
-// 1024, until what is left is few enough to compare with one another.
+// 1024, until a wave can compare what is left.
 template <typename R, typename Each>
 __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Each& each, int n, bool by_rank, double limit, u64 lo,
                                            u64 hi, u64 mass0, u64* mass) {
   const int tid = threadIdx.x;
+  constexpr int PER = BINS / PICK;
   u64 rank0 = 0;                      // before the window
   int inside = n;
   auto reaches = [&](u64 rank, u64 weight) { return by_rank ? (double)rank >= limit : (double)weight >= limit; };
@@ -635,22 +775,35 @@ __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Eac
     });
     __syncthreads();
     // the first digit whose end reaches the limit
-    const u64 m0 = C.bin.mass[2 * tid], m1 = C.bin.mass[2 * tid + 1];
-    const uint32_t n0 = C.bin.count[2 * tid], n1 = C.bin.count[2 * tid + 1];
-    u64 all_m, all_n;
-    const u64 m = group_prefix<PICK>(m0 + m1, row.S->red, &all_m) + mass0;
-    const u64 rank = group_prefix<PICK>((u64)(n0 + n1), row.S->red, &all_n) + rank0;
+    u64 m = 0, rank = 0, all_m, all_n;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      m += C.bin.mass[tid * PER + i];
+      rank += C.bin.count[tid * PER + i];
+    }
+    m = group_prefix<PICK>(m, C.red, &all_m) + mass0;
+    rank = group_prefix<PICK>(rank, C.red, &all_n) + rank0;
     int hit = INT32_MAX;
-    if (n1 && reaches(rank, m)) hit = 2 * tid + 1;
-    if (n0 && reaches(rank - n1, m - m1)) hit = 2 * tid;
-    const int d = group_min<PICK>(hit, row.S->redi);
+    u64 hit_m = 0, hit_n = 0;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i) {
+      const u64 w = C.bin.mass[tid * PER + i], k = C.bin.count[tid * PER + i];
+      if (k && reaches(rank, m)) {
+        hit = tid * PER + i;
+        hit_m = m - w;
+        hit_n = rank - k;
+      }
+      m -= w;
+      rank -= k;
+    }
+    const int d = group_min<PICK>(hit, C.redi);
     if (d == INT32_MAX) {             // the limit lies behind the last token
       *mass = mass0 + all_m;
       return 0;
     }
     if (hit == d) {
-      C.mass = hit & 1 ? m - m1 : m - m1 - m0;
-      C.rank = hit & 1 ? rank - n1 : rank - n1 - n0;
+      C.mass = hit_m;
+      C.rank = hit_n;
     }
     __syncthreads();
     mass0 = C.mass;
@@ -660,7 +813,7 @@ __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Eac
     hi = min(hi, lo + ((1ull << shift) - 1));
   }
   __syncthreads();
-  if (tid == 0) { C.n_few = 0; C.found = 0; C.mass = mass0; }
+  if (tid == 0) C.n_few = 0;
   __syncthreads();
   each([&](float x, int id) {
     const u64 p = place_of(x, id);
@@ -671,16 +824,21 @@ __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Eac
     }
   });
   __syncthreads();
-  inside = C.n_few;
-  if (tid < inside) {
-    u64 before = mass0, rank = rank0;
-    compare_few(C, inside, C.few[tid], rank, before);
-    const u64 end = before + C.weight[tid];
-    if (!reaches(rank, before) && reaches(rank + 1, end)) {
-      C.found = C.few[tid];
-      C.mass = end;
-    } else if (rank + 1 == rank0 + inside && !reaches(rank + 1, end)) {
-      C.mass = end;                   // the limit lies behind the last token
+  if (tid < 64) {
+    const int k = C.n_few;
+    const u64 p = tid < k ? C.few[tid] : 0, w = tid < k ? C.weight[tid] : 0;
+    int rank = 0;
+    u64 before = mass0;
+    compare(k, p, w, rank, before);
+    const uint64_t ends = __ballot(tid < k && !reaches(rank0 + rank, before) && reaches(rank0 + rank + 1, before + w));
+    const u64 all = lane_of(wave_prefix(w), 63);
+    if (tid == 0) {
+      C.found = ends ? 1 : 0;
+      C.mass = mass0 + all;           // the limit lies behind the last token
+    }
+    if (ends && tid == first_lane(ends)) {
+      C.found = p;
+      C.mass = before + w;
     }
   }
   __syncthreads();
@@ -688,235 +846,195 @@ __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Eac
   return C.found;
 }
 
-__device__ __forceinline__ u64 lane_of(u64 v, int lane) {
-  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
-         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
-}
-
-template <typename T, bool VEC, bool CUT>
-__global__ __launch_bounds__(PICK, 4) void k_draw_pick(DrawArgs A, int segs, int parts) {
-  __shared__ RowMemory S;
-  __shared__ ActiveMemory<PICK> active;
-  __shared__ typename std::conditional<CUT, CutMemory, int>::type cut;
-  __shared__ u64 start;
+template <typename T, bool VEC>
+__global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int parts) {
+  __shared__ CutMemory C;
   const int r = blockIdx.x, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
-  const double u = A.u64 ? ((const double*)A.u)[r] : (double)((const float*)A.u)[r];
-  Row<T, VEC, PICK> row{};
-  row.S = &S;
-  if (!row.read(A, r, segs, o) || !(u >= 0.0 && u < 1.0)) {
-    if (tid == 0) {
-      A.token[r] = -1;
-      A.logprob[r] = A.kept[r] = __uint_as_float(0x7FC00000u);
-    }
+  const double u = given_u(A, r);
+  const bool binned = by_bins(o);
+  DrawRow info{};
+  Segments S;
+  float t0 = 0.f;                     // no token below it is kept
+  if (binned) {
+    info = A.info[r];
+    t0 = info.t0;
+    S.segs = segs;
+    S.top_of = A.seg_m + (int64_t)r * segs;
+    S.zmax = info.zmax;
+    S.total = info.total;
+    S.c = o.c;
+  } else {
+    info.good = S.read(A, r, segs, o);   // every wave alike: none waits for another
+  }
+  if (!info.good || !(u >= 0.0 && u < 1.0)) {
+    if (tid == 0) no_answer(A, r);
     return;
   }
-  auto answer = [&](int id, float zi, double kept) {
-    const double lw = ((double)zi - (double)row.zmax) * row.c * 0.6931471805599453;
-    A.token[r] = id;
-    A.logprob[r] = (float)(lw - log(row.total));
-    A.kept[r] = (float)(o.temperature == 0.0 ? 0.0 : lw - log(kept));
-  };
-  static_assert(PICK == SEG, "a thread a token of a segment");
-  auto token = [&](int s) {
-    const int i = s * SEG + tid;
-    return i < A.vocab ? ld_f32<T>(row.z + i) : -INFINITY;
-  };
-  // The token of segment s at which the running sum, `before` in front of the segment,
-  // passes `want`; w is the weight of the thread's token.
-  auto finish = [&](int s, float zi, auto w, auto before, double want, double kept) {
-    decltype(w) all;
-    const auto end = group_prefix<PICK>(w, reinterpret_cast<decltype(w)*>(S.red), &all) + before;
-    int hit = group_min<PICK>(w > 0 && (double)end > want ? tid : INT32_MAX, S.redi);
-    if (hit == INT32_MAX) hit = -group_min<PICK>(w > 0 ? -tid : 1, S.redi);   // roundings next to u = 1: the last with a weight
-    if (tid == hit) answer(s * SEG + tid, zi, kept);
-  };
-  // The first of n entries at whose end the running sum of f(entry) passes `want`, and the
-  // sum in front of it.  Where roundings next to u = 1 leave none: the last that has a
-  // weight, and nothing that its tokens could pass.
-  auto find_entry = [&](int n, auto f, double& want, auto& before) {
-    using V = typename std::remove_reference<decltype(before)>::type;
-    V run = before;
-    int last = 0;
-#pragma unroll 1
-    for (int base = 0; base < n; base += PICK) {
-      const int i = base + tid;
-      const V w = i < n ? f(i) : 0;
-      V all;
-      const V end = group_prefix<PICK>(w, reinterpret_cast<V*>(S.red), &all) + run;
-      const int at = group_min<PICK>(w > 0 && (double)end > want ? i : INT32_MAX, S.redi);
-      if (at != INT32_MAX) {
-        if (i == at) *reinterpret_cast<V*>(&start) = end - w;
-        __syncthreads();
-        before = *reinterpret_cast<V*>(&start);
-        return at;
-      }
-      last = max(last, -group_min<PICK>(w > 0 ? -i : 0, S.redi));
-      run += all;
+  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, S.zmax, S.c};
+  if (!binned && (o.temperature == 0.0 || !o.by_k)) {   // nothing is cut here
+    if (tid < 64) draw_plain<T, VEC>(A, r, S, z, o, u);
+    return;
+  }
+  const float min_z = o.by_min ? min_p_border(o, S.zmax) : -INFINITY;
+  u64 border = o.by_min ? (u64)key_of(min_z) << ID_BITS : 0;
+  const bool whole_list = binned && info.listed <= LIST;   // the border's bin is listed, the rest summed
+  if (!binned) {
+    float* const strips = reinterpret_cast<float*>(C.list);   // where k is too many for the segments
+    int n_strips = 0;
+    if (2 * o.top_k > segs && 4 * segs <= LIST) {
+      n_strips = 8 * segs;
+      for (int i = tid; i < n_strips; i += PICK) strips[i] = A.strip_m[(int64_t)r * n_strips + i];
+      __syncthreads();
     }
-    want = INFINITY;
-    return last;
-  };
+    t0 = S.least(strips, n_strips, o.top_k, false, 1.0);
+    if (!o.by_p) t0 = fmaxf(t0, min_z);                    // top-p takes its share of all the k
+    __syncthreads();
+  }
+  if (tid == 0) {
+    C.n_list = whole_list ? info.listed : 0;
+    C.lo = ~0ull;
+    C.hi = 0;
+  }
+  __syncthreads();
+  if (whole_list) {
+    for (int i = tid; i < info.listed; i += PICK) C.list[i] = A.list[(int64_t)r * LIST + i];
+  } else {
+    z.template tokens<PICK>(C.active, S.top_of, t0, 0, segs, [&](float x, int id) {
+      const int i = atomicAdd(&C.n_list, 1);
+      if (i < LIST) C.list[i] = place_of(x, id);
+    });
+  }
+  __syncthreads();
+  const int n_list = C.n_list;
 
-  __syncthreads();                    // S.m is there
-  if (o.temperature == 0.0) {         // the first of the largest
-    int top = INT32_MAX;
-    for (int i = tid; i < segs; i += PICK)
-      if (S.m[i] == row.zmax) top = min(top, i);
-    top = group_min<PICK>(top, S.redi);
-    const float zi = token(top);
-    const int at = group_min<PICK>(zi == row.zmax ? tid : INT32_MAX, S.redi);
-    if (tid == at) answer(top * SEG + tid, zi, 1.0);
-    return;
-  }
-  if (!CUT || !(o.by_k || o.by_p || o.by_min)) {   // every token can be drawn
-    double before = 0.0, want = u * row.total;
-    const int at = find_entry(segs, [&](int i) { return row.share_of(S.m[i], A.seg_s[(int64_t)r * segs + i]); }, want, before);
-    const float zi = token(at);
-    finish(at, zi, zi == -INFINITY ? 0.0 : weight_of(zi, row.zmax, row.c), before, want, row.total);
-    return;
-  }
-  if constexpr (CUT) {
-    CutMemory& C = *&cut;
-    const float min_z = o.by_min ? min_p_border(o, row.zmax) : -INFINITY;
-    u64 border = o.by_min ? (u64)key_of(min_z) << ID_BITS : 0;
-    float t0;                         // no token below it is kept
-    DrawRow info{};
-    bool binned = by_bins(o);
-    if (binned) {
-      info = A.info[r];
-      binned = info.listed <= LIST;
-      t0 = info.t0;
-    } else {                          // top-p takes its share of all the k
-      float* const strips = reinterpret_cast<float*>(C.list);   // where k is too many for the segments
-      int n_strips = 0;
-      if (o.by_k && 2 * o.top_k > segs && 4 * segs <= LIST) {
-        n_strips = 8 * segs;
-        for (int i = tid; i < n_strips; i += PICK) strips[i] = A.strip_m[(int64_t)r * n_strips + i];
-        __syncthreads();
-      }
-      t0 = row.least(strips, n_strips, o.by_k ? o.top_k : 0, false, 1.0);
-      if (!o.by_p) t0 = fmaxf(t0, min_z);
+  // Few of all that can be kept: a lane each of one wave, compared with one another and
+  // drawn from by their ids.
+  if (!whole_list && n_list <= FEW) {
+    if (tid >= 64) return;
+    const bool is = tid < n_list;
+    const u64 p = is ? C.list[tid] : 0, w = is ? z.fixed(z_of(p)) : 0;
+    const int id = is ? id_of(p) : INT32_MAX;
+    int rank = 0;
+    u64 before = 0, all = 0;
+    compare(n_list, p, w, rank, before);
+    bool in = is && (!o.by_k || rank < o.top_k);
+    if (o.by_p) {
+      const double share = o.by_k ? (double)lane_of(wave_prefix(in ? w : 0), 63) : S.total * FIXED_ONE;
+      in = in && (double)before < mass_limit(o, share);
     }
-    if (tid == 0) C.n_list = 0;
-    __syncthreads();
-    if (binned) {
-      if (tid == 0) C.n_list = info.listed;
-      for (int i = tid; i < info.listed; i += PICK) C.list[i] = A.list[(int64_t)r * LIST + i];
-    } else {
-      row.tokens(active, t0, 0, segs, [&](float x, int id) {
-        const int i = atomicAdd(&C.n_list, 1);
-        if (i < LIST) C.list[i] = place_of(x, id);
-      });
-    }
-    __syncthreads();
-    const int n_list = C.n_list;
-    // Few: a lane each of one wave, compared with one another and drawn from by their ids.
-    if (!binned && n_list <= 64) {
-      if (tid >= 64) return;
-      const bool is = tid < n_list;
-      const u64 p = is ? C.list[tid] : 0, w = is ? row.fixed(z_of(p)) : 0;
-      const int id = is ? id_of(p) : INT32_MAX;
-      u64 before = 0, all = 0;
-      int rank = 0;
-      for (int j = 0; j < n_list; ++j) {
-        const bool in_front = lane_of(p, j) > p;
-        rank += in_front;
-        before += in_front ? lane_of(w, j) : 0;
-      }
-      bool in = is && (!o.by_k || rank < o.top_k);
-      if (o.by_p) {
-        double share = row.total * FIXED_ONE;
-        if (o.by_k) {
-          for (uint64_t left = __ballot(in); left; left &= left - 1) all += lane_of(w, __ffsll((unsigned long long)left) - 1);
-          share = (double)all;
-        }
-        in = in && (double)before < mass_limit(o, share);
-      }
-      in = in && p >= border;
-      u64 end = 0;
-      all = 0;
-      for (uint64_t left = __ballot(in); left; left &= left - 1) {
-        const int j = __ffsll((unsigned long long)left) - 1;
-        const u64 x = lane_of(w, j);
-        all += x;
-        end += __builtin_amdgcn_readlane(id, j) <= id ? x : 0;
-      }
-      const double want = u * (double)all;
-      const uint64_t past = __ballot(in && w > 0 && (double)end > want), some = __ballot(in && w > 0);
-      // the lowest id of those past it; roundings next to u = 1: the highest with a weight
-      int hit = past ? INT32_MAX : -1;
-      for (uint64_t left = past ? past : some; left; left &= left - 1) {
-        const int x = __builtin_amdgcn_readlane(id, __ffsll((unsigned long long)left) - 1);
-        hit = past ? min(hit, x) : max(hit, x);
-      }
-      if (in && id == hit) answer(id, z_of(p), (double)all / FIXED_ONE);
-      return;
-    }
-    auto each = [&](auto f) {
-      if (n_list <= LIST) {
-        for (int i = tid; i < n_list; i += PICK) f(z_of(C.list[i]), id_of(C.list[i]));
-      } else {
-        row.tokens(active, t0, 0, segs, f);
-      }
-    };
-    const u64 lo = place_of(t0, (1 << ID_BITS) - 1), hi = place_of(row.zmax, 0);
-    double share = row.total * FIXED_ONE;
+    in = in && p >= border;
+    u64 end = 0;
 #pragma unroll 1
-    for (int rule = 0; rule < 2; ++rule) {
-      if (rule == 0 ? !o.by_k : !o.by_p || (binned && info.bin == BINS)) continue;
-      u64 mass;
-      border = max(border, find_border(row, C, each, n_list, rule == 0, rule == 0 ? (double)o.top_k : mass_limit(o, share), lo, hi,
-                                       binned ? info.above : 0, &mass));
-      share = (double)mass;
+    for (uint64_t left = __ballot(in); left; left &= left - 1) {
+      const int j = first_lane(left);
+      const u64 x = lane_of(w, j);
+      all += x;
+      end += __builtin_amdgcn_readlane(id, j) <= id ? x : 0;
     }
-    // What is kept of each segment or, where the histogram knows the parts', of each part
-    // and then of that part's segments.
-    __syncthreads();
-    int s0 = 0, s1 = segs;
-    u64 before = 0, mine = 0, kept;
-    double want = 0.0;
-    if (binned) {
-      for (int i = tid; i < parts; i += PICK) C.seg[i] = A.part_kept[(int64_t)r * parts + i];
-      __syncthreads();
-      for (int i = tid; i < n_list; i += PICK)
-        if (C.list[i] >= border) {
-          const int s = id_of(C.list[i]) / SEG;
-          int p = (int)((int64_t)s * parts / segs);
-          while (part_start(p + 1, segs, parts) <= s) ++p;
-          atomicAdd(&C.seg[p], row.fixed(z_of(C.list[i])));
-        }
-      __syncthreads();
-      for (int i = tid; i < parts; i += PICK) mine += C.seg[i];
-      group_prefix<PICK>(mine, S.red, &kept);
-      want = u * (double)kept;
-      const int p = find_entry(parts, [&](int i) { return C.seg[i]; }, want, before);
-      s0 = part_start(p, segs, parts);
-      s1 = part_start(p + 1, segs, parts);
-      __syncthreads();
+    const double want = u * (double)all;
+    const uint64_t past = __ballot(in && w > 0 && (double)end > want), some = __ballot(in && w > 0);
+    // the lowest id of those past it; roundings next to u = 1: the highest with a weight
+    int hit = past ? INT32_MAX : -1;
+#pragma unroll 1
+    for (uint64_t left = past ? past : some; left; left &= left - 1) {
+      const int x = __builtin_amdgcn_readlane(id, first_lane(left));
+      hit = past ? min(hit, x) : max(hit, x);
     }
-    for (int i = tid; i < segs; i += PICK) C.seg[i] = 0;
-    __syncthreads();
-    if (!binned && n_list <= LIST) {
-      each([&](float x, int id) {
-        if (place_of(x, id) >= border) atomicAdd(&C.seg[id / SEG], row.fixed(x));
-      });
-    } else {
-      row.tokens(active, t0, s0, s1, [&](float x, int id) {
-        if (place_of(x, id) >= border) atomicAdd(&C.seg[id / SEG], row.fixed(x));
-      });
-    }
-    __syncthreads();
-    if (!binned) {
-      for (int i = tid; i < segs; i += PICK) mine += C.seg[i];
-      group_prefix<PICK>(mine, S.red, &kept);
-      want = u * (double)kept;
-    }
-    const int at = s0 + find_entry(s1 - s0, [&](int i) { return C.seg[s0 + i]; }, want, before);
-    const float zi = token(at);
-    const int id = at * SEG + tid;
-    finish(at, zi, id < A.vocab && place_of(zi, id) >= border ? row.fixed(zi) : (u64)0, before, want, (double)kept / FIXED_ONE);
+    if (in && id == hit) answer(A, r, id, z_of(p), S.zmax, S.c, S.total, (double)all / FIXED_ONE);
+    return;
   }
+
+  auto each = [&](auto f) {
+    if (n_list <= LIST) {
+      for (int i = tid; i < n_list; i += PICK) f(z_of(C.list[i]), id_of(C.list[i]));
+    } else {
+      z.template tokens<PICK>(C.active, S.top_of, t0, 0, segs, f);
+    }
+  };
+  u64 lo = place_of(t0, (1 << ID_BITS) - 1), hi = place_of(S.zmax, 0);
+  if (n_list <= LIST) {               // no wider than the list is
+    u64 least = ~0ull, most = 0;
+    for (int i = tid; i < n_list; i += PICK) {
+      least = min(least, C.list[i]);
+      most = max(most, C.list[i]);
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) {
+      least = min(least, __shfl_xor(least, x, 64));
+      most = max(most, __shfl_xor(most, x, 64));
+    }
+    if ((tid & 63) == 0) {
+      atomicMin(&C.lo, least);
+      atomicMax(&C.hi, most);
+    }
+    __syncthreads();
+    lo = C.lo;
+    hi = C.hi;
+  }
+  double share = S.total * FIXED_ONE;
+#pragma unroll 1
+  for (int rule = 0; rule < 2; ++rule) {
+    if (rule == 0 ? !o.by_k : !o.by_p || (whole_list && info.bin == BINS)) continue;
+    u64 mass;
+    border = max(border, find_border(z, C, each, n_list, rule == 0, rule == 0 ? (double)o.top_k : mass_limit(o, share), lo, hi,
+                                     whole_list ? info.above : 0, &mass));
+    share = (double)mass;
+  }
+  // What is kept of each segment or, where the histogram knows the parts', of each part
+  // and then of that part's segments.
+  __syncthreads();
+  const int lane = tid & 63;
+  int s0 = 0, s1 = segs;
+  u64 before = 0, kept = 0;
+  double want = 0.0;
+  if (whole_list) {
+    for (int i = tid; i < parts; i += PICK) C.seg[i] = A.part_kept[(int64_t)r * parts + i];
+    __syncthreads();
+    for (int i = tid; i < n_list; i += PICK)
+      if (C.list[i] >= border) {
+        const int s = id_of(C.list[i]) / SEG;
+        int p = (int)((int64_t)s * parts / segs);
+        while (part_start(p + 1, segs, parts) <= s) ++p;
+        atomicAdd(&C.seg[p], z.fixed(z_of(C.list[i])));
+      }
+    __syncthreads();
+    for (int i = lane; i < parts; i += 64) kept += C.seg[i];
+    kept = lane_of(wave_prefix(kept), 63);
+    want = u * (double)kept;
+    const int p = entry_at(parts, [&](int i) { return C.seg[i]; }, want, before);
+    s0 = part_start(p, segs, parts);
+    s1 = part_start(p + 1, segs, parts);
+    __syncthreads();
+  }
+  for (int i = tid; i < segs; i += PICK) C.seg[i] = 0;
+  __syncthreads();
+  if (!whole_list && n_list <= LIST) {
+    each([&](float x, int id) {
+      if (place_of(x, id) >= border) atomicAdd(&C.seg[id / SEG], z.fixed(x));
+    });
+  } else {                            // a segment's tokens add up within their wave
+    z.template segments<PICK>(C.active, S.top_of, t0, s0, s1, [&](int s, const float (&v)[8], int first) {
+      u64 sum = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (v[e] >= t0 && place_of(v[e], first + e) >= border) sum += z.fixed(v[e]);
+#pragma unroll
+      for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, 64);
+      if (lane == 0) C.seg[s] = sum;
+    });
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  if (!whole_list) {
+    for (int i = lane; i < segs; i += 64) kept += C.seg[i];
+    kept = lane_of(wave_prefix(kept), 63);
+    want = u * (double)kept;
+  }
+  const int at = s0 + entry_at(s1 - s0, [&](int i) { return C.seg[s0 + i]; }, want, before);
+  float at_z;
+  const int id = z.token_at(at, before, want, [&](float x, int i) { return place_of(x, i) >= border ? z.fixed(x) : (u64)0; }, at_z);
+  if (lane == 0) answer(A, r, id, at_z, S.zmax, S.c, S.total, (double)kept / FIXED_ONE);
 }
 
 int segments(int vocab) { return (vocab + SEG - 1) / SEG; }
@@ -960,19 +1078,21 @@ hipError_t run(const DrawArgs& a, hipStream_t st) {
   if (items > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((items + SCAN_WAVES - 1) / SCAN_WAVES)), scan(64 * SCAN_WAVES), row(PICK);
   hipError_t e;
+  const dim3 waves((unsigned)((a.rows + 3) / 4)), four(256);
   if (!may_cut(a)) {
     if ((e = kv8_launch(k_draw_scan<T, VEC, false>, grid, scan, st, a, segs, per_row, (unsigned)items)) != hipSuccess) return e;
-    return kv8_launch(k_draw_pick<T, VEC, false>, dim3(a.rows), row, st, a, segs, 0);
+    return kv8_launch(k_draw_plain<T, VEC>, waves, four, st, a, segs);
   }
   if ((e = kv8_launch(k_draw_scan<T, VEC, true>, grid, scan, st, a, segs, per_row, (unsigned)items)) != hipSuccess) return e;
   const int parts = parts_of(a);
   if (a.bins) {
     if ((int64_t)a.rows * parts > INT32_MAX) return hipErrorInvalidValue;
     const dim3 g((unsigned)(a.rows * parts));
+    if ((e = kv8_launch(k_draw_rows, waves, four, st, a, segs)) != hipSuccess) return e;
     if ((e = kv8_launch(k_draw_bins<T, VEC>, g, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
     if ((e = kv8_launch(k_draw_collect<T, VEC>, g, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
   }
-  return kv8_launch(k_draw_pick<T, VEC, true>, dim3(a.rows), row, st, a, segs, parts);
+  return kv8_launch(k_draw_pick<T, VEC>, dim3(a.rows), row, st, a, segs, parts);
 }
 
 }  // namespace
