@@ -10,21 +10,21 @@
 // A vocabulary has as many places where a draw turns on the running sum, so that sums
 // which are 1e-8 off, as those of fp32 weights are, draw another token in one row of a
 // thousand.  Weights are therefore fp64, by a polynomial of their own (exp2_64, 1e-12):
-// 16 instructions a token, which still fit under the bytes of fp32 logits.  Where
+// 14 instructions a token, which still fit under the bytes of fp32 logits.  Where
 // something is cut the weights are whole numbers, w 2^42 to nearest: their sums do not
 // depend on any order, so atomics give the same draw on every run.
 //
 // Launches:
-// * scan, a wave four segments of 512 tokens: maximum, and sum of weights with respect to
-//   it; maxima of strips of 64.  It streams the logits once.
-// * where nothing can be cut: plain, a wave a row.  The segment at which the running sum
-//   passes, then the token.
-// * only where top-p or min-p may cut a row without top-k: rows (a wave a row: its sum, and
-//   the least z that can be kept), bins and collect (some workgroups a row, each a part of
-//   it).  The bins add up weights by z; collect finds the bin in which the border of top-p
-//   lies, sums what each part keeps above it, and lists the tokens in it.
+// * scan, a wave pairs of segments of 512 tokens: maximum, and sum of weights with respect
+//   to it; maxima of strips of 64.  It streams the logits once.
+// * where nothing can be cut: plain, a workgroup a row.  The segment at which the running
+//   sum passes, then the token.
+// * only where top-p or min-p may cut a row without top-k: bins and collect (some workgroups
+//   a row, each a part of it).  The bins find the row's sum and the least z that can be
+//   kept, and add up weights by z; collect finds the bin in which the border of top-p lies,
+//   sums what each part keeps above it, and lists the tokens in it.
 // * pick, a workgroup a row: the border, then where the running sum passes.
-// All after the scan look only at segments that can hold kept tokens:
+// All after the scan look only at strips that can hold kept tokens:
 // * weights below 2^-43 of the largest count nothing;
 // * k segments, or strips, with a maximum of t or more hold k tokens of t or more, so the
 //   border of top-k lies there or above;
@@ -42,12 +42,14 @@ typedef unsigned long long u64;
 
 constexpr int SEG = 512;              // tokens of a segment
 constexpr int MAX_SEGS = 2048;        // of a row: 2^20 tokens
+constexpr int STRIP = 64;              // tokens of a strip
+constexpr int STRIPS = SEG / STRIP;
+constexpr int STEPS = 512;            // that the octaves are told apart in for top-k
 constexpr int SCAN_WAVES = 4;
-constexpr int PICK = 256;             // threads of a row's pick
+constexpr int SCAN_FILL = 32768;        // waves of the scan, where there are segments for so many
 constexpr int PART = 256;             // threads of a part of a row's histogram
 constexpr int BINS = 1024;            // of z, 16 an octave of weight
 constexpr int LIST = 4096;            // tokens that a row's list holds
-constexpr int FEW = 64;               // tokens that a wave compares with one another
 constexpr int ID_BITS = 20;
 constexpr double LOG2E = 1.4426950408889634;
 constexpr double FIXED_ONE = 4398046511104.0;   // 2^42
@@ -99,22 +101,25 @@ struct Exp2 {
       asm("" : "+s"(a[i]));
     }
   }
-  __device__ __forceinline__ double operator()(double t) const {
-    constexpr double shifter = 6755399441055744.0;            // 1.5 * 2^52: the sum's low bits are t to nearest
-    const double s = t + shifter, f = t - (s - shifter);
+  static constexpr double SHIFTER = 6755399441055744.0;       // 1.5 * 2^52: low bits of a sum with it are the other part's, to nearest
+  // 2^f times 2 to the whole number in the low bits of s
+  __device__ __forceinline__ double at(double f, double s) const {
     double p = __builtin_bit_cast(double, a[0]);
 #pragma unroll
     for (int i = 1; i < N; ++i) p = fma(p, f, __builtin_bit_cast(double, a[i]));
     p = fma(p, f, 1.0);
-    u32x2_t w = __builtin_bit_cast(u32x2_t, p);               // n into the exponent: of the high word alone
+    u32x2_t w = __builtin_bit_cast(u32x2_t, p);               // into the exponent: of the high word alone
     w[1] += __builtin_bit_cast(u32x2_t, s)[0] << 20;
     return __builtin_bit_cast(double, w);
   }
+  __device__ __forceinline__ double operator()(double t) const {
+    const double s = t + SHIFTER;
+    return at(t - (s - SHIFTER), s);
+  }
 };
-__device__ __forceinline__ double exp2_64(double t) { return Exp2()(t); }
 // The weight of z with respect to top (finite, no less): octaves below 1000 count nothing.
-__device__ __forceinline__ double weight_of(float z, float top, double c) {
-  return exp2_64(fmax(((double)z - (double)top) * c, -1000.0));
+__device__ __forceinline__ double weight_of(const Exp2& exp2, float z, float top, double c) {
+  return exp2(fmax(((double)z - (double)top) * c, -1000.0));
 }
 // w 2^42 to nearest.
 __device__ __forceinline__ u64 fixed_of(double w) {
@@ -124,27 +129,13 @@ __device__ __forceinline__ u64 fixed_of(double w) {
 // NaN where either is.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// The wave's sum, in lane 63 alone: lanes past a row's end, and rows without a source, add
-// 0; what the middle rows take in twice never gets there.
+// Another lane's value, for sums of which the last lane of some alone is of use: past a
+// row's end, and for rows without a source, 0.
 template <int CTRL>
 __device__ __forceinline__ double moved(double v) {
   const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
   return __builtin_bit_cast(double, u32x2_t{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, 0xf, 0xf, true),
                                             (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, 0xf, 0xf, true)});
-}
-__device__ __forceinline__ double sum_to_63(double v) {
-  v += moved<0x111>(v);               // row_shr 1, 2, 4, 8, then row_bcast 15 and 31
-  v += moved<0x112>(v);
-  v += moved<0x114>(v);
-  v += moved<0x118>(v);
-  v += moved<0x142>(v);
-  v += moved<0x143>(v);
-  return v;
-}
-__device__ __forceinline__ double from_63(double v) {
-  const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
-  return __builtin_bit_cast(double, u32x2_t{(uint32_t)__builtin_amdgcn_readlane((int)w[0], 63),
-                                            (uint32_t)__builtin_amdgcn_readlane((int)w[1], 63)});
 }
 // Maxima over lanes go by whole numbers in the order of z, NaN above all: one lane move
 // and comparison a step.
@@ -169,90 +160,155 @@ __device__ __forceinline__ float max_nan_wave(float z) {
   v = max_moved<0x143>(v);
   return of_rank(__builtin_amdgcn_readlane(v, 63));
 }
-__device__ __forceinline__ float sum_wave(float v) { return (float)from_63(sum_to_63((double)v)); }
-
+// Eight tokens of a row from the i-th on; -inf past its end.
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int i, int n, float (&v)[8]) {
-  if (VEC && i + 8 <= n) {
-    ld_elems<8, true>(p + i, v);
-  } else {
+struct Eight {
+  typedef T vec __attribute__((ext_vector_type(8), aligned(16)));
+  vec t;
+  __device__ __forceinline__ void load_whole(const T* p) { t = *reinterpret_cast<const vec*>(p); }
+  __device__ __forceinline__ void load(const T* p, int i, int n) {
+    t = (vec)(sizeof(T) == 2 ? (T)0xFF80 : (T)-INFINITY);
+    if (i >= n) return;
+    if (VEC && i + 8 <= n) {
+      t = *reinterpret_cast<const vec*>(p + i);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = i + e < n ? ld_f32<T>(p + i + e) : -INFINITY;
+      for (int e = 0; e < 8; ++e)
+        if (i + e < n) t[e] = p[i + e];
+    }
   }
+  __device__ __forceinline__ float operator[](int e) const {
+    const T x = t[e];
+    return ld_f32<T>(&x);
+  }
+};
+
+// Where 2^(z c) of a segment's tokens is not out of all bounds, their weights are taken with
+// respect to the whole octave next to the maximum's m c, else to m itself.
+__device__ __forceinline__ bool by_octave(float m, double c) { return fabs((double)m * c) < 1024.0 && c > 1e-30 && fabsf(m) < 1e38f; }
+// A segment's weight with respect to the row's maximum.
+__device__ __forceinline__ double share_of(const Exp2& exp2, float m, double s, float zmax, double c) {
+  if (m == -INFINITY) return 0.0;
+  const double t = by_octave(m, c) ? fma(-(double)zmax, c, rint((double)m * c)) : ((double)m - (double)zmax) * c;
+  return s * exp2(fmax(t, -1000.0));
 }
 
 // ---------------------------------------------------------------- scan
-// Four segments a wave: their loads are on their way together, and the lane moves of one
-// fill the waits of another.
+// A wave goes through `per` pairs of segments, the next pair on its way all the time.  The
+// code is kept small here and below: each kernel starts with none of it in the instruction
+// cache, and lines that are run once cost more than what is in them.
 template <typename T, bool VEC, bool CUT>
-__global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int segs, unsigned per_row, unsigned items) {
-  constexpr int U = 4;
+__global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int segs, unsigned per_row, unsigned items, unsigned per) {
   const int lane = threadIdx.x & 63;
-  const unsigned item = blockIdx.x * SCAN_WAVES + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  unsigned item = (blockIdx.x * SCAN_WAVES + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * per;
   if (item >= items) return;
-  const unsigned r = item / per_row;
-  const int s0 = (int)(item - r * per_row) * U;
+  const unsigned end = min(items, item + per);
+  unsigned r = item / per_row;
+  int s = (int)(item - r * per_row) * 2;
   const T* z = (const T*)A.logits + r * A.row;
-  float v[U][8], m[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) load8<T, VEC>(z, (s0 + j) * SEG + 8 * lane, A.vocab, v[j]);
-  const double c = octaves_per_logit(A, r);
-  int rank[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    float top = v[j][0];
-#pragma unroll
-    for (int e = 1; e < 8; ++e) top = max_nan(top, v[j][e]);
-    rank[j] = rank_of(top);
-  }
-  auto step = [&](auto ctrl) {
-#pragma unroll
-    for (int j = 0; j < U; ++j) rank[j] = max_moved<decltype(ctrl)::value>(rank[j]);
-  };
-  step(std::integral_constant<int, 0x111>{});
-  step(std::integral_constant<int, 0x112>{});
-  step(std::integral_constant<int, 0x114>{});
-  if constexpr (CUT) {                            // lanes 7, 15, ..: of eight lanes
-#pragma unroll
-    for (int j = 0; j < U; ++j)
-      if ((lane & 7) == 7 && s0 + j < segs) A.strip_m[((int64_t)r * segs + s0 + j) * 8 + (lane >> 3)] = of_rank(rank[j]);
-  }
-  step(std::integral_constant<int, 0x118>{});
-  step(std::integral_constant<int, 0x142>{});
-  step(std::integral_constant<int, 0x143>{});
-  bool plain = true;                              // finite maxima, z c - m c good to 2^-44
-  double mc[U], s[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    m[j] = of_rank(__builtin_amdgcn_readlane(rank[j], 63));
-    mc[j] = (double)m[j] * c;
-    plain = plain && fabs(mc[j]) < 1024.0;
-    s[j] = 0.0;
-  }
   const Exp2 exp2;
-  if (plain) {
-#pragma unroll
-    for (int j = 0; j < U; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[j] += exp2(fmax(fma((double)v[j][e], c, -mc[j]), -1000.0));
-  } else {
-#pragma unroll
-    for (int j = 0; j < U; ++j)
-      if (m[j] > -INFINITY && m[j] < INFINITY)    // else the sum is not looked at, or nothing
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[j] += weight_of(v[j][e], m[j], c);
-  }
-#pragma unroll
-  for (int j = 0; j < U; ++j) s[j] = sum_to_63(s[j]);
-#pragma unroll
-  for (int j = 0; j < U; ++j)
-    if (lane == 63 && s0 + j < segs) {
-      A.seg_m[(int64_t)r * segs + s0 + j] = m[j];
-      A.seg_s[(int64_t)r * segs + s0 + j] = s[j];
+  double c = octaves_per_logit(A, r);
+#pragma unroll 1
+  for (;;) {
+    Eight<T, VEC> v[2];
+    const int64_t at = (int64_t)r * segs + s;
+    if (VEC && (s + 2) * SEG <= A.vocab) {
+      v[0].load_whole(z + s * SEG + 8 * lane);
+      v[1].load_whole(z + (s + 1) * SEG + 8 * lane);
+    } else {
+      v[0].load(z, s * SEG + 8 * lane, A.vocab);
+      v[1].load(z, (s + 1) * SEG + 8 * lane, A.vocab);
     }
-  if (CUT && A.bins) {                            // the histogram begins empty
-    const int per = (BINS + (int)per_row - 1) / (int)per_row, b0 = s0 / U * per;
-    for (int i = b0 + lane; i < min(b0 + per, BINS); i += 64) A.bins[(int64_t)r * BINS + i] = 0;
+    int rank[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float top = v[j][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = max_nan(top, v[j][e]);
+      rank[j] = rank_of(top);
+    }
+    auto step = [&](auto ctrl) {
+      rank[0] = max_moved<decltype(ctrl)::value>(rank[0]);
+      rank[1] = max_moved<decltype(ctrl)::value>(rank[1]);
+    };
+    if constexpr (CUT) {                          // of eight lanes, in lanes 7, 15, ..
+      step(std::integral_constant<int, 0x111>{});
+      step(std::integral_constant<int, 0x112>{});
+      step(std::integral_constant<int, 0x114>{});
+      if ((lane & 7) == 7) {
+        float* strip = A.strip_m + at * STRIPS + (lane >> 3);
+        strip[0] = of_rank(rank[0]);
+        if (s + 1 < segs) strip[STRIPS] = of_rank(rank[1]);
+      }
+    }
+    // the halves of the wave take a segment each
+    auto swapped = __builtin_amdgcn_permlane32_swap((uint32_t)rank[0], (uint32_t)rank[1], false, false);
+    int both = max((int)swapped[0], (int)swapped[1]);
+    if constexpr (!CUT) {
+      both = max_moved<0x111>(both);
+      both = max_moved<0x112>(both);
+      both = max_moved<0x114>(both);
+    }
+    both = max_moved<0x118>(both);
+    both = max_moved<0x142>(both);
+    float m[2] = {of_rank(__builtin_amdgcn_readlane(both, 31)), of_rank(__builtin_amdgcn_readlane(both, 63))};
+    if (s + 1 >= segs) m[1] = m[0];
+    double sum[2] = {0.0, 0.0};
+    if (by_octave(m[0], c) && by_octave(m[1], c)) {
+      // z c, and the whole octave next to it in the low bits of s; where z is 1000 octaves
+      // down already it goes no further
+      const float reach = 1000.f * __builtin_amdgcn_rcpf((float)c);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float least = m[j] - reach;
+        const double shifter = Exp2::SHIFTER - rint((double)m[j] * c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const double x = (double)__builtin_amdgcn_fmed3f(v[j][e], least, 3.0e38f), n = fma(x, c, shifter);
+          sum[j] += exp2.at(fma(x, c, shifter - n), n);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (m[j] > -INFINITY && m[j] < INFINITY) {   // else the sum is not looked at, or nothing
+          const bool octave = by_octave(m[j], c);
+          const double top = rint((double)m[j] * c);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const double z = (double)v[j][e], t = octave ? fma(z, c, -top) : (z - (double)m[j]) * c;
+            sum[j] += exp2(fmax(t, -1000.0));
+          }
+        }
+    }
+    const u32x2_t a = __builtin_bit_cast(u32x2_t, sum[0]), b = __builtin_bit_cast(u32x2_t, sum[1]);
+    const auto low = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
+    const auto high = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+    double all = __builtin_bit_cast(double, u32x2_t{low[0], high[0]}) + __builtin_bit_cast(double, u32x2_t{low[1], high[1]});
+    all += moved<0x111>(all);
+    all += moved<0x112>(all);
+    all += moved<0x114>(all);
+    all += moved<0x118>(all);
+    all += moved<0x142>(all);
+    const int half = lane >> 5;
+    if ((lane & 31) == 31 && s + half < segs) {
+      A.seg_m[at + half] = half ? m[1] : m[0];
+      A.seg_s[at + half] = all;
+    }
+    if (CUT && A.bins) {                          // the histogram begins empty
+      const int share = (BINS + (int)per_row - 1) / (int)per_row, b0 = s / 2 * share;
+      u64* bins = A.bins + (at - s) / segs * BINS;
+#pragma unroll 1
+      for (int i = b0 + lane; i < min(b0 + share, BINS); i += 64) bins[i] = 0;
+    }
+    if (++item == end) return;
+    s += 2;
+    if (s >= segs) {
+      s = 0;
+      ++r;
+      z += A.row;
+      c = octaves_per_logit(A, r);
+    }
   }
 }
 
@@ -263,22 +319,52 @@ __device__ __forceinline__ uint32_t key_of(float z) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
-// A token's place in the order, its own: a larger one comes first.
-__device__ __forceinline__ u64 place_of(float z, int id) {
-  return (u64)key_of(z) << ID_BITS | (uint32_t)((1 << ID_BITS) - 1 - id);
-}
-__device__ __forceinline__ float z_of(u64 place) { return of_key((uint32_t)(place >> ID_BITS)); }
-__device__ __forceinline__ int id_of(u64 place) { return (1 << ID_BITS) - 1 - (int)(place & ((1 << ID_BITS) - 1)); }
+// A token's place in the order, its own: a larger one comes first.  bf16's are 36 bits
+// wide, so that few distinct values with many ids each do not leave most windows empty.
+template <typename T>
+struct Places {
+  static constexpr int DROP = sizeof(T) == 2 ? 16 : 0;
+  static __device__ __forceinline__ u64 of(float z, int id) {
+    return (u64)(key_of(z) >> DROP) << ID_BITS | (uint32_t)((1 << ID_BITS) - 1 - id);
+  }
+  static __device__ __forceinline__ float z(u64 place) {
+    const uint32_t k = (uint32_t)(place >> ID_BITS) << DROP;
+    return of_key(DROP && !(k & 0x80000000u) ? k | 0xFFFFu : k);
+  }
+  static __device__ __forceinline__ int id(u64 place) { return (1 << ID_BITS) - 1 - (int)(place & ((1 << ID_BITS) - 1)); }
+  // the lowest of a z that is not below t
+  static __device__ __forceinline__ u64 from(float t) {
+    const u64 p = (u64)(key_of(t) >> DROP) << ID_BITS;
+    return z(p) < t ? p + (1ull << ID_BITS) : p;
+  }
+};
 
+// A value of another lane, 0 where there is none or the lane's row of 16 is not in ROWS.
+template <int CTRL, int ROWS, typename V>
+__device__ __forceinline__ V shifted(V v) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, true));
+  } else {
+    const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+    return __builtin_bit_cast(V, u32x2_t{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, ROWS, 0xF, true),
+                                         (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, ROWS, 0xF, true)});
+  }
+}
+template <typename V>
+__device__ __forceinline__ V wave_prefix(V v) {                      // inclusive
+  v += shifted<0x111, 0xF>(v);
+  v += shifted<0x112, 0xF>(v);
+  v += shifted<0x114, 0xF>(v);
+  v += shifted<0x118, 0xF>(v);
+  v += shifted<0x142, 0xA>(v);
+  v += shifted<0x143, 0xC>(v);
+  return v;
+}
 // Over a workgroup of N threads; `red` holds a value a wave.
 template <int N, typename V>
 __device__ __forceinline__ V group_prefix(V v, V* red, V* total) {   // inclusive
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const V y = __shfl_up(v, o, 64);
-    if (lane >= o) v += y;
-  }
+  v = wave_prefix(v);
   __syncthreads();
   if (lane == 63) red[w] = v;
   __syncthreads();
@@ -294,23 +380,19 @@ __device__ __forceinline__ V group_prefix(V v, V* red, V* total) {   // inclusiv
 template <int N>
 __device__ __forceinline__ int group_min(int v, int* red) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+  v = -v;
+  v = max_moved<0x111>(v);
+  v = max_moved<0x112>(v);
+  v = max_moved<0x114>(v);
+  v = max_moved<0x118>(v);
+  v = max_moved<0x142>(v);
+  v = max_moved<0x143>(v);
   __syncthreads();
-  if (lane == 0) red[w] = v;
+  if (lane == 63) red[w] = -v;
   __syncthreads();
+  v = red[0];
 #pragma unroll
-  for (int i = 0; i < N / 64; ++i) v = min(v, red[i]);
-  return v;
-}
-template <typename V>
-__device__ __forceinline__ V wave_prefix(V v) {                      // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const V y = __shfl_up(v, o, 64);
-    if (lane >= o) v += y;
-  }
+  for (int i = 1; i < N / 64; ++i) v = min(v, red[i]);
   return v;
 }
 template <typename V>
@@ -340,190 +422,110 @@ __device__ __forceinline__ float min_p_border(const RowOpts& o, float zmax) {
 // Part p of a row's segments: a run of them.
 __device__ __forceinline__ int part_start(int p, int segs, int parts) { return (int)((int64_t)p * segs / parts); }
 
-// The segments of a row, for one wave: lane l has those numbered l + 64 j, the first REGS
-// in registers, others from memory again and again.
-struct Segments {
-  static constexpr int REGS = 8;      // 262144 tokens
-  const float* top_of;
-  const double* sum_of;
-  int segs;
-  float zmax;
-  double c, total;
-  float top[REGS];
-  double share[REGS];
+// z that many octaves of weight below the largest, a little lower for what was rounded on
+// the way.
+__device__ __forceinline__ float octaves_below(float zmax, float octaves, double c) {
+  const float t = (float)((double)zmax - ((double)octaves + 2e-3) / c);
+  return t <= -3.4e38f ? -INFINITY : of_key(key_of(t) - 2);
+}
 
-  __device__ __forceinline__ double share_of(float m, double s) const { return m == -INFINITY ? 0.0 : s * weight_of(m, zmax, c); }
-  // f(index, maximum, share) for every segment of the lane, in order; past the last -inf and 0
-  template <typename F>
-  __device__ __forceinline__ void each(F f) const {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int j = 0; j < REGS; ++j)
-      if (64 * j < segs) f(lane + 64 * j, top[j], share[j]);
-#pragma unroll 1
-    for (int i = lane + 64 * REGS; i - lane < segs; i += 64) {
-      const float m = i < segs ? top_of[i] : -INFINITY;
-      f(i, m, i < segs ? share_of(m, sum_of[i]) : 0.0);
-    }
-  }
-  // False where the row has no answer.
-  __device__ __forceinline__ bool read(const DrawArgs& A, int r, int n, const RowOpts& o) {
-    const int lane = threadIdx.x & 63;
-    top_of = A.seg_m + (int64_t)r * n;
-    sum_of = A.seg_s + (int64_t)r * n;
-    segs = n;
-    c = o.c;
-    float m = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < REGS; ++j) {
-      const int i = lane + 64 * j;
-      top[j] = i < segs ? top_of[i] : -INFINITY;
-      share[j] = i < segs ? sum_of[i] : 0.0;
-    }
-#pragma unroll
-    for (int j = 0; j < REGS; ++j) m = max_nan(m, top[j]);
-#pragma unroll 1
-    for (int i = lane + 64 * REGS; i < segs; i += 64) m = max_nan(m, top_of[i]);
-    zmax = max_nan_wave(m);
-    if (!(zmax > -INFINITY && zmax < INFINITY) || !usable(o)) return false;   // NaN too
-    double part = 0.0;
-#pragma unroll
-    for (int j = 0; j < REGS; ++j)
-      if (64 * j < segs) {
-        share[j] = share_of(top[j], share[j]);
-        part += share[j];
-      }
-#pragma unroll 1
-    for (int i = lane + 64 * REGS; i < segs; i += 64) part += share_of(top_of[i], sum_of[i]);
-    total = from_63(sum_to_63(part));
-    return true;
-  }
-  // The least z that can be kept (see above), the octaves that are left halved again and
-  // again.  strips (n_strips of them, or none): taken in the place of the segments.
-  __device__ __forceinline__ float least(const float* strips, int n_strips, int k, bool by_p, double p) const {
-    const int lane = threadIdx.x & 63;
-    float lo = 0.f, hi = FIXED_OCTAVES;
-    if (by_p || (k > 0 && k <= max(n_strips, segs))) {
-      const float spare = (float)((1.0 - fmax(p, 0.0)) * total * (1.0 - 1e-5)), cf = bin_factor(c);
-#pragma unroll 1
-      for (int round = 0; round < 8; ++round) {
-        const float y = 0.5f * (lo + hi);
-        bool pass;
-        if (by_p) {
-          const float cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
-          float below = 0.f;
-          each([&](int, float m, double part) { below += (zmax - m) * cf <= y ? fminf((float)part, cap) : (float)part; });
-          pass = sum_wave(below) <= spare;
-        } else {
-          int count = 0;
-          if (n_strips) {
-#pragma unroll 4
-            for (int i = lane; i < n_strips; i += 64) count += (zmax - strips[i]) * cf <= y;
-            count = wave_sum_dpp(count);
-          } else {
-            each([&](int, float m, double) { count += __popcll(__ballot((zmax - m) * cf <= y)); });
-          }
-          pass = count >= k;
-        }
-        if (pass) hi = y;
-        else lo = y;
-      }
-    }
-    const float t = (float)((double)zmax - ((double)hi + 2e-3) / c);
-    return t <= -3.4e38f ? -INFINITY : of_key(key_of(t) - 2);   // 2e-3 and two steps: what was rounded on the way
-  }
+// What the scan knows of a row, put together by a workgroup of N threads.
+struct Row {
+  float zmax;
+  double total;
+  bool good;                          // whether it has an answer
 };
-
-// Where f of a row's tokens can be had from: its logits.
-template <typename T, bool VEC>
-struct Logits {
-  const T* z;
-  int vocab;
-  float zmax;
-  double c;
-
-  __device__ __forceinline__ u64 fixed(float x) const { return x == -INFINITY ? 0 : fixed_of(weight_of(x, zmax, c)); }
-  // f(segment, its tokens' z, 8 a lane, the first's id) for the segments s0 .. s1 - 1 that
-  // have a token of t0 or more, by their maxima top_of; called by N threads, whose waves
-  // take them in turn, four on their way at once.
-  template <int N, typename F>
-  __device__ __forceinline__ void segments(uint16_t (&seg)[N / 64][MAX_SEGS * 64 / N + 1], const float* top_of, float t0, int s0,
-                                           int s1, F f) const {
-    constexpr int W = N / 64, U = 4;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    int found = 0;
+template <int N>
+__device__ __forceinline__ Row read_row(const DrawArgs& A, const Exp2& exp2, int r, int segs, const RowOpts& o, double* red, int* redi) {
+  const float* top = A.seg_m + (int64_t)r * segs;
+  const double* sum = A.seg_s + (int64_t)r * segs;
+  const int tid = threadIdx.x;
+  int most = rank_of(-INFINITY);
 #pragma unroll 2
-    for (int base = s0; base < s1; base += 64) {
-      const float top = base + lane < s1 ? top_of[base + lane] : -INFINITY;
-      const bool on = top >= t0 && top > -INFINITY;
-      const uint64_t mask = __ballot(on);
-      const int at = found + __popcll(mask & ((1ull << lane) - 1));
-      if (on && at % W == wave) seg[wave][at / W] = (uint16_t)(base + lane);
-      found += __popcll(mask);
-    }
-    const int n = (found - wave + W - 1) / W;
+  for (int i = tid; i < segs; i += N) most = max(most, rank_of(top[i]));
+  Row w;
+  w.zmax = of_rank(-group_min<N>(-most, redi));
+  w.total = 0.0;
+  w.good = w.zmax > -INFINITY && w.zmax < INFINITY && usable(o);     // NaN too is none
+  if (!w.good) return w;
+  double part = 0.0;
 #pragma unroll 1
-    for (int a = 0; a < n; a += U) {
-      float v[U][8];
-      int s[U];
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        s[j] = a + j < n ? __builtin_amdgcn_readfirstlane((int)seg[wave][a + j]) : -1;
-        load8<T, VEC>(z, s[j] < 0 ? vocab : s[j] * SEG + 8 * lane, vocab, v[j]);
-      }
-#pragma unroll
-      for (int j = 0; j < U; ++j)
-        if (s[j] >= 0) f(s[j], v[j], s[j] * SEG + 8 * lane);
-    }
-  }
-  // f(z, id) for their tokens of t0 or more.
-  template <int N, typename F>
-  __device__ __forceinline__ void tokens(uint16_t (&seg)[N / 64][MAX_SEGS * 64 / N + 1], const float* top_of, float t0, int s0,
-                                         int s1, F f) const {
-    segments<N>(seg, top_of, t0, s0, s1, [&](int, const float (&v)[8], int first) {
-      float top = v[0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, v[e]);
-      if (top >= t0 && top > -INFINITY)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (v[e] >= t0 && v[e] > -INFINITY) f(v[e], first + e);   // tokens past the vocabulary are -inf
-    });
-  }
-  // By one wave: the token of segment s at which the running sum of weigh(z, id), `before` in
-  // front of the segment, passes `want`; the last with a weight where none does.
-  template <typename V, typename W>
-  __device__ __forceinline__ int token_at(int s, V before, double want, W weigh, float& at) const {
-    const int first = s * SEG + 8 * ((int)threadIdx.x & 63);
-    float v[8];
-    load8<T, VEC>(z, first, vocab, v);
-    V w[8], sum = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      w[e] = first + e < vocab ? weigh(v[e], first + e) : 0;
-      sum += w[e];
-    }
-    V run = wave_prefix(sum) + before - sum;
-    int hit = INT32_MAX, last = -1;
-    float z_hit = 0.f, z_last = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      run += w[e];
-      if (w[e] > 0) {
-        last = first + e;
-        z_last = v[e];
-        if (hit == INT32_MAX && (double)run > want) {
-          hit = first + e;
-          z_hit = v[e];
-        }
-      }
-    }
-    const uint64_t hits = __ballot(hit != INT32_MAX), lasts = __ballot(last >= 0);
-    const int from = hits ? first_lane(hits) : last_lane(lasts | 1);
-    at = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(hits ? z_hit : z_last), from));
-    return __builtin_amdgcn_readlane(hits ? hit : last, from);
-  }
+  for (int i = tid; i < segs; i += N) part += share_of(exp2, top[i], sum[i], w.zmax, o.c);
+  group_prefix<N>(part, red, &w.total);
+  return w;
+}
+
+// The least z that top-p can keep (see above): every wave of the workgroup tries another
+// distance from the top, in octaves, and what is left between two of them is tried again.
+struct MassMemory {
+  float share[MAX_SEGS], down[MAX_SEGS];
+  int pass[4];
 };
+template <int N>
+__device__ __forceinline__ float least_of_mass(const DrawArgs& A, const Exp2& exp2, int r, int segs, const RowOpts& o, const Row& w,
+                                               MassMemory& M) {
+  constexpr int W = N / 64;
+  static_assert(W <= 4, "a flag a wave");
+  const float* top = A.seg_m + (int64_t)r * segs;
+  const double* sum = A.seg_s + (int64_t)r * segs;
+  const float cf = bin_factor(o.c);
+  const double spare = (1.0 - fmax(o.top_p, 0.0)) * w.total * (1.0 - 1e-5);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float lo = 0.f, hi = FIXED_OCTAVES;
+#pragma unroll 1
+  for (int i = tid; i < segs; i += N) {
+    M.share[i] = (float)share_of(exp2, top[i], sum[i], w.zmax, o.c);
+    M.down[i] = (w.zmax - top[i]) * cf;
+  }
+#pragma unroll 1
+  for (int round = 0; round < 4; ++round) {
+    __syncthreads();
+    const float step = (hi - lo) * (1.f / (W + 1)), y = lo + step * (float)(wave + 1), cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
+    double below = 0.0;
+#pragma unroll 2
+    for (int i = lane; i < segs; i += 64) below += M.down[i] <= y ? fminf(M.share[i], cap) : M.share[i];
+    below = lane_of(wave_prefix(below), 63);
+    if (lane == 0) M.pass[wave] = below <= spare;
+    __syncthreads();
+    int first = W;
+#pragma unroll
+    for (int i = W - 1; i >= 0; --i) first = M.pass[i] ? i : first;
+    if (first < W) hi = lo + step * (float)(first + 1);
+    lo += step * (float)first;
+  }
+  return octaves_below(w.zmax, hi, o.c);
+}
+
+// The least z that top-k can keep: k of the n maxima `of` (segments' or strips') reach it.
+// By a workgroup of N threads, which counts them by their distance from the top.
+template <int N>
+__device__ __forceinline__ float least_of(const float* of, int n, int k, float zmax, double c, uint32_t (&count)[STEPS], int* red) {
+  constexpr int PER = STEPS > N ? STEPS / N : 1;
+  const int tid = threadIdx.x;
+  const float cf = bin_factor(c);
+  if (k > n) return octaves_below(zmax, FIXED_OCTAVES, c);
+  for (int i = tid; i < STEPS; i += N) count[i] = 0;
+  __syncthreads();
+#pragma unroll 4
+  for (int i = tid; i < n; i += N) {
+    const float step = (zmax - of[i]) * cf * (STEPS / FIXED_OCTAVES);
+    if (step < (float)STEPS) atomicAdd(&count[(int)step], 1u);
+  }
+  __syncthreads();
+  uint32_t sum = 0, all;
+  if (tid * PER < STEPS)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += count[tid * PER + i];
+  sum = group_prefix<N>(sum, (uint32_t*)red, &all);
+  int hit = STEPS - 1;
+#pragma unroll
+  for (int i = PER - 1; i >= 0; --i)
+    if (tid * PER < STEPS) {
+      if (sum >= (uint32_t)k) hit = tid * PER + i;
+      sum -= count[tid * PER + i];
+    }
+  return octaves_below(zmax, (float)(group_min<N>(hit, red) + 1) * (FIXED_OCTAVES / STEPS), c);
+}
 
 // By one wave: the first of n entries, a lane each in turn, at whose end the running sum of
 // f(entry), `before` in front of them, passes `want`, and the sum in front of it.  Where
@@ -550,6 +552,109 @@ __device__ __forceinline__ int entry_at(int n, F f, double& want, V& before) {
   return last;
 }
 
+// Where f of a row's tokens can be had from: its logits.
+template <typename T, bool VEC>
+struct Logits {
+  const T* z;
+  int vocab;
+  float zmax;
+  double c;
+  const Exp2& exp2;
+
+  __device__ __forceinline__ double weight(float x) const { return x == -INFINITY ? 0.0 : weight_of(exp2, x, zmax, c); }
+  __device__ __forceinline__ u64 fixed(float x) const { return x == -INFINITY ? 0 : fixed_of(weight_of(exp2, x, zmax, c)); }
+  // f(its tokens' z, 8 a lane, the first's id) for the strips i0 .. i1 - 1 that have a token
+  // of t0 or more, by their maxima top_of: eight strips of eight lanes each at a time, the
+  // next eight on their way.  Called by N threads, whose waves take up to 64 strips in turn.
+  template <int N, typename F>
+  __device__ __forceinline__ void strips(const float* top_of, float t0, int i0, int i1, F f) const {
+    constexpr int W = N / 64;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int share = min(max((i1 - i0 + 8 * W - 1) / (8 * W) * 8, 8), 64);
+    int base = i0 + share * wave;
+    float top = lane < share && base + lane < i1 ? top_of[base + lane] : -INFINITY;
+#pragma unroll 1
+    for (; base < i1; base += share * W) {
+      const bool on = top >= t0 && top > -INFINITY;
+      const int next = base + share * W + lane;
+      if (lane < share && next < i1) top = top_of[next];
+      else top = -INFINITY;
+      const uint64_t mask = __ballot(on);
+      const int found = __popcll(mask), in_front = __popcll(mask & ((1ull << lane) - 1));
+      // lane j has the number of the j-th of them
+      const int order = __builtin_amdgcn_ds_permute(4 * (on ? in_front : found + lane - in_front), lane);
+      auto fetch = [&](Eight<T, VEC>& v, int& first, int a) {
+        const int k = a + (lane >> 3), strip = base + __builtin_amdgcn_ds_bpermute(4 * k, order);
+        first = k < found ? strip * STRIP + 8 * (lane & 7) : vocab;
+        v.load(z, first, vocab);
+      };
+      Eight<T, VEC> v, after;
+      int first, first_after;
+      if (found) fetch(v, first, 0);
+#pragma unroll 1
+      for (int a = 0; a < found; a += 8) {
+        fetch(after, first_after, a + 8);
+        f(v, first);
+        v = after;
+        first = first_after;
+      }
+    }
+  }
+  // f(z, id) for their tokens of t0 or more.  DENSE: most of them are.
+  template <int N, bool DENSE, typename F>
+  __device__ __forceinline__ void tokens(const float* top_of, float t0, int i0, int i1, F f) const {
+    strips<N>(top_of, t0, i0, i1, [&](const Eight<T, VEC>& v, int first) {
+      if constexpr (DENSE) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (v[e] >= t0 && v[e] > -INFINITY) f(v[e], first + e);   // tokens past the vocabulary are -inf
+      } else {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) hits |= (uint32_t)(v[e] >= t0 && v[e] > -INFINITY) << e;
+#pragma unroll 1
+        while (hits) {
+          const int at = __ffs((int)hits) - 1;
+          hits &= hits - 1;
+          float x = v[0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) x = e == at ? v[e] : x;
+          f(x, first + at);
+        }
+      }
+    });
+  }
+  // By a workgroup of N threads: the token of segment s at which the running sum of
+  // weigh(z, id), `before` in front of the segment, passes `want`; the last with a weight
+  // where none does.  sums: [STRIPS] in shared memory.
+  template <int N, typename V, typename W>
+  __device__ __forceinline__ int token_at(int s, V before, double want, W weigh, V* sums, float& at_z) const {
+    const int lane = threadIdx.x & 63;
+    float x;
+    int id;
+    auto end_of = [&](int strip, V& w) {
+      id = s * SEG + strip * STRIP + lane;
+      x = id < vocab ? ld_f32<T>(z + id) : -INFINITY;
+      w = id < vocab ? weigh(x, id) : 0;
+      return wave_prefix(w);
+    };
+    V w;
+    __syncthreads();
+#pragma unroll 1
+    for (int j = threadIdx.x >> 6; j < STRIPS; j += N / 64) {
+      const V end = end_of(j, w);
+      if (lane == 63) sums[j] = end;
+    }
+    __syncthreads();
+    const int at = entry_at(STRIPS, [&](int j) { return sums[j]; }, want, before);
+    const V end = end_of(at, w) + before;
+    const uint64_t past = __ballot(w > 0 && (double)end > want), some = __ballot(w > 0);
+    const int from = past ? first_lane(past) : last_lane(some | 1);
+    at_z = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), from));
+    return __builtin_amdgcn_readlane(id, from);
+  }
+};
+
 __device__ __forceinline__ double given_u(const DrawArgs& A, int r) {
   return A.u64 ? ((const double*)A.u)[r] : (double)((const float*)A.u)[r];
 }
@@ -564,96 +669,99 @@ __device__ __forceinline__ void answer(const DrawArgs& A, int r, int id, float z
   A.kept[r] = (float)(lw - log(kept));
 }
 
-// By one wave: a row of which nothing is cut, or all but the first of the largest (T = 0).
-template <typename T, bool VEC>
-__device__ __forceinline__ void draw_plain(const DrawArgs& A, int r, const Segments& S, const Logits<T, VEC>& z, const RowOpts& o,
-                                           double u) {
-  double want = u * S.total, before = 0.0;
-  float at_z;
-  int at = -1, id;
-  if (o.temperature == 0.0) {
-    S.each([&](int i, float m, double) {
-      const uint64_t mask = __ballot(m == S.zmax);
-      if (at < 0 && mask) at = __builtin_amdgcn_readfirstlane(i) + first_lane(mask);
-    });
-    id = z.token_at(at, 0.0, 0.0, [&](float x, int) { return x == S.zmax ? 1.0 : 0.0; }, at_z);
-  } else {
-    int last = 0;
-    S.each([&](int i, float, double w) {
-      if (at >= 0) return;
-      const double end = wave_prefix(w) + before;
-      const uint64_t past = __ballot(w > 0.0 && end > want), some = __ballot(w > 0.0);
-      const int base = __builtin_amdgcn_readfirstlane(i);
-      if (past) {
-        at = base + first_lane(past);
-        before = lane_of(end - w, first_lane(past));
-      } else {
-        if (some) last = base + last_lane(some);
-        before = lane_of(end, 63);
-      }
-    });
-    if (at < 0) {                     // roundings next to u = 1
-      at = last;
-      want = INFINITY;
-    }
-    id = z.token_at(at, before, want, [&](float x, int) { return x == -INFINITY ? 0.0 : weight_of(x, S.zmax, S.c); }, at_z);
+// By a workgroup of N threads: a row of which nothing is cut, or all but the first of the
+// largest (T = 0).
+template <int N>
+struct PlainMemory {
+  double red[N / 64], before, sums[STRIPS];
+  int redi[N / 64];
+};
+template <int N, typename T, bool VEC>
+__device__ __forceinline__ void draw_plain(const DrawArgs& A, PlainMemory<N>& P, int r, int segs, const Row& w, const Logits<T, VEC>& z,
+                                           const RowOpts& o, double u) {
+  const float* top = A.seg_m + (int64_t)r * segs;
+  const double* sum = A.seg_s + (int64_t)r * segs;
+  const int tid = threadIdx.x;
+  const bool greedy = o.temperature == 0.0;
+  double want = greedy ? 0.0 : u * w.total, before = 0.0;
+  int at = INT32_MAX, last = 0;
+#pragma unroll 1
+  for (int base = 0; base < segs && at == INT32_MAX; base += N) {
+    const int i = base + tid;
+    double x = 0.0, all;
+    if (i < segs) x = greedy ? (double)(top[i] == w.zmax) : share_of(z.exp2, top[i], sum[i], w.zmax, o.c);
+    const double end = group_prefix<N>(x, P.red, &all) + before;
+    at = group_min<N>(x > 0.0 && end > want ? i : INT32_MAX, P.redi);
+    if (at == i) P.before = end - x;
+    last = max(last, -group_min<N>(x > 0.0 ? -i : 0, P.redi));
+    before += all;
   }
-  if ((threadIdx.x & 63) == 0) {
-    answer(A, r, id, at_z, S.zmax, S.c, S.total, S.total);
-    if (o.temperature == 0.0) A.kept[r] = 0.f;
+  __syncthreads();
+  if (at == INT32_MAX) {              // roundings next to u = 1
+    at = last;
+    want = INFINITY;
+  } else {
+    before = P.before;
+  }
+  if (greedy) before = 0.0;
+  float at_z;
+  const int id = z.template token_at<N>(
+      at, before, want, [&](float x, int) { return greedy ? (double)(x == w.zmax) : z.weight(x); }, P.sums, at_z);
+  if (tid == 0) {
+    answer(A, r, id, at_z, w.zmax, o.c, w.total, w.total);
+    if (greedy) A.kept[r] = 0.f;
   }
 }
 
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_draw_plain(DrawArgs A, int segs) {
-  const int r = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
-  if (r >= A.rows) return;
+__global__ __launch_bounds__(PART) void k_draw_plain(DrawArgs A, int segs) {
+  __shared__ PlainMemory<PART> P;
+  const int r = blockIdx.x;
   const RowOpts o = row_opts(A, r);
   const double u = given_u(A, r);
-  Segments S;
-  if (!S.read(A, r, segs, o) || !(u >= 0.0 && u < 1.0)) {
-    if ((threadIdx.x & 63) == 0) no_answer(A, r);
+  const Exp2 exp2;
+  const Row w = read_row<PART>(A, exp2, r, segs, o, P.red, P.redi);
+  if (!w.good || !(u >= 0.0 && u < 1.0)) {
+    if (threadIdx.x == 0) no_answer(A, r);
     return;
   }
-  draw_plain<T, VEC>(A, r, S, Logits<T, VEC>{(const T*)A.logits + r * A.row, A.vocab, S.zmax, S.c}, o, u);
+  draw_plain<PART>(A, P, r, segs, w, Logits<T, VEC>{(const T*)A.logits + r * A.row, A.vocab, w.zmax, o.c, exp2}, o, u);
 }
 
-// ---------------------------------------------------------------- rows, bins, collect
-__global__ __launch_bounds__(256) void k_draw_rows(DrawArgs A, int segs) {
-  const int r = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
-  if (r >= A.rows) return;
-  const RowOpts o = row_opts(A, r);
-  if (!by_bins(o)) return;
-  Segments S;
-  const bool good = S.read(A, r, segs, o);
-  float t0 = 0.f;
-  if (good) {
-    t0 = S.least(nullptr, 0, 0, o.by_p, o.top_p);
-    if (o.by_min) t0 = fmaxf(t0, min_p_border(o, S.zmax));
-  }
-  if ((threadIdx.x & 63) == 0) A.info[r] = DrawRow{S.total, S.zmax, t0, good, 0, BINS, 0};
-}
-
+// ---------------------------------------------------------------- bins, collect
 template <typename T, bool VEC>
 __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int parts) {
-  __shared__ uint16_t active[PART / 64][MAX_SEGS * 64 / PART + 1];
-  __shared__ u64 mass[BINS];
+  __shared__ union {
+    u64 mass[BINS];
+    MassMemory least;
+  } L;
+  __shared__ double red[PART / 64];
+  __shared__ int redi[PART / 64];
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
   if (!by_bins(o)) return;
-  const DrawRow info = A.info[r];
-  if (!info.good) return;
-  for (int i = tid; i < BINS; i += PART) mass[i] = 0;
+  const Exp2 exp2;
+  const Row w = read_row<PART>(A, exp2, r, segs, o, red, redi);
+  float t0 = 0.f;
+  if (w.good) {
+    t0 = o.by_p ? least_of_mass<PART>(A, exp2, r, segs, o, w, L.least) : octaves_below(w.zmax, FIXED_OCTAVES, o.c);
+    if (o.by_min) t0 = fmaxf(t0, min_p_border(o, w.zmax));
+  }
+  if (part == 0 && tid == 0) A.info[r] = DrawRow{w.total, w.zmax, t0, w.good, 0, BINS, 0};
+  if (!w.good) return;
+  __syncthreads();
+  for (int i = tid; i < BINS; i += PART) L.mass[i] = 0;
   __syncthreads();
   const float c = bin_factor(o.c);
-  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, info.zmax, o.c};
-  z.template tokens<PART>(active, A.seg_m + (int64_t)r * segs, info.t0, part_start(part, segs, parts),
-                          part_start(part + 1, segs, parts),
-                          [&](float x, int) { atomicAdd(&mass[bin_of(x, info.zmax, c)], z.fixed(x)); });
+  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, w.zmax, o.c, exp2};
+  z.template tokens<PART, true>(A.strip_m + (int64_t)r * segs * STRIPS, t0, part_start(part, segs, parts) * STRIPS,
+                                part_start(part + 1, segs, parts) * STRIPS,
+                                [&](float x, int) { atomicAdd(&L.mass[bin_of(x, w.zmax, c)], z.fixed(x)); });
   __syncthreads();
   u64* bins = A.part_bins + (int64_t)blockIdx.x * BINS;
+#pragma unroll 1
   for (int i = tid; i < BINS; i += PART) {
-    const u64 m = mass[i];
+    const u64 m = L.mass[i];
     bins[i] = m;
     if (m) atomicAdd(&A.bins[(int64_t)r * BINS + i], m);
   }
@@ -661,7 +769,6 @@ __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int pa
 
 template <typename T, bool VEC>
 __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int parts) {
-  __shared__ uint16_t active[PART / 64][MAX_SEGS * 64 / PART + 1];
   __shared__ u64 red[8], list[LIST];
   __shared__ int redi[8], n_list, at;
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
@@ -707,12 +814,13 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
   if (tid == 0) A.part_kept[blockIdx.x] = all;
   if (border == BINS) return;
   const float c = bin_factor(o.c);
-  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, info.zmax, o.c};
-  z.template tokens<PART>(active, A.seg_m + (int64_t)r * segs, info.t0, part_start(part, segs, parts),
-                          part_start(part + 1, segs, parts), [&](float x, int id) {
+  const Exp2 exp2;
+  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, info.zmax, o.c, exp2};
+  z.template tokens<PART, true>(A.strip_m + (int64_t)r * segs * STRIPS, info.t0, part_start(part, segs, parts) * STRIPS,
+                          part_start(part + 1, segs, parts) * STRIPS, [&](float x, int id) {
                             if (bin_of(x, info.zmax, c) != border) return;
                             const int k = atomicAdd(&n_list, 1);
-                            if (k < LIST) list[k] = place_of(x, id);
+                            if (k < LIST) list[k] = Places<T>::of(x, id);
                           });
   __syncthreads();
   const int n = n_list;
@@ -724,50 +832,79 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
 }
 
 // ---------------------------------------------------------------- pick
+template <int N>
 struct CutMemory {
+  static constexpr int FEW = N / 4 < 128 ? 128 : N / 4;   // tokens that are compared with one another
+  struct Token { u64 place, weight; };
   union {
     struct { u64 mass[BINS]; uint32_t count[BINS]; } bin;
     u64 seg[MAX_SEGS];                // kept weight of each segment
+    uint32_t steps[STEPS];
+    PlainMemory<N> plain;
   };
   u64 list[LIST];                     // places of the tokens that can be kept
-  uint16_t active[PICK / 64][MAX_SEGS * 64 / PICK + 1];
-  u64 few[FEW], weight[FEW];
-  u64 red[8], found, mass, rank, lo, hi;
-  int redi[8], n_list, n_few;
+  Token few[FEW];
+  u64 before[FEW];
+  int rank[FEW];
+  u64 red[N / 64], sums[STRIPS], found, mass, rank0, lo, hi;
+  int redi[N / 64], n_list, n_few;
 };
 
-// By one wave, a token (place p, weight w) in each of the first n lanes: how many of them
-// come before the lane's, and what those weigh.
-__device__ __forceinline__ void compare(int n, u64 p, u64 w, int& rank, u64& before) {
-#pragma unroll 1
-  for (int j = 0; j < n; ++j) {
-    const bool in_front = lane_of(p, j) > p;
-    rank += in_front;
-    before += in_front ? lane_of(w, j) : 0;
+// The first n <= FEW tokens of C.few, a thread each and the rest of the workgroup to share
+// their comparisons: how many of them come before the thread's, and what those weigh.
+template <int N>
+__device__ __forceinline__ void compare(CutMemory<N>& C, int n, int& rank, u64& before) {
+  constexpr int FEW = CutMemory<N>::FEW;
+  const int tid = threadIdx.x;
+  const int room = n <= 64 ? 64 : n <= 128 ? 128 : 256, groups = N / room, mine = tid % room, per = (n + groups - 1) / groups;
+  static_assert(FEW <= 256 && FEW <= N, "a thread has one token at most");
+  if (tid < n) {
+    C.before[tid] = 0;
+    C.rank[tid] = 0;
   }
+  __syncthreads();
+  int k = 0;
+  u64 w = 0;
+  if (mine < n) {
+    const u64 p = C.few[mine].place;
+    const int end = min(n, (tid / room + 1) * per);
+#pragma unroll 4
+    for (int j = tid / room * per; j < end; ++j) {
+      const bool in_front = C.few[j].place > p;
+      k += in_front;
+      w += in_front ? C.few[j].weight : 0;
+    }
+    if (k) {
+      atomicAdd(&C.rank[mine], k);
+      atomicAdd(&C.before[mine], w);
+    }
+  }
+  __syncthreads();
+  rank = tid < n ? C.rank[tid] : 0;
+  before = tid < n ? C.before[tid] : 0;
 }
 
 // The border of top-k (by rank: fewer than `limit` tokens come before) or top-p (less
 // than `limit` of weight does) among the tokens that `each` gives, n of them, mass0 of
 // weight in front of them, none outside the places lo .. hi: the place of the last that is
 // kept, 0 if all of them are; mass: the weight up to it.  Windows of places, ever finer by
-// 1024, until a wave can compare what is left.
-template <typename R, typename Each>
-__device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Each& each, int n, bool by_rank, double limit, u64 lo,
+// 1024, until what is left can be compared.
+template <typename P, int N, typename R, typename Each>
+__device__ __forceinline__ u64 find_border(const R& row, CutMemory<N>& C, const Each& each, int n, bool by_rank, double limit, u64 lo,
                                            u64 hi, u64 mass0, u64* mass) {
+  constexpr int FEW = CutMemory<N>::FEW, PER = BINS / N;
   const int tid = threadIdx.x;
-  constexpr int PER = BINS / PICK;
   u64 rank0 = 0;                      // before the window
   int inside = n;
   auto reaches = [&](u64 rank, u64 weight) { return by_rank ? (double)rank >= limit : (double)weight >= limit; };
 #pragma unroll 1
   while (inside > FEW) {              // places differ: at the latest a window of one has one token
     __syncthreads();
-    for (int i = tid; i < BINS; i += PICK) { C.bin.mass[i] = 0; C.bin.count[i] = 0; }
+    for (int i = tid; i < BINS; i += N) { C.bin.mass[i] = 0; C.bin.count[i] = 0; }
     __syncthreads();
     const int shift = max(54 - __clzll((long long)(hi - lo | 1)), 0);   // (hi - lo) >> shift is below 1024
     each([&](float x, int id) {
-      const u64 p = place_of(x, id);
+      const u64 p = P::of(x, id);
       if (p < lo || p > hi) return;
       const int d = BINS - 1 - (int)((p - lo) >> shift);
       atomicAdd(&C.bin.mass[d], row.fixed(x));
@@ -781,8 +918,8 @@ __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Eac
       m += C.bin.mass[tid * PER + i];
       rank += C.bin.count[tid * PER + i];
     }
-    m = group_prefix<PICK>(m, C.red, &all_m) + mass0;
-    rank = group_prefix<PICK>(rank, C.red, &all_n) + rank0;
+    m = group_prefix<N>(m, C.red, &all_m) + mass0;
+    rank = group_prefix<N>(rank, C.red, &all_n) + rank0;
     int hit = INT32_MAX;
     u64 hit_m = 0, hit_n = 0;
 #pragma unroll
@@ -796,18 +933,18 @@ __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Eac
       m -= w;
       rank -= k;
     }
-    const int d = group_min<PICK>(hit, C.redi);
+    const int d = group_min<N>(hit, C.redi);
     if (d == INT32_MAX) {             // the limit lies behind the last token
       *mass = mass0 + all_m;
       return 0;
     }
     if (hit == d) {
       C.mass = hit_m;
-      C.rank = hit_n;
+      C.rank0 = hit_n;
     }
     __syncthreads();
     mass0 = C.mass;
-    rank0 = C.rank;
+    rank0 = C.rank0;
     inside = (int)min(C.bin.count[d], (uint32_t)FEW + 1);
     lo += (u64)(BINS - 1 - d) << shift;
     hi = min(hi, lo + ((1ull << shift) - 1));
@@ -816,80 +953,65 @@ __device__ __forceinline__ u64 find_border(const R& row, CutMemory& C, const Eac
   if (tid == 0) C.n_few = 0;
   __syncthreads();
   each([&](float x, int id) {
-    const u64 p = place_of(x, id);
-    if (p >= lo && p <= hi) {
-      const int i = atomicAdd(&C.n_few, 1);
-      C.few[i] = p;
-      C.weight[i] = row.fixed(x);
-    }
+    const u64 p = P::of(x, id);
+    if (p >= lo && p <= hi) C.few[atomicAdd(&C.n_few, 1)] = {p, row.fixed(x)};
   });
+  if (tid == 0) C.found = 0;
   __syncthreads();
-  if (tid < 64) {
-    const int k = C.n_few;
-    const u64 p = tid < k ? C.few[tid] : 0, w = tid < k ? C.weight[tid] : 0;
-    int rank = 0;
-    u64 before = mass0;
-    compare(k, p, w, rank, before);
-    const uint64_t ends = __ballot(tid < k && !reaches(rank0 + rank, before) && reaches(rank0 + rank + 1, before + w));
-    const u64 all = lane_of(wave_prefix(w), 63);
-    if (tid == 0) {
-      C.found = ends ? 1 : 0;
-      C.mass = mass0 + all;           // the limit lies behind the last token
-    }
-    if (ends && tid == first_lane(ends)) {
-      C.found = p;
-      C.mass = before + w;
-    }
+  const int k = C.n_few;
+  int rank;
+  u64 before;
+  compare(C, k, rank, before);
+  const u64 p = tid < k ? C.few[tid].place : 0, w = tid < k ? C.few[tid].weight : 0;
+  const u64 end = mass0 + before + w;
+  if (tid < k && !reaches(rank0 + rank, mass0 + before) && reaches(rank0 + rank + 1, end)) {
+    C.found = p;
+    C.mass = end;
   }
+  if (tid < k && rank == k - 1) C.hi = end;   // the limit may lie behind the last token
   __syncthreads();
-  *mass = C.mass;
-  return C.found;
+  const u64 found = C.found;
+  *mass = found ? C.mass : k ? C.hi : mass0;
+  return found;
 }
 
-template <typename T, bool VEC>
-__global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int parts) {
-  __shared__ CutMemory C;
-  const int r = blockIdx.x, tid = threadIdx.x;
+template <typename T, bool VEC, int N>
+__global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts) {
+  typedef Places<T> P;
+  __shared__ CutMemory<N> C;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const RowOpts o = row_opts(A, r);
   const double u = given_u(A, r);
   const bool binned = by_bins(o);
+  const Exp2 exp2;
   DrawRow info{};
-  Segments S;
+  Row w;
   float t0 = 0.f;                     // no token below it is kept
   if (binned) {
     info = A.info[r];
     t0 = info.t0;
-    S.segs = segs;
-    S.top_of = A.seg_m + (int64_t)r * segs;
-    S.zmax = info.zmax;
-    S.total = info.total;
-    S.c = o.c;
+    w = Row{info.zmax, info.total, info.good != 0};
   } else {
-    info.good = S.read(A, r, segs, o);   // every wave alike: none waits for another
+    w = read_row<N>(A, exp2, r, segs, o, C.plain.red, C.redi);
   }
-  if (!info.good || !(u >= 0.0 && u < 1.0)) {
+  if (!w.good || !(u >= 0.0 && u < 1.0)) {
     if (tid == 0) no_answer(A, r);
     return;
   }
-  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, S.zmax, S.c};
+  const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, w.zmax, o.c, exp2};
   if (!binned && (o.temperature == 0.0 || !o.by_k)) {   // nothing is cut here
-    if (tid < 64) draw_plain<T, VEC>(A, r, S, z, o, u);
+    draw_plain<N>(A, C.plain, r, segs, w, z, o, u);
     return;
   }
-  const float min_z = o.by_min ? min_p_border(o, S.zmax) : -INFINITY;
-  u64 border = o.by_min ? (u64)key_of(min_z) << ID_BITS : 0;
+  const float min_z = o.by_min ? min_p_border(o, w.zmax) : -INFINITY;
+  u64 border = o.by_min ? P::from(min_z) : 0;
   const bool whole_list = binned && info.listed <= LIST;   // the border's bin is listed, the rest summed
+  const int n_strips = segs * STRIPS;
+  const float* const strip_m = A.strip_m + (int64_t)r * n_strips;
   if (!binned) {
-    float* const strips = reinterpret_cast<float*>(C.list);   // where k is too many for the segments
-    int n_strips = 0;
-    if (2 * o.top_k > segs && 4 * segs <= LIST) {
-      n_strips = 8 * segs;
-      for (int i = tid; i < n_strips; i += PICK) strips[i] = A.strip_m[(int64_t)r * n_strips + i];
-      __syncthreads();
-    }
-    t0 = S.least(strips, n_strips, o.top_k, false, 1.0);
+    const bool many = 2 * o.top_k > segs;                  // for segments' maxima to tell
+    t0 = least_of<N>(many ? strip_m : A.seg_m + (int64_t)r * segs, many ? n_strips : segs, o.top_k, w.zmax, o.c, C.steps, C.redi);
     if (!o.by_p) t0 = fmaxf(t0, min_z);                    // top-p takes its share of all the k
-    __syncthreads();
   }
   if (tid == 0) {
     C.n_list = whole_list ? info.listed : 0;
@@ -898,64 +1020,62 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
   }
   __syncthreads();
   if (whole_list) {
-    for (int i = tid; i < info.listed; i += PICK) C.list[i] = A.list[(int64_t)r * LIST + i];
+    for (int i = tid; i < info.listed; i += N) C.list[i] = A.list[(int64_t)r * LIST + i];
   } else {
-    z.template tokens<PICK>(C.active, S.top_of, t0, 0, segs, [&](float x, int id) {
+    z.template tokens<N, false>(strip_m, t0, 0, n_strips, [&](float x, int id) {
       const int i = atomicAdd(&C.n_list, 1);
-      if (i < LIST) C.list[i] = place_of(x, id);
+      if (i < LIST) C.list[i] = P::of(x, id);
     });
   }
   __syncthreads();
   const int n_list = C.n_list;
 
-  // Few of all that can be kept: a lane each of one wave, compared with one another and
-  // drawn from by their ids.
-  if (!whole_list && n_list <= FEW) {
-    if (tid >= 64) return;
+  // Few of all that can be kept: a thread each, compared with one another and drawn from by
+  // their ids.
+  if (!whole_list && n_list <= CutMemory<N>::FEW) {
     const bool is = tid < n_list;
-    const u64 p = is ? C.list[tid] : 0, w = is ? z.fixed(z_of(p)) : 0;
-    const int id = is ? id_of(p) : INT32_MAX;
-    int rank = 0;
-    u64 before = 0, all = 0;
-    compare(n_list, p, w, rank, before);
+    const u64 p = is ? C.list[tid] : 0, mine = is ? z.fixed(P::z(p)) : 0;
+    const int id = P::id(p);
+    if (is) C.few[tid] = {p, mine};
+    __syncthreads();
+    int rank;
+    u64 before, all;
+    compare(C, n_list, rank, before);
     bool in = is && (!o.by_k || rank < o.top_k);
     if (o.by_p) {
-      const double share = o.by_k ? (double)lane_of(wave_prefix(in ? w : 0), 63) : S.total * FIXED_ONE;
+      double share = w.total * FIXED_ONE;
+      if (o.by_k) {
+        group_prefix<N>(in ? mine : (u64)0, C.red, &all);
+        share = (double)all;
+      }
       in = in && (double)before < mass_limit(o, share);
     }
     in = in && p >= border;
-    u64 end = 0;
-#pragma unroll 1
-    for (uint64_t left = __ballot(in); left; left &= left - 1) {
-      const int j = first_lane(left);
-      const u64 x = lane_of(w, j);
-      all += x;
-      end += __builtin_amdgcn_readlane(id, j) <= id ? x : 0;
-    }
+    group_prefix<N>(in ? mine : (u64)0, C.red, &all);
     const double want = u * (double)all;
-    const uint64_t past = __ballot(in && w > 0 && (double)end > want), some = __ballot(in && w > 0);
-    // the lowest id of those past it; roundings next to u = 1: the highest with a weight
-    int hit = past ? INT32_MAX : -1;
-#pragma unroll 1
-    for (uint64_t left = past ? past : some; left; left &= left - 1) {
-      const int x = __builtin_amdgcn_readlane(id, first_lane(left));
-      hit = past ? min(hit, x) : max(hit, x);
-    }
-    if (in && id == hit) answer(A, r, id, z_of(p), S.zmax, S.c, S.total, (double)all / FIXED_ONE);
+    // again by id, the lowest first, of what is kept: the first whose end passes
+    if (is) C.few[tid] = {(u64)(0xFFFFFFFFu - id), in ? mine : 0};
+    __syncthreads();
+    compare(C, n_list, rank, before);
+    const bool can = in && mine > 0;
+    const int past = group_min<N>(can && (double)(before + mine) > want ? id : INT32_MAX, C.redi);
+    // roundings next to u = 1: the highest with a weight
+    const int hit = past < INT32_MAX ? past : -group_min<N>(can ? -id : 0, C.redi);
+    if (can && id == hit) answer(A, r, id, P::z(p), w.zmax, o.c, w.total, (double)all / FIXED_ONE);
     return;
   }
 
   auto each = [&](auto f) {
     if (n_list <= LIST) {
-      for (int i = tid; i < n_list; i += PICK) f(z_of(C.list[i]), id_of(C.list[i]));
+      for (int i = tid; i < n_list; i += N) f(P::z(C.list[i]), P::id(C.list[i]));
     } else {
-      z.template tokens<PICK>(C.active, S.top_of, t0, 0, segs, f);
+      z.template tokens<N, false>(strip_m, t0, 0, n_strips, f);
     }
   };
-  u64 lo = place_of(t0, (1 << ID_BITS) - 1), hi = place_of(S.zmax, 0);
+  u64 lo = P::of(t0, (1 << ID_BITS) - 1), hi = P::of(w.zmax, 0);
   if (n_list <= LIST) {               // no wider than the list is
     u64 least = ~0ull, most = 0;
-    for (int i = tid; i < n_list; i += PICK) {
+    for (int i = tid; i < n_list; i += N) {
       least = min(least, C.list[i]);
       most = max(most, C.list[i]);
     }
@@ -964,7 +1084,7 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
       least = min(least, __shfl_xor(least, x, 64));
       most = max(most, __shfl_xor(most, x, 64));
     }
-    if ((tid & 63) == 0) {
+    if (lane == 0 && most) {
       atomicMin(&C.lo, least);
       atomicMax(&C.hi, most);
     }
@@ -972,31 +1092,30 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
     lo = C.lo;
     hi = C.hi;
   }
-  double share = S.total * FIXED_ONE;
+  double share = w.total * FIXED_ONE;
 #pragma unroll 1
   for (int rule = 0; rule < 2; ++rule) {
     if (rule == 0 ? !o.by_k : !o.by_p || (whole_list && info.bin == BINS)) continue;
     u64 mass;
-    border = max(border, find_border(z, C, each, n_list, rule == 0, rule == 0 ? (double)o.top_k : mass_limit(o, share), lo, hi,
-                                     whole_list ? info.above : 0, &mass));
+    border = max(border, find_border<P>(z, C, each, n_list, rule == 0, rule == 0 ? (double)o.top_k : mass_limit(o, share), lo, hi,
+                                        whole_list ? info.above : 0, &mass));
     share = (double)mass;
   }
   // What is kept of each segment or, where the histogram knows the parts', of each part
   // and then of that part's segments.
   __syncthreads();
-  const int lane = tid & 63;
   int s0 = 0, s1 = segs;
   u64 before = 0, kept = 0;
   double want = 0.0;
   if (whole_list) {
-    for (int i = tid; i < parts; i += PICK) C.seg[i] = A.part_kept[(int64_t)r * parts + i];
+    for (int i = tid; i < parts; i += N) C.seg[i] = A.part_kept[(int64_t)r * parts + i];
     __syncthreads();
-    for (int i = tid; i < n_list; i += PICK)
+    for (int i = tid; i < n_list; i += N)
       if (C.list[i] >= border) {
-        const int s = id_of(C.list[i]) / SEG;
+        const int s = P::id(C.list[i]) / SEG;
         int p = (int)((int64_t)s * parts / segs);
         while (part_start(p + 1, segs, parts) <= s) ++p;
-        atomicAdd(&C.seg[p], z.fixed(z_of(C.list[i])));
+        atomicAdd(&C.seg[p], z.fixed(P::z(C.list[i])));
       }
     __syncthreads();
     for (int i = lane; i < parts; i += 64) kept += C.seg[i];
@@ -1007,25 +1126,25 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
     s1 = part_start(p + 1, segs, parts);
     __syncthreads();
   }
-  for (int i = tid; i < segs; i += PICK) C.seg[i] = 0;
+  for (int i = s0 + tid; i < s1; i += N) C.seg[i] = 0;
   __syncthreads();
   if (!whole_list && n_list <= LIST) {
     each([&](float x, int id) {
-      if (place_of(x, id) >= border) atomicAdd(&C.seg[id / SEG], z.fixed(x));
+      if (P::of(x, id) >= border) atomicAdd(&C.seg[id / SEG], z.fixed(x));
     });
-  } else {                            // a segment's tokens add up within their wave
-    z.template segments<PICK>(C.active, S.top_of, t0, s0, s1, [&](int s, const float (&v)[8], int first) {
+  } else {                            // a strip's tokens add up within its lanes
+    z.template strips<N>(strip_m, t0, s0 * STRIPS, s1 * STRIPS, [&](const Eight<T, VEC>& v, int first) {
       u64 sum = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (v[e] >= t0 && place_of(v[e], first + e) >= border) sum += z.fixed(v[e]);
-#pragma unroll
-      for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, 64);
-      if (lane == 0) C.seg[s] = sum;
+        if (v[e] >= t0 && P::of(v[e], first + e) >= border) sum += z.fixed(v[e]);
+      sum += shifted<0x111, 0xF>(sum);   // to the last of the eight lanes
+      sum += shifted<0x112, 0xF>(sum);
+      sum += shifted<0x114, 0xF>(sum);
+      if ((lane & 7) == 7 && sum) atomicAdd(&C.seg[first / SEG], sum);
     });
   }
   __syncthreads();
-  if (tid >= 64) return;
   if (!whole_list) {
     for (int i = lane; i < segs; i += 64) kept += C.seg[i];
     kept = lane_of(wave_prefix(kept), 63);
@@ -1033,9 +1152,13 @@ __global__ __launch_bounds__(PICK) void k_draw_pick(DrawArgs A, int segs, int pa
   }
   const int at = s0 + entry_at(s1 - s0, [&](int i) { return C.seg[s0 + i]; }, want, before);
   float at_z;
-  const int id = z.token_at(at, before, want, [&](float x, int i) { return place_of(x, i) >= border ? z.fixed(x) : (u64)0; }, at_z);
-  if (lane == 0) answer(A, r, id, at_z, S.zmax, S.c, S.total, (double)kept / FIXED_ONE);
+  const int id = z.template token_at<N>(
+      at, before, want, [&](float x, int i) { return P::of(x, i) >= border ? z.fixed(x) : (u64)0; }, C.sums, at_z);
+  if (tid == 0) answer(A, r, id, at_z, w.zmax, o.c, w.total, (double)kept / FIXED_ONE);
 }
+
+// Up to as many rows as there are compute units each has one of them: sixteen waves.
+constexpr int PICK_WIDE_ROWS = 256;
 
 int segments(int vocab) { return (vocab + SEG - 1) / SEG; }
 
@@ -1066,33 +1189,32 @@ Scratch scratch_of(const DrawArgs& a) {
   s.info = s.list + 8 * binned * LIST;
   s.seg_m = s.info + (int64_t)sizeof(DrawRow) * binned;
   s.strip_m = s.seg_m + 4 * n;
-  s.end = (s.strip_m + (may_cut(a) ? 32 * n : 0) + 15) / 16 * 16;
+  s.end = (s.strip_m + (may_cut(a) ? 4 * STRIPS * n : 0) + 15) / 16 * 16;
   return s;
 }
 
 template <typename T, bool VEC>
 hipError_t run(const DrawArgs& a, hipStream_t st) {
-  const int segs = segments(a.vocab);
-  const unsigned per_row = (unsigned)(segs + 3) / 4;
+  const int segs = segments(a.vocab), parts = parts_of(a);
+  const unsigned per_row = (unsigned)(segs + 1) / 2;
   const int64_t items = (int64_t)a.rows * per_row;
-  if (items > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)((items + SCAN_WAVES - 1) / SCAN_WAVES)), scan(64 * SCAN_WAVES), row(PICK);
+  if (items > INT32_MAX / 2 || (int64_t)a.rows * parts > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t per = std::max<int64_t>(1, items / SCAN_FILL), waves = (items + per - 1) / per;
+  const dim3 scan((unsigned)((waves + SCAN_WAVES - 1) / SCAN_WAVES)), part((unsigned)(a.rows * parts)), rows(a.rows);
   hipError_t e;
-  const dim3 waves((unsigned)((a.rows + 3) / 4)), four(256);
   if (!may_cut(a)) {
-    if ((e = kv8_launch(k_draw_scan<T, VEC, false>, grid, scan, st, a, segs, per_row, (unsigned)items)) != hipSuccess) return e;
-    return kv8_launch(k_draw_plain<T, VEC>, waves, four, st, a, segs);
+    if ((e = kv8_launch(k_draw_scan<T, VEC, false>, scan, dim3(64 * SCAN_WAVES), st, a, segs, per_row, (unsigned)items, (unsigned)per)) != hipSuccess)
+      return e;
+    return kv8_launch(k_draw_plain<T, VEC>, rows, dim3(PART), st, a, segs);
   }
-  if ((e = kv8_launch(k_draw_scan<T, VEC, true>, grid, scan, st, a, segs, per_row, (unsigned)items)) != hipSuccess) return e;
-  const int parts = parts_of(a);
+  if ((e = kv8_launch(k_draw_scan<T, VEC, true>, scan, dim3(64 * SCAN_WAVES), st, a, segs, per_row, (unsigned)items, (unsigned)per)) != hipSuccess)
+    return e;
   if (a.bins) {
-    if ((int64_t)a.rows * parts > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 g((unsigned)(a.rows * parts));
-    if ((e = kv8_launch(k_draw_rows, waves, four, st, a, segs)) != hipSuccess) return e;
-    if ((e = kv8_launch(k_draw_bins<T, VEC>, g, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
-    if ((e = kv8_launch(k_draw_collect<T, VEC>, g, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
+    if ((e = kv8_launch(k_draw_bins<T, VEC>, part, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
+    if ((e = kv8_launch(k_draw_collect<T, VEC>, part, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
   }
-  return kv8_launch(k_draw_pick<T, VEC>, dim3(a.rows), row, st, a, segs, parts);
+  if (a.rows <= PICK_WIDE_ROWS) return kv8_launch(k_draw_pick<T, VEC, 1024>, rows, dim3(1024), st, a, segs, parts);
+  return kv8_launch(k_draw_pick<T, VEC, 256>, rows, dim3(256), st, a, segs, parts);
 }
 
 }  // namespace
