@@ -60,6 +60,13 @@ __global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ par
 // Scores are formed transposed, S^T = K Q^T, so that a lane ends up with the
 // probabilities of one column for just those tokens whose V^T operand it loads.
 // Every node sees the context: only steps that reach into the tree are masked.
+// What bounds it: matrix and vector instructions, which take the units in turn.  A step of 32
+// tokens x 16 columns x 128 dims is 16 MFMAs, 64 conversions of codes and some 80 others,
+// about 1200 clocks a wave at four waves a SIMD, and a wave's start and end weigh as much as
+// eight steps.  Tried at 64 trees of 4 to 63 nodes over 512 to 4500 tokens, 12 heads (83 us):
+// 32 columns a wave 84 us (two waves a SIMD), four waves of 16 columns over codes that
+// come straight into LDS once 89 us (its barriers cost what the shared loads save), keys as
+// e4m3 operands beside queries in two e4m3 pieces 84 us.
 constexpr int tree_pieces(int size) { return size == 2 ? 1 : 3; }   // bf16 pieces of a query and of a probability
 constexpr int tree_waves(int size, int hd) { return size == 2 || hd == 64 ? 4 : 3; }   // of a SIMD, by the registers
 
@@ -83,14 +90,49 @@ __device__ __forceinline__ int find_group(const Kv8Rows& b, int x, int rep, int 
   return lo;
 }
 
+// The sequence of up to 64 whose column groups hold number x, the longest first: those that
+// take longest are not left for the end.  -1: none has it; key: its first group.  A lane a
+// sequence, every wave of the workgroup compares with some of them.
+template <int W>
+__device__ __forceinline__ int find_group_sorted(const Kv8Rows& b, int x, int rep, int shift, int (&sum)[W][64], int& key) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  int r0 = 0, n = 0, len = -1;
+  if (lane < b.n_seqs) {
+    kv8_seq_rows(b, lane, r0, n);
+    len = kv8_len(b, lane);
+  }
+  const int groups = n > 0 ? (int)(((int64_t)n * rep + (1 << shift) - 1) >> shift) : 0;
+  int first = 0;
+  for (int t = wave; t < b.n_seqs; t += W) {
+    const int l = __builtin_amdgcn_readlane(len, t), g = __builtin_amdgcn_readlane(groups, t);
+    first += l > len || (l == len && t < lane) ? g : 0;
+  }
+  sum[wave][lane] = first;
+  __syncthreads();
+  first = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) first += sum[w][lane];
+  const uint64_t here = __ballot(x >= first && x < first + groups);
+  if (!here) return -1;
+  const int s = __ffsll((unsigned long long)here) - 1;
+  key = __builtin_amdgcn_readlane(first, s);
+  return s;
+}
+
+// The largest of a lane's scores; NaN where one is: it stays out of the running maximum.
+__device__ __forceinline__ float top8(const f32x4_t (&s)[2]) {
+  auto most = [](float a, float b) { return __builtin_elementwise_maximum(a, b); };
+  return most(most(most(s[0][0], s[0][1]), most(s[0][2], s[0][3])), most(most(s[1][0], s[1][1]), most(s[1][2], s[1][3])));
+}
+
 // Four dims of column c: the waves' results joined, NaN values of the tokens that its
 // node does see put back (the steps cleared them), and stored, or kept for the join of
 // the chunks.
 template <typename T, int HD, int W>
 __device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W], const float (&sum)[W], const f32x4_t (&acc)[W],
-                                           int64_t c, int d, int rep, int kvh, int r0, int ctx0, int split, int c0, int c1,
+                                           uint32_t c, int d, int rep, int kvh, int r0, int ctx0, int split, int c0, int c1,
                                            bool fix, const int32_t* tab) {
-  const int node = (int)((uint64_t)c / (unsigned)rep), head = kvh * rep + (int)(c - (int64_t)node * rep);
+  const int node = (int)(c / (uint32_t)rep), head = kvh * rep + (int)(c - (uint32_t)node * rep);
   float M = ml[0];
 #pragma unroll
   for (int w = 1; w < W; ++w) M = fmaxf(M, ml[w]);
@@ -130,27 +172,31 @@ __device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W
 }
 
 template <typename T, int HD, int W>
-__global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_attn(Kv8Attn A, unsigned groups, unsigned items) {
+__global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_attn(Kv8Attn A, unsigned items) {
   constexpr int QP = tree_pieces(sizeof(T)), PP = QP;
   constexpr int NJ = HD / 64;       // 16-byte loads of a block per lane
   constexpr int LDO = HD + 4;
   __shared__ __attribute__((aligned(16))) float sO[W][16][LDO];
   __shared__ float sM[W][16], sL[W][16];
-  __shared__ int sNan[W];
+  __shared__ int sNan[W], sFind[W][64];
 
   // Blocks are dealt to the 8 XCDs in turn; runs of eight items, column groups that
   // read the same tokens, stay on one.
   unsigned item = (blockIdx.x >> 6) * 64 + (blockIdx.x & 7) * 8 + (blockIdx.x >> 3 & 7);
   if (item >= items) return;
-  const int x = (int)(item % groups);
-  item /= groups;
+  // eight groups, then those of the other kv heads and chunks, then the next eight
+  const unsigned others = (unsigned)(A.c.n_kv * A.plan.n_split), eight = (item >> 3) / others;
+  const int x = (int)(eight * 8 + (item & 7));
+  item = (item >> 3) - eight * others;
   const int kvh = (int)(item % (unsigned)A.c.n_kv), split = (int)(item / (unsigned)A.c.n_kv);
   const int rep = A.n_q / A.c.n_kv;
-  int key, r0, n;
-  const int s = find_group(A.b, x, rep, 4, key);
+  int key = 0, r0, n;
+  // where one round of workgroups does not hold them all the order counts
+  const int s = A.b.n_seqs <= 64 && gridDim.x > 256 ? find_group_sorted(A.b, x, rep, 4, sFind, key) : find_group(A.b, x, rep, 4, key);
+  if (s < 0) return;
   kv8_seq_rows(A.b, s, r0, n);
-  const int64_t col0 = (int64_t)(x - key) * 16;
-  if (x < key || col0 >= (int64_t)n * rep) return;
+  const uint32_t cols = (uint32_t)n * rep, col0 = (uint32_t)(x - key) * 16;   // each an output row's head: below 2^32
+  if (x < key || col0 >= cols) return;
   const int len = kv8_len(A.b, s), ctx0 = len - n;      // node i is token ctx0 + i
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int cl = lane & 15, grp = lane >> 4;
@@ -202,9 +248,9 @@ __global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_
   f32x4_t o[NJ][4];
   bf16x8_t qf[2 * NJ][QP];
   const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
-  const int64_t c = col0 + cl;
-  const bool valid = c < (int64_t)n * rep;
-  const int node = valid ? (int)((uint64_t)c / (unsigned)rep) : 0, head = kvh * rep + (valid ? (int)(c - (int64_t)node * rep) : 0);
+  const uint32_t c = col0 + cl;
+  const bool valid = c < cols;
+  const int node = valid ? (int)(c / (uint32_t)rep) : 0, head = kvh * rep + (valid ? (int)(c - (uint32_t)node * rep) : 0);
   const int row = valid && ctx0 + node >= 0 ? r0 + node : -1;   // -1: the column sees nothing, as padding, or is none
   const T* qp = (const T*)A.q.p + max(row, 0) * A.q.row + head * A.q.head;
 #pragma unroll
@@ -272,8 +318,7 @@ __global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_
       }
     }
     bf16x8_t pf[PP];
-    float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])),
-                     fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3]))) * sc;
+    float mx = top8(st) * sc;
     if (__any(mx > m + KV8_SLACK)) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -330,7 +375,7 @@ __global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_
   for (int w = 0; w < W; ++w) fix |= sNan[w] != 0;
   for (int i = tid; i < 16 * (HD / 4); i += 64 * W) {
     const int h = i / (HD / 4), d = i % (HD / 4) * 4;
-    if (col0 + h >= (int64_t)n * rep) break;
+    if (col0 + h >= cols) break;
     float ml[W], sum[W];
     f32x4_t acc[W];
 #pragma unroll
@@ -554,11 +599,11 @@ __global__ __launch_bounds__(64 * ACCEPT_WAVES) void k_kv8_accept(AcceptArgs A) 
 template <typename T, int HD>
 hipError_t run(const Kv8Attn& a, hipStream_t st) {
   const int rep = a.n_q / a.c.n_kv;
-  const int64_t groups = (int64_t)a.b.rows * rep / 16 + a.b.n_seqs, items = groups * a.c.n_kv * a.plan.n_split;
+  const int64_t groups = ((int64_t)a.b.rows * rep / 16 + a.b.n_seqs + 7) / 8 * 8, items = groups * a.c.n_kv * a.plan.n_split;
   if (items > INT32_MAX - 64) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((items + 63) / 64 * 64));
-  if (a.plan.waves == 8) return kv8_launch(k_kv8_tree_attn<T, HD, 8>, grid, dim3(512), st, a, (unsigned)groups, (unsigned)items);
-  return kv8_launch(k_kv8_tree_attn<T, HD, 4>, grid, dim3(256), st, a, (unsigned)groups, (unsigned)items);
+  if (a.plan.waves == 8) return kv8_launch(k_kv8_tree_attn<T, HD, 8>, grid, dim3(512), st, a, (unsigned)items);
+  return kv8_launch(k_kv8_tree_attn<T, HD, 4>, grid, dim3(256), st, a, (unsigned)items);
 }
 
 template <typename T, int HD>
@@ -572,11 +617,11 @@ hipError_t merge(const Kv8Attn& a, hipStream_t st) {
 
 // Tiles where trees are wide and contexts long: 2 trees of 64 nodes, 28 heads, at 60 to
 // 131 thousand tokens 202 us, by 16 columns 246; 64 of 64 nodes, 12 heads, at 4000 tokens
-// 200 and 185.  Elsewhere 16 columns a workgroup: half the trees of 4 to 63 nodes at 512
-// to 4500 tokens 84 us, by tiles 103.  A context is cut only where that fills the chip,
+// 200 and 185.  Elsewhere 16 columns a workgroup: 64 trees of 4 to 63 nodes at 512
+// to 4500 tokens 83 us, by tiles 103.  A context is cut only where that fills the chip,
 // since the chunks' partial results and the join's launch cost more than they even out
-// (84 us in one piece, 92 in two, 101 in four), and 8 waves share a workgroup's tokens
-// where one round holds them.
+// (83 us in one piece, 128 in two), and 8 waves share a workgroup's tokens where one round
+// holds them.
 Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int words, int max_len) {
   Kv8TreePlan p{};
   const int64_t rep = n_q / n_kv, cols = ((int64_t)rows * rep + n_seqs - 1) / n_seqs;
