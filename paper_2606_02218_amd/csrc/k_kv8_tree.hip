@@ -12,10 +12,11 @@
 namespace {
 
 // ---------------------------------------------------------------- masks
-// A wave a sequence: the parents go to LDS, and each lane walks up from its nodes.
-// Parents come before their children, so a walk meets the bits of a mask from the
-// highest word down and ends after at most n steps.  Latency bound: 8 trees of 5 to
-// 16 nodes and 509 of 17 to 64 take one chain of loads and some depth LDS reads.
+// A wave a sequence.  Up to 64 nodes, a lane each: whoever a node sees of its ancestors it
+// passes on, and the reach doubles each time, so six rounds do.  Else the parents go to LDS,
+// and each lane walks up from its nodes: parents come before their children, so a walk meets
+// the bits of a mask from the highest word down and ends after at most n steps.  Latency
+// bound.
 constexpr int TREE_STAGED = 2048;     // parents of a tree that LDS holds
 
 __global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ parent, Kv8Rows b, int words,
@@ -27,6 +28,25 @@ __global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ par
   if (n <= 0) return;
   const int first = max(n - kv8_len(b, s), 0);          // nodes before it are padding
   const int ctx = max(kv8_len(b, s) - n, 0);
+  if (n <= 64) {
+    const int up = lane < n ? parent[r0 + lane] : -1;
+    // no parent: neither the node nor what is behind it counts
+    int far = up >= -1 && up < lane && lane >= first ? up >= first ? up : lane : lane | 64;
+    uint64_t bits = 1ull << lane;
+#pragma unroll 1
+    for (int reach = 1; reach < 64; reach *= 2) {
+      const int at = far & 63, next = __shfl(far, at, 64);
+      bits |= (uint64_t)__shfl((unsigned long long)bits, at, 64);
+      far = next | (far & 64);
+    }
+    if (lane >= n) return;
+    const bool ok = far < 64;
+    uint64_t* out = mask + (int64_t)(r0 + lane) * words;
+    out[0] = ok ? bits : 0;
+    for (int w = 1; w < words; ++w) out[w] = 0;
+    pos[r0 + lane] = ok ? (int)min((int64_t)ctx + __popcll(bits) - 1, (int64_t)INT32_MAX) : -1;
+    return;
+  }
   for (int i = lane; i < min(n, TREE_STAGED); i += 64) sp[i] = parent[r0 + i];
   __syncthreads();
   for (int i = lane; i < n; i += 64) {
@@ -172,7 +192,7 @@ __device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W
 }
 
 template <typename T, int HD, int W>
-__global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_attn(Kv8Attn A, unsigned items) {
+__global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_attn(Kv8Attn A, unsigned eights, unsigned items) {
   constexpr int QP = tree_pieces(sizeof(T)), PP = QP;
   constexpr int NJ = HD / 64;       // 16-byte loads of a block per lane
   constexpr int LDO = HD + 4;
@@ -184,11 +204,11 @@ __global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_
   // read the same tokens, stay on one.
   unsigned item = (blockIdx.x >> 6) * 64 + (blockIdx.x & 7) * 8 + (blockIdx.x >> 3 & 7);
   if (item >= items) return;
-  // eight groups, then those of the other kv heads and chunks, then the next eight
-  const unsigned others = (unsigned)(A.c.n_kv * A.plan.n_split), eight = (item >> 3) / others;
-  const int x = (int)(eight * 8 + (item & 7));
-  item = (item >> 3) - eight * others;
-  const int kvh = (int)(item % (unsigned)A.c.n_kv), split = (int)(item / (unsigned)A.c.n_kv);
+  // eight groups, then those of the other kv heads, then the next eight; chunk after chunk
+  unsigned run = item >> 3;
+  const int kvh = (int)(run % (unsigned)A.c.n_kv);
+  run /= (unsigned)A.c.n_kv;
+  const int split = (int)(run / eights), x = (int)(run - (unsigned)split * eights) * 8 + (int)(item & 7);
   const int rep = A.n_q / A.c.n_kv;
   int key = 0, r0, n;
   // where one round of workgroups does not hold them all the order counts
@@ -599,11 +619,11 @@ __global__ __launch_bounds__(64 * ACCEPT_WAVES) void k_kv8_accept(AcceptArgs A) 
 template <typename T, int HD>
 hipError_t run(const Kv8Attn& a, hipStream_t st) {
   const int rep = a.n_q / a.c.n_kv;
-  const int64_t groups = ((int64_t)a.b.rows * rep / 16 + a.b.n_seqs + 7) / 8 * 8, items = groups * a.c.n_kv * a.plan.n_split;
+  const int64_t eights = ((int64_t)a.b.rows * rep / 16 + a.b.n_seqs + 7) / 8, items = eights * 8 * a.c.n_kv * a.plan.n_split;
   if (items > INT32_MAX - 64) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((items + 63) / 64 * 64));
-  if (a.plan.waves == 8) return kv8_launch(k_kv8_tree_attn<T, HD, 8>, grid, dim3(512), st, a, (unsigned)items);
-  return kv8_launch(k_kv8_tree_attn<T, HD, 4>, grid, dim3(256), st, a, (unsigned)items);
+  if (a.plan.waves == 8) return kv8_launch(k_kv8_tree_attn<T, HD, 8>, grid, dim3(512), st, a, (unsigned)eights, (unsigned)items);
+  return kv8_launch(k_kv8_tree_attn<T, HD, 4>, grid, dim3(256), st, a, (unsigned)eights, (unsigned)items);
 }
 
 template <typename T, int HD>
