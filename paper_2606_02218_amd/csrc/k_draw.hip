@@ -48,6 +48,7 @@ constexpr int STEPS = 512;            // that the octaves are told apart in for 
 constexpr int SCAN_WAVES = 4;
 constexpr int SCAN_FILL = 32768;        // waves of the scan, where there are segments for so many
 constexpr int PART = 256;             // threads of a part of a row's histogram
+constexpr int PICK = 512;             // threads of a row's pick: 8, 64 and 505 rows 12, 19, 16 us; 256 threads 16, 23, 18; 1024 12, 21, 27
 constexpr int BINS = 1024;            // of z, 16 an octave of weight
 constexpr int LIST = 4096;            // tokens that a row's list holds
 constexpr int ID_BITS = 20;
@@ -662,11 +663,16 @@ __device__ __forceinline__ void no_answer(const DrawArgs& A, int r) {
   A.token[r] = -1;
   A.logprob[r] = A.kept[r] = __uint_as_float(0x7FC00000u);
 }
-__device__ __forceinline__ void answer(const DrawArgs& A, int r, int id, float z, float zmax, double c, double total, double kept) {
-  const double lw = ((double)z - (double)zmax) * c * 0.6931471805599453;
-  A.token[r] = id;
-  A.logprob[r] = (float)(lw - log(total));
-  A.kept[r] = (float)(lw - log(kept));
+// By two threads, the first of them and another of its wave: a logarithm each.
+__device__ __forceinline__ void answer(const DrawArgs& A, int r, bool first, int id, float z, float zmax, double c, double total,
+                                       double kept) {
+  const float lp = (float)(((double)z - (double)zmax) * c * 0.6931471805599453 - log(first ? total : kept));
+  if (first) {
+    A.token[r] = id;
+    A.logprob[r] = lp;
+  } else {
+    A.kept[r] = lp;
+  }
 }
 
 // By a workgroup of N threads: a row of which nothing is cut, or all but the first of the
@@ -707,10 +713,7 @@ __device__ __forceinline__ void draw_plain(const DrawArgs& A, PlainMemory<N>& P,
   float at_z;
   const int id = z.template token_at<N>(
       at, before, want, [&](float x, int) { return greedy ? (double)(x == w.zmax) : z.weight(x); }, P.sums, at_z);
-  if (tid == 0) {
-    answer(A, r, id, at_z, w.zmax, o.c, w.total, w.total);
-    if (greedy) A.kept[r] = 0.f;
-  }
+  if (tid < 2) answer(A, r, tid == 0, id, at_z, w.zmax, o.c, w.total, greedy ? 1.0 : w.total);
 }
 
 template <typename T, bool VEC>
@@ -1060,8 +1063,11 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
     const bool can = in && mine > 0;
     const int past = group_min<N>(can && (double)(before + mine) > want ? id : INT32_MAX, C.redi);
     // roundings next to u = 1: the highest with a weight
-    const int hit = past < INT32_MAX ? past : -group_min<N>(can ? -id : 0, C.redi);
-    if (can && id == hit) answer(A, r, id, P::z(p), w.zmax, o.c, w.total, (double)all / FIXED_ONE);
+    int hit = past;
+    if (past == INT32_MAX) hit = -group_min<N>(can ? -id : 0, C.redi);
+    if (can && id == hit) C.found = p;
+    __syncthreads();
+    if (tid < 2) answer(A, r, tid == 0, hit, P::z(C.found), w.zmax, o.c, w.total, (double)all / FIXED_ONE);
     return;
   }
 
@@ -1154,11 +1160,8 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
   float at_z;
   const int id = z.template token_at<N>(
       at, before, want, [&](float x, int i) { return P::of(x, i) >= border ? z.fixed(x) : (u64)0; }, C.sums, at_z);
-  if (tid == 0) answer(A, r, id, at_z, w.zmax, o.c, w.total, (double)kept / FIXED_ONE);
+  if (tid < 2) answer(A, r, tid == 0, id, at_z, w.zmax, o.c, w.total, (double)kept / FIXED_ONE);
 }
-
-// Up to as many rows as there are compute units each has one of them: sixteen waves.
-constexpr int PICK_WIDE_ROWS = 256;
 
 int segments(int vocab) { return (vocab + SEG - 1) / SEG; }
 
@@ -1213,8 +1216,7 @@ hipError_t run(const DrawArgs& a, hipStream_t st) {
     if ((e = kv8_launch(k_draw_bins<T, VEC>, part, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
     if ((e = kv8_launch(k_draw_collect<T, VEC>, part, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
   }
-  if (a.rows <= PICK_WIDE_ROWS) return kv8_launch(k_draw_pick<T, VEC, 1024>, rows, dim3(1024), st, a, segs, parts);
-  return kv8_launch(k_draw_pick<T, VEC, 256>, rows, dim3(256), st, a, segs, parts);
+  return kv8_launch(k_draw_pick<T, VEC, PICK>, rows, dim3(PICK), st, a, segs, parts);
 }
 
 }  // namespace
