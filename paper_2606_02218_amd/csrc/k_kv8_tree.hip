@@ -145,24 +145,28 @@ __device__ __forceinline__ float top8(const f32x4_t (&s)[2]) {
   return most(most(most(s[0][0], s[0][1]), most(s[0][2], s[0][3])), most(most(s[1][0], s[1][1]), most(s[1][2], s[1][3])));
 }
 
-// Four dims of column c: the waves' results joined, NaN values of the tokens that its
+// N dims of column c from d on: the waves' results joined, NaN values of the tokens that its
 // node does see put back (the steps cleared them), and stored, or kept for the join of
 // the chunks.
-template <typename T, int HD, int W>
-__device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W], const float (&sum)[W], const f32x4_t (&acc)[W],
-                                           uint32_t c, int d, int rep, int kvh, int r0, int ctx0, int split, int c0, int c1,
-                                           bool fix, const int32_t* tab) {
+template <typename T, int HD, int W, int N>
+__device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W], const float (&sum)[W],
+                                           const float* (&acc)[W], uint32_t c, int d, int rep, int kvh, int r0, int ctx0, int split,
+                                           int c0, int c1, bool fix, const int32_t* tab) {
   const int node = (int)(c / (uint32_t)rep), head = kvh * rep + (int)(c - (uint32_t)node * rep);
   float M = ml[0];
 #pragma unroll
   for (int w = 1; w < W; ++w) M = fmaxf(M, ml[w]);
-  float L = 0.f;
-  f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float L = 0.f, o[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) o[e] = 0.f;
 #pragma unroll
   for (int w = 0; w < W; ++w) {                         // a wave without steps has weight 0
     const float f = ml[w] == M ? 1.f : __builtin_amdgcn_exp2f(ml[w] - M);
     L += f * sum[w];
-    o += f * acc[w];
+    float x[N];
+    ld_elems<N, true>(acc[w] + d, x);
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] += f * x[e];
   }
   if (fix && ctx0 + node >= 0) {
     const uint64_t* mask = A.mask + (int64_t)(r0 + node) * A.words;
@@ -172,18 +176,18 @@ __device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W
       if (b < 0) continue;                              // its scores are NaN
       const uint8_t* v = A.c.v + (int64_t)b * (16 * HD) + (t >> 2 & 3) * (4 * HD) + d * 4 + (t & 3);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < N; ++e)
         if ((v[4 * e] & 0x7F) == 0x7F) o[e] = __uint_as_float(0x7FC00000u);
     }
   }
   if (A.plan.n_split == 1) {
     const float inv = L == 0.f ? 0.f : 1.0f / L;        // 0: the row sees nothing
-    const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    st_elems<4, true>((T*)A.out + ((int64_t)(r0 + node) * A.n_q + head) * HD + d, v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] *= inv;
+    st_elems<N, true>((T*)A.out + ((int64_t)(r0 + node) * A.n_q + head) * HD + d, o);
   } else {
     const int64_t slot = ((int64_t)(r0 + node) * A.plan.n_split + split) * A.n_q + head;
-    const float v[4] = {o[0], o[1], o[2], o[3]};
-    if (c0 < c1) st_elems<4, true>(A.part_o + slot * HD + d, v);
+    if (c0 < c1) st_elems<N, true>(A.part_o + slot * HD + d, o);
     if (d == 0) {
       A.part_ml[2 * slot] = M;
       A.part_ml[2 * slot + 1] = L;
@@ -393,19 +397,18 @@ __global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_
   bool fix = false;
 #pragma unroll
   for (int w = 0; w < W; ++w) fix |= sNan[w] != 0;
-  for (int i = tid; i < 16 * (HD / 4); i += 64 * W) {
-    const int h = i / (HD / 4), d = i % (HD / 4) * 4;
-    if (col0 + h >= cols) break;
-    float ml[W], sum[W];
-    f32x4_t acc[W];
+  constexpr int N = 16 * HD / (64 * W);
+  const int h = tid / (HD / N), d = tid % (HD / N) * N;
+  if (col0 + h >= cols) return;
+  float ml[W], sum[W];
+  const float* acc[W];
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      ml[w] = sM[w][h];
-      sum[w] = sL[w][h];
-      acc[w] = *reinterpret_cast<const f32x4_t*>(&sO[w][h][d]);
-    }
-    tree_store<T, HD, W>(A, ml, sum, acc, col0 + h, d, rep, kvh, r0, ctx0, split, c0, c1, fix, tab);
+  for (int w = 0; w < W; ++w) {
+    ml[w] = sM[w][h];
+    sum[w] = sL[w][h];
+    acc[w] = sO[w][h];
   }
+  tree_store<T, HD, W, N>(A, ml, sum, acc, col0 + h, d, rep, kvh, r0, ctx0, split, c0, c1, fix, tab);
 }
 
 // A wave per row and head joins the chunks' partial results in order; a chunk that
