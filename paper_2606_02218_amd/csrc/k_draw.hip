@@ -9,7 +9,7 @@
 //
 // A vocabulary has as many places where a draw turns on the running sum, so that sums
 // which are 1e-8 off, as those of fp32 weights are, draw another token in one row of a
-// thousand.  Weights are therefore fp64, by a polynomial of their own (exp2_64, 1e-12):
+// thousand.  Weights are therefore fp64, by a polynomial of their own (Exp2, 1e-12):
 // 14 instructions a token, which still fit under the bytes of fp32 logits.  Where
 // something is cut the weights are whole numbers, w 2^42 to nearest: their sums do not
 // depend on any order, so atomics give the same draw on every run.
@@ -42,13 +42,14 @@ typedef unsigned long long u64;
 
 constexpr int SEG = 512;              // tokens of a segment
 constexpr int MAX_SEGS = 2048;        // of a row: 2^20 tokens
-constexpr int STRIP = 64;              // tokens of a strip
+constexpr int STRIP = 64;             // tokens of a strip
 constexpr int STRIPS = SEG / STRIP;
 constexpr int STEPS = 512;            // that the octaves are told apart in for top-k
 constexpr int SCAN_WAVES = 4;
-constexpr int SCAN_FILL = 32768;        // waves of the scan, where there are segments for so many
+constexpr int SCAN_FILL = 32768;      // waves of the scan, where there are segments for so many
 constexpr int PART = 256;             // threads of a part of a row's histogram
-constexpr int PICK = 512;             // threads of a row's pick: 8, 64 and 505 rows 12, 19, 16 us; 256 threads 16, 23, 18; 1024 12, 21, 27
+// threads of a row's pick: 8, 64 and 505 rows take 12, 19, 16 us; by 256 threads 16, 23, 18; by 1024 12, 21, 27
+constexpr int PICK = 512;
 constexpr int BINS = 1024;            // of z, 16 an octave of weight
 constexpr int LIST = 4096;            // tokens that a row's list holds
 constexpr int ID_BITS = 20;
@@ -102,7 +103,8 @@ struct Exp2 {
       asm("" : "+s"(a[i]));
     }
   }
-  static constexpr double SHIFTER = 6755399441055744.0;       // 1.5 * 2^52: low bits of a sum with it are the other part's, to nearest
+  static constexpr double SHIFTER = 6755399441055744.0;       // 1.5 * 2^52: the low bits of a sum with it are
+                                                               // the other part, to nearest
   // 2^f times 2 to the whole number in the low bits of s
   __device__ __forceinline__ double at(double f, double s) const {
     double p = __builtin_bit_cast(double, a[0]);
@@ -130,13 +132,16 @@ __device__ __forceinline__ u64 fixed_of(double w) {
 // NaN where either is.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// Another lane's value, for sums of which the last lane of some alone is of use: past a
-// row's end, and for rows without a source, 0.
-template <int CTRL>
-__device__ __forceinline__ double moved(double v) {
-  const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
-  return __builtin_bit_cast(double, u32x2_t{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, 0xf, 0xf, true),
-                                            (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, 0xf, 0xf, true)});
+// A value of another lane, 0 where there is none or the lane's row of 16 is not in ROWS.
+template <int CTRL, int ROWS, typename V>
+__device__ __forceinline__ V shifted(V v) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, true));
+  } else {
+    const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+    return __builtin_bit_cast(V, u32x2_t{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, ROWS, 0xF, true),
+                                         (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, ROWS, 0xF, true)});
+  }
 }
 // Maxima over lanes go by whole numbers in the order of z, NaN above all: one lane move
 // and comparison a step.
@@ -151,16 +156,6 @@ template <int CTRL>
 __device__ __forceinline__ int max_moved(int v) {
   return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false));
 }
-__device__ __forceinline__ float max_nan_wave(float z) {
-  int v = rank_of(z);
-  v = max_moved<0x111>(v);
-  v = max_moved<0x112>(v);
-  v = max_moved<0x114>(v);
-  v = max_moved<0x118>(v);
-  v = max_moved<0x142>(v);
-  v = max_moved<0x143>(v);
-  return of_rank(__builtin_amdgcn_readlane(v, 63));
-}
 // Eight tokens of a row from the i-th on; -inf past its end.
 template <typename T, bool VEC>
 struct Eight {
@@ -168,7 +163,8 @@ struct Eight {
   vec t;
   __device__ __forceinline__ void load_whole(const T* p) { t = *reinterpret_cast<const vec*>(p); }
   __device__ __forceinline__ void load(const T* p, int i, int n) {
-    t = (vec)(sizeof(T) == 2 ? (T)0xFF80 : (T)-INFINITY);
+    if constexpr (sizeof(T) == 2) t = (vec)(T)0xFF80;
+    else t = (vec)-INFINITY;
     if (i >= n) return;
     if (VEC && i + 8 <= n) {
       t = *reinterpret_cast<const vec*>(p + i);
@@ -186,7 +182,9 @@ struct Eight {
 
 // Where 2^(z c) of a segment's tokens is not out of all bounds, their weights are taken with
 // respect to the whole octave next to the maximum's m c, else to m itself.
-__device__ __forceinline__ bool by_octave(float m, double c) { return fabs((double)m * c) < 1024.0 && c > 1e-30 && fabsf(m) < 1e38f; }
+__device__ __forceinline__ bool by_octave(float m, double c) {
+  return fabs((double)m * c) < 1024.0 && c > 1e-30 && fabsf(m) < 1e38f;
+}
 // A segment's weight with respect to the row's maximum.
 __device__ __forceinline__ double share_of(const Exp2& exp2, float m, double s, float zmax, double c) {
   if (m == -INFINITY) return 0.0;
@@ -195,11 +193,16 @@ __device__ __forceinline__ double share_of(const Exp2& exp2, float m, double s, 
 }
 
 // ---------------------------------------------------------------- scan
-// A wave goes through `per` pairs of segments, the next pair on its way all the time.  The
-// code is kept small here and below: each kernel starts with none of it in the instruction
-// cache, and lines that are run once cost more than what is in them.
+// A wave goes through `per` pairs of segments, whose loads are on their way together; the
+// halves of the wave then take the pair's lane moves.  The code is kept small here and below:
+// each kernel starts with none of it in the instruction cache, and lines that are run once
+// cost more than what is in them (the pick of 505 rows 35 us with 94 KB of code, 22 with 39).
+// 512 rows of 151936 fp32 logits 60 us, 5.2 TB/s: fp64 instructions, 14 a token, take as long
+// as the read; 64 rows of 152064 bf16 ones 12 us, those alone.
+// The next pair held in registers ahead 64 us, segments one by one 70.
 template <typename T, bool VEC, bool CUT>
-__global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int segs, unsigned per_row, unsigned items, unsigned per) {
+__global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int segs, unsigned per_row, unsigned items,
+                                                                 unsigned per) {
   const int lane = threadIdx.x & 63;
   unsigned item = (blockIdx.x * SCAN_WAVES + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * per;
   if (item >= items) return;
@@ -286,11 +289,11 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void k_draw_scan(DrawArgs A, int s
     const auto low = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
     const auto high = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
     double all = __builtin_bit_cast(double, u32x2_t{low[0], high[0]}) + __builtin_bit_cast(double, u32x2_t{low[1], high[1]});
-    all += moved<0x111>(all);
-    all += moved<0x112>(all);
-    all += moved<0x114>(all);
-    all += moved<0x118>(all);
-    all += moved<0x142>(all);
+    all += shifted<0x111, 0xF>(all);
+    all += shifted<0x112, 0xF>(all);
+    all += shifted<0x114, 0xF>(all);
+    all += shifted<0x118, 0xF>(all);
+    all += shifted<0x142, 0xF>(all);
     const int half = lane >> 5;
     if ((lane & 31) == 31 && s + half < segs) {
       A.seg_m[at + half] = half ? m[1] : m[0];
@@ -340,17 +343,6 @@ struct Places {
   }
 };
 
-// A value of another lane, 0 where there is none or the lane's row of 16 is not in ROWS.
-template <int CTRL, int ROWS, typename V>
-__device__ __forceinline__ V shifted(V v) {
-  if constexpr (sizeof(V) == 4) {
-    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, true));
-  } else {
-    const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
-    return __builtin_bit_cast(V, u32x2_t{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, ROWS, 0xF, true),
-                                         (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, ROWS, 0xF, true)});
-  }
-}
 template <typename V>
 __device__ __forceinline__ V wave_prefix(V v) {                      // inclusive
   v += shifted<0x111, 0xF>(v);
@@ -437,7 +429,8 @@ struct Row {
   bool good;                          // whether it has an answer
 };
 template <int N>
-__device__ __forceinline__ Row read_row(const DrawArgs& A, const Exp2& exp2, int r, int segs, const RowOpts& o, double* red, int* redi) {
+__device__ __forceinline__ Row read_row(const DrawArgs& A, const Exp2& exp2, int r, int segs, const RowOpts& o, double* red,
+                                        int* redi) {
   const float* top = A.seg_m + (int64_t)r * segs;
   const double* sum = A.seg_s + (int64_t)r * segs;
   const int tid = threadIdx.x;
@@ -481,7 +474,8 @@ __device__ __forceinline__ float least_of_mass(const DrawArgs& A, const Exp2& ex
 #pragma unroll 1
   for (int round = 0; round < 4; ++round) {
     __syncthreads();
-    const float step = (hi - lo) * (1.f / (W + 1)), y = lo + step * (float)(wave + 1), cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
+    const float step = (hi - lo) * (1.f / (W + 1)), y = lo + step * (float)(wave + 1);
+    const float cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
     double below = 0.0;
 #pragma unroll 2
     for (int i = lane; i < segs; i += 64) below += M.down[i] <= y ? fminf(M.share[i], cap) : M.share[i];
@@ -683,8 +677,8 @@ struct PlainMemory {
   int redi[N / 64];
 };
 template <int N, typename T, bool VEC>
-__device__ __forceinline__ void draw_plain(const DrawArgs& A, PlainMemory<N>& P, int r, int segs, const Row& w, const Logits<T, VEC>& z,
-                                           const RowOpts& o, double u) {
+__device__ __forceinline__ void draw_plain(const DrawArgs& A, PlainMemory<N>& P, int r, int segs, const Row& w,
+                                           const Logits<T, VEC>& z, const RowOpts& o, double u) {
   const float* top = A.seg_m + (int64_t)r * segs;
   const double* sum = A.seg_s + (int64_t)r * segs;
   const int tid = threadIdx.x;
@@ -893,8 +887,8 @@ __device__ __forceinline__ void compare(CutMemory<N>& C, int n, int& rank, u64& 
 // kept, 0 if all of them are; mass: the weight up to it.  Windows of places, ever finer by
 // 1024, until what is left can be compared.
 template <typename P, int N, typename R, typename Each>
-__device__ __forceinline__ u64 find_border(const R& row, CutMemory<N>& C, const Each& each, int n, bool by_rank, double limit, u64 lo,
-                                           u64 hi, u64 mass0, u64* mass) {
+__device__ __forceinline__ u64 find_border(const R& row, CutMemory<N>& C, const Each& each, int n, bool by_rank, double limit,
+                                           u64 lo, u64 hi, u64 mass0, u64* mass) {
   constexpr int FEW = CutMemory<N>::FEW, PER = BINS / N;
   const int tid = threadIdx.x;
   u64 rank0 = 0;                      // before the window
@@ -1166,7 +1160,9 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
 int segments(int vocab) { return (vocab + SEG - 1) / SEG; }
 
 // Whether rows may be cut, and whether some may go by histogram.
-bool may_cut(const DrawArgs& a) { return a.top_k_rows || a.top_p_rows || a.min_p_rows || a.top_k > 0 || a.top_p < 1.0 || a.min_p > 0.0; }
+bool may_cut(const DrawArgs& a) {
+  return a.top_k_rows || a.top_p_rows || a.min_p_rows || a.top_k > 0 || a.top_p < 1.0 || a.min_p > 0.0;
+}
 bool may_bin(const DrawArgs& a) {
   return (a.top_k_rows || a.top_k == 0 || a.top_k >= a.vocab) && (a.top_p_rows || a.min_p_rows || a.top_p < 1.0 || a.min_p > 0.0);
 }
@@ -1203,15 +1199,15 @@ hipError_t run(const DrawArgs& a, hipStream_t st) {
   const int64_t items = (int64_t)a.rows * per_row;
   if (items > INT32_MAX / 2 || (int64_t)a.rows * parts > INT32_MAX) return hipErrorInvalidValue;
   const int64_t per = std::max<int64_t>(1, items / SCAN_FILL), waves = (items + per - 1) / per;
-  const dim3 scan((unsigned)((waves + SCAN_WAVES - 1) / SCAN_WAVES)), part((unsigned)(a.rows * parts)), rows(a.rows);
+  const dim3 grid((unsigned)((waves + SCAN_WAVES - 1) / SCAN_WAVES)), scan(64 * SCAN_WAVES);
+  const dim3 part((unsigned)(a.rows * parts)), rows(a.rows);
+  const unsigned n = (unsigned)items, each = (unsigned)per;
   hipError_t e;
   if (!may_cut(a)) {
-    if ((e = kv8_launch(k_draw_scan<T, VEC, false>, scan, dim3(64 * SCAN_WAVES), st, a, segs, per_row, (unsigned)items, (unsigned)per)) != hipSuccess)
-      return e;
+    if ((e = kv8_launch(k_draw_scan<T, VEC, false>, grid, scan, st, a, segs, per_row, n, each)) != hipSuccess) return e;
     return kv8_launch(k_draw_plain<T, VEC>, rows, dim3(PART), st, a, segs);
   }
-  if ((e = kv8_launch(k_draw_scan<T, VEC, true>, scan, dim3(64 * SCAN_WAVES), st, a, segs, per_row, (unsigned)items, (unsigned)per)) != hipSuccess)
-    return e;
+  if ((e = kv8_launch(k_draw_scan<T, VEC, true>, grid, scan, st, a, segs, per_row, n, each)) != hipSuccess) return e;
   if (a.bins) {
     if ((e = kv8_launch(k_draw_bins<T, VEC>, part, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;
     if ((e = kv8_launch(k_draw_collect<T, VEC>, part, dim3(PART), st, a, segs, parts)) != hipSuccess) return e;

@@ -80,13 +80,15 @@ __global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ par
 // Scores are formed transposed, S^T = K Q^T, so that a lane ends up with the
 // probabilities of one column for just those tokens whose V^T operand it loads.
 // Every node sees the context: only steps that reach into the tree are masked.
-// What bounds it: matrix and vector instructions, which take the units in turn.  A step of 32
-// tokens x 16 columns x 128 dims is 16 MFMAs, 64 conversions of codes and some 80 others,
-// about 1200 clocks a wave at four waves a SIMD, and a wave's start and end weigh as much as
-// eight steps.  Tried at 64 trees of 4 to 63 nodes over 512 to 4500 tokens, 12 heads (83 us):
-// 32 columns a wave 84 us (two waves a SIMD), four waves of 16 columns over codes that
-// come straight into LDS once 89 us (its barriers cost what the shared loads save), keys as
-// e4m3 operands beside queries in two e4m3 pieces 84 us.
+// What bounds it: vector issue, and the caches' lines.  A step of 32 tokens x 16 columns x
+// 128 dims is 16 MFMAs, 64 conversions of codes and some 60 others, and a wave's start and
+// end weigh as much as eight steps.  64 trees of 4 to 63 nodes over 512 to 4500 tokens, 12
+// heads, 83 us (0.43 PFLOP/s): 1400 clocks of a SIMD a step, vector instructions in 55 % of
+// them, MFMAs busy in 18 %, three waves a SIMD that wait for memory 40 % of their time.
+// Tried there: 32 columns a wave 84 us (two waves a SIMD); four waves of 16 columns, and two
+// or four halves of the tokens, over codes that come straight into LDS once 89 and 93 (the
+// longest context's chain, and barriers); keys as e4m3 operands beside queries in two e4m3
+// pieces 84; every line of a later step touched ahead 108, of a quarter of the steps 86.
 constexpr int tree_pieces(int size) { return size == 2 ? 1 : 3; }   // bf16 pieces of a query and of a probability
 constexpr int tree_waves(int size, int hd) { return size == 2 || hd == 64 ? 4 : 3; }   // of a SIMD, by the registers
 
