@@ -19,7 +19,7 @@
 //   to it; maxima of strips of 64.  It streams the logits once.
 // * where nothing can be cut: plain, a workgroup a row.  The segment at which the running
 //   sum passes, then the token.
-// * only where top-p or min-p may cut a row without top-k: bins and collect (some workgroups
+// * only where top-p, or min-p in few rows, may cut more than 4096 tokens without top-k: bins and collect (some workgroups
 //   a row, each a part of it).  The bins find the row's sum and the least z that can be
 //   kept, and add up weights by z; collect finds the bin in which the border of top-p lies,
 //   sums what each part keeps above it, and lists the tokens in it.
@@ -50,8 +50,9 @@ constexpr int SCAN_FILL = 32768;      // waves of the scan, where there are segm
 constexpr int PART = 256;             // threads of a part of a row's histogram
 // threads of a row's pick: 8, 64 and 505 rows take 12, 19, 16 us; by 256 threads 16, 23, 18; by 1024 12, 21, 27
 constexpr int PICK = 512;
-constexpr int BINS = 1024;            // of z, 16 an octave of weight
+constexpr int BINS = 1024;            // of z in a row's histogram
 constexpr int LIST = 4096;            // tokens that a row's list holds
+constexpr int ROWS_FULL = 256;        // rows that keep the chip busy, a workgroup each
 constexpr int ID_BITS = 20;
 constexpr double LOG2E = 1.4426950408889634;
 constexpr double FIXED_ONE = 4398046511104.0;   // 2^42
@@ -177,6 +178,19 @@ struct Eight {
   __device__ __forceinline__ float operator[](int e) const {
     const T x = t[e];
     return ld_f32<T>(&x);
+  }
+  // a bit for each that is t0 or more; tokens past the vocabulary are -inf
+  __device__ __forceinline__ uint32_t from(float t0) const {
+    uint32_t hits = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) hits |= (uint32_t)((*this)[e] >= t0 && (*this)[e] > -INFINITY) << e;
+    return hits;
+  }
+  __device__ __forceinline__ float at(int k) const {
+    float x = (*this)[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) x = e == k ? (*this)[e] : x;
+    return x;
   }
 };
 
@@ -397,15 +411,22 @@ __device__ __forceinline__ V lane_of(V v, int lane) {
 __device__ __forceinline__ int first_lane(uint64_t mask) { return __ffsll((unsigned long long)mask) - 1; }
 __device__ __forceinline__ int last_lane(uint64_t mask) { return 63 - __clzll((long long)mask); }
 
-// Bin of z, 16 an octave of weight: falls as z grows.
-__device__ __forceinline__ int bin_of(float z, float zmax, float c) {
-  return (int)fminf(((zmax - z) * c) * 16.f, (float)(BINS - 1));
+// Bin of z: falls as z grows.  The bins share out what lies between t0 and the maximum, and
+// hold a sixteenth of an octave of weight at most.
+__device__ __forceinline__ float bins_per_logit(float zmax, float t0, float c) {
+  return fminf(fmaxf(16.f * c, (float)(BINS - 1) / (zmax - t0)), 3.0e38f);
 }
+__device__ __forceinline__ int bin_of(float z, float zmax, float per) { return (int)fminf((zmax - z) * per, (float)(BINS - 1)); }
 __device__ __forceinline__ float bin_factor(double c) { return (float)fmin(c, 3.0e38); }
 // Weight, or u of it, at which top-p ends: the first token is always kept.
 __device__ __forceinline__ double mass_limit(const RowOpts& o, double all) { return fmax((double)o.top_p * all, 0.5); }
-// Which rows go by histogram: top-k's are few and the pick finds them alone.
-__device__ __forceinline__ bool by_bins(const RowOpts& o) { return o.temperature != 0.0 && !o.by_k && (o.by_p || o.by_min); }
+// Which rows go by histogram: top-k's tokens are few, and so are a small vocabulary's; the
+// pick finds their border alone.  min-p's is known, and what it leaves takes one workgroup a
+// row as long as several where it is most of the row (64 rows of 152064: 77 us, by parts 43),
+// unless there are rows enough (500 of 50257: 96, 116).
+__device__ __forceinline__ bool by_bins(const RowOpts& o, const DrawArgs& A) {
+  return o.temperature != 0.0 && !o.by_k && A.vocab > LIST && (o.by_p || (o.by_min && A.rows < ROWS_FULL));
+}
 // min-p's border: the least fp32 value that is not below max z + T ln(min_p).
 __device__ __forceinline__ float min_p_border(const RowOpts& o, float zmax) {
   const double lowest = (double)zmax + o.temperature * log(fmin(o.min_p, 1.0));
@@ -491,21 +512,19 @@ __device__ __forceinline__ float least_of_mass(const DrawArgs& A, const Exp2& ex
   return octaves_below(w.zmax, hi, o.c);
 }
 
-// The least z that top-k can keep: k of the n maxima `of` (segments' or strips') reach it.
-// By a workgroup of N threads, which counts them by their distance from the top.
-template <int N>
-__device__ __forceinline__ float least_of(const float* of, int n, int k, float zmax, double c, uint32_t (&count)[STEPS], int* red) {
+// The least z that top-k can keep: k values reach it of those that `each` gives a workgroup
+// of N threads, maxima or the tokens' own.  They are counted by their distance from the top.
+template <int N, typename Each>
+__device__ __forceinline__ float least_of(const Each& each, int k, float zmax, double c, uint32_t (&count)[STEPS], int* red) {
   constexpr int PER = STEPS > N ? STEPS / N : 1;
   const int tid = threadIdx.x;
-  const float cf = bin_factor(c);
-  if (k > n) return octaves_below(zmax, FIXED_OCTAVES, c);
+  const float per = bin_factor(c) * (STEPS / FIXED_OCTAVES);
   for (int i = tid; i < STEPS; i += N) count[i] = 0;
   __syncthreads();
-#pragma unroll 4
-  for (int i = tid; i < n; i += N) {
-    const float step = (zmax - of[i]) * cf * (STEPS / FIXED_OCTAVES);
+  each([&](float z) {
+    const float step = (zmax - z) * per;
     if (step < (float)STEPS) atomicAdd(&count[(int)step], 1u);
-  }
+  });
   __syncthreads();
   uint32_t sum = 0, all;
   if (tid * PER < STEPS)
@@ -604,17 +623,10 @@ struct Logits {
         for (int e = 0; e < 8; ++e)
           if (v[e] >= t0 && v[e] > -INFINITY) f(v[e], first + e);   // tokens past the vocabulary are -inf
       } else {
-        uint32_t hits = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) hits |= (uint32_t)(v[e] >= t0 && v[e] > -INFINITY) << e;
 #pragma unroll 1
-        while (hits) {
+        for (uint32_t hits = v.from(t0); hits; hits &= hits - 1) {
           const int at = __ffs((int)hits) - 1;
-          hits &= hits - 1;
-          float x = v[0];
-#pragma unroll
-          for (int e = 1; e < 8; ++e) x = e == at ? v[e] : x;
-          f(x, first + at);
+          f(v.at(at), first + at);
         }
       }
     });
@@ -736,7 +748,7 @@ __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int pa
   __shared__ int redi[PART / 64];
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
-  if (!by_bins(o)) return;
+  if (!by_bins(o, A)) return;
   const Exp2 exp2;
   const Row w = read_row<PART>(A, exp2, r, segs, o, red, redi);
   float t0 = 0.f;
@@ -749,11 +761,11 @@ __global__ __launch_bounds__(PART) void k_draw_bins(DrawArgs A, int segs, int pa
   __syncthreads();
   for (int i = tid; i < BINS; i += PART) L.mass[i] = 0;
   __syncthreads();
-  const float c = bin_factor(o.c);
+  const float per = bins_per_logit(w.zmax, t0, bin_factor(o.c));
   const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, w.zmax, o.c, exp2};
   z.template tokens<PART, true>(A.strip_m + (int64_t)r * segs * STRIPS, t0, part_start(part, segs, parts) * STRIPS,
                                 part_start(part + 1, segs, parts) * STRIPS,
-                                [&](float x, int) { atomicAdd(&L.mass[bin_of(x, w.zmax, c)], z.fixed(x)); });
+                                [&](float x, int) { atomicAdd(&L.mass[bin_of(x, w.zmax, per)], z.fixed(x)); });
   __syncthreads();
   u64* bins = A.part_bins + (int64_t)blockIdx.x * BINS;
 #pragma unroll 1
@@ -770,7 +782,7 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
   __shared__ int redi[8], n_list, at;
   const int r = blockIdx.x / parts, part = blockIdx.x - r * parts, tid = threadIdx.x;
   const RowOpts o = row_opts(A, r);
-  if (!by_bins(o)) return;
+  if (!by_bins(o, A)) return;
   const DrawRow info = A.info[r];
   if (!info.good) return;
   if (tid == 0) n_list = 0;
@@ -781,28 +793,25 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
     mine[i] = A.bins[(int64_t)r * BINS + tid * PER + i];
     own[i] = A.part_bins[(int64_t)blockIdx.x * BINS + tid * PER + i];
   }
-  int border = BINS;                  // the bin in which top-p's border lies
-  if (o.by_p) {
-    const double limit = mass_limit(o, info.total * FIXED_ONE);
-    u64 sum = 0;
+  const double limit = mass_limit(o, info.total * FIXED_ONE);
+  u64 sum = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += mine[i];
-    u64 end = group_prefix<PART>(sum, red, &all);
-    int hit = BINS;
-    u64 before = end;
+  for (int i = 0; i < PER; ++i) sum += mine[i];
+  u64 end = group_prefix<PART>(sum, red, &all);
+  int hit = BINS;
+  u64 before = end;
 #pragma unroll
-    for (int i = PER - 1; i >= 0; --i) {
-      if (mine[i] && (double)end >= limit) {
-        hit = tid * PER + i;
-        before = end - mine[i];
-      }
-      end -= mine[i];
+  for (int i = PER - 1; i >= 0; --i) {
+    if (o.by_p && mine[i] && (double)end >= limit) {
+      hit = tid * PER + i;
+      before = end - mine[i];
     }
-    border = group_min<PART>(hit, redi);
-    if (part == 0 && hit == border && border < BINS) {
-      A.info[r].bin = border;
-      A.info[r].above = before;
-    }
+    end -= mine[i];
+  }
+  const int border = group_min<PART>(hit, redi);   // the bin in which top-p's border lies
+  if (part == 0 && hit == border && border < BINS) {
+    A.info[r].bin = border;
+    A.info[r].above = before;
   }
 #pragma unroll
   for (int i = 0; i < PER; ++i)
@@ -810,12 +819,12 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
   group_prefix<PART>(kept, red, &all);
   if (tid == 0) A.part_kept[blockIdx.x] = all;
   if (border == BINS) return;
-  const float c = bin_factor(o.c);
+  const float per = bins_per_logit(info.zmax, info.t0, bin_factor(o.c));
   const Exp2 exp2;
   const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, info.zmax, o.c, exp2};
   z.template tokens<PART, true>(A.strip_m + (int64_t)r * segs * STRIPS, info.t0, part_start(part, segs, parts) * STRIPS,
                           part_start(part + 1, segs, parts) * STRIPS, [&](float x, int id) {
-                            if (bin_of(x, info.zmax, c) != border) return;
+                            if (bin_of(x, info.zmax, per) != border) return;
                             const int k = atomicAdd(&n_list, 1);
                             if (k < LIST) list[k] = Places<T>::of(x, id);
                           });
@@ -979,7 +988,7 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const RowOpts o = row_opts(A, r);
   const double u = given_u(A, r);
-  const bool binned = by_bins(o);
+  const bool binned = by_bins(o, A);
   const Exp2 exp2;
   DrawRow info{};
   Row w;
@@ -996,7 +1005,7 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
     return;
   }
   const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, w.zmax, o.c, exp2};
-  if (!binned && (o.temperature == 0.0 || !o.by_k)) {   // nothing is cut here
+  if (o.temperature == 0.0 || !(o.by_k || o.by_p || o.by_min)) {   // nothing is cut here
     draw_plain<N>(A, C.plain, r, segs, w, z, o, u);
     return;
   }
@@ -1005,23 +1014,47 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
   const bool whole_list = binned && info.listed <= LIST;   // the border's bin is listed, the rest summed
   const int n_strips = segs * STRIPS;
   const float* const strip_m = A.strip_m + (int64_t)r * n_strips;
-  if (!binned) {
-    const bool many = 2 * o.top_k > segs;                  // for segments' maxima to tell
-    t0 = least_of<N>(many ? strip_m : A.seg_m + (int64_t)r * segs, many ? n_strips : segs, o.top_k, w.zmax, o.c, C.steps, C.redi);
-    if (!o.by_p) t0 = fmaxf(t0, min_z);                    // top-p takes its share of all the k
+  const bool known = !binned && !o.by_k && !o.by_p;        // the border: no list is needed
+  if (o.by_k) {
+    // segments' maxima tell where there are twice as many, else strips', else the tokens
+    const float far = octaves_below(w.zmax, FIXED_OCTAVES, o.c);
+    const bool coarse = 2 * o.top_k <= segs;
+    const int n = coarse ? segs : n_strips;
+    const float* const top = coarse ? A.seg_m + (int64_t)r * segs : strip_m;
+    t0 = least_of<N>(
+        [&](auto f) {
+          if (2 * o.top_k <= n) {
+#pragma unroll 4
+            for (int i = tid; i < n; i += N) f(top[i]);
+          } else {
+            z.template tokens<N, true>(strip_m, far, 0, n_strips, [&](float x, int) { f(x); });
+          }
+        },
+        o.top_k, w.zmax, o.c, C.steps, C.redi);
+  } else if (!binned) {
+    t0 = octaves_below(w.zmax, FIXED_OCTAVES, o.c);
   }
+  if (!binned && !(o.by_k && o.by_p)) t0 = fmaxf(t0, min_z);   // top-p takes its share of all the k
   if (tid == 0) {
-    C.n_list = whole_list ? info.listed : 0;
+    C.n_list = whole_list ? info.listed : known ? LIST + 1 : 0;
     C.lo = ~0ull;
     C.hi = 0;
   }
   __syncthreads();
   if (whole_list) {
     for (int i = tid; i < info.listed; i += N) C.list[i] = A.list[(int64_t)r * LIST + i];
-  } else {
-    z.template tokens<N, false>(strip_m, t0, 0, n_strips, [&](float x, int id) {
-      const int i = atomicAdd(&C.n_list, 1);
-      if (i < LIST) C.list[i] = P::of(x, id);
+  } else if (!known) {
+    z.template strips<N>(strip_m, t0, 0, n_strips, [&](const Eight<T, VEC>& v, int first) {
+      uint32_t hits = v.from(t0);
+      const int mine = __popc(hits), end = wave_prefix(mine);
+      int at = 0;
+      if (lane == 63) at = atomicAdd(&C.n_list, end);
+      at = __builtin_amdgcn_readlane(at, 63) + end - mine;
+#pragma unroll 1
+      for (; hits; hits &= hits - 1, ++at) {
+        const int e = __ffs((int)hits) - 1;
+        if (at < LIST) C.list[at] = P::of(v.at(e), first + e);
+      }
     });
   }
   __syncthreads();
@@ -1164,7 +1197,8 @@ bool may_cut(const DrawArgs& a) {
   return a.top_k_rows || a.top_p_rows || a.min_p_rows || a.top_k > 0 || a.top_p < 1.0 || a.min_p > 0.0;
 }
 bool may_bin(const DrawArgs& a) {
-  return (a.top_k_rows || a.top_k == 0 || a.top_k >= a.vocab) && (a.top_p_rows || a.min_p_rows || a.top_p < 1.0 || a.min_p > 0.0);
+  return a.vocab > LIST && (a.top_k_rows || a.top_k == 0 || a.top_k >= a.vocab) && 
+         (a.top_p_rows || a.top_p < 1.0 || (a.rows < ROWS_FULL && (a.min_p_rows || a.min_p > 0.0)));
 }
 
 // Parts of a row in the histogram: enough to fill the chip, of eight segments at least,

@@ -107,6 +107,36 @@ def test_largest_vocabulary_and_many_rows():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["peaked", "flat", "equal", "few values"])
+@pytest.mark.parametrize("rows,vocab", [(3, 4096), (3, 4097), (255, 4099), (257, 4099), (4, 20011)])
+def test_both_sides_of_each_choice(rows, vocab, kind, dtype):
+    """Lists and histograms, a workgroup a row and several, k by segments, strips and tokens."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(rows + vocab)
+    z = logits(rng, rows, vocab, kind, dtype)
+    for s in (dict(top_p=0.9), dict(min_p=0.02), dict(top_p=0.8, min_p=0.02), dict(top_k=4), dict(top_k=5, top_p=0.9),
+              dict(top_k=vocab // 128), dict(top_k=vocab // 128 + 1, min_p=0.05), dict(top_k=vocab // 64 + 40, top_p=0.95),
+              dict(top_k=vocab - 1)):
+        u = torch.from_numpy(rng.random(rows)).cuda()
+        check(z, u, rg.sample(z, u, **s), **s)
+
+
+@pytest.mark.parametrize("rows", [30, 300])
+def test_rows_that_go_different_ways(rows):
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(rows)
+    vocab = 4200
+    z = logits(rng, rows, vocab, "flat", BF16)
+    u = torch.from_numpy(rng.random(rows)).cuda()
+    some = lambda p, a, b: torch.from_numpy(np.where(rng.random(rows) < p, a, b))  # noqa: E731
+    s = dict(temperature=some(0.1, 0.0, rng.uniform(0.1, 2, rows)).float().cuda(),
+             top_k=some(0.5, 0, rng.integers(1, 4400, rows)).int().cuda(),
+             top_p=some(0.4, 1.0, rng.uniform(0.05, 1, rows)).float().cuda(),
+             min_p=some(0.5, 0.0, rng.uniform(0, 0.6, rows)).float().cuda())
+    check(z, u, rg.sample(z, u, **s), **s)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_settings_by_row_strides_and_repeats(dtype):
     import paper_2606_02218_amd as rg
     rng = np.random.default_rng(4)
