@@ -506,8 +506,9 @@ int rg_kv8_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32
  *   mask      DEVICE uint64 [rows, words]
  *   pos       DEVICE int32 [rows]
  * Padding rows, rows whose parent is not in [-1, i) and rows behind such a one
- * get an empty mask and position -1 (rg_rope makes that NaN).  RG_EINVAL for NULL
- * pointers, negative sizes, words outside [1, 64], n_seqs past 2^24. */
+ * get an empty mask and position -1 (rg_rope makes that NaN).  mask and pos overlap
+ * neither each other nor what the call reads.  RG_EINVAL for NULL pointers,
+ * negative sizes, words outside [1, 64], n_seqs past 2^24. */
 int rg_kv8_tree(const int32_t* parent, const int32_t* seq_off, const int32_t* seq_len, int32_t n_seqs, int32_t rows,
                 int32_t words, uint64_t* mask, int32_t* pos, void* stream);
 
@@ -584,6 +585,7 @@ int64_t rg_sample_scratch(int32_t rows, int32_t vocab, const rg_sample_options* 
  *             from (T = 0: 0)
  *   scratch   DEVICE, 16-byte aligned, of rg_sample_scratch() bytes, that nothing else
  *             uses until the call's kernels have run
+ * None of the last four overlaps another array of the call.
  * Tokens with logit -inf have weight 0 and are never drawn, nor are those below 2^-43
  * of the largest weight where something is cut.  A row with a NaN or +inf among its
  * logits, without any finite one, with u outside [0, 1), or with a temperature below

@@ -1258,7 +1258,7 @@ hipError_t launch_draw(DrawArgs a, void* scratch, hipStream_t st) {
   if (a.vocab < 1 || a.vocab > DRAW_MAX_VOCAB) return hipErrorInvalidValue;
   const Scratch s = scratch_of(a);
   char* p = (char*)scratch;
-  a.c = a.temperature == 0.0 ? LOG2E : LOG2E / a.temperature;
+  a.c = a.temperature == 0.0 ? LOG2E : std::min(LOG2E / a.temperature, 1e300);   // finite: 0 c is 0
   a.seg_s = (double*)(p + s.seg_s);
   a.seg_m = (float*)(p + s.seg_m);
   a.strip_m = (float*)(p + s.strip_m);

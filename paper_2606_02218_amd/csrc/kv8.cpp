@@ -234,8 +234,8 @@ int rg_kv8_tree(const int32_t* parent, const int32_t* seq_off, const int32_t* se
 
 int64_t rg_kv8_tree_attention_scratch(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t rows, int32_t n_seqs,
                                       int32_t words, int32_t max_len) {
-  if ((dtype != RG_DTYPE_F32 && dtype != RG_DTYPE_BF16) || n_q < 1 || n_kv < 1 || n_q % n_kv || n_q / n_kv > 128 || head_dim < 1 || rows < 0 ||
-      n_seqs < 0 || max_len < 1 || words < 1 || words > RG_KV8_TREE_WORDS)
+  if ((dtype != RG_DTYPE_F32 && dtype != RG_DTYPE_BF16) || n_q < 1 || n_kv < 1 || n_q % n_kv || n_q / n_kv > 128 ||
+      head_dim < 1 || rows < 0 || n_seqs < 0 || max_len < 1 || words < 1 || words > RG_KV8_TREE_WORDS)
     return bad("rg_kv8_tree_attention_scratch", "bad sizes");
   if (rows == 0 || n_seqs == 0) return 0;
   return 4 * kv8_tree_part_floats(rows, kv8_tree_plan(dtype, rows, n_seqs, n_q, n_kv, words, max_len), n_q, head_dim);

@@ -238,6 +238,26 @@ def test_extreme_temperatures_and_logits():
     check(big, u[:2], rg.sample(big, u[:2]))
 
 
+@pytest.mark.parametrize("vocab", [900, 5000])
+@pytest.mark.parametrize("s", [dict(), dict(top_k=3), dict(top_p=0.9), dict(min_p=0.5), dict(top_k=40, top_p=0.5, min_p=0.1)])
+def test_the_ends_of_temperature(s, vocab):
+    """1 / T past the largest double, and no logit telling from another."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(vocab)
+    z = logits(rng, 3, vocab, "flat", F32)
+    u = torch.from_numpy(rng.random(3)).cuda()
+    token, lp, kept = rg.sample(z, u, temperature=5e-324, **s)
+    assert torch.equal(token.long(), z.argmax(1)) and bool((lp == 0).all()) and bool((kept == 0).all())
+    z[:, :40] = z.amax(1, keepdim=True)    # of equal ones the u-th
+    token, lp, kept = rg.sample(z, u, temperature=5e-324)
+    for r in range(3):                     # the first 40 and, where it lies behind them, the row's largest itself
+        ids = (z[r] == z[r].max()).nonzero().flatten().tolist()
+        assert len(ids) in (40, 41) and token[r].item() == ids[int(u[r].item() * len(ids))]
+        assert abs(lp[r].item() + np.log(len(ids))) < 2.0 ** -22
+    z = logits(rng, 3, vocab, "flat", F32)
+    check(z, u, rg.sample(z, u, temperature=1.7e308, **s), temperature=1.7e308, **s)
+
+
 @pytest.mark.parametrize("s", [dict(), dict(top_k=20, top_p=0.9)])
 def test_graphs_and_streams(s):
     import paper_2606_02218_amd as rg
