@@ -130,6 +130,23 @@ def test_split_contexts(dtype, nodes, old):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hd,seqs", [(128, 40), (64, 64), (64, 65)])
+def test_more_than_a_round_of_workgroups(dtype, hd, seqs):
+    """Up to 64 sequences the longest go first, equal lengths and empty ones among them; past 64 in their order."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(seqs)
+    nodes = [int(n) for n in rng.integers(0, 60, seqs)]
+    old = [int(n) for n in rng.choice([0, 5, 130, 130, 301], seqs)]
+    b = Batch([a + c for a, c in zip(nodes, old)], 2, hd, 32, seed=seqs)
+    trees = [parents(n, "tree", b.rng) if n else np.zeros(0, int) for n in nodes]
+    mask, _ = all_masks(trees, 1, old, b.lengths())
+    assert sum(nodes) * 6 // 16 * 2 > 256
+    q = rounded(b.rng.normal(0, 1.5, (sum(nodes), 12, hd)), dtype)
+    out = rg.kv8_tree_attention(b.cache, dev(q, dtype), dev(b.tab), dev(b.lengths()), offsets(nodes), as_mask(mask), max_len=400)
+    check(b, q, nodes, mask, out, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_any_mask(dtype):
     """Masks that are no tree's: random bits, without the node itself, empty ones, bits past the nodes."""
     import paper_2606_02218_amd as rg
