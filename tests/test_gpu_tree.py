@@ -262,6 +262,100 @@ def test_output_in_the_queries_place():
         assert torch.equal(rg.kv8_tree_attention(b.cache, q, *args, out=q), want) and torch.equal(q, want)
 
 
+# ---------------------------------------------------------------- wide trees over long contexts: tiles of 128 rows
+LONG = 1 << 14                # a bound that asks for them, whatever the lengths, from 256 columns a sequence on
+
+
+@pytest.mark.parametrize("hd,n_kv,rep,nodes,old", [
+    (128, 1, 7, [64, 64], [9001, 37]), (128, 2, 7, [90, 1, 64], [100, 600, 2050]), (64, 2, 8, [64, 33, 0, 40], [0, 63, 7, 1200]),
+    (64, 1, 33, [33, 0, 17, 40], [7, 9, 100, 200]), (128, 1, 128, [5, 1, 9], [0, 63, 64]), (64, 1, 1, [512], [5000]),
+    (128, 1, 1, [300], [0]), (64, 3, 6, [65, 128, 3], [129, 0, 3000])])
+def test_wide_trees_over_long_contexts(hd, n_kv, rep, nodes, old):
+    import paper_2606_02218_amd as rg
+    assert sum(nodes) * rep / len(nodes) > 255
+    b = Batch([a + c for a, c in zip(nodes, old)], n_kv, hd, 16 if rep % 2 else 64, seed=hd + rep)
+    trees = [parents(n, "tree", b.rng) if n else np.zeros(0, int) for n in nodes]
+    mask, _ = all_masks(trees, words_of(nodes), old, b.lengths())
+    q = rounded(b.rng.normal(0, 1.5, (sum(nodes), n_kv * rep, hd)), BF16)
+    args = (b.cache, dev(q, BF16), dev(b.tab), dev(b.lengths()), offsets(nodes), as_mask(mask))
+    for bound in (LONG, 1 << 19):
+        out = rg.kv8_tree_attention(*args, max_len=bound)
+        check(b, q, nodes, mask, out, BF16)
+        assert all(torch.equal(out, rg.kv8_tree_attention(*args, max_len=bound)) for _ in range(2))
+    check(b, q, nodes, mask, rg.kv8_tree_attention(*args, max_len=LONG, scale=0.05), BF16, 0.05)
+
+
+def test_wide_trees_any_mask_padding_and_rows_of_nobody():
+    import paper_2606_02218_amd as rg
+    nodes, lens = [40, 9, 130, 60], [40, 4, 150, 0]              # 5 rows of the second are padding, all of the last
+    b = Batch(lens, 2, 64, 32, seed=5)
+    rows = sum(nodes) + 6
+    mask = b.rng.integers(0, 2 ** 63, (rows, 3)).astype(np.uint64) * np.uint64(2) + np.uint64(1)
+    mask[::5] = 0                                       # with no context these rows see nothing
+    mask[1::7] = np.uint64(2 ** 64 - 1)
+    q = rounded(b.rng.normal(0, 1.5, (rows, 10, 64)), BF16)
+    for words in (3, 1):
+        for cut in (0, -7):
+            n = b.lengths()
+            n[3] = cut
+            m = np.ascontiguousarray(mask[:, :words])
+            out = torch.full((rows, 10, 64), 9.0, device="cuda", dtype=BF16)
+            rg.kv8_tree_attention(b.cache, dev(q, BF16), dev(b.tab), dev(n), offsets(nodes), as_mask(m), out=out, max_len=LONG)
+            check(b, q, nodes, m, out, BF16)
+            got = host(out)
+            assert (got[-6:] == 9.0).all() and not got[179:239].any() and not got[40:45].any()
+            assert not got[[i for i in range(40) if i % 5 == 0 and i % 7 != 1]].any()
+
+
+@pytest.mark.parametrize("old", [45, 3000])
+def test_wide_trees_what_a_node_does_not_see(old):
+    """NaN codes in nodes, and pages outside the pool and the table."""
+    import paper_2606_02218_amd as rg
+    n, hd = 40, 64
+    b = Batch([old + n], 1, hd, 16, seed=8)
+    p = parents(n, "tree", b.rng)
+    mask, _ = tree.masks(p, 1, old)
+    q = rounded(b.rng.normal(0, 1.5, (n, 8, hd)), BF16)
+    args = (dev(q, BF16), dev(b.tab), dev(b.lengths()), offsets([n]), as_mask(mask))
+    clean = host(rg.kv8_tree_attention(b.cache, *args, max_len=LONG))
+    page, sub = b.places(0, -(-(old + n) // 16))
+    v, k = b.cache.v.view(torch.uint8), b.cache.k.view(torch.uint8)
+    sees = tree.seen(mask, old + n, n)
+    t = old + 11
+    for d in (5, 33):
+        v[int(page[t // 16]), 0, int(sub[t // 16]), (t % 16 // 4) * 4 * hd + d * 4 + t % 4] = 0x7F
+    out = host(rg.kv8_tree_attention(b.cache, *args, max_len=LONG))
+    rest = [d for d in range(hd) if d not in (5, 33)]
+    for i in range(n):
+        if sees[i, t]:
+            assert np.isnan(out[i][:, [5, 33]]).all() and np.array_equal(out[i][:, rest], clean[i][:, rest])
+        else:
+            assert np.array_equal(out[i], clean[i]), i
+    t = old + 7
+    k[int(page[t // 16]), 0, int(sub[t // 16]), (t % 16) * 16 + 9] = 0xFF
+    out2 = host(rg.kv8_tree_attention(b.cache, *args, max_len=LONG))
+    for i in range(n):
+        assert np.isnan(out2[i]).all() if sees[i, t] else np.array_equal(out2[i], out[i], equal_nan=True), i
+    for lost in (b.pages + 5, -3):
+        tab = b.tab.copy()
+        tab[0, (old + 30) // 16] = lost
+        hit = sees[:, (old + 30) // 16 * 16:(old + 30) // 16 * 16 + 16].any(1)
+        out3 = host(rg.kv8_tree_attention(b.cache, args[0], dev(tab), *args[2:], max_len=LONG))
+        for i in range(n):
+            assert np.isnan(out3[i]).all() if hit[i] else np.array_equal(out3[i], out2[i], equal_nan=True), i
+
+
+def test_wide_trees_in_the_queries_place():
+    import paper_2606_02218_amd as rg
+    for old, bound in ((50, LONG), (4000, LONG), (50, 8192)):
+        b = Batch([old + 30], 2, 128, 16, seed=old)
+        mask, _ = tree.masks(parents(30, "tree", b.rng), 1, old)
+        q = dev(rounded(b.rng.normal(0, 1.5, (30, 28, 128)), BF16), BF16)
+        args = (dev(b.tab), dev(b.lengths()), offsets([30]), as_mask(mask))
+        want = rg.kv8_tree_attention(b.cache, q, *args, max_len=bound)
+        assert torch.equal(rg.kv8_tree_attention(b.cache, q, *args, out=q, max_len=bound), want) and torch.equal(q, want)
+
+
 # ---------------------------------------------------------------- accepted paths
 def accepted(b, nodes, old, trees, last, words):
     """The oracle's caches after the accept; its lengths."""
