@@ -848,17 +848,13 @@ hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStr
   return w ? run<float, 128, OUT_F32>(a, st) : run<float, 64, OUT_F32>(a, st);
 }
 
-hipError_t launch_kv8_tree_tiles(int dtype, const Kv8Attn& a, hipStream_t st) {
+hipError_t launch_kv8_tree_tiles(const Kv8Attn& a, hipStream_t st) {
   const int np = KV8_TILE_Q / (a.n_q / a.c.n_kv);
   const int64_t grid = ((int64_t)a.b.rows / np + a.b.n_seqs) * a.c.n_kv * a.plan.n_split;
   if (grid > INT32_MAX || np < 1 || a.words > KV8_TREE_TILE_WORDS) return hipErrorInvalidValue;
   const dim3 g((unsigned)grid), t(64 * KV8_WAVES);
-  const bool w = a.c.hd == 128;
-  if (dtype == 1)
-    return w ? kv8_launch(k_kv8_tiles<bf16_t, 128, OUT_BF16, true>, g, t, st, a)
-             : kv8_launch(k_kv8_tiles<bf16_t, 64, OUT_BF16, true>, g, t, st, a);
-  return w ? kv8_launch(k_kv8_tiles<float, 128, OUT_F32, true>, g, t, st, a)
-           : kv8_launch(k_kv8_tiles<float, 64, OUT_F32, true>, g, t, st, a);
+  return a.c.hd == 128 ? kv8_launch(k_kv8_tiles<bf16_t, 128, OUT_BF16, true>, g, t, st, a)
+                       : kv8_launch(k_kv8_tiles<bf16_t, 64, OUT_BF16, true>, g, t, st, a);
 }
 
 hipError_t launch_kv8_merge(int dtype, bool planes, const Kv8Attn& a, hipStream_t st) {

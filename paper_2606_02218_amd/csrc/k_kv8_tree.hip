@@ -676,7 +676,7 @@ hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& t, hipStream_
     return hipErrorInvalidValue;
   const bool w = a.c.hd == 128;
   hipError_t e;
-  if (t.plan.tiles) e = launch_kv8_tree_tiles(dtype, a, st);
+  if (t.plan.tiles) e = launch_kv8_tree_tiles(a, st);
   else if (dtype == 1) e = w ? run<bf16_t, 128>(a, st) : run<bf16_t, 64>(a, st);
   else e = w ? run<float, 128>(a, st) : run<float, 64>(a, st);
   if (e != hipSuccess || a.plan.n_split == 1) return e;

@@ -469,8 +469,8 @@ struct Kv8TreeAttn {
 inline int64_t kv8_tree_part_floats(int64_t rows, const Kv8TreePlan& p, int n_q, int hd) {
   return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
 }
-// The tiles' pass over the cache; the tree's join has to follow where n_split > 1.
-hipError_t launch_kv8_tree_tiles(int dtype, const Kv8Attn& a, hipStream_t st);
+// The tiles' pass over the cache, bf16; the tree's join has to follow where n_split > 1.
+hipError_t launch_kv8_tree_tiles(const Kv8Attn& a, hipStream_t st);
 hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& a, hipStream_t st);
 // Moves the nodes of mask row last[s] behind the context; new_len: tokens then.
 hipError_t launch_kv8_accept(const Kv8Pool& c, const Kv8Rows& b, const uint64_t* mask, int words, const int32_t* last,
