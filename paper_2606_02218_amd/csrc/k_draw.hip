@@ -19,8 +19,8 @@
 //   to it; maxima of strips of 64.  It streams the logits once.
 // * where nothing can be cut: plain, a workgroup a row.  The segment at which the running
 //   sum passes, then the token.
-// * only where top-p, or min-p in few rows, may cut more than 4096 tokens without top-k: bins and collect (some workgroups
-//   a row, each a part of it).  The bins find the row's sum and the least z that can be
+// * only where top-p or min-p may cut rows without top-k that one workgroup would be slow
+//   at: bins and collect (some workgroups a row, each a part of it).  The bins find the row's sum and the least z that can be
 //   kept, and add up weights by z; collect finds the bin in which the border of top-p lies,
 //   sums what each part keeps above it, and lists the tokens in it.
 // * pick, a workgroup a row: the border, then where the running sum passes.
@@ -420,12 +420,19 @@ __device__ __forceinline__ int bin_of(float z, float zmax, float per) { return (
 __device__ __forceinline__ float bin_factor(double c) { return (float)fmin(c, 3.0e38); }
 // Weight, or u of it, at which top-p ends: the first token is always kept.
 __device__ __forceinline__ double mass_limit(const RowOpts& o, double all) { return fmax((double)o.top_p * all, 0.5); }
-// Which rows go by histogram: top-k's tokens are few, and so are a small vocabulary's; the
-// pick finds their border alone.  min-p's is known, and what it leaves takes one workgroup a
-// row as long as several where it is most of the row (64 rows of 152064: 77 us, by parts 43),
-// unless there are rows enough (500 of 50257: 96, 116).
+// Whether the pick deals with every row alone.  A small vocabulary's tokens are few.  Rows
+// enough for all units need no more workgroups, where the vocabulary is not so large that
+// one is slower at it (all rows by top-p: 512 rows of 5000 28 us, by several workgroups 41;
+// 300 of 32000 65, 60; 256 of 151936 177, 134), or some rows' top-k leaves it few of them
+// (505 rows of 32000, a tenth of them by top-p alone: 40, 51).
+__host__ __device__ __forceinline__ bool alone(const DrawArgs& A) {
+  return A.vocab <= LIST || (A.rows >= ROWS_FULL && A.vocab <= (A.top_k_rows ? 1 << 16 : 1 << 14));
+}
+// Which rows several workgroups look at, by a histogram.  top-k's tokens are few.  min-p's
+// border is known, but summing up what it leaves takes one workgroup a row long where that
+// is most of it (64 rows of 152064: 77 us, by several 43).
 __device__ __forceinline__ bool by_bins(const RowOpts& o, const DrawArgs& A) {
-  return o.temperature != 0.0 && !o.by_k && A.vocab > LIST && (o.by_p || (o.by_min && A.rows < ROWS_FULL));
+  return o.temperature != 0.0 && !o.by_k && (o.by_p || (o.by_min && A.rows < ROWS_FULL)) && !alone(A);
 }
 // min-p's border: the least fp32 value that is not below max z + T ln(min_p).
 __device__ __forceinline__ float min_p_border(const RowOpts& o, float zmax) {
@@ -474,13 +481,13 @@ __device__ __forceinline__ Row read_row(const DrawArgs& A, const Exp2& exp2, int
 // distance from the top, in octaves, and what is left between two of them is tried again.
 struct MassMemory {
   float share[MAX_SEGS], down[MAX_SEGS];
-  int pass[4];
+  int pass[8];
 };
 template <int N>
 __device__ __forceinline__ float least_of_mass(const DrawArgs& A, const Exp2& exp2, int r, int segs, const RowOpts& o, const Row& w,
                                                MassMemory& M) {
   constexpr int W = N / 64;
-  static_assert(W <= 4, "a flag a wave");
+  static_assert(W == 4 || W == 8, "a flag a wave, and about 700 steps in all");
   const float* top = A.seg_m + (int64_t)r * segs;
   const double* sum = A.seg_s + (int64_t)r * segs;
   const float cf = bin_factor(o.c);
@@ -493,7 +500,7 @@ __device__ __forceinline__ float least_of_mass(const DrawArgs& A, const Exp2& ex
     M.down[i] = (w.zmax - top[i]) * cf;
   }
 #pragma unroll 1
-  for (int round = 0; round < 4; ++round) {
+  for (int round = 0; round < (W == 4 ? 4 : 3); ++round) {
     __syncthreads();
     const float step = (hi - lo) * (1.f / (W + 1)), y = lo + step * (float)(wave + 1);
     const float cap = (float)SEG * __builtin_amdgcn_exp2f(-y);
@@ -847,6 +854,7 @@ struct CutMemory {
     u64 seg[MAX_SEGS];                // kept weight of each segment
     uint32_t steps[STEPS];
     PlainMemory<N> plain;
+    MassMemory least;
   };
   u64 list[LIST];                     // places of the tokens that can be kept
   Token few[FEW];
@@ -1014,7 +1022,11 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
   const bool whole_list = binned && info.listed <= LIST;   // the border's bin is listed, the rest summed
   const int n_strips = segs * STRIPS;
   const float* const strip_m = A.strip_m + (int64_t)r * n_strips;
-  const bool known = !binned && !o.by_k && !o.by_p;        // the border: no list is needed
+  bool known = !binned && !o.by_k && !o.by_p;              // the border: no list is needed
+  const bool own_bins = !binned && !o.by_k && o.by_p && A.vocab > LIST;
+  int bin = BINS;                                          // of those the one in which the border lies
+  float per = 0.f;
+  u64 above = whole_list ? info.above : 0;
   if (o.by_k) {
     // segments' maxima tell where there are twice as many, else strips', else the tokens
     const float far = octaves_below(w.zmax, FIXED_OCTAVES, o.c);
@@ -1031,10 +1043,41 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
           }
         },
         o.top_k, w.zmax, o.c, C.steps, C.redi);
+  } else if (own_bins) {
+    t0 = least_of_mass<N>(A, exp2, r, segs, o, w, C.least);
   } else if (!binned) {
     t0 = octaves_below(w.zmax, FIXED_OCTAVES, o.c);
   }
   if (!binned && !(o.by_k && o.by_p)) t0 = fmaxf(t0, min_z);   // top-p takes its share of all the k
+  if (own_bins) {
+    constexpr int PER = BINS / N;
+    per = bins_per_logit(w.zmax, t0, bin_factor(o.c));
+    __syncthreads();
+    for (int i = tid; i < BINS; i += N) C.bin.mass[i] = 0;
+    __syncthreads();
+    z.template tokens<N, true>(strip_m, t0, 0, n_strips,
+                               [&](float x, int) { atomicAdd(&C.bin.mass[bin_of(x, w.zmax, per)], z.fixed(x)); });
+    __syncthreads();
+    u64 mine[PER], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += mine[i] = C.bin.mass[tid * PER + i];
+    u64 end = group_prefix<N>(sum, C.red, &all);
+    int hit = BINS;
+    u64 front = 0;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i) {
+      if (mine[i] && (double)end >= mass_limit(o, w.total * FIXED_ONE)) {
+        hit = tid * PER + i;
+        front = end - mine[i];
+      }
+      end -= mine[i];
+    }
+    bin = group_min<N>(hit, C.redi);
+    known = bin == BINS;
+    if (hit == bin && !known) C.mass = front;
+    __syncthreads();
+    if (!known) above = C.mass;
+  }
   if (tid == 0) {
     C.n_list = whole_list ? info.listed : known ? LIST + 1 : 0;
     C.lo = ~0ull;
@@ -1046,6 +1089,10 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
   } else if (!known) {
     z.template strips<N>(strip_m, t0, 0, n_strips, [&](const Eight<T, VEC>& v, int first) {
       uint32_t hits = v.from(t0);
+      if (own_bins)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (bin_of(v[e], w.zmax, per) != bin) hits &= ~(1u << e);
       const int mine = __popc(hits), end = wave_prefix(mine);
       int at = 0;
       if (lane == 63) at = atomicAdd(&C.n_list, end);
@@ -1062,7 +1109,7 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
 
   // Few of all that can be kept: a thread each, compared with one another and drawn from by
   // their ids.
-  if (!whole_list && n_list <= CutMemory<N>::FEW) {
+  if (!whole_list && !own_bins && n_list <= CutMemory<N>::FEW) {
     const bool is = tid < n_list;
     const u64 p = is ? C.list[tid] : 0, mine = is ? z.fixed(P::z(p)) : 0;
     const int id = P::id(p);
@@ -1128,10 +1175,10 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
   double share = w.total * FIXED_ONE;
 #pragma unroll 1
   for (int rule = 0; rule < 2; ++rule) {
-    if (rule == 0 ? !o.by_k : !o.by_p || (whole_list && info.bin == BINS)) continue;
+    if (rule == 0 ? !o.by_k : !o.by_p || known || (whole_list && info.bin == BINS)) continue;
     u64 mass;
     border = max(border, find_border<P>(z, C, each, n_list, rule == 0, rule == 0 ? (double)o.top_k : mass_limit(o, share), lo, hi,
-                                        whole_list ? info.above : 0, &mass));
+                                        n_list <= LIST ? above : 0, &mass));
     share = (double)mass;
   }
   // What is kept of each segment or, where the histogram knows the parts', of each part
@@ -1161,7 +1208,7 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
   }
   for (int i = s0 + tid; i < s1; i += N) C.seg[i] = 0;
   __syncthreads();
-  if (!whole_list && n_list <= LIST) {
+  if (!whole_list && !own_bins && n_list <= LIST) {
     each([&](float x, int id) {
       if (P::of(x, id) >= border) atomicAdd(&C.seg[id / SEG], z.fixed(x));
     });
@@ -1197,7 +1244,7 @@ bool may_cut(const DrawArgs& a) {
   return a.top_k_rows || a.top_p_rows || a.min_p_rows || a.top_k > 0 || a.top_p < 1.0 || a.min_p > 0.0;
 }
 bool may_bin(const DrawArgs& a) {
-  return a.vocab > LIST && (a.top_k_rows || a.top_k == 0 || a.top_k >= a.vocab) && 
+  return !alone(a) && (a.top_k_rows || a.top_k == 0 || a.top_k >= a.vocab) &&
          (a.top_p_rows || a.top_p < 1.0 || (a.rows < ROWS_FULL && (a.min_p_rows || a.min_p > 0.0)));
 }
 
