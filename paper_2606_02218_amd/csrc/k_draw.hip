@@ -52,6 +52,7 @@ constexpr int PART = 256;             // threads of a part of a row's histogram
 constexpr int PICK = 512;
 constexpr int BINS = 1024;            // of z in a row's histogram
 constexpr int LIST = 4096;            // tokens that a row's list holds
+constexpr int OWN_BINS = 1024;        // tokens past which the pick goes by a histogram of its own (4000: 18-20 us, by a list 25-27)
 constexpr int ROWS_FULL = 256;        // rows that keep the chip busy, a workgroup each
 constexpr int ID_BITS = 20;
 constexpr double LOG2E = 1.4426950408889634;
@@ -420,13 +421,13 @@ __device__ __forceinline__ int bin_of(float z, float zmax, float per) { return (
 __device__ __forceinline__ float bin_factor(double c) { return (float)fmin(c, 3.0e38); }
 // Weight, or u of it, at which top-p ends: the first token is always kept.
 __device__ __forceinline__ double mass_limit(const RowOpts& o, double all) { return fmax((double)o.top_p * all, 0.5); }
-// Whether the pick deals with every row alone.  A small vocabulary's tokens are few.  Rows
-// enough for all units need no more workgroups, where the vocabulary is not so large that
-// one is slower at it (all rows by top-p: 512 rows of 5000 28 us, by several workgroups 41;
-// 300 of 32000 65, 60; 256 of 151936 177, 134), or some rows' top-k leaves it few of them
-// (505 rows of 32000, a tenth of them by top-p alone: 40, 51).
+// Whether the pick deals with every row alone.  Top-p by several workgroups a row takes
+// three launches, by one a histogram of its own: 2 to 150 rows of 5000 28-32 and 22-23 us, of
+// 16000 28-36 and 28-31, of 32000 29-46 and 40-46.  Where rows are enough for all units and
+// top-k's own may leave it few of them, it pays further (505 rows of 32000, a tenth of them
+// by top-p alone: 51, 40).
 __host__ __device__ __forceinline__ bool alone(const DrawArgs& A) {
-  return A.vocab <= LIST || (A.rows >= ROWS_FULL && A.vocab <= (A.top_k_rows ? 1 << 16 : 1 << 14));
+  return A.vocab <= (A.rows >= ROWS_FULL && A.top_k_rows ? 1 << 16 : 1 << 14);
 }
 // Which rows several workgroups look at, by a histogram.  top-k's tokens are few.  min-p's
 // border is known, but summing up what it leaves takes one workgroup a row long where that
@@ -1023,7 +1024,7 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
   const int n_strips = segs * STRIPS;
   const float* const strip_m = A.strip_m + (int64_t)r * n_strips;
   bool known = !binned && !o.by_k && !o.by_p;              // the border: no list is needed
-  const bool own_bins = !binned && !o.by_k && o.by_p && A.vocab > LIST;
+  const bool own_bins = !binned && !o.by_k && o.by_p && A.vocab > OWN_BINS;
   int bin = BINS;                                          // of those the one in which the border lies
   float per = 0.f;
   u64 above = whole_list ? info.above : 0;
