@@ -198,7 +198,7 @@ struct Eight {
 // Where 2^(z c) of a segment's tokens is not out of all bounds, their weights are taken with
 // respect to the whole octave next to the maximum's m c, else to m itself.
 __device__ __forceinline__ bool by_octave(float m, double c) {
-  return fabs((double)m * c) < 1024.0 && c > 1e-30 && fabsf(m) < 1e38f;
+  return fabs((double)m * c) < 1024.0 && c > 1e-30 && c < 1e30 && fabsf(m) < 1e38f;
 }
 // A segment's weight with respect to the row's maximum.
 __device__ __forceinline__ double share_of(const Exp2& exp2, float m, double s, float zmax, double c) {
@@ -831,11 +831,11 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
   const Exp2 exp2;
   const Logits<T, VEC> z{(const T*)A.logits + r * A.row, A.vocab, info.zmax, o.c, exp2};
   z.template tokens<PART, true>(A.strip_m + (int64_t)r * segs * STRIPS, info.t0, part_start(part, segs, parts) * STRIPS,
-                          part_start(part + 1, segs, parts) * STRIPS, [&](float x, int id) {
-                            if (bin_of(x, info.zmax, per) != border) return;
-                            const int k = atomicAdd(&n_list, 1);
-                            if (k < LIST) list[k] = Places<T>::of(x, id);
-                          });
+                                part_start(part + 1, segs, parts) * STRIPS, [&](float x, int id) {
+                                  if (bin_of(x, info.zmax, per) != border) return;
+                                  const int k = atomicAdd(&n_list, 1);
+                                  if (k < LIST) list[k] = Places<T>::of(x, id);
+                                });
   __syncthreads();
   const int n = n_list;
   if (n == 0) return;

@@ -257,6 +257,28 @@ def test_the_ends_of_temperature(s, vocab):
     check(z, u, rg.sample(z, u, temperature=1.7e308, **s), temperature=1.7e308, **s)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("t", [1e-300, 1e-40, 1e-33, 1e-29, 1e-6, 1.0, 1e6, 1e29, 1e32, 1e300])
+def test_a_largest_logit_of_zero(t, dtype):
+    """Nothing tells z / T from z where z is 0: each way of scaling it."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(8)
+    z = logits(rng, 3, 1500, "flat", dtype)
+    z = z - z.amax(1, keepdim=True)
+    u = torch.from_numpy(rng.random(3)).cuda()
+    for s in (dict(), dict(top_k=30), dict(top_p=0.9), dict(min_p=0.1)):
+        got = rg.sample(z, u, temperature=t, **s)
+        if 1e-6 <= t:
+            check(z, u, got, temperature=t, **s)
+        else:
+            for r in range(3):             # the u-th of those at the top, or of all that some rule leaves of them
+                top = (z[r] == 0).nonzero().flatten().tolist()
+                assert got[0][r].item() in top and abs(got[1][r].item() + np.log(len(top))) < 2.0 ** -22
+        if 1e-38 <= t <= 1e38:
+            row = rg.sample(z, u, temperature=torch.full((3,), t, device="cuda"), **s)
+            assert torch.equal(row[0], rg.sample(z, u, temperature=float(np.float32(t)), **s)[0])
+
+
 @pytest.mark.parametrize("s", [dict(), dict(top_k=20, top_p=0.9)])
 def test_graphs_and_streams(s):
     import paper_2606_02218_amd as rg
