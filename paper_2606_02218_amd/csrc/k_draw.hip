@@ -848,7 +848,7 @@ __global__ __launch_bounds__(PART) void k_draw_collect(DrawArgs A, int segs, int
 // ---------------------------------------------------------------- pick
 template <int N>
 struct CutMemory {
-  static constexpr int FEW = N / 4 < 128 ? 128 : N / 4;   // tokens that are compared with one another
+  static constexpr int FEW = 128;       // tokens that are compared with one another (256: 22 us in place of 18)
   struct Token { u64 place, weight; };
   union {
     struct { u64 mass[BINS]; uint32_t count[BINS]; } bin;
@@ -871,8 +871,8 @@ template <int N>
 __device__ __forceinline__ void compare(CutMemory<N>& C, int n, int& rank, u64& before) {
   constexpr int FEW = CutMemory<N>::FEW;
   const int tid = threadIdx.x;
-  const int room = n <= 64 ? 64 : n <= 128 ? 128 : 256, groups = N / room, mine = tid % room, per = (n + groups - 1) / groups;
-  static_assert(FEW <= 256 && FEW <= N, "a thread has one token at most");
+  const int room = n <= 64 ? 64 : 128, groups = N / room, mine = tid % room, per = (n + groups - 1) / groups;
+  static_assert(FEW == 128 && FEW <= N, "a thread has one token at most");
   if (tid < n) {
     C.before[tid] = 0;
     C.rank[tid] = 0;
