@@ -410,10 +410,7 @@ __device__ __forceinline__ bool tile_of(const Kv8Rows& b, int np, int k, int& s,
 // Values [block][half hh][e][m]: a piece is dim DT m + e, tokens 4 hh .. + 3 and
 // 8 + 4 hh .. + 3 of a block, those whose probabilities lane half hh holds.  Lanes
 // read neighbouring pieces.
-//
-// TREE: rows are nodes of drafted trees (launch_kv8_tree_attention).  Every node sees the
-// context; pieces that reach into the tree are masked by each column's bits.
-template <typename T, int HD, int OUT, bool TREE>
+template <typename T, int HD, int OUT>
 __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8_tiles(Kv8Attn A) {
   constexpr int QP = q_pieces(OUT), PP = p_pieces(OUT, true);
   constexpr int NK = HD / 16;       // 32x32x16 steps over the head's dims
@@ -421,7 +418,6 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   constexpr int BLK = 16 * HD;      // bytes of a block
   __shared__ u32x4_t sK[2][HD / 8][32], sV[2][2][2][DT][32];
   __shared__ int sNan[2][KV8_WAVES];
-  __shared__ uint64_t sMask[TREE ? KV8_TREE_TILE_WORDS : 1][KV8_TILE_Q];
 
   // Blocks are dealt to the 8 XCDs in turn, so with the kv heads side by side an
   // XCD keeps to few of them.
@@ -433,9 +429,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   int s, r0, n, skip;               // the tile's sequence, its rows, those before the tile
   if (!tile_of(A.b, np, (int)(item / (unsigned)A.plan.n_split), s, r0, n, skip)) return;
   const int nr = min(np, n - skip);
-  const int slot0 = kv8_len(A.b, s) - n;         // the sequence's first row
-  const int pos0 = slot0 + skip;                 // position of the tile's first row
-  const int seen = TREE ? tree_tokens(A.c, A.b, kv8_len(A.b, s), n, A.words) : 0;
+  const int pos0 = kv8_len(A.b, s) - n + skip;   // position of the tile's first row
   r0 += skip;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c32 = lane & 31, hh = lane >> 5;
@@ -443,42 +437,13 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   const bool valid = qi < nr * rep;
   const int row = r0 + (valid ? qi / rep : 0), head = kvh * rep + (valid ? qi % rep : 0);
   const int most = kv8_most(A.c, A.b);
-  const int limit = TREE ? 0 : valid ? min(pos0 + qi / rep + 1, most) : 0;   // tokens the column sees
-  const int wmax = TREE ? seen : pos0 + min(nr - 1, (wave * 32 + 31) / rep) + 1;   // most of any column of the wave
-  // Tokens that every row of the tile sees.  In a vector register: the choice between the
-  // two variants of a piece as a scalar branch spills 237 registers of bf16 tiles.
-  int whole = TREE ? max(slot0, 0) : min(pos0 + 1, most);
-  if constexpr (TREE) asm volatile("" : "+v"(whole));
+  const int limit = valid ? min(pos0 + qi / rep + 1, most) : 0;      // tokens the column sees
+  const int wmax = pos0 + min(nr - 1, (wave * 32 + 31) / rep) + 1;   // most of any column of the wave
+  const int whole = min(pos0 + 1, most);  // tokens that every row of the tile sees
   const bool active = wave * 32 < nr * rep;
-  const int end = TREE ? seen : min(pos0 + nr, most);   // tokens that the tile's last row sees
-  if constexpr (TREE) {               // the columns' masks; a padding row sees nothing
-    const bool sees = valid && pos0 + qi / rep >= 0;
-    if (hh == 0)
-      for (int w = 0; w < A.words; ++w) sMask[w][qi] = sees ? A.mask[(int64_t)row * A.words + w] : 0;
-    __syncthreads();
-  }
-  // the column's bits of the 32 tokens from t0 on: context where they come before the tree
-  auto window = [&](int t0) {
-    const int b = t0 - slot0, w = b >> 6, o = b & 63;
-    uint32_t x;
-    if (b < 0) {
-      x = valid ? (uint32_t)(sMask[0][qi] << -b) | ((1u << -b) - 1u) : 0u;
-    } else {
-      uint64_t y = w < A.words ? sMask[w][qi] >> o : 0;
-      if (o > 32 && w + 1 < A.words) y |= sMask[w + 1][qi] << (64 - o);
-      x = (uint32_t)y;
-    }
-    return end - t0 < 32 ? x & ((1u << (end - t0)) - 1u) : x;
-  };
+  const int end = min(pos0 + nr, most);   // tokens that the tile's last row sees
   const int64_t c0l = (int64_t)split * A.plan.chunk;
-  if (A.plan.n_split > 1 && c0l >= end && !(TREE && split == 0)) {
-    if (TREE && valid && hh == 0) {       // the join looks at every chunk's sum
-      float* ml = part_ml(A, (int64_t)row * A.plan.n_split + split, head);
-      ml[0] = -INFINITY;
-      ml[1] = 0.f;
-    }
-    return;
-  }
+  if (A.plan.n_split > 1 && c0l >= end) return;
   const int c0 = (int)c0l, c1 = split == A.plan.n_split - 1 ? end : min(end, c0 + A.plan.chunk);
   const int32_t* tab = kv8_table(A.b, s);
 
@@ -563,21 +528,17 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   // its dims NaN.  A product counts them: ones at the NaN codes, ones at the tokens
   // in sight.
   auto nan_values = [&](int t0) {
-    const uint32_t bits = TREE ? window(t0) : 0u;
 #pragma unroll 1
     for (int b = 0; b < 2; ++b) {
       if (t0 + 16 * b >= c1) break;
       const int nid = kv8_block(A.c, tab, A.b.tab_stride, (t0 >> 4) + b, kvh);
       if (nid < 0) continue;        // its keys made the rows NaN
       const int left = limit - t0 - 16 * b - 4 * hh;
-      uint32_t in_sight[4];
+      uint32_t seen[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int t = i < 2 ? 2 * i : 4 + 2 * i;   // tokens t, t + 1 behind 4 hh
-        if constexpr (TREE)
-          in_sight[i] = (bits >> (16 * b + 4 * hh + t) & 1u) * 0x3F80u | (bits >> (16 * b + 4 * hh + t + 1) & 1u) * 0x3F800000u;
-        else
-          in_sight[i] = (t < left ? 0x3F80u : 0u) | (t + 1 < left ? 0x3F800000u : 0u);
+        seen[i] = (t < left ? 0x3F80u : 0u) | (t + 1 < left ? 0x3F800000u : 0u);
       }
       const uint32_t* vp = reinterpret_cast<const uint32_t*>(A.c.v + (int64_t)nid * BLK + hh * (4 * HD)) + DT * c32;
 #pragma unroll
@@ -594,7 +555,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
         for (int i = 0; i < 16; ++i) n[i] = 0.f;
         n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
             __builtin_bit_cast(bf16x8_t, u32x4_t{one[0], one[1], one[2], one[3]}),
-            __builtin_bit_cast(bf16x8_t, u32x4_t{in_sight[0], in_sight[1], in_sight[2], in_sight[3]}), n, 0, 0, 0);
+            __builtin_bit_cast(bf16x8_t, u32x4_t{seen[0], seen[1], seen[2], seen[3]}), n, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           if (n[i] > 0.f) o[e][i] = __uint_as_float(0x7FC00000u);
@@ -619,10 +580,9 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
     }
     if constexpr (masked) {
       const int left = limit - t0 - 4 * hh;
-      const uint32_t bits = TREE ? window(t0) >> (4 * hh) : 0u;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        if (TREE ? !(bits >> (8 * (i / 4) + i % 4) & 1u) : 8 * (i / 4) + i % 4 >= left) st[i] = -INFINITY;
+        if (8 * (i / 4) + i % 4 >= left) st[i] = -INFINITY;
         if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // all compares at once spill scalar registers
       }
     }
@@ -693,7 +653,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
   // a lane's outputs: dims DT * (8 (i / 4) + 4 hh + i % 4) + e
   constexpr int NV = 4 * DT;        // consecutive dims for one i / 4
   if (A.plan.n_split == 1) {
-    const float inv = (TREE ? l != 0.f : limit > 0) ? 1.0f / l : 0.f;
+    const float inv = limit > 0 ? 1.0f / l : 0.f;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float v[NV];
@@ -703,7 +663,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, OUT == OUT_BF16 ? 3 : 2) void k_kv8
         for (int e = 0; e < DT; ++e) v[DT * i + e] = o[e][4 * g + i] * inv;
       put<OUT>(A, row, head, DT * (8 * g + 4 * hh), v);
     }
-  } else if (TREE || limit > c0) {
+  } else if (limit > c0) {
     const int64_t slot = (int64_t)row * A.plan.n_split + split;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -780,7 +740,7 @@ hipError_t run(const Kv8Attn& a, hipStream_t st) {
     const int np = KV8_TILE_Q / rep;
     const int64_t tiles = (int64_t)a.b.rows / np + a.b.n_seqs, grid = tiles * a.c.n_kv * a.plan.n_split;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    return kv8_launch(k_kv8_tiles<T, HD, OUT, false>, dim3((unsigned)grid), dim3(64 * KV8_WAVES), st, a);
+    return kv8_launch(k_kv8_tiles<T, HD, OUT>, dim3((unsigned)grid), dim3(64 * KV8_WAVES), st, a);
   }
   const int htiles = (rep + 15) / 16;
   const int64_t items = (int64_t)a.b.rows * a.c.n_kv * htiles * a.plan.n_split;
@@ -846,15 +806,6 @@ hipError_t launch_kv8_attention(int dtype, bool planes, const Kv8Attn& a, hipStr
   if (planes) return w ? run<float, 128, OUT_PLANES>(a, st) : run<float, 64, OUT_PLANES>(a, st);
   if (dtype == 1) return w ? run<bf16_t, 128, OUT_BF16>(a, st) : run<bf16_t, 64, OUT_BF16>(a, st);
   return w ? run<float, 128, OUT_F32>(a, st) : run<float, 64, OUT_F32>(a, st);
-}
-
-hipError_t launch_kv8_tree_tiles(const Kv8Attn& a, hipStream_t st) {
-  const int np = KV8_TILE_Q / (a.n_q / a.c.n_kv);
-  const int64_t grid = ((int64_t)a.b.rows / np + a.b.n_seqs) * a.c.n_kv * a.plan.n_split;
-  if (grid > INT32_MAX || np < 1 || a.words > KV8_TREE_TILE_WORDS) return hipErrorInvalidValue;
-  const dim3 g((unsigned)grid), t(64 * KV8_WAVES);
-  return a.c.hd == 128 ? kv8_launch(k_kv8_tiles<bf16_t, 128, OUT_BF16, true>, g, t, st, a)
-                       : kv8_launch(k_kv8_tiles<bf16_t, 64, OUT_BF16, true>, g, t, st, a);
 }
 
 hipError_t launch_kv8_merge(int dtype, bool planes, const Kv8Attn& a, hipStream_t st) {

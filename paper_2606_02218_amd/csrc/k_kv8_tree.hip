@@ -74,21 +74,21 @@ __global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ par
 }
 
 // ---------------------------------------------------------------- attention
-// The tree's queries of one kv head, nodes x heads, are packed as columns, 16 of them a
-// workgroup.  Its waves take 32-token steps in turn straight from memory, 16 bytes a
+// The tree's queries of one kv head, nodes x heads, are packed as columns, 16 or 32 of
+// them a workgroup.  Its waves take 32-token steps in turn straight from memory, 16 bytes a
 // lane, and join in LDS.
 // Scores are formed transposed, S^T = K Q^T, so that a lane ends up with the
 // probabilities of one column for just those tokens whose V^T operand it loads.
 // Every node sees the context: only steps that reach into the tree are masked.
-// What bounds it: vector issue, and the caches' lines.  A step of 32 tokens x 16 columns x
-// 128 dims is 16 MFMAs, 64 conversions of codes and some 60 others, and a wave's start and
+// What bounds the 16: vector issue, and the caches' lines.  A step of 32 tokens x 16 columns
+// x 128 dims is 16 MFMAs, 64 conversions of codes and some 60 others, and a wave's start and
 // end weigh as much as eight steps.  64 trees of 4 to 63 nodes over 512 to 4500 tokens, 12
-// heads, 83 us (0.43 PFLOP/s): 1400 clocks of a SIMD a step, vector instructions in 55 % of
-// them, MFMAs busy in 18 %, three waves a SIMD that wait for memory 40 % of their time.
-// Tried there: 32 columns a wave 84 us (two waves a SIMD); four waves of 16 columns, and two
-// or four halves of the tokens, over codes that come straight into LDS once 89 and 93 (the
+// heads, take 83 us, 1400 clocks of a SIMD a step, vector instructions in 55 % of them and
+// MFMAs busy in 18 %; by 32 columns 72.  Tried there: four waves of 16 columns, and two or
+// four parts of the tokens, over codes that come straight into LDS once 89 and 93 (the
 // longest context's chain, and barriers); keys as e4m3 operands beside queries in two e4m3
 // pieces 84; every line of a later step touched ahead 108, of a quarter of the steps 86.
+constexpr int WIDE_WAVES = 4;
 constexpr int tree_pieces(int size) { return size == 2 ? 1 : 3; }   // bf16 pieces of a query and of a probability
 constexpr int tree_waves(int size, int hd) { return size == 2 || hd == 64 ? 4 : 3; }   // of a SIMD, by the registers
 
@@ -198,7 +198,8 @@ __device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W
 }
 
 template <typename T, int HD, int W>
-__global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_attn(Kv8Attn A, unsigned eights, unsigned items) {
+__global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_attn(Kv8Attn A, unsigned eights,
+                                                                                      unsigned items) {
   constexpr int QP = tree_pieces(sizeof(T)), PP = QP;
   constexpr int NJ = HD / 64;       // 16-byte loads of a block per lane
   constexpr int LDO = HD + 4;
@@ -413,6 +414,232 @@ __global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_
   tree_store<T, HD, W, N>(A, ml, sum, acc, col0 + h, d, rep, kvh, r0, ctx0, split, c0, c1, fix, tab);
 }
 
+// The same for 32 columns a workgroup: a step's codes pass the caches and are converted
+// once for twice as many.  The queries' operands are shared by the waves and stay in LDS.
+// What bounds it: matrix and vector issue.  A step of 32 tokens and 128 dims is 16 products of
+// 32 x 32 x 16, which hold the vector unit for half of their 32 clocks each, and 64
+// conversions, 16 exponentials and some 80 others.  64 trees of 64 nodes, 12 heads, at 4000
+// tokens 154 us, 0.66 PFLOP/s; 2 of 64, 28 heads, at 60 to 131 thousand 211 (0.64).
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * WIDE_WAVES, sizeof(T) == 2 ? 3 : 2) void k_kv8_tree_wide(Kv8Attn A, unsigned eights,
+                                                                                            unsigned items) {
+  constexpr int QP = tree_pieces(sizeof(T)), PP = QP, W = WIDE_WAVES;
+  constexpr int NK = HD / 16;       // products over the head's dims
+  constexpr int NL = HD / 32;       // 16-byte loads of a step's keys per lane
+  constexpr int DT = HD / 32;       // 32-dim tiles of the output: tile e holds dims DT * row + e
+  constexpr int LDO = HD + 4;
+  union Memory {
+    u32x4_t q[NK][QP][2][32];       // [product][piece][half][column]
+    float o[W][16][LDO];
+  };
+  __shared__ Memory mem;
+  __shared__ float sM[W][32], sL[W][32];
+  __shared__ int sNan[W], sFind[W][64];
+
+  unsigned item = (blockIdx.x >> 6) * 64 + (blockIdx.x & 7) * 8 + (blockIdx.x >> 3 & 7);
+  if (item >= items) return;
+  unsigned run = item >> 3;
+  const int kvh = (int)(run % (unsigned)A.c.n_kv);
+  run /= (unsigned)A.c.n_kv;
+  const int split = (int)(run / eights), x = (int)(run - (unsigned)split * eights) * 8 + (int)(item & 7);
+  const int rep = A.n_q / A.c.n_kv;
+  int key = 0, r0, n;
+  const int s =
+      A.b.n_seqs <= 64 && gridDim.x > 256 ? find_group_sorted(A.b, x, rep, 5, sFind, key) : find_group(A.b, x, rep, 5, key);
+  if (s < 0) return;
+  kv8_seq_rows(A.b, s, r0, n);
+  const uint32_t cols = (uint32_t)n * rep, col0 = (uint32_t)(x - key) * 32;
+  if (x < key || col0 >= cols) return;
+  const int len = kv8_len(A.b, s), ctx0 = len - n;      // node i is token ctx0 + i
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c32 = lane & 31, hh = lane >> 5;
+  const int total = tree_tokens(A.c, A.b, len, n, A.words);
+  const int64_t c0l = (int64_t)split * A.plan.chunk;
+  const int c0 = (int)std::min<int64_t>(c0l, total);
+  const int c1 = split == A.plan.n_split - 1 ? total : (int)std::min<int64_t>(total, c0l + A.plan.chunk);
+  const int steps = (c1 - c0 + 31) / 32, last_blk = (max(c1, 1) - 1) >> 4;
+  const int mine = (steps - wave + W - 1) / W;
+  const int whole = min(max(ctx0, 0), c1);
+  const int32_t* tab = kv8_table(A.b, s);
+
+  // Keys: lane c32 a token, 16 dims of every other 32; values: dims DT c32 .. of the
+  // token quads hh and 2 + hh of both blocks.
+  const uint8_t* kl = A.c.k + hh * 256 + (c32 & 15) * 16;
+  const uint8_t* vl = A.c.v + hh * (4 * HD) + c32 * (4 * DT);
+  typedef uint32_t vals_t __attribute__((ext_vector_type(DT)));
+  u32x4_t kr[NL];
+  vals_t vr[2][2];
+  int ids = 0;                      // lane i: block i & 1 of step i >> 1 of the current 32 steps
+  float kss = 1.f, vss = 1.f;
+  auto lists = [&](int i0) {
+    const int st = wave + W * (i0 + (lane >> 1));
+    const int blk = min((c0 >> 4) + 2 * st + (lane & 1), last_blk);
+    ids = kv8_block(A.c, tab, A.b.tab_stride, blk, kvh);
+    kss = ids < 0 ? 1.f : A.c.k_scale[ids];
+    vss = ids < 0 ? 1.f : A.c.v_scale[ids];
+  };
+  auto fetch_k = [&](int i) {
+    const int i0 = __builtin_amdgcn_readlane(ids, 2 * (i & 31)), i1 = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + 1);
+    const uint8_t* p = kl + (int64_t)max(c32 < 16 ? i0 : i1, 0) * (16 * HD);
+#pragma unroll
+    for (int j = 0; j < NL; ++j) kr[j] = *reinterpret_cast<const u32x4_t*>(p + j * 512);
+  };
+  auto fetch_v = [&](int i) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* p = vl + (int64_t)max(__builtin_amdgcn_readlane(ids, 2 * (i & 31) + h), 0) * (16 * HD);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) vr[h][g] = *reinterpret_cast<const vals_t*>(p + g * (8 * HD));
+    }
+  };
+  if (mine > 0) {
+    lists(0);
+    fetch_k(0);
+    fetch_v(0);
+  }
+  const bool vec = (((uintptr_t)A.q.p | (A.q.row * sizeof(T)) | (A.q.head * sizeof(T))) & 15) == 0;
+  for (int i = tid; i < NK * 64; i += 64 * W) {         // the columns' queries
+    const int kk = i >> 6, half = i >> 5 & 1, cc = i & 31;
+    const uint32_t c = col0 + cc;
+    const int node = (int)(c / (uint32_t)rep), head = kvh * rep + (int)(c - (uint32_t)node * rep);
+    const bool ok = c < cols && ctx0 + node >= 0;
+    bf16x8_t f[QP];
+    const T* at = (const T*)A.q.p + (r0 + (ok ? node : 0)) * A.q.row + head * A.q.head;
+    query8<T, QP>(at + 16 * ((kk & ~1) + half) + 8 * (kk & 1), ok, vec, f);
+#pragma unroll
+    for (int p = 0; p < QP; ++p) mem.q[kk][p][half][cc] = __builtin_bit_cast(u32x4_t, f[p]);
+  }
+  const uint32_t c = col0 + c32;
+  const int node_ = (int)(c / (uint32_t)rep);
+  const int row = c < cols && ctx0 + node_ >= 0 ? r0 + node_ : -1;   // -1: the column sees nothing
+  const float sc = A.scale * KV8_LOG2E;
+  float m = -INFINITY, l = 0.f;
+  f32x16_t o[DT];
+#pragma unroll
+  for (int e = 0; e < DT; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[e][i] = 0.f;
+  bool nan = false;
+  __syncthreads();
+
+  for (int i = 0; i < mine; ++i) {
+    const int t0 = c0 + 32 * (wave + W * i);
+    int id[2];
+    float ks[2], vs[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      id[h] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + h);
+      ks[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kss), 2 * (i & 31) + h));
+      vs[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vss), 2 * (i & 31) + h));
+    }
+    const float kscale = c32 < 16 ? ks[0] : ks[1];
+    f32x16_t st;                    // lane's tokens: 8 (i / 4) + 4 hh + i % 4 of the step
+#pragma unroll
+    for (int e = 0; e < 16; ++e) st[e] = id[e >> 3] < 0 ? __uint_as_float(0x7FC00000u) : 0.f;   // a lost page's: NaN
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+      const bf16x8_t kf = kv8_bf16x8(kr[kk >> 1][2 * (kk & 1)], kr[kk >> 1][2 * (kk & 1) + 1], kscale, kscale);
+#pragma unroll
+      for (int p = 0; p < QP; ++p)
+        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8_t, mem.q[kk][p][hh][c32]), st, 0, 0, 0);
+    }
+    if (i + 1 < mine) {
+      if (((i + 1) & 31) == 0) lists(i + 1);
+      fetch_k(i + 1);
+    }
+    if (t0 + 32 > whole) {
+      const uint32_t there = c1 - t0 < 32 ? (1u << (c1 - t0)) - 1u : ~0u;
+      uint32_t seen = 0;
+      if (row >= 0) seen = mask_window(A.mask + (int64_t)row * A.words, A.words, t0 - ctx0) & there;
+      seen >>= 4 * hh;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!(seen >> (8 * (e / 4) + e % 4) & 1)) st[e] = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int left = id[h] < 0 ? 0 : min(max(c1 - t0 - 16 * h - 8 * g - 4 * hh, 0), 4);
+          const uint32_t keep = left == 4 ? ~0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+          for (int e = 0; e < DT; ++e) {
+            const uint32_t w = vr[h][g][e] & keep;
+            nan |= has_nan_code(w);
+            vr[h][g][e] = clear_nan(w);
+          }
+        }
+    }
+    float mx = st[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = __builtin_elementwise_maximum(mx, st[e]);
+    mx *= sc;
+    if (__any(mx > m + KV8_SLACK)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = fmaxf(m, mx);
+      const float alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      l *= alpha;
+#pragma unroll
+      for (int e = 0; e < DT; ++e) o[e] *= alpha;
+      m = mn;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {   // 16 tokens
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(fmaf(st[8 * h + e], sc, -ms));
+        l += p[e];
+      }
+      bf16x8_t pf[PP];
+      operand8<PP>(p, pf);
+#pragma unroll
+      for (int e = 0; e < DT; ++e) {
+        const bf16x8_t vf = kv8_bf16x8(vr[h][0][e], vr[h][1][e], vs[h], vs[h]);
+#pragma unroll
+        for (int q = 0; q < PP; ++q) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[q], o[e], 0, 0, 0);
+      }
+    }
+    if (i + 1 < mine) fetch_v(i + 1);
+  }
+
+  const bool any_nan = __any(nan);
+  if (lane == 0) sNan[wave] = any_nan;
+  l += __shfl_xor(l, 32, 64);
+  if (hh == 0) {
+    sM[wave][c32] = m;
+    sL[wave][c32] = l;
+  }
+  bool fix = false;
+  for (int half = 0; half < 2; ++half) {                // 16 columns at a time: dims DT * (8 (i / 4) + 4 hh + i % 4) + e
+    __syncthreads();                                    // the queries, or the other half, have been read
+    if (c32 >> 4 == half) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < DT; ++e) mem.o[wave][c32 & 15][DT * (8 * g + 4 * hh + i) + e] = o[e][4 * g + i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) fix |= sNan[w] != 0;
+    constexpr int N = 16 * HD / (64 * W);
+    const int h = 16 * half + tid / (HD / N), d = tid % (HD / N) * N;
+    if (col0 + h < cols) {
+      float ml[W], sum[W];
+      const float* acc[W];
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        ml[w] = sM[w][h];
+        sum[w] = sL[w][h];
+        acc[w] = mem.o[w][h & 15];
+      }
+      tree_store<T, HD, W, N>(A, ml, sum, acc, col0 + h, d, rep, kvh, r0, ctx0, split, c0, c1, fix, tab);
+    }
+  }
+}
+
 // A wave per row and head joins the chunks' partial results in order; a chunk that
 // the row sees nothing of has sum 0 and its outputs are not looked at.
 constexpr int TREE_MAX_SPLIT = 64;
@@ -622,13 +849,17 @@ __global__ __launch_bounds__(64 * ACCEPT_WAVES) void k_kv8_accept(AcceptArgs A) 
 }
 
 template <typename T, int HD>
-hipError_t run(const Kv8Attn& a, hipStream_t st) {
+hipError_t run(const Kv8TreeAttn& t, hipStream_t st) {
+  const Kv8Attn& a = t.a;
   const int rep = a.n_q / a.c.n_kv;
-  const int64_t eights = ((int64_t)a.b.rows * rep / 16 + a.b.n_seqs + 7) / 8, items = eights * 8 * a.c.n_kv * a.plan.n_split;
+  const int64_t eights = ((int64_t)a.b.rows * rep / (t.plan.wide ? 32 : 16) + a.b.n_seqs + 7) / 8;
+  const int64_t items = eights * 8 * a.c.n_kv * a.plan.n_split;
   if (items > INT32_MAX - 64) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((items + 63) / 64 * 64));
-  if (a.plan.waves == 8) return kv8_launch(k_kv8_tree_attn<T, HD, 8>, grid, dim3(512), st, a, (unsigned)eights, (unsigned)items);
-  return kv8_launch(k_kv8_tree_attn<T, HD, 4>, grid, dim3(256), st, a, (unsigned)eights, (unsigned)items);
+  const unsigned e = (unsigned)eights, n = (unsigned)items;
+  if (t.plan.wide) return kv8_launch(k_kv8_tree_wide<T, HD>, grid, dim3(64 * WIDE_WAVES), st, a, e, n);
+  if (a.plan.waves == 8) return kv8_launch(k_kv8_tree_attn<T, HD, 8>, grid, dim3(512), st, a, e, n);
+  return kv8_launch(k_kv8_tree_attn<T, HD, 4>, grid, dim3(256), st, a, e, n);
 }
 
 template <typename T, int HD>
@@ -640,23 +871,24 @@ hipError_t merge(const Kv8Attn& a, hipStream_t st) {
 
 }  // namespace
 
-// Tiles where trees are wide and contexts long: 2 trees of 64 nodes, 28 heads, at 60 to
-// 131 thousand tokens 202 us, by 16 columns 246; 64 of 64 nodes, 12 heads, at 4000 tokens
-// 200 and 185.  Elsewhere 16 columns a workgroup: 64 trees of 4 to 63 nodes at 512
-// to 4500 tokens 83 us, by tiles 103.  A context is cut only where that fills the chip,
-// since the chunks' partial results and the join's launch cost more than they even out
-// (83 us in one piece, 128 in two), and 8 waves share a workgroup's tokens where one round
-// holds them.
-Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int words, int max_len) {
+// 32 columns a workgroup where sequences have 64 and more on average and there are, with
+// their contexts cut into chunks of 640 tokens and more, workgroups enough: three a compute
+// unit (fp32 two), of which half at least.  64 trees of 64 nodes, 12 heads, at 4000 tokens
+// 154 us, by 16 columns 199; 3 of 40 to 60, 28 heads, at 20 to 25 thousand 101 and 171; but 8
+// of 20 to 30, 12 heads, at 1000 to 1500 17 and 12, 48 of 5 to 10 21 and 19.  Else 16
+// columns, whose contexts are cut only where that fills the chip, since the chunks' partial
+// results and the join's launch cost more than they even out (64 trees of 4 to 63 nodes at
+// 512 to 4500 tokens 83 us in one piece, 92 in two), and 8 waves share a workgroup's tokens
+// where one round holds them.
+Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int max_len) {
   Kv8TreePlan p{};
-  const int64_t rep = n_q / n_kv, cols = ((int64_t)rows * rep + n_seqs - 1) / n_seqs;
-  p.tiles = dtype == 1 && cols >= 256 && max_len >= 8192 && words <= KV8_TREE_TILE_WORDS;
-  const int64_t wgs = p.tiles ? std::max<int64_t>((int64_t)rows / (128 / rep) + n_seqs / 2, 1) * n_kv
-                              : ((int64_t)rows * rep / 16 + n_seqs / 2 + 1) * n_kv;
-  p.waves = wgs <= 256 ? 8 : 4;
-  int64_t n = 1;
-  if (p.tiles) n = std::min<int64_t>(768 / wgs, max_len / 512);
-  else if (max_len >= 2048) n = std::min<int64_t>(256 / wgs, max_len / 640);
+  const int64_t rep = n_q / n_kv, cols = (int64_t)rows * rep / n_seqs, most = max_len / 640;
+  const auto groups = [&](int of) { return ((int64_t)rows * rep / of + n_seqs / 2 + 1) * n_kv; };
+  const int64_t wide = groups(32), full = dtype == 1 ? 768 : 512;
+  const int64_t cut = max_len < 2048 ? 1 : std::max<int64_t>(1, std::min(full / wide, most));
+  p.wide = cols >= 64 && wide * cut >= 384;
+  p.waves = groups(16) <= 256 ? 8 : 4;
+  int64_t n = p.wide ? cut : max_len < 2048 ? 1 : std::min(256 / groups(16), most);
   n = std::max<int64_t>(1, std::min<int64_t>(n, TREE_MAX_SPLIT));
   p.chunk = (int)std::min<int64_t>((((int64_t)max_len + n - 1) / n + 63) / 64 * 64, 1 << 30);
   p.n_split = (int)((max_len + (int64_t)p.chunk - 1) / p.chunk);
@@ -676,9 +908,8 @@ hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& t, hipStream_
     return hipErrorInvalidValue;
   const bool w = a.c.hd == 128;
   hipError_t e;
-  if (t.plan.tiles) e = launch_kv8_tree_tiles(a, st);
-  else if (dtype == 1) e = w ? run<bf16_t, 128>(a, st) : run<bf16_t, 64>(a, st);
-  else e = w ? run<float, 128>(a, st) : run<float, 64>(a, st);
+  if (dtype == 1) e = w ? run<bf16_t, 128>(t, st) : run<bf16_t, 64>(t, st);
+  else e = w ? run<float, 128>(t, st) : run<float, 64>(t, st);
   if (e != hipSuccess || a.plan.n_split == 1) return e;
   if (dtype == 1) return w ? merge<bf16_t, 128>(a, st) : merge<bf16_t, 64>(a, st);
   return w ? merge<float, 128>(a, st) : merge<float, 64>(a, st);

@@ -238,7 +238,7 @@ int64_t rg_kv8_tree_attention_scratch(int32_t dtype, int32_t n_q, int32_t n_kv, 
       head_dim < 1 || rows < 0 || n_seqs < 0 || max_len < 1 || words < 1 || words > RG_KV8_TREE_WORDS)
     return bad("rg_kv8_tree_attention_scratch", "bad sizes");
   if (rows == 0 || n_seqs == 0) return 0;
-  return 4 * kv8_tree_part_floats(rows, kv8_tree_plan(dtype, rows, n_seqs, n_q, n_kv, words, max_len), n_q, head_dim);
+  return 4 * kv8_tree_part_floats(rows, kv8_tree_plan(dtype, rows, n_seqs, n_q, n_kv, max_len), n_q, head_dim);
 }
 
 int rg_kv8_tree_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* q, int64_t q_row,
@@ -262,7 +262,7 @@ int rg_kv8_tree_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, 
   a.words = words;
   a.n_q = n_q;
   a.scale = scale;
-  t.plan = kv8_tree_plan(dtype, a.b.rows, a.b.n_seqs, n_q, a.c.n_kv, words, max_len);
+  t.plan = kv8_tree_plan(dtype, a.b.rows, a.b.n_seqs, n_q, a.c.n_kv, max_len);
   a.plan.waves = t.plan.waves;
   a.plan.n_split = t.plan.n_split;
   a.plan.chunk = t.plan.chunk;

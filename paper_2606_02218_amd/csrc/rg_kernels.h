@@ -453,15 +453,13 @@ hipError_t launch_kv8_merge(int dtype, bool planes, const Kv8Attn& a, hipStream_
 // Trees of drafted tokens (k_kv8_tree.hip): each row's mask of `words` 64-bit words,
 // a bit for each ancestor and itself, and its position.
 hipError_t launch_kv8_tree(const int32_t* parent, const Kv8Rows& b, int words, uint64_t* mask, int32_t* pos, hipStream_t st);
-// How a tree attention is cut: tiles (of 128 query rows, launch_kv8_tree_tiles), or 16
-// columns (nodes x heads of a kv head) a workgroup of 4 or 8 waves; the context into
-// n_split chunks of `chunk` tokens.
+// How a tree attention is cut: 32 columns (nodes x heads of a kv head) a workgroup (wide),
+// or 16 of them one of 4 or 8 waves; the context into n_split chunks of `chunk` tokens.
 struct Kv8TreePlan {
-  bool tiles;
+  bool wide;
   int waves, n_split, chunk;
 };
-constexpr int KV8_TREE_TILE_WORDS = 8;   // most mask words of a tile, which keeps them in LDS
-Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int words, int max_len);
+Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int max_len);
 struct Kv8TreeAttn {
   Kv8Attn a;        // its plan's chunks as the tree's
   Kv8TreePlan plan;
@@ -469,8 +467,6 @@ struct Kv8TreeAttn {
 inline int64_t kv8_tree_part_floats(int64_t rows, const Kv8TreePlan& p, int n_q, int hd) {
   return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
 }
-// The tiles' pass over the cache, bf16; the tree's join has to follow where n_split > 1.
-hipError_t launch_kv8_tree_tiles(const Kv8Attn& a, hipStream_t st);
 hipError_t launch_kv8_tree_attention(int dtype, const Kv8TreeAttn& a, hipStream_t st);
 // Moves the nodes of mask row last[s] behind the context; new_len: tokens then.
 hipError_t launch_kv8_accept(const Kv8Pool& c, const Kv8Rows& b, const uint64_t* mask, int words, const int32_t* last,

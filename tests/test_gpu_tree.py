@@ -130,17 +130,17 @@ def test_split_contexts(dtype, nodes, old):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("hd,seqs", [(128, 40), (64, 64), (64, 65)])
-def test_more_than_a_round_of_workgroups(dtype, hd, seqs):
+@pytest.mark.parametrize("hd,seqs,most", [(128, 40, 60), (64, 64, 60), (64, 65, 60), (128, 64, 15), (64, 65, 15), (128, 200, 10)])
+def test_more_than_a_round_of_workgroups(dtype, hd, seqs, most):
     """Up to 64 sequences the longest go first, equal lengths and empty ones among them; past 64 in their order."""
     import paper_2606_02218_amd as rg
     rng = np.random.default_rng(seqs)
-    nodes = [int(n) for n in rng.integers(0, 60, seqs)]
+    nodes = [int(n) for n in rng.integers(0, most, seqs)]
     old = [int(n) for n in rng.choice([0, 5, 130, 130, 301], seqs)]
     b = Batch([a + c for a, c in zip(nodes, old)], 2, hd, 32, seed=seqs)
     trees = [parents(n, "tree", b.rng) if n else np.zeros(0, int) for n in nodes]
     mask, _ = all_masks(trees, 1, old, b.lengths())
-    assert sum(nodes) * 6 // 16 * 2 > 256
+    assert (sum(nodes) * 6 // 16 + seqs) * 2 > 256
     q = rounded(b.rng.normal(0, 1.5, (sum(nodes), 12, hd)), dtype)
     out = rg.kv8_tree_attention(b.cache, dev(q, dtype), dev(b.tab), dev(b.lengths()), offsets(nodes), as_mask(mask), max_len=400)
     check(b, q, nodes, mask, out, dtype)
@@ -262,27 +262,28 @@ def test_output_in_the_queries_place():
         assert torch.equal(rg.kv8_tree_attention(b.cache, q, *args, out=q), want) and torch.equal(q, want)
 
 
-# ---------------------------------------------------------------- wide trees over long contexts: tiles of 128 rows
-LONG = 1 << 14                # a bound that asks for them, whatever the lengths, from 256 columns a sequence on
+# ---------------------------------------------------------------- wide trees over long contexts: 32 columns a workgroup
+LONG = 1 << 14                # a bound that asks for them, in chunks, whatever the lengths
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("hd,n_kv,rep,nodes,old", [
     (128, 1, 7, [64, 64], [9001, 37]), (128, 2, 7, [90, 1, 64], [100, 600, 2050]), (64, 2, 8, [64, 33, 0, 40], [0, 63, 7, 1200]),
     (64, 1, 33, [33, 0, 17, 40], [7, 9, 100, 200]), (128, 1, 128, [5, 1, 9], [0, 63, 64]), (64, 1, 1, [512], [5000]),
     (128, 1, 1, [300], [0]), (64, 3, 6, [65, 128, 3], [129, 0, 3000])])
-def test_wide_trees_over_long_contexts(hd, n_kv, rep, nodes, old):
+def test_wide_trees_over_long_contexts(hd, n_kv, rep, nodes, old, dtype):
     import paper_2606_02218_amd as rg
     assert sum(nodes) * rep / len(nodes) > 255
     b = Batch([a + c for a, c in zip(nodes, old)], n_kv, hd, 16 if rep % 2 else 64, seed=hd + rep)
     trees = [parents(n, "tree", b.rng) if n else np.zeros(0, int) for n in nodes]
     mask, _ = all_masks(trees, words_of(nodes), old, b.lengths())
-    q = rounded(b.rng.normal(0, 1.5, (sum(nodes), n_kv * rep, hd)), BF16)
-    args = (b.cache, dev(q, BF16), dev(b.tab), dev(b.lengths()), offsets(nodes), as_mask(mask))
+    q = rounded(b.rng.normal(0, 1.5, (sum(nodes), n_kv * rep, hd)), dtype)
+    args = (b.cache, dev(q, dtype), dev(b.tab), dev(b.lengths()), offsets(nodes), as_mask(mask))
     for bound in (LONG, 1 << 19):
         out = rg.kv8_tree_attention(*args, max_len=bound)
-        check(b, q, nodes, mask, out, BF16)
+        check(b, q, nodes, mask, out, dtype)
         assert all(torch.equal(out, rg.kv8_tree_attention(*args, max_len=bound)) for _ in range(2))
-    check(b, q, nodes, mask, rg.kv8_tree_attention(*args, max_len=LONG, scale=0.05), BF16, 0.05)
+    check(b, q, nodes, mask, rg.kv8_tree_attention(*args, max_len=LONG, scale=0.05), dtype, 0.05)
 
 
 def test_wide_trees_any_mask_padding_and_rows_of_nobody():
