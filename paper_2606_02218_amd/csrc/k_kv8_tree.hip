@@ -84,7 +84,7 @@ __global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ par
 // x 128 dims is 16 MFMAs, 64 conversions of codes and some 60 others, and a wave's start and
 // end weigh as much as eight steps.  64 trees of 4 to 63 nodes over 512 to 4500 tokens, 12
 // heads, take 83 us, 1400 clocks of a SIMD a step, vector instructions in 55 % of them and
-// MFMAs busy in 18 %; by 32 columns 72.  Tried there: four waves of 16 columns, and two or
+// MFMAs busy in 18 %; by 32 columns 70.  Tried there: four waves of 16 columns, and two or
 // four parts of the tokens, over codes that come straight into LDS once 89 and 93 (the
 // longest context's chain, and barriers); keys as e4m3 operands beside queries in two e4m3
 // pieces 84; every line of a later step touched ahead 108, of a quarter of the steps 86.
@@ -429,11 +429,13 @@ __global__ __launch_bounds__(64 * W, tree_waves(sizeof(T), HD)) void k_kv8_tree_
 }
 
 // The same for 32 columns a workgroup: a step's codes pass the caches and are converted
-// once for twice as many.  The queries' operands are shared by the waves and stay in LDS.
+// once for twice as many.  The queries' operands come through LDS, where the waves share
+// them.
 // What bounds it: matrix and vector issue.  A step of 32 tokens and 128 dims is 16 products of
 // 32 x 32 x 16, which hold the vector unit for half of their 32 clocks each, and 64
 // conversions, 16 exponentials and some 80 others.  64 trees of 64 nodes, 12 heads, at 4000
-// tokens 154 us, 0.66 PFLOP/s; 2 of 64, 28 heads, at 60 to 131 thousand 211 (0.64).
+// tokens 154 us, 0.66 PFLOP/s; 2 of 64, 28 heads, at 60 to 131 thousand 200 (0.67), vector
+// instructions in 52 % of the cycles, MFMAs busy in 31 %.
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * WIDE_WAVES, sizeof(T) == 2 ? 3 : 2) void k_kv8_tree_wide(Kv8Attn A, unsigned eights,
                                                                                             unsigned items) {
