@@ -165,8 +165,9 @@ __device__ __forceinline__ void weigh8(const float (&p)[8], bf16x8_t (&out)[N], 
 }
 
 // N dims of column c from d on: the waves' results joined, NaN values of the tokens that its
-// node does see put back (the steps cleared them), and stored, or kept for the join of
-// the chunks.
+// node does see put back, and stored, or kept for the join of the chunks.  Steps that reach
+// into the tree cleared them, so the first token to look at is that of the step with the
+// first node, which may hold up to 31 of the context's (chunks begin at whole steps).
 template <typename T, int HD, int W, int N>
 __device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W], const float (&sum)[W],
                                            const float* (&acc)[W], uint32_t c, int d, int rep, int kvh, int r0, int ctx0, int split,
@@ -189,7 +190,7 @@ __device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W
   }
   if (fix && ctx0 + node >= 0) {
     const uint64_t* mask = A.mask + (int64_t)(r0 + node) * A.words;
-    for (int t = max(max(ctx0, 0), c0); t < c1; ++t) {
+    for (int t = max(max(ctx0, 0) & ~31, c0); t < c1; ++t) {
       if (!(mask_window(mask, A.words, t - ctx0) & 1)) continue;
       const int b = kv8_block(A.c, tab, A.b.tab_stride, t >> 4, kvh);
       if (b < 0) continue;                              // its scores are NaN

@@ -1,6 +1,8 @@
 """Drafted trees over the 8-bit cache against the float64 oracle: masks and
 positions, attention of the nodes, the accepted path's move, and a round of them
 together."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -219,6 +221,57 @@ def test_what_a_node_does_not_see(dtype, split):
             assert np.isnan(out2[i]).all()
         else:
             assert np.array_equal(out2[i], out[i], equal_nan=True), i
+
+
+def cuts(b, n_q, nodes, words, bound, dtype):
+    """Whether the call takes 32 columns a workgroup, and in how many chunks, by the rule that the library states
+    beside its plan; the chunks are those that its scratch has room for."""
+    import paper_2606_02218_amd as rg
+    rep, rows, seqs = n_q // b.n_kv, sum(nodes), len(nodes)
+    of = lambda cols: (rows * rep // cols + seqs // 2 + 1) * b.n_kv  # noqa: E731
+    cut = 1 if bound < 2048 else max(1, min((768 if dtype == BF16 else 512) // of(32), bound // 640))
+    wide = rows * rep // seqs >= 64 and of(32) * cut >= 384
+    want = cut if wide else 1 if bound < 2048 else max(1, min(256 // of(16), bound // 640))
+    lib = rg.load_library()
+    lib.rg_kv8_tree_attention_scratch.restype = ctypes.c_int64
+    size = lib.rg_kv8_tree_attention_scratch(int(dtype == BF16), n_q, b.n_kv, b.hd, rows, seqs, words, bound)
+    n = size // (4 * rows * n_q * (b.hd + 2)) or 1
+    chunk = -(-(-(-bound // min(want, 64))) // 64) * 64
+    assert n == -(-bound // chunk), (n, want, chunk)
+    return wide, n
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_kv,rep,n,wide,old,bound,chunks", [
+    (1, 2, 40, False, 45, 85, 1), (1, 2, 40, False, 64, 104, 1), (1, 2, 40, False, 20, 60, 1), (2, 70, 33, False, 1993, 2026, 1),
+    (1, 2, 40, False, 3000, 3040, 4), (1, 2, 40, False, 45, 1 << 14, 25), (24, 11, 70, True, 45, 115, 1),
+    (24, 11, 70, True, 20, 90, 1), (24, 11, 70, True, 3000, 3070, 1), (8, 11, 70, True, 3000, 3070, 2)])
+def test_nan_values_of_the_context(n_kv, rep, n, wide, old, bound, chunks, hd, dtype):
+    """Every node sees the context: a NaN value there makes a dim of all of them NaN, in the step that also holds the
+    first nodes as in those before it, and nothing else."""
+    import paper_2606_02218_amd as rg
+    b = Batch([old + n], n_kv, hd, 16, seed=old + hd)
+    mask, _ = tree.masks(parents(n, "tree", b.rng), 2, old)
+    mask[n // 2] = 0                                    # sees the context alone
+    is_wide, pieces = cuts(b, n_kv * rep, [n], 2, bound, dtype)
+    assert is_wide == wide and min(pieces, 2) == min(chunks, 2)
+    q = rounded(b.rng.normal(0, 1.5, (n, n_kv * rep, hd)), dtype)
+    args = (b.cache, dev(q, dtype), dev(b.tab), dev(b.lengths()), offsets([n]), as_mask(mask))
+    clean = host(rg.kv8_tree_attention(*args, max_len=bound))
+    page, sub = b.places(0, -(-(old + n) // 16))
+    v = b.cache.v.view(torch.uint8)
+    last = n_kv - 1
+    for t in sorted({0, 7, old // 32 * 32 - 1, old // 32 * 32, old - 1} - {-1, old}):
+        d = (5 * t + 3) % hd
+        at = int(page[t // 16]), last, int(sub[t // 16]), (t % 16 // 4) * 4 * hd + d * 4 + t % 4
+        was = v[at].item()
+        v[at] = 0x7F if t % 2 else 0xFF
+        out = host(rg.kv8_tree_attention(*args, max_len=bound))
+        assert np.isnan(out[:, last * rep:, d]).all(), t
+        out[:, last * rep:, d] = clean[:, last * rep:, d]
+        assert np.array_equal(out, clean), t
+        v[at] = was
 
 
 def test_lost_pages():
