@@ -451,7 +451,8 @@ __device__ __forceinline__ float octaves_below(float zmax, float octaves, double
   return t <= -3.4e38f ? -INFINITY : of_key(key_of(t) - 2);
 }
 
-// What the scan knows of a row, put together by a workgroup of N threads.
+// What the scan knows of a row, put together by a workgroup of N threads.  No barrier stands
+// behind the last reads of `red`: only what begins with one may write it next.
 struct Row {
   float zmax;
   double total;
@@ -862,6 +863,9 @@ struct CutMemory {
   u64 before[FEW];
   int rank[FEW];
   u64 red[N / 64], sums[STRIPS], found, mass, rank0, lo, hi;
+  // the row's sum: of its own, since what comes next fills the union while other waves may
+  // still be reading it
+  double total[N / 64];
   int redi[N / 64], n_list, n_few;
 };
 
@@ -1007,7 +1011,7 @@ __global__ __launch_bounds__(N) void k_draw_pick(DrawArgs A, int segs, int parts
     t0 = info.t0;
     w = Row{info.zmax, info.total, info.good != 0};
   } else {
-    w = read_row<N>(A, exp2, r, segs, o, C.plain.red, C.redi);
+    w = read_row<N>(A, exp2, r, segs, o, C.total, C.redi);
   }
   if (!w.good || !(u >= 0.0 && u < 1.0)) {
     if (tid == 0) no_answer(A, r);

@@ -307,3 +307,25 @@ def test_graphs_and_streams(s):
         torch.cuda.synchronize()
         for _, out in graphs:
             assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,vocab", [(40, 1025), (300, 5000), (64, 16384), (260, 32000)])
+def test_the_same_call_gives_the_same_bits(rows, vocab, dtype):
+    """Rows that a workgroup searches by itself, where the sum comes right before the search: many calls, alone and
+    beside others, with the oracle's draws."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(vocab)
+    z = logits(rng, rows, vocab, "peaked", dtype)
+    u = torch.from_numpy(rng.random(rows)).cuda()
+    full = lambda x, t: torch.full((rows,), x, device="cuda", dtype=t)  # noqa: E731
+    k = torch.from_numpy(np.where(rng.random(rows) < 0.5, 0, rng.integers(1, 60, rows))).int().cuda()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in (dict(top_p=0.9, top_k=full(0, torch.int32)), dict(top_p=0.7, min_p=0.02, top_k=full(0, torch.int32)),
+              dict(top_p=full(0.8, F32), top_k=k), dict(top_k=40, top_p=0.9)):
+        want = rg.sample(z, u, **s)
+        check(z, u, want, **s)
+        torch.cuda.synchronize()
+        got = [rg.sample(z, u, stream=streams[i % 2], **s) for i in range(40)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x in got for a, b in zip(x, want))

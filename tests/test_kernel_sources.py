@@ -47,3 +47,23 @@ def test_restrict_pointers_of_a_call_are_distinct():
             args = re.findall(r"(?<![\w.>])(?:ep|a|sm|p)\.\w+(?![\w.\[(])", m.group(2))
             ptrs = [x for x in args if x.split(".")[1] in ("x", "C", "q_out", "kv_pool", "part", "norm_g", "tgt_z")]
             assert len(ptrs) == len(set(ptrs)), (name, m.group(0)[:120])
+
+
+def test_a_rows_sum_lies_in_no_union():
+    """The sampler's read_row ends with each wave's reads of its buffer and no barrier behind them, and the searches that
+    follow store into the workgroup's union before their first barrier: the buffer is none of that union's members."""
+    s = _source("k_draw.hip")
+    members = set()
+    for m in re.finditer(r"\bunion\s*\{", s):
+        depth, at = 1, m.end()
+        while depth:
+            depth += {"{": 1, "}": -1}.get(s[at], 0)
+            at += 1
+        body = re.sub(r"\{[^{}]*\}", "", s[m.end():at - 1])
+        members |= {re.search(r"(\w+)\s*(?:\[[^\]]*\])?\s*$", d).group(1) for d in body.split(";") if d.strip()}
+    assert {"bin", "seg", "steps", "plain", "least", "mass"} <= members
+    calls = re.findall(r"= read_row<\w+>\(([^;]*)\);", s)
+    assert len(calls) == 3
+    for args in calls:
+        for buffer in args.split(",")[-2:]:
+            assert not set(buffer.strip().split(".")) & members, args
