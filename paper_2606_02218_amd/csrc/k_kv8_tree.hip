@@ -12,64 +12,77 @@
 namespace {
 
 // ---------------------------------------------------------------- masks
-// A wave a sequence.  Up to 64 nodes, a lane each: whoever a node sees of its ancestors it
-// passes on, and the reach doubles each time, so six rounds do.  Else the parents go to LDS,
-// and each lane walks up from its nodes: parents come before their children, so a walk meets
-// the bits of a mask from the highest word down and ends after at most n steps.  Latency
-// bound.
-constexpr int TREE_STAGED = 2048;     // parents of a tree that LDS holds
+// A wave a sequence, 64 nodes at a time, a lane each: whoever a node sees of its ancestors it
+// passes on, and the reach doubles each time, so six rounds do.  What the 64 see of earlier
+// nodes comes from the rows that the wave wrote before.  Latency bound, and by the length alone:
+// 8 trees of 130, 500, 2048 nodes take 5, 11, 85 us whatever their shape, 2 of 4096 290.  By walks
+// up from each node, n^2 / 128 steps where they are a chain, chains took 58, 424, 6400 us and 25 ms,
+// stars 4.5, 8.6, 58 and 176 us.
 
-__global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ parent, Kv8Rows b, int words,
-                                                 uint64_t* __restrict__ mask, int32_t* __restrict__ pos) {
-  __shared__ int32_t sp[TREE_STAGED];
+// Lane `lane`'s node of up to 64, whose parent is lane `up` (-1: none of them): the bits of
+// the node and its ancestors among them, and the first of these.  False where it or one of
+// them is not `right`.
+__device__ __forceinline__ bool tree_bits(int lane, int up, bool right, uint64_t& bits, int& root) {
+  int far = right ? up >= 0 ? up : lane : lane | 64;
+  bits = 1ull << lane;
+#pragma unroll 1
+  for (int reach = 1; reach < 64; reach *= 2) {
+    const int at = far & 63, next = __shfl(far, at, 64);
+    bits |= (uint64_t)__shfl((unsigned long long)bits, at, 64);
+    far = next | (far & 64);
+  }
+  root = far & 63;
+  return far < 64;
+}
+
+__global__ __launch_bounds__(64) void k_kv8_tree(const int32_t* __restrict__ parent, Kv8Rows b, int words, uint64_t* mask,
+                                                 int32_t* pos) {
   const int s = blockIdx.x, lane = threadIdx.x;
   int r0, n;
   kv8_seq_rows(b, s, r0, n);
   if (n <= 0) return;
   const int first = max(n - kv8_len(b, s), 0);          // nodes before it are padding
   const int ctx = max(kv8_len(b, s) - n, 0);
+  int next = lane < n ? parent[r0 + lane] : -1;
   if (n <= 64) {
-    const int up = lane < n ? parent[r0 + lane] : -1;
+    uint64_t bits;
+    int root;
     // no parent: neither the node nor what is behind it counts
-    int far = up >= -1 && up < lane && lane >= first ? up >= first ? up : lane : lane | 64;
-    uint64_t bits = 1ull << lane;
-#pragma unroll 1
-    for (int reach = 1; reach < 64; reach *= 2) {
-      const int at = far & 63, next = __shfl(far, at, 64);
-      bits |= (uint64_t)__shfl((unsigned long long)bits, at, 64);
-      far = next | (far & 64);
-    }
+    const bool ok = tree_bits(lane, next >= first ? next : -1, next >= -1 && next < lane && lane >= first, bits, root);
     if (lane >= n) return;
-    const bool ok = far < 64;
     uint64_t* out = mask + (int64_t)(r0 + lane) * words;
     out[0] = ok ? bits : 0;
     for (int w = 1; w < words; ++w) out[w] = 0;
     pos[r0 + lane] = ok ? (int)min((int64_t)ctx + __popcll(bits) - 1, (int64_t)INT32_MAX) : -1;
     return;
   }
-  for (int i = lane; i < min(n, TREE_STAGED); i += 64) sp[i] = parent[r0 + i];
-  __syncthreads();
-  for (int i = lane; i < n; i += 64) {
-    uint64_t* out = mask + (int64_t)(r0 + i) * words;
-    int w = words - 1, depth = -1, a = i;
-    uint64_t bits = 0;
-    bool ok = i >= first;
-    while (ok && a >= first) {                          // a walk never goes up in number: it ends
-      if ((a >> 6) < words) {
-        for (; w > (a >> 6); --w) { out[w] = bits; bits = 0; }
-        bits |= 1ull << (a & 63);
+  for (int base = 0;; base += 64) {
+    const int i = base + lane, up = next, left = n - base;
+    if (left > 64) next = lane < left - 64 ? parent[r0 + i + 64] : -1;
+    const int out = up >= first && up < base ? up : -1;
+    uint64_t bits;
+    int root;
+    bool ok = tree_bits(lane, up >= max(first, base) ? up - base : -1, lane < left && up >= -1 && up < i && i >= first, bits, root);
+    const int back = __shfl(out, root, 64);             // the ancestor before the 64, if there is one
+    const int at = ok && back >= 0 ? pos[r0 + back] : ctx - 1;
+    ok = ok && (back < 0 || at >= 0);                   // no earlier one of its ancestors was wrong
+    if (lane < left) {
+      uint64_t* row = mask + (int64_t)(r0 + i) * words;
+      const uint64_t* old = mask + (int64_t)(r0 + max(back, 0)) * words;
+      const int known = ok && back >= 0 ? min((back >> 6) + 1, words) : 0;
+#pragma unroll 1
+      for (int w = 0; w < words; w += 8) {              // eight loads on their way together
+        uint64_t x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = w + e < known ? old[w + e] : 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (w + e < words) row[w + e] = ok && w + e == base >> 6 ? x[e] | bits : x[e];
       }
-      ++depth;
-      const int up = a < TREE_STAGED ? sp[a] : parent[r0 + a];
-      ok = up >= -1 && up < a;                          // no parent: neither the node nor what is behind it counts
-      a = up;
+      pos[r0 + i] = ok ? (int)min((int64_t)at + __popcll(bits), (int64_t)INT32_MAX) : -1;
     }
-    if (ok) {
-      for (; w >= 0; --w) { out[w] = bits; bits = 0; }
-    } else {
-      for (w = 0; w < words; ++w) out[w] = 0;
-    }
-    pos[r0 + i] = ok ? (int)min((int64_t)ctx + depth, (int64_t)INT32_MAX) : -1;
+    if (left <= 64) return;
+    __syncthreads();                                    // these rows can be read
   }
 }
 

@@ -72,6 +72,46 @@ def test_masks_of_wrong_parents_and_padding():
     assert bool((mask[-3:] == 77).all()) and bool((pos[-3:] == 77).all())
 
 
+def long_masks(parent, words, context, first=0):
+    """tree.masks for trees whose paths are too long to be written out: by each node's parent."""
+    mask, pos = np.zeros((len(parent), words), np.uint64), np.full(len(parent), -1)
+    for i in range(first, len(parent)):
+        p = int(parent[i])
+        if not -1 <= p < i or (p >= first and pos[p] < 0):
+            continue
+        pos[i] = context
+        if p >= first:
+            mask[i], pos[i] = mask[p], pos[p] + 1
+        if i < 64 * words:
+            mask[i, i // 64] |= np.uint64(1) << np.uint64(i % 64)
+    return mask, pos
+
+
+@pytest.mark.parametrize("kind", ["chain", "star", "forest", "tree", "wrong"])
+@pytest.mark.parametrize("n,words", [(2048, 64), (2049, 33), (4096, 64), (4100, 64), (70001, 7), (300000, 1)])
+def test_masks_of_long_trees(kind, n, words):
+    """Work grows with the nodes, not with their square: a chain of 300 thousand, wrong parents, padding and short
+    trees beside them."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(n)
+    p = parents(n, "tree" if kind == "wrong" else kind, rng)
+    if kind == "wrong":                                # what is behind these is nothing
+        at = rng.choice(n, 5, replace=False)
+        p[at] = [-2, -2 ** 31, 2 ** 31 - 1, at[3], min(at[4] + 70, n)]
+        p[rng.choice(n, n // 30, replace=False)] = -1
+        p[n - 40] = 2
+    side = parents(65, "tree", rng)
+    first = 77 if kind == "forest" else 0              # rows that are padding
+    lens = [9 + 65, n - first if first else n + 1234, 5 + 65]
+    parent = np.concatenate([side, p, side]).astype(np.int32)
+    mask, pos = rg.kv8_tree(dev(parent), dev(np.array(lens, np.int32)), offsets([65, n, 65]), words=words)
+    want = [long_masks(side, words, 9), long_masks(p, words, 0 if first else 1234, first), long_masks(side, words, 5)]
+    if n < 2100:
+        assert all(np.array_equal(a, b) for a, b in zip(want[1], tree.masks(p, words, 0 if first else 1234, first)))
+    assert np.array_equal(pos.cpu().numpy(), np.concatenate([x[1] for x in want]))
+    assert np.array_equal(mask.cpu().numpy().view(np.uint64), np.concatenate([x[0] for x in want]))
+
+
 # ---------------------------------------------------------------- attention
 P_STEP = {BF16: 2.0 ** -8, F32: 2.0 ** -24}      # half a step of a probability as it enters the product
 
