@@ -284,10 +284,14 @@ int rg_kv8_accept(const rg_kv8_cache* cache, const rg_kv8_batch* batch, const ui
   if (rows.n_seqs == 0) return RG_OK;
   if (!batch->seq_off || !batch->seq_len || !new_len) return bad(who, "NULL seq_off, seq_len or new_len");
   if (rows.rows > 0 && (!mask || !last)) return bad(who, "NULL mask or last");
-  // read by workgroups of the sequence that writes it
-  auto meets = [&](const int32_t* p, int64_t n) { return p && p < new_len + rows.n_seqs && new_len < p + n; };
-  if (meets(batch->seq_len, rows.n_seqs) || meets(last, rows.n_seqs) || meets(batch->seq_off, (int64_t)rows.n_seqs + 1) ||
-      meets(batch->tab_row, rows.n_seqs) || meets(batch->page_tab, (int64_t)batch->tab_rows * batch->tab_stride))
+  // read by workgroups of the sequence that writes it, and of others
+  auto meets = [&](const void* p, int64_t bytes) {
+    return p && (const char*)p < (const char*)(new_len + rows.n_seqs) && (const char*)new_len < (const char*)p + bytes;
+  };
+  const int64_t n = rows.n_seqs, blocks = (int64_t)pool.pages * pool.n_kv << pool.sub_shift, codes = blocks * 16 * pool.hd;
+  if (meets(batch->seq_len, 4 * n) || meets(last, 4 * n) || meets(batch->seq_off, 4 * (n + 1)) || meets(batch->tab_row, 4 * n) ||
+      meets(batch->page_tab, 4 * (int64_t)batch->tab_rows * batch->tab_stride) || meets(mask, 8 * (int64_t)rows.rows * words) ||
+      meets(pool.k, codes) || meets(pool.v, codes) || meets(pool.k_scale, 4 * blocks) || meets(pool.v_scale, 4 * blocks))
     return bad(who, "new_len overlaps what the call reads");
   return launched(who, launch_kv8_accept(pool, rows, mask, words, last, new_len, (hipStream_t)stream));
 }

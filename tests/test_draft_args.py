@@ -177,6 +177,17 @@ def test_library_refuses_accept():
     assert call(batch=dict(n_seqs=0, rows=0)) == 0
 
 
+def test_library_refuses_lengths_in_masks_and_caches():
+    """new_len on what the accept reads beyond the batch: the first and the last four bytes of each, and next to them."""
+    lib = _lib()
+    at = lambda i: 1 << (30 + i)  # noqa: E731
+    cache = _cache(k=at(1), v=at(2), k_scale=at(3), v_scale=at(4))           # 16 blocks of 1024 codes
+    call = lambda new: lib.rg_kv8_accept(C.byref(cache), C.byref(_batch()), at(0), 3, at(5), new, None)  # noqa: E731
+    for i, size in ((0, 5 * 3 * 8), (1, 16 << 10), (2, 16 << 10), (3, 64), (4, 64), (5, 8)):
+        for new in (at(i) - 4, at(i), at(i) + size - 4):
+            _refused(call(new), -1, b"overlaps")
+
+
 def test_library_refuses_samples():
     from paper_2606_02218_amd import _draft
     lib = _lib()
