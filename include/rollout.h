@@ -592,9 +592,10 @@ int64_t rg_sample_scratch(int32_t rows, int32_t vocab, const rg_sample_options* 
  * 0, infinite or NaN, or a NaN top_p or min_p of its own gets token -1 and NaN.
  * Weights are within 2e-12 of their value, their sums fp64 or, where something is cut,
  * whole numbers of 2^-42 of the largest weight.  No atomic changes a result: the same
- * call gives the same bits.  Enqueues two to four kernels, keeps no state.
- * RG_EINVAL for NULL pointers (but the options'), bad sizes, numbers outside the ranges above
- * or too little scratch; RG_EUNSUPPORTED for vocab past 2^20. */
+ * call gives the same bits.  Enqueues two to four kernels, keeps no state.  RG_EHIP, with
+ * nothing enqueued, for 2^23 rows and more (2^24 where nothing is cut), or 2^30 and more pairs
+ * of segments of 512 tokens.  RG_EINVAL for NULL pointers (but the options'), bad sizes,
+ * numbers outside the ranges above or too little scratch; RG_EUNSUPPORTED for vocab past 2^20. */
 int rg_sample(int32_t dtype, const void* logits, int64_t logits_row, int32_t rows, int32_t vocab, int32_t u_dtype, const void* u,
               const rg_sample_options* options, int32_t* tokens, float* logprobs, float* kept_logprobs, void* scratch,
               int64_t scratch_bytes, void* stream);

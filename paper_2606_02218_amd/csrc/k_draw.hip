@@ -1283,7 +1283,9 @@ hipError_t run(const DrawArgs& a, hipStream_t st) {
   const int segs = segments(a.vocab), parts = parts_of(a);
   const unsigned per_row = (unsigned)(segs + 1) / 2;
   const int64_t items = (int64_t)a.rows * per_row;
-  if (items > INT32_MAX / 2 || (int64_t)a.rows * parts > INT32_MAX) return hipErrorInvalidValue;
+  // the scan does not run where a launch behind it would be one of 2^32 threads
+  const int64_t threads = std::max<int64_t>((int64_t)a.rows * (may_cut(a) ? PICK : PART), a.bins ? (int64_t)a.rows * parts * PART : 0);
+  if (items > INT32_MAX / 2 || threads >> 32) return hipErrorInvalidValue;
   const int64_t per = std::max<int64_t>(1, items / SCAN_FILL), waves = (items + per - 1) / per;
   const dim3 grid((unsigned)((waves + SCAN_WAVES - 1) / SCAN_WAVES)), scan(64 * SCAN_WAVES);
   const dim3 part((unsigned)(a.rows * parts)), rows(a.rows);

@@ -161,6 +161,27 @@ def test_settings_by_row_strides_and_repeats(dtype):
     check(one, u, rg.sample(one, u, top_k=20), top_k=20)
 
 
+def test_more_rows_than_a_launch_takes():
+    """Refused before the first kernel: outputs and scratch stay as they were."""
+    import ctypes as C
+
+    import paper_2606_02218_amd as rg
+    from paper_2606_02218_amd import _draft
+    rows = 1 << 23
+    z = torch.zeros(1, 1, device="cuda").expand(rows, 1)
+    u = torch.zeros(rows, device="cuda")
+    lib = _draft._library()
+    o = _draft.rg_sample_options(1.0, 0.9, 0.0, 0)
+    need = lib.rg_sample_scratch(rows, 1, C.byref(o))
+    token, lp, scratch = (torch.full((n,), 77, dtype=torch.int32, device="cuda") for n in (rows, 2 * rows, need // 4))
+    rc = lib.rg_sample(0, z.data_ptr(), 0, rows, 1, 0, u.data_ptr(), C.byref(o), token.data_ptr(), lp.data_ptr(),
+                       lp.data_ptr() + 4 * rows, scratch.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+    assert rc == -3 and b"rg_sample" in lib.rg_last_error()
+    torch.cuda.synchronize()
+    assert all(bool((x == 77).all()) for x in (token, lp, scratch))
+    assert bool((rg.sample(z[1:], u[1:], top_p=0.9)[0] == 0).all())
+
+
 def test_frequencies():
     """20000 draws from eight tokens: counts within five deviations, both ways of drawing."""
     import paper_2606_02218_amd as rg
