@@ -909,6 +909,7 @@ hipError_t merge(const Kv8Attn& a, hipStream_t st) {
 // where one round holds them.
 Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int max_len) {
   Kv8TreePlan p{};
+  max_len = std::min(max_len, 1 << 30);                 // a table's most: one chunk, where nothing else asks for more
   const int64_t rep = n_q / n_kv, cols = (int64_t)rows * rep / n_seqs, most = max_len / 640;
   const auto groups = [&](int of) { return ((int64_t)rows * rep / of + n_seqs / 2 + 1) * n_kv; };
   const int64_t wide = groups(32), full = dtype == 1 ? 768 : 512;

@@ -161,6 +161,13 @@ def test_library_refuses_attention():
         assert s(*a) == -1
 
 
+def test_bounds_past_a_tables_most_ask_for_no_chunk_more():
+    s = _lib().rg_kv8_tree_attention_scratch
+    for a in [(1, 12, 2, 128, 100000, 10, 1), (0, 12, 2, 128, 100000, 10, 1), (1, 28, 4, 128, 128, 2, 1), (1, 2, 1, 64, 3, 1, 1)]:
+        assert s(*a, 2 ** 31 - 1) == s(*a, 1 << 30)
+    assert s(1, 12, 2, 128, 100000, 10, 1, 2 ** 31 - 1) == 0
+
+
 def test_library_refuses_accept():
     lib = _lib()
     p = [C.c_void_p(1 << (20 + i)) for i in range(8)]
