@@ -521,9 +521,9 @@ int64_t rg_kv8_tree_attention_scratch(int32_t dtype, int32_t n_q, int32_t n_kv, 
  * masks show them: rg_kv8_attention with j over those tokens, its arguments, limits,
  * numbers of bits (bf16 queries as they are, their probabilities as bf16; fp32 ones
  * and theirs with all 24 bits) and errors.  seq_off is required.  A row that sees
- * nothing, as a padding row, gets zeros; a row that sees a token whose page is not in
- * the table or the pool gets NaN.  What a row does not see does not touch it, whatever
- * the codes.
+ * nothing, as a padding row, gets zeros; a head none of whose tokens has a weight (scores
+ * of -inf), and a row that sees a token whose page is not in the table or the pool, NaN.
+ * What a row does not see does not touch it, whatever the codes.
  *   mask   DEVICE uint64 [rows, words], words in [1, 64] */
 int rg_kv8_tree_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, int32_t dtype, const void* q, int64_t q_row,
                           int64_t q_head, int32_t n_q, const uint64_t* mask, int32_t words, void* out, float scale,

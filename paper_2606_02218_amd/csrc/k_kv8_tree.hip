@@ -177,6 +177,20 @@ __device__ __forceinline__ void weigh8(const float (&p)[8], bf16x8_t (&out)[N], 
   }
 }
 
+// Whether a row, node of its sequence, sees any of the tokens c0 .. c1 - 1.
+__device__ __forceinline__ bool sees_any(const Kv8Attn& A, int row, int node, int ctx0, int c0, int c1) {
+  if (ctx0 + node < 0) return false;
+  if (c0 < min(ctx0, c1)) return true;
+  for (int t = max(c0, max(ctx0, 0)); t < c1; t += 32) {
+    const uint32_t bits = mask_window(A.mask + (int64_t)row * A.words, A.words, t - ctx0);
+    if (c1 - t < 32 ? bits & ((1u << (c1 - t)) - 1u) : bits) return true;
+  }
+  return false;
+}
+// A sum of weights that is -0 is that of no tokens: what sees some, all with a score of -inf,
+// has +0 and its output is 0 / 0.
+__device__ __forceinline__ bool is_none(float sum) { return __float_as_uint(sum) == 0x80000000u; }
+
 // N dims of column c from d on: the waves' results joined, NaN values of the tokens that its
 // node does see put back, and stored, or kept for the join of the chunks.  Steps that reach
 // into the tree cleared them, so the first token to look at is that of the step with the
@@ -213,8 +227,9 @@ __device__ __forceinline__ void tree_store(const Kv8Attn& A, const float (&ml)[W
         if ((v[4 * e] & 0x7F) == 0x7F) o[e] = __uint_as_float(0x7FC00000u);
     }
   }
+  if (L == 0.f && !sees_any(A, r0 + node, node, ctx0, c0, c1)) L = -0.f;
   if (A.plan.n_split == 1) {
-    const float inv = L == 0.f ? 0.f : 1.0f / L;        // 0: the row sees nothing
+    const float inv = is_none(L) ? 0.f : 1.0f / L;
 #pragma unroll
     for (int e = 0; e < N; ++e) o[e] *= inv;
     st_elems<N, true>((T*)A.out + ((int64_t)(r0 + node) * A.n_q + head) * HD + d, o);
@@ -680,7 +695,7 @@ __global__ __launch_bounds__(256) void k_kv8_tree_merge(Kv8Attn A) {
   const int head = (int)(at - r * A.n_q);
   if (r >= A.b.rows || r < A.b.seq_off[0] || r >= A.b.seq_off[A.b.n_seqs]) return;
   const int64_t slot0 = r * A.plan.n_split * A.n_q + head;
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = -0.f;
   if (lane < A.plan.n_split) {
     const float* ml = A.part_ml + 2 * (slot0 + (int64_t)lane * A.n_q);
     m = ml[0];
@@ -688,7 +703,7 @@ __global__ __launch_bounds__(256) void k_kv8_tree_merge(Kv8Attn A) {
   }
   const float M = wave_max(m);
   const float w = l == 0.f ? 0.f : m == M ? 1.f : __builtin_amdgcn_exp2f(m - M);
-  const float L = wave_sum(w * l), inv = L == 0.f ? 0.f : 1.0f / L;
+  const float L = wave_sum(w * l), inv = __all(is_none(l)) ? 0.f : 1.0f / L;
   float acc[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i) acc[i] = 0.f;

@@ -314,6 +314,43 @@ def test_nan_values_of_the_context(n_kv, rep, n, wide, old, bound, chunks, hd, d
         v[at] = was
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_kv,rep,n,wide,bound", [(1, 2, 40, False, 900), (1, 2, 40, False, 3100), (24, 11, 70, True, 900),
+                                                   (3, 11, 70, True, 3100)])
+def test_scores_of_minus_infinity(n_kv, rep, n, wide, bound, hd, dtype):
+    """A row that sees tokens, none of them with a weight, is NaN as in kv8_attention; one that sees nothing is zero;
+    one token with a weight is enough, whatever the chunks."""
+    import paper_2606_02218_amd as rg
+    old, nodes = [45, 0, 3000 if bound > 2048 else 300], [n, n, n]
+    b = Batch([c + n for c in old], n_kv, hd, 16, seed=n)
+    mask = np.concatenate([tree.masks(parents(n, "tree", b.rng), 2, c)[0] for c in old])
+    mask[n + 3] = mask[n + 17] = 0                       # with no context these rows see nothing
+    is_wide, pieces = cuts(b, n_kv * rep, nodes, 2, bound, dtype)
+    assert is_wide == wide and (pieces > 1) == (bound > 2048)
+    b.cache.k.view(torch.uint8).fill_(0x40)              # 2
+    b.cache.k_scale.fill_(1.0)
+    q = np.zeros((3 * n, n_kv * rep, hd))
+    q[:, :, 0] = -3.0e38
+    q[:, 1::2, 0] = 0.0                                  # every other head's scores are 0
+    args = (b.cache, dev(q, dtype), dev(b.tab), dev(b.lengths()), offsets(nodes), as_mask(mask))
+    out = host(rg.kv8_tree_attention(*args, max_len=bound))
+    none = [n + 3, n + 17]
+    some = [i for i in range(3 * n) if i not in none]
+    assert not out[none].any() and np.isnan(out[some][:, ::2]).all() and np.isfinite(out[some][:, 1::2]).all()
+    one = rg.kv8_attention(b.cache, args[1][:3], args[2], args[3])
+    assert np.isnan(host(one)[:, ::2]).all()
+    page, sub = b.places(2, 1)
+    k = b.cache.k.view(torch.uint8)
+    k[int(page[0]), :, int(sub[0])] = 0                  # 16 tokens of the third sequence have scores of 0
+    out = host(rg.kv8_tree_attention(*args, max_len=bound))
+    mean = b.v[2].values()[:16].mean(0).repeat(rep, 0)
+    # 16 exact probabilities of 1/16, sums of 16 terms, one rounding of the output
+    bound_ = np.abs(b.v[2].values()[:16]).mean(0).repeat(rep, 0) * 16 * 2.0 ** -24 + np.abs(mean) * 1.01 * P_STEP[dtype] + 1e-30
+    assert np.all(np.abs(out[2 * n:, ::2] - mean[::2]) <= bound_[::2])
+    assert np.isnan(out[:n, ::2]).all() and not out[none].any()
+
+
 def test_lost_pages():
     """Pages outside the pool or the table: NaN where a row sees a token of theirs, nothing elsewhere."""
     import paper_2606_02218_amd as rg
