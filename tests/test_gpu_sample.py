@@ -350,3 +350,92 @@ def test_the_same_call_gives_the_same_bits(rows, vocab, dtype):
         got = [rg.sample(z, u, stream=streams[i % 2], **s) for i in range(40)]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for x in got for a, b in zip(x, want))
+
+
+# ---------------------------------------------------------------- the sums, as exact as they are said to be
+WEIGHT = 2e-12                # a weight's relative error, as rollout.h has it
+ONE = 2.0 ** 42               # whole numbers of a weight of 1
+ADDED = 64 * 2.0 ** -53       # some 50 additions and products of doubles, each off by half a step
+
+
+class Sums:
+    """A row's weights in 80 bits; where something is cut, the whole numbers that they round to, and how far each can be
+    off since the weight is (0 for all but those next to a half)."""
+
+    def __init__(self, z, t, cut):
+        z = np.asarray(z, np.longdouble)
+        self.w = np.exp((z - z.max()) / np.longdouble(t))
+        self.z, self.order = z, np.argsort(-z, kind="stable")
+        self.cut, self.value, self.off = cut, self.w, WEIGHT * self.w
+        if cut:
+            x = self.w * np.longdouble(ONE)
+            self.value = np.rint(x)
+            self.off = np.maximum(self.value - np.rint(x * (1 - WEIGHT)), np.rint(x * (1 + WEIGHT)) - self.value)
+
+    def spans(self, ids):
+        """For ids in order: the shares of u from and to which each is drawn, and how far those can be off.  A share is
+        R / (R + S), R the running sum and S what is behind it.  Whole numbers are the same ones wherever they are
+        added, so with R off by r and S by s the share is off by (r S + s R) / (R + S)^2.  Uncut rows' weights are taken
+        twice, for the sum T and again for the running sum, each time with an error of its own: with R off by r, and T,
+        by itself, by e T, R / T is off by (r + e R) / T."""
+        v, run, off = self.value[ids], np.cumsum(self.value[ids]), np.cumsum(self.off[ids])
+        share = run / run[-1]
+        if self.cut:
+            slack = (off * (1 - share) + (off[-1] - off) * share) / run[-1]
+        else:
+            slack = (off + WEIGHT * run) / run[-1]
+        return (run - v) / run[-1], share, slack * (1 + 1e-6) + ADDED
+
+
+def rules(o, z, t):
+    """Settings whose kept tokens no error of a sum can change, and those tokens."""
+    n = len(z)
+    w, order = o.w, o.order
+    run = np.cumsum(w[order])
+    few = min(20, n)
+    yield dict(top_k=few), order[:few]
+    many = min(3000, n // 2)
+    yield dict(top_k=many), order[:many]
+    for k, p in ((0, 0.9), (0, 0.5), (many, 0.8)):        # the border in the middle of a token
+        of = run[k - 1] if k else run[-1]
+        i = int(np.searchsorted(run, p * of))
+        yield dict(top_k=k, top_p=float((run[i] - w[order[i]] / 2) / of)), order[:i + 1]
+    values = np.unique(z)[::-1]
+    i = np.searchsorted(-values, -(values[0] + t * math.log(0.02)))
+    at = (values[i - 1] + values[min(i, len(values) - 1)]) / 2
+    yield dict(min_p=float(np.exp((at - values[0]) / np.longdouble(t)))), np.flatnonzero(z >= at)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["flat", "peaked"])
+@pytest.mark.parametrize("vocab,rows", [(151936, 3), (16000, 3), (5003, 3), (900, 3), (32000, 5)])
+@pytest.mark.parametrize("t", [1.0, 0.7])
+def test_draws_turn_where_exact_sums_do(vocab, rows, kind, dtype, t):
+    """Uniform numbers just inside both ends of tokens' shares, as near as the weights' stated error lets them be (some
+    1e-12, where sums of fp32 weights are 1e-8 off), and the log-probabilities."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(vocab)
+    z = logits(rng, rows, vocab, kind, dtype)
+    host = z.double().cpu().numpy()
+    tested = 0
+    for r in range(rows):
+        plain, cut = Sums(host[r], t, False), Sums(host[r], t, True)
+        for o, (s, kept) in [(plain, (dict(), np.arange(vocab)))] + [(cut, x) for x in rules(cut, host[r], t)]:
+            ids = np.sort(kept)
+            a, b, slack = o.spans(ids)
+            good = np.flatnonzero((b - a > 8 * slack) & (o.value[ids] > 0))
+            at = np.unique(np.r_[good[:2], good[-2:], rng.choice(good, min(40, len(good)), replace=False)])
+            before = np.where(at > 0, slack[np.maximum(at - 1, 0)], 0)
+            u = np.r_[(a[at] + before).astype(np.float64), (b[at] - slack[at]).astype(np.float64)]
+            ok = (u >= 0) & (u < 1)
+            want = np.r_[ids[at], ids[at]][ok]
+            got = rg.sample(z[r:r + 1].expand(len(want), vocab), torch.from_numpy(u[ok]).cuda(), temperature=t, **s)
+            token, lp, kp = (x.cpu().numpy() for x in got)
+            assert np.array_equal(token, want), (r, s, np.flatnonzero(token != want)[:5])
+            x = (o.z[want] - o.z.max()) / np.longdouble(t)
+            for y, total, off in ((lp, o.w.sum(), WEIGHT), (kp, o.value[ids].sum() / (ONE if o is cut else 1),
+                                                            float(o.off[ids].sum() / o.value[ids].sum()))):
+                ref = x - np.log(total)
+                assert np.all(np.abs(y - ref) <= off + np.abs(ref) * (2.0 ** -24 * (1 + 1e-6)) + 1e-13), (r, s)
+            tested += len(want)
+    assert tested > 100 * rows

@@ -476,6 +476,61 @@ def test_wide_trees_what_a_node_does_not_see(old):
             assert np.isnan(out3[i]).all() if hit[i] else np.array_equal(out3[i], out2[i], equal_nan=True), i
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_kv,rep,old,bound,pieces", [(24, 11, 45, 1000, 1), (24, 11, 3000, 1 << 14, 1), (3, 11, 3000, 3300, 2)])
+def test_32_columns_what_a_node_does_not_see(n_kv, rep, old, bound, pieces, hd, dtype):
+    """The 32-column kernel, as its plan says: NaN codes that some nodes see, pages outside the pool and the table in
+    the tree and in the context, tables that end early or lack the sequence, lengths past everything."""
+    import paper_2606_02218_amd as rg
+    n, far = 70, 2                                       # the tree in question, and a second sequence beside it
+    nodes, olds = [n, n], [old, 31]
+    b = Batch([c + n for c in olds], n_kv, hd, 16, capacity=old + n + 60, seed=old + hd)
+    wide, cut = cuts(b, n_kv * rep, nodes, far, bound, dtype)
+    assert wide and min(cut, 2) == pieces
+    trees = [parents(n, "tree", b.rng) for _ in nodes]
+    mask, _ = all_masks(trees, far, olds, b.lengths())
+    q = rounded(b.rng.normal(0, 1.5, (2 * n, n_kv * rep, hd)), dtype)
+    args = (dev(q, dtype), dev(b.tab), dev(b.lengths()), offsets(nodes), as_mask(mask))
+    run = lambda tab=args[1], lens=args[2], **k: host(rg.kv8_tree_attention(  # noqa: E731
+        b.cache, args[0], tab, lens, *args[3:], max_len=bound, **k))
+    clean = run()
+    if n_kv * rep < 40:
+        check(b, q, nodes, mask, torch.from_numpy(clean), dtype)
+    sees = tree.seen(mask[:n], old + n, n)
+    page, sub = b.places(0, -(-(old + n) // 16))
+    v, k = b.cache.v.view(torch.uint8), b.cache.k.view(torch.uint8)
+    h, here = 1, slice(rep, 2 * rep)                     # the kv head with bad codes, its query heads
+    t = old + 11
+    for d in (5, hd - 31):
+        v[int(page[t // 16]), h, int(sub[t // 16]), (t % 16 // 4) * 4 * hd + d * 4 + t % 4] = 0x7F
+    want = clean.copy()
+    for d in (5, hd - 31):
+        want[:n, here, d] = np.where(sees[:, t, None], np.nan, want[:n, here, d])
+    assert sees[:, t].any() and not sees[:, t].all()
+    assert np.array_equal(run(), want, equal_nan=True)
+    t = old + 67
+    k[int(page[t // 16]), h, int(sub[t // 16]), (9 // 16) * 256 + (t % 16) * 16 + 9] = 0xFF
+    want[:n, here] = np.where(sees[:, t, None, None], np.nan, want[:n, here])
+    assert np.array_equal(run(), want, equal_nan=True)
+    for lost, t in ((b.pages + 5, old + 20), (-3, old + 66), (2 ** 31 - 1, old - 40), (b.pages, 3)):
+        tab = b.tab.copy()
+        tab[0, t // 16] = lost
+        hit = sees[:, t // 16 * 16:t // 16 * 16 + 16].any(1)
+        bad = want.copy()
+        bad[:n][hit] = np.nan
+        assert np.array_equal(run(dev(tab)), bad, equal_nan=True), t
+    short = (old + 40) // 16                             # pages of a table that ends inside the tree
+    bad = want.copy()
+    bad[:n][sees[:, short * 16:].any(1)] = np.nan
+    bad[n:][tree.seen(mask[n:], 31 + n, n)[:, short * 16:].any(1)] = np.nan
+    assert np.array_equal(run(dev(np.ascontiguousarray(b.tab[:, :short]))), bad, equal_nan=True)
+    bad = want.copy()
+    bad[:n] = np.nan
+    assert np.array_equal(run(tab_row=dev(np.array([9, 1], np.int32))), bad, equal_nan=True)
+    assert np.array_equal(run(lens=dev(np.array([2 ** 31 - 1, 31 + n], np.int32))), bad, equal_nan=True)
+
+
 def test_wide_trees_in_the_queries_place():
     import paper_2606_02218_amd as rg
     for old, bound in ((50, LONG), (4000, LONG), (50, 8192)):
