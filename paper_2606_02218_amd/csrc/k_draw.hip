@@ -424,10 +424,12 @@ __device__ __forceinline__ double mass_limit(const RowOpts& o, double all) { ret
 // Whether the pick deals with every row alone.  Top-p by several workgroups a row takes
 // three launches, by one a histogram of its own: 2 to 150 rows of 5000 28-32 and 22-23 us, of
 // 16000 28-36 and 28-31, of 32000 29-46 and 40-46.  Where rows are enough for all units and
-// top-k's own may leave it few of them, it pays further (505 rows of 32000, a tenth of them
-// by top-p alone: 51, 40).
+// have k of their own, which may leave the launches few of them, it pays further: 505 rows of
+// 20000 bf16 tokens, all by top-p alone, half, a tenth of them, 57, 50, 42 us and 42, 40, 35;
+// of 32000 65, 57, 48 and 57, 56, 50 (near-uniform logits 78, 69, 54 and 72, 71, 70); but of
+// 50257 138, 117, 93 and 158, 145, 133, of 65536 100, 82, 70 and 111, 106, 86.
 __host__ __device__ __forceinline__ bool alone(const DrawArgs& A) {
-  return A.vocab <= (A.rows >= ROWS_FULL && A.top_k_rows ? 1 << 16 : 1 << 14);
+  return A.vocab <= (A.rows >= ROWS_FULL && A.top_k_rows ? 1 << 15 : 1 << 14);
 }
 // Which rows several workgroups look at, by a histogram.  top-k's tokens are few.  min-p's
 // border is known, but summing up what it leaves takes one workgroup a row long where that

@@ -136,6 +136,19 @@ def test_rows_that_go_different_ways(rows, vocab):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,vocab", [(255, 32768), (256, 32768), (256, 32769), (256, 50257)])
+def test_rows_with_k_of_their_own_in_larger_vocabularies(rows, vocab, dtype):
+    """A workgroup a row up to some size, several past it: half of the rows by top-p or min-p alone."""
+    import paper_2606_02218_amd as rg
+    rng = np.random.default_rng(rows + vocab)
+    z = logits(rng, rows, vocab, "peaked", dtype)
+    u = torch.from_numpy(rng.random(rows)).cuda()
+    k = torch.from_numpy(np.where(rng.random(rows) < 0.5, 0, rng.integers(1, 60, rows))).int().cuda()
+    for s in (dict(top_k=k, top_p=0.9), dict(top_k=k, min_p=0.05), dict(top_k=k * 0, top_p=0.5, min_p=0.001)):
+        check(z, u, rg.sample(z, u, **s), **s)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_settings_by_row_strides_and_repeats(dtype):
     import paper_2606_02218_amd as rg
     rng = np.random.default_rng(4)
