@@ -105,6 +105,26 @@ constexpr int WIDE_WAVES = 4;
 constexpr int tree_pieces(int size) { return size == 2 ? 1 : 3; }   // bf16 pieces of a query and of a probability
 constexpr int tree_waves(int size, int hd) { return size == 2 || hd == 64 ? 4 : 3; }   // of a SIMD, by the registers
 
+// 32 bits of a node's mask from bit b on; bits before 0, the context's, are set.
+__device__ __forceinline__ uint32_t mask_window(const uint64_t* m, int words, int b) {
+  if (b < 0) return b <= -32 ? ~0u : (uint32_t)(m[0] << -b) | ((1u << -b) - 1u);
+  const int w = b >> 6, o = b & 63;
+  uint64_t x = w < words ? m[w] >> o : 0;
+  if (o > 32 && w + 1 < words) x |= m[w + 1] << (64 - o);
+  return (uint32_t)x;
+}
+
+// Tokens of a sequence that some node of its tree may see: the nodes, n of them, are its
+// last ones, those past the mask have no bit, and there is no walk over what the table
+// has not.
+__device__ __forceinline__ int tree_tokens(const Kv8Pool& c, const Kv8Rows& b, int len, int n, int words) {
+  const int64_t ctx0 = (int64_t)len - n, ctx = ctx0 > 0 ? ctx0 : 0, far = ctx0 + 64 * words;
+  int64_t t = far > ctx ? far : ctx;
+  if (len < t) t = len;
+  const int64_t most = (int64_t)kv8_most(c, b) + 64 * words;
+  return (int)(t < most ? t : most);
+}
+
 // The sequence whose column groups hold number x: sequence s has its groups of
 // 2^shift columns at (first row * rep >> shift) + s and on.  64 candidates a step.
 __device__ __forceinline__ int find_group(const Kv8Rows& b, int x, int rep, int shift, int& key) {
@@ -894,12 +914,12 @@ template <typename T, int HD>
 hipError_t run(const Kv8TreeAttn& t, hipStream_t st) {
   const Kv8Attn& a = t.a;
   const int rep = a.n_q / a.c.n_kv;
-  const int64_t eights = ((int64_t)a.b.rows * rep / (t.plan.wide ? 32 : 16) + a.b.n_seqs + 7) / 8;
+  const int64_t eights = ((int64_t)a.b.rows * rep / (t.wide ? 32 : 16) + a.b.n_seqs + 7) / 8;
   const int64_t items = eights * 8 * a.c.n_kv * a.plan.n_split;
   if (items > INT32_MAX - 64) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((items + 63) / 64 * 64));
   const unsigned e = (unsigned)eights, n = (unsigned)items;
-  if (t.plan.wide) return kv8_launch(k_kv8_tree_wide<T, HD>, grid, dim3(64 * WIDE_WAVES), st, a, e, n);
+  if (t.wide) return kv8_launch(k_kv8_tree_wide<T, HD>, grid, dim3(64 * WIDE_WAVES), st, a, e, n);
   if (a.plan.waves == 8) return kv8_launch(k_kv8_tree_attn<T, HD, 8>, grid, dim3(512), st, a, e, n);
   return kv8_launch(k_kv8_tree_attn<T, HD, 4>, grid, dim3(256), st, a, e, n);
 }
@@ -914,8 +934,8 @@ hipError_t merge(const Kv8Attn& a, hipStream_t st) {
 }  // namespace
 
 // 32 columns a workgroup where sequences have 64 and more on average and there are, with
-// their contexts cut into chunks of 640 tokens and more, workgroups enough: three a compute
-// unit (fp32 two), of which half at least.  64 trees of 64 nodes, 12 heads, at 4000 tokens
+// their contexts cut into chunks of 640 tokens and more, workgroups enough: as many as three a
+// compute unit (fp32 two), 384 of them at least.  64 trees of 64 nodes, 12 heads, at 4000 tokens
 // 154 us, by 16 columns 199; 3 of 40 to 60, 28 heads, at 20 to 25 thousand 101 and 171; but 8
 // of 20 to 30, 12 heads, at 1000 to 1500 17 and 12, 48 of 5 to 10 21 and 19.  Else 16
 // columns, whose contexts are cut only where that fills the chip, since the chunks' partial

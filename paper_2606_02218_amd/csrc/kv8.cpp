@@ -93,8 +93,7 @@ int rope_args(const char* who, const float* co, const float* si, int32_t n_pos, 
   return RG_OK;
 }
 
-// What the calls on drafted trees ask of their batch beyond cache_args: offsets, and
-// masks where they read them.
+// What the calls on drafted trees ask beyond cache_args: offsets, and a mask's width.
 int tree_args(const char* who, const rg_kv8_batch* b, int32_t words) {
   if (words < 1 || words > RG_KV8_TREE_WORDS) return bad(who, "words must be in [1, 64]");
   if (b->rows > 0 && !b->seq_off) return bad(who, "NULL seq_off");
@@ -262,11 +261,12 @@ int rg_kv8_tree_attention(const rg_kv8_cache* cache, const rg_kv8_batch* batch, 
   a.words = words;
   a.n_q = n_q;
   a.scale = scale;
-  t.plan = kv8_tree_plan(dtype, a.b.rows, a.b.n_seqs, n_q, a.c.n_kv, max_len);
-  a.plan.waves = t.plan.waves;
-  a.plan.n_split = t.plan.n_split;
-  a.plan.chunk = t.plan.chunk;
-  const int64_t need = 4 * kv8_tree_part_floats(a.b.rows, t.plan, n_q, a.c.hd);
+  const Kv8TreePlan plan = kv8_tree_plan(dtype, a.b.rows, a.b.n_seqs, n_q, a.c.n_kv, max_len);
+  t.wide = plan.wide;
+  a.plan.waves = plan.waves;
+  a.plan.n_split = plan.n_split;
+  a.plan.chunk = plan.chunk;
+  const int64_t need = 4 * kv8_tree_part_floats(a.b.rows, plan, n_q, a.c.hd);
   if (need > 0 && (!scratch || scratch_bytes < need))
     return bad(who, "scratch is smaller than rg_kv8_tree_attention_scratch()");
   a.part_o = (float*)scratch;

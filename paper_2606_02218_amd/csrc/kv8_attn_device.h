@@ -56,23 +56,3 @@ __device__ __forceinline__ uint32_t clear_nan(uint32_t w) {
   const uint32_t hit = (((w & KV8_NAN4) + 0x01010101u) & 0x80808080u) >> 7;
   return w & ~(hit * 0xFFu);
 }
-
-// 32 bits of a node's mask from bit b on; bits before 0, the context's, are set.
-__device__ __forceinline__ uint32_t mask_window(const uint64_t* m, int words, int b) {
-  if (b < 0) return b <= -32 ? ~0u : (uint32_t)(m[0] << -b) | ((1u << -b) - 1u);
-  const int w = b >> 6, o = b & 63;
-  uint64_t x = w < words ? m[w] >> o : 0;
-  if (o > 32 && w + 1 < words) x |= m[w + 1] << (64 - o);
-  return (uint32_t)x;
-}
-
-// Tokens of a sequence that some node of its tree may see: the nodes, n of them, are its
-// last ones, those past the mask have no bit, and there is no walk over what the table
-// has not.
-__device__ __forceinline__ int tree_tokens(const Kv8Pool& c, const Kv8Rows& b, int len, int n, int words) {
-  const int64_t ctx0 = (int64_t)len - n, ctx = ctx0 > 0 ? ctx0 : 0, far = ctx0 + 64 * words;
-  int64_t t = far > ctx ? far : ctx;
-  if (len < t) t = len;
-  const int64_t most = (int64_t)kv8_most(c, b) + 64 * words;
-  return (int)(t < most ? t : most);
-}

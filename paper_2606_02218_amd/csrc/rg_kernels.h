@@ -441,8 +441,8 @@ struct Kv8Attn {
   Kv8Plan plan;
   float* part_o;    // n_split > 1: unnormalised outputs [rows][n_split][n_q][hd]
   float* part_ml;   // and their (max, sum) [rows][n_split][n_q][2]
-  const uint64_t* mask;   // launch_kv8_tree_tiles: what each row sees of its tree
-  int words;
+  const uint64_t* mask;   // launch_kv8_tree_attention: what each row sees of its tree,
+  int words;              // 64-bit words a row
 };
 inline int64_t kv8_part_floats(int64_t rows, const Kv8Plan& p, int n_q, int hd) {
   return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
@@ -461,8 +461,8 @@ struct Kv8TreePlan {
 };
 Kv8TreePlan kv8_tree_plan(int dtype, int rows, int n_seqs, int n_q, int n_kv, int max_len);
 struct Kv8TreeAttn {
-  Kv8Attn a;        // its plan's chunks as the tree's
-  Kv8TreePlan plan;
+  Kv8Attn a;        // its plan has the tree plan's waves and chunks
+  bool wide;
 };
 inline int64_t kv8_tree_part_floats(int64_t rows, const Kv8TreePlan& p, int n_q, int hd) {
   return p.n_split > 1 ? rows * p.n_split * n_q * (hd + 2) : 0;
