@@ -94,10 +94,10 @@ def kv8_tree(parent, seq_len, seq_off, words: int = 1, stream=None):
       seq_off  int32 [sequences + 1]: each sequence's nodes
     ``mask`` is int64 [rows, words], bit i % 64 of word i / 64 for node i: its
     own and its ancestors'.  A word holds 64 nodes and those past the last word have no
-    bit, so that nobody sees them, themselves among it: a tree of more than 64 nodes
-    needs ``words`` of its nodes / 64, rounded up.  ``pos`` is int32 [rows], the context's length plus the
-    node's depth.  Rows past the last sequence's are not written.  See rg_kv8_tree
-    in rollout.h for padding and for parents that are none."""
+    bit, so that no node sees them, not even they themselves: a tree of more than 64
+    nodes needs ``words`` of nodes / 64, rounded up.  ``pos`` is int32 [rows], the
+    context's length plus the node's depth.  Rows past the last sequence's are not
+    written.  See rg_kv8_tree in rollout.h for padding and for parents that are none."""
     lib = _ready or _library()
     if stream is None:
         try:
